@@ -207,6 +207,84 @@ int cmsd_lmhead_confidence(const void* hidden, const void* weight, int R, int d,
                            void* stream);
 
 /*
+ * The head's loss, for training a drafter: softmax cross entropy of the logits
+ * z = h W^T of R hidden states over the whole vocabulary, without keeping z.
+ *   lse_r  = log sum_v exp(z_rv)
+ *   loss_r = lse_r - z_r,label(r)
+ *   hidden: bf16 [R][d], weight: bf16 [V][d], device, row-major, 16-byte
+ *     aligned; d a multiple of 8, 8 <= d <= 2^20; 2 <= V; R*V < 2^46; R == 0 is
+ *     a valid empty call (its workspace is that of R = 1).  Entries of kept rows
+ *     and of the weight must be finite.
+ *   labels: int32 [R] device.  A row whose label is ignore_index is ignored
+ *     (prompt or padding): its hidden state is not used, whatever it holds, it
+ *     costs no products, and its loss and lse are 0.  ignore_index may be any
+ *     number, an entry of the vocabulary too.  Another label outside [0, V) is
+ *     ignored as well and sets bit 0 of the workspace's error word.
+ *   loss, lse: float [R] device; loss may be NULL.  lse is what
+ *     cmsd_lmhead_loss_backward takes.
+ *   ws: cmsd_lmhead_loss_workspace_bytes(R, d, V) bytes, 16-byte aligned, on the
+ *     current device.  It needs no initialisation but for the error word, which
+ *     cmsd_workspace_init zeroes and cmsd_workspace_errors reads (bit 0 as
+ *     above; bit 2: a wait inside a kernel gave up, the results are void).
+ * Products are of exact bf16 values, accumulated in fp32 in an order that does
+ * not depend on other rows' contents; equal calls give equal results.
+ */
+size_t cmsd_lmhead_loss_workspace_bytes(int R, int d, int V);
+int cmsd_lmhead_loss(const void* hidden, const void* weight, const int32_t* labels, int R, int d, int V,
+                     int ignore_index, float* loss, float* lse, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * The gradients of cmsd_lmhead_loss, given dL/dloss_r:
+ *   P_rv     = (exp(z_rv - lse_r) - [v = label(r)]) grad_loss_r   (0 in ignored rows)
+ *   d_hidden = P W      bf16 [R][d], 0 in ignored rows
+ *   d_weight = P^T h    bf16 [V][d]
+ * Either output may be NULL, and its products are then left out (both NULL is
+ * CMSD_EINVAL).  Sizes, inputs, labels and the error word as for
+ * cmsd_lmhead_loss; lse: float [R], that call's output; grad_loss: float [R]
+ * device (the mean over n kept rows has 1 / n; entries of ignored rows are not
+ * used).  P is formed again from h and W in pieces of the vocabulary of at most
+ * 128 MB (and at least 256 entries), rounded to bf16 for the two products, which
+ * are accumulated in fp32 and rounded to bf16 once.  Both outputs are written
+ * whole, not added to.
+ */
+size_t cmsd_lmhead_loss_backward_workspace_bytes(int R, int d, int V);
+int cmsd_lmhead_loss_backward(const void* hidden, const void* weight, const int32_t* labels, const float* lse,
+                              const float* grad_loss, int R, int d, int V, int ignore_index, void* d_hidden,
+                              void* d_weight, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * Rows of numbers as symmetric 8-bit integers with a scale for each row: the
+ * channels (vocabulary entries) of a head's weight, or hidden states (tokens).
+ *   a_r = max_j |x_rj|, scale_r = a_r / 127, q_rj = 127 x_rj / a_r rounded to the
+ *   nearest whole number, ties to the even one (exactly so for either dtype).
+ * A row of zeros gives q 0 and scale 0; a row with an infinity or a NaN gives q 0
+ * and that infinity or a NaN as its scale, so that products with it show it.
+ *   x: dtype [R][d] device, row-major, 16-byte aligned; d a multiple of 16,
+ *   16 <= d <= 65536; R*d < 2^46; q: int8 [R][d], 16-byte aligned; scale: float
+ *   [R].  R == 0 is a valid empty call.
+ */
+int cmsd_quantize_rows(const void* x, int dtype, int R, int d, int8_t* q, float* scale, void* stream);
+
+/*
+ * The logits of a head in 8-bit integers:
+ *   logits_rv = (sum_j hidden_q_rj weight_q_vj) hidden_scale_r weight_scale_v
+ * The sum is exact; it is rounded to fp32, multiplied in fp32 in this order, and
+ * rounded to dtype (CMSD_F32 or CMSD_BF16) once.
+ *   hidden_q: int8 [R][d], weight_q: int8 [V][d], device, row-major, 16-byte
+ *     aligned, any values of the type; d a multiple of 16, 16 <= d <= 65536;
+ *     2 <= V; R*V < 2^46; R == 0 is a valid empty call (its workspace is that of
+ *     R = 1).  hidden_scale: float [R], weight_scale: float [V], device.
+ *   logits: dtype [R][V] device, 16-byte aligned: what cmsd_confidence and its
+ *     companions read with R = B*K.
+ *   ws: cmsd_lmhead_i8_workspace_bytes(R, d, V) bytes, 16-byte aligned, on the
+ *     current device; error word as for cmsd_lmhead_loss (bit 2 alone).
+ */
+size_t cmsd_lmhead_i8_workspace_bytes(int R, int d, int V);
+int cmsd_lmhead_i8(const int8_t* hidden_q, const float* hidden_scale, const int8_t* weight_q,
+                   const float* weight_scale, int R, int d, int V, void* logits, int dtype, void* ws,
+                   size_t ws_bytes, void* stream);
+
+/*
  * Verification (Sec. III.B(c)) given the confidence of each present position.
  * draft_tokens: int32 [B][K] device, the drafted token of each position.
  * conf: float [B][K] device, C_t (e.g. from cmsd_confidence).

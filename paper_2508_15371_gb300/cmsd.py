@@ -79,6 +79,14 @@ _SIGS = {
     "cmsd_lmhead_workspace_bytes": (_c_sz, [_c_int, _c_int, _c_int]),
     "cmsd_lmhead_confidence": (_c_int, [_vp, _vp, _c_int, _c_int, _c_int, _vp, _vp, _vp, _vp, _vp, _vp,
                                         _vp, _vp, _c_sz, _vp]),
+    "cmsd_lmhead_loss_workspace_bytes": (_c_sz, [_c_int, _c_int, _c_int]),
+    "cmsd_lmhead_loss": (_c_int, [_vp, _vp, _vp, _c_int, _c_int, _c_int, _c_int, _vp, _vp, _vp, _c_sz, _vp]),
+    "cmsd_lmhead_loss_backward_workspace_bytes": (_c_sz, [_c_int, _c_int, _c_int]),
+    "cmsd_lmhead_loss_backward": (_c_int, [_vp, _vp, _vp, _vp, _vp, _c_int, _c_int, _c_int, _c_int, _vp, _vp,
+                                           _vp, _c_sz, _vp]),
+    "cmsd_quantize_rows": (_c_int, [_vp, _c_int, _c_int, _c_int, _vp, _vp, _vp]),
+    "cmsd_lmhead_i8_workspace_bytes": (_c_sz, [_c_int, _c_int, _c_int]),
+    "cmsd_lmhead_i8": (_c_int, [_vp, _vp, _vp, _vp, _c_int, _c_int, _c_int, _vp, _c_int, _vp, _c_sz, _vp]),
     "cmsd_philox_u32": (_c_u32, [_c_u64, _c_u32, _c_u32, _c_u32, _c_u32, _c_int]),
     "cmsd_philox_fill": (_c_int, [_c_u64, _c_u32, _c_u32, _c_u32, _c_u32, _vp, _c_sz, _vp]),
     "cmsd_profile_start": (_c_int, [_c_int]),
@@ -283,6 +291,142 @@ def lmhead_confidence(hidden, weight, p=None, logits=False, out=None, ws=None):
                                       _ptr(o["margin"]), _ptr(o["argmax"]), _ptr(o["conf"]), _ptr(o["lse"]),
                                       _ptr(o.get("logits")), _ptr(ws), ws.numel(), _stream())
     _check(rc, "cmsd_lmhead_confidence")
+    return o
+
+
+def _need_current(**ts):
+    """Contiguous CUDA tensors on the current device (None where an argument is not given)."""
+    _need_cuda(*ts.values())
+    cur = _torch().cuda.current_device()
+    for name, t in ts.items():
+        if t is not None and t.get_device() != cur:
+            raise CmsdError(f"{name} must be on the current device")
+
+
+def _need_shape(name, t, shape, dtype):
+    if t is None or tuple(t.shape) != tuple(shape) or t.dtype != dtype:
+        got = "nothing" if t is None else f"{t.dtype} {tuple(t.shape)}"
+        raise CmsdError(f"{name} must be {dtype} {tuple(shape)}, got {got}")
+
+
+def _head_sizes(hidden, weight, dtype):
+    if hidden.dim() != 2 or weight.dim() != 2 or hidden.shape[1] != weight.shape[1]:
+        raise CmsdError("hidden [R, d] and weight [V, d] must share d")
+    if hidden.dtype != dtype or weight.dtype != dtype:
+        raise CmsdError(f"hidden and weight must be {dtype}")
+    return hidden.shape[0], hidden.shape[1], weight.shape[0]
+
+
+def _head_workspace(what, R, d, V):
+    torch = _torch()
+    n = int(getattr(lib(), what)(int(R), int(d), int(V)))
+    if n == 0:
+        raise CmsdError(f"{what}: sizes out of range")
+    ws = torch.empty(n, dtype=torch.uint8, device="cuda")
+    _check(lib().cmsd_workspace_init(_ptr(ws), 4, _stream()), "cmsd_workspace_init")   # the error word
+    return ws
+
+
+def lmhead_loss_workspace(R, d, V):
+    """A workspace for lmhead_loss(R, d, V) on the current device (workspace_errors reads its error word)."""
+    return _head_workspace("cmsd_lmhead_loss_workspace_bytes", R, d, V)
+
+
+def lmhead_loss_backward_workspace(R, d, V):
+    """A workspace for lmhead_loss_backward(R, d, V) on the current device."""
+    return _head_workspace("cmsd_lmhead_loss_backward_workspace_bytes", R, d, V)
+
+
+def lmhead_i8_workspace(R, d, V):
+    """A workspace for lmhead_i8(R, d, V) on the current device."""
+    return _head_workspace("cmsd_lmhead_i8_workspace_bytes", R, d, V)
+
+
+def lmhead_loss(hidden, weight, labels, ignore_index=-100, out=None, ws=None):
+    """Softmax cross entropy of the head's logits hidden @ weight.T, which are not kept.
+
+    hidden: bf16 [R, d], weight: bf16 [V, d], labels: int32 [R].  Returns dict
+    loss and lse ([R], float32; 0 in rows whose label is ignore_index)."""
+    torch = _torch()
+    R, d, V = _head_sizes(hidden, weight, torch.bfloat16)
+    _need_shape("labels", labels, (R,), torch.int32)
+    o = {n: _out(out, n, (R,), torch.float32, hidden.device) for n in ("loss", "lse")}
+    if o["loss"] is not None:
+        _need_shape("loss", o["loss"], (R,), torch.float32)
+    _need_shape("lse", o["lse"], (R,), torch.float32)
+    _need_current(hidden=hidden, weight=weight, labels=labels, ws=ws, **o)
+    ws = ws if ws is not None else lmhead_loss_workspace(R, d, V)
+    rc = lib().cmsd_lmhead_loss(_ptr(hidden), _ptr(weight), _ptr(labels), R, d, V, int(ignore_index),
+                                _ptr(o["loss"]), _ptr(o["lse"]), _ptr(ws), ws.numel(), _stream())
+    _check(rc, "cmsd_lmhead_loss")
+    return o
+
+
+def lmhead_loss_backward(hidden, weight, labels, lse, grad_loss, ignore_index=-100, hidden_grad=True,
+                         weight_grad=True, out=None, ws=None):
+    """The gradients of lmhead_loss: lse is its output, grad_loss (float32 [R]) is dL/dloss.
+
+    Returns dict d_hidden (bf16 [R, d], with hidden_grad) and d_weight (bf16
+    [V, d], with weight_grad), written whole."""
+    torch = _torch()
+    R, d, V = _head_sizes(hidden, weight, torch.bfloat16)
+    _need_shape("labels", labels, (R,), torch.int32)
+    _need_shape("lse", lse, (R,), torch.float32)
+    _need_shape("grad_loss", grad_loss, (R,), torch.float32)
+    o = {}
+    if hidden_grad:
+        o["d_hidden"] = _out(out, "d_hidden", (R, d), torch.bfloat16, hidden.device)
+        _need_shape("d_hidden", o["d_hidden"], (R, d), torch.bfloat16)
+    if weight_grad:
+        o["d_weight"] = _out(out, "d_weight", (V, d), torch.bfloat16, hidden.device)
+        _need_shape("d_weight", o["d_weight"], (V, d), torch.bfloat16)
+    _need_current(hidden=hidden, weight=weight, labels=labels, lse=lse, grad_loss=grad_loss, ws=ws, **o)
+    ws = ws if ws is not None else lmhead_loss_backward_workspace(R, d, V)
+    rc = lib().cmsd_lmhead_loss_backward(_ptr(hidden), _ptr(weight), _ptr(labels), _ptr(lse), _ptr(grad_loss),
+                                         R, d, V, int(ignore_index), _ptr(o.get("d_hidden")),
+                                         _ptr(o.get("d_weight")), _ptr(ws), ws.numel(), _stream())
+    _check(rc, "cmsd_lmhead_loss_backward")
+    return o
+
+
+def quantize_rows(x, out=None):
+    """Rows of x ([R, d], float32 or bfloat16) as symmetric 8-bit integers: dict q (int8 [R, d]) and
+    scale (float32 [R], the row's largest magnitude over 127)."""
+    torch = _torch()
+    if x.dim() != 2:
+        raise CmsdError("x must be [R, d]")
+    if x.dtype not in (torch.float32, torch.bfloat16):
+        raise CmsdError(f"x must be float32 or bfloat16, got {x.dtype}")
+    R, d = x.shape
+    o = {"q": _out(out, "q", (R, d), torch.int8, x.device),
+         "scale": _out(out, "scale", (R,), torch.float32, x.device)}
+    _need_shape("q", o["q"], (R, d), torch.int8)
+    _need_shape("scale", o["scale"], (R,), torch.float32)
+    _need_current(x=x, **o)
+    rc = lib().cmsd_quantize_rows(_ptr(x), _dtype_code(x), R, d, _ptr(o["q"]), _ptr(o["scale"]), _stream())
+    _check(rc, "cmsd_quantize_rows")
+    return o
+
+
+def lmhead_i8(hidden_q, hidden_scale, weight_q, weight_scale, dtype=None, out=None, ws=None):
+    """The logits of a head in 8-bit integers: hidden_q int8 [R, d] with a scale for each token, weight_q
+    int8 [V, d] with one for each vocabulary entry (quantize_rows makes both).  Returns dict logits
+    ([R, V], dtype float32 or bfloat16 (the default))."""
+    torch = _torch()
+    dtype = torch.bfloat16 if dtype is None else dtype
+    if dtype not in (torch.float32, torch.bfloat16):
+        raise CmsdError(f"logits are float32 or bfloat16, not {dtype}")
+    R, d, V = _head_sizes(hidden_q, weight_q, torch.int8)
+    _need_shape("hidden_scale", hidden_scale, (R,), torch.float32)
+    _need_shape("weight_scale", weight_scale, (V,), torch.float32)
+    o = {"logits": _out(out, "logits", (R, V), dtype, hidden_q.device)}
+    _need_shape("logits", o["logits"], (R, V), dtype)
+    _need_current(hidden_q=hidden_q, hidden_scale=hidden_scale, weight_q=weight_q, weight_scale=weight_scale,
+                  ws=ws, **o)
+    ws = ws if ws is not None else lmhead_i8_workspace(R, d, V)
+    rc = lib().cmsd_lmhead_i8(_ptr(hidden_q), _ptr(hidden_scale), _ptr(weight_q), _ptr(weight_scale), R, d, V,
+                              _ptr(o["logits"]), _dtype_code(o["logits"]), _ptr(ws), ws.numel(), _stream())
+    _check(rc, "cmsd_lmhead_i8")
     return o
 
 

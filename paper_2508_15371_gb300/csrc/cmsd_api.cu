@@ -608,6 +608,54 @@ int lm_layout(int R, int V, LmLayout* L) {
   L->total = o;
   return CMSD_OK;
 }
+// Workspaces of the head's loss: the error word at offset 0, then the packed
+// rows; the forward pass's partial statistics or the backward pass's piece.
+int check_head(int R, int d, int V, int step, int most) {
+  if (R < 0 || d < step || d % step != 0 || d > most || V < 2) return CMSD_EINVAL;
+  if ((double)R * (double)V >= 70368744177664.0) return CMSD_EINVAL;   // 2^46 logits
+  return CMSD_OK;
+}
+int check_loss(int R, int d, int V) { return check_head(R, d, V, 8, 1 << 20); }
+int check_i8(int R, int d, int V) { return check_head(R, d, V, 16, 1 << 16); }
+size_t loss_layout(HeadLossArgs& a, bool backward, char* w) {
+  size_t o = 0;
+  auto take = [&](size_t bytes) {
+    char* p = w ? w + o : nullptr;
+    o += up(bytes);
+    return p;
+  };
+  const int64_t R = a.R > 0 ? a.R : 1;
+  const int64_t Rp = (R + kHeadTile - 1) / kHeadTile * kHeadTile;
+  a.Rp = (int)Rp;
+  a.err = (unsigned*)take(sizeof(unsigned));
+  a.n = (int*)take(sizeof(int));
+  a.pos = (int*)take((size_t)R * 4);
+  a.lab = (int*)take((size_t)Rp * 4);
+  a.packed = (uint16_t*)take((size_t)Rp * a.d * 2);
+  if (!backward) {
+    a.zlab = (float*)take((size_t)Rp * 4);
+    a.part = (float2*)take((size_t)((a.V + kHeadPart - 1) / kHeadPart) * Rp * 8);
+    return o;
+  }
+  a.plse = (float*)take((size_t)Rp * 4);
+  a.pgrad = (float*)take((size_t)Rp * 4);
+  // a piece of at most 128 MB, of the fewest equal pieces of whole tiles
+  const int64_t vt = ((int64_t)a.V + kHeadTile - 1) / kHeadTile;
+  int64_t most = (64ll << 20) / Rp / kHeadTile;
+  if (most < 1) most = 1;
+  const int64_t pieces = (vt + most - 1) / most;
+  a.Vc = (int)((vt + pieces - 1) / pieces * kHeadTile);
+  a.split = head_split(a.Rp, a.d, a.Vc);
+  a.dz = (uint16_t*)take((size_t)Rp * a.Vc * 2);
+  a.dh = (float*)take((size_t)a.split * Rp * a.d * 4);
+  return o;
+}
+size_t i8_layout(HeadI8Args& a, char* w) {
+  const size_t h = up((size_t)(a.R > 0 ? a.R : 1) * a.d * 2);
+  a.err = (unsigned*)w;
+  a.h16 = (uint16_t*)(w ? w + kAlign : nullptr);
+  return kAlign + h;
+}
 int check_lmhead(int R, int d, int V) {
   if (R < 0 || d < 64 || d % 64 != 0 || d > (1 << 20) || V < 2) return CMSD_EINVAL;
   if ((double)R * (double)V >= 70368744177664.0) return CMSD_EINVAL;   // 2^46 logits
@@ -689,6 +737,111 @@ int cmsd_lmhead_confidence(const void* hidden, const void* weight, int R, int d,
   h.part = (Partial*)(w + L.part);
   h.err = a.ws.err;
   cudaError_t e = launch_lmhead(h, a, (cudaStream_t)stream);
+  return e == cudaSuccess ? CMSD_OK : cuda_fail(e);
+}
+
+size_t cmsd_lmhead_loss_workspace_bytes(int R, int d, int V) {
+  if (check_loss(R, d, V)) return 0;
+  HeadLossArgs a = {};
+  a.R = R; a.d = d; a.V = V;
+  return loss_layout(a, false, nullptr);
+}
+
+int cmsd_lmhead_loss(const void* hidden, const void* weight, const int32_t* labels, int R, int d, int V,
+                     int ignore_index, float* loss, float* lse, void* ws, size_t ws_bytes, void* stream) {
+  const int rc = check_loss(R, d, V);
+  if (rc) return rc;
+  if (R == 0) return CMSD_OK;
+  if (!hidden || !weight || !labels || !lse) return CMSD_EINVAL;
+  if (!aligned16(hidden) || !aligned16(weight)) return CMSD_EALIGN;
+  HeadLossArgs a = {};
+  a.R = R; a.d = d; a.V = V; a.ignore = ignore_index;
+  if (!ws || ws_bytes < loss_layout(a, false, nullptr)) return CMSD_ENOWS;
+  if (!aligned16(ws)) return CMSD_EALIGN;
+  loss_layout(a, false, (char*)ws);
+  a.hidden = (const uint16_t*)hidden;
+  a.weight = (const uint16_t*)weight;
+  a.labels = labels;
+  a.loss = loss;
+  a.lse = lse;
+  const cudaError_t e = launch_head_loss(a, (cudaStream_t)stream);
+  return e == cudaSuccess ? CMSD_OK : cuda_fail(e);
+}
+
+size_t cmsd_lmhead_loss_backward_workspace_bytes(int R, int d, int V) {
+  if (check_loss(R, d, V)) return 0;
+  HeadLossArgs a = {};
+  a.R = R; a.d = d; a.V = V;
+  return loss_layout(a, true, nullptr);
+}
+
+int cmsd_lmhead_loss_backward(const void* hidden, const void* weight, const int32_t* labels, const float* lse,
+                              const float* grad_loss, int R, int d, int V, int ignore_index, void* d_hidden,
+                              void* d_weight, void* ws, size_t ws_bytes, void* stream) {
+  const int rc = check_loss(R, d, V);
+  if (rc) return rc;
+  if (!d_hidden && !d_weight) return CMSD_EINVAL;
+  if (d_weight && !aligned16(d_weight)) return CMSD_EALIGN;
+  if (R == 0) {                                  // no rows: the weight's gradient is zero
+    if (!d_weight) return CMSD_OK;
+    const cudaError_t e = cudaMemsetAsync(d_weight, 0, (size_t)V * d * 2, (cudaStream_t)stream);
+    return e == cudaSuccess ? CMSD_OK : cuda_fail(e);
+  }
+  if (!hidden || !weight || !labels || !lse || !grad_loss) return CMSD_EINVAL;
+  if (!aligned16(hidden) || !aligned16(weight) || (d_hidden && !aligned16(d_hidden))) return CMSD_EALIGN;
+  HeadLossArgs a = {};
+  a.R = R; a.d = d; a.V = V; a.ignore = ignore_index;
+  if (!ws || ws_bytes < loss_layout(a, true, nullptr)) return CMSD_ENOWS;
+  if (!aligned16(ws)) return CMSD_EALIGN;
+  loss_layout(a, true, (char*)ws);
+  a.hidden = (const uint16_t*)hidden;
+  a.weight = (const uint16_t*)weight;
+  a.labels = labels;
+  a.lse_in = lse;
+  a.grad = grad_loss;
+  a.d_hidden = (uint16_t*)d_hidden;
+  a.d_weight = (uint16_t*)d_weight;
+  const cudaError_t e = launch_head_loss_backward(a, (cudaStream_t)stream);
+  return e == cudaSuccess ? CMSD_OK : cuda_fail(e);
+}
+
+int cmsd_quantize_rows(const void* x, int dtype, int R, int d, int8_t* q, float* scale, void* stream) {
+  if (dtype != CMSD_F32 && dtype != CMSD_BF16) return CMSD_EDTYPE;
+  if (R < 0 || d < 16 || d % 16 != 0 || d > (1 << 16)) return CMSD_EINVAL;
+  if (R == 0) return CMSD_OK;
+  if (!x || !q || !scale) return CMSD_EINVAL;
+  if (!aligned16(x) || !aligned16(q)) return CMSD_EALIGN;
+  const cudaError_t e = launch_quantize_rows(x, dtype, R, d, q, scale, (cudaStream_t)stream);
+  return e == cudaSuccess ? CMSD_OK : cuda_fail(e);
+}
+
+size_t cmsd_lmhead_i8_workspace_bytes(int R, int d, int V) {
+  if (check_i8(R, d, V)) return 0;
+  HeadI8Args a = {};
+  a.R = R; a.d = d; a.V = V;
+  return i8_layout(a, nullptr);
+}
+
+int cmsd_lmhead_i8(const int8_t* hidden_q, const float* hidden_scale, const int8_t* weight_q,
+                   const float* weight_scale, int R, int d, int V, void* logits, int dtype, void* ws,
+                   size_t ws_bytes, void* stream) {
+  if (dtype != CMSD_F32 && dtype != CMSD_BF16) return CMSD_EDTYPE;
+  const int rc = check_i8(R, d, V);
+  if (rc) return rc;
+  if (R == 0) return CMSD_OK;
+  if (!hidden_q || !hidden_scale || !weight_q || !weight_scale || !logits) return CMSD_EINVAL;
+  if (!aligned16(hidden_q) || !aligned16(weight_q) || !aligned16(logits)) return CMSD_EALIGN;
+  HeadI8Args a = {};
+  a.R = R; a.d = d; a.V = V; a.dtype = dtype;
+  if (!ws || ws_bytes < i8_layout(a, nullptr)) return CMSD_ENOWS;
+  if (!aligned16(ws)) return CMSD_EALIGN;
+  i8_layout(a, (char*)ws);
+  a.hidden = hidden_q;
+  a.weight = weight_q;
+  a.hidden_scale = hidden_scale;
+  a.weight_scale = weight_scale;
+  a.logits = logits;
+  const cudaError_t e = launch_head_i8(a, (cudaStream_t)stream);
   return e == cudaSuccess ? CMSD_OK : cuda_fail(e);
 }
 

@@ -1,0 +1,126 @@
+"""The head's loss, its gradients, the 8-bit rows and the 8-bit product without
+a GPU: argument errors are found on the host before anything is enqueued, and
+workspace sizes depend on the sizes of the call alone."""
+import ctypes
+import os
+
+import pytest
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+PKG = os.path.join(ROOT, "paper_2508_15371_gb300")
+A = 4096            # an address that nothing reads: every call here is refused
+
+
+@pytest.fixture(scope="module")
+def cmsd():
+    if not os.path.exists(os.path.join(PKG, "libcmsd.so")):
+        from paper_2508_15371_gb300 import build
+        build.build()
+    from paper_2508_15371_gb300 import cmsd as c
+    c.lib()
+    return c
+
+
+def _loss(c, R=4, d=64, V=100, hidden=A, weight=A, labels=A, loss=A, lse=A, ws=A, ws_bytes=None):
+    n = c.lib().cmsd_lmhead_loss_workspace_bytes(R, d, V) if ws_bytes is None else ws_bytes
+    return c.lib().cmsd_lmhead_loss(hidden, weight, labels, R, d, V, -100, loss, lse, ws, n, None)
+
+
+def _back(c, R=4, d=64, V=100, hidden=A, weight=A, labels=A, lse=A, grad=A, dh=A, dw=A, ws=A, ws_bytes=None):
+    n = c.lib().cmsd_lmhead_loss_backward_workspace_bytes(R, d, V) if ws_bytes is None else ws_bytes
+    return c.lib().cmsd_lmhead_loss_backward(hidden, weight, labels, lse, grad, R, d, V, -100, dh, dw, ws, n, None)
+
+
+def _i8(c, R=4, d=64, V=100, h=A, hs=A, w=A, wsc=A, out=A, dtype=1, ws=A, ws_bytes=None):
+    n = c.lib().cmsd_lmhead_i8_workspace_bytes(R, d, V) if ws_bytes is None else ws_bytes
+    return c.lib().cmsd_lmhead_i8(h, hs, w, wsc, R, d, V, out, dtype, ws, n, None)
+
+
+def _quant(c, R=4, d=64, x=A, q=A, scale=A, dtype=1):
+    return c.lib().cmsd_quantize_rows(x, dtype, R, d, q, scale, None)
+
+
+@pytest.mark.parametrize("kw", [dict(R=-1), dict(d=0), dict(d=4), dict(d=12), dict(d=(1 << 20) + 8), dict(V=1),
+                                dict(R=1 << 23, V=1 << 23)])
+def test_loss_sizes_refused(cmsd, kw):
+    assert _loss(cmsd, **kw) == cmsd.EINVAL
+    assert _back(cmsd, **kw) == cmsd.EINVAL
+    a = dict(R=4, d=64, V=100)
+    a.update(kw)
+    assert cmsd.lib().cmsd_lmhead_loss_workspace_bytes(a["R"], a["d"], a["V"]) == 0
+    assert cmsd.lib().cmsd_lmhead_loss_backward_workspace_bytes(a["R"], a["d"], a["V"]) == 0
+
+
+def test_loss_pointers_refused(cmsd):
+    for name in ("hidden", "weight", "labels", "lse"):
+        assert _loss(cmsd, **{name: None}) == cmsd.EINVAL, name
+    for name in ("hidden", "weight", "ws"):
+        assert _loss(cmsd, **{name: A + 8}) == cmsd.EALIGN, name
+    assert _loss(cmsd, ws=None) == cmsd.ENOWS
+    n = cmsd.lib().cmsd_lmhead_loss_workspace_bytes(4, 64, 100)
+    assert _loss(cmsd, ws_bytes=n - 1) == cmsd.ENOWS
+    assert _loss(cmsd, R=0, hidden=None, weight=None, labels=None, lse=None, ws=None) == cmsd.OK
+
+
+def test_backward_pointers_refused(cmsd):
+    for name in ("hidden", "weight", "labels", "lse", "grad"):
+        assert _back(cmsd, **{name: None}) == cmsd.EINVAL, name
+    for name in ("hidden", "weight", "dh", "dw", "ws"):
+        assert _back(cmsd, **{name: A + 8}) == cmsd.EALIGN, name
+    assert _back(cmsd, dh=None, dw=None) == cmsd.EINVAL
+    assert _back(cmsd, R=0, dh=None, dw=None) == cmsd.EINVAL
+    assert _back(cmsd, R=0, dw=None) == cmsd.OK
+    assert _back(cmsd, R=0, dw=A + 8) == cmsd.EALIGN
+    assert _back(cmsd, ws=None) == cmsd.ENOWS
+    n = cmsd.lib().cmsd_lmhead_loss_backward_workspace_bytes(4, 64, 100)
+    assert _back(cmsd, ws_bytes=n - 1) == cmsd.ENOWS
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(R=-1), "EINVAL"), (dict(d=8), "EINVAL"), (dict(d=24), "EINVAL"), (dict(d=(1 << 16) + 16), "EINVAL"),
+    (dict(V=1), "EINVAL"), (dict(R=1 << 23, V=1 << 23), "EINVAL"), (dict(dtype=2), "EDTYPE"),
+    (dict(h=None), "EINVAL"), (dict(hs=None), "EINVAL"), (dict(w=None), "EINVAL"), (dict(wsc=None), "EINVAL"),
+    (dict(out=None), "EINVAL"), (dict(h=A + 8), "EALIGN"), (dict(w=A + 4), "EALIGN"), (dict(out=A + 2), "EALIGN"),
+    (dict(ws=None), "ENOWS"), (dict(ws_bytes=16), "ENOWS"), (dict(ws=A + 8), "EALIGN"),
+    (dict(R=0, h=None, hs=None, w=None, wsc=None, out=None, ws=None), "OK")])
+def test_i8_refused(cmsd, kw, code):
+    assert _i8(cmsd, **kw) == getattr(cmsd, code)
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(R=-1), "EINVAL"), (dict(d=8), "EINVAL"), (dict(d=40), "EINVAL"), (dict(d=(1 << 16) + 16), "EINVAL"),
+    (dict(dtype=-1), "EDTYPE"), (dict(x=None), "EINVAL"), (dict(q=None), "EINVAL"), (dict(scale=None), "EINVAL"),
+    (dict(x=A + 8), "EALIGN"), (dict(q=A + 4), "EALIGN"), (dict(R=0, x=None, q=None, scale=None), "OK")])
+def test_quantize_refused(cmsd, kw, code):
+    assert _quant(cmsd, **kw) == getattr(cmsd, code)
+
+
+def test_workspaces_do_not_hold_the_logits(cmsd):
+    """At most a sixteenth of the bf16 logits forward; backward a piece of 128 MB, the sums of d_hidden and
+    the packed rows, whatever the vocabulary."""
+    R, d = 4096, 2048
+    for V in (128256, 1 << 20):
+        logits = 2 * R * V
+        assert cmsd.lib().cmsd_lmhead_loss_workspace_bytes(R, d, V) <= logits // 16 + 4 * R * d
+        assert cmsd.lib().cmsd_lmhead_loss_backward_workspace_bytes(R, d, V) <= (128 << 20) + 40 * R * d
+
+
+def test_binding_refuses_before_the_library(cmsd):
+    torch = pytest.importorskip("torch")
+    h, w = torch.zeros(4, 64, dtype=torch.bfloat16), torch.zeros(100, 64, dtype=torch.bfloat16)
+    y = torch.zeros(4, dtype=torch.int32)
+    f = torch.zeros(4)
+    bad = [lambda: cmsd.lmhead_loss(h.float(), w, y), lambda: cmsd.lmhead_loss(h, w[:, :32], y),
+           lambda: cmsd.lmhead_loss(h, w, y.long()), lambda: cmsd.lmhead_loss(h, w, y[:3]),
+           lambda: cmsd.lmhead_loss(h, w, y, out={"lse": f[:2], "loss": f}),
+           lambda: cmsd.lmhead_loss(h, w, y, out={"lse": None, "loss": f}),
+           lambda: cmsd.lmhead_loss_backward(h, w, y, f.double(), f),
+           lambda: cmsd.lmhead_loss_backward(h, w, y, f, f[:1]),
+           lambda: cmsd.lmhead_loss_backward(h, w, y, f, f, out={"d_weight": w.float()}),
+           lambda: cmsd.quantize_rows(h[0]), lambda: cmsd.quantize_rows(h.half()),
+           lambda: cmsd.lmhead_i8(h, f, w, f), lambda: cmsd.lmhead_i8(h.char(), f, w.char(), f),
+           lambda: cmsd.lmhead_i8(h.char(), f, w.char(), torch.zeros(100), dtype=torch.float16),
+           lambda: cmsd.lmhead_loss(h, w, y, out={"lse": f, "loss": f})]      # CPU tensors: there is no CPU path
+    for call in bad:
+        with pytest.raises(cmsd.CmsdError):
+            call()
