@@ -12,6 +12,7 @@
 #include <vector>
 
 #include "cmsd.h"
+#include "cmsd_head.h"
 #include "cmsd_internal.h"
 #include "cmsd_philox.cuh"
 

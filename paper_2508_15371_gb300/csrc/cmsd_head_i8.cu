@@ -3,7 +3,7 @@
 #include <cuda_bf16.h>
 
 #include "cmsd_device.cuh"
-#include "cmsd_internal.h"
+#include "cmsd_head.h"
 
 namespace cmsd {
 namespace {
