@@ -8,13 +8,12 @@
 // P (bf16), then P W, summed over the pieces in fp32, and P^T h.
 #include <cuda_bf16.h>
 
-#include "cmsd_device.cuh"
 #include "cmsd_head.h"
+#include "cmsd_tc.cuh"
 
 namespace cmsd {
 namespace {
 
-__device__ __forceinline__ float bf(uint16_t x) { return __uint_as_float((uint32_t)x << 16); }
 __device__ __forceinline__ uint16_t to_bf(float x) { return __bfloat16_as_ushort(__float2bfloat16_rn(x)); }
 __device__ __forceinline__ bool kept(const HeadLossArgs& a, int label) {
   return label != a.ignore && label >= 0 && label < a.V;
@@ -74,7 +73,7 @@ __global__ void __launch_bounds__(kPackThreads) head_pack_kernel(const HeadLossA
   }
   if (r1 == a.R) {
     if (tid == 0) *a.n = base;
-    const int end = min(a.Rp, (base + kHeadTile - 1) / kHeadTile * kHeadTile);
+    const int end = min(a.Rp, max(1, (base + kHeadTile - 1) / kHeadTile) * kHeadTile);
     const size_t from = (size_t)base * a.d / 8, to = (size_t)end * a.d / 8;
     for (size_t j = from + tid; j < to; j += kPackThreads) reinterpret_cast<uint4*>(a.packed)[j] = make_uint4(0, 0, 0, 0);
     for (int p = base + tid; p < end; p += kPackThreads) {
@@ -87,98 +86,362 @@ __global__ void __launch_bounds__(kPackThreads) head_pack_kernel(const HeadLossA
   }
 }
 
-// ---- the products ---------------------------------------------------------------------
-enum Op { kOpStats, kOpDz, kOpDh, kOpDw };
-constexpr int kTM = 64, kTN = 128, kTK = 16;
+// ---- the products -------------------------------------------------------------------
+//
+// Three products of one shape: 256 x 256 outputs of a pair of CTAs
+// (tcgen05.mma, cta_group::2: each CTA holds 128 rows of A, 128 of B's 256
+// columns' rows, and 128 rows of the accumulator), summed over K in steps of
+// 64.  A pair reads (256 + 256) * 2 bytes of its operands per K from L2 for
+// 256 * 256 products; one CTA alone with a 128 x 256 tile would read half as
+// much again per product, and L2 would bound the tensor cores.
+//   logits   A = packed rows, B = weight, K = d; both rows of 128 bytes along K
+//   d_hidden A = P, B = weight (its rows run along N), K = the piece's entries
+//   d_weight A = P (its rows run along M), B = packed rows (along N), K = rows
+// One pair runs through its share of the tiles, which are dealt out ahead:
+//   warp 0      lane 0 fills the ring of stages (TMA), each CTA its own halves,
+//               counted at the first CTA's barrier;
+//   warp 1      lane 0 of the first CTA issues the MMAs of both;
+//   warps 2..9  the epilogue: warp w reads TMEM lanes 32 (w mod 4) .., the two
+//               warps of a quarter 128 of the 256 columns each.
+// Barriers: full (TMA -> MMA), empty (MMA -> TMA, in both CTAs), tfull (MMA ->
+// epilogue, in both) and tempty (both epilogues -> MMA) for each of the two
+// accumulators.  Every wait is bounded.
+enum Op { kOpStats, kOpDz, kOpGrad };
+constexpr int kPairTile = kHeadTile;
+constexpr int kStages = 6;
+constexpr int kHalfBytes = 128 * 128;                 // 128 rows of 64 bf16
+constexpr int kStageBytes = 2 * kHalfBytes;           // A's and B's half
+constexpr int kEpiWarps = 8;
+constexpr int kPairThreads = 64 + 32 * kEpiWarps;
+constexpr size_t kPairSmem = 1024 + (size_t)kStages * kStageBytes + 8 * (2 * kStages + 4) + 16;
+constexpr int kTmemCols = 512;
+static_assert(kPairSmem <= 227 * 1024, "shared memory");
+
+// One tile of a pair: rows and columns of 256, K from k0 in blocks of 64.
+struct Tile {
+  int m, n;              // tile indices
+  int k0, kb;            // first block of 64 of K and their number
+  bool dw;               // kOpGrad: d_weight's product
+  int part;              // kOpGrad: part of d_hidden's K
+};
+struct Work {
+  int pairs, pair;
+  int mt, nt;            // kOpStats, kOpDz: tiles of rows and of the vocabulary; kOpGrad: of rows and of d
+  int total;             // tiles of this pair
+  int kd;                // blocks of K of the logits, or of a part of d_hidden
+  int kall;              // blocks of the whole piece (kOpGrad)
+  int kw;                // blocks of K of d_weight
+  int nh, mine_h;        // tiles of d_hidden, and this pair's
+  int lead, boost, first, stride;   // d_weight: see below
+};
+
+// Tiles of the logits go round the pairs with the rows first, so that pairs
+// running together share the weight's tile and the packed rows.  Tiles of
+// d_hidden, the longer ones, go round first; pairs with one of them less then
+// take `boost` tiles of d_weight more, and the rest goes round.
+template <int OP>
+__device__ __forceinline__ Work work_of(const HeadLossArgs& a, int n, int vlen, bool want_h, bool want_w) {
+  Work w;
+  w.pairs = gridDim.x / 2;
+  w.pair = blockIdx.x / 2;
+  const int rows = max(1, (n + kPairTile - 1) / kPairTile);
+  if (OP != kOpGrad) {
+    w.mt = OP == kOpStats ? (n + kPairTile - 1) / kPairTile : rows;
+    w.nt = (vlen + kPairTile - 1) / kPairTile;
+    w.kd = (a.d + 63) / 64;
+    const int all = w.mt * w.nt;
+    w.total = all > w.pair ? (all - w.pair + w.pairs - 1) / w.pairs : 0;
+    return w;
+  }
+  w.mt = rows;
+  w.nt = (a.d + kPairTile - 1) / kPairTile;
+  w.kall = (vlen + 63) / 64;
+  w.kd = (w.kall + a.split - 1) / a.split;
+  w.kw = max(1, (n + 63) / 64);
+  w.nh = want_h ? w.mt * w.nt * a.split : 0;
+  const int nw = want_w ? (vlen + kPairTile - 1) / kPairTile * w.nt : 0;
+  const int rem = w.nh % w.pairs;                  // pairs [0, rem) have one tile of d_hidden more
+  w.mine_h = w.nh / w.pairs + (w.pair < rem ? 1 : 0);
+  w.lead = rem > 0 && w.pair >= rem ? w.pairs - rem : 0;      // this pair catches up with so many others
+  const int behind = rem > 0 ? w.pairs - rem : 0;
+  int boost = behind > 0 ? (w.kd + w.kw / 2) / w.kw : 0;
+  if ((long long)boost * behind > nw) boost = behind > 0 ? (nw + behind - 1) / behind : 0;
+  const int early = min(nw, boost * behind);
+  w.boost = 0;
+  if (w.lead > 0) {
+    const int at = w.pair - rem;
+    w.boost = early > at ? (early - at + behind - 1) / behind : 0;
+  }
+  // the rest goes round, beginning behind the early ones
+  const int turn = behind > 0 ? (w.pair - rem + w.pairs) % w.pairs : w.pair;
+  w.first = early + turn;
+  w.stride = w.pairs;
+  const int late = nw > w.first ? (nw - w.first + w.pairs - 1) / w.pairs : 0;
+  w.total = w.mine_h + w.boost + late;
+  if (w.lead > 0) w.lead = w.pair - rem;           // index of the first early tile
+  return w;
+}
+template <int OP>
+__device__ __forceinline__ Tile tile_of(const HeadLossArgs& a, const Work& w, int i) {
+  Tile t;
+  t.dw = false;
+  t.part = 0;
+  t.k0 = 0;
+  if (OP != kOpGrad) {
+    const int j = w.pair + i * w.pairs;
+    t.n = j / w.mt;
+    t.m = j - t.n * w.mt;
+    t.kb = w.kd;
+    return t;
+  }
+  if (i < w.mine_h) {
+    const int j = w.pair + i * w.pairs;
+    const int per = w.mt * w.nt;
+    t.part = j / per;
+    const int r = j - t.part * per;
+    t.m = r / w.nt;
+    t.n = r - t.m * w.nt;
+    t.k0 = t.part * w.kd;
+    t.kb = max(0, min(w.kd, w.kall - t.k0));
+    return t;
+  }
+  i -= w.mine_h;
+  const int behind_early = i < w.boost ? w.lead + i * (w.pairs - w.nh % w.pairs) : w.first + (i - w.boost) * w.stride;
+  t.dw = true;
+  t.m = behind_early / w.nt;                       // tile of the vocabulary
+  t.n = behind_early - t.m * w.nt;
+  t.kb = w.kw;
+  return t;
+}
+
+struct Maps {
+  CUtensorMap rows_k;      // packed rows in boxes of 64 (d) x 128 rows
+  CUtensorMap rows_n;      // packed rows in boxes of 64 (d) x 64 rows
+  CUtensorMap weight_k;    // weight, 64 (d) x 128 entries
+  CUtensorMap weight_n;    // weight, 64 (d) x 64 entries
+  CUtensorMap dz_k;        // P, 64 (entries) x 128 rows
+  CUtensorMap dz_m;        // P, 64 (entries) x 64 rows
+};
+
+__device__ __forceinline__ uint32_t pack_bf(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
 
 // v0, vlen: the piece of the vocabulary; first: the first piece
 template <int OP>
-__global__ void __launch_bounds__(256) head_gemm_kernel(const HeadLossArgs a, int v0, int vlen, int first) {
-  __shared__ float sa[kTK][kTM + 4], sb[kTK][kTN + 4];
-  __shared__ float s_m[kTM][17], s_s[kTM][17];
-  const int n = *a.n;
-  const int M = OP == kOpDw ? vlen : n, N = OP == kOpStats || OP == kOpDz ? vlen : a.d;
-  const int K = OP == kOpStats || OP == kOpDz ? a.d : (OP == kOpDh ? vlen : n);
-  const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
-  const int n0 = blockIdx.x * kTN;
-  const int Mt = OP == kOpDz ? (M + kHeadTile - 1) / kHeadTile * kHeadTile : M;
-  for (int m0 = blockIdx.y * kTM; m0 < Mt; m0 += gridDim.y * kTM) {
-    float acc[4][8] = {};
-    for (int k0 = 0; k0 < K; k0 += kTK) {
-      __syncthreads();
-      for (int e = tid; e < kTK * kTM; e += 256) {
-        const int k = e % kTK, m = e / kTK;
-        float x = 0.f;
-        if (m0 + m < M && k0 + k < K) {
-          const size_t i = m0 + m, j = k0 + k;
-          x = bf(OP == kOpDh ? a.dz[i * a.Vc + j] : (OP == kOpDw ? a.dz[j * a.Vc + i] : a.packed[i * a.d + j]));
-        }
-        sa[k][m] = x;
-      }
-      for (int e = tid; e < kTK * kTN; e += 256) {
-        const int k = e % kTK, m = e / kTK;
-        float x = 0.f;
-        if (n0 + m < N && k0 + k < K) {
-          const size_t i = n0 + m, j = k0 + k;
-          x = bf(OP == kOpDh ? a.weight[(v0 + j) * a.d + i]
-                             : (OP == kOpDw ? a.packed[j * a.d + i] : a.weight[(v0 + i) * a.d + j]));
-        }
-        sb[k][m] = x;
-      }
-      __syncthreads();
-#pragma unroll
-      for (int k = 0; k < kTK; ++k)
-#pragma unroll
-        for (int u = 0; u < 4; ++u)
-#pragma unroll
-          for (int t = 0; t < 8; ++t) acc[u][t] = fmaf(sa[k][ty * 4 + u], sb[k][tx + 16 * t], acc[u][t]);
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
+    head_pair_kernel(const HeadLossArgs a, const int v0, const int vlen, const int first,
+                     const __grid_constant__ Maps maps) {
+  extern __shared__ __align__(1024) unsigned char pair_smem[];
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const uint32_t rank = cluster_rank();
+  const uint32_t raw = smem_addr(pair_smem);
+  const uint32_t base = (raw + 1023u) & ~1023u;
+  const uint32_t bars = base + kStages * kStageBytes;
+  const uint32_t full = bars, empty = bars + 8 * kStages, tfull = bars + 16 * kStages, tempty = tfull + 16;
+  uint32_t* s_taddr = reinterpret_cast<uint32_t*>(pair_smem + (bars - raw) + 8 * (2 * kStages + 4));
+  if (tid == 0) {
+    for (int k = 0; k < kStages; ++k) {
+      mbar_init(full + 8 * k, 1);
+      mbar_init(empty + 8 * k, 1);
     }
-#pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      const int m = m0 + ty * 4 + u;
-      if (OP == kOpStats) {
-        float mx = -pos_inf(), s = 0.f;
-#pragma unroll
-        for (int t = 0; t < 8; ++t)
-          if (n0 + tx + 16 * t < N) mx = fmaxf(mx, acc[u][t] * kLog2e);
-#pragma unroll
-        for (int t = 0; t < 8; ++t)
-          if (n0 + tx + 16 * t < N) {
-            s += ex2(acc[u][t] * kLog2e - mx);
-            if (m < M && a.lab[m] == n0 + tx + 16 * t) a.zlab[m] = acc[u][t];
+    for (int b = 0; b < 2; ++b) {
+      mbar_init(tfull + 8 * b, 1);
+      mbar_init(tempty + 8 * b, 2 * kEpiWarps);
+    }
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(s_taddr)),
+                 "r"(kTmemCols)
+                 : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+  }
+  tmem_fence_before();
+  cluster_sync_all();
+  // everything above overlaps the end of what precedes this grid on the stream
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  tmem_fence_after();
+  const uint32_t tbase = *s_taddr;
+  const int n = *a.n;
+  const Work w = work_of<OP>(a, n, vlen, a.d_hidden != nullptr, a.d_weight != nullptr);
+  bool ok = true;
+
+  if (warp == 0) {
+    // ---- this CTA's halves of the operands --------------------------------------
+    if (lane == 0) {
+      // what earlier kernels wrote with plain stores is read by the copy engine
+      asm volatile("fence.proxy.async.global;" ::: "memory");
+      const uint32_t full0 = map_to(full, 0);
+      int g = 0;
+      for (int i = 0; i < w.total; ++i) {
+        const Tile t = tile_of<OP>(a, w, i);
+        const int am = t.m * kPairTile + (int)rank * 128, bn = t.n * kPairTile + (int)rank * 128;
+        for (int kb = 0; kb < t.kb; ++kb, ++g) {
+          const int s = g % kStages;
+          if (g >= kStages && ok) ok = mbar_wait_cluster(empty + 8 * s, (uint32_t)((g / kStages - 1) & 1));
+          if (rank == 0) mbar_arrive_tx(full + 8 * s, 2 * kStageBytes);
+          const uint32_t sa = base + s * kStageBytes, sb = sa + kHalfBytes, bar = full0 + 8 * s;
+          const int k = (t.k0 + kb) * 64;
+          if (OP != kOpGrad) {
+            tma_box_pair(sa, &maps.rows_k, k, am, bar);
+            tma_box_pair(sb, &maps.weight_k, k, v0 + bn, bar);
+          } else if (!t.dw) {
+            tma_box_pair(sa, &maps.dz_k, k, am, bar);
+            tma_box_pair(sb, &maps.weight_n, bn, v0 + k, bar);
+            tma_box_pair(sb + kHalfBytes / 2, &maps.weight_n, bn + 64, v0 + k, bar);
+          } else {
+            tma_box_pair(sa, &maps.dz_m, am, k, bar);
+            tma_box_pair(sa + kHalfBytes / 2, &maps.dz_m, am + 64, k, bar);
+            tma_box_pair(sb, &maps.rows_n, bn, k, bar);
+            tma_box_pair(sb + kHalfBytes / 2, &maps.rows_n, bn + 64, k, bar);
           }
-        s_m[ty * 4 + u][tx] = mx;
-        s_s[ty * 4 + u][tx] = s;
-      } else if (m < Mt) {
+        }
+      }
+      // the last stages are consumed before this CTA's shared memory goes
+      for (int k = (g > kStages ? g - kStages : 0); k < g; ++k)
+        if (ok) ok = mbar_wait_cluster(empty + 8 * (k % kStages), (uint32_t)((k / kStages) & 1));
+    }
+  } else if (warp == 1) {
+    // ---- the MMAs of both CTAs -----------------------------------------------------
+    if (lane == 0 && rank == 0) {
+      const uint32_t empty1 = map_to(empty, 1), tfull1 = map_to(tfull, 1);
+      const uint32_t empty0 = map_to(empty, 0), tfull0 = map_to(tfull, 0);
+      int g = 0;
+      for (int i = 0; i < w.total; ++i) {
+        const Tile t = tile_of<OP>(a, w, i);
+        const int b = i & 1;
+        if (i >= 2 && ok) ok = mbar_wait_cluster(tempty + 8 * b, (uint32_t)((i / 2 - 1) & 1));
+        tmem_fence_after();
+        const uint32_t d = tbase + (uint32_t)(b * 256);
+        const uint32_t idesc = OP != kOpGrad ? mma_idesc(256, 256, true, false, false)
+                                             : (t.dw ? mma_idesc(256, 256, true, true, true)
+                                                     : mma_idesc(256, 256, true, false, true));
+        // K = 16 further: 32 bytes along the rows, or 16 rows
+        const uint64_t da = OP == kOpGrad && t.dw ? 2048 >> 4 : 32 >> 4, db = OP == kOpGrad ? 2048 >> 4 : 32 >> 4;
+        for (int kb = 0; kb < t.kb; ++kb, ++g) {
+          const int s = g % kStages;
+          if (ok) ok = mbar_wait_cluster(full + 8 * s, (uint32_t)((g / kStages) & 1));
+          tmem_fence_after();
+          const uint64_t ad = mma_desc(base + s * kStageBytes, kHalfBytes / 2);
+          const uint64_t bd = mma_desc(base + s * kStageBytes + kHalfBytes, kHalfBytes / 2);
 #pragma unroll
-        for (int t = 0; t < 8; ++t) {
-          const int j = n0 + tx + 16 * t;
-          if (OP == kOpDz) {
-            float p = 0.f;
-            if (m < M && j < N)
-              p = (ex2((acc[u][t] - a.plse[m]) * kLog2e) - (a.lab[m] == v0 + j ? 1.f : 0.f)) * a.pgrad[m];
-            if (j < a.Vc) a.dz[(size_t)m * a.Vc + j] = to_bf(p);
-          } else if (j < N) {
-            if (OP == kOpDh) {
-              float* p = a.dh + (size_t)m * a.d + j;
-              *p = first ? acc[u][t] : *p + acc[u][t];
-            } else {
-              a.d_weight[(size_t)(v0 + m) * a.d + j] = to_bf(acc[u][t]);
+          for (int ks = 0; ks < 4; ++ks) mma_pair(d, ad + ks * da, bd + ks * db, idesc, (kb | ks) != 0);
+          mma_commit_pair(empty0 + 8 * s);
+          mma_commit_pair(empty1 + 8 * s);
+        }
+        mma_commit_pair(tfull0 + 8 * b);
+        mma_commit_pair(tfull1 + 8 * b);
+      }
+    }
+    __syncwarp();
+  } else {
+    // ---- the epilogue -----------------------------------------------------------------
+    const uint32_t tempty0 = map_to(tempty, 0);
+    const int q = warp & 3, half = (warp - 2) >> 2;
+    for (int i = 0; i < w.total; ++i) {
+      const Tile t = tile_of<OP>(a, w, i);
+      const int b = i & 1;
+      if (ok) ok = mbar_wait_cluster(tfull + 8 * b, (uint32_t)((i / 2) & 1));
+      __syncwarp();
+      tmem_fence_after();
+      const int row = t.m * kPairTile + (int)rank * 128 + q * 32 + lane;
+      const int col = t.n * kPairTile + half * 128;
+      const uint32_t src = tbase + ((uint32_t)(q * 32) << 16) + (uint32_t)(b * 256 + half * 128);
+      const bool live = row < n;
+      int lab = -1;
+      float lse2 = 0.f, gr = 0.f, mx = -pos_inf(), sum = 0.f;
+      if (OP != kOpGrad && live) lab = a.lab[row] - v0;
+      if (OP == kOpDz && live) {
+        lse2 = a.plse[row] * kLog2e;
+        gr = a.pgrad[row];
+      }
+#pragma unroll 1
+      for (int c = 0; c < 128; c += 32) {
+        float z[32];
+        if (t.kb > 0) {
+          tmem_ld32(src + c, z);
+        } else {
+#pragma unroll
+          for (int k = 0; k < 32; ++k) z[k] = 0.f;
+        }
+        if (c == 96) {
+          tmem_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive_cluster(tempty0 + 8 * b);   // this warp's columns have been read
+        }
+        const int j0 = col + c;
+        if (OP == kOpStats) {
+          if (j0 + 32 > vlen) {
+#pragma unroll
+            for (int k = 0; k < 32; ++k)
+              if (j0 + k >= vlen) z[k] = -pos_inf();
+          }
+          if (j0 < vlen) {
+            float m4[4] = {z[0], z[1], z[2], z[3]};
+#pragma unroll
+            for (int k = 4; k < 32; ++k) m4[k & 3] = fmaxf(m4[k & 3], z[k]);
+            const float nm = fmaxf(mx, fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])) * kLog2e);
+            float s4[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int k = 0; k < 32; ++k) s4[k & 3] += ex2(fmaf(z[k], kLog2e, -nm));
+            sum = sum * ex2(mx - nm) + ((s4[0] + s4[1]) + (s4[2] + s4[3]));
+            mx = nm;
+            if (lab >= j0 && lab < j0 + 32) {
+              float zl = z[0];
+#pragma unroll
+              for (int k = 1; k < 32; ++k) zl = lab == j0 + k ? z[k] : zl;
+              a.zlab[row] = zl;
             }
           }
+        } else if (OP == kOpDz) {
+          float p[32];
+#pragma unroll
+          for (int k = 0; k < 32; ++k)
+            p[k] = live && j0 + k < vlen
+                       ? (ex2(fmaf(z[k], kLog2e, -lse2)) - (lab == j0 + k ? 1.f : 0.f)) * gr
+                       : 0.f;
+          uint4* dst = reinterpret_cast<uint4*>(a.dz + (size_t)row * a.Vc + j0);
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            dst[k] = make_uint4(pack_bf(p[8 * k], p[8 * k + 1]), pack_bf(p[8 * k + 2], p[8 * k + 3]),
+                                pack_bf(p[8 * k + 4], p[8 * k + 5]), pack_bf(p[8 * k + 6], p[8 * k + 7]));
+        } else if (t.dw) {
+          if (row < vlen) {
+            uint4* dst = reinterpret_cast<uint4*>(a.d_weight + (size_t)(v0 + row) * a.d + j0);
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+              if (j0 + 8 * k < a.d)
+                dst[k] = make_uint4(pack_bf(z[8 * k], z[8 * k + 1]), pack_bf(z[8 * k + 2], z[8 * k + 3]),
+                                    pack_bf(z[8 * k + 4], z[8 * k + 5]), pack_bf(z[8 * k + 6], z[8 * k + 7]));
+          }
+        } else if (live) {
+          float4* dst = reinterpret_cast<float4*>(a.dh + ((size_t)t.part * a.Rp + row) * a.d + j0);
+#pragma unroll
+          for (int k = 0; k < 8; ++k)
+            if (j0 + 4 * k < a.d) {
+              float4 x = make_float4(z[4 * k], z[4 * k + 1], z[4 * k + 2], z[4 * k + 3]);
+              if (!first) {
+                const float4 y = dst[k];
+                x = make_float4(x.x + y.x, x.y + y.y, x.z + y.z, x.w + y.w);
+              }
+              dst[k] = x;
+            }
         }
       }
-    }
-    if (OP == kOpStats) {
-      __syncthreads();
-      if (tid < kTM && m0 + tid < M) {
-        float mx = -pos_inf(), s = 0.f;
-        for (int t = 0; t < 16; ++t) mx = fmaxf(mx, s_m[tid][t]);
-        for (int t = 0; t < 16; ++t) s += s_s[tid][t] > 0.f ? s_s[tid][t] * ex2(s_m[tid][t] - mx) : 0.f;
-        a.part[(size_t)blockIdx.x * a.Rp + m0 + tid] = make_float2(mx, s);
-      }
+      if (OP == kOpStats && live && col < vlen) a.part[(size_t)(col / kHeadPart) * a.Rp + row] = make_float2(mx, sum);
     }
   }
+  if (!ok) atomicOr(a.err, 4u);
+  __syncwarp();
+  tmem_fence_before();
+  cluster_sync_all();
+  tmem_fence_after();
+  if (warp == 1)
+    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tbase), "r"(kTmemCols) : "memory");
 }
 
 // ---- a row's tiles merged -----------------------------------------------------------
@@ -232,30 +495,83 @@ cudaError_t launch_pack(const HeadLossArgs& a, cudaStream_t s) {
   head_pack_kernel<<<tiles(a.R, rows), kPackThreads, 0, s>>>(a, rows);
   return cudaGetLastError();
 }
+
+bool encode_maps(const HeadLossArgs& a, bool backward, Maps* m) {
+  const CUtensorMapDataType t = CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
+  bool ok = tma_matrix(&m->rows_k, t, 2, a.packed, a.d, a.Rp, 128) && tma_matrix(&m->weight_k, t, 2, a.weight, a.d, a.V, 128);
+  if (!backward) {
+    m->rows_n = m->weight_n = m->dz_k = m->dz_m = m->rows_k;       // not read
+    return ok;
+  }
+  return ok && tma_matrix(&m->rows_n, t, 2, a.packed, a.d, a.Rp, 64) && tma_matrix(&m->weight_n, t, 2, a.weight, a.d, a.V, 64) &&
+         tma_matrix(&m->dz_k, t, 2, a.dz, a.Vc, a.Rp, 128) && tma_matrix(&m->dz_m, t, 2, a.dz, a.Vc, a.Rp, 64);
+}
+
+// `most`: tiles at most; one pair of CTAs for each two SMs runs through them
+template <int OP>
+cudaError_t launch_pairs(const HeadLossArgs& a, int v0, int vlen, int first, int64_t most, const Maps& maps,
+                         cudaStream_t s) {
+  static unsigned long long done = 0ull;
+  int dev = 0, sms = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+  if (e != cudaSuccess) return e;
+  const unsigned long long bit = 1ull << (dev & 63);
+  if (!(__atomic_load_n(&done, __ATOMIC_ACQUIRE) & bit)) {
+    e = cudaFuncSetAttribute(head_pair_kernel<OP>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kPairSmem);
+    if (e != cudaSuccess) return e;
+    __atomic_fetch_or(&done, bit, __ATOMIC_ACQ_REL);
+  }
+  int64_t pairs = sms / 2 > 0 ? sms / 2 : 1;
+  if (pairs > most) pairs = most;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(2 * pairs));
+  cfg.blockDim = dim3(kPairThreads);
+  cfg.dynamicSmemBytes = kPairSmem;
+  cfg.stream = s;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, head_pair_kernel<OP>, a, v0, vlen, first, maps);
+}
 }  // namespace
 
-int head_split(int Rp, int d, int Vc) { return 1; }
+// Parts that d_hidden's sum over a piece is cut into, so that about as many
+// tiles as pairs of SMs exist; a part has at least four blocks of 64.
+int head_split(int Rp, int d, int Vc) {
+  const int64_t t = (int64_t)(Rp / kPairTile) * ((d + kPairTile - 1) / kPairTile);
+  int64_t s = 76 / t;
+  if (s > Vc / 256) s = Vc / 256;
+  return s < 1 ? 1 : (int)s;
+}
 
 cudaError_t launch_head_loss(const HeadLossArgs& a, cudaStream_t s) {
+  Maps maps;
+  if (!encode_maps(a, false, &maps)) return cudaErrorInvalidValue;
   cudaError_t e = launch_pack(a, s);
   if (e != cudaSuccess) return e;
-  const unsigned my = min(tiles(a.R, kTM), 65535u);
-  head_gemm_kernel<kOpStats><<<dim3(tiles(a.V, kTN), my), 256, 0, s>>>(a, 0, a.V, 1);
-  head_merge_kernel<<<tiles(a.R, 8), 256, 0, s>>>(a, (int)tiles(a.V, kTN));
+  e = launch_pairs<kOpStats>(a, 0, a.V, 1, (int64_t)(a.Rp / kPairTile) * tiles(a.V, kPairTile), maps, s);
+  if (e != cudaSuccess) return e;
+  head_merge_kernel<<<tiles(a.R, 8), 256, 0, s>>>(a, (int)tiles(a.V, kHeadPart));
   return cudaGetLastError();
 }
 
 cudaError_t launch_head_loss_backward(const HeadLossArgs& a, cudaStream_t s) {
+  Maps maps;
+  if (!encode_maps(a, true, &maps)) return cudaErrorInvalidValue;
   cudaError_t e = launch_pack(a, s);
   if (e != cudaSuccess) return e;
-  const unsigned my = min(tiles(a.Rp, kTM), 65535u);
+  const int64_t mt = a.Rp / kPairTile, dt = tiles(a.d, kPairTile);
   for (int64_t v0 = 0; v0 < a.V; v0 += a.Vc) {
     const int vlen = (int)min((int64_t)a.Vc, a.V - v0);
-    head_gemm_kernel<kOpDz><<<dim3(tiles(a.Vc, kTN), my), 256, 0, s>>>(a, (int)v0, vlen, 0);
-    if (a.d_hidden)
-      head_gemm_kernel<kOpDh><<<dim3(tiles(a.d, kTN), my), 256, 0, s>>>(a, (int)v0, vlen, v0 == 0);
-    if (a.d_weight)
-      head_gemm_kernel<kOpDw><<<dim3(tiles(a.d, kTN), min(tiles(vlen, kTM), 65535u)), 256, 0, s>>>(a, (int)v0, vlen, 0);
+    const int64_t vt = tiles(vlen, kPairTile);
+    e = launch_pairs<kOpDz>(a, (int)v0, vlen, v0 == 0, mt * vt, maps, s);
+    if (e != cudaSuccess) return e;
+    const int64_t most = (a.d_hidden ? mt * dt * a.split : 0) + (a.d_weight ? vt * dt : 0);
+    e = launch_pairs<kOpGrad>(a, (int)v0, vlen, v0 == 0, most, maps, s);
+    if (e != cudaSuccess) return e;
   }
   if (a.d_hidden) head_unpack_kernel<<<tiles(a.R, 8), 256, 0, s>>>(a);
   return cudaGetLastError();
