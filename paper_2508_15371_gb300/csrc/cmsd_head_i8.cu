@@ -16,59 +16,194 @@ __device__ __forceinline__ void i8_to_half(uint32_t w, uint32_t& lo, uint32_t& h
 }
 
 // ---- rows as 8-bit integers ---------------------------------------------------
-constexpr int kQuantThreads = 256;
+//
+// One pass: a row's numbers stay in the registers of its warp (or of the eight
+// warps of a CTA for wide rows) between the search for the largest and the
+// rounding, so memory, 2 or 4 bytes read and one written per number, bounds it.
 
-// 127 x / a rounded to the nearest whole number, ties to the even one, exactly:
-// the quotient by r ~ 1 / a decides unless it lies within 2^-12 of a tie (it is
-// off by less than 127 * 2^-21); there the sign of 127 x - c a, c the tie, does,
-// from the two products' roundings (each product's error is one fma, and the
-// difference of the rounded products is exact, as they are within a factor of
-// two of each other).  0 <= x <= a, both scaled so that nothing overflows.
-__device__ __forceinline__ float quantize_abs(float x, float a, float r) {
+// 127 x / a rounded to the nearest whole number, ties to the even one, exactly,
+// where an approximation t of the quotient is within 2^-12 of a tie: the sign of
+// 127 x - c a, c the tie, decides, from the two products' roundings (each
+// product's error is one fma, and the difference of the rounded products is
+// exact, as they are within a factor of two of each other).  0 <= x <= a, both
+// scaled so that nothing overflows.
+__device__ __noinline__ float quantize_abs(float x, float a) {
   const float hi = __fmul_rn(127.f, x);
-  const float t = hi * r;
-  float q = rintf(t);
-  const float f = fabsf(t - q);
-  if (f > 0.5f - 0x1p-12f) {
-    const float k = floorf(t), c = k + 0.5f;
-    const float lo = __fmaf_rn(127.f, x, -hi);
-    const float ph = __fmul_rn(c, a), pl = __fmaf_rn(c, a, -ph);
-    const float past = (hi - ph) + (lo - pl);
-    const bool odd = ((int)k & 1) != 0;
-    q = past > 0.f || (past == 0.f && odd) ? k + 1.f : k;
-  }
-  return q;
+  const float t = __fdividef(hi, a);
+  const float q = rintf(t);
+  if (fabsf(t - q) <= 0.5f - 0x1p-12f) return q;
+  const float k = floorf(t), c = k + 0.5f;
+  const float lo = __fmaf_rn(127.f, x, -hi);
+  const float ph = __fmul_rn(c, a), pl = __fmaf_rn(c, a, -ph);
+  const float past = (hi - ph) + (lo - pl);
+  const bool odd = ((int)k & 1) != 0;
+  return past > 0.f || (past == 0.f && odd) ? k + 1.f : k;
 }
 
-__device__ __forceinline__ float load_f(const float* p, size_t i) { return p[i]; }
-__device__ __forceinline__ float load_f(const __nv_bfloat16* p, size_t i) { return __bfloat162float(p[i]); }
+template <typename T>
+struct QuantVec;                                    // 16 bytes of a row
+template <>
+struct QuantVec<float> {
+  static constexpr int kN = 4;
+  static __device__ __forceinline__ float get(const uint4& v, int j) {
+    return __uint_as_float(j == 0 ? v.x : (j == 1 ? v.y : (j == 2 ? v.z : v.w)));
+  }
+  static __device__ __forceinline__ uint32_t mag(const uint4& v) {
+    return max(max(v.x & 0x7FFFFFFFu, v.y & 0x7FFFFFFFu), max(v.z & 0x7FFFFFFFu, v.w & 0x7FFFFFFFu));
+  }
+};
+template <>
+struct QuantVec<__nv_bfloat16> {
+  static constexpr int kN = 8;
+  static __device__ __forceinline__ float get(const uint4& v, int j) {
+    const uint32_t w = j < 2 ? v.x : (j < 4 ? v.y : (j < 6 ? v.z : v.w));
+    return j & 1 ? bf_hi(w) : bf_lo(w);
+  }
+  static __device__ __forceinline__ uint32_t mag(const uint4& v) {
+    const uint32_t m = __vmaxu2(__vmaxu2(v.x & 0x7FFF7FFFu, v.y & 0x7FFF7FFFu),
+                                __vmaxu2(v.z & 0x7FFF7FFFu, v.w & 0x7FFF7FFFu));
+    return max(m & 0xFFFF0000u, m << 16);
+  }
+};
+
+struct QuantRow {
+  float a, f, k;         // largest magnitude scaled by f, 127 / a
+  bool fine, plain;      // finite and not zero; no scaling needed
+};
+// the bits of |x| order like its value, an infinity and then NaNs on top
+__device__ __forceinline__ QuantRow quant_row(uint32_t m) {
+  QuantRow r;
+  const float a0 = __uint_as_float(m);
+  r.fine = m != 0 && m < 0x7F800000u;
+  r.plain = a0 >= 0x1p-60f && a0 <= 0x1p60f;
+  r.f = r.plain ? 1.f : (a0 < 1.f ? 0x1p100f : 0x1p-100f);
+  r.a = r.fine ? a0 * r.f : 1.f;
+  r.k = 127.f / r.a;
+  return r;
+}
+// one 16-byte vector as kN bytes in words o[0 .. kN / 4)
+template <typename T>
+__device__ __forceinline__ void quant_vec(const uint4& v, const QuantRow& r, uint32_t* o) {
+  using Q = QuantVec<T>;
+  constexpr float kMagic = 12582912.f;              // 1.5 * 2^23: adding it rounds to a whole number
+  uint32_t y[Q::kN];
+  float off = 1.f;
+  if (r.plain) {
+    off = 0.f;
+#pragma unroll
+    for (int j = 0; j < Q::kN; ++j) {
+      const float x = Q::get(v, j);
+      const float s = __fmaf_rn(x, r.k, kMagic);
+      off = fmaxf(off, fabsf(__fmaf_rn(x, r.k, kMagic - s)));
+      y[j] = __float_as_uint(s);
+    }
+  }
+  if (off > 0.5f - 0x1p-16f) {                      // near a tie (x r.k is off by 127 * 2^-24 at most), or scaled
+#pragma unroll 1
+    for (int j = 0; j < Q::kN; ++j) {
+      const float x = Q::get(v, j);
+      const float q = r.fine ? quantize_abs(fabsf(x) * r.f, r.a) : 0.f;
+      const uint32_t b = (uint32_t)(int)copysignf(q, x);
+#pragma unroll
+      for (int u = 0; u < Q::kN; ++u) y[u] = u == j ? b : y[u];
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < Q::kN / 4; ++j)
+    o[j] = __byte_perm(__byte_perm(y[4 * j], y[4 * j + 1], 0x0040), __byte_perm(y[4 * j + 2], y[4 * j + 3], 0x0040),
+                       0x5410);
+}
+template <typename T>
+__device__ __forceinline__ void quant_store(int8_t* dst, const uint32_t* o) {
+  if (QuantVec<T>::kN == 8)
+    *reinterpret_cast<uint2*>(dst) = make_uint2(o[0], o[1]);
+  else
+    *reinterpret_cast<uint32_t*>(dst) = o[0];
+}
+
+constexpr int kQuantThreads = 128;                  // four rows of a warp each
+constexpr int kQuantWide = 256;                     // one row
+// rows of up to 32 * NV vectors, a warp each
+template <typename T, int NV>
+__global__ void __launch_bounds__(kQuantThreads) quantize_warp_kernel(const T* __restrict__ x, int R, int d,
+                                                                      int8_t* __restrict__ q, float* __restrict__ scale) {
+  constexpr int kN = QuantVec<T>::kN;
+  const int lane = threadIdx.x & 31, vecs = d / kN;
+  const int r = blockIdx.x * (kQuantThreads / 32) + (threadIdx.x >> 5);
+  if (r >= R) return;
+  const uint4* src = reinterpret_cast<const uint4*>(x + (size_t)r * d);
+  uint4 v[NV];
+  uint32_t m = 0;
+#pragma unroll
+  for (int i = 0; i < NV; ++i) v[i] = lane + 32 * i < vecs ? ld_stream(src + lane + 32 * i) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+  for (int i = 0; i < NV; ++i) m = max(m, QuantVec<T>::mag(v[i]));
+  m = __reduce_max_sync(kFull, m);
+  const QuantRow row = quant_row(m);
+  int8_t* dst = q + (size_t)r * d;
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    uint32_t o[kN / 4];
+    quant_vec<T>(v[i], row, o);
+    if (lane + 32 * i < vecs) quant_store<T>(dst + (lane + 32 * i) * kN, o);
+  }
+  if (lane == 0) scale[r] = __fdiv_rn(__uint_as_float(m), 127.f);
+}
+// wider rows, a CTA each: up to kQuantWide * NV vectors in registers, what lies
+// beyond is read twice
+template <typename T, int NV>
+__global__ void __launch_bounds__(kQuantWide) quantize_cta_kernel(const T* __restrict__ x, int R, int d,
+                                                                  int8_t* __restrict__ q, float* __restrict__ scale) {
+  constexpr int kN = QuantVec<T>::kN;
+  __shared__ uint32_t s_max[2][kQuantWide / 32];
+  const int tid = threadIdx.x, vecs = d / kN;
+  int turn = 0;
+  for (int r = blockIdx.x; r < R; r += gridDim.x, turn ^= 1) {
+    const uint4* src = reinterpret_cast<const uint4*>(x + (size_t)r * d);
+    uint4 v[NV];
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+      v[i] = tid + kQuantWide * i < vecs ? ld_stream(src + tid + kQuantWide * i) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+    for (int i = 0; i < NV; ++i) m = max(m, QuantVec<T>::mag(v[i]));
+    for (int i = tid + kQuantWide * NV; i < vecs; i += kQuantWide) m = max(m, QuantVec<T>::mag(src[i]));
+    m = __reduce_max_sync(kFull, m);
+    if ((tid & 31) == 0) s_max[turn][tid >> 5] = m;  // (two arrays in turn: one barrier a row)
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < kQuantWide / 32; ++w) m = max(m, s_max[turn][w]);
+    const QuantRow row = quant_row(m);
+    int8_t* dst = q + (size_t)r * d;
+    uint32_t o[kN / 4];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      quant_vec<T>(v[i], row, o);
+      if (tid + kQuantWide * i < vecs) quant_store<T>(dst + (tid + kQuantWide * i) * kN, o);
+    }
+    for (int i = tid + kQuantWide * NV; i < vecs; i += kQuantWide) {
+      quant_vec<T>(src[i], row, o);
+      quant_store<T>(dst + i * kN, o);
+    }
+    if (tid == 0) scale[r] = __fdiv_rn(__uint_as_float(m), 127.f);
+  }
+}
 
 template <typename T>
-__global__ void __launch_bounds__(kQuantThreads) quantize_kernel(const T* __restrict__ x, int R, int d,
-                                                                 int8_t* __restrict__ q, float* __restrict__ scale) {
-  __shared__ uint32_t s_max[kQuantThreads / 32];
-  const int tid = threadIdx.x;
-  for (int r = blockIdx.x; r < R; r += gridDim.x) {
-    const T* row = x + (size_t)r * d;
-    // the bits of |x| order like its value, an infinity and then NaNs on top
-    uint32_t m = 0;
-    for (int j = tid; j < d; j += kQuantThreads) m = max(m, __float_as_uint(load_f(row, j)) & 0x7FFFFFFFu);
-    m = __reduce_max_sync(kFull, m);
-    if ((tid & 31) == 0) s_max[tid >> 5] = m;
-    __syncthreads();
-    for (int w = 0; w < kQuantThreads / 32; ++w) m = max(m, s_max[w]);
-    __syncthreads();
-    const float a0 = __uint_as_float(m);
-    const bool fine = m != 0 && m < 0x7F800000u;
-    const float f = a0 < 0x1p-60f ? 0x1p100f : (a0 > 0x1p60f ? 0x1p-100f : 1.f);
-    const float a = fine ? a0 * f : 1.f, inv = 1.f / a;
-    for (int j = tid; j < d; j += kQuantThreads) {
-      const float v = load_f(row, j);
-      const float u = fine ? quantize_abs(fabsf(v) * f, a, inv) : 0.f;
-      q[(size_t)r * d + j] = (int8_t)(int)copysignf(u, v);
-    }
-    if (tid == 0) scale[r] = __fdiv_rn(a0, 127.f);
-  }
+cudaError_t launch_quantize(const T* x, int R, int d, int8_t* q, float* scale, cudaStream_t s) {
+  const int vecs = d / QuantVec<T>::kN;
+  const unsigned rows = (unsigned)((R + kQuantThreads / 32 - 1) / (kQuantThreads / 32));
+  if (vecs <= 32 * 4)
+    quantize_warp_kernel<T, 4><<<rows, kQuantThreads, 0, s>>>(x, R, d, q, scale);
+  else if (vecs <= 32 * 8)
+    quantize_warp_kernel<T, 8><<<rows, kQuantThreads, 0, s>>>(x, R, d, q, scale);
+  else if (vecs <= 32 * 16)
+    quantize_warp_kernel<T, 16><<<rows, kQuantThreads, 0, s>>>(x, R, d, q, scale);
+  else if (vecs <= kQuantWide * 4)
+    quantize_cta_kernel<T, 4><<<(unsigned)(R < (1 << 20) ? R : 1 << 20), kQuantWide, 0, s>>>(x, R, d, q, scale);
+  else
+    quantize_cta_kernel<T, 8><<<(unsigned)(R < (1 << 20) ? R : 1 << 20), kQuantWide, 0, s>>>(x, R, d, q, scale);
+  return cudaGetLastError();
 }
 
 // ---- the product ----------------------------------------------------------------
@@ -88,17 +223,16 @@ __global__ void __launch_bounds__(kQuantThreads) quantize_kernel(const T* __rest
 //   warp 0      lane 0 fills the ring: 128 bytes of K of the tile's weight rows,
 //               and the same K of the tokens (fp16, from the workspace);
 //   warp 1      lane 0 issues the MMAs;
-//   warps 2..9  thread = one vocabulary entry: turns its row of a stage into
-//               fp16, and adds up and scales its row of sums.  The first stage
-//               of the next 1024 of K is turned before the sums of the last are
-//               read, so that the MMAs resume at once.
+//   warps 2..17 two sets of eight, thread = one vocabulary entry: a set turns
+//               its rows of every second stage into fp16 in its own buffer, and
+//               adds up and scales every second group of 16 tokens.
 // Barriers: full (TMA -> fp16 and MMA), afull / aempty (fp16 <-> MMA, two
 // buffers in tensor memory), empty (MMA -> TMA), dfull / dempty (MMA <-> sums).
 // Every wait is bounded.
 constexpr int kI8Tile = 256;                        // vocabulary entries per tile at most
 constexpr int kI8K = 128;                           // K per stage
 constexpr int kI8Exact = 1024 / kI8K;               // stages whose sums are exact in fp32
-constexpr int kI8Threads = 64 + kI8Tile;
+constexpr int kI8Threads = 64 + 2 * kI8Tile;
 constexpr int kI8WStage = kI8Tile * kI8K;
 template <int NT>
 struct I8Shape {
@@ -108,11 +242,6 @@ struct I8Shape {
   static constexpr size_t kSmem = 1024 + (size_t)kStages * kStage + 8 * (2 * kStages + 6) + 16;
   static_assert(kSmem <= 227 * 1024, "shared memory");
 };
-__device__ __forceinline__ float ld_volatile_f(const float* p) {
-  float x;
-  asm volatile("ld.global.f32 %0, [%1];" : "=f"(x) : "l"(p) : "memory");
-  return x;
-}
 struct I8Plan {
   int height;            // vocabulary entries per tile (a multiple of 8)
   int cols;              // tokens per tile (a multiple of 16, at most 128)
@@ -154,11 +283,11 @@ __global__ void __launch_bounds__(kI8Threads, 1)
       mbar_init(empty + 8 * k, 1);
     }
     for (int b = 0; b < 2; ++b) {
-      mbar_init(afull + 8 * b, 8);
+      mbar_init(afull + 8 * b, kI8Tile / 32);
       mbar_init(aempty + 8 * b, 1);
     }
     mbar_init(dfull, 1);
-    mbar_init(dempty, 8);
+    mbar_init(dempty, 2 * kI8Tile / 32);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == 1) {
@@ -196,7 +325,7 @@ __global__ void __launch_bounds__(kI8Threads, 1)
         const int v = t / p.rt, r = t - v * p.rt;
         const uint32_t dst = base + s * S::kStage;
         if (g >= kStages) {
-          if (ok) ok = mbar_wait(empty + 8 * s, (uint32_t)((g / kStages - 1) & 1));
+          if (ok) ok = bar_wait<false>(empty + 8 * s, (uint32_t)((g / kStages - 1) & 1));
           mbar_arrive_tx(full + 8 * s, bytes);
           tma_box(dst, &map_w, k, v * p.height, full + 8 * s);
         }
@@ -205,54 +334,135 @@ __global__ void __launch_bounds__(kI8Threads, 1)
       }
       // nothing is in flight into this CTA when it ends
       for (int g = (G > kStages ? G - kStages : 0); g < G; ++g)
-        if (ok) ok = mbar_wait(empty + 8 * (g % kStages), (uint32_t)((g / kStages) & 1));
+        if (ok) ok = bar_wait<false>(empty + 8 * (g % kStages), (uint32_t)((g / kStages) & 1));
     }
   } else if (warp == 1) {
-    if (lane == 0) {
-      const uint32_t idesc = mma_idesc(128, p.cols, false, false, false);
-      int c = 0;                                    // sums handed over
-      for (int g = 0; g < G; ++g) {
-        const int s = g % kStages, b = g & 1, k = g % ks;
-        if (k % kI8Exact == 0) {
-          if (c > 0 && ok) ok = mbar_wait(dempty, (uint32_t)((c - 1) & 1));
-        }
-        if (ok) ok = mbar_wait(full + 8 * s, (uint32_t)((g / kStages) & 1));
-        if (ok) ok = mbar_wait(afull + 8 * b, (uint32_t)((g / 2) & 1));
-        tmem_fence_after();
-        const uint32_t hs = base + s * S::kStage + kI8WStage;
+    // the whole warp runs through the stages, so that what the MMAs take is
+    // formed in uniform registers; one lane issues
+    const bool leader = elect_lane();
+    const uint32_t idesc = mma_idesc(128, p.cols, false, false, false);
+    const uint32_t half = (uint32_t)p.cols * 128 >> 4;       // the second 64 of K, in units of 16 bytes
+    int c = 0, s = 0, k = 0;                        // sums handed over; ring slot; stage of the tile
+    uint32_t phase = 0;
+    for (int g = 0; g < G; ++g) {
+      const int b = g & 1;
+      const uint32_t more = k % kI8Exact != 0;
+      if (!more && c > 0 && ok) ok = bar_wait<false>(dempty, (uint32_t)((c - 1) & 1));
+      if (ok) ok = bar_wait<false>(full + 8 * s, phase);
+      if (ok) ok = bar_wait<false>(afull + 8 * b, (uint32_t)((g / 2) & 1));
+      tmem_fence_after();
+      const uint64_t h0 = mma_desc(base + s * S::kStage + kI8WStage, 0), h1 = h0 + half;
+      const uint32_t at = abase + b * 128;
+      const bool ends = k % kI8Exact == kI8Exact - 1 || k == ks - 1;
+      if (leader) {
 #pragma unroll
         for (int sub = 0; sub < 2; ++sub) {
-          if (sub * 128 >= p.height) break;
+          if (sub * 128 < p.height) {
+            mma_tmem_a(tbase + sub * 128, at + sub * 64, h0, idesc, more);
 #pragma unroll
-          for (int j = 0; j < kI8K / 16; ++j)
-            mma_tmem_a(tbase + sub * 128, abase + b * 128 + sub * 64 + j * 8,
-                       mma_desc(hs + (j >> 2) * p.cols * 128, 0) + (uint64_t)(2 * (j & 3)), idesc,
-                       (k % kI8Exact) != 0 || j != 0);
+            for (int j = 1; j < kI8K / 16; ++j)
+              mma_tmem_a(tbase + sub * 128, at + sub * 64 + j * 8, (j >> 2 ? h1 : h0) + (uint64_t)(2 * (j & 3)), idesc, 1);
+          }
         }
         mma_commit(aempty + 8 * b);
         mma_commit(empty + 8 * s);
-        if (k % kI8Exact == kI8Exact - 1 || k == ks - 1) {
-          mma_commit(dfull);
-          ++c;
-        }
+        if (ends) mma_commit(dfull);
+      }
+      __syncwarp();
+      c += ends;
+      if (++k == ks) k = 0;
+      if (++s == kStages) {
+        s = 0;
+        phase ^= 1;
       }
     }
-    __syncwarp();
   } else {
-    const int q = warp & 3, sub = (warp - 2) >> 2;
+    const int q = warp & 3, sub = ((warp - 2) >> 2) & 1, set = (warp - 2) >> 3;
     const int row = sub * 128 + q * 32 + lane;      // vocabulary entry within the tile
     const uint32_t quarter = (uint32_t)(q * 32) << 16;
     const uint32_t wrow = (uint32_t)row * 128, x8 = (uint32_t)(row & 7);
-    int acc[NT];
+    // sums of this set's groups of 16 tokens (every second one)
+    constexpr int kGroups = NT / 16, kMine = kGroups > 1 ? kGroups / 2 : 1;
+    int acc[16 * kMine];
 #pragma unroll
-    for (int n = 0; n < NT; ++n) acc[n] = 0;
-    int c = 0, due = -1;                            // stage whose sums are to be read next, -1: none
-    bool waited = false;
-    for (int g = 0; g <= G; ++g) {
+    for (int n = 0; n < 16 * kMine; ++n) acc[n] = 0;
+    int c = 0, tile = 0;                            // sums read so far; tiles done
+    int end = min(kI8Exact, ks) - 1;                // the stage whose sums are read next
+    // reads the sums that end at stage `end`, and scales and writes a tile's last
+    auto read_sums = [&]() {
+      const bool last = end == (tile + 1) * ks - 1;
+      const int t = (int)blockIdx.x + tile * (int)gridDim.x;
+      const int vi = t / p.rt, r0 = (t - vi * p.rt) * p.cols, v = vi * p.height + row;
+      const bool mine = last && row < p.height && v < a.V;
+      float ws = 0.f, hs[(NT + 31) / 32];
+      if (last) {                                   // (loaded ahead of the wait)
+#pragma unroll
+        for (int i = 0; i < (NT + 31) / 32; ++i) hs[i] = __ldg(a.hidden_scale + min(r0 + 32 * i + lane, a.R - 1));
+        if (mine) ws = __ldg(a.weight_scale + v);
+      }
+      if (ok) ok = bar_wait<false>(dfull, (uint32_t)(c & 1));
+      ++c;
+      __syncwarp();
+      tmem_fence_after();
+      const uint32_t src = tbase + quarter + sub * 128 + 16 * set;
+#pragma unroll
+      for (int i = 0; i < kMine; ++i) {
+        if (16 * (2 * i + set) < p.cols) {
+          float z[16];
+          tmem_ld16_ahead(src + 32 * i, z);
+          tmem_ld_wait(z);
+#pragma unroll
+          for (int j = 0; j < 16; ++j) acc[16 * i + j] += __float2int_rn(z[j]);
+        }
+      }
+      tmem_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive_local(dempty);
+      if (last) {
+        if (tile == 0) asm volatile("griddepcontrol.wait;" ::: "memory");   // (what precedes this grid may still use them)
+        char* out = reinterpret_cast<char*>(a.logits) + ((size_t)(r0 + 16 * set) * a.V + v) * (kBf16 ? 2 : 4);
+        const size_t step = (size_t)a.V * (kBf16 ? 2 : 4);
+        const int rows = mine ? min(a.R - r0, p.cols) - 16 * set : 0;       // of this set's first group on
+#pragma unroll
+        for (int i = 0; i < kMine; ++i) {
+#pragma unroll
+          for (int j = 0; j < 16; ++j) {
+            const float h = __shfl_sync(kFull, hs[i], 16 * set + j);
+            if (32 * i + j < rows) {
+              const float z = (float)acc[16 * i + j] * h * ws;
+              if (kBf16)
+                *reinterpret_cast<__nv_bfloat16*>(out) = __float2bfloat16_rn(z);
+              else
+                *reinterpret_cast<float*>(out) = z;
+            }
+            out += step;
+            acc[16 * i + j] = 0;
+          }
+          out += 16 * step;
+        }
+        ++tile;
+      }
+      end = last ? tile * ks + min(kI8Exact, ks) - 1 : min(end + kI8Exact, (tile + 1) * ks - 1);
+    };
+    // Sums that ended at this set's last stage or before are read first: the
+    // MMAs wait for it.  What ended at the other set's is read after this set's
+    // next stage has been turned, which the MMAs want at once then.
+    bool turned = false;
+    for (int g = set; g < G + 2;) {
+      if (end < (turned ? g : g - 1) && end < G) {
+        read_sums();
+        continue;
+      }
+      if (turned) {
+        turned = false;
+        g += 2;
+        continue;
+      }
+      turned = true;
       if (g < G) {
-        const int s = g % kStages, b = g & 1;
-        if (ok) ok = mbar_wait(full + 8 * s, (uint32_t)((g / kStages) & 1));
-        if (g >= 2 && ok) ok = mbar_wait(aempty + 8 * b, (uint32_t)((g / 2 - 1) & 1));
+        const int s = g % kStages;
+        if (ok) ok = bar_wait<false>(full + 8 * s, (uint32_t)((g / kStages) & 1));
+        if (g >= 2 && ok) ok = bar_wait<false>(aempty + 8 * set, (uint32_t)((g / 2 - 1) & 1));
         __syncwarp();
         tmem_fence_after();
         const uint32_t src = base + s * S::kStage + wrow;
@@ -272,67 +482,13 @@ __global__ void __launch_bounds__(kI8Threads, 1)
             i8_to_half(w2, o[8 * j + 4], o[8 * j + 5]);
             i8_to_half(w3, o[8 * j + 6], o[8 * j + 7]);
           }
-          tmem_st(abase + quarter + b * 128 + sub * 64 + kCols * h, o);
+          tmem_st(abase + quarter + set * 128 + sub * 64 + kCols * h, o);
         }
         tmem_st_wait();
         tmem_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive_local(afull + 8 * b);
+        if (lane == 0) mbar_arrive_local(afull + 8 * set);
       }
-      // the sums that ended at the stage before this one
-      if (due >= 0) {
-        if (ok) ok = mbar_wait(dfull, (uint32_t)(c & 1));
-        ++c;
-        __syncwarp();
-        tmem_fence_after();
-#pragma unroll
-        for (int n = 0; n < NT; n += 16) {
-          if (n < p.cols) {
-            float z[16];
-            tmem_ld16(tbase + quarter + sub * 128 + n, z);
-#pragma unroll
-            for (int j = 0; j < 16; ++j) acc[n + j] += __float2int_rn(z[j]);
-          }
-        }
-        tmem_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive_local(dempty);
-        if (due % ks == ks - 1) {                   // the tile's last: scaled and written
-          if (!waited) {                            // what the call before may still read or write
-            asm volatile("griddepcontrol.wait;" ::: "memory");
-            waited = true;
-          }
-          const int t = (int)blockIdx.x + due / ks * (int)gridDim.x;
-          const int vi = t / p.rt, r0 = (t - vi * p.rt) * p.cols;
-          const int v = vi * p.height + row;
-          if (row < p.height && v < a.V) {
-            const float ws = a.weight_scale[v];
-#pragma unroll
-            for (int n0 = 0; n0 < NT; n0 += 16) {
-              if (n0 < p.cols) {
-                float hs[16];                       // (sixteen at a time: more would cost the sums their registers)
-#pragma unroll
-                for (int j = 0; j < 16; ++j) hs[j] = ld_volatile_f(a.hidden_scale + min(r0 + n0 + j, a.R - 1));
-#pragma unroll
-                for (int j = 0; j < 16; ++j) {
-                  const int r = r0 + n0 + j;
-                  const float z = (float)acc[n0 + j] * hs[j] * ws;
-                  if (r < a.R) {
-                    const size_t at = (size_t)r * a.V + v;
-                    if (kBf16)
-                      reinterpret_cast<__nv_bfloat16*>(a.logits)[at] = __float2bfloat16_rn(z);
-                    else
-                      reinterpret_cast<float*>(a.logits)[at] = z;
-                  }
-                }
-              }
-            }
-          }
-#pragma unroll
-          for (int n = 0; n < NT; ++n) acc[n] = 0;
-        }
-      }
-      due = g < G && ((g % ks) % kI8Exact == kI8Exact - 1 || g % ks == ks - 1) ? g : -1;
     }
   }
   if (!ok) atomicOr(a.err, 4u);
@@ -378,12 +534,8 @@ cudaError_t launch_i8_cols(const HeadI8Args& a, const I8Plan& p, int grid, int d
 }  // namespace
 
 cudaError_t launch_quantize_rows(const void* x, int dtype, int R, int d, int8_t* q, float* scale, cudaStream_t s) {
-  const int grid = R < (1 << 20) ? R : 1 << 20;
-  if (dtype == 0)
-    quantize_kernel<float><<<grid, kQuantThreads, 0, s>>>((const float*)x, R, d, q, scale);
-  else
-    quantize_kernel<__nv_bfloat16><<<grid, kQuantThreads, 0, s>>>((const __nv_bfloat16*)x, R, d, q, scale);
-  return cudaGetLastError();
+  return dtype == 0 ? launch_quantize((const float*)x, R, d, q, scale, s)
+                    : launch_quantize((const __nv_bfloat16*)x, R, d, q, scale, s);
 }
 
 cudaError_t launch_head_i8(const HeadI8Args& a, cudaStream_t s) {

@@ -282,7 +282,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
         const int am = t.m * kPairTile + (int)rank * 128, bn = t.n * kPairTile + (int)rank * 128;
         for (int kb = 0; kb < t.kb; ++kb, ++g) {
           const int s = g % kStages;
-          if (g >= kStages && ok) ok = mbar_wait_cluster(empty + 8 * s, (uint32_t)((g / kStages - 1) & 1));
+          if (g >= kStages && ok) ok = bar_wait<true>(empty + 8 * s, (uint32_t)((g / kStages - 1) & 1));
           if (rank == 0) mbar_arrive_tx(full + 8 * s, 2 * kStageBytes);
           const uint32_t sa = base + s * kStageBytes, sb = sa + kHalfBytes, bar = full0 + 8 * s;
           const int k = (t.k0 + kb) * 64;
@@ -303,7 +303,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
       }
       // the last stages are consumed before this CTA's shared memory goes
       for (int k = (g > kStages ? g - kStages : 0); k < g; ++k)
-        if (ok) ok = mbar_wait_cluster(empty + 8 * (k % kStages), (uint32_t)((k / kStages) & 1));
+        if (ok) ok = bar_wait<true>(empty + 8 * (k % kStages), (uint32_t)((k / kStages) & 1));
     }
   } else if (warp == 1) {
     // ---- the MMAs of both CTAs -----------------------------------------------------
@@ -314,7 +314,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
       for (int i = 0; i < w.total; ++i) {
         const Tile t = tile_of<OP>(a, w, i);
         const int b = i & 1;
-        if (i >= 2 && ok) ok = mbar_wait_cluster(tempty + 8 * b, (uint32_t)((i / 2 - 1) & 1));
+        if (i >= 2 && ok) ok = bar_wait<true>(tempty + 8 * b, (uint32_t)((i / 2 - 1) & 1));
         tmem_fence_after();
         const uint32_t d = tbase + (uint32_t)(b * 256);
         const uint32_t idesc = OP != kOpGrad ? mma_idesc(256, 256, true, false, false)
@@ -324,7 +324,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
         const uint64_t da = OP == kOpGrad && t.dw ? 2048 >> 4 : 32 >> 4, db = OP == kOpGrad ? 2048 >> 4 : 32 >> 4;
         for (int kb = 0; kb < t.kb; ++kb, ++g) {
           const int s = g % kStages;
-          if (ok) ok = mbar_wait_cluster(full + 8 * s, (uint32_t)((g / kStages) & 1));
+          if (ok) ok = bar_wait<true>(full + 8 * s, (uint32_t)((g / kStages) & 1));
           tmem_fence_after();
           const uint64_t ad = mma_desc(base + s * kStageBytes, kHalfBytes / 2);
           const uint64_t bd = mma_desc(base + s * kStageBytes + kHalfBytes, kHalfBytes / 2);
@@ -345,7 +345,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
     for (int i = 0; i < w.total; ++i) {
       const Tile t = tile_of<OP>(a, w, i);
       const int b = i & 1;
-      if (ok) ok = mbar_wait_cluster(tfull + 8 * b, (uint32_t)((i / 2) & 1));
+      if (ok) ok = bar_wait<true>(tfull + 8 * b, (uint32_t)((i / 2) & 1));
       __syncwarp();
       tmem_fence_after();
       const int row = t.m * kPairTile + (int)rank * 128 + q * 32 + lane;
