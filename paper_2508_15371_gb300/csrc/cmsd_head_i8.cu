@@ -67,7 +67,7 @@ struct QuantVec<__nv_bfloat16> {
 };
 
 struct QuantRow {
-  float a, f, k;         // largest magnitude scaled by f, 127 / a
+  float a, f, k, kl;     // largest magnitude scaled by f; 127 / a and what rounding it left out
   bool fine, plain;      // finite and not zero; no scaling needed
 };
 // the bits of |x| order like its value, an infinity and then NaNs on top
@@ -79,13 +79,20 @@ __device__ __forceinline__ QuantRow quant_row(uint32_t m) {
   r.f = r.plain ? 1.f : (a0 < 1.f ? 0x1p100f : 0x1p-100f);
   r.a = r.fine ? a0 * r.f : 1.f;
   r.k = 127.f / r.a;
+  r.kl = __fmaf_rn(-r.k, r.a, 127.f) / r.a;
   return r;
 }
-// one 16-byte vector as kN bytes in words o[0 .. kN / 4)
+// One 16-byte vector as kN bytes in words o[0 .. kN / 4).  x k rounded by adding
+// 1.5 * 2^23; the distance of x (k + kl) from it, exact to 2^-24, shows a tie.
+// Ties of bf16 numbers are common (every x = a / 2 is one) and stand apart:
+// with x = X 2^e, a = A 2^f, X and A below 256 and f - e <= 8, 127 x / a is a tie
+// or at least 2^-7 / (2 A) > 2^-17 from one.  Ties of fp32 numbers are rare, but
+// others lie as near, and an exact comparison decides.
 template <typename T>
 __device__ __forceinline__ void quant_vec(const uint4& v, const QuantRow& r, uint32_t* o) {
   using Q = QuantVec<T>;
-  constexpr float kMagic = 12582912.f;              // 1.5 * 2^23: adding it rounds to a whole number
+  constexpr float kMagic = 12582912.f;              // 1.5 * 2^23
+  constexpr float kTie = Q::kN == 8 ? 0.5f - 0x1p-18f : 0.5f - 0x1p-22f;
   uint32_t y[Q::kN];
   float off = 1.f;
   if (r.plain) {
@@ -94,18 +101,27 @@ __device__ __forceinline__ void quant_vec(const uint4& v, const QuantRow& r, uin
     for (int j = 0; j < Q::kN; ++j) {
       const float x = Q::get(v, j);
       const float s = __fmaf_rn(x, r.k, kMagic);
-      off = fmaxf(off, fabsf(__fmaf_rn(x, r.k, kMagic - s)));
+      off = fmaxf(off, fabsf(__fmaf_rn(x, r.kl, __fmaf_rn(x, r.k, kMagic - s))));
       y[j] = __float_as_uint(s);
     }
   }
-  if (off > 0.5f - 0x1p-16f) {                      // near a tie (x r.k is off by 127 * 2^-24 at most), or scaled
-#pragma unroll 1
-    for (int j = 0; j < Q::kN; ++j) {
-      const float x = Q::get(v, j);
-      const float q = r.fine ? quantize_abs(fabsf(x) * r.f, r.a) : 0.f;
-      const uint32_t b = (uint32_t)(int)copysignf(q, x);
+  if (off > kTie) {
+    if (Q::kN == 8 && r.plain) {
 #pragma unroll
-      for (int u = 0; u < Q::kN; ++u) y[u] = u == j ? b : y[u];
+      for (int j = 0; j < Q::kN; ++j) {             // k + 1/2: half of it is a quarter from the even one's half
+        const float x = Q::get(v, j), q = __uint_as_float(y[j]) - kMagic;
+        const float even = 2.f * rintf(0.5f * (x * r.k));
+        if (fabsf(__fmaf_rn(x, r.kl, __fmaf_rn(x, r.k, -q))) > kTie) y[j] = __float_as_uint(even + kMagic);
+      }
+    } else {
+#pragma unroll 1
+      for (int j = 0; j < Q::kN; ++j) {
+        const float x = Q::get(v, j);
+        const float q = r.fine ? quantize_abs(fabsf(x) * r.f, r.a) : 0.f;
+        const uint32_t b = (uint32_t)(int)copysignf(q, x);
+#pragma unroll
+        for (int u = 0; u < Q::kN; ++u) y[u] = u == j ? b : y[u];
+      }
     }
   }
 #pragma unroll

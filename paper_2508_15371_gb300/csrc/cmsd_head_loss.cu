@@ -21,32 +21,45 @@ __device__ __forceinline__ bool kept(const HeadLossArgs& a, int label) {
 
 // ---- the kept rows, packed --------------------------------------------------------
 constexpr int kPackThreads = 256;
-// Each CTA packs `rows` consecutive rows: it counts the kept rows before its
-// own in the labels (a prefix of them, read again by every CTA), then copies.
-// The last one also writes the count and fills up to the next whole tile.
-__global__ void __launch_bounds__(kPackThreads) head_pack_kernel(const HeadLossArgs a, int rows) {
-  __shared__ int s_sum[kPackThreads / 32];
-  __shared__ int s_base;
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int r0 = blockIdx.x * rows, r1 = min(a.R, r0 + rows);
+constexpr int kPackWarps = kPackThreads / 32;
+constexpr int kPackZero = 8;                         // CTAs that fill rows behind the last with zeros
+// kept rows among labels [0, r), the whole CTA's answer
+__device__ __forceinline__ int count_kept(const HeadLossArgs& a, int r) {
+  __shared__ int s_sum[kPackWarps];
   int c = 0;
-  for (int r = tid; r < r0; r += kPackThreads) c += kept(a, a.labels[r]);
+  for (int k = threadIdx.x; k < r; k += kPackThreads) c += kept(a, a.labels[k]);
   c = __reduce_add_sync(kFull, c);
-  if (lane == 0) s_sum[warp] = c;
+  if ((threadIdx.x & 31) == 0) s_sum[threadIdx.x >> 5] = c;
   __syncthreads();
-  if (tid == 0) {
-    int b = 0;
-    for (int w = 0; w < kPackThreads / 32; ++w) b += s_sum[w];
-    s_base = b;
+  c = 0;
+#pragma unroll
+  for (int w = 0; w < kPackWarps; ++w) c += s_sum[w];
+  return c;
+}
+// Each CTA packs `rows` consecutive rows: it counts the kept rows before its
+// own in the labels (a prefix of them, read again by every CTA), then copies,
+// a warp a row.  The last kPackZero CTAs count them all and fill up to the next
+// multiple of 64 rows, the step of d_weight's sum, with zeros.
+__global__ void __launch_bounds__(kPackThreads) head_pack_kernel(const HeadLossArgs a, int rows, int row_ctas) {
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  if ((int)blockIdx.x >= row_ctas) {
+    const int z = blockIdx.x - row_ctas, n = count_kept(a, a.R);
+    const int end = max(1, (n + 63) / 64) * 64;
+    if (z == 0 && tid == 0) *a.n = n;
+    for (int p = n + z * kPackWarps + warp; p < end; p += kPackZero * kPackWarps) {
+      uint4* dst = reinterpret_cast<uint4*>(a.packed + (size_t)p * a.d);
+      for (int j = lane; j < a.d / 8; j += 32) dst[j] = make_uint4(0, 0, 0, 0);
+    }
+    return;
   }
-  __syncthreads();
-  int base = s_base;
-  // one warp a row, in turn
-  for (int r = r0; r < r1; r += kPackThreads / 32) {
+  const int r0 = blockIdx.x * rows, r1 = min(a.R, r0 + rows);
+  int base = count_kept(a, r0);
+  for (int r = r0; r < r1; r += kPackWarps) {
     // every warp knows the places of the group's rows
     const int mine = r + lane;
-    const int label = lane < kPackThreads / 32 && mine < r1 ? a.labels[mine] : a.ignore;
-    const bool in = lane < kPackThreads / 32 && mine < r1;
+    const bool in = lane < kPackWarps && mine < r1;
+    const int label = in ? a.labels[mine] : a.ignore;
     const unsigned k = __ballot_sync(kFull, in && kept(a, label));
     if (warp == 0 && in) {
       const bool keep = (k >> lane) & 1u;
@@ -54,6 +67,7 @@ __global__ void __launch_bounds__(kPackThreads) head_pack_kernel(const HeadLossA
       a.pos[mine] = keep ? p : -1;
       if (keep) {
         a.lab[p] = label;
+        a.row[p] = mine;
         if (a.plse) {
           a.plse[p] = a.lse_in[mine];
           a.pgrad[p] = a.grad[mine];
@@ -67,22 +81,10 @@ __global__ void __launch_bounds__(kPackThreads) head_pack_kernel(const HeadLossA
       const int p = base + __popc(k & ((1u << warp) - 1u));
       const uint4* src = reinterpret_cast<const uint4*>(a.hidden + (size_t)row * a.d);
       uint4* dst = reinterpret_cast<uint4*>(a.packed + (size_t)p * a.d);
+#pragma unroll 4
       for (int j = lane; j < a.d / 8; j += 32) dst[j] = src[j];
     }
     base += __popc(k);
-  }
-  if (r1 == a.R) {
-    if (tid == 0) *a.n = base;
-    const int end = min(a.Rp, max(1, (base + kHeadTile - 1) / kHeadTile) * kHeadTile);
-    const size_t from = (size_t)base * a.d / 8, to = (size_t)end * a.d / 8;
-    for (size_t j = from + tid; j < to; j += kPackThreads) reinterpret_cast<uint4*>(a.packed)[j] = make_uint4(0, 0, 0, 0);
-    for (int p = base + tid; p < end; p += kPackThreads) {
-      a.lab[p] = -1;
-      if (a.plse) {
-        a.plse[p] = 0.f;
-        a.pgrad[p] = 0.f;
-      }
-    }
   }
 }
 
@@ -445,54 +447,104 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
 }
 
 // ---- a row's tiles merged -----------------------------------------------------------
-__global__ void __launch_bounds__(256) head_merge_kernel(const HeadLossArgs a, int parts) {
-  const int lane = threadIdx.x & 31;
-  const int r = blockIdx.x * 8 + (threadIdx.x >> 5);
-  if (r >= a.R) return;
-  const int p = a.pos[r];
-  float lse = 0.f, loss = 0.f;
-  if (p >= 0) {
-    float m = -pos_inf(), s = 0.f;
-    for (int t = lane; t < parts; t += 32) {
-      const float2 x = a.part[(size_t)t * a.Rp + p];
-      const float mm = fmaxf(m, x.x);
-      s = s * ex2(m - mm) + x.y * ex2(x.x - mm);
-      m = mm;
-    }
-    for (int o = 16; o; o >>= 1) {
-      const float m2 = __shfl_xor_sync(kFull, m, o), s2 = __shfl_xor_sync(kFull, s, o);
-      const float mm = fmaxf(m, m2);
-      s = (s > 0.f ? s * ex2(m - mm) : 0.f) + (s2 > 0.f ? s2 * ex2(m2 - mm) : 0.f);
-      m = mm;
-    }
-    lse = m * kLn2 + logf(s);
-    loss = lse - a.zlab[p];
+// Four rows a CTA (32 bytes of each tile's statistics), 64 tiles at a time.
+constexpr int kMergeThreads = 256;
+__device__ __forceinline__ void fold(float& m, float& s, float m2, float s2) {
+  const float mm = fmaxf(m, m2);
+  s = (s > 0.f ? s * ex2(m - mm) : 0.f) + (s2 > 0.f ? s2 * ex2(m2 - mm) : 0.f);
+  m = mm;
+}
+__global__ void __launch_bounds__(kMergeThreads) head_merge_kernel(const HeadLossArgs a, int parts) {
+  __shared__ float s_m[kMergeThreads / 32][4], s_s[kMergeThreads / 32][4];
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  const int n = *a.n, p = blockIdx.x * 4 + (tid & 3);
+  // ignored rows (each CTA sees to four rows of either kind)
+  if (tid < 4 && p < a.R && a.pos[p] < 0) {
+    a.lse[p] = 0.f;
+    if (a.loss) a.loss[p] = 0.f;
   }
-  if (lane == 0) {
+  if ((int)blockIdx.x * 4 >= n) return;
+  float m = -pos_inf(), s = 0.f;
+  if (p < n) {
+    constexpr int kBatch = 8;
+    for (int t0 = tid >> 2; t0 < parts; t0 += kBatch * (kMergeThreads / 4)) {
+      float2 x[kBatch];
+#pragma unroll
+      for (int j = 0; j < kBatch; ++j) {
+        const int t = t0 + j * (kMergeThreads / 4);
+        x[j] = t < parts ? __ldcg(a.part + (size_t)t * a.Rp + p) : make_float2(-pos_inf(), 0.f);
+      }
+      float mm = m;
+#pragma unroll
+      for (int j = 0; j < kBatch; ++j) mm = fmaxf(mm, x[j].x);
+      s = s > 0.f ? s * ex2(m - mm) : 0.f;
+#pragma unroll
+      for (int j = 0; j < kBatch; ++j) s += x[j].y * ex2(x[j].x - mm);
+      m = mm;
+    }
+  }
+#pragma unroll
+  for (int o = 16; o >= 4; o >>= 1) fold(m, s, __shfl_xor_sync(kFull, m, o), __shfl_xor_sync(kFull, s, o));
+  if (lane < 4) {
+    s_m[warp][lane] = m;
+    s_s[warp][lane] = s;
+  }
+  __syncthreads();
+  if (tid < 4 && p < n) {
+#pragma unroll
+    for (int w = 1; w < kMergeThreads / 32; ++w) fold(m, s, s_m[w][tid], s_s[w][tid]);
+    const float lse = m * kLn2 + logf(s);
+    const int r = a.row[p];
     a.lse[r] = lse;
-    if (a.loss) a.loss[r] = loss;
+    if (a.loss) a.loss[r] = lse - a.zlab[p];
   }
 }
 
 // ---- the hidden states' gradient, rounded and put back in place -------------------
 __global__ void __launch_bounds__(256) head_unpack_kernel(const HeadLossArgs a) {
-  const int lane = threadIdx.x & 31;
-  const int r = blockIdx.x * 8 + (threadIdx.x >> 5);
-  if (r >= a.R) return;
-  const int p = a.pos[r];
-  for (int j = lane; j < a.d; j += 32) {
-    float x = 0.f;
-    if (p >= 0)
-      for (int k = 0; k < a.split; ++k) x += a.dh[((size_t)k * a.Rp + p) * a.d + j];
-    a.d_hidden[(size_t)r * a.d + j] = to_bf(x);
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  const int per = a.d / 4;                           // four columns a thread
+  const size_t total = (size_t)a.R * per, step = (size_t)a.Rp * a.d;
+  for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (size_t)gridDim.x * 256) {
+    const int r = (int)(i / per), j = (int)(i - (size_t)r * per) * 4;
+    const int p = a.pos[r];
+    float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (p >= 0) {
+      const float* src = a.dh + (size_t)p * a.d + j;
+#pragma unroll 8
+      for (int k = 0; k < a.split; ++k) {
+        const float4 y = __ldcg(reinterpret_cast<const float4*>(src + k * step));
+        x = make_float4(x.x + y.x, x.y + y.y, x.z + y.z, x.w + y.w);
+      }
+    }
+    *reinterpret_cast<uint2*>(a.d_hidden + (size_t)r * a.d + j) = make_uint2(pack_bf(x.x, x.y), pack_bf(x.z, x.w));
   }
 }
 
 unsigned tiles(int64_t n, int t) { return (unsigned)((n + t - 1) / t); }
+// a launch that may begin before what precedes it on the stream has ended
+template <typename... P, typename... A>
+cudaError_t launch_early(void (*kernel)(P...), unsigned grid, unsigned threads, size_t smem, cudaStream_t s, A... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(grid);
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = s;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
 cudaError_t launch_pack(const HeadLossArgs& a, cudaStream_t s) {
-  int rows = 16;
+  int rows = kPackWarps;
   while ((int64_t)rows * 1024 < a.R) rows *= 2;
-  head_pack_kernel<<<tiles(a.R, rows), kPackThreads, 0, s>>>(a, rows);
+  const int ctas = (int)tiles(a.R, rows);
+  head_pack_kernel<<<ctas + kPackZero, kPackThreads, 0, s>>>(a, rows, ctas);
   return cudaGetLastError();
 }
 
@@ -524,27 +576,28 @@ cudaError_t launch_pairs(const HeadLossArgs& a, int v0, int vlen, int first, int
   }
   int64_t pairs = sms / 2 > 0 ? sms / 2 : 1;
   if (pairs > most) pairs = most;
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)(2 * pairs));
-  cfg.blockDim = dim3(kPairThreads);
-  cfg.dynamicSmemBytes = kPairSmem;
-  cfg.stream = s;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, head_pair_kernel<OP>, a, v0, vlen, first, maps);
+  return launch_early(head_pair_kernel<OP>, (unsigned)(2 * pairs), kPairThreads, kPairSmem, s, a, v0, vlen, first, maps);
 }
 }  // namespace
 
-// Parts that d_hidden's sum over a piece is cut into, so that about as many
-// tiles as pairs of SMs exist; a part has at least four blocks of 64.
+// Parts that d_hidden's sum over a piece is cut into, so that its tiles fill the
+// pairs of SMs: the least of rounds / parts, each part charged for its sums' way
+// through memory (8 bytes a sum and piece at 5 TB/s, against 2 Vc operations at
+// 1.7 PFLOP/s).  R=4096 d=2048 V=128256, both gradients: one part 2.96 ms, four
+// 3.07.  A part has at least four blocks of 64.
 int head_split(int Rp, int d, int Vc) {
   const int64_t t = (int64_t)(Rp / kPairTile) * ((d + kPairTile - 1) / kPairTile);
-  int64_t s = 76 / t;
-  if (s > Vc / 256) s = Vc / 256;
-  return s < 1 ? 1 : (int)s;
+  const int most = Vc / 256 < 32 ? Vc / 256 : 32;
+  int best = 1;
+  double least = 0.0;
+  for (int k = 1; k <= most; ++k) {
+    const double cost = (double)((t * k + 75) / 76) / k * (1.0 + 1400.0 / Vc * k);
+    if (k == 1 || cost < least) {
+      best = k;
+      least = cost;
+    }
+  }
+  return best;
 }
 
 cudaError_t launch_head_loss(const HeadLossArgs& a, cudaStream_t s) {
@@ -554,8 +607,7 @@ cudaError_t launch_head_loss(const HeadLossArgs& a, cudaStream_t s) {
   if (e != cudaSuccess) return e;
   e = launch_pairs<kOpStats>(a, 0, a.V, 1, (int64_t)(a.Rp / kPairTile) * tiles(a.V, kPairTile), maps, s);
   if (e != cudaSuccess) return e;
-  head_merge_kernel<<<tiles(a.R, 8), 256, 0, s>>>(a, (int)tiles(a.V, kHeadPart));
-  return cudaGetLastError();
+  return launch_early(head_merge_kernel, tiles(a.R, 4), kMergeThreads, 0, s, a, (int)tiles(a.V, kHeadPart));
 }
 
 cudaError_t launch_head_loss_backward(const HeadLossArgs& a, cudaStream_t s) {
@@ -573,8 +625,9 @@ cudaError_t launch_head_loss_backward(const HeadLossArgs& a, cudaStream_t s) {
     e = launch_pairs<kOpGrad>(a, (int)v0, vlen, v0 == 0, most, maps, s);
     if (e != cudaSuccess) return e;
   }
-  if (a.d_hidden) head_unpack_kernel<<<tiles(a.R, 8), 256, 0, s>>>(a);
-  return cudaGetLastError();
+  if (!a.d_hidden) return cudaSuccess;
+  const int64_t n4 = (int64_t)a.R * (a.d / 4);
+  return launch_early(head_unpack_kernel, tiles(n4 < 256 * 8192 ? n4 : 256 * 8192, 256), 256, 0, s, a);
 }
 
 }  // namespace cmsd
