@@ -653,10 +653,11 @@ size_t loss_layout(HeadLossArgs& a, bool backward, char* w) {
   return o;
 }
 size_t i8_layout(HeadI8Args& a, char* w) {
-  const size_t h = up((size_t)(a.R > 0 ? a.R : 1) * a.d * 2);
+  const size_t R = a.R > 0 ? a.R : 1, h = up(R * a.d * 2);
   a.err = (unsigned*)w;
   a.h16 = (uint16_t*)(w ? w + kAlign : nullptr);
-  return kAlign + h;
+  a.mag = (int*)(w ? w + kAlign + h : nullptr);
+  return kAlign + h + up(R * 4);
 }
 int check_lmhead(int R, int d, int V) {
   if (R < 0 || d < 64 || d % 64 != 0 || d > (1 << 20) || V < 2) return CMSD_EINVAL;

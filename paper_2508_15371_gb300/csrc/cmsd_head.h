@@ -53,6 +53,7 @@ struct HeadI8Args {
   void* logits;                  // dtype [R][V]
   unsigned* err;
   uint16_t* h16;                 // fp16 [R][d]: the hidden integers as the tensor cores take them
+  int* mag;                      // [R] sum of each token's magnitudes
 };
 cudaError_t launch_quantize_rows(const void* x, int dtype, int R, int d, int8_t* q, float* scale, cudaStream_t s);
 cudaError_t launch_head_i8(const HeadI8Args& a, cudaStream_t s);

@@ -225,10 +225,13 @@ cudaError_t launch_quantize(const T* x, int R, int d, int8_t* q, float* scale, c
 // ---- the product ----------------------------------------------------------------
 //
 // A whole number of 8 bits is exact in fp16, its products are exact in the
-// tensor cores and their sums exact in fp32 up to 2^24: 1024 products of at
-// most 2^14.  So the integers go through the fp16 tensor cores (GB300's integer
-// tensor rate is far below), and the sums of each 1024 entries of K are added
-// up as 32-bit integers.  Only the 8-bit weight is read from memory; its bytes
+// tensor cores and their sums exact in fp32 up to 2^24.  So the integers go
+// through the fp16 tensor cores (GB300's integer tensor rate is far below).
+// Where every token of a tile has magnitudes that add up to at most 2^17, as
+// rows scaled by their largest do up to a few thousand entries, no sum with
+// 8-bit weights passes 2^24 and all of K is summed by the tensor cores; else the
+// sums of each 1024 entries (of products of at most 2^14) are added up as 32-bit
+// integers.  Either way the sum is exact.  Only the 8-bit weight is read from memory; its bytes
 // become fp16 on their way into tensor memory, where the MMA takes its A from:
 // byte + 128 is placed into the low mantissa bits of 1024.0, and 1152 is
 // subtracted, both exact.
@@ -264,20 +267,58 @@ struct I8Plan {
   int vt, rt;            // tiles of the vocabulary and of the tokens
 };
 
-__global__ void __launch_bounds__(256) head_i8_tokens_kernel(const HeadI8Args a) {
+// the tokens as fp16, and the sum of each one's magnitudes; a CTA a token
+constexpr int kTokenThreads = 128;
+__global__ void __launch_bounds__(kTokenThreads) head_i8_tokens_kernel(const HeadI8Args a) {
+  __shared__ int s_sum[kTokenThreads / 32];
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  const size_t n = (size_t)a.R * a.d / 16;
-  for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (size_t)gridDim.x * 256) {
-    const uint4 x = reinterpret_cast<const uint4*>(a.hidden)[i];
-    uint32_t h[8];
-    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+  const int tid = threadIdx.x, vecs = a.d / 16;
+  for (int r = blockIdx.x; r < a.R; r += gridDim.x) {
+    const uint4* src = reinterpret_cast<const uint4*>(a.hidden + (size_t)r * a.d);
+    uint4* dst = reinterpret_cast<uint4*>(a.h16 + (size_t)r * a.d);
+    unsigned sum = 0;
+    for (int i = tid; i < vecs; i += kTokenThreads) {
+      const uint4 x = src[i];
+      uint32_t h[8];
+      const uint32_t w[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
-    for (int k = 0; k < 4; ++k) i8_to_half(w[k], h[2 * k], h[2 * k + 1]);
-    uint4* dst = reinterpret_cast<uint4*>(a.h16) + 2 * i;
-    dst[0] = make_uint4(h[0], h[1], h[2], h[3]);
-    dst[1] = make_uint4(h[4], h[5], h[6], h[7]);
+      for (int k = 0; k < 4; ++k) {
+        i8_to_half(w[k], h[2 * k], h[2 * k + 1]);
+        sum = __dp4a(__vabsdiffs4(w[k], 0u), 0x01010101u, sum);   // (|-128| is 128)
+      }
+      dst[2 * i] = make_uint4(h[0], h[1], h[2], h[3]);
+      dst[2 * i + 1] = make_uint4(h[4], h[5], h[6], h[7]);
+    }
+    sum = __reduce_add_sync(kFull, sum);
+    if ((tid & 31) == 0) s_sum[tid >> 5] = (int)sum;
+    __syncthreads();
+    if (tid == 0) {
+      int all = 0;
+#pragma unroll
+      for (int w = 0; w < kTokenThreads / 32; ++w) all += s_sum[w];
+      a.mag[r] = all;
+    }
+    __syncthreads();
   }
 }
+
+// Whether a tile of tokens needs the sums of each 1024 entries apart.  The
+// magnitudes are requested a tile ahead; tiles of one round of tokens are alike.
+struct I8Span {
+  int m[4];
+  __device__ __forceinline__ void request(const HeadI8Args& a, const I8Plan& p, int t) {
+    const int r0 = t % p.rt * p.cols, lane = threadIdx.x & 31;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int n = lane + 32 * i;
+      m[i] = n < p.cols && r0 + n < a.R ? __ldcg(a.mag + r0 + n) : 0;
+    }
+  }
+  __device__ __forceinline__ int stages(int ks) const {            // per sum
+    const int most = __reduce_max_sync(kFull, max(max(m[0], m[1]), max(m[2], m[3])));
+    return most <= (1 << 17) ? ks : min(kI8Exact, ks);
+  }
+};
 
 template <int NT, bool kBf16>
 __global__ void __launch_bounds__(kI8Threads, 1)
@@ -359,17 +400,23 @@ __global__ void __launch_bounds__(kI8Threads, 1)
     const uint32_t idesc = mma_idesc(128, p.cols, false, false, false);
     const uint32_t half = (uint32_t)p.cols * 128 >> 4;       // the second 64 of K, in units of 16 bytes
     int c = 0, s = 0, k = 0;                        // sums handed over; ring slot; stage of the tile
+    int part = 0, t = (int)blockIdx.x;              // stage of the sum; tile
     uint32_t phase = 0;
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    I8Span span;
+    span.request(a, p, t);
+    int len = span.stages(ks);
     for (int g = 0; g < G; ++g) {
       const int b = g & 1;
-      const uint32_t more = k % kI8Exact != 0;
+      const uint32_t more = part != 0;
+      if (k == 0) span.request(a, p, t + (int)gridDim.x);
       if (!more && c > 0 && ok) ok = bar_wait<false>(dempty, (uint32_t)((c - 1) & 1));
       if (ok) ok = bar_wait<false>(full + 8 * s, phase);
       if (ok) ok = bar_wait<false>(afull + 8 * b, (uint32_t)((g / 2) & 1));
       tmem_fence_after();
       const uint64_t h0 = mma_desc(base + s * S::kStage + kI8WStage, 0), h1 = h0 + half;
       const uint32_t at = abase + b * 128;
-      const bool ends = k % kI8Exact == kI8Exact - 1 || k == ks - 1;
+      const bool ends = part == len - 1 || k == ks - 1;
       if (leader) {
 #pragma unroll
         for (int sub = 0; sub < 2; ++sub) {
@@ -386,7 +433,12 @@ __global__ void __launch_bounds__(kI8Threads, 1)
       }
       __syncwarp();
       c += ends;
-      if (++k == ks) k = 0;
+      part = ends ? 0 : part + 1;
+      if (++k == ks) {
+        k = 0;
+        t += (int)gridDim.x;
+        len = span.stages(ks);
+      }
       if (++s == kStages) {
         s = 0;
         phase ^= 1;
@@ -403,10 +455,11 @@ __global__ void __launch_bounds__(kI8Threads, 1)
 #pragma unroll
     for (int n = 0; n < 16 * kMine; ++n) acc[n] = 0;
     int c = 0, tile = 0;                            // sums read so far; tiles done
-    int end = min(kI8Exact, ks) - 1;                // the stage whose sums are read next
+    int len = 0, end = 0;                           // stages per sum; the stage whose sums are read next
+    I8Span span;
     // reads the sums that end at stage `end`, and scales and writes a tile's last
     auto read_sums = [&]() {
-      const bool last = end == (tile + 1) * ks - 1;
+      const bool last = end == (tile + 1) * ks - 1, whole = len == ks;
       const int t = (int)blockIdx.x + tile * (int)gridDim.x;
       const int vi = t / p.rt, r0 = (t - vi * p.rt) * p.cols, v = vi * p.height + row;
       const bool mine = last && row < p.height && v < a.V;
@@ -415,6 +468,7 @@ __global__ void __launch_bounds__(kI8Threads, 1)
 #pragma unroll
         for (int i = 0; i < (NT + 31) / 32; ++i) hs[i] = __ldg(a.hidden_scale + min(r0 + 32 * i + lane, a.R - 1));
         if (mine) ws = __ldg(a.weight_scale + v);
+        span.request(a, p, t + (int)gridDim.x);
       }
       if (ok) ok = bar_wait<false>(dfull, (uint32_t)(c & 1));
       ++c;
@@ -427,15 +481,23 @@ __global__ void __launch_bounds__(kI8Threads, 1)
           float z[16];
           tmem_ld16_ahead(src + 32 * i, z);
           tmem_ld_wait(z);
+          if (whole) {
 #pragma unroll
-          for (int j = 0; j < 16; ++j) acc[16 * i + j] += __float2int_rn(z[j]);
+            for (int j = 0; j < 16; ++j) acc[16 * i + j] = __float_as_int(z[j]);
+          } else {
+#pragma unroll
+            for (int j = 0; j < 16; ++j) acc[16 * i + j] += __float2int_rn(z[j]);
+          }
         }
       }
       tmem_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive_local(dempty);
       if (last) {
-        if (tile == 0) asm volatile("griddepcontrol.wait;" ::: "memory");   // (what precedes this grid may still use them)
+        if (!whole) {
+#pragma unroll
+          for (int n = 0; n < 16 * kMine; ++n) acc[n] = __float_as_int((float)acc[n]);
+        }
         char* out = reinterpret_cast<char*>(a.logits) + ((size_t)(r0 + 16 * set) * a.V + v) * (kBf16 ? 2 : 4);
         const size_t step = (size_t)a.V * (kBf16 ? 2 : 4);
         const int rows = mine ? min(a.R - r0, p.cols) - 16 * set : 0;       // of this set's first group on
@@ -445,7 +507,7 @@ __global__ void __launch_bounds__(kI8Threads, 1)
           for (int j = 0; j < 16; ++j) {
             const float h = __shfl_sync(kFull, hs[i], 16 * set + j);
             if (32 * i + j < rows) {
-              const float z = (float)acc[16 * i + j] * h * ws;
+              const float z = __int_as_float(acc[16 * i + j]) * h * ws;
               if (kBf16)
                 *reinterpret_cast<__nv_bfloat16*>(out) = __float2bfloat16_rn(z);
               else
@@ -457,15 +519,16 @@ __global__ void __launch_bounds__(kI8Threads, 1)
           out += 16 * step;
         }
         ++tile;
+        len = span.stages(ks);
       }
-      end = last ? tile * ks + min(kI8Exact, ks) - 1 : min(end + kI8Exact, (tile + 1) * ks - 1);
+      end = last ? tile * ks + len - 1 : min(end + len, (tile + 1) * ks - 1);
     };
     // Sums that ended at this set's last stage or before are read first: the
     // MMAs wait for it.  What ended at the other set's is read after this set's
     // next stage has been turned, which the MMAs want at once then.
     bool turned = false;
     for (int g = set; g < G + 2;) {
-      if (end < (turned ? g : g - 1) && end < G) {
+      if (end < (turned ? g : g - 1) && end < G && len > 0) {
         read_sums();
         continue;
       }
@@ -504,6 +567,12 @@ __global__ void __launch_bounds__(kI8Threads, 1)
         tmem_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive_local(afull + 8 * set);
+      }
+      if (len == 0) {                               // the first stage did not wait for the tokens' kernel
+        asm volatile("griddepcontrol.wait;" ::: "memory");
+        span.request(a, p, (int)blockIdx.x);
+        len = span.stages(ks);
+        end = len - 1;
       }
     }
   }
@@ -574,11 +643,11 @@ cudaError_t launch_head_i8(const HeadI8Args& a, cudaStream_t s) {
   if (!tma_matrix(&mw, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, a.weight, a.d, a.V, p.height) ||
       !tma_matrix(&mh, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, a.h16, a.d, a.R, p.cols))
     return cudaErrorInvalidValue;
-  const int64_t n16 = (int64_t)a.R * a.d / 16;
-  head_i8_tokens_kernel<<<(unsigned)(n16 < 256 * 2048 ? (n16 + 255) / 256 : 2048), 256, 0, s>>>(a);
+  head_i8_tokens_kernel<<<a.R < 65536 ? a.R : 65536, kTokenThreads, 0, s>>>(a);
   e = cudaGetLastError();
   if (e != cudaSuccess) return e;
   const int64_t tiles = (int64_t)p.vt * p.rt;
+  if (tiles + sms >= (1ll << 31)) return cudaErrorInvalidValue;     // (64 TB of logits)
   const int grid = tiles < sms ? (int)tiles : sms;
   return a.dtype == 0 ? launch_i8_cols<false>(a, p, grid, dev, mw, mh, s) : launch_i8_cols<true>(a, p, grid, dev, mw, mh, s);
 }

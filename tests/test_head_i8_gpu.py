@@ -139,6 +139,21 @@ def test_largest_sums(cmsd, d):
     _same(cmsd.lmhead_i8(hq, one, wq, onev, dtype=torch.float32)["logits"], _logits(hq, one, wq, onev, torch.float32))
 
 
+@pytest.mark.parametrize("R,d,V", [(300, 2576, 1500), (40, 1536, 40000), (129, 8192, 700)])
+def test_large_tokens_among_small_ones(cmsd, R, d, V):
+    """Tokens whose magnitudes add up to more than 2^17, just to it, and to less, in one tile and in others."""
+    hq, wq = _ints(R, d, 9), _ints(V, d, 10, full=True)
+    hq.clamp_(-30, 30)
+    hq[R // 2] = 127
+    hq[R - 1] = 0
+    hq[R - 1, :1024] = -128                          # 2^17 exactly
+    hq[R // 3] = hq[R - 1]
+    hq[R // 3, 1024] = 1
+    hs, wsc = torch.rand(R, device="cuda"), torch.rand(V, device="cuda")
+    wq[3], wq[V - 1] = -128, 127
+    _same(cmsd.lmhead_i8(hq, hs, wq, wsc, dtype=torch.float32)["logits"], _logits(hq, hs, wq, wsc, torch.float32))
+
+
 def test_scales_of_any_kind(cmsd):
     """Zeros, infinities and NaN in the scales show in their rows and columns alone."""
     R, d, V = 20, 64, 300
