@@ -239,26 +239,34 @@ cudaError_t launch_quantize(const T* x, int R, int d, int8_t* q, float* scale, c
 // The MMA's M is the vocabulary (a tile of up to 256 entries: two accumulators
 // of 128 lanes) and its N the tokens (up to 128), so the weight, the large
 // operand, passes through registers once, and B's tile serves both accumulators.
-//   warp 0      lane 0 fills the ring: 128 bytes of K of the tile's weight rows,
-//               and the same K of the tokens (fp16, from the workspace);
+//   warp 0      lane 0 fills a ring with 128 bytes of K of the tile's weight rows;
+//   warp 18     lane 0 another with the tokens' (fp16, from the workspace);
 //   warp 1      lane 0 issues the MMAs;
 //   warps 2..17 two sets of eight, thread = one vocabulary entry: a set turns
-//               its rows of every second stage into fp16 in its own buffer, and
-//               adds up and scales every second group of 16 tokens.
-// Barriers: full (TMA -> fp16 and MMA), afull / aempty (fp16 <-> MMA, two
-// buffers in tensor memory), empty (MMA -> TMA), dfull / dempty (MMA <-> sums).
+//               its half of each stage's K into fp16, and adds up and scales
+//               every second group of 16 tokens.
+// Barriers: wfull / wempty (TMA <-> fp16), hfull / hempty (TMA <-> MMA), afull /
+// aempty (fp16 <-> MMA, two buffers in tensor memory for each half), dfull /
+// dempty (MMA <-> sums; two sets of accumulators where a tile has at most 64
+// tokens).
 // Every wait is bounded.
 constexpr int kI8Tile = 256;                        // vocabulary entries per tile at most
 constexpr int kI8K = 128;                           // K per stage
 constexpr int kI8Exact = 1024 / kI8K;               // stages whose sums are exact in fp32
-constexpr int kI8Threads = 64 + 2 * kI8Tile;
+constexpr int kI8Threads = 96 + 2 * kI8Tile;
 constexpr int kI8WStage = kI8Tile * kI8K;
 template <int NT>
 struct I8Shape {
   static constexpr int kHStage = NT * kI8K * 2;
-  static constexpr int kStage = kI8WStage + kHStage;
-  static constexpr int kStages = NT == 128 ? 3 : (NT == 64 ? 4 : 5);
-  static constexpr size_t kSmem = 1024 + (size_t)kStages * kStage + 8 * (2 * kStages + 6) + 16;
+  // a stage of the weight is free again as soon as it has been turned, one of
+  // the tokens only after its MMAs: rings of their own keep more of the weight
+  // in flight
+  static constexpr int kW = NT == 128 ? 3 : (NT == 64 ? 4 : 5);
+  static constexpr int kH = NT == 128 ? 3 : (NT == 64 ? 5 : (NT == 32 ? 6 : 8));
+  static constexpr int kSums = NT <= 64 ? 2 : 1;    // sets of accumulators
+  static constexpr int kBars = 2 * kW + 2 * kH + 12;
+  static constexpr size_t kStageBytes = (size_t)kW * kI8WStage + (size_t)kH * kHStage;
+  static constexpr size_t kSmem = 1024 + kStageBytes + 8 * kBars + 16;
   static_assert(kSmem <= 227 * 1024, "shared memory");
 };
 struct I8Plan {
@@ -325,26 +333,33 @@ __global__ void __launch_bounds__(kI8Threads, 1)
     head_i8_kernel(const HeadI8Args a, const I8Plan p, const __grid_constant__ CUtensorMap map_w,
                    const __grid_constant__ CUtensorMap map_h) {
   using S = I8Shape<NT>;
-  constexpr int kStages = S::kStages;
   extern __shared__ __align__(1024) unsigned char i8_smem[];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const uint32_t raw = smem_addr(i8_smem);
-  const uint32_t base = (raw + 1023u) & ~1023u;
-  const uint32_t bars = base + kStages * S::kStage;
-  const uint32_t full = bars, empty = bars + 8 * kStages, afull = bars + 16 * kStages, aempty = afull + 16;
-  const uint32_t dfull = afull + 32, dempty = afull + 40;
-  uint32_t* s_taddr = reinterpret_cast<uint32_t*>(i8_smem + (bars - raw) + 8 * (2 * kStages + 6));
+  const uint32_t base = (raw + 1023u) & ~1023u, hbase = base + S::kW * kI8WStage;
+  const uint32_t bars = base + (uint32_t)S::kStageBytes;
+  const uint32_t wfull = bars, wempty = wfull + 8 * S::kW;
+  const uint32_t hfull = wempty + 8 * S::kW, hempty = hfull + 8 * S::kH;
+  const uint32_t afull = hempty + 8 * S::kH, aempty = afull + 32;    // [half][buffer]
+  const uint32_t dfull = aempty + 32, dempty = dfull + 16;
+  uint32_t* s_taddr = reinterpret_cast<uint32_t*>(i8_smem + (bars - raw) + 8 * S::kBars);
   if (tid == 0) {
-    for (int k = 0; k < kStages; ++k) {
-      mbar_init(full + 8 * k, 1);
-      mbar_init(empty + 8 * k, 1);
+    for (int k = 0; k < S::kW; ++k) {
+      mbar_init(wfull + 8 * k, 1);
+      mbar_init(wempty + 8 * k, 2 * kI8Tile / 32);
     }
-    for (int b = 0; b < 2; ++b) {
+    for (int k = 0; k < S::kH; ++k) {
+      mbar_init(hfull + 8 * k, 1);
+      mbar_init(hempty + 8 * k, 1);
+    }
+    for (int b = 0; b < 4; ++b) {
       mbar_init(afull + 8 * b, kI8Tile / 32);
       mbar_init(aempty + 8 * b, 1);
     }
-    mbar_init(dfull, 1);
-    mbar_init(dempty, 2 * kI8Tile / 32);
+    for (int b = 0; b < 2; ++b) {
+      mbar_init(dfull + 8 * b, 1);
+      mbar_init(dempty + 8 * b, 2 * kI8Tile / 32);
+    }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == 1) {
@@ -357,7 +372,8 @@ __global__ void __launch_bounds__(kI8Threads, 1)
   __syncthreads();
   tmem_fence_after();
   const uint32_t tbase = *s_taddr;
-  const uint32_t abase = tbase + 256;               // two buffers of two blocks of 64 columns
+  const uint32_t abase = tbase + 256;               // [half][buffer][128 entries] of 32 columns
+  constexpr int kSubCols = 128 / S::kSums;          // columns of an accumulator
   const int ks = (a.d + kI8K - 1) / kI8K;           // stages per tile
   const int tiles = p.vt * p.rt;
   const int mine = tiles > (int)blockIdx.x ? (tiles - (int)blockIdx.x + (int)gridDim.x - 1) / (int)gridDim.x : 0;
@@ -365,33 +381,43 @@ __global__ void __launch_bounds__(kI8Threads, 1)
   bool ok = true;
 
   if (warp == 0) {
+    // The weight does not wait for the tokens' kernel: that one has started, so
+    // what precedes it on the stream has ended.
     if (lane == 0) {
-      const uint32_t bytes = (uint32_t)(p.height * kI8K + p.cols * kI8K * 2);
-      // the weight's first stages do not wait for the tokens' kernel: it has
-      // started, so what precedes it on the stream has ended
-      int issued = G < kStages ? G : kStages;
-      for (int g = 0; g < issued; ++g) {
-        const int t = (int)blockIdx.x + g / ks * (int)gridDim.x;
-        mbar_arrive_tx(full + 8 * g, bytes);
-        tma_box(base + g * S::kStage, &map_w, g % ks * kI8K, t / p.rt * p.height, full + 8 * g);
-      }
-      asm volatile("griddepcontrol.wait;" ::: "memory");
-      asm volatile("fence.proxy.async.global;" ::: "memory");
-      for (int g = 0; g < G; ++g) {
-        const int s = g % kStages, t = (int)blockIdx.x + g / ks * (int)gridDim.x, k = g % ks * kI8K;
-        const int v = t / p.rt, r = t - v * p.rt;
-        const uint32_t dst = base + s * S::kStage;
-        if (g >= kStages) {
-          if (ok) ok = bar_wait<false>(empty + 8 * s, (uint32_t)((g / kStages - 1) & 1));
-          mbar_arrive_tx(full + 8 * s, bytes);
-          tma_box(dst, &map_w, k, v * p.height, full + 8 * s);
+      const uint32_t bytes = (uint32_t)(p.height * kI8K);
+      int g = 0;
+      for (int i = 0; i < mine; ++i) {
+        const int y = ((int)blockIdx.x + i * (int)gridDim.x) / p.rt * p.height;
+        for (int k = 0; k < ks; ++k, ++g) {
+          const int s = g % S::kW;
+          if (g >= S::kW && ok) ok = bar_wait<false>(wempty + 8 * s, (uint32_t)((g / S::kW - 1) & 1));
+          mbar_arrive_tx(wfull + 8 * s, bytes);
+          tma_box(base + s * kI8WStage, &map_w, k * kI8K, y, wfull + 8 * s);
         }
-        tma_box(dst + kI8WStage, &map_h, k, r * p.cols, full + 8 * s);
-        tma_box(dst + kI8WStage + p.cols * 128, &map_h, k + 64, r * p.cols, full + 8 * s);
       }
       // nothing is in flight into this CTA when it ends
-      for (int g = (G > kStages ? G - kStages : 0); g < G; ++g)
-        if (ok) ok = bar_wait<false>(empty + 8 * (g % kStages), (uint32_t)((g / kStages) & 1));
+      for (int k = (g > S::kW ? g - S::kW : 0); k < g; ++k)
+        if (ok) ok = bar_wait<false>(wempty + 8 * (k % S::kW), (uint32_t)((k / S::kW) & 1));
+    }
+  } else if (warp == 18) {
+    if (lane == 0) {
+      const uint32_t bytes = (uint32_t)(p.cols * kI8K * 2);
+      asm volatile("griddepcontrol.wait;" ::: "memory");
+      asm volatile("fence.proxy.async.global;" ::: "memory");
+      int g = 0;
+      for (int i = 0; i < mine; ++i) {
+        const int y = ((int)blockIdx.x + i * (int)gridDim.x) % p.rt * p.cols;
+        for (int k = 0; k < ks; ++k, ++g) {
+          const int s = g % S::kH;
+          if (g >= S::kH && ok) ok = bar_wait<false>(hempty + 8 * s, (uint32_t)((g / S::kH - 1) & 1));
+          mbar_arrive_tx(hfull + 8 * s, bytes);
+          const uint32_t dst = hbase + s * S::kHStage;
+          tma_box(dst, &map_h, k * kI8K, y, hfull + 8 * s);
+          tma_box(dst + p.cols * 128, &map_h, k * kI8K + 64, y, hfull + 8 * s);
+        }
+      }
+      for (int k = (g > S::kH ? g - S::kH : 0); k < g; ++k)
+        if (ok) ok = bar_wait<false>(hempty + 8 * (k % S::kH), (uint32_t)((k / S::kH) & 1));
     }
   } else if (warp == 1) {
     // the whole warp runs through the stages, so that what the MMAs take is
@@ -408,30 +434,36 @@ __global__ void __launch_bounds__(kI8Threads, 1)
     int len = span.stages(ks);
     for (int g = 0; g < G; ++g) {
       const int b = g & 1;
-      const uint32_t more = part != 0;
       if (k == 0) span.request(a, p, t + (int)gridDim.x);
-      if (!more && c > 0 && ok) ok = bar_wait<false>(dempty, (uint32_t)((c - 1) & 1));
-      if (ok) ok = bar_wait<false>(full + 8 * s, phase);
-      if (ok) ok = bar_wait<false>(afull + 8 * b, (uint32_t)((g / 2) & 1));
-      tmem_fence_after();
-      const uint64_t h0 = mma_desc(base + s * S::kStage + kI8WStage, 0), h1 = h0 + half;
-      const uint32_t at = abase + b * 128;
+      const int db = c % S::kSums;
+      if (part == 0 && c >= S::kSums && ok) ok = bar_wait<false>(dempty + 8 * db, (uint32_t)((c / S::kSums - 1) & 1));
+      if (ok) ok = bar_wait<false>(hfull + 8 * s, phase);
+      const uint64_t h0 = mma_desc(hbase + s * S::kHStage, 0);
+      const uint32_t d = tbase + db * 128;
       const bool ends = part == len - 1 || k == ks - 1;
-      if (leader) {
 #pragma unroll
-        for (int sub = 0; sub < 2; ++sub) {
-          if (sub * 128 < p.height) {
-            mma_tmem_a(tbase + sub * 128, at + sub * 64, h0, idesc, more);
+      for (int h = 0; h < 2; ++h) {
+        if (ok) ok = bar_wait<false>(afull + 16 * h + 8 * b, (uint32_t)((g / 2) & 1));
+        tmem_fence_after();
+        const uint32_t at = abase + h * 128 + b * 64;
+        if (leader) {
 #pragma unroll
-            for (int j = 1; j < kI8K / 16; ++j)
-              mma_tmem_a(tbase + sub * 128, at + sub * 64 + j * 8, (j >> 2 ? h1 : h0) + (uint64_t)(2 * (j & 3)), idesc, 1);
+          for (int sub = 0; sub < 2; ++sub) {
+            if (sub * 128 < p.height) {
+#pragma unroll
+              for (int j = 0; j < 4; ++j)
+                mma_tmem_a(d + sub * kSubCols, at + sub * 32 + j * 8, (h ? h0 + half : h0) + (uint64_t)(2 * j), idesc,
+                           h + j > 0 ? 1u : (uint32_t)(part != 0));
+            }
+          }
+          mma_commit(aempty + 16 * h + 8 * b);
+          if (h == 1) {
+            mma_commit(hempty + 8 * s);
+            if (ends) mma_commit(dfull + 8 * db);
           }
         }
-        mma_commit(aempty + 8 * b);
-        mma_commit(empty + 8 * s);
-        if (ends) mma_commit(dfull);
+        __syncwarp();
       }
-      __syncwarp();
       c += ends;
       part = ends ? 0 : part + 1;
       if (++k == ks) {
@@ -439,7 +471,7 @@ __global__ void __launch_bounds__(kI8Threads, 1)
         t += (int)gridDim.x;
         len = span.stages(ks);
       }
-      if (++s == kStages) {
+      if (++s == S::kH) {
         s = 0;
         phase ^= 1;
       }
@@ -451,129 +483,132 @@ __global__ void __launch_bounds__(kI8Threads, 1)
     const uint32_t wrow = (uint32_t)row * 128, x8 = (uint32_t)(row & 7);
     // sums of this set's groups of 16 tokens (every second one)
     constexpr int kGroups = NT / 16, kMine = kGroups > 1 ? kGroups / 2 : 1;
-    int acc[16 * kMine];
-#pragma unroll
-    for (int n = 0; n < 16 * kMine; ++n) acc[n] = 0;
-    int c = 0, tile = 0;                            // sums read so far; tiles done
-    int len = 0, end = 0;                           // stages per sum; the stage whose sums are read next
+    asm volatile("griddepcontrol.wait;" ::: "memory");
     I8Span span;
-    // reads the sums that end at stage `end`, and scales and writes a tile's last
-    auto read_sums = [&]() {
-      const bool last = end == (tile + 1) * ks - 1, whole = len == ks;
-      const int t = (int)blockIdx.x + tile * (int)gridDim.x;
-      const int vi = t / p.rt, r0 = (t - vi * p.rt) * p.cols, v = vi * p.height + row;
-      const bool mine = last && row < p.height && v < a.V;
-      float ws = 0.f, hs[(NT + 31) / 32];
-      if (last) {                                   // (loaded ahead of the wait)
+    span.request(a, p, (int)blockIdx.x);
+    int len = span.stages(ks);                      // stages per sum
+    int g = 0, c = 0;                               // stages turned; sums read
+    // this set's half of stage g as fp16 into tensor memory
+    auto turn = [&]() {
+      const int s = g % S::kW, b = g & 1;
+      if (ok) ok = bar_wait<false>(wfull + 8 * s, (uint32_t)((g / S::kW) & 1));
+      __syncwarp();
+      const uint32_t src = base + s * kI8WStage + wrow;
+      uint32_t o[32];
 #pragma unroll
-        for (int i = 0; i < (NT + 31) / 32; ++i) hs[i] = __ldg(a.hidden_scale + min(r0 + 32 * i + lane, a.R - 1));
-        if (mine) ws = __ldg(a.weight_scale + v);
-        span.request(a, p, t + (int)gridDim.x);
+      for (int j = 0; j < 4; ++j) {
+        uint32_t w0, w1, w2, w3;
+        asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];"
+                     : "=r"(w0), "=r"(w1), "=r"(w2), "=r"(w3)
+                     : "r"(src + (((uint32_t)(4 * set + j) ^ x8) << 4)));
+        i8_to_half(w0, o[8 * j], o[8 * j + 1]);
+        i8_to_half(w1, o[8 * j + 2], o[8 * j + 3]);
+        i8_to_half(w2, o[8 * j + 4], o[8 * j + 5]);
+        i8_to_half(w3, o[8 * j + 6], o[8 * j + 7]);
       }
-      if (ok) ok = bar_wait<false>(dfull, (uint32_t)(c & 1));
-      ++c;
+      __syncwarp();
+      if (lane == 0) mbar_arrive_local(wempty + 8 * s);       // (its bytes are in registers)
+      if (g >= 2 && ok) ok = bar_wait<false>(aempty + 16 * set + 8 * b, (uint32_t)((g / 2 - 1) & 1));
       __syncwarp();
       tmem_fence_after();
-      const uint32_t src = tbase + quarter + sub * 128 + 16 * set;
+      tmem_st32(abase + quarter + set * 128 + b * 64 + sub * 32, o);
+      tmem_st_wait();
+      tmem_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive_local(afull + 16 * set + 8 * b);
+      ++g;
+    };
+    auto sum_wait = [&]() {
+      if (ok) ok = bar_wait<false>(dfull + 8 * (c % S::kSums), (uint32_t)((c / S::kSums) & 1));
+      __syncwarp();
+      tmem_fence_after();
+    };
+    auto sum_done = [&]() {
+      tmem_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive_local(dempty + 8 * (c % S::kSums));
+      ++c;
+    };
+    for (int tile = 0; tile < mine; ++tile) {
+      const int t = (int)blockIdx.x + tile * (int)gridDim.x;
+      const int vi = t / p.rt, r0 = (t - vi * p.rt) * p.cols, v = vi * p.height + row;
+      const bool in = row < p.height && v < a.V;
+      float ws = 0.f, hs[(NT + 31) / 32];
+      float z[16 * kMine];
+      // Sums are read after the stage behind their last has been turned (the
+      // next tile's first, too), so that the MMAs find work when they resume.
+      if (len == ks) {
+#pragma unroll 1
+        for (int k = tile == 0 ? 0 : 1; k <= ks; ++k)
+          if (g < G) turn();
+      } else {
+        int acc[16 * kMine];
+#pragma unroll
+        for (int n = 0; n < 16 * kMine; ++n) acc[n] = 0;
+#pragma unroll 1
+        for (int k = tile == 0 ? 0 : 1; k <= ks; ++k) {
+          if (g < G) turn();
+          if (k > 0 && k < ks && k % len == 0) {
+            sum_wait();
+            const uint32_t src = tbase + quarter + (c % S::kSums) * 128 + sub * kSubCols + 16 * set;
+#pragma unroll
+            for (int i = 0; i < kMine; ++i) {
+              if (16 * (2 * i + set) < p.cols) {
+                float y[16];
+                tmem_ld16_ahead(src + 32 * i, y);
+                tmem_ld_wait(y);
+#pragma unroll
+                for (int j = 0; j < 16; ++j) acc[16 * i + j] += __float2int_rn(y[j]);
+              }
+            }
+            sum_done();
+          }
+        }
+#pragma unroll
+        for (int n = 0; n < 16 * kMine; ++n) z[n] = __int_as_float(acc[n]);
+      }
+#pragma unroll
+      for (int i = 0; i < (NT + 31) / 32; ++i) hs[i] = __ldg(a.hidden_scale + min(r0 + 32 * i + lane, a.R - 1));
+      if (in) ws = __ldg(a.weight_scale + v);
+      span.request(a, p, t + (int)gridDim.x);
+      sum_wait();
+      const uint32_t src = tbase + quarter + (c % S::kSums) * 128 + sub * kSubCols + 16 * set;
 #pragma unroll
       for (int i = 0; i < kMine; ++i) {
         if (16 * (2 * i + set) < p.cols) {
-          float z[16];
-          tmem_ld16_ahead(src + 32 * i, z);
-          tmem_ld_wait(z);
-          if (whole) {
+          float y[16];
+          tmem_ld16_ahead(src + 32 * i, y);
+          tmem_ld_wait(y);
+          if (len == ks) {
 #pragma unroll
-            for (int j = 0; j < 16; ++j) acc[16 * i + j] = __float_as_int(z[j]);
+            for (int j = 0; j < 16; ++j) z[16 * i + j] = y[j];
           } else {
 #pragma unroll
-            for (int j = 0; j < 16; ++j) acc[16 * i + j] += __float2int_rn(z[j]);
+            for (int j = 0; j < 16; ++j) z[16 * i + j] = (float)(__float_as_int(z[16 * i + j]) + __float2int_rn(y[j]));
           }
         }
       }
-      tmem_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive_local(dempty);
-      if (last) {
-        if (!whole) {
+      sum_done();
+      char* out = reinterpret_cast<char*>(a.logits) + ((size_t)(r0 + 16 * set) * a.V + v) * (kBf16 ? 2 : 4);
+      const size_t step = (size_t)a.V * (kBf16 ? 2 : 4);
+      const int rows = in ? min(a.R - r0, p.cols) - 16 * set : 0;           // of this set's first group on
 #pragma unroll
-          for (int n = 0; n < 16 * kMine; ++n) acc[n] = __float_as_int((float)acc[n]);
-        }
-        char* out = reinterpret_cast<char*>(a.logits) + ((size_t)(r0 + 16 * set) * a.V + v) * (kBf16 ? 2 : 4);
-        const size_t step = (size_t)a.V * (kBf16 ? 2 : 4);
-        const int rows = mine ? min(a.R - r0, p.cols) - 16 * set : 0;       // of this set's first group on
+      for (int i = 0; i < kMine; ++i) {
 #pragma unroll
-        for (int i = 0; i < kMine; ++i) {
-#pragma unroll
-          for (int j = 0; j < 16; ++j) {
-            const float h = __shfl_sync(kFull, hs[i], 16 * set + j);
-            if (32 * i + j < rows) {
-              const float z = __int_as_float(acc[16 * i + j]) * h * ws;
-              if (kBf16)
-                *reinterpret_cast<__nv_bfloat16*>(out) = __float2bfloat16_rn(z);
-              else
-                *reinterpret_cast<float*>(out) = z;
-            }
-            out += step;
-            acc[16 * i + j] = 0;
+        for (int j = 0; j < 16; ++j) {
+          const float h = __shfl_sync(kFull, hs[i], 16 * set + j);
+          if (32 * i + j < rows) {
+            const float x = z[16 * i + j] * h * ws;
+            if (kBf16)
+              *reinterpret_cast<__nv_bfloat16*>(out) = __float2bfloat16_rn(x);
+            else
+              *reinterpret_cast<float*>(out) = x;
           }
-          out += 16 * step;
+          out += step;
         }
-        ++tile;
-        len = span.stages(ks);
+        out += 16 * step;
       }
-      end = last ? tile * ks + len - 1 : min(end + len, (tile + 1) * ks - 1);
-    };
-    // Sums that ended at this set's last stage or before are read first: the
-    // MMAs wait for it.  What ended at the other set's is read after this set's
-    // next stage has been turned, which the MMAs want at once then.
-    bool turned = false;
-    for (int g = set; g < G + 2;) {
-      if (end < (turned ? g : g - 1) && end < G && len > 0) {
-        read_sums();
-        continue;
-      }
-      if (turned) {
-        turned = false;
-        g += 2;
-        continue;
-      }
-      turned = true;
-      if (g < G) {
-        const int s = g % kStages;
-        if (ok) ok = bar_wait<false>(full + 8 * s, (uint32_t)((g / kStages) & 1));
-        if (g >= 2 && ok) ok = bar_wait<false>(aempty + 8 * set, (uint32_t)((g / 2 - 1) & 1));
-        __syncwarp();
-        tmem_fence_after();
-        const uint32_t src = base + s * S::kStage + wrow;
-        // 64 columns, as many at a time as registers are left beside the sums
-        constexpr int kCols = NT == 128 ? 16 : 32;
-#pragma unroll
-        for (int h = 0; h < 64 / kCols; ++h) {
-          uint32_t o[kCols];
-#pragma unroll
-          for (int j = 0; j < kCols / 8; ++j) {
-            uint32_t w0, w1, w2, w3;
-            asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];"
-                         : "=r"(w0), "=r"(w1), "=r"(w2), "=r"(w3)
-                         : "r"(src + ((((uint32_t)(h * (kCols / 8) + j)) ^ x8) << 4)));
-            i8_to_half(w0, o[8 * j], o[8 * j + 1]);
-            i8_to_half(w1, o[8 * j + 2], o[8 * j + 3]);
-            i8_to_half(w2, o[8 * j + 4], o[8 * j + 5]);
-            i8_to_half(w3, o[8 * j + 6], o[8 * j + 7]);
-          }
-          tmem_st(abase + quarter + set * 128 + sub * 64 + kCols * h, o);
-        }
-        tmem_st_wait();
-        tmem_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive_local(afull + 8 * set);
-      }
-      if (len == 0) {                               // the first stage did not wait for the tokens' kernel
-        asm volatile("griddepcontrol.wait;" ::: "memory");
-        span.request(a, p, (int)blockIdx.x);
-        len = span.stages(ks);
-        end = len - 1;
-      }
+      len = span.stages(ks);
     }
   }
   if (!ok) atomicOr(a.err, 4u);
