@@ -236,43 +236,40 @@ cudaError_t launch_quantize(const T* x, int R, int d, int8_t* q, float* scale, c
 // byte + 128 is placed into the low mantissa bits of 1024.0, and 1152 is
 // subtracted, both exact.
 //
-// The MMA's M is the vocabulary (a tile of up to 256 entries: two accumulators
-// of 128 lanes) and its N the tokens (up to 128), so the weight, the large
-// operand, passes through registers once, and B's tile serves both accumulators.
-//   warp 0      lane 0 fills a ring with 128 bytes of K of the tile's weight rows;
-//   warp 18     lane 0 another with the tokens' (fp16, from the workspace);
-//   warp 1      lane 0 issues the MMAs;
-//   warps 2..17 two sets of eight, thread = one vocabulary entry: a set turns
-//               its half of each stage's K into fp16, and adds up and scales
-//               every second group of 16 tokens.
+// The MMA's M is the vocabulary: a pair of CTAs (cta_group::2) with up to 128
+// entries each, so that a stage of the tokens (N, up to 128 of them, half in each
+// CTA) is read from L2 once for both.  Each CTA:
+//   warp 0       lane 0 fills a ring with 128 bytes of K of its weight rows;
+//   warp 2       lane 0 another with its half of the tokens' (fp16, from the
+//                workspace), counted at the first CTA's barriers;
+//   warp 1       of the first CTA: one lane issues the MMAs of both;
+//   warps 4..11  turn the weight into fp16 in tensor memory: thread = 64 of K of
+//                one entry;
+//   warps 12..19 add up, scale and write the sums: thread = one entry, every
+//                second group of 16 tokens.
 // Barriers: wfull / wempty (TMA <-> fp16), hfull / hempty (TMA <-> MMA), afull /
-// aempty (fp16 <-> MMA, two buffers in tensor memory for each half), dfull /
-// dempty (MMA <-> sums; two sets of accumulators where a tile has at most 64
-// tokens).
-// Every wait is bounded.
-constexpr int kI8Tile = 256;                        // vocabulary entries per tile at most
+// aempty (fp16 <-> MMA, four buffers in tensor memory), dfull / dempty (MMA <->
+// sums, two sets of accumulators).  Every wait is bounded.
+constexpr int kI8Rows = 128;                        // vocabulary entries per CTA and tile at most
 constexpr int kI8K = 128;                           // K per stage
-constexpr int kI8Exact = 1024 / kI8K;               // stages whose sums are exact in fp32
-constexpr int kI8Threads = 96 + 2 * kI8Tile;
-constexpr int kI8WStage = kI8Tile * kI8K;
+constexpr int kI8Exact = 1024 / kI8K;               // stages whose sums are exact in fp32 whatever the tokens
+constexpr int kI8Threads = 640;
+constexpr int kI8WStage = kI8Rows * kI8K;
+constexpr int kI8A = 4;                             // buffers of the fp16 weight: 64 columns each
 template <int NT>
 struct I8Shape {
-  static constexpr int kHStage = NT * kI8K * 2;
-  // a stage of the weight is free again as soon as it has been turned, one of
-  // the tokens only after its MMAs: rings of their own keep more of the weight
-  // in flight
-  static constexpr int kW = NT == 128 ? 3 : (NT == 64 ? 4 : 5);
-  static constexpr int kH = NT == 128 ? 3 : (NT == 64 ? 5 : (NT == 32 ? 6 : 8));
-  static constexpr int kSums = NT <= 64 ? 2 : 1;    // sets of accumulators
-  static constexpr int kBars = 2 * kW + 2 * kH + 12;
+  static constexpr int kHStage = NT / 2 * kI8K * 2; // this CTA's half of the tokens
+  static constexpr int kW = NT == 128 ? 7 : 8;
+  static constexpr int kH = NT == 128 ? 6 : 8;
+  static constexpr int kBars = 2 * kW + 2 * kH + 2 * kI8A + 4;
   static constexpr size_t kStageBytes = (size_t)kW * kI8WStage + (size_t)kH * kHStage;
   static constexpr size_t kSmem = 1024 + kStageBytes + 8 * kBars + 16;
   static_assert(kSmem <= 227 * 1024, "shared memory");
 };
 struct I8Plan {
-  int height;            // vocabulary entries per tile (a multiple of 8)
-  int cols;              // tokens per tile (a multiple of 16, at most 128)
-  int vt, rt;            // tiles of the vocabulary and of the tokens
+  int height;            // vocabulary entries per CTA and tile
+  int cols;              // tokens per tile (a multiple of 32, at most 128)
+  int vt, rt;            // tiles (of two CTAs) of the vocabulary and of the tokens
 };
 
 // the tokens as fp16, and the sum of each one's magnitudes; a CTA a token
@@ -329,55 +326,54 @@ struct I8Span {
 };
 
 template <int NT, bool kBf16>
-__global__ void __launch_bounds__(kI8Threads, 1)
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kI8Threads, 1)
     head_i8_kernel(const HeadI8Args a, const I8Plan p, const __grid_constant__ CUtensorMap map_w,
                    const __grid_constant__ CUtensorMap map_h) {
   using S = I8Shape<NT>;
   extern __shared__ __align__(1024) unsigned char i8_smem[];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int rank = (int)cluster_rank(), pair = blockIdx.x / 2, pairs = gridDim.x / 2;
   const uint32_t raw = smem_addr(i8_smem);
   const uint32_t base = (raw + 1023u) & ~1023u, hbase = base + S::kW * kI8WStage;
   const uint32_t bars = base + (uint32_t)S::kStageBytes;
   const uint32_t wfull = bars, wempty = wfull + 8 * S::kW;
   const uint32_t hfull = wempty + 8 * S::kW, hempty = hfull + 8 * S::kH;
-  const uint32_t afull = hempty + 8 * S::kH, aempty = afull + 32;    // [half][buffer]
-  const uint32_t dfull = aempty + 32, dempty = dfull + 16;
+  const uint32_t afull = hempty + 8 * S::kH, aempty = afull + 8 * kI8A;
+  const uint32_t dfull = aempty + 8 * kI8A, dempty = dfull + 16;
   uint32_t* s_taddr = reinterpret_cast<uint32_t*>(i8_smem + (bars - raw) + 8 * S::kBars);
   if (tid == 0) {
     for (int k = 0; k < S::kW; ++k) {
       mbar_init(wfull + 8 * k, 1);
-      mbar_init(wempty + 8 * k, 2 * kI8Tile / 32);
+      mbar_init(wempty + 8 * k, 8);
     }
     for (int k = 0; k < S::kH; ++k) {
       mbar_init(hfull + 8 * k, 1);
       mbar_init(hempty + 8 * k, 1);
     }
-    for (int b = 0; b < 4; ++b) {
-      mbar_init(afull + 8 * b, kI8Tile / 32);
+    for (int b = 0; b < kI8A; ++b) {
+      mbar_init(afull + 8 * b, 16);                 // the turning warps of both CTAs
       mbar_init(aempty + 8 * b, 1);
     }
     for (int b = 0; b < 2; ++b) {
       mbar_init(dfull + 8 * b, 1);
-      mbar_init(dempty + 8 * b, 2 * kI8Tile / 32);
+      mbar_init(dempty + 8 * b, 16);                // the summing warps of both CTAs
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == 1) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(s_taddr)),
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(s_taddr)),
                  "r"(512)
                  : "memory");
-    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
   }
   tmem_fence_before();
-  __syncthreads();
+  cluster_sync_all();
   tmem_fence_after();
-  const uint32_t tbase = *s_taddr;
-  const uint32_t abase = tbase + 256;               // [half][buffer][128 entries] of 32 columns
-  constexpr int kSubCols = 128 / S::kSums;          // columns of an accumulator
+  const uint32_t tbase = *s_taddr;                  // two sets of 128 columns of sums
+  const uint32_t abase = tbase + 256;               // kI8A buffers of 64 columns
   const int ks = (a.d + kI8K - 1) / kI8K;           // stages per tile
   const int tiles = p.vt * p.rt;
-  const int mine = tiles > (int)blockIdx.x ? (tiles - (int)blockIdx.x + (int)gridDim.x - 1) / (int)gridDim.x : 0;
-  const int G = mine * ks;
+  const int mine = tiles > pair ? (tiles - pair + pairs - 1) / pairs : 0;
   bool ok = true;
 
   if (warp == 0) {
@@ -387,7 +383,7 @@ __global__ void __launch_bounds__(kI8Threads, 1)
       const uint32_t bytes = (uint32_t)(p.height * kI8K);
       int g = 0;
       for (int i = 0; i < mine; ++i) {
-        const int y = ((int)blockIdx.x + i * (int)gridDim.x) / p.rt * p.height;
+        const int y = ((pair + i * pairs) / p.rt * 2 + rank) * p.height;
         for (int k = 0; k < ks; ++k, ++g) {
           const int s = g % S::kW;
           if (g >= S::kW && ok) ok = bar_wait<false>(wempty + 8 * s, (uint32_t)((g / S::kW - 1) & 1));
@@ -399,99 +395,92 @@ __global__ void __launch_bounds__(kI8Threads, 1)
       for (int k = (g > S::kW ? g - S::kW : 0); k < g; ++k)
         if (ok) ok = bar_wait<false>(wempty + 8 * (k % S::kW), (uint32_t)((k / S::kW) & 1));
     }
-  } else if (warp == 18) {
+  } else if (warp == 2) {
     if (lane == 0) {
-      const uint32_t bytes = (uint32_t)(p.cols * kI8K * 2);
+      const uint32_t bytes = (uint32_t)(p.cols * kI8K * 2);  // both halves
+      const int half = p.cols / 2;
+      const uint32_t hfull0 = map_to(hfull, 0);
       asm volatile("griddepcontrol.wait;" ::: "memory");
       asm volatile("fence.proxy.async.global;" ::: "memory");
       int g = 0;
       for (int i = 0; i < mine; ++i) {
-        const int y = ((int)blockIdx.x + i * (int)gridDim.x) % p.rt * p.cols;
+        const int y = (pair + i * pairs) % p.rt * p.cols + rank * half;
         for (int k = 0; k < ks; ++k, ++g) {
           const int s = g % S::kH;
-          if (g >= S::kH && ok) ok = bar_wait<false>(hempty + 8 * s, (uint32_t)((g / S::kH - 1) & 1));
-          mbar_arrive_tx(hfull + 8 * s, bytes);
+          if (g >= S::kH && ok) ok = bar_wait<true>(hempty + 8 * s, (uint32_t)((g / S::kH - 1) & 1));
+          if (rank == 0) mbar_arrive_tx(hfull + 8 * s, bytes);
           const uint32_t dst = hbase + s * S::kHStage;
-          tma_box(dst, &map_h, k * kI8K, y, hfull + 8 * s);
-          tma_box(dst + p.cols * 128, &map_h, k * kI8K + 64, y, hfull + 8 * s);
+          tma_box_pair(dst, &map_h, k * kI8K, y, hfull0 + 8 * s);
+          tma_box_pair(dst + half * 128, &map_h, k * kI8K + 64, y, hfull0 + 8 * s);
         }
       }
       for (int k = (g > S::kH ? g - S::kH : 0); k < g; ++k)
-        if (ok) ok = bar_wait<false>(hempty + 8 * (k % S::kH), (uint32_t)((k / S::kH) & 1));
+        if (ok) ok = bar_wait<true>(hempty + 8 * (k % S::kH), (uint32_t)((k / S::kH) & 1));
     }
   } else if (warp == 1) {
     // the whole warp runs through the stages, so that what the MMAs take is
     // formed in uniform registers; one lane issues
-    const bool leader = elect_lane();
-    const uint32_t idesc = mma_idesc(128, p.cols, false, false, false);
-    const uint32_t half = (uint32_t)p.cols * 128 >> 4;       // the second 64 of K, in units of 16 bytes
-    int c = 0, s = 0, k = 0;                        // sums handed over; ring slot; stage of the tile
-    int part = 0, t = (int)blockIdx.x;              // stage of the sum; tile
-    uint32_t phase = 0;
-    asm volatile("griddepcontrol.wait;" ::: "memory");
-    I8Span span;
-    span.request(a, p, t);
-    int len = span.stages(ks);
-    for (int g = 0; g < G; ++g) {
-      const int b = g & 1;
-      if (k == 0) span.request(a, p, t + (int)gridDim.x);
-      const int db = c % S::kSums;
-      if (part == 0 && c >= S::kSums && ok) ok = bar_wait<false>(dempty + 8 * db, (uint32_t)((c / S::kSums - 1) & 1));
-      if (ok) ok = bar_wait<false>(hfull + 8 * s, phase);
-      const uint64_t h0 = mma_desc(hbase + s * S::kHStage, 0);
-      const uint32_t d = tbase + db * 128;
-      const bool ends = part == len - 1 || k == ks - 1;
+    if (rank == 0) {
+      const bool leader = elect_lane();
+      const uint32_t idesc = mma_idesc(256, p.cols, false, false, false);
+      const uint32_t half = (uint32_t)p.cols * 64 >> 4;      // the second 64 of K, in units of 16 bytes
+      const uint32_t hempty0 = map_to(hempty, 0), hempty1 = map_to(hempty, 1);
+      const uint32_t aempty0 = map_to(aempty, 0), aempty1 = map_to(aempty, 1);
+      const uint32_t dfull0 = map_to(dfull, 0), dfull1 = map_to(dfull, 1);
+      int c = 0, s = 0, g = 0;                      // sums handed over; ring slot; stage
+      uint32_t phase = 0;
+      asm volatile("griddepcontrol.wait;" ::: "memory");
+      I8Span span;
+      span.request(a, p, pair);
+      for (int i = 0; i < mine; ++i) {
+        const int len = span.stages(ks);
+        span.request(a, p, pair + (i + 1) * pairs);
+        for (int k = 0, part = 0; k < ks; ++k, ++g) {
+          const int b = g % kI8A, db = c & 1;
+          const bool ends = part == len - 1 || k == ks - 1;
+          if (part == 0 && c >= 2 && ok) ok = bar_wait<true>(dempty + 8 * db, (uint32_t)((c / 2 - 1) & 1));
+          if (ok) ok = bar_wait<true>(hfull + 8 * s, phase);
+          if (ok) ok = bar_wait<true>(afull + 8 * b, (uint32_t)((g / kI8A) & 1));
+          tmem_fence_after();
+          const uint64_t h0 = mma_desc(hbase + s * S::kHStage, 0), h1 = h0 + half;
+          const uint32_t d = tbase + db * 128, at = abase + b * 64;
+          if (leader) {
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        if (ok) ok = bar_wait<false>(afull + 16 * h + 8 * b, (uint32_t)((g / 2) & 1));
-        tmem_fence_after();
-        const uint32_t at = abase + h * 128 + b * 64;
-        if (leader) {
-#pragma unroll
-          for (int sub = 0; sub < 2; ++sub) {
-            if (sub * 128 < p.height) {
-#pragma unroll
-              for (int j = 0; j < 4; ++j)
-                mma_tmem_a(d + sub * kSubCols, at + sub * 32 + j * 8, (h ? h0 + half : h0) + (uint64_t)(2 * j), idesc,
-                           h + j > 0 ? 1u : (uint32_t)(part != 0));
+            for (int j = 0; j < kI8K / 16; ++j)
+              mma_pair_tmem_a(d, at + j * 8, (j >> 2 ? h1 : h0) + (uint64_t)(2 * (j & 3)), idesc,
+                              j > 0 ? 1u : (uint32_t)(part != 0));
+            mma_commit_pair(aempty0 + 8 * b);
+            mma_commit_pair(aempty1 + 8 * b);
+            mma_commit_pair(hempty0 + 8 * s);
+            mma_commit_pair(hempty1 + 8 * s);
+            if (ends) {
+              mma_commit_pair(dfull0 + 8 * db);
+              mma_commit_pair(dfull1 + 8 * db);
             }
           }
-          mma_commit(aempty + 16 * h + 8 * b);
-          if (h == 1) {
-            mma_commit(hempty + 8 * s);
-            if (ends) mma_commit(dfull + 8 * db);
+          __syncwarp();
+          c += ends;
+          part = ends ? 0 : part + 1;
+          if (++s == S::kH) {
+            s = 0;
+            phase ^= 1;
           }
         }
-        __syncwarp();
-      }
-      c += ends;
-      part = ends ? 0 : part + 1;
-      if (++k == ks) {
-        k = 0;
-        t += (int)gridDim.x;
-        len = span.stages(ks);
-      }
-      if (++s == S::kH) {
-        s = 0;
-        phase ^= 1;
       }
     }
-  } else {
-    const int q = warp & 3, sub = ((warp - 2) >> 2) & 1, set = (warp - 2) >> 3;
-    const int row = sub * 128 + q * 32 + lane;      // vocabulary entry within the tile
+    __syncwarp();
+  } else if (warp >= 4 && warp < 12) {
+    const int q = warp & 3, half = (warp - 4) >> 2;
+    const int row = q * 32 + lane;                  // entry within this CTA's part
     const uint32_t quarter = (uint32_t)(q * 32) << 16;
     const uint32_t wrow = (uint32_t)row * 128, x8 = (uint32_t)(row & 7);
-    // sums of this set's groups of 16 tokens (every second one)
-    constexpr int kGroups = NT / 16, kMine = kGroups > 1 ? kGroups / 2 : 1;
-    asm volatile("griddepcontrol.wait;" ::: "memory");
-    I8Span span;
-    span.request(a, p, (int)blockIdx.x);
-    int len = span.stages(ks);                      // stages per sum
-    int g = 0, c = 0;                               // stages turned; sums read
-    // this set's half of stage g as fp16 into tensor memory
-    auto turn = [&]() {
-      const int s = g % S::kW, b = g & 1;
-      if (ok) ok = bar_wait<false>(wfull + 8 * s, (uint32_t)((g / S::kW) & 1));
+    const uint32_t afull0 = map_to(afull, 0);
+    const int G = mine * ks;
+    int s = 0;
+    uint32_t phase = 0;
+    for (int g = 0; g < G; ++g) {
+      const int b = g % kI8A;
+      if (ok) ok = bar_wait<false>(wfull + 8 * s, phase);
       __syncwarp();
       const uint32_t src = base + s * kI8WStage + wrow;
       uint32_t o[32];
@@ -500,124 +489,110 @@ __global__ void __launch_bounds__(kI8Threads, 1)
         uint32_t w0, w1, w2, w3;
         asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];"
                      : "=r"(w0), "=r"(w1), "=r"(w2), "=r"(w3)
-                     : "r"(src + (((uint32_t)(4 * set + j) ^ x8) << 4)));
+                     : "r"(src + (((uint32_t)(4 * half + j) ^ x8) << 4)));
         i8_to_half(w0, o[8 * j], o[8 * j + 1]);
         i8_to_half(w1, o[8 * j + 2], o[8 * j + 3]);
         i8_to_half(w2, o[8 * j + 4], o[8 * j + 5]);
         i8_to_half(w3, o[8 * j + 6], o[8 * j + 7]);
       }
       __syncwarp();
-      if (lane == 0) mbar_arrive_local(wempty + 8 * s);       // (its bytes are in registers)
-      if (g >= 2 && ok) ok = bar_wait<false>(aempty + 16 * set + 8 * b, (uint32_t)((g / 2 - 1) & 1));
+      if (lane == 0) mbar_arrive_local(wempty + 8 * s);      // (its bytes are in registers)
+      if (g >= kI8A && ok) ok = bar_wait<true>(aempty + 8 * b, (uint32_t)((g / kI8A - 1) & 1));
       __syncwarp();
       tmem_fence_after();
-      tmem_st32(abase + quarter + set * 128 + b * 64 + sub * 32, o);
+      tmem_st32(abase + quarter + b * 64 + half * 32, o);
       tmem_st_wait();
       tmem_fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive_local(afull + 16 * set + 8 * b);
-      ++g;
-    };
-    auto sum_wait = [&]() {
-      if (ok) ok = bar_wait<false>(dfull + 8 * (c % S::kSums), (uint32_t)((c / S::kSums) & 1));
-      __syncwarp();
-      tmem_fence_after();
-    };
-    auto sum_done = [&]() {
-      tmem_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive_local(dempty + 8 * (c % S::kSums));
-      ++c;
-    };
-    for (int tile = 0; tile < mine; ++tile) {
-      const int t = (int)blockIdx.x + tile * (int)gridDim.x;
-      const int vi = t / p.rt, r0 = (t - vi * p.rt) * p.cols, v = vi * p.height + row;
+      if (lane == 0) mbar_arrive_cluster(afull0 + 8 * b);
+      if (++s == S::kW) {
+        s = 0;
+        phase ^= 1;
+      }
+    }
+    // the last arrivals at this CTA's barriers are in before it ends
+    for (int g = (G > kI8A ? G - kI8A : 0); g < G; ++g)
+      if (ok) ok = bar_wait<true>(aempty + 8 * (g % kI8A), (uint32_t)((g / kI8A) & 1));
+  } else if (warp >= 12) {
+    const int q = warp & 3, set = (warp - 12) >> 2;
+    const int row = q * 32 + lane;
+    const uint32_t quarter = (uint32_t)(q * 32) << 16;
+    const uint32_t dempty0 = map_to(dempty, 0);
+    constexpr int kMine = NT / 32;                  // this set's groups of 16 tokens (every second one)
+    int c = 0;
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    I8Span span;
+    span.request(a, p, pair);
+    for (int i = 0; i < mine; ++i) {
+      const int t = pair + i * pairs;
+      const int vi = t / p.rt, r0 = (t - vi * p.rt) * p.cols, v = (vi * 2 + rank) * p.height + row;
       const bool in = row < p.height && v < a.V;
-      float ws = 0.f, hs[(NT + 31) / 32];
-      float z[16 * kMine];
-      // Sums are read after the stage behind their last has been turned (the
-      // next tile's first, too), so that the MMAs find work when they resume.
-      if (len == ks) {
-#pragma unroll 1
-        for (int k = tile == 0 ? 0 : 1; k <= ks; ++k)
-          if (g < G) turn();
-      } else {
-        int acc[16 * kMine];
+      const int len = span.stages(ks), sums = (ks + len - 1) / len;
+      span.request(a, p, t + pairs);
+      float ws = 0.f, hs[kMine];
 #pragma unroll
-        for (int n = 0; n < 16 * kMine; ++n) acc[n] = 0;
-#pragma unroll 1
-        for (int k = tile == 0 ? 0 : 1; k <= ks; ++k) {
-          if (g < G) turn();
-          if (k > 0 && k < ks && k % len == 0) {
-            sum_wait();
-            const uint32_t src = tbase + quarter + (c % S::kSums) * 128 + sub * kSubCols + 16 * set;
-#pragma unroll
-            for (int i = 0; i < kMine; ++i) {
-              if (16 * (2 * i + set) < p.cols) {
-                float y[16];
-                tmem_ld16_ahead(src + 32 * i, y);
-                tmem_ld_wait(y);
-#pragma unroll
-                for (int j = 0; j < 16; ++j) acc[16 * i + j] += __float2int_rn(y[j]);
-              }
-            }
-            sum_done();
-          }
-        }
-#pragma unroll
-        for (int n = 0; n < 16 * kMine; ++n) z[n] = __int_as_float(acc[n]);
-      }
-#pragma unroll
-      for (int i = 0; i < (NT + 31) / 32; ++i) hs[i] = __ldg(a.hidden_scale + min(r0 + 32 * i + lane, a.R - 1));
+      for (int u = 0; u < kMine; ++u) hs[u] = __ldg(a.hidden_scale + min(r0 + 32 * u + lane, a.R - 1));
       if (in) ws = __ldg(a.weight_scale + v);
-      span.request(a, p, t + (int)gridDim.x);
-      sum_wait();
-      const uint32_t src = tbase + quarter + (c % S::kSums) * 128 + sub * kSubCols + 16 * set;
+      int acc[16 * kMine];
 #pragma unroll
-      for (int i = 0; i < kMine; ++i) {
-        if (16 * (2 * i + set) < p.cols) {
-          float y[16];
-          tmem_ld16_ahead(src + 32 * i, y);
-          tmem_ld_wait(y);
-          if (len == ks) {
+      for (int n = 0; n < 16 * kMine; ++n) acc[n] = 0;
+#pragma unroll 1
+      for (int k = 0; k < sums; ++k, ++c) {
+        if (ok) ok = bar_wait<true>(dfull + 8 * (c & 1), (uint32_t)((c / 2) & 1));
+        __syncwarp();
+        tmem_fence_after();
+        const uint32_t src = tbase + quarter + (c & 1) * 128 + 16 * set;
 #pragma unroll
-            for (int j = 0; j < 16; ++j) z[16 * i + j] = y[j];
-          } else {
+        for (int u = 0; u < kMine; ++u) {
+          if (16 * (2 * u + set) < p.cols) {
+            float y[16];
+            tmem_ld16_ahead(src + 32 * u, y);
+            tmem_ld_wait(y);
+            if (sums == 1) {                        // the sum itself
 #pragma unroll
-            for (int j = 0; j < 16; ++j) z[16 * i + j] = (float)(__float_as_int(z[16 * i + j]) + __float2int_rn(y[j]));
+              for (int j = 0; j < 16; ++j) acc[16 * u + j] = __float_as_int(y[j]);
+            } else {
+#pragma unroll
+              for (int j = 0; j < 16; ++j) acc[16 * u + j] += __float2int_rn(y[j]);
+            }
           }
         }
+        tmem_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive_cluster(dempty0 + 8 * (c & 1));
       }
-      sum_done();
+      if (sums > 1) {
+#pragma unroll
+        for (int n = 0; n < 16 * kMine; ++n) acc[n] = __float_as_int((float)acc[n]);
+      }
       char* out = reinterpret_cast<char*>(a.logits) + ((size_t)(r0 + 16 * set) * a.V + v) * (kBf16 ? 2 : 4);
       const size_t step = (size_t)a.V * (kBf16 ? 2 : 4);
       const int rows = in ? min(a.R - r0, p.cols) - 16 * set : 0;           // of this set's first group on
 #pragma unroll
-      for (int i = 0; i < kMine; ++i) {
+      for (int u = 0; u < kMine; ++u) {
 #pragma unroll
         for (int j = 0; j < 16; ++j) {
-          const float h = __shfl_sync(kFull, hs[i], 16 * set + j);
-          if (32 * i + j < rows) {
-            const float x = z[16 * i + j] * h * ws;
+          const float h = __shfl_sync(kFull, hs[u], 16 * set + j);
+          if (32 * u + j < rows) {
+            const float y = __int_as_float(acc[16 * u + j]) * h * ws;
             if (kBf16)
-              *reinterpret_cast<__nv_bfloat16*>(out) = __float2bfloat16_rn(x);
+              *reinterpret_cast<__nv_bfloat16*>(out) = __float2bfloat16_rn(y);
             else
-              *reinterpret_cast<float*>(out) = x;
+              *reinterpret_cast<float*>(out) = y;
           }
           out += step;
         }
         out += 16 * step;
       }
-      len = span.stages(ks);
     }
   }
   if (!ok) atomicOr(a.err, 4u);
   __syncwarp();
   tmem_fence_before();
-  __syncthreads();
+  cluster_sync_all();
   tmem_fence_after();
   if (warp == 1)
-    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tbase), "r"(512) : "memory");
+    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tbase), "r"(512) : "memory");
 }
 
 template <int NT, bool kBf16>
@@ -646,7 +621,6 @@ cudaError_t launch_i8(const HeadI8Args& a, const I8Plan& p, int grid, int dev, c
 template <bool kBf16>
 cudaError_t launch_i8_cols(const HeadI8Args& a, const I8Plan& p, int grid, int dev, const CUtensorMap& mw,
                            const CUtensorMap& mh, cudaStream_t s) {
-  if (p.cols <= 16) return launch_i8<16, kBf16>(a, p, grid, dev, mw, mh, s);
   if (p.cols <= 32) return launch_i8<32, kBf16>(a, p, grid, dev, mw, mh, s);
   if (p.cols <= 64) return launch_i8<64, kBf16>(a, p, grid, dev, mw, mh, s);
   return launch_i8<128, kBf16>(a, p, grid, dev, mw, mh, s);
@@ -664,26 +638,26 @@ cudaError_t launch_head_i8(const HeadI8Args& a, cudaStream_t s) {
   if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
   if (e != cudaSuccess) return e;
   if (sms < 1) sms = 1;
+  const int64_t pairs = sms / 2 > 0 ? sms / 2 : 1;
   I8Plan p;
   p.rt = (a.R + 127) / 128;
-  p.cols = ((a.R + p.rt - 1) / p.rt + 15) / 16 * 16;
+  p.cols = ((a.R + p.rt - 1) / p.rt + 31) / 32 * 32;
   p.rt = (a.R + p.cols - 1) / p.cols;
   // one tile of tokens: the weight is streamed once, so its rows are spread
   // evenly over the SMs; more of them: whole tiles
-  const int64_t wave = (int64_t)sms * kI8Tile;
-  const int64_t waves = (a.V + wave - 1) / wave;
-  p.height = p.rt > 1 ? kI8Tile : (int)(((a.V + sms * waves - 1) / (sms * waves) + 7) / 8 * 8);
-  p.vt = (a.V + p.height - 1) / p.height;
+  const int64_t wave = pairs * 2 * kI8Rows, waves = (a.V + wave - 1) / wave;
+  p.height = p.rt > 1 ? kI8Rows : (int)(((a.V + 2 * pairs * waves - 1) / (2 * pairs * waves) + 3) / 4 * 4);
+  p.vt = (int)((a.V + 2 * (int64_t)p.height - 1) / (2 * p.height));
   CUtensorMap mw, mh;
   if (!tma_matrix(&mw, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, a.weight, a.d, a.V, p.height) ||
-      !tma_matrix(&mh, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, a.h16, a.d, a.R, p.cols))
+      !tma_matrix(&mh, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, a.h16, a.d, a.R, p.cols / 2))
     return cudaErrorInvalidValue;
   head_i8_tokens_kernel<<<a.R < 65536 ? a.R : 65536, kTokenThreads, 0, s>>>(a);
   e = cudaGetLastError();
   if (e != cudaSuccess) return e;
   const int64_t tiles = (int64_t)p.vt * p.rt;
-  if (tiles + sms >= (1ll << 31)) return cudaErrorInvalidValue;     // (64 TB of logits)
-  const int grid = tiles < sms ? (int)tiles : sms;
+  if (tiles + pairs >= (1ll << 31)) return cudaErrorInvalidValue;   // (64 TB of logits)
+  const int grid = (int)(2 * (tiles < pairs ? tiles : pairs));
   return a.dtype == 0 ? launch_i8_cols<false>(a, p, grid, dev, mw, mh, s) : launch_i8_cols<true>(a, p, grid, dev, mw, mh, s);
 }
 
