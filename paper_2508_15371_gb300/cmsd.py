@@ -294,27 +294,45 @@ def lmhead_confidence(hidden, weight, p=None, logits=False, out=None, ws=None):
     return o
 
 
-def _need_current(**ts):
-    """Contiguous CUDA tensors on the current device (None where an argument is not given)."""
-    _need_cuda(*ts.values())
-    cur = _torch().cuda.current_device()
-    for name, t in ts.items():
-        if t is not None and t.get_device() != cur:
+def _need(*specs):
+    """Each (name, tensor, shape, dtype) a contiguous CUDA tensor of that shape and type on the current
+    device; returns its index."""
+    cur = None
+    for name, t, shape, dtype in specs:
+        if t is None or t.dtype is not dtype or t.shape != shape:
+            got = "nothing" if t is None else f"{t.dtype} {tuple(t.shape)}"
+            raise CmsdError(f"{name} must be {dtype} {tuple(shape)}, got {got}")
+        if not t.is_cuda:
+            raise CmsdError(f"{name} must be a CUDA tensor (the library has no CPU path)")
+        if cur is None:
+            cur = _torch_mod.cuda.current_device()
+        if t.get_device() != cur:
             raise CmsdError(f"{name} must be on the current device")
+        if not t.is_contiguous():
+            raise CmsdError(f"{name} must be contiguous")
+    return cur
 
 
-def _need_shape(name, t, shape, dtype):
-    if t is None or tuple(t.shape) != tuple(shape) or t.dtype != dtype:
-        got = "nothing" if t is None else f"{t.dtype} {tuple(t.shape)}"
-        raise CmsdError(f"{name} must be {dtype} {tuple(shape)}, got {got}")
+def _need_ws(ws, cur):
+    if not ws.is_cuda or ws.get_device() != cur or not ws.is_contiguous():
+        raise CmsdError("the workspace must be contiguous on the current device")
+    return ws.numel() * ws.element_size()
 
 
-def _head_sizes(hidden, weight, dtype):
+def _stream_of(cur):
+    return _raw_stream(cur) if _raw_stream is not None else _torch_mod.cuda.current_stream().cuda_stream
+
+
+def _head_sizes(hidden, weight):
     if hidden.dim() != 2 or weight.dim() != 2 or hidden.shape[1] != weight.shape[1]:
         raise CmsdError("hidden [R, d] and weight [V, d] must share d")
-    if hidden.dtype != dtype or weight.dtype != dtype:
-        raise CmsdError(f"hidden and weight must be {dtype}")
     return hidden.shape[0], hidden.shape[1], weight.shape[0]
+
+
+def _given(out, name, shape, dtype, like):
+    if out is not None and name in out:
+        return out[name]
+    return _torch_mod.empty(shape, dtype=dtype, device=like.device)
 
 
 def _head_workspace(what, R, d, V):
@@ -348,18 +366,17 @@ def lmhead_loss(hidden, weight, labels, ignore_index=-100, out=None, ws=None):
     hidden: bf16 [R, d], weight: bf16 [V, d], labels: int32 [R].  Returns dict
     loss and lse ([R], float32; 0 in rows whose label is ignore_index)."""
     torch = _torch()
-    R, d, V = _head_sizes(hidden, weight, torch.bfloat16)
-    _need_shape("labels", labels, (R,), torch.int32)
-    o = {n: _out(out, n, (R,), torch.float32, hidden.device) for n in ("loss", "lse")}
-    if o["loss"] is not None:
-        _need_shape("loss", o["loss"], (R,), torch.float32)
-    _need_shape("lse", o["lse"], (R,), torch.float32)
-    _need_current(hidden=hidden, weight=weight, labels=labels, ws=ws, **o)
+    R, d, V = _head_sizes(hidden, weight)
+    f32, bf16 = torch.float32, torch.bfloat16
+    loss, lse = _given(out, "loss", (R,), f32, hidden), _given(out, "lse", (R,), f32, hidden)
+    cur = _need(("hidden", hidden, (R, d), bf16), ("weight", weight, (V, d), bf16), ("labels", labels, (R,), torch.int32),
+                ("loss", loss, (R,), f32), ("lse", lse, (R,), f32))
     ws = ws if ws is not None else lmhead_loss_workspace(R, d, V)
-    rc = lib().cmsd_lmhead_loss(_ptr(hidden), _ptr(weight), _ptr(labels), R, d, V, int(ignore_index),
-                                _ptr(o["loss"]), _ptr(o["lse"]), _ptr(ws), ws.numel(), _stream())
-    _check(rc, "cmsd_lmhead_loss")
-    return o
+    rc = lib().cmsd_lmhead_loss(hidden.data_ptr(), weight.data_ptr(), labels.data_ptr(), R, d, V, int(ignore_index),
+                                loss.data_ptr(), lse.data_ptr(), ws.data_ptr(), _need_ws(ws, cur), _stream_of(cur))
+    if rc != OK:
+        _check(rc, "cmsd_lmhead_loss")
+    return {"loss": loss, "lse": lse}
 
 
 def lmhead_loss_backward(hidden, weight, labels, lse, grad_loss, ignore_index=-100, hidden_grad=True,
@@ -369,23 +386,24 @@ def lmhead_loss_backward(hidden, weight, labels, lse, grad_loss, ignore_index=-1
     Returns dict d_hidden (bf16 [R, d], with hidden_grad) and d_weight (bf16
     [V, d], with weight_grad), written whole."""
     torch = _torch()
-    R, d, V = _head_sizes(hidden, weight, torch.bfloat16)
-    _need_shape("labels", labels, (R,), torch.int32)
-    _need_shape("lse", lse, (R,), torch.float32)
-    _need_shape("grad_loss", grad_loss, (R,), torch.float32)
+    R, d, V = _head_sizes(hidden, weight)
+    f32, bf16 = torch.float32, torch.bfloat16
     o = {}
+    specs = [("hidden", hidden, (R, d), bf16), ("weight", weight, (V, d), bf16), ("labels", labels, (R,), torch.int32),
+             ("lse", lse, (R,), f32), ("grad_loss", grad_loss, (R,), f32)]
     if hidden_grad:
-        o["d_hidden"] = _out(out, "d_hidden", (R, d), torch.bfloat16, hidden.device)
-        _need_shape("d_hidden", o["d_hidden"], (R, d), torch.bfloat16)
+        o["d_hidden"] = _given(out, "d_hidden", (R, d), bf16, hidden)
+        specs.append(("d_hidden", o["d_hidden"], (R, d), bf16))
     if weight_grad:
-        o["d_weight"] = _out(out, "d_weight", (V, d), torch.bfloat16, hidden.device)
-        _need_shape("d_weight", o["d_weight"], (V, d), torch.bfloat16)
-    _need_current(hidden=hidden, weight=weight, labels=labels, lse=lse, grad_loss=grad_loss, ws=ws, **o)
+        o["d_weight"] = _given(out, "d_weight", (V, d), bf16, hidden)
+        specs.append(("d_weight", o["d_weight"], (V, d), bf16))
+    cur = _need(*specs)
     ws = ws if ws is not None else lmhead_loss_backward_workspace(R, d, V)
-    rc = lib().cmsd_lmhead_loss_backward(_ptr(hidden), _ptr(weight), _ptr(labels), _ptr(lse), _ptr(grad_loss),
-                                         R, d, V, int(ignore_index), _ptr(o.get("d_hidden")),
-                                         _ptr(o.get("d_weight")), _ptr(ws), ws.numel(), _stream())
-    _check(rc, "cmsd_lmhead_loss_backward")
+    rc = lib().cmsd_lmhead_loss_backward(hidden.data_ptr(), weight.data_ptr(), labels.data_ptr(), lse.data_ptr(),
+                                         grad_loss.data_ptr(), R, d, V, int(ignore_index), _ptr(o.get("d_hidden")),
+                                         _ptr(o.get("d_weight")), ws.data_ptr(), _need_ws(ws, cur), _stream_of(cur))
+    if rc != OK:
+        _check(rc, "cmsd_lmhead_loss_backward")
     return o
 
 
@@ -398,14 +416,13 @@ def quantize_rows(x, out=None):
     if x.dtype not in (torch.float32, torch.bfloat16):
         raise CmsdError(f"x must be float32 or bfloat16, got {x.dtype}")
     R, d = x.shape
-    o = {"q": _out(out, "q", (R, d), torch.int8, x.device),
-         "scale": _out(out, "scale", (R,), torch.float32, x.device)}
-    _need_shape("q", o["q"], (R, d), torch.int8)
-    _need_shape("scale", o["scale"], (R,), torch.float32)
-    _need_current(x=x, **o)
-    rc = lib().cmsd_quantize_rows(_ptr(x), _dtype_code(x), R, d, _ptr(o["q"]), _ptr(o["scale"]), _stream())
-    _check(rc, "cmsd_quantize_rows")
-    return o
+    q, scale = _given(out, "q", (R, d), torch.int8, x), _given(out, "scale", (R,), torch.float32, x)
+    cur = _need(("x", x, (R, d), x.dtype), ("q", q, (R, d), torch.int8), ("scale", scale, (R,), torch.float32))
+    rc = lib().cmsd_quantize_rows(x.data_ptr(), F32 if x.dtype is torch.float32 else BF16, R, d, q.data_ptr(),
+                                  scale.data_ptr(), _stream_of(cur))
+    if rc != OK:
+        _check(rc, "cmsd_quantize_rows")
+    return {"q": q, "scale": scale}
 
 
 def lmhead_i8(hidden_q, hidden_scale, weight_q, weight_scale, dtype=None, out=None, ws=None):
@@ -416,18 +433,19 @@ def lmhead_i8(hidden_q, hidden_scale, weight_q, weight_scale, dtype=None, out=No
     dtype = torch.bfloat16 if dtype is None else dtype
     if dtype not in (torch.float32, torch.bfloat16):
         raise CmsdError(f"logits are float32 or bfloat16, not {dtype}")
-    R, d, V = _head_sizes(hidden_q, weight_q, torch.int8)
-    _need_shape("hidden_scale", hidden_scale, (R,), torch.float32)
-    _need_shape("weight_scale", weight_scale, (V,), torch.float32)
-    o = {"logits": _out(out, "logits", (R, V), dtype, hidden_q.device)}
-    _need_shape("logits", o["logits"], (R, V), dtype)
-    _need_current(hidden_q=hidden_q, hidden_scale=hidden_scale, weight_q=weight_q, weight_scale=weight_scale,
-                  ws=ws, **o)
+    R, d, V = _head_sizes(hidden_q, weight_q)
+    f32, i8 = torch.float32, torch.int8
+    logits = _given(out, "logits", (R, V), dtype, hidden_q)
+    cur = _need(("hidden_q", hidden_q, (R, d), i8), ("hidden_scale", hidden_scale, (R,), f32),
+                ("weight_q", weight_q, (V, d), i8), ("weight_scale", weight_scale, (V,), f32),
+                ("logits", logits, (R, V), dtype))
     ws = ws if ws is not None else lmhead_i8_workspace(R, d, V)
-    rc = lib().cmsd_lmhead_i8(_ptr(hidden_q), _ptr(hidden_scale), _ptr(weight_q), _ptr(weight_scale), R, d, V,
-                              _ptr(o["logits"]), _dtype_code(o["logits"]), _ptr(ws), ws.numel(), _stream())
-    _check(rc, "cmsd_lmhead_i8")
-    return o
+    rc = lib().cmsd_lmhead_i8(hidden_q.data_ptr(), hidden_scale.data_ptr(), weight_q.data_ptr(), weight_scale.data_ptr(),
+                              R, d, V, logits.data_ptr(), F32 if dtype is f32 else BF16, ws.data_ptr(),
+                              _need_ws(ws, cur), _stream_of(cur))
+    if rc != OK:
+        _check(rc, "cmsd_lmhead_i8")
+    return {"logits": logits}
 
 
 def verify(draft, target, tokens, conf, draft_lse=None, k_row=None, p=None, seed=0, iteration=0,
