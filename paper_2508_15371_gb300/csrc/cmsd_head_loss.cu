@@ -14,7 +14,6 @@
 namespace cmsd {
 namespace {
 
-__device__ __forceinline__ uint16_t to_bf(float x) { return __bfloat16_as_ushort(__float2bfloat16_rn(x)); }
 __device__ __forceinline__ bool kept(const HeadLossArgs& a, int label) {
   return label != a.ignore && label >= 0 && label < a.V;
 }
@@ -115,7 +114,8 @@ constexpr int kHalfBytes = 128 * 128;                 // 128 rows of 64 bf16
 constexpr int kStageBytes = 2 * kHalfBytes;           // A's and B's half
 constexpr int kEpiWarps = 8;
 constexpr int kPairThreads = 64 + 32 * kEpiWarps;
-constexpr size_t kPairSmem = 1024 + (size_t)kStages * kStageBytes + 8 * (2 * kStages + 4) + 16;
+constexpr int kOutBytes = 32 * 128;                   // a warp's 32 rows of 128 bytes on their way out
+constexpr size_t kPairSmem = 1024 + (size_t)kStages * kStageBytes + (size_t)kEpiWarps * kOutBytes + 8 * (2 * kStages + 4) + 16;
 constexpr int kTmemCols = 512;
 static_assert(kPairSmem <= 227 * 1024, "shared memory");
 
@@ -223,6 +223,9 @@ struct Maps {
   CUtensorMap weight_n;    // weight, 64 (d) x 64 entries
   CUtensorMap dz_k;        // P, 64 (entries) x 128 rows
   CUtensorMap dz_m;        // P, 64 (entries) x 64 rows
+  CUtensorMap dz_out;      // P, 64 (entries) x 32 rows
+  CUtensorMap dw_out;      // d_weight, 64 (d) x 32 entries
+  CUtensorMap dh_out;      // d_hidden's parts, 32 (d) x 32 rows
 };
 
 __device__ __forceinline__ uint32_t pack_bf(float lo, float hi) {
@@ -241,7 +244,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
   const uint32_t rank = cluster_rank();
   const uint32_t raw = smem_addr(pair_smem);
   const uint32_t base = (raw + 1023u) & ~1023u;
-  const uint32_t bars = base + kStages * kStageBytes;
+  const uint32_t bars = base + kStages * kStageBytes + kEpiWarps * kOutBytes;
   const uint32_t full = bars, empty = bars + 8 * kStages, tfull = bars + 16 * kStages, tempty = tfull + 16;
   uint32_t* s_taddr = reinterpret_cast<uint32_t*>(pair_smem + (bars - raw) + 8 * (2 * kStages + 4));
   if (tid == 0) {
@@ -344,13 +347,36 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
     // ---- the epilogue -----------------------------------------------------------------
     const uint32_t tempty0 = map_to(tempty, 0);
     const int q = warp & 3, half = (warp - 2) >> 2;
+    // this warp's rows on their way out: 128 bytes of each, swizzled as the boxes are
+    const uint32_t obuf = base + kStages * kStageBytes + (warp - 2) * kOutBytes, orow = obuf + lane * 128;
+    const uint32_t x8 = (uint32_t)(lane & 7);
+    // 32 columns of 32 rows as bf16; a box of 64 goes out with every second call
+    auto out_bf16 = [&](const float (&v)[32], int c, int y, int x, bool inside, const CUtensorMap* map) {
+      if ((c & 32) == 0) {
+        if (lane == 0) tma_store_wait_read();
+        __syncwarp();
+      }
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        st_shared(orow + (((uint32_t)(k + (c & 32) / 8) ^ x8) << 4), pack_bf(v[8 * k], v[8 * k + 1]),
+                  pack_bf(v[8 * k + 2], v[8 * k + 3]), pack_bf(v[8 * k + 4], v[8 * k + 5]),
+                  pack_bf(v[8 * k + 6], v[8 * k + 7]));
+      if (c & 32) {
+        smem_to_copies();
+        __syncwarp();
+        if (lane == 0 && inside) {                   // (part of a box may lie outside, not all of it)
+          tma_store(map, x - 32, y, obuf);
+          tma_store_commit();
+        }
+      }
+    };
     for (int i = 0; i < w.total; ++i) {
       const Tile t = tile_of<OP>(a, w, i);
       const int b = i & 1;
       if (ok) ok = bar_wait<true>(tfull + 8 * b, (uint32_t)((i / 2) & 1));
       __syncwarp();
       tmem_fence_after();
-      const int row = t.m * kPairTile + (int)rank * 128 + q * 32 + lane;
+      const int row0 = t.m * kPairTile + (int)rank * 128 + q * 32, row = row0 + lane;
       const int col = t.n * kPairTile + half * 128;
       const uint32_t src = tbase + ((uint32_t)(q * 32) << 16) + (uint32_t)(b * 256 + half * 128);
       const bool live = row < n;
@@ -406,36 +432,30 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
             p[k] = live && j0 + k < vlen
                        ? (ex2(fmaf(z[k], kLog2e, -lse2)) - (lab == j0 + k ? 1.f : 0.f)) * gr
                        : 0.f;
-          uint4* dst = reinterpret_cast<uint4*>(a.dz + (size_t)row * a.Vc + j0);
-#pragma unroll
-          for (int k = 0; k < 4; ++k)
-            dst[k] = make_uint4(pack_bf(p[8 * k], p[8 * k + 1]), pack_bf(p[8 * k + 2], p[8 * k + 3]),
-                                pack_bf(p[8 * k + 4], p[8 * k + 5]), pack_bf(p[8 * k + 6], p[8 * k + 7]));
+          out_bf16(p, c, row0, j0, true, &maps.dz_out);
         } else if (t.dw) {
-          if (row < vlen) {
-            uint4* dst = reinterpret_cast<uint4*>(a.d_weight + (size_t)(v0 + row) * a.d + j0);
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-              if (j0 + 8 * k < a.d)
-                dst[k] = make_uint4(pack_bf(z[8 * k], z[8 * k + 1]), pack_bf(z[8 * k + 2], z[8 * k + 3]),
-                                    pack_bf(z[8 * k + 4], z[8 * k + 5]), pack_bf(z[8 * k + 6], z[8 * k + 7]));
-          }
-        } else if (live) {
-          float4* dst = reinterpret_cast<float4*>(a.dh + ((size_t)t.part * a.Rp + row) * a.d + j0);
+          out_bf16(z, c, v0 + row0, j0, v0 + row0 < a.V && (j0 & ~63) < a.d, &maps.dw_out);
+        } else {
+          if (lane == 0) tma_store_wait_read();
+          __syncwarp();
 #pragma unroll
           for (int k = 0; k < 8; ++k)
-            if (j0 + 4 * k < a.d) {
-              float4 x = make_float4(z[4 * k], z[4 * k + 1], z[4 * k + 2], z[4 * k + 3]);
-              if (!first) {
-                const float4 y = dst[k];
-                x = make_float4(x.x + y.x, x.y + y.y, x.z + y.z, x.w + y.w);
-              }
-              dst[k] = x;
-            }
+            st_shared(orow + (((uint32_t)k ^ x8) << 4), __float_as_uint(z[4 * k]), __float_as_uint(z[4 * k + 1]),
+                      __float_as_uint(z[4 * k + 2]), __float_as_uint(z[4 * k + 3]));
+          smem_to_copies();
+          __syncwarp();
+          if (lane == 0 && j0 < a.d) {
+            if (first)
+              tma_store(&maps.dh_out, j0, t.part * a.Rp + row0, obuf);
+            else                                     // (one addition a piece: the order is that of the pieces)
+              tma_add(&maps.dh_out, j0, t.part * a.Rp + row0, obuf);
+            tma_store_commit();
+          }
         }
       }
       if (OP == kOpStats && live && col < vlen) a.part[(size_t)(col / kHeadPart) * a.Rp + row] = make_float2(mx, sum);
     }
+    if (OP != kOpStats && lane == 0) tma_store_wait();
   }
   if (!ok) atomicOr(a.err, 4u);
   __syncwarp();
@@ -552,11 +572,16 @@ bool encode_maps(const HeadLossArgs& a, bool backward, Maps* m) {
   const CUtensorMapDataType t = CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
   bool ok = tma_matrix(&m->rows_k, t, 2, a.packed, a.d, a.Rp, 128) && tma_matrix(&m->weight_k, t, 2, a.weight, a.d, a.V, 128);
   if (!backward) {
-    m->rows_n = m->weight_n = m->dz_k = m->dz_m = m->rows_k;       // not read
+    m->rows_n = m->weight_n = m->dz_k = m->dz_m = m->dz_out = m->dw_out = m->dh_out = m->rows_k;   // not read
     return ok;
   }
+  m->dw_out = m->dh_out = m->rows_k;
+  if (a.d_weight) ok = ok && tma_matrix(&m->dw_out, t, 2, a.d_weight, a.d, a.V, 32);
+  if (a.d_hidden)
+    ok = ok && tma_matrix(&m->dh_out, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, a.dh, a.d, (int64_t)a.split * a.Rp, 32);
   return ok && tma_matrix(&m->rows_n, t, 2, a.packed, a.d, a.Rp, 64) && tma_matrix(&m->weight_n, t, 2, a.weight, a.d, a.V, 64) &&
-         tma_matrix(&m->dz_k, t, 2, a.dz, a.Vc, a.Rp, 128) && tma_matrix(&m->dz_m, t, 2, a.dz, a.Vc, a.Rp, 64);
+         tma_matrix(&m->dz_k, t, 2, a.dz, a.Vc, a.Rp, 128) && tma_matrix(&m->dz_m, t, 2, a.dz, a.Vc, a.Rp, 64) &&
+         tma_matrix(&m->dz_out, t, 2, a.dz, a.Vc, a.Rp, 32);
 }
 
 // `most`: tiles at most; one pair of CTAs for each two SMs runs through them
