@@ -148,7 +148,7 @@ __device__ __forceinline__ Work work_of(const HeadLossArgs& a, int n, int vlen, 
   w.pair = blockIdx.x / 2;
   const int rows = max(1, (n + kPairTile - 1) / kPairTile);
   if (OP != kOpGrad) {
-    w.mt = OP == kOpStats ? (n + kPairTile - 1) / kPairTile : rows;
+    w.mt = rows;
     w.nt = (vlen + kPairTile - 1) / kPairTile;
     w.kd = (a.d + 63) / 64;
     const int all = w.mt * w.nt;
@@ -234,10 +234,12 @@ __device__ __forceinline__ uint32_t pack_bf(float lo, float hi) {
   return r;
 }
 
-// v0, vlen: the piece of the vocabulary; first: the first piece
+// v0, vlen: the piece of the vocabulary; first: the first piece; arows: rows of
+// A's boxes along K (fewer than 128, and none for the second CTA, where there are
+// no more: what lies in the other lanes reaches no result)
 template <int OP>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
-    head_pair_kernel(const HeadLossArgs a, const int v0, const int vlen, const int first,
+    head_pair_kernel(const HeadLossArgs a, const int v0, const int vlen, const int first, const int arows,
                      const __grid_constant__ Maps maps) {
   extern __shared__ __align__(1024) unsigned char pair_smem[];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -266,21 +268,36 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
   }
   tmem_fence_before();
   cluster_sync_all();
-  // everything above overlaps the end of what precedes this grid on the stream
-  asm volatile("griddepcontrol.wait;" ::: "memory");
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   tmem_fence_after();
   const uint32_t tbase = *s_taddr;
-  const int n = *a.n;
-  const Work w = work_of<OP>(a, n, vlen, a.d_hidden != nullptr, a.d_weight != nullptr);
   bool ok = true;
+  // Everything up to its griddepcontrol.wait, in each warp that waits for it
+  // below, overlaps the end of what precedes this grid on the stream.
+  Work w0;                                           // of one tile of rows
+  w0.pairs = gridDim.x / 2;
+  w0.pair = blockIdx.x / 2;
+  w0.nt = (vlen + kPairTile - 1) / kPairTile;
+  w0.kd = (a.d + 63) / 64;
 
   if (warp == 0) {
     // ---- this CTA's halves of the operands --------------------------------------
     if (lane == 0) {
+      const uint32_t full0 = map_to(full, 0);
+      const bool narrow = arows < 128;
+      const uint32_t bytes = narrow ? kStageBytes + (uint32_t)arows * 128 : 2 * kStageBytes;   // of both CTAs
+      // One tile of rows: the first tile's weight does not depend on how many
+      // there are, nor on the kernel before (which has started, so that what
+      // precedes it on the stream has ended).
+      const int early = OP != kOpGrad && a.Rp == kPairTile && w0.pair < w0.nt ? min(kStages, w0.kd) : 0;
+      for (int s = 0; s < early; ++s) {
+        if (rank == 0) mbar_arrive_tx(full + 8 * s, bytes);
+        tma_box_pair(base + s * kStageBytes + kHalfBytes, &maps.weight_k, s * 64,
+                     v0 + w0.pair * kPairTile + (int)rank * 128, full0 + 8 * s);
+      }
+      asm volatile("griddepcontrol.wait;" ::: "memory");
       // what earlier kernels wrote with plain stores is read by the copy engine
       asm volatile("fence.proxy.async.global;" ::: "memory");
-      const uint32_t full0 = map_to(full, 0);
+      const Work w = work_of<OP>(a, *a.n, vlen, a.d_hidden != nullptr, a.d_weight != nullptr);
       int g = 0;
       for (int i = 0; i < w.total; ++i) {
         const Tile t = tile_of<OP>(a, w, i);
@@ -288,14 +305,14 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
         for (int kb = 0; kb < t.kb; ++kb, ++g) {
           const int s = g % kStages;
           if (g >= kStages && ok) ok = bar_wait<true>(empty + 8 * s, (uint32_t)((g / kStages - 1) & 1));
-          if (rank == 0) mbar_arrive_tx(full + 8 * s, 2 * kStageBytes);
+          if (rank == 0 && g >= early) mbar_arrive_tx(full + 8 * s, OP == kOpGrad && t.dw ? 2 * kStageBytes : bytes);
           const uint32_t sa = base + s * kStageBytes, sb = sa + kHalfBytes, bar = full0 + 8 * s;
           const int k = (t.k0 + kb) * 64;
           if (OP != kOpGrad) {
-            tma_box_pair(sa, &maps.rows_k, k, am, bar);
-            tma_box_pair(sb, &maps.weight_k, k, v0 + bn, bar);
+            if (!narrow || rank == 0) tma_box_pair(sa, &maps.rows_k, k, am, bar);
+            if (g >= early) tma_box_pair(sb, &maps.weight_k, k, v0 + bn, bar);
           } else if (!t.dw) {
-            tma_box_pair(sa, &maps.dz_k, k, am, bar);
+            if (!narrow || rank == 0) tma_box_pair(sa, &maps.dz_k, k, am, bar);
             tma_box_pair(sb, &maps.weight_n, bn, v0 + k, bar);
             tma_box_pair(sb + kHalfBytes / 2, &maps.weight_n, bn + 64, v0 + k, bar);
           } else {
@@ -312,6 +329,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
     }
   } else if (warp == 1) {
     // ---- the MMAs of both CTAs -----------------------------------------------------
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    const Work w = work_of<OP>(a, *a.n, vlen, a.d_hidden != nullptr, a.d_weight != nullptr);
     if (lane == 0 && rank == 0) {
       const uint32_t empty1 = map_to(empty, 1), tfull1 = map_to(tfull, 1);
       const uint32_t empty0 = map_to(empty, 0), tfull0 = map_to(tfull, 0);
@@ -345,6 +365,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
     __syncwarp();
   } else {
     // ---- the epilogue -----------------------------------------------------------------
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const int n = *a.n;
+    const Work w = work_of<OP>(a, n, vlen, a.d_hidden != nullptr, a.d_weight != nullptr);
     const uint32_t tempty0 = map_to(tempty, 0);
     const int q = warp & 3, half = (warp - 2) >> 2;
     // this warp's rows on their way out: 128 bytes of each, swizzled as the boxes are
@@ -526,21 +549,32 @@ __global__ void __launch_bounds__(kMergeThreads) head_merge_kernel(const HeadLos
 __global__ void __launch_bounds__(256) head_unpack_kernel(const HeadLossArgs a) {
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
-  const int per = a.d / 4;                           // four columns a thread
+  const int per = a.d / 4;                           // four columns and every fourth part a thread
   const size_t total = (size_t)a.R * per, step = (size_t)a.Rp * a.d;
-  for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (size_t)gridDim.x * 256) {
-    const int r = (int)(i / per), j = (int)(i - (size_t)r * per) * 4;
-    const int p = a.pos[r];
+  const int lane = threadIdx.x & 31, sub = lane >> 3;
+  const size_t warps = (size_t)gridDim.x * 8, warp = (size_t)blockIdx.x * 8 + (threadIdx.x >> 5);
+  for (size_t i0 = warp * 8; i0 < total; i0 += warps * 8) {
+    const size_t i = i0 + (lane & 7);
+    const int r = i < total ? (int)(i / per) : 0, j = (int)(i - (size_t)r * per) * 4;
+    const int p = i < total ? a.pos[r] : -1;
     float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
     if (p >= 0) {
       const float* src = a.dh + (size_t)p * a.d + j;
-#pragma unroll 8
-      for (int k = 0; k < a.split; ++k) {
+#pragma unroll 4
+      for (int k = sub; k < a.split; k += 4) {
         const float4 y = __ldcg(reinterpret_cast<const float4*>(src + k * step));
         x = make_float4(x.x + y.x, x.y + y.y, x.z + y.z, x.w + y.w);
       }
     }
-    *reinterpret_cast<uint2*>(a.d_hidden + (size_t)r * a.d + j) = make_uint2(pack_bf(x.x, x.y), pack_bf(x.z, x.w));
+#pragma unroll
+    for (int o = 8; o <= 16; o <<= 1) {
+      x.x += __shfl_xor_sync(kFull, x.x, o);
+      x.y += __shfl_xor_sync(kFull, x.y, o);
+      x.z += __shfl_xor_sync(kFull, x.z, o);
+      x.w += __shfl_xor_sync(kFull, x.w, o);
+    }
+    if (sub == 0 && i < total)
+      *reinterpret_cast<uint2*>(a.d_hidden + (size_t)r * a.d + j) = make_uint2(pack_bf(x.x, x.y), pack_bf(x.z, x.w));
   }
 }
 
@@ -568,9 +602,10 @@ cudaError_t launch_pack(const HeadLossArgs& a, cudaStream_t s) {
   return cudaGetLastError();
 }
 
+int box_rows(const HeadLossArgs& a) { return a.R <= 128 ? (a.R + 7) / 8 * 8 : 128; }
 bool encode_maps(const HeadLossArgs& a, bool backward, Maps* m) {
   const CUtensorMapDataType t = CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
-  bool ok = tma_matrix(&m->rows_k, t, 2, a.packed, a.d, a.Rp, 128) && tma_matrix(&m->weight_k, t, 2, a.weight, a.d, a.V, 128);
+  bool ok = tma_matrix(&m->rows_k, t, 2, a.packed, a.d, a.Rp, box_rows(a)) && tma_matrix(&m->weight_k, t, 2, a.weight, a.d, a.V, 128);
   if (!backward) {
     m->rows_n = m->weight_n = m->dz_k = m->dz_m = m->dz_out = m->dw_out = m->dh_out = m->rows_k;   // not read
     return ok;
@@ -580,7 +615,7 @@ bool encode_maps(const HeadLossArgs& a, bool backward, Maps* m) {
   if (a.d_hidden)
     ok = ok && tma_matrix(&m->dh_out, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, a.dh, a.d, (int64_t)a.split * a.Rp, 32);
   return ok && tma_matrix(&m->rows_n, t, 2, a.packed, a.d, a.Rp, 64) && tma_matrix(&m->weight_n, t, 2, a.weight, a.d, a.V, 64) &&
-         tma_matrix(&m->dz_k, t, 2, a.dz, a.Vc, a.Rp, 128) && tma_matrix(&m->dz_m, t, 2, a.dz, a.Vc, a.Rp, 64) &&
+         tma_matrix(&m->dz_k, t, 2, a.dz, a.Vc, a.Rp, box_rows(a)) && tma_matrix(&m->dz_m, t, 2, a.dz, a.Vc, a.Rp, 64) &&
          tma_matrix(&m->dz_out, t, 2, a.dz, a.Vc, a.Rp, 32);
 }
 
@@ -601,7 +636,7 @@ cudaError_t launch_pairs(const HeadLossArgs& a, int v0, int vlen, int first, int
   }
   int64_t pairs = sms / 2 > 0 ? sms / 2 : 1;
   if (pairs > most) pairs = most;
-  return launch_early(head_pair_kernel<OP>, (unsigned)(2 * pairs), kPairThreads, kPairSmem, s, a, v0, vlen, first, maps);
+  return launch_early(head_pair_kernel<OP>, (unsigned)(2 * pairs), kPairThreads, kPairSmem, s, a, v0, vlen, first, a.R <= 128 ? box_rows(a) : 128, maps);
 }
 }  // namespace
 
@@ -652,7 +687,7 @@ cudaError_t launch_head_loss_backward(const HeadLossArgs& a, cudaStream_t s) {
   }
   if (!a.d_hidden) return cudaSuccess;
   const int64_t n4 = (int64_t)a.R * (a.d / 4);
-  return launch_early(head_unpack_kernel, tiles(n4 < 256 * 8192 ? n4 : 256 * 8192, 256), 256, 0, s, a);
+  return launch_early(head_unpack_kernel, tiles(n4 < 64 * 16384 ? n4 : 64 * 16384, 64), 256, 0, s, a);
 }
 
 }  // namespace cmsd
