@@ -636,7 +636,8 @@ size_t loss_layout(HeadLossArgs& a, bool backward, char* w) {
   a.packed = (uint16_t*)take((size_t)Rp * a.d * 2);
   if (!backward) {
     a.zlab = (float*)take((size_t)Rp * 4);
-    a.part = (float2*)take((size_t)((a.V + kHeadPart - 1) / kHeadPart) * Rp * 8);
+    const int64_t parts = ((int64_t)a.V + kHeadPart - 1) / kHeadPart;
+    a.part = (float2*)take((size_t)(parts > kFewParts || Rp > kHeadTile ? parts : kFewParts) * Rp * 8);
     return o;
   }
   a.plse = (float*)take((size_t)Rp * 4);

@@ -11,6 +11,7 @@ namespace cmsd {
 // that ignored rows cost no products and their contents reach no sum.
 constexpr int kHeadTile = 256;                  // rows of a packed block, columns of a vocabulary tile
 constexpr int kHeadPart = 128;                  // vocabulary entries per partial statistic of the loss
+constexpr int kFewParts = 152;                  // partial statistics at most where there are few rows
 struct HeadLossArgs {
   const uint16_t* hidden;        // bf16 [R][d]
   const uint16_t* weight;        // bf16 [V][d]
@@ -33,7 +34,7 @@ struct HeadLossArgs {
   float* pgrad;
   uint16_t* packed;              // bf16 [Rp][d], zeros from row n to the next multiple of 64
   float* zlab;                   // [Rp] logit of the label (forward)
-  float2* part;                  // [ceil(V / kHeadPart)][Rp] (maximum, sum) in base 2 (forward)
+  float2* part;                  // [max(ceil(V / kHeadPart), kFewParts)][Rp] (maximum, sum) in base 2 (forward)
   int Vc;                        // vocabulary entries per piece, a multiple of kHeadTile (backward)
   int split;                     // parts that a piece's sum for d_hidden is cut into
   uint16_t* dz;                  // bf16 [Rp][Vc]

@@ -489,14 +489,298 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
     asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tbase), "r"(kTmemCols) : "memory");
 }
 
-// ---- a row's tiles merged -----------------------------------------------------------
-// Four rows a CTA (32 bytes of each tile's statistics), 64 tiles at a time.
-constexpr int kMergeThreads = 256;
+// (maximum, sum) of two sets of entries, in base 2
 __device__ __forceinline__ void fold(float& m, float& s, float m2, float s2) {
   const float mm = fmaxf(m, m2);
   s = (s > 0.f ? s * ex2(m - mm) : 0.f) + (s2 > 0.f ? s2 * ex2(m2 - mm) : 0.f);
   m = mm;
 }
+
+// ---- few rows ------------------------------------------------------------------------
+//
+// With up to 128 rows the products are bound by memory as long as the tensor
+// cores do no more than they must: a tile of 256 rows takes 512 cycles for 64 of
+// K however few of them are live (R=33 d=1024 V=32001: the loss 26 us), in which
+// memory delivers half a tile more.  So the roles change: the MMA's M is the
+// vocabulary (or d, for d_hidden) and its N the rows, in multiples of 32.
+//   logits    A = weight (128 entries a CTA at most), B = packed rows, K = d
+//   d_hidden  A = weight (its rows run along M = d), B = P, K = entries
+// (d_weight's product has few rows as its K, and stays as it is.)  The warps and
+// barriers are those of head_pair_kernel.  A thread of the epilogue holds one
+// entry's logits of all rows; a row's maximum and sum go across the warp's lanes
+// by halving the rows in play with each exchange, 31 exchanges for 32 rows, which
+// leaves row c with lane c.  All of a pair's tiles are folded before anything is
+// written.
+enum FewOp { kFewStats, kFewDz, kFewDh };
+constexpr int kFewRows = 128;
+constexpr int kFewStages = 9;
+constexpr int kFewBBytes = kFewRows / 2 * 128;         // this CTA's half of the rows
+constexpr int kFewStage = kHalfBytes + kFewBBytes;
+constexpr size_t kFewTable = (size_t)kFewRows * 16;    // each row's label, lse and gradient
+constexpr size_t kFewRed = (size_t)kEpiWarps * 2 * 32 * 8;
+constexpr size_t kFewSmem =
+    1024 + (size_t)kFewStages * kFewStage + kFewTable + kFewRed + 8 * (2 * kFewStages + 4) + 16;
+static_assert(kFewSmem <= 227 * 1024, "shared memory");
+
+// w[c] of every lane reduced over the warp's lanes: lane c gets row c's
+template <typename F>
+__device__ __forceinline__ float across(float (&w)[32], int lane, F f) {
+#pragma unroll
+  for (int o = 16; o; o >>= 1) {
+    const bool up = lane & o;
+#pragma unroll
+    for (int i = 0; i < o; ++i) {
+      const float keep = up ? w[i + o] : w[i], send = up ? w[i] : w[i + o];
+      w[i] = f(keep, __shfl_xor_sync(kFull, send, o));
+    }
+  }
+  return w[0];
+}
+
+struct FewPlan {
+  int height;            // entries of the vocabulary per CTA and tile (kFewStats, kFewDz)
+  int cols;              // rows, a multiple of 32
+  int tiles;
+};
+template <int OP>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
+    head_few_kernel(const HeadLossArgs a, const FewPlan p, const int v0, const int vlen, const int first,
+                    const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b) {
+  extern __shared__ __align__(1024) unsigned char few_smem[];
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int rank = (int)cluster_rank(), pair = blockIdx.x / 2, pairs = gridDim.x / 2;
+  const uint32_t raw = smem_addr(few_smem);
+  const uint32_t base = (raw + 1023u) & ~1023u;
+  unsigned char* sm = few_smem + (base - raw);
+  int4* s_table = reinterpret_cast<int4*>(sm + kFewStages * kFewStage);
+  float2* s_red = reinterpret_cast<float2*>(sm + kFewStages * kFewStage + kFewTable);
+  const uint32_t bars = base + (uint32_t)(kFewStages * kFewStage + kFewTable + kFewRed);
+  const uint32_t full = bars, empty = bars + 8 * kFewStages, tfull = bars + 16 * kFewStages, tempty = tfull + 16;
+  uint32_t* s_taddr = reinterpret_cast<uint32_t*>(sm + (bars - base) + 8 * (2 * kFewStages + 4));
+  if (tid == 0) {
+    for (int k = 0; k < kFewStages; ++k) {
+      mbar_init(full + 8 * k, 1);
+      mbar_init(empty + 8 * k, 1);
+    }
+    for (int b = 0; b < 2; ++b) {
+      mbar_init(tfull + 8 * b, 1);
+      mbar_init(tempty + 8 * b, 2 * kEpiWarps);
+    }
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(s_taddr)),
+                 "r"(256)
+                 : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+  }
+  tmem_fence_before();
+  cluster_sync_all();
+  tmem_fence_after();
+  const uint32_t tbase = *s_taddr;                  // two accumulators of 128 columns
+  const int mine = p.tiles > pair ? (p.tiles - pair + pairs - 1) / pairs : 0;
+  const int dt = (a.d + 255) / 256;
+  const int kall = OP == kFewDh ? (vlen + 63) / 64 : (a.d + 63) / 64;
+  const int kpart = OP == kFewDh ? (kall + a.split - 1) / a.split : kall;
+  // a tile's first block of K and their number
+  auto first_block = [&](int t) { return OP == kFewDh ? t / dt * kpart : 0; };
+  auto blocks = [&](int t) { return max(0, min(kpart, kall - first_block(t))); };
+  bool ok = true;
+
+  if (warp == 0) {
+    if (lane == 0) {
+      const uint32_t full0 = map_to(full, 0);
+      const uint32_t bytes = (OP == kFewDh ? 2 * kHalfBytes : (uint32_t)p.height * 256) + (uint32_t)p.cols * 128;
+      auto load_a = [&](int t, int k, int s) {
+        const uint32_t dst = base + s * kFewStage;
+        if (OP == kFewDh) {
+          const int x = t % dt * 256 + rank * 128, y = v0 + k * 64;
+          tma_box_pair(dst, &map_a, x, y, full0 + 8 * s);
+          tma_box_pair(dst + kHalfBytes / 2, &map_a, x + 64, y, full0 + 8 * s);
+        } else {
+          tma_box_pair(dst, &map_a, k * 64, v0 + (t * 2 + rank) * p.height, full0 + 8 * s);
+        }
+      };
+      // the weight's first stages do not wait for the kernel before (which has
+      // started, so that what precedes it on the stream has ended)
+      const int early = mine > 0 ? min(kFewStages, blocks(pair)) : 0;
+      for (int s = 0; s < early; ++s) {
+        if (rank == 0) mbar_arrive_tx(full + 8 * s, bytes);
+        load_a(pair, first_block(pair) + s, s);
+      }
+      asm volatile("griddepcontrol.wait;" ::: "memory");
+      asm volatile("fence.proxy.async.global;" ::: "memory");
+      int g = 0;
+      for (int i = 0; i < mine; ++i) {
+        const int t = pair + i * pairs, k0 = first_block(t), kb = blocks(t);
+        for (int k = 0; k < kb; ++k, ++g) {
+          const int s = g % kFewStages;
+          if (g >= kFewStages && ok) ok = bar_wait<true>(empty + 8 * s, (uint32_t)((g / kFewStages - 1) & 1));
+          if (g >= early) {
+            if (rank == 0) mbar_arrive_tx(full + 8 * s, bytes);
+            load_a(t, k0 + k, s);
+          }
+          tma_box_pair(base + s * kFewStage + kHalfBytes, &map_b, (k0 + k) * 64, rank * (p.cols / 2), full0 + 8 * s);
+        }
+      }
+      for (int k = (g > kFewStages ? g - kFewStages : 0); k < g; ++k)
+        if (ok) ok = bar_wait<true>(empty + 8 * (k % kFewStages), (uint32_t)((k / kFewStages) & 1));
+    }
+  } else if (warp == 1) {
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    if (rank == 0) {
+      const bool leader = elect_lane();
+      const uint32_t empty1 = map_to(empty, 1), tfull1 = map_to(tfull, 1);
+      const uint32_t empty0 = map_to(empty, 0), tfull0 = map_to(tfull, 0);
+      const uint32_t idesc = mma_idesc(256, p.cols, true, OP == kFewDh, false);
+      constexpr uint64_t da = OP == kFewDh ? 2048 >> 4 : 32 >> 4;   // K = 16 further: 16 rows, or 32 bytes
+      int g = 0, s = 0;
+      uint32_t phase = 0;
+      for (int i = 0; i < mine; ++i) {
+        const int b = i & 1, kb = blocks(pair + i * pairs);
+        if (i >= 2 && ok) ok = bar_wait<true>(tempty + 8 * b, (uint32_t)((i / 2 - 1) & 1));
+        tmem_fence_after();
+        const uint32_t d = tbase + (uint32_t)(b * 128);
+        for (int k = 0; k < kb; ++k, ++g) {
+          if (ok) ok = bar_wait<true>(full + 8 * s, phase);
+          tmem_fence_after();
+          const uint64_t ad = mma_desc(base + s * kFewStage, kHalfBytes / 2);
+          const uint64_t bd = mma_desc(base + s * kFewStage + kHalfBytes, 0);
+          if (leader) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) mma_pair(d, ad + j * da, bd + (uint64_t)(2 * j), idesc, (k | j) != 0);
+            mma_commit_pair(empty0 + 8 * s);
+            mma_commit_pair(empty1 + 8 * s);
+          }
+          __syncwarp();
+          if (++s == kFewStages) {
+            s = 0;
+            phase ^= 1;
+          }
+        }
+        if (leader) {
+          mma_commit_pair(tfull0 + 8 * b);
+          mma_commit_pair(tfull1 + 8 * b);
+        }
+        __syncwarp();
+      }
+    }
+  } else {
+    const int q = warp & 3, half = (warp - 2) >> 2, e = tid - 64;
+    const uint32_t tempty0 = map_to(tempty, 0);
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const int n = *a.n;
+    if (OP != kFewDh) {
+      for (int c = e; c < p.cols; c += 32 * kEpiWarps) {
+        int4 x = make_int4(-1, 0, 0, 0);
+        if (c < n) {
+          x.x = a.lab[c] - v0;
+          if (OP == kFewDz) {
+            x.y = __float_as_int(a.plse[c] * kLog2e);
+            x.z = __float_as_int(a.pgrad[c]);
+          }
+        }
+        s_table[c] = x;
+      }
+      asm volatile("bar.sync 1, 256;" ::: "memory");
+    }
+    // this warp's rows: every second group of 32
+    float mx[2] = {-pos_inf(), -pos_inf()}, sum[2] = {0.f, 0.f};
+    for (int i = 0; i < mine; ++i) {
+      const int t = pair + i * pairs, b = i & 1;
+      const int at = q * 32 + lane;                  // this thread's entry within the CTA's part
+      const int v = OP == kFewDh ? t % dt * 256 + rank * 128 + at : (t * 2 + rank) * p.height + at;
+      const bool live = OP == kFewDh ? v < a.d : at < p.height && v < vlen;
+      const bool some = blocks(t) > 0;
+      if (ok) ok = bar_wait<true>(tfull + 8 * b, (uint32_t)((i / 2) & 1));
+      __syncwarp();
+      tmem_fence_after();
+      const uint32_t src = tbase + ((uint32_t)(q * 32) << 16) + (uint32_t)(b * 128);
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const int c0 = 32 * (2 * u + half);
+        const bool more = u == 0 && c0 + 64 < p.cols;
+        float z[32];
+        if (c0 < p.cols) tmem_ld32(src + c0, z);
+        if (!more && (u == 0 || c0 < p.cols)) {
+          tmem_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive_cluster(tempty0 + 8 * b);     // this warp's columns have been read
+        }
+        if (c0 >= p.cols) break;
+        if (OP == kFewStats) {
+          const int lab = s_table[c0 + lane].x, from = v - lane;
+          unsigned hit = __ballot_sync(kFull, lab >= from && lab < from + 32 && q * 32 + lab - from < p.height);
+          while (hit) {                              // a row whose label is an entry of this warp's
+            const int c = __ffs(hit) - 1;
+            hit &= hit - 1;
+            float zc = z[0];
+#pragma unroll
+            for (int k = 1; k < 32; ++k) zc = c == k ? z[k] : zc;
+            if (__shfl_sync(kFull, lab, c) == v) a.zlab[c0 + c] = zc;
+          }
+          float x[32];
+#pragma unroll
+          for (int k = 0; k < 32; ++k) {
+            z[k] = live ? z[k] : -pos_inf();
+            x[k] = z[k] * kLog2e;
+          }
+          const float tm = across(x, lane, [](float f, float g) { return fmaxf(f, g); });
+          const float nm = fmaxf(mx[u], tm), ref = nm > -pos_inf() ? nm : 0.f;
+#pragma unroll
+          for (int k = 0; k < 32; ++k) x[k] = ex2(fmaf(z[k], kLog2e, -__shfl_sync(kFull, ref, k)));
+          const float ts = across(x, lane, [](float f, float g) { return f + g; });
+          sum[u] = (sum[u] > 0.f ? sum[u] * ex2(mx[u] - ref) : 0.f) + ts;
+          mx[u] = nm;
+        } else if (OP == kFewDz) {
+          uint16_t* dst = a.dz + (size_t)c0 * a.Vc + v;
+#pragma unroll
+          for (int k = 0; k < 32; ++k) {
+            const int4 x = s_table[c0 + k];
+            const float pr = (ex2(fmaf(z[k], kLog2e, -__int_as_float(x.y))) - (x.x == v ? 1.f : 0.f)) * __int_as_float(x.z);
+            if (live) dst[(size_t)k * a.Vc] = c0 + k < n ? (uint16_t)pack_bf(pr, 0.f) : (uint16_t)0;
+          }
+        } else {
+          float* dst = a.dh + ((size_t)(t / dt) * a.Rp + c0) * a.d + v;
+#pragma unroll
+          for (int k = 0; k < 32; ++k)
+            if (live && c0 + k < n) {
+              const float y = some ? z[k] : 0.f;
+              dst[(size_t)k * a.d] = first ? y : dst[(size_t)k * a.d] + y;
+            }
+        }
+      }
+    }
+    if (OP == kFewStats) {
+#pragma unroll
+      for (int u = 0; u < 2; ++u) s_red[((warp - 2) * 2 + u) * 32 + lane] = make_float2(mx[u], sum[u]);
+      asm volatile("bar.sync 1, 256;" ::: "memory");
+      // row e: the four warps of its group, quarter by quarter (warps 2..5 or 6..9)
+      if (e < p.cols) {
+        const int g = e >> 5, w = (g & 1) * 4, u = g >> 1;
+        float m = -pos_inf(), s = 0.f;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const float2 x = s_red[((w + k) * 2 + u) * 32 + (e & 31)];
+          fold(m, s, x.x, x.y);
+        }
+        a.part[(size_t)blockIdx.x * a.Rp + e] = make_float2(m, s);
+      }
+    }
+  }
+  if (!ok) atomicOr(a.err, 4u);
+  __syncwarp();
+  tmem_fence_before();
+  cluster_sync_all();
+  tmem_fence_after();
+  if (warp == 1)
+    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tbase), "r"(256) : "memory");
+}
+
+// ---- a row's tiles merged -----------------------------------------------------------
+// Four rows a CTA (32 bytes of each tile's statistics), 64 tiles at a time.
+constexpr int kMergeThreads = 256;
 __global__ void __launch_bounds__(kMergeThreads) head_merge_kernel(const HeadLossArgs a, int parts) {
   __shared__ float s_m[kMergeThreads / 32][4], s_s[kMergeThreads / 32][4];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -620,23 +904,58 @@ bool encode_maps(const HeadLossArgs& a, bool backward, Maps* m) {
 }
 
 // `most`: tiles at most; one pair of CTAs for each two SMs runs through them
-template <int OP>
-cudaError_t launch_pairs(const HeadLossArgs& a, int v0, int vlen, int first, int64_t most, const Maps& maps,
-                         cudaStream_t s) {
-  static unsigned long long done = 0ull;
+template <typename K>
+cudaError_t allow_smem(K kernel, size_t smem, unsigned long long* done, int* pairs) {
   int dev = 0, sms = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
   if (e != cudaSuccess) return e;
   const unsigned long long bit = 1ull << (dev & 63);
-  if (!(__atomic_load_n(&done, __ATOMIC_ACQUIRE) & bit)) {
-    e = cudaFuncSetAttribute(head_pair_kernel<OP>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kPairSmem);
+  if (!(__atomic_load_n(done, __ATOMIC_ACQUIRE) & bit)) {
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e != cudaSuccess) return e;
-    __atomic_fetch_or(&done, bit, __ATOMIC_ACQ_REL);
+    __atomic_fetch_or(done, bit, __ATOMIC_ACQ_REL);
   }
-  int64_t pairs = sms / 2 > 0 ? sms / 2 : 1;
-  if (pairs > most) pairs = most;
+  *pairs = sms / 2 > 0 ? sms / 2 : 1;
+  return cudaSuccess;
+}
+template <int OP>
+cudaError_t launch_pairs(const HeadLossArgs& a, int v0, int vlen, int first, int64_t most, const Maps& maps,
+                         cudaStream_t s) {
+  static unsigned long long done = 0ull;
+  int pairs = 0;
+  const cudaError_t e = allow_smem(head_pair_kernel<OP>, kPairSmem, &done, &pairs);
+  if (e != cudaSuccess) return e;
+  if (pairs > most) pairs = (int)most;
   return launch_early(head_pair_kernel<OP>, (unsigned)(2 * pairs), kPairThreads, kPairSmem, s, a, v0, vlen, first, a.R <= 128 ? box_rows(a) : 128, maps);
+}
+
+// kFewStats, kFewDz: *ctas gets the CTAs, each of which leaves one partial
+// statistic a row (kFewParts at most)
+template <int OP>
+cudaError_t launch_few(const HeadLossArgs& a, int v0, int vlen, int first, int* ctas, cudaStream_t s) {
+  static unsigned long long done = 0ull;
+  int pairs = 0;
+  const cudaError_t e = allow_smem(head_few_kernel<OP>, kFewSmem, &done, &pairs);
+  if (e != cudaSuccess) return e;
+  if (pairs > kFewParts / 2) pairs = kFewParts / 2;
+  FewPlan p;
+  p.cols = (a.R + 31) / 32 * 32;
+  // the vocabulary spread evenly over the pairs' rounds
+  const int64_t wave = (int64_t)pairs * 256, waves = (vlen + wave - 1) / wave;
+  p.height = (int)(((vlen + 2 * pairs * waves - 1) / (2 * pairs * waves) + 7) / 8 * 8);
+  p.tiles = OP == kFewDh ? (int)tiles(a.d, 256) * a.split : (int)tiles(vlen, 2 * p.height);
+  const CUtensorMapDataType t = CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
+  CUtensorMap ma, mb;
+  bool ok = tma_matrix(&ma, t, 2, a.weight, a.d, a.V, OP == kFewDh ? 64 : p.height);
+  if (OP == kFewDh)                                  // (P's entries and rows that were not written read as zeros)
+    ok = ok && tma_matrix(&mb, t, 2, a.dz, vlen, p.cols, p.cols / 2, a.Vc);
+  else
+    ok = ok && tma_matrix(&mb, t, 2, a.packed, a.d, a.Rp, p.cols / 2);
+  if (!ok) return cudaErrorInvalidValue;
+  if (pairs > p.tiles) pairs = p.tiles;
+  if (ctas) *ctas = 2 * pairs;
+  return launch_early(head_few_kernel<OP>, (unsigned)(2 * pairs), kPairThreads, kFewSmem, s, a, p, v0, vlen, first, ma, mb);
 }
 }  // namespace
 
@@ -665,9 +984,13 @@ cudaError_t launch_head_loss(const HeadLossArgs& a, cudaStream_t s) {
   if (!encode_maps(a, false, &maps)) return cudaErrorInvalidValue;
   cudaError_t e = launch_pack(a, s);
   if (e != cudaSuccess) return e;
-  e = launch_pairs<kOpStats>(a, 0, a.V, 1, (int64_t)(a.Rp / kPairTile) * tiles(a.V, kPairTile), maps, s);
+  int parts = (int)tiles(a.V, kHeadPart);
+  if (a.R <= kFewRows)
+    e = launch_few<kFewStats>(a, 0, a.V, 1, &parts, s);
+  else
+    e = launch_pairs<kOpStats>(a, 0, a.V, 1, (int64_t)(a.Rp / kPairTile) * tiles(a.V, kPairTile), maps, s);
   if (e != cudaSuccess) return e;
-  return launch_early(head_merge_kernel, tiles(a.R, 4), kMergeThreads, 0, s, a, (int)tiles(a.V, kHeadPart));
+  return launch_early(head_merge_kernel, tiles(a.R, 4), kMergeThreads, 0, s, a, parts);
 }
 
 cudaError_t launch_head_loss_backward(const HeadLossArgs& a, cudaStream_t s) {
@@ -679,6 +1002,19 @@ cudaError_t launch_head_loss_backward(const HeadLossArgs& a, cudaStream_t s) {
   for (int64_t v0 = 0; v0 < a.V; v0 += a.Vc) {
     const int vlen = (int)min((int64_t)a.Vc, a.V - v0);
     const int64_t vt = tiles(vlen, kPairTile);
+    if (a.R <= kFewRows) {
+      e = launch_few<kFewDz>(a, (int)v0, vlen, 1, nullptr, s);
+      if (e == cudaSuccess && a.d_hidden) e = launch_few<kFewDh>(a, (int)v0, vlen, v0 == 0, nullptr, s);
+      if (e != cudaSuccess) return e;
+      if (!a.d_weight) continue;
+      HeadLossArgs w = a;
+      w.d_hidden = nullptr;
+      if (!tma_matrix(&maps.dz_m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, a.dz, vlen, (a.R + 31) / 32 * 32, 64, a.Vc))
+        return cudaErrorInvalidValue;
+      e = launch_pairs<kOpGrad>(w, (int)v0, vlen, v0 == 0, vt * dt, maps, s);
+      if (e != cudaSuccess) return e;
+      continue;
+    }
     e = launch_pairs<kOpDz>(a, (int)v0, vlen, v0 == 0, mt * vt, maps, s);
     if (e != cudaSuccess) return e;
     const int64_t most = (a.d_hidden ? mt * dt * a.split : 0) + (a.d_weight ? vt * dt : 0);

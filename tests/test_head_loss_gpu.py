@@ -98,7 +98,8 @@ def _check_grads(o, h, w, y, lse, grad, V):
 
 # rows about a tile of 128 and 256, vocabularies about one of 128 and 256, widths about a box of 64
 SIZES = [(1, 8, 2), (1, 64, 128), (2, 72, 257), (33, 136, 1000), (64, 64, 129), (127, 128, 255), (128, 200, 256),
-         (129, 8, 300), (255, 512, 511), (256, 264, 513), (257, 320, 4099), (600, 1040, 770), (5, 2048, 32001)]
+         (129, 8, 300), (255, 512, 511), (256, 264, 513), (257, 320, 4099), (600, 1040, 770), (5, 2048, 32001),
+         (32, 1000, 20000), (96, 96, 5000), (97, 2056, 39001), (16, 704, 1 << 18)]
 
 
 @pytest.mark.parametrize("R,d,V", SIZES)
@@ -128,7 +129,7 @@ def test_one_gradient_alone_is_the_same(cmsd, R, d, V, hidden, weight):
         cmsd.lmhead_loss_backward(h, w, y, lse, g, hidden_grad=False, weight_grad=False)
 
 
-@pytest.mark.parametrize("R,d,V", [(2048, 64, 40000), (1000, 128, 150000)])
+@pytest.mark.parametrize("R,d,V", [(2048, 64, 40000), (1000, 128, 150000), (100, 72, 300001)])
 def test_vocabulary_in_pieces(cmsd, R, d, V):
     """P over the whole vocabulary is over 128 MB: several pieces, the last one short."""
     h, w, y, g = _inputs(R, d, V, ignored=0.1)
