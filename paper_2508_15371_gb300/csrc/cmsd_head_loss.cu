@@ -234,12 +234,10 @@ __device__ __forceinline__ uint32_t pack_bf(float lo, float hi) {
   return r;
 }
 
-// v0, vlen: the piece of the vocabulary; first: the first piece; arows: rows of
-// A's boxes along K (fewer than 128, and none for the second CTA, where there are
-// no more: what lies in the other lanes reaches no result)
+// v0, vlen: the piece of the vocabulary; first: the first piece
 template <int OP>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
-    head_pair_kernel(const HeadLossArgs a, const int v0, const int vlen, const int first, const int arows,
+    head_pair_kernel(const HeadLossArgs a, const int v0, const int vlen, const int first,
                      const __grid_constant__ Maps maps) {
   extern __shared__ __align__(1024) unsigned char pair_smem[];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -283,14 +281,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
     // ---- this CTA's halves of the operands --------------------------------------
     if (lane == 0) {
       const uint32_t full0 = map_to(full, 0);
-      const bool narrow = arows < 128;
-      const uint32_t bytes = narrow ? kStageBytes + (uint32_t)arows * 128 : 2 * kStageBytes;   // of both CTAs
       // One tile of rows: the first tile's weight does not depend on how many
       // there are, nor on the kernel before (which has started, so that what
       // precedes it on the stream has ended).
       const int early = OP != kOpGrad && a.Rp == kPairTile && w0.pair < w0.nt ? min(kStages, w0.kd) : 0;
       for (int s = 0; s < early; ++s) {
-        if (rank == 0) mbar_arrive_tx(full + 8 * s, bytes);
+        if (rank == 0) mbar_arrive_tx(full + 8 * s, 2 * kStageBytes);   // of both CTAs
         tma_box_pair(base + s * kStageBytes + kHalfBytes, &maps.weight_k, s * 64,
                      v0 + w0.pair * kPairTile + (int)rank * 128, full0 + 8 * s);
       }
@@ -305,14 +301,14 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
         for (int kb = 0; kb < t.kb; ++kb, ++g) {
           const int s = g % kStages;
           if (g >= kStages && ok) ok = bar_wait<true>(empty + 8 * s, (uint32_t)((g / kStages - 1) & 1));
-          if (rank == 0 && g >= early) mbar_arrive_tx(full + 8 * s, OP == kOpGrad && t.dw ? 2 * kStageBytes : bytes);
+          if (rank == 0 && g >= early) mbar_arrive_tx(full + 8 * s, 2 * kStageBytes);
           const uint32_t sa = base + s * kStageBytes, sb = sa + kHalfBytes, bar = full0 + 8 * s;
           const int k = (t.k0 + kb) * 64;
           if (OP != kOpGrad) {
-            if (!narrow || rank == 0) tma_box_pair(sa, &maps.rows_k, k, am, bar);
+            tma_box_pair(sa, &maps.rows_k, k, am, bar);
             if (g >= early) tma_box_pair(sb, &maps.weight_k, k, v0 + bn, bar);
           } else if (!t.dw) {
-            if (!narrow || rank == 0) tma_box_pair(sa, &maps.dz_k, k, am, bar);
+            tma_box_pair(sa, &maps.dz_k, k, am, bar);
             tma_box_pair(sb, &maps.weight_n, bn, v0 + k, bar);
             tma_box_pair(sb + kHalfBytes / 2, &maps.weight_n, bn + 64, v0 + k, bar);
           } else {
@@ -511,6 +507,9 @@ __device__ __forceinline__ void fold(float& m, float& s, float m2, float s2) {
 // by halving the rows in play with each exchange, 31 exchanges for 32 rows, which
 // leaves row c with lane c.  All of a pair's tiles are folded before anything is
 // written.
+// The rows are not packed: an ignored row is a column of the MMA that is not
+// read, and a row of zeros in P.  d_weight's product, whose K the rows are, takes
+// a copy of them in which the ignored ones are zeros.
 enum FewOp { kFewStats, kFewDz, kFewDh };
 constexpr int kFewRows = 128;
 constexpr int kFewStages = 9;
@@ -670,18 +669,30 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
     const int q = warp & 3, half = (warp - 2) >> 2, e = tid - 64;
     const uint32_t tempty0 = map_to(tempty, 0);
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    const int n = *a.n;
     if (OP != kFewDh) {
       for (int c = e; c < p.cols; c += 32 * kEpiWarps) {
         int4 x = make_int4(-1, 0, 0, 0);
-        if (c < n) {
-          x.x = a.lab[c] - v0;
+        const int label = c < a.R ? a.labels[c] : a.ignore;
+        if (kept(a, label)) {
+          x.x = label - v0;
+          x.w = 1;
           if (OP == kFewDz) {
-            x.y = __float_as_int(a.plse[c] * kLog2e);
-            x.z = __float_as_int(a.pgrad[c]);
+            x.y = __float_as_int(a.lse_in[c] * kLog2e);
+            x.z = __float_as_int(a.grad[c]);
           }
+        } else if (label != a.ignore && blockIdx.x == 0) {
+          atomicOr(a.err, 1u);
         }
         s_table[c] = x;
+      }
+      if (OP == kFewDz && a.d_weight && first) {     // a CTA a row, and some of zeros
+        for (int r = blockIdx.x; r < (a.R + 63) / 64 * 64; r += gridDim.x) {
+          const bool keep = r < a.R && kept(a, a.labels[r]);
+          const uint4* src = reinterpret_cast<const uint4*>(a.hidden + (size_t)(keep ? r : 0) * a.d);
+          for (int j = e; j < a.d / 8; j += 32 * kEpiWarps)
+            reinterpret_cast<uint4*>(a.packed + (size_t)r * a.d)[j] = keep ? src[j] : make_uint4(0, 0, 0, 0);
+        }
+        if (blockIdx.x == 0 && e == 0) *a.n = a.R;
       }
       asm volatile("bar.sync 1, 256;" ::: "memory");
     }
@@ -739,13 +750,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
           for (int k = 0; k < 32; ++k) {
             const int4 x = s_table[c0 + k];
             const float pr = (ex2(fmaf(z[k], kLog2e, -__int_as_float(x.y))) - (x.x == v ? 1.f : 0.f)) * __int_as_float(x.z);
-            if (live) dst[(size_t)k * a.Vc] = c0 + k < n ? (uint16_t)pack_bf(pr, 0.f) : (uint16_t)0;
+            if (live) dst[(size_t)k * a.Vc] = x.w ? (uint16_t)pack_bf(pr, 0.f) : (uint16_t)0;
           }
         } else {
           float* dst = a.dh + ((size_t)(t / dt) * a.Rp + c0) * a.d + v;
 #pragma unroll
           for (int k = 0; k < 32; ++k)
-            if (live && c0 + k < n) {
+            if (live && c0 + k < a.R) {
               const float y = some ? z[k] : 0.f;
               dst[(size_t)k * a.d] = first ? y : dst[(size_t)k * a.d] + y;
             }
@@ -781,18 +792,23 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
 // ---- a row's tiles merged -----------------------------------------------------------
 // Four rows a CTA (32 bytes of each tile's statistics), 64 tiles at a time.
 constexpr int kMergeThreads = 256;
+// kFew: the rows are not packed
+template <bool kFew>
 __global__ void __launch_bounds__(kMergeThreads) head_merge_kernel(const HeadLossArgs a, int parts) {
   __shared__ float s_m[kMergeThreads / 32][4], s_s[kMergeThreads / 32][4];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
-  const int n = *a.n, p = blockIdx.x * 4 + (tid & 3);
+  const int n = kFew ? a.R : *a.n, p = blockIdx.x * 4 + (tid & 3);
   // ignored rows (each CTA sees to four rows of either kind)
-  if (tid < 4 && p < a.R && a.pos[p] < 0) {
+  const bool gone = p < a.R && (kFew ? !kept(a, a.labels[p]) : a.pos[p] < 0);
+  if (tid < 4 && gone) {
     a.lse[p] = 0.f;
     if (a.loss) a.loss[p] = 0.f;
   }
   if ((int)blockIdx.x * 4 >= n) return;
+  const float zl = tid < 4 && p < n ? a.zlab[p] : 0.f;          // (requested with the statistics)
+  const int r = kFew || p >= n ? p : a.row[p];
   float m = -pos_inf(), s = 0.f;
   if (p < n) {
     constexpr int kBatch = 8;
@@ -819,17 +835,17 @@ __global__ void __launch_bounds__(kMergeThreads) head_merge_kernel(const HeadLos
     s_s[warp][lane] = s;
   }
   __syncthreads();
-  if (tid < 4 && p < n) {
+  if (tid < 4 && p < n && !(kFew && gone)) {
 #pragma unroll
     for (int w = 1; w < kMergeThreads / 32; ++w) fold(m, s, s_m[w][tid], s_s[w][tid]);
     const float lse = m * kLn2 + logf(s);
-    const int r = a.row[p];
     a.lse[r] = lse;
-    if (a.loss) a.loss[r] = lse - a.zlab[p];
+    if (a.loss) a.loss[r] = lse - zl;
   }
 }
 
 // ---- the hidden states' gradient, rounded and put back in place -------------------
+template <bool kFew>
 __global__ void __launch_bounds__(256) head_unpack_kernel(const HeadLossArgs a) {
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
@@ -840,7 +856,7 @@ __global__ void __launch_bounds__(256) head_unpack_kernel(const HeadLossArgs a) 
   for (size_t i0 = warp * 8; i0 < total; i0 += warps * 8) {
     const size_t i = i0 + (lane & 7);
     const int r = i < total ? (int)(i / per) : 0, j = (int)(i - (size_t)r * per) * 4;
-    const int p = i < total ? a.pos[r] : -1;
+    const int p = i < total ? (kFew ? (kept(a, a.labels[r]) ? r : -1) : a.pos[r]) : -1;
     float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
     if (p >= 0) {
       const float* src = a.dh + (size_t)p * a.d + j;
@@ -863,9 +879,11 @@ __global__ void __launch_bounds__(256) head_unpack_kernel(const HeadLossArgs a) 
 }
 
 unsigned tiles(int64_t n, int t) { return (unsigned)((n + t - 1) / t); }
-// a launch that may begin before what precedes it on the stream has ended
+// a launch that may begin before what precedes it on the stream has ended (early:
+// the first launch of a call does not)
 template <typename... P, typename... A>
-cudaError_t launch_early(void (*kernel)(P...), unsigned grid, unsigned threads, size_t smem, cudaStream_t s, A... args) {
+cudaError_t launch(bool early, void (*kernel)(P...), unsigned grid, unsigned threads, size_t smem, cudaStream_t s,
+                   A... args) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(grid);
   cfg.blockDim = dim3(threads);
@@ -875,7 +893,7 @@ cudaError_t launch_early(void (*kernel)(P...), unsigned grid, unsigned threads, 
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = 1;
+  cfg.numAttrs = early ? 1 : 0;
   return cudaLaunchKernelEx(&cfg, kernel, args...);
 }
 cudaError_t launch_pack(const HeadLossArgs& a, cudaStream_t s) {
@@ -886,10 +904,9 @@ cudaError_t launch_pack(const HeadLossArgs& a, cudaStream_t s) {
   return cudaGetLastError();
 }
 
-int box_rows(const HeadLossArgs& a) { return a.R <= 128 ? (a.R + 7) / 8 * 8 : 128; }
 bool encode_maps(const HeadLossArgs& a, bool backward, Maps* m) {
   const CUtensorMapDataType t = CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
-  bool ok = tma_matrix(&m->rows_k, t, 2, a.packed, a.d, a.Rp, box_rows(a)) && tma_matrix(&m->weight_k, t, 2, a.weight, a.d, a.V, 128);
+  bool ok = tma_matrix(&m->rows_k, t, 2, a.packed, a.d, a.Rp, 128) && tma_matrix(&m->weight_k, t, 2, a.weight, a.d, a.V, 128);
   if (!backward) {
     m->rows_n = m->weight_n = m->dz_k = m->dz_m = m->dz_out = m->dw_out = m->dh_out = m->rows_k;   // not read
     return ok;
@@ -899,7 +916,7 @@ bool encode_maps(const HeadLossArgs& a, bool backward, Maps* m) {
   if (a.d_hidden)
     ok = ok && tma_matrix(&m->dh_out, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, a.dh, a.d, (int64_t)a.split * a.Rp, 32);
   return ok && tma_matrix(&m->rows_n, t, 2, a.packed, a.d, a.Rp, 64) && tma_matrix(&m->weight_n, t, 2, a.weight, a.d, a.V, 64) &&
-         tma_matrix(&m->dz_k, t, 2, a.dz, a.Vc, a.Rp, box_rows(a)) && tma_matrix(&m->dz_m, t, 2, a.dz, a.Vc, a.Rp, 64) &&
+         tma_matrix(&m->dz_k, t, 2, a.dz, a.Vc, a.Rp, 128) && tma_matrix(&m->dz_m, t, 2, a.dz, a.Vc, a.Rp, 64) &&
          tma_matrix(&m->dz_out, t, 2, a.dz, a.Vc, a.Rp, 32);
 }
 
@@ -927,13 +944,13 @@ cudaError_t launch_pairs(const HeadLossArgs& a, int v0, int vlen, int first, int
   const cudaError_t e = allow_smem(head_pair_kernel<OP>, kPairSmem, &done, &pairs);
   if (e != cudaSuccess) return e;
   if (pairs > most) pairs = (int)most;
-  return launch_early(head_pair_kernel<OP>, (unsigned)(2 * pairs), kPairThreads, kPairSmem, s, a, v0, vlen, first, a.R <= 128 ? box_rows(a) : 128, maps);
+  return launch(true, head_pair_kernel<OP>, (unsigned)(2 * pairs), kPairThreads, kPairSmem, s, a, v0, vlen, first, maps);
 }
 
 // kFewStats, kFewDz: *ctas gets the CTAs, each of which leaves one partial
 // statistic a row (kFewParts at most)
 template <int OP>
-cudaError_t launch_few(const HeadLossArgs& a, int v0, int vlen, int first, int* ctas, cudaStream_t s) {
+cudaError_t launch_few(bool early, const HeadLossArgs& a, int v0, int vlen, int first, int* ctas, cudaStream_t s) {
   static unsigned long long done = 0ull;
   int pairs = 0;
   const cudaError_t e = allow_smem(head_few_kernel<OP>, kFewSmem, &done, &pairs);
@@ -951,11 +968,11 @@ cudaError_t launch_few(const HeadLossArgs& a, int v0, int vlen, int first, int* 
   if (OP == kFewDh)                                  // (P's entries and rows that were not written read as zeros)
     ok = ok && tma_matrix(&mb, t, 2, a.dz, vlen, p.cols, p.cols / 2, a.Vc);
   else
-    ok = ok && tma_matrix(&mb, t, 2, a.packed, a.d, a.Rp, p.cols / 2);
+    ok = ok && tma_matrix(&mb, t, 2, a.hidden, a.d, a.R, p.cols / 2);
   if (!ok) return cudaErrorInvalidValue;
   if (pairs > p.tiles) pairs = p.tiles;
   if (ctas) *ctas = 2 * pairs;
-  return launch_early(head_few_kernel<OP>, (unsigned)(2 * pairs), kPairThreads, kFewSmem, s, a, p, v0, vlen, first, ma, mb);
+  return launch(early, head_few_kernel<OP>, (unsigned)(2 * pairs), kPairThreads, kFewSmem, s, a, p, v0, vlen, first, ma, mb);
 }
 }  // namespace
 
@@ -980,50 +997,52 @@ int head_split(int Rp, int d, int Vc) {
 }
 
 cudaError_t launch_head_loss(const HeadLossArgs& a, cudaStream_t s) {
+  if (a.R <= kFewRows) {
+    int parts = 0;
+    const cudaError_t e = launch_few<kFewStats>(false, a, 0, a.V, 1, &parts, s);
+    if (e != cudaSuccess) return e;
+    return launch(true, head_merge_kernel<true>, tiles(a.R, 4), kMergeThreads, 0, s, a, parts);
+  }
   Maps maps;
   if (!encode_maps(a, false, &maps)) return cudaErrorInvalidValue;
   cudaError_t e = launch_pack(a, s);
   if (e != cudaSuccess) return e;
-  int parts = (int)tiles(a.V, kHeadPart);
-  if (a.R <= kFewRows)
-    e = launch_few<kFewStats>(a, 0, a.V, 1, &parts, s);
-  else
-    e = launch_pairs<kOpStats>(a, 0, a.V, 1, (int64_t)(a.Rp / kPairTile) * tiles(a.V, kPairTile), maps, s);
+  e = launch_pairs<kOpStats>(a, 0, a.V, 1, (int64_t)(a.Rp / kPairTile) * tiles(a.V, kPairTile), maps, s);
   if (e != cudaSuccess) return e;
-  return launch_early(head_merge_kernel, tiles(a.R, 4), kMergeThreads, 0, s, a, parts);
+  return launch(true, head_merge_kernel<false>, tiles(a.R, 4), kMergeThreads, 0, s, a, (int)tiles(a.V, kHeadPart));
 }
 
 cudaError_t launch_head_loss_backward(const HeadLossArgs& a, cudaStream_t s) {
+  const bool few = a.R <= kFewRows;
   Maps maps;
-  if (!encode_maps(a, true, &maps)) return cudaErrorInvalidValue;
-  cudaError_t e = launch_pack(a, s);
+  cudaError_t e = cudaSuccess;
+  if ((!few || a.d_weight) && !encode_maps(a, true, &maps)) return cudaErrorInvalidValue;
+  if (!few) e = launch_pack(a, s);
   if (e != cudaSuccess) return e;
   const int64_t mt = a.Rp / kPairTile, dt = tiles(a.d, kPairTile);
   for (int64_t v0 = 0; v0 < a.V; v0 += a.Vc) {
-    const int vlen = (int)min((int64_t)a.Vc, a.V - v0);
+    const int vlen = (int)min((int64_t)a.Vc, a.V - v0), first = v0 == 0;
     const int64_t vt = tiles(vlen, kPairTile);
-    if (a.R <= kFewRows) {
-      e = launch_few<kFewDz>(a, (int)v0, vlen, 1, nullptr, s);
-      if (e == cudaSuccess && a.d_hidden) e = launch_few<kFewDh>(a, (int)v0, vlen, v0 == 0, nullptr, s);
-      if (e != cudaSuccess) return e;
-      if (!a.d_weight) continue;
-      HeadLossArgs w = a;
+    HeadLossArgs w = a;
+    if (few) {
+      e = launch_few<kFewDz>(!first, a, (int)v0, vlen, first, nullptr, s);
+      if (e == cudaSuccess && a.d_hidden) e = launch_few<kFewDh>(true, a, (int)v0, vlen, first, nullptr, s);
+      if (e == cudaSuccess && a.d_weight &&
+          !tma_matrix(&maps.dz_m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, a.dz, vlen, (a.R + 31) / 32 * 32, 64, a.Vc))
+        e = cudaErrorInvalidValue;
       w.d_hidden = nullptr;
-      if (!tma_matrix(&maps.dz_m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, a.dz, vlen, (a.R + 31) / 32 * 32, 64, a.Vc))
-        return cudaErrorInvalidValue;
-      e = launch_pairs<kOpGrad>(w, (int)v0, vlen, v0 == 0, vt * dt, maps, s);
-      if (e != cudaSuccess) return e;
-      continue;
+    } else {
+      e = launch_pairs<kOpDz>(a, (int)v0, vlen, first, mt * vt, maps, s);
     }
-    e = launch_pairs<kOpDz>(a, (int)v0, vlen, v0 == 0, mt * vt, maps, s);
     if (e != cudaSuccess) return e;
-    const int64_t most = (a.d_hidden ? mt * dt * a.split : 0) + (a.d_weight ? vt * dt : 0);
-    e = launch_pairs<kOpGrad>(a, (int)v0, vlen, v0 == 0, most, maps, s);
+    const int64_t most = (w.d_hidden ? mt * dt * a.split : 0) + (w.d_weight ? vt * dt : 0);
+    if (most > 0) e = launch_pairs<kOpGrad>(w, (int)v0, vlen, first, most, maps, s);
     if (e != cudaSuccess) return e;
   }
   if (!a.d_hidden) return cudaSuccess;
   const int64_t n4 = (int64_t)a.R * (a.d / 4);
-  return launch_early(head_unpack_kernel, tiles(n4 < 64 * 16384 ? n4 : 64 * 16384, 64), 256, 0, s, a);
+  return launch(true, few ? head_unpack_kernel<true> : head_unpack_kernel<false>,
+                tiles(n4 < 64 * 16384 ? n4 : 64 * 16384, 64), 256, 0, s, a);
 }
 
 }  // namespace cmsd

@@ -108,7 +108,7 @@ def _same(got, want):
 # kept apart
 SIZES = [(1, 16, 2), (1, 128, 256), (2, 144, 257), (16, 1024, 1000), (17, 1040, 4099), (33, 2064, 513),
          (64, 2048, 2000), (65, 112, 255), (127, 1008, 300), (128, 3104, 129), (130, 4096, 1025), (300, 272, 70001),
-         (513, 512, 640)]
+         (513, 512, 640), (20, 4096, 900), (20, 4112, 901), (128, 1024, 33001), (97, 1360, 2500), (3, 65536, 600)]
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
