@@ -231,13 +231,14 @@ cudaError_t launch_quantize(const T* x, int R, int d, int8_t* q, float* scale, c
 // rows scaled by their largest do up to a few thousand entries, no sum with
 // 8-bit weights passes 2^24 and all of K is summed by the tensor cores; else the
 // sums of each 1024 entries (of products of at most 2^14) are added up as 32-bit
-// integers.  Either way the sum is exact.  Only the 8-bit weight is read from memory; its bytes
+// integers, 64 tokens of the tile at a time (the registers hold no more).  Either
+// way the sum is exact.  Only the 8-bit weight is read from memory; its bytes
 // become fp16 on their way into tensor memory, where the MMA takes its A from:
 // byte + 128 is placed into the low mantissa bits of 1024.0, and 1152 is
 // subtracted, both exact.
 //
 // The MMA's M is the vocabulary: a pair of CTAs (cta_group::2) with up to 128
-// entries each, so that a stage of the tokens (N, up to 128 of them, half in each
+// entries each, so that a stage of the tokens (N, up to 192 of them, half in each
 // CTA) is read from L2 once for both.  Each CTA:
 //   warp 0       lane 0 fills a ring with 128 bytes of K of its weight rows;
 //   warp 2       lane 0 another with its half of the tokens' (fp16, from the
@@ -248,27 +249,29 @@ cudaError_t launch_quantize(const T* x, int R, int d, int8_t* q, float* scale, c
 //   warps 12..19 add up, scale and write the sums: thread = one entry, every
 //                second group of 16 tokens.
 // Barriers: wfull / wempty (TMA <-> fp16), hfull / hempty (TMA <-> MMA), afull /
-// aempty (fp16 <-> MMA, four buffers in tensor memory), dfull / dempty (MMA <->
-// sums, two sets of accumulators).  Every wait is bounded.
+// aempty (fp16 <-> MMA, buffers in tensor memory), dfull / dempty (MMA <-> sums,
+// two sets of accumulators).  Every wait is bounded.
 constexpr int kI8Rows = 128;                        // vocabulary entries per CTA and tile at most
 constexpr int kI8K = 128;                           // K per stage
 constexpr int kI8Exact = 1024 / kI8K;               // stages whose sums are exact in fp32 whatever the tokens
 constexpr int kI8Threads = 640;
 constexpr int kI8WStage = kI8Rows * kI8K;
-constexpr int kI8A = 4;                             // buffers of the fp16 weight: 64 columns each
+constexpr int kI8Part = 64;                         // tokens at a time where sums are kept apart
 template <int NT>
 struct I8Shape {
   static constexpr int kHStage = NT / 2 * kI8K * 2; // this CTA's half of the tokens
-  static constexpr int kW = NT == 128 ? 7 : 8;
-  static constexpr int kH = NT == 128 ? 6 : 8;
-  static constexpr int kBars = 2 * kW + 2 * kH + 2 * kI8A + 4;
+  static constexpr int kW = NT == 192 ? 6 : (NT == 128 ? 7 : 8);
+  static constexpr int kH = NT == 192 ? 5 : (NT == 128 ? 6 : 8);
+  static constexpr int kSum = NT == 192 ? 192 : 128;        // columns of an accumulator
+  static constexpr int kA = (512 - 2 * kSum) / 64;  // buffers of the fp16 weight: 64 columns each
+  static constexpr int kBars = 2 * kW + 2 * kH + 2 * kA + 4;
   static constexpr size_t kStageBytes = (size_t)kW * kI8WStage + (size_t)kH * kHStage;
   static constexpr size_t kSmem = 1024 + kStageBytes + 8 * kBars + 16;
   static_assert(kSmem <= 227 * 1024, "shared memory");
 };
 struct I8Plan {
   int height;            // vocabulary entries per CTA and tile
-  int cols;              // tokens per tile (a multiple of 32, at most 128)
+  int cols;              // tokens per tile (a multiple of 32, at most 192)
   int vt, rt;            // tiles (of two CTAs) of the vocabulary and of the tokens
 };
 
@@ -307,28 +310,47 @@ __global__ void __launch_bounds__(kTokenThreads) head_i8_tokens_kernel(const Hea
   }
 }
 
-// Whether a tile of tokens needs the sums of each 1024 entries apart.  The
-// magnitudes are requested a tile ahead; tiles of one round of tokens are alike.
+// Whether a tile of tokens needs the sums of each 1024 entries apart.  Where
+// there are several tiles of tokens the next one's magnitudes are requested a tile
+// ahead (and not later: the loads are volatile).
 struct I8Span {
-  int m[4];
+  int m[6];
+  bool is;
   __device__ __forceinline__ void request(const HeadI8Args& a, const I8Plan& p, int t) {
     const int r0 = t % p.rt * p.cols, lane = threadIdx.x & 31;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < 6; ++i) {
       const int n = lane + 32 * i;
-      m[i] = n < p.cols && r0 + n < a.R ? __ldcg(a.mag + r0 + n) : 0;
+      m[i] = 0;
+      if (n < p.cols && r0 + n < a.R)
+        asm volatile("ld.global.cg.s32 %0, [%1];" : "=r"(m[i]) : "l"(a.mag + r0 + n) : "memory");
     }
   }
-  __device__ __forceinline__ int stages(int ks) const {            // per sum
-    const int most = __reduce_max_sync(kFull, max(max(m[0], m[1]), max(m[2], m[3])));
-    return most <= (1 << 17) ? ks : min(kI8Exact, ks);
+  __device__ __forceinline__ void take() {
+    is = __reduce_max_sync(kFull, max(max(max(m[0], m[1]), max(m[2], m[3])), max(m[4], m[5]))) > (1 << 17);
+  }
+  // the pair's first tile, after the tokens' kernel; each further one
+  __device__ __forceinline__ bool first(const HeadI8Args& a, const I8Plan& p, int t, int pairs) {
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    request(a, p, t);
+    take();
+    if (p.rt > 1) request(a, p, t + pairs);
+    return is;
+  }
+  __device__ __forceinline__ bool next(const HeadI8Args& a, const I8Plan& p, int t, int pairs) {
+    if (p.rt > 1) {
+      take();
+      request(a, p, t + pairs);
+    }
+    return is;
   }
 };
 
+// map_h, map_p: the tokens in boxes of half a tile, of half a part
 template <int NT, bool kBf16>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kI8Threads, 1)
     head_i8_kernel(const HeadI8Args a, const I8Plan p, const __grid_constant__ CUtensorMap map_w,
-                   const __grid_constant__ CUtensorMap map_h) {
+                   const __grid_constant__ CUtensorMap map_h, const __grid_constant__ CUtensorMap map_p) {
   using S = I8Shape<NT>;
   extern __shared__ __align__(1024) unsigned char i8_smem[];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -338,8 +360,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kI8Threads, 1)
   const uint32_t bars = base + (uint32_t)S::kStageBytes;
   const uint32_t wfull = bars, wempty = wfull + 8 * S::kW;
   const uint32_t hfull = wempty + 8 * S::kW, hempty = hfull + 8 * S::kH;
-  const uint32_t afull = hempty + 8 * S::kH, aempty = afull + 8 * kI8A;
-  const uint32_t dfull = aempty + 8 * kI8A, dempty = dfull + 16;
+  const uint32_t afull = hempty + 8 * S::kH, aempty = afull + 8 * S::kA;
+  const uint32_t dfull = aempty + 8 * S::kA, dempty = dfull + 16;
   uint32_t* s_taddr = reinterpret_cast<uint32_t*>(i8_smem + (bars - raw) + 8 * S::kBars);
   if (tid == 0) {
     for (int k = 0; k < S::kW; ++k) {
@@ -350,7 +372,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kI8Threads, 1)
       mbar_init(hfull + 8 * k, 1);
       mbar_init(hempty + 8 * k, 1);
     }
-    for (int b = 0; b < kI8A; ++b) {
+    for (int b = 0; b < S::kA; ++b) {
       mbar_init(afull + 8 * b, 16);                 // the turning warps of both CTAs
       mbar_init(aempty + 8 * b, 1);
     }
@@ -369,81 +391,107 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kI8Threads, 1)
   tmem_fence_before();
   cluster_sync_all();
   tmem_fence_after();
-  const uint32_t tbase = *s_taddr;                  // two sets of 128 columns of sums
-  const uint32_t abase = tbase + 256;               // kI8A buffers of 64 columns
-  const int ks = (a.d + kI8K - 1) / kI8K;           // stages per tile
+  const uint32_t tbase = *s_taddr;                  // two accumulators
+  const uint32_t abase = tbase + 2 * S::kSum;       // kA buffers of 64 columns
+  const int ks = (a.d + kI8K - 1) / kI8K;           // stages per pass
   const int tiles = p.vt * p.rt;
   const int mine = tiles > pair ? (tiles - pair + pairs - 1) / pairs : 0;
+  const int parts = (p.cols + kI8Part - 1) / kI8Part;
+  const int part_cols = min(p.cols, kI8Part);
+  // A tile takes one pass over K, or one for each part of its tokens.
+  I8Span span;
   bool ok = true;
 
   if (warp == 0) {
-    // The weight does not wait for the tokens' kernel: that one has started, so
-    // what precedes it on the stream has ended.
-    if (lane == 0) {
-      const uint32_t bytes = (uint32_t)(p.height * kI8K);
-      int g = 0;
-      for (int i = 0; i < mine; ++i) {
-        const int y = ((pair + i * pairs) / p.rt * 2 + rank) * p.height;
-        for (int k = 0; k < ks; ++k, ++g) {
-          const int s = g % S::kW;
-          if (g >= S::kW && ok) ok = bar_wait<false>(wempty + 8 * s, (uint32_t)((g / S::kW - 1) & 1));
-          mbar_arrive_tx(wfull + 8 * s, bytes);
-          tma_box(base + s * kI8WStage, &map_w, k * kI8K, y, wfull + 8 * s);
+    // The weight's first stages do not wait for the tokens' kernel: that one has
+    // started, so what precedes it on the stream has ended.
+    const uint32_t bytes = (uint32_t)(p.height * kI8K);
+    int s = 0, g = 0;
+    uint32_t phase = 1;                             // (of the round before: a new barrier's is over)
+    for (int i = 0; i < mine; ++i) {
+      const int y = ((pair + i * pairs) / p.rt * 2 + rank) * p.height;
+      int passes = 1;
+      for (int j = 0; j < passes; ++j) {
+        if (lane == 0) {
+          for (int k = 0; k < ks; ++k, ++g) {
+            if (ok) ok = bar_wait<false>(wempty + 8 * s, phase);
+            mbar_arrive_tx(wfull + 8 * s, bytes);
+            tma_box(base + s * kI8WStage, &map_w, k * kI8K, y, wfull + 8 * s);
+            if (++s == S::kW) {
+              s = 0;
+              phase ^= 1;
+            }
+          }
+        }
+        __syncwarp();
+        if (j == 0) {                               // how often the tile's weight is wanted
+          const int t = pair + i * pairs;
+          passes = (i == 0 ? span.first(a, p, t, pairs) : span.next(a, p, t, pairs)) ? parts : 1;
         }
       }
-      // nothing is in flight into this CTA when it ends
-      for (int k = (g > S::kW ? g - S::kW : 0); k < g; ++k)
-        if (ok) ok = bar_wait<false>(wempty + 8 * (k % S::kW), (uint32_t)((k / S::kW) & 1));
     }
+    g = __shfl_sync(kFull, g, 0);
+    // nothing is in flight into this CTA when it ends
+    for (int k = (g > S::kW ? g - S::kW : 0); k < g; ++k)
+      if (ok) ok = bar_wait<false>(wempty + 8 * (k % S::kW), (uint32_t)((k / S::kW) & 1));
   } else if (warp == 2) {
-    if (lane == 0) {
-      const uint32_t bytes = (uint32_t)(p.cols * kI8K * 2);  // both halves
-      const int half = p.cols / 2;
-      const uint32_t hfull0 = map_to(hfull, 0);
-      asm volatile("griddepcontrol.wait;" ::: "memory");
-      asm volatile("fence.proxy.async.global;" ::: "memory");
-      int g = 0;
-      for (int i = 0; i < mine; ++i) {
-        const int y = (pair + i * pairs) % p.rt * p.cols + rank * half;
-        for (int k = 0; k < ks; ++k, ++g) {
-          const int s = g % S::kH;
-          if (g >= S::kH && ok) ok = bar_wait<true>(hempty + 8 * s, (uint32_t)((g / S::kH - 1) & 1));
-          if (rank == 0) mbar_arrive_tx(hfull + 8 * s, bytes);
-          const uint32_t dst = hbase + s * S::kHStage;
-          tma_box_pair(dst, &map_h, k * kI8K, y, hfull0 + 8 * s);
-          tma_box_pair(dst + half * 128, &map_h, k * kI8K + 64, y, hfull0 + 8 * s);
+    const uint32_t hfull0 = map_to(hfull, 0);
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("fence.proxy.async.global;" ::: "memory");
+    int s = 0, g = 0;
+    uint32_t phase = 1;
+    for (int i = 0; i < mine; ++i) {
+      const int t = pair + i * pairs;
+      const bool apart = i == 0 ? span.first(a, p, t, pairs) : span.next(a, p, t, pairs);
+      const int passes = apart ? parts : 1, cols = apart ? part_cols : p.cols, half = cols / 2;
+      const CUtensorMap* map = apart ? &map_p : &map_h;
+      for (int j = 0; j < passes; ++j) {
+        const int y = t % p.rt * p.cols + j * kI8Part + rank * half;
+        if (lane == 0) {
+          for (int k = 0; k < ks; ++k, ++g) {
+            if (ok) ok = bar_wait<true>(hempty + 8 * s, phase);
+            if (rank == 0) mbar_arrive_tx(hfull + 8 * s, (uint32_t)(cols * kI8K * 2));   // both halves
+            const uint32_t dst = hbase + s * S::kHStage;
+            tma_box_pair(dst, map, k * kI8K, y, hfull0 + 8 * s);
+            tma_box_pair(dst + half * 128, map, k * kI8K + 64, y, hfull0 + 8 * s);
+            if (++s == S::kH) {
+              s = 0;
+              phase ^= 1;
+            }
+          }
         }
+        __syncwarp();
       }
-      for (int k = (g > S::kH ? g - S::kH : 0); k < g; ++k)
-        if (ok) ok = bar_wait<true>(hempty + 8 * (k % S::kH), (uint32_t)((k / S::kH) & 1));
     }
+    g = __shfl_sync(kFull, g, 0);
+    for (int k = (g > S::kH ? g - S::kH : 0); k < g; ++k)
+      if (ok) ok = bar_wait<true>(hempty + 8 * (k % S::kH), (uint32_t)((k / S::kH) & 1));
   } else if (warp == 1) {
     // the whole warp runs through the stages, so that what the MMAs take is
     // formed in uniform registers; one lane issues
     if (rank == 0) {
       const bool leader = elect_lane();
-      const uint32_t idesc = mma_idesc(256, p.cols, false, false, false);
-      const uint32_t half = (uint32_t)p.cols * 64 >> 4;      // the second 64 of K, in units of 16 bytes
       const uint32_t hempty0 = map_to(hempty, 0), hempty1 = map_to(hempty, 1);
       const uint32_t aempty0 = map_to(aempty, 0), aempty1 = map_to(aempty, 1);
       const uint32_t dfull0 = map_to(dfull, 0), dfull1 = map_to(dfull, 1);
-      int c = 0, s = 0, g = 0;                      // sums handed over; ring slot; stage
-      uint32_t phase = 0;
-      asm volatile("griddepcontrol.wait;" ::: "memory");
-      I8Span span;
-      span.request(a, p, pair);
+      int c = 0, s = 0, b = 0;                      // sums handed over; ring slot; buffer
+      uint32_t phase = 0, aphase = 0;
       for (int i = 0; i < mine; ++i) {
-        const int len = span.stages(ks);
-        span.request(a, p, pair + (i + 1) * pairs);
-        for (int k = 0, part = 0; k < ks; ++k, ++g) {
-          const int b = g % kI8A, db = c & 1;
+        const int t = pair + i * pairs;
+        const bool apart = i == 0 ? span.first(a, p, t, pairs) : span.next(a, p, t, pairs);
+        const int len = apart ? min(kI8Exact, ks) : ks, steps = (apart ? parts : 1) * ks;
+        const uint32_t cols = (uint32_t)(apart ? part_cols : p.cols);
+        const uint32_t idesc = mma_idesc(256, 0, false, false, false) | (cols >> 3) << 17;
+        const uint32_t half = cols * 64 >> 4;       // the second 64 of K, in units of 16 bytes
+        for (int g = 0, k = 0, part = 0; g < steps; ++g) {
+          const int db = c & 1;
           const bool ends = part == len - 1 || k == ks - 1;
           if (part == 0 && c >= 2 && ok) ok = bar_wait<true>(dempty + 8 * db, (uint32_t)((c / 2 - 1) & 1));
           if (ok) ok = bar_wait<true>(hfull + 8 * s, phase);
-          if (ok) ok = bar_wait<true>(afull + 8 * b, (uint32_t)((g / kI8A) & 1));
+          if (ok) ok = bar_wait<true>(afull + 8 * b, aphase);
           tmem_fence_after();
           const uint64_t h0 = mma_desc(hbase + s * S::kHStage, 0), h1 = h0 + half;
-          const uint32_t d = tbase + db * 128, at = abase + b * 64;
+          const uint32_t d = tbase + db * S::kSum, at = abase + b * 64;
           if (leader) {
 #pragma unroll
             for (int j = 0; j < kI8K / 16; ++j)
@@ -461,9 +509,14 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kI8Threads, 1)
           __syncwarp();
           c += ends;
           part = ends ? 0 : part + 1;
+          if (++k == ks) k = 0;
           if (++s == S::kH) {
             s = 0;
             phase ^= 1;
+          }
+          if (++b == S::kA) {
+            b = 0;
+            aphase ^= 1;
           }
         }
       }
@@ -475,114 +528,148 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kI8Threads, 1)
     const uint32_t quarter = (uint32_t)(q * 32) << 16;
     const uint32_t wrow = (uint32_t)row * 128, x8 = (uint32_t)(row & 7);
     const uint32_t afull0 = map_to(afull, 0);
-    const int G = mine * ks;
-    int s = 0;
-    uint32_t phase = 0;
-    for (int g = 0; g < G; ++g) {
-      const int b = g % kI8A;
-      if (ok) ok = bar_wait<false>(wfull + 8 * s, phase);
-      __syncwarp();
-      const uint32_t src = base + s * kI8WStage + wrow;
-      uint32_t o[32];
+    int s = 0, b = 0, g = 0;
+    uint32_t phase = 0, aphase = 1;
+    // the first pass does not wait for the tokens' kernel
+    for (int i = 0, left = mine > 0 ? ks : 0; left > 0;) {
+      do {
+        if (ok) ok = bar_wait<false>(wfull + 8 * s, phase);
+        __syncwarp();
+        const uint32_t src = base + s * kI8WStage + wrow;
+        uint32_t o[32];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        uint32_t w0, w1, w2, w3;
-        asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];"
-                     : "=r"(w0), "=r"(w1), "=r"(w2), "=r"(w3)
-                     : "r"(src + (((uint32_t)(4 * half + j) ^ x8) << 4)));
-        i8_to_half(w0, o[8 * j], o[8 * j + 1]);
-        i8_to_half(w1, o[8 * j + 2], o[8 * j + 3]);
-        i8_to_half(w2, o[8 * j + 4], o[8 * j + 5]);
-        i8_to_half(w3, o[8 * j + 6], o[8 * j + 7]);
-      }
-      __syncwarp();
-      if (lane == 0) mbar_arrive_local(wempty + 8 * s);      // (its bytes are in registers)
-      if (g >= kI8A && ok) ok = bar_wait<true>(aempty + 8 * b, (uint32_t)((g / kI8A - 1) & 1));
-      __syncwarp();
-      tmem_fence_after();
-      tmem_st32(abase + quarter + b * 64 + half * 32, o);
-      tmem_st_wait();
-      tmem_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive_cluster(afull0 + 8 * b);
-      if (++s == S::kW) {
-        s = 0;
-        phase ^= 1;
-      }
+        for (int j = 0; j < 4; ++j) {
+          uint32_t w0, w1, w2, w3;
+          asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];"
+                       : "=r"(w0), "=r"(w1), "=r"(w2), "=r"(w3)
+                       : "r"(src + (((uint32_t)(4 * half + j) ^ x8) << 4)));
+          i8_to_half(w0, o[8 * j], o[8 * j + 1]);
+          i8_to_half(w1, o[8 * j + 2], o[8 * j + 3]);
+          i8_to_half(w2, o[8 * j + 4], o[8 * j + 5]);
+          i8_to_half(w3, o[8 * j + 6], o[8 * j + 7]);
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive_local(wempty + 8 * s);    // (its bytes are in registers)
+        if (ok) ok = bar_wait<true>(aempty + 8 * b, aphase);
+        __syncwarp();
+        tmem_fence_after();
+        tmem_st32(abase + quarter + b * 64 + half * 32, o);
+        tmem_st_wait();
+        tmem_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive_cluster(afull0 + 8 * b);
+        if (++s == S::kW) {
+          s = 0;
+          phase ^= 1;
+        }
+        if (++b == S::kA) {
+          b = 0;
+          aphase ^= 1;
+        }
+        ++g;
+      } while (--left > 0);
+      if (g == ks && span.first(a, p, pair, pairs)) left = ks * (parts - 1);
+      if (left == 0 && ++i < mine) left = span.next(a, p, pair + i * pairs, pairs) ? ks * parts : ks;
     }
     // the last arrivals at this CTA's barriers are in before it ends
-    for (int g = (G > kI8A ? G - kI8A : 0); g < G; ++g)
-      if (ok) ok = bar_wait<true>(aempty + 8 * (g % kI8A), (uint32_t)((g / kI8A) & 1));
+    const int G = g;
+    for (g = (G > S::kA ? G - S::kA : 0); g < G; ++g)
+      if (ok) ok = bar_wait<true>(aempty + 8 * (g % S::kA), (uint32_t)((g / S::kA) & 1));
   } else if (warp >= 12) {
     const int q = warp & 3, set = (warp - 12) >> 2;
     const int row = q * 32 + lane;
     const uint32_t quarter = (uint32_t)(q * 32) << 16;
     const uint32_t dempty0 = map_to(dempty, 0);
     constexpr int kMine = NT / 32;                  // this set's groups of 16 tokens (every second one)
+    const size_t step = (size_t)a.V * (kBf16 ? 2 : 4);
     int c = 0;
-    asm volatile("griddepcontrol.wait;" ::: "memory");
-    I8Span span;
-    span.request(a, p, pair);
     for (int i = 0; i < mine; ++i) {
       const int t = pair + i * pairs;
+      const bool apart = i == 0 ? span.first(a, p, t, pairs) : span.next(a, p, t, pairs);
       const int vi = t / p.rt, r0 = (t - vi * p.rt) * p.cols, v = (vi * 2 + rank) * p.height + row;
       const bool in = row < p.height && v < a.V;
-      const int len = span.stages(ks), sums = (ks + len - 1) / len;
-      span.request(a, p, t + pairs);
-      float ws = 0.f, hs[kMine];
+      float ws = 0.f, hs[kMine];                    // lane l: the scale of token 32 u + l
 #pragma unroll
       for (int u = 0; u < kMine; ++u) hs[u] = __ldg(a.hidden_scale + min(r0 + 32 * u + lane, a.R - 1));
       if (in) ws = __ldg(a.weight_scale + v);
-      int acc[16 * kMine];
-#pragma unroll
-      for (int n = 0; n < 16 * kMine; ++n) acc[n] = 0;
-#pragma unroll 1
-      for (int k = 0; k < sums; ++k, ++c) {
-        if (ok) ok = bar_wait<true>(dfull + 8 * (c & 1), (uint32_t)((c / 2) & 1));
-        __syncwarp();
-        tmem_fence_after();
-        const uint32_t src = tbase + quarter + (c & 1) * 128 + 16 * set;
-#pragma unroll
-        for (int u = 0; u < kMine; ++u) {
-          if (16 * (2 * u + set) < p.cols) {
-            float y[16];
-            tmem_ld16_ahead(src + 32 * u, y);
-            tmem_ld_wait(y);
-            if (sums == 1) {                        // the sum itself
-#pragma unroll
-              for (int j = 0; j < 16; ++j) acc[16 * u + j] = __float_as_int(y[j]);
-            } else {
-#pragma unroll
-              for (int j = 0; j < 16; ++j) acc[16 * u + j] += __float2int_rn(y[j]);
-            }
-          }
-        }
-        tmem_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive_cluster(dempty0 + 8 * (c & 1));
-      }
-      if (sums > 1) {
-#pragma unroll
-        for (int n = 0; n < 16 * kMine; ++n) acc[n] = __float_as_int((float)acc[n]);
-      }
-      char* out = reinterpret_cast<char*>(a.logits) + ((size_t)(r0 + 16 * set) * a.V + v) * (kBf16 ? 2 : 4);
-      const size_t step = (size_t)a.V * (kBf16 ? 2 : 4);
-      const int rows = in ? min(a.R - r0, p.cols) - 16 * set : 0;           // of this set's first group on
-#pragma unroll
-      for (int u = 0; u < kMine; ++u) {
+      const int rows = in ? min(a.R - r0, p.cols) : 0;
+      // 16 tokens' logits from n on
+      auto write = [&](const float (&y)[16], float scales, int n) {
+        char* out = reinterpret_cast<char*>(a.logits) + ((size_t)(r0 + n) * a.V + v) * (kBf16 ? 2 : 4);
 #pragma unroll
         for (int j = 0; j < 16; ++j) {
-          const float h = __shfl_sync(kFull, hs[u], 16 * set + j);
-          if (32 * u + j < rows) {
-            const float y = __int_as_float(acc[16 * u + j]) * h * ws;
+          const float h = __shfl_sync(kFull, scales, 16 * set + j);
+          if (n + j < rows) {
+            const float z = y[j] * h * ws;
             if (kBf16)
-              *reinterpret_cast<__nv_bfloat16*>(out) = __float2bfloat16_rn(y);
+              *reinterpret_cast<__nv_bfloat16*>(out) = __float2bfloat16_rn(z);
             else
-              *reinterpret_cast<float*>(out) = y;
+              *reinterpret_cast<float*>(out) = z;
           }
           out += step;
         }
-        out += 16 * step;
+      };
+      auto sum_wait = [&]() {
+        if (ok) ok = bar_wait<true>(dfull + 8 * (c & 1), (uint32_t)((c / 2) & 1));
+        __syncwarp();
+        tmem_fence_after();
+      };
+      auto sum_done = [&]() {
+        tmem_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive_cluster(dempty0 + 8 * (c & 1));
+        ++c;
+      };
+      if (!apart) {
+        sum_wait();
+        const uint32_t src = tbase + quarter + (c & 1) * S::kSum + 16 * set;
+#pragma unroll
+        for (int u = 0; u < kMine; ++u) {
+          const int n = 16 * (2 * u + set);
+          float y[16];
+          if (n < p.cols) {
+            tmem_ld16_ahead(src + 32 * u, y);
+            tmem_ld_wait(y);
+          }
+          if (n < p.cols && n + 32 >= p.cols) sum_done();     // (this set's last)
+          if (n < p.cols) write(y, hs[u], n);
+        }
+        continue;
+      }
+      const int len = min(kI8Exact, ks), sums = (ks + len - 1) / len;
+#pragma unroll
+      for (int j = 0; j < (NT + kI8Part - 1) / kI8Part; ++j) {
+        if (j < parts) {
+          int acc[2][16];
+#pragma unroll
+          for (int n = 0; n < 32; ++n) acc[n / 16][n % 16] = 0;
+#pragma unroll 1
+          for (int k = 0; k < sums; ++k) {
+            sum_wait();
+            const uint32_t src = tbase + quarter + (c & 1) * S::kSum + 16 * set;
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+              if (16 * (2 * u + set) < part_cols) {
+                float y[16];
+                tmem_ld16_ahead(src + 32 * u, y);
+                tmem_ld_wait(y);
+#pragma unroll
+                for (int n = 0; n < 16; ++n) acc[u][n] += __float2int_rn(y[n]);
+              }
+            }
+            sum_done();
+          }
+#pragma unroll
+          for (int u = 0; u < 2; ++u) {
+            const int n = j * kI8Part + 16 * (2 * u + set);
+            if (2 * j + u < kMine && n < p.cols) {
+              float y[16];
+#pragma unroll
+              for (int m = 0; m < 16; ++m) y[m] = (float)acc[u][m];
+              write(y, hs[2 * j + u < kMine ? 2 * j + u : 0], n);
+            }
+          }
+        }
       }
     }
   }
@@ -597,7 +684,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kI8Threads, 1)
 
 template <int NT, bool kBf16>
 cudaError_t launch_i8(const HeadI8Args& a, const I8Plan& p, int grid, int dev, const CUtensorMap& mw,
-                      const CUtensorMap& mh, cudaStream_t s) {
+                      const CUtensorMap& mh, const CUtensorMap& mp, cudaStream_t s) {
   static unsigned long long done = 0ull;
   const unsigned long long bit = 1ull << (dev & 63);
   if (!(__atomic_load_n(&done, __ATOMIC_ACQUIRE) & bit)) {
@@ -616,14 +703,15 @@ cudaError_t launch_i8(const HeadI8Args& a, const I8Plan& p, int grid, int dev, c
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, head_i8_kernel<NT, kBf16>, a, p, mw, mh);
+  return cudaLaunchKernelEx(&cfg, head_i8_kernel<NT, kBf16>, a, p, mw, mh, mp);
 }
 template <bool kBf16>
 cudaError_t launch_i8_cols(const HeadI8Args& a, const I8Plan& p, int grid, int dev, const CUtensorMap& mw,
-                           const CUtensorMap& mh, cudaStream_t s) {
-  if (p.cols <= 32) return launch_i8<32, kBf16>(a, p, grid, dev, mw, mh, s);
-  if (p.cols <= 64) return launch_i8<64, kBf16>(a, p, grid, dev, mw, mh, s);
-  return launch_i8<128, kBf16>(a, p, grid, dev, mw, mh, s);
+                           const CUtensorMap& mh, const CUtensorMap& mp, cudaStream_t s) {
+  if (p.cols <= 32) return launch_i8<32, kBf16>(a, p, grid, dev, mw, mh, mp, s);
+  if (p.cols <= 64) return launch_i8<64, kBf16>(a, p, grid, dev, mw, mh, mp, s);
+  if (p.cols <= 128) return launch_i8<128, kBf16>(a, p, grid, dev, mw, mh, mp, s);
+  return launch_i8<192, kBf16>(a, p, grid, dev, mw, mh, mp, s);
 }
 }  // namespace
 
@@ -640,7 +728,7 @@ cudaError_t launch_head_i8(const HeadI8Args& a, cudaStream_t s) {
   if (sms < 1) sms = 1;
   const int64_t pairs = sms / 2 > 0 ? sms / 2 : 1;
   I8Plan p;
-  p.rt = (a.R + 127) / 128;
+  p.rt = (a.R + 191) / 192;
   p.cols = ((a.R + p.rt - 1) / p.rt + 31) / 32 * 32;
   p.rt = (a.R + p.cols - 1) / p.cols;
   // one tile of tokens: the weight is streamed once, so its rows are spread
@@ -648,9 +736,10 @@ cudaError_t launch_head_i8(const HeadI8Args& a, cudaStream_t s) {
   const int64_t wave = pairs * 2 * kI8Rows, waves = (a.V + wave - 1) / wave;
   p.height = p.rt > 1 ? kI8Rows : (int)(((a.V + 2 * pairs * waves - 1) / (2 * pairs * waves) + 3) / 4 * 4);
   p.vt = (int)((a.V + 2 * (int64_t)p.height - 1) / (2 * p.height));
-  CUtensorMap mw, mh;
+  CUtensorMap mw, mh, mp;
   if (!tma_matrix(&mw, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, a.weight, a.d, a.V, p.height) ||
-      !tma_matrix(&mh, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, a.h16, a.d, a.R, p.cols / 2))
+      !tma_matrix(&mh, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, a.h16, a.d, a.R, p.cols / 2) ||
+      !tma_matrix(&mp, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, a.h16, a.d, a.R, (p.cols < kI8Part ? p.cols : kI8Part) / 2))
     return cudaErrorInvalidValue;
   head_i8_tokens_kernel<<<a.R < 65536 ? a.R : 65536, kTokenThreads, 0, s>>>(a);
   e = cudaGetLastError();
@@ -658,7 +747,7 @@ cudaError_t launch_head_i8(const HeadI8Args& a, cudaStream_t s) {
   const int64_t tiles = (int64_t)p.vt * p.rt;
   if (tiles + pairs >= (1ll << 31)) return cudaErrorInvalidValue;   // (64 TB of logits)
   const int grid = (int)(2 * (tiles < pairs ? tiles : pairs));
-  return a.dtype == 0 ? launch_i8_cols<false>(a, p, grid, dev, mw, mh, s) : launch_i8_cols<true>(a, p, grid, dev, mw, mh, s);
+  return a.dtype == 0 ? launch_i8_cols<false>(a, p, grid, dev, mw, mh, mp, s) : launch_i8_cols<true>(a, p, grid, dev, mw, mh, mp, s);
 }
 
 }  // namespace cmsd

@@ -104,10 +104,10 @@ def _same(got, want):
     assert not bad.any(), (int(bad.sum()), torch.nonzero(bad)[:4].tolist())
 
 
-# rows about 16, 32, 64, 128; vocabularies about 128 and 256; widths about 128 and about 1024, whose sums are
+# rows about 16, 32, 64, 128, 192; vocabularies about 128 and 256; widths about 128 and about 1024, whose sums are
 # kept apart
 SIZES = [(1, 16, 2), (1, 128, 256), (2, 144, 257), (16, 1024, 1000), (17, 1040, 4099), (33, 2064, 513),
-         (64, 2048, 2000), (65, 112, 255), (127, 1008, 300), (128, 3104, 129), (130, 4096, 1025), (300, 272, 70001),
+         (64, 2048, 2000), (65, 112, 255), (127, 1008, 300), (128, 3104, 129), (130, 4096, 1025), (300, 272, 70001), (192, 256, 1000), (193, 256, 999), (385, 144, 500),
          (513, 512, 640), (20, 4096, 900), (20, 4112, 901), (128, 1024, 33001), (97, 1360, 2500), (3, 65536, 600)]
 
 
@@ -139,7 +139,8 @@ def test_largest_sums(cmsd, d):
     _same(cmsd.lmhead_i8(hq, one, wq, onev, dtype=torch.float32)["logits"], _logits(hq, one, wq, onev, torch.float32))
 
 
-@pytest.mark.parametrize("R,d,V", [(300, 2576, 1500), (40, 1536, 40000), (129, 8192, 700)])
+@pytest.mark.parametrize("R,d,V", [(300, 2576, 1500), (40, 1536, 40000), (129, 8192, 700), (191, 1200, 900),
+                                   (600, 1296, 3000), (90, 2064, 45000)])
 def test_large_tokens_among_small_ones(cmsd, R, d, V):
     """Tokens whose magnitudes add up to more than 2^17, just to it, and to less, in one tile and in others."""
     hq, wq = _ints(R, d, 9), _ints(V, d, 10, full=True)
