@@ -212,20 +212,23 @@ int cmsd_lmhead_confidence(const void* hidden, const void* weight, int R, int d,
  *   lse_r  = log sum_v exp(z_rv)
  *   loss_r = lse_r - z_r,label(r)
  *   hidden: bf16 [R][d], weight: bf16 [V][d], device, row-major, 16-byte
- *     aligned; d a multiple of 8, 8 <= d <= 2^20; 2 <= V; R*V < 2^46; R == 0 is
- *     a valid empty call (its workspace is that of R = 1).  Entries of kept rows
- *     and of the weight must be finite.
+ *     aligned; d a multiple of 8, 8 <= d <= 2^20; 2 <= V <= 2^30; R <= 2^28; R*V,
+ *     R*d and V*d below 2^46; R == 0 is a valid empty call (its workspace is that
+ *     of R = 1).  Entries of kept rows and of the weight must be finite.
  *   labels: int32 [R] device.  A row whose label is ignore_index is ignored
- *     (prompt or padding): its hidden state is not used, whatever it holds, it
- *     costs no products, and its loss and lse are 0.  ignore_index may be any
- *     number, an entry of the vocabulary too.  Another label outside [0, V) is
- *     ignored as well and sets bit 0 of the workspace's error word.
+ *     (prompt or padding): its hidden state reaches no result, whatever it holds,
+ *     it costs no products where there are more than 128 rows, and its loss and
+ *     lse are 0.  ignore_index may be any number, an entry of the vocabulary too.
+ *     Another label outside [0, V) is ignored as well and sets bit 0 of the
+ *     workspace's error word.
  *   loss, lse: float [R] device; loss may be NULL.  lse is what
  *     cmsd_lmhead_loss_backward takes.
  *   ws: cmsd_lmhead_loss_workspace_bytes(R, d, V) bytes, 16-byte aligned, on the
  *     current device.  It needs no initialisation but for the error word, which
  *     cmsd_workspace_init zeroes and cmsd_workspace_errors reads (bit 0 as
  *     above; bit 2: a wait inside a kernel gave up, the results are void).
+ * Outputs and workspace share no bytes with each other or with an input
+ * (CMSD_EINVAL), here and in the three entry points below.
  * Products are of exact bf16 values, accumulated in fp32 in an order that does
  * not depend on other rows' contents; equal calls give equal results.
  */
@@ -260,7 +263,7 @@ int cmsd_lmhead_loss_backward(const void* hidden, const void* weight, const int3
  * A row of zeros gives q 0 and scale 0; a row with an infinity or a NaN gives q 0
  * and that infinity or a NaN as its scale, so that products with it show it.
  *   x: dtype [R][d] device, row-major, 16-byte aligned; d a multiple of 16,
- *   16 <= d <= 65536; R*d < 2^46; q: int8 [R][d], 16-byte aligned; scale: float
+ *   16 <= d <= 65536; R*d below 2^46; q: int8 [R][d], 16-byte aligned; scale: float
  *   [R].  R == 0 is a valid empty call.
  */
 int cmsd_quantize_rows(const void* x, int dtype, int R, int d, int8_t* q, float* scale, void* stream);
@@ -272,8 +275,8 @@ int cmsd_quantize_rows(const void* x, int dtype, int R, int d, int8_t* q, float*
  * rounded to dtype (CMSD_F32 or CMSD_BF16) once.
  *   hidden_q: int8 [R][d], weight_q: int8 [V][d], device, row-major, 16-byte
  *     aligned, any values of the type; d a multiple of 16, 16 <= d <= 65536;
- *     2 <= V; R*V < 2^46; R == 0 is a valid empty call (its workspace is that of
- *     R = 1).  hidden_scale: float [R], weight_scale: float [V], device.
+ *     2 <= V <= 2^30; R <= 2^28; R*V, R*d and V*d below 2^46; R == 0 is a valid
+ *     empty call (its workspace is that of R = 1).  hidden_scale: float [R], weight_scale: float [V], device.
  *   logits: dtype [R][V] device, 16-byte aligned: what cmsd_confidence and its
  *     companions read with R = B*K.
  *   ws: cmsd_lmhead_i8_workspace_bytes(R, d, V) bytes, 16-byte aligned, on the

@@ -612,9 +612,30 @@ int lm_layout(int R, int V, LmLayout* L) {
 // Workspaces of the head's loss: the error word at offset 0, then the packed
 // rows; the forward pass's partial statistics or the backward pass's piece.
 int check_head(int R, int d, int V, int step, int most) {
-  if (R < 0 || d < step || d % step != 0 || d > most || V < 2) return CMSD_EINVAL;
-  if ((double)R * (double)V >= 70368744177664.0) return CMSD_EINVAL;   // 2^46 logits
+  if (R < 0 || R > (1 << 28) || d < step || d % step != 0 || d > most || V < 2 || V > (1 << 30)) return CMSD_EINVAL;
+  const double limit = 70368744177664.0;                               // 2^46 logits, entries
+  if ((double)R * V >= limit || (double)R * d >= limit || (double)V * d >= limit) return CMSD_EINVAL;
   return CMSD_OK;
+}
+bool aligned4(const void* p) { return ((uintptr_t)p & 3u) == 0; }
+// [a, a + na) and [b, b + nb) have bytes in common (null: none)
+bool overlap(const void* a, size_t na, const void* b, size_t nb) {
+  return a && b && (uintptr_t)a < (uintptr_t)b + nb && (uintptr_t)b < (uintptr_t)a + na;
+}
+struct Span {
+  const void* p;
+  size_t n;
+};
+// an output that shares bytes with an input, the workspace or another output
+template <size_t N, size_t M>
+bool outputs_overlap(const Span (&out)[N], const Span (&in)[M]) {
+  for (size_t i = 0; i < N; ++i) {
+    for (size_t j = 0; j < M; ++j)
+      if (overlap(out[i].p, out[i].n, in[j].p, in[j].n)) return true;
+    for (size_t j = 0; j < i; ++j)
+      if (overlap(out[i].p, out[i].n, out[j].p, out[j].n)) return true;
+  }
+  return false;
 }
 int check_loss(int R, int d, int V) { return check_head(R, d, V, 8, 1 << 20); }
 int check_i8(int R, int d, int V) { return check_head(R, d, V, 16, 1 << 16); }
@@ -757,11 +778,16 @@ int cmsd_lmhead_loss(const void* hidden, const void* weight, const int32_t* labe
   if (rc) return rc;
   if (R == 0) return CMSD_OK;
   if (!hidden || !weight || !labels || !lse) return CMSD_EINVAL;
-  if (!aligned16(hidden) || !aligned16(weight)) return CMSD_EALIGN;
+  if (!aligned16(hidden) || !aligned16(weight) || !aligned4(labels) || !aligned4(loss) || !aligned4(lse))
+    return CMSD_EALIGN;
   HeadLossArgs a = {};
   a.R = R; a.d = d; a.V = V; a.ignore = ignore_index;
-  if (!ws || ws_bytes < loss_layout(a, false, nullptr)) return CMSD_ENOWS;
+  const size_t need = loss_layout(a, false, nullptr), r4 = (size_t)R * 4;
+  if (!ws || ws_bytes < need) return CMSD_ENOWS;
   if (!aligned16(ws)) return CMSD_EALIGN;
+  if (outputs_overlap({{loss, r4}, {lse, r4}, {ws, need}},
+                      {{hidden, (size_t)R * d * 2}, {weight, (size_t)V * d * 2}, {labels, r4}}))
+    return CMSD_EINVAL;
   loss_layout(a, false, (char*)ws);
   a.hidden = (const uint16_t*)hidden;
   a.weight = (const uint16_t*)weight;
@@ -792,11 +818,18 @@ int cmsd_lmhead_loss_backward(const void* hidden, const void* weight, const int3
     return e == cudaSuccess ? CMSD_OK : cuda_fail(e);
   }
   if (!hidden || !weight || !labels || !lse || !grad_loss) return CMSD_EINVAL;
-  if (!aligned16(hidden) || !aligned16(weight) || (d_hidden && !aligned16(d_hidden))) return CMSD_EALIGN;
+  if (!aligned16(hidden) || !aligned16(weight) || !aligned16(d_hidden) || !aligned4(labels) || !aligned4(lse) ||
+      !aligned4(grad_loss))
+    return CMSD_EALIGN;
   HeadLossArgs a = {};
   a.R = R; a.d = d; a.V = V; a.ignore = ignore_index;
-  if (!ws || ws_bytes < loss_layout(a, true, nullptr)) return CMSD_ENOWS;
+  const size_t need = loss_layout(a, true, nullptr), r4 = (size_t)R * 4;
+  const size_t hb = (size_t)R * d * 2, wb = (size_t)V * d * 2;
+  if (!ws || ws_bytes < need) return CMSD_ENOWS;
   if (!aligned16(ws)) return CMSD_EALIGN;
+  if (outputs_overlap({{d_hidden, hb}, {d_weight, wb}, {ws, need}},
+                      {{hidden, hb}, {weight, wb}, {labels, r4}, {lse, r4}, {grad_loss, r4}}))
+    return CMSD_EINVAL;
   loss_layout(a, true, (char*)ws);
   a.hidden = (const uint16_t*)hidden;
   a.weight = (const uint16_t*)weight;
@@ -811,10 +844,13 @@ int cmsd_lmhead_loss_backward(const void* hidden, const void* weight, const int3
 
 int cmsd_quantize_rows(const void* x, int dtype, int R, int d, int8_t* q, float* scale, void* stream) {
   if (dtype != CMSD_F32 && dtype != CMSD_BF16) return CMSD_EDTYPE;
-  if (R < 0 || d < 16 || d % 16 != 0 || d > (1 << 16)) return CMSD_EINVAL;
+  if (R < 0 || d < 16 || d % 16 != 0 || d > (1 << 16) || (double)R * d >= 70368744177664.0) return CMSD_EINVAL;
   if (R == 0) return CMSD_OK;
   if (!x || !q || !scale) return CMSD_EINVAL;
-  if (!aligned16(x) || !aligned16(q)) return CMSD_EALIGN;
+  if (!aligned16(x) || !aligned16(q) || !aligned4(scale)) return CMSD_EALIGN;
+  if (outputs_overlap({{q, (size_t)R * d}, {scale, (size_t)R * 4}},
+                      {{x, (size_t)R * d * (dtype == CMSD_F32 ? 4 : 2)}}))
+    return CMSD_EINVAL;
   const cudaError_t e = launch_quantize_rows(x, dtype, R, d, q, scale, (cudaStream_t)stream);
   return e == cudaSuccess ? CMSD_OK : cuda_fail(e);
 }
@@ -834,11 +870,18 @@ int cmsd_lmhead_i8(const int8_t* hidden_q, const float* hidden_scale, const int8
   if (rc) return rc;
   if (R == 0) return CMSD_OK;
   if (!hidden_q || !hidden_scale || !weight_q || !weight_scale || !logits) return CMSD_EINVAL;
-  if (!aligned16(hidden_q) || !aligned16(weight_q) || !aligned16(logits)) return CMSD_EALIGN;
+  if (!aligned16(hidden_q) || !aligned16(weight_q) || !aligned16(logits) || !aligned4(hidden_scale) ||
+      !aligned4(weight_scale))
+    return CMSD_EALIGN;
   HeadI8Args a = {};
   a.R = R; a.d = d; a.V = V; a.dtype = dtype;
-  if (!ws || ws_bytes < i8_layout(a, nullptr)) return CMSD_ENOWS;
+  const size_t need = i8_layout(a, nullptr);
+  if (!ws || ws_bytes < need) return CMSD_ENOWS;
   if (!aligned16(ws)) return CMSD_EALIGN;
+  if (outputs_overlap({{logits, (size_t)R * V * (dtype == CMSD_F32 ? 4 : 2)}, {ws, need}},
+                      {{hidden_q, (size_t)R * d}, {weight_q, (size_t)V * d}, {hidden_scale, (size_t)R * 4},
+                       {weight_scale, (size_t)V * 4}}))
+    return CMSD_EINVAL;
   i8_layout(a, (char*)ws);
   a.hidden = hidden_q;
   a.weight = weight_q;

@@ -533,6 +533,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kI8Threads, 1)
     // the first pass does not wait for the tokens' kernel
     for (int i = 0, left = mine > 0 ? ks : 0; left > 0;) {
       do {
+        if (ok) ok = bar_wait<true>(aempty + 8 * b, aphase);
         if (ok) ok = bar_wait<false>(wfull + 8 * s, phase);
         __syncwarp();
         const uint32_t src = base + s * kI8WStage + wrow;
@@ -550,8 +551,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kI8Threads, 1)
         }
         __syncwarp();
         if (lane == 0) mbar_arrive_local(wempty + 8 * s);    // (its bytes are in registers)
-        if (ok) ok = bar_wait<true>(aempty + 8 * b, aphase);
-        __syncwarp();
         tmem_fence_after();
         tmem_st32(abase + quarter + b * 64 + half * 32, o);
         tmem_st_wait();

@@ -8,7 +8,8 @@ import pytest
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 PKG = os.path.join(ROOT, "paper_2508_15371_gb300")
-A = 4096            # an address that nothing reads: every call here is refused
+A = 4096            # addresses that nothing reads: every call here is refused
+H, W, Y, X1, X2, O1, O2, WS = (A + (k << 32) for k in range(8))      # far enough apart
 
 
 @pytest.fixture(scope="module")
@@ -21,27 +22,28 @@ def cmsd():
     return c
 
 
-def _loss(c, R=4, d=64, V=100, hidden=A, weight=A, labels=A, loss=A, lse=A, ws=A, ws_bytes=None):
+def _loss(c, R=4, d=64, V=100, hidden=H, weight=W, labels=Y, loss=O1, lse=O2, ws=WS, ws_bytes=None):
     n = c.lib().cmsd_lmhead_loss_workspace_bytes(R, d, V) if ws_bytes is None else ws_bytes
     return c.lib().cmsd_lmhead_loss(hidden, weight, labels, R, d, V, -100, loss, lse, ws, n, None)
 
 
-def _back(c, R=4, d=64, V=100, hidden=A, weight=A, labels=A, lse=A, grad=A, dh=A, dw=A, ws=A, ws_bytes=None):
+def _back(c, R=4, d=64, V=100, hidden=H, weight=W, labels=Y, lse=X1, grad=X2, dh=O1, dw=O2, ws=WS, ws_bytes=None):
     n = c.lib().cmsd_lmhead_loss_backward_workspace_bytes(R, d, V) if ws_bytes is None else ws_bytes
     return c.lib().cmsd_lmhead_loss_backward(hidden, weight, labels, lse, grad, R, d, V, -100, dh, dw, ws, n, None)
 
 
-def _i8(c, R=4, d=64, V=100, h=A, hs=A, w=A, wsc=A, out=A, dtype=1, ws=A, ws_bytes=None):
+def _i8(c, R=4, d=64, V=100, h=H, hs=X1, w=W, wsc=X2, out=O1, dtype=1, ws=WS, ws_bytes=None):
     n = c.lib().cmsd_lmhead_i8_workspace_bytes(R, d, V) if ws_bytes is None else ws_bytes
     return c.lib().cmsd_lmhead_i8(h, hs, w, wsc, R, d, V, out, dtype, ws, n, None)
 
 
-def _quant(c, R=4, d=64, x=A, q=A, scale=A, dtype=1):
+def _quant(c, R=4, d=64, x=H, q=O1, scale=O2, dtype=1):
     return c.lib().cmsd_quantize_rows(x, dtype, R, d, q, scale, None)
 
 
 @pytest.mark.parametrize("kw", [dict(R=-1), dict(d=0), dict(d=4), dict(d=12), dict(d=(1 << 20) + 8), dict(V=1),
-                                dict(R=1 << 23, V=1 << 23)])
+                                dict(R=1 << 23, V=1 << 23), dict(R=(1 << 28) + 1), dict(V=(1 << 30) + 1),
+                                dict(R=1 << 27, d=1 << 20), dict(V=1 << 27, d=1 << 20)])
 def test_loss_sizes_refused(cmsd, kw):
     assert _loss(cmsd, **kw) == cmsd.EINVAL
     assert _back(cmsd, **kw) == cmsd.EINVAL
@@ -56,6 +58,8 @@ def test_loss_pointers_refused(cmsd):
         assert _loss(cmsd, **{name: None}) == cmsd.EINVAL, name
     for name in ("hidden", "weight", "ws"):
         assert _loss(cmsd, **{name: A + 8}) == cmsd.EALIGN, name
+    for name in ("labels", "loss", "lse"):
+        assert _loss(cmsd, **{name: A + 2}) == cmsd.EALIGN, name
     assert _loss(cmsd, ws=None) == cmsd.ENOWS
     n = cmsd.lib().cmsd_lmhead_loss_workspace_bytes(4, 64, 100)
     assert _loss(cmsd, ws_bytes=n - 1) == cmsd.ENOWS
@@ -67,6 +71,8 @@ def test_backward_pointers_refused(cmsd):
         assert _back(cmsd, **{name: None}) == cmsd.EINVAL, name
     for name in ("hidden", "weight", "dh", "dw", "ws"):
         assert _back(cmsd, **{name: A + 8}) == cmsd.EALIGN, name
+    for name in ("labels", "lse", "grad"):
+        assert _back(cmsd, **{name: A + 2}) == cmsd.EALIGN, name
     assert _back(cmsd, dh=None, dw=None) == cmsd.EINVAL
     assert _back(cmsd, R=0, dh=None, dw=None) == cmsd.EINVAL
     assert _back(cmsd, R=0, dw=None) == cmsd.OK
@@ -79,6 +85,8 @@ def test_backward_pointers_refused(cmsd):
 @pytest.mark.parametrize("kw,code", [
     (dict(R=-1), "EINVAL"), (dict(d=8), "EINVAL"), (dict(d=24), "EINVAL"), (dict(d=(1 << 16) + 16), "EINVAL"),
     (dict(V=1), "EINVAL"), (dict(R=1 << 23, V=1 << 23), "EINVAL"), (dict(dtype=2), "EDTYPE"),
+    (dict(R=(1 << 28) + 1), "EINVAL"), (dict(V=(1 << 30) + 1), "EINVAL"), (dict(hs=A + 2), "EALIGN"),
+    (dict(wsc=A + 1), "EALIGN"),
     (dict(h=None), "EINVAL"), (dict(hs=None), "EINVAL"), (dict(w=None), "EINVAL"), (dict(wsc=None), "EINVAL"),
     (dict(out=None), "EINVAL"), (dict(h=A + 8), "EALIGN"), (dict(w=A + 4), "EALIGN"), (dict(out=A + 2), "EALIGN"),
     (dict(ws=None), "ENOWS"), (dict(ws_bytes=16), "ENOWS"), (dict(ws=A + 8), "EALIGN"),
@@ -90,9 +98,26 @@ def test_i8_refused(cmsd, kw, code):
 @pytest.mark.parametrize("kw,code", [
     (dict(R=-1), "EINVAL"), (dict(d=8), "EINVAL"), (dict(d=40), "EINVAL"), (dict(d=(1 << 16) + 16), "EINVAL"),
     (dict(dtype=-1), "EDTYPE"), (dict(x=None), "EINVAL"), (dict(q=None), "EINVAL"), (dict(scale=None), "EINVAL"),
+    (dict(R=1 << 30, d=1 << 16), "EINVAL"), (dict(scale=A + 2), "EALIGN"),
     (dict(x=A + 8), "EALIGN"), (dict(q=A + 4), "EALIGN"), (dict(R=0, x=None, q=None, scale=None), "OK")])
 def test_quantize_refused(cmsd, kw, code):
     assert _quant(cmsd, **kw) == getattr(cmsd, code)
+
+
+def test_outputs_share_no_bytes(cmsd):
+    """An output in an input's, the workspace's or another output's place, or on its last or first bytes."""
+    R, d, V = 4, 64, 100
+    hb, wb, ib = R * d * 2, V * d * 2, R * d
+    for kw in (dict(lse=Y), dict(loss=O2), dict(lse=O1 + R * 4 - 4), dict(loss=H + hb - 4), dict(lse=WS), dict(ws=W)):
+        assert _loss(cmsd, **kw) == cmsd.EINVAL, kw
+    for kw in (dict(dh=H), dict(dw=W), dict(dw=H - 16), dict(dh=W + wb - 16), dict(dh=O2 + 16), dict(ws=O1), dict(dh=X1),
+               dict(dw=WS + 256)):
+        assert _back(cmsd, **kw) == cmsd.EINVAL, kw
+    assert _back(cmsd, dw=None, dh=H) == cmsd.EINVAL
+    for kw in (dict(out=H), dict(out=W), dict(out=X1 - 16), dict(out=WS), dict(ws=X2)):
+        assert _i8(cmsd, **kw) == cmsd.EINVAL, kw
+    for kw in (dict(q=H), dict(q=H + hb - 16), dict(scale=H), dict(scale=O1 + ib - 4)):
+        assert _quant(cmsd, **kw) == cmsd.EINVAL, kw
 
 
 def test_workspaces_do_not_hold_the_logits(cmsd):

@@ -202,6 +202,45 @@ def test_guard_bands_streams_and_graph(cmsd):
         _same(out, _logits(r["q"], r["scale"], wq, wsc, torch.float32))
 
 
+@pytest.mark.parametrize("R,d,V", [(40, 2576, 1500), (300, 2576, 1500)])
+def test_a_graph_replayed_with_larger_and_smaller_tokens(cmsd, R, d, V):
+    """What the tokens hold decides how sums are formed: not what they held at the capture."""
+    wq = _ints(V, d, 12, full=True)
+    small, large = _ints(R, d, 13).clamp_(-20, 20), _ints(R, d, 14, full=True)
+    large[::2] = 127
+    hq = small.clone()
+    hs, wsc = torch.rand(R, device="cuda"), torch.rand(V, device="cuda")
+    out = {"logits": torch.empty(R, V, device="cuda")}
+    ws = cmsd.lmhead_i8_workspace(R, d, V)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        cmsd.lmhead_i8(hq, hs, wq, wsc, dtype=torch.float32, out=out, ws=ws)
+    for src in (small, large, small, large):
+        hq.copy_(src)
+        graph.replay()
+        torch.cuda.synchronize()
+        _same(out["logits"], _logits(src, hs, wq, wsc, torch.float32))
+    assert cmsd.workspace_errors(ws) == 0
+
+
+def test_calls_at_once_on_two_streams(cmsd):
+    sizes = [(20, 512, 4000), (260, 272, 3000)]
+    data = [(_ints(R, d, 1), torch.rand(R, device="cuda"), _ints(V, d, 2), torch.rand(V, device="cuda"))
+            for R, d, V in sizes]
+    spaces = [cmsd.lmhead_i8_workspace(*z) for z in sizes]
+    want = [_logits(*x, torch.bfloat16) for x in data]
+    streams = [torch.cuda.Stream() for _ in sizes]
+    torch.cuda.synchronize()
+    got = []
+    for _ in range(20):
+        for i, st in enumerate(streams):
+            with torch.cuda.stream(st):
+                got.append((i, cmsd.lmhead_i8(*data[i], ws=spaces[i])["logits"]))
+    torch.cuda.synchronize()
+    for i, z in got:
+        _same(z, want[i])
+
+
 def test_offsets_past_32_bits(cmsd):
     """2.6 G logits, and 2.2 G numbers quantised."""
     R, d, V = 20000, 16, 128256

@@ -325,6 +325,59 @@ def test_equal_calls_on_streams_and_in_a_graph(cmsd):
             assert torch.equal(out[k], ref[k]), k
 
 
+def test_calls_at_once_on_two_streams(cmsd):
+    """Each with its own workspace; both kinds of kernels, many times over."""
+    sizes = [(70, 256, 3000), (700, 136, 2500)]
+    data = [_inputs(R, d, V, ignored=0.3) for R, d, V in sizes]
+    streams = [torch.cuda.Stream() for _ in sizes]
+
+    def step(i, wf, wb):
+        h, w, y, g = data[i]
+        o = cmsd.lmhead_loss(h, w, y, ws=wf)
+        o.update(cmsd.lmhead_loss_backward(h, w, y, o["lse"], g, ws=wb))
+        return o
+
+    spaces = [(cmsd.lmhead_loss_workspace(*z), cmsd.lmhead_loss_backward_workspace(*z)) for z in sizes]
+    want = [step(i, *spaces[i]) for i in range(2)]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(20):
+        for i, st in enumerate(streams):
+            with torch.cuda.stream(st):
+                got[i].append(step(i, *spaces[i]))
+    torch.cuda.synchronize()
+    for i in range(2):
+        for o in got[i]:
+            assert all(torch.equal(o[k], want[i][k]) for k in want[i])
+        assert cmsd.workspace_errors(spaces[i][0]) == 0 and cmsd.workspace_errors(spaces[i][1]) == 0
+
+
+@pytest.mark.parametrize("R", [6, 200])
+def test_without_the_loss(cmsd, R):
+    """lse alone, as a gradient needs it."""
+    h, w, y, _ = _inputs(R, 64, 500, ignored=0.3)
+    want = cmsd.lmhead_loss(h, w, y)["lse"]
+    ws = cmsd.lmhead_loss_workspace(R, 64, 500)
+    lse = torch.full((R,), 9.0, device="cuda")
+    rc = cmsd.lib().cmsd_lmhead_loss(h.data_ptr(), w.data_ptr(), y.data_ptr(), R, 64, 500, IGNORE, None, lse.data_ptr(),
+                                     ws.data_ptr(), ws.numel(), cmsd._stream())
+    assert rc == cmsd.OK and torch.equal(lse, want)
+
+
+def test_binding_refuses_on_the_device(cmsd):
+    h, w, y, g = _inputs(8, 64, 300)
+    lse = cmsd.lmhead_loss(h, w, y)["lse"]
+    small = cmsd.lmhead_loss_workspace(8, 64, 300)[:64]
+    wide = torch.zeros(8, 128, dtype=torch.bfloat16, device="cuda")
+    for call in (lambda: cmsd.lmhead_loss(wide[:, :64], w, y), lambda: cmsd.lmhead_loss(h, w, y.cpu()),
+                 lambda: cmsd.lmhead_loss(h, w, y, ws=small), lambda: cmsd.lmhead_loss(h, w, y, ws=small.cpu()),
+                 lambda: cmsd.lmhead_loss_backward(h, w, y, lse, g, out={"d_hidden": h}),
+                 lambda: cmsd.lmhead_loss_backward(h, w, y, lse, g, out={"d_weight": w}),
+                 lambda: cmsd.lmhead_loss(h.reshape(-1)[4:4 + 7 * 64].view(7, 64), w, y[:7])):
+        with pytest.raises(cmsd.CmsdError):
+            call()
+
+
 def test_offsets_past_32_bits(cmsd):
     """A weight of 2.4 G entries (4.9 GB): rows from its far end."""
     R, d, V = 3, 8192, 300000
