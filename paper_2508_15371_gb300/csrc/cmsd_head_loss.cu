@@ -53,6 +53,14 @@ __global__ void __launch_bounds__(kPackThreads) head_pack_kernel(const HeadLossA
     return;
   }
   const int r0 = blockIdx.x * rows, r1 = min(a.R, r0 + rows);
+  // a warp's first row is requested before its place is known
+  constexpr int kAhead = 8;
+  const int vecs = a.d / 8;
+  uint4 v[kAhead];
+  const uint4* ahead = reinterpret_cast<const uint4*>(a.hidden + (size_t)min(r0 + warp, a.R - 1) * a.d);
+#pragma unroll
+  for (int u = 0; u < kAhead; ++u)
+    if (lane + 32 * u < vecs) v[u] = ahead[lane + 32 * u];
   int base = count_kept(a, r0);
   for (int r = r0; r < r1; r += kPackWarps) {
     // every warp knows the places of the group's rows
@@ -80,8 +88,14 @@ __global__ void __launch_bounds__(kPackThreads) head_pack_kernel(const HeadLossA
       const int p = base + __popc(k & ((1u << warp) - 1u));
       const uint4* src = reinterpret_cast<const uint4*>(a.hidden + (size_t)row * a.d);
       uint4* dst = reinterpret_cast<uint4*>(a.packed + (size_t)p * a.d);
+      int j = lane;
+      if (r == r0) {
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u, j += 32)
+          if (j < vecs) dst[j] = v[u];
+      }
 #pragma unroll 4
-      for (int j = lane; j < a.d / 8; j += 32) dst[j] = src[j];
+      for (; j < vecs; j += 32) dst[j] = src[j];
     }
     base += __popc(k);
   }
@@ -98,6 +112,8 @@ __global__ void __launch_bounds__(kPackThreads) head_pack_kernel(const HeadLossA
 //   logits   A = packed rows, B = weight, K = d; both rows of 128 bytes along K
 //   d_hidden A = P, B = weight (its rows run along N), K = the piece's entries
 //   d_weight A = P (its rows run along M), B = packed rows (along N), K = rows
+// (kOpFewGrad, with few rows: d_hidden has A = weight (along M = d), B = P, N the
+// rows.)
 // One pair runs through its share of the tiles, which are dealt out ahead:
 //   warp 0      lane 0 fills the ring of stages (TMA), each CTA its own halves,
 //               counted at the first CTA's barrier;
@@ -107,7 +123,8 @@ __global__ void __launch_bounds__(kPackThreads) head_pack_kernel(const HeadLossA
 // Barriers: full (TMA -> MMA), empty (MMA -> TMA, in both CTAs), tfull (MMA ->
 // epilogue, in both) and tempty (both epilogues -> MMA) for each of the two
 // accumulators.  Every wait is bounded.
-enum Op { kOpStats, kOpDz, kOpGrad };
+enum Op { kOpStats, kOpDz, kOpGrad, kOpFewGrad };
+__host__ __device__ constexpr bool grad_op(int op) { return op == kOpGrad || op == kOpFewGrad; }
 constexpr int kPairTile = kHeadTile;
 constexpr int kStages = 6;
 constexpr int kHalfBytes = 128 * 128;                 // 128 rows of 64 bf16
@@ -140,14 +157,16 @@ struct Work {
 // Tiles of the logits go round the pairs with the rows first, so that pairs
 // running together share the weight's tile and the packed rows.  Tiles of
 // d_hidden, the longer ones, go round first; pairs with one of them less then
-// take `boost` tiles of d_weight more, and the rest goes round.
+// take `boost` tiles of d_weight more, and the rest goes round.  With few rows
+// d_hidden's tiles read the weight and d_weight's are all writing, so every second
+// pair runs through its tiles from the end.
 template <int OP>
 __device__ __forceinline__ Work work_of(const HeadLossArgs& a, int n, int vlen, bool want_h, bool want_w) {
   Work w;
   w.pairs = gridDim.x / 2;
   w.pair = blockIdx.x / 2;
-  const int rows = max(1, (n + kPairTile - 1) / kPairTile);
-  if (OP != kOpGrad) {
+  const int rows = OP == kOpFewGrad ? 1 : max(1, (n + kPairTile - 1) / kPairTile);
+  if (!grad_op(OP)) {
     w.mt = rows;
     w.nt = (vlen + kPairTile - 1) / kPairTile;
     w.kd = (a.d + 63) / 64;
@@ -166,7 +185,8 @@ __device__ __forceinline__ Work work_of(const HeadLossArgs& a, int n, int vlen, 
   w.mine_h = w.nh / w.pairs + (w.pair < rem ? 1 : 0);
   w.lead = rem > 0 && w.pair >= rem ? w.pairs - rem : 0;      // this pair catches up with so many others
   const int behind = rem > 0 ? w.pairs - rem : 0;
-  int boost = behind > 0 ? (w.kd + w.kw / 2) / w.kw : 0;
+  const int cost = OP == kOpFewGrad ? w.kw + 4 : w.kw;        // of a tile of d_weight, with few rows its writing
+  int boost = behind > 0 ? (w.kd + cost / 2) / cost : 0;
   if ((long long)boost * behind > nw) boost = behind > 0 ? (nw + behind - 1) / behind : 0;
   const int early = min(nw, boost * behind);
   w.boost = 0;
@@ -186,10 +206,11 @@ __device__ __forceinline__ Work work_of(const HeadLossArgs& a, int n, int vlen, 
 template <int OP>
 __device__ __forceinline__ Tile tile_of(const HeadLossArgs& a, const Work& w, int i) {
   Tile t;
+  if (OP == kOpFewGrad && (w.pair & 1)) i = w.total - 1 - i;
   t.dw = false;
   t.part = 0;
   t.k0 = 0;
-  if (OP != kOpGrad) {
+  if (!grad_op(OP)) {
     const int j = w.pair + i * w.pairs;
     t.n = j / w.mt;
     t.m = j - t.n * w.mt;
@@ -234,10 +255,11 @@ __device__ __forceinline__ uint32_t pack_bf(float lo, float hi) {
   return r;
 }
 
-// v0, vlen: the piece of the vocabulary; first: the first piece
+// v0, vlen: the piece of the vocabulary; first: the first piece; cols: kOpFewGrad's
+// rows, a multiple of 32
 template <int OP>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
-    head_pair_kernel(const HeadLossArgs a, const int v0, const int vlen, const int first,
+    head_pair_kernel(const HeadLossArgs a, const int v0, const int vlen, const int first, const int cols,
                      const __grid_constant__ Maps maps) {
   extern __shared__ __align__(1024) unsigned char pair_smem[];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -284,7 +306,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
       // One tile of rows: the first tile's weight does not depend on how many
       // there are, nor on the kernel before (which has started, so that what
       // precedes it on the stream has ended).
-      const int early = OP != kOpGrad && a.Rp == kPairTile && w0.pair < w0.nt ? min(kStages, w0.kd) : 0;
+      const int early = !grad_op(OP) && a.Rp == kPairTile && w0.pair < w0.nt ? min(kStages, w0.kd) : 0;
       for (int s = 0; s < early; ++s) {
         if (rank == 0) mbar_arrive_tx(full + 8 * s, 2 * kStageBytes);   // of both CTAs
         tma_box_pair(base + s * kStageBytes + kHalfBytes, &maps.weight_k, s * 64,
@@ -301,12 +323,17 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
         for (int kb = 0; kb < t.kb; ++kb, ++g) {
           const int s = g % kStages;
           if (g >= kStages && ok) ok = bar_wait<true>(empty + 8 * s, (uint32_t)((g / kStages - 1) & 1));
-          if (rank == 0 && g >= early) mbar_arrive_tx(full + 8 * s, 2 * kStageBytes);
+          if (rank == 0 && g >= early)
+            mbar_arrive_tx(full + 8 * s, OP == kOpFewGrad && !t.dw ? 2 * kHalfBytes + (uint32_t)cols * 128 : 2 * kStageBytes);
           const uint32_t sa = base + s * kStageBytes, sb = sa + kHalfBytes, bar = full0 + 8 * s;
           const int k = (t.k0 + kb) * 64;
-          if (OP != kOpGrad) {
+          if (!grad_op(OP)) {
             tma_box_pair(sa, &maps.rows_k, k, am, bar);
             if (g >= early) tma_box_pair(sb, &maps.weight_k, k, v0 + bn, bar);
+          } else if (OP == kOpFewGrad && !t.dw) {
+            tma_box_pair(sa, &maps.weight_n, bn, v0 + k, bar);
+            tma_box_pair(sa + kHalfBytes / 2, &maps.weight_n, bn + 64, v0 + k, bar);
+            tma_box_pair(sb, &maps.dz_k, k, (int)rank * (cols / 2), bar);
           } else if (!t.dw) {
             tma_box_pair(sa, &maps.dz_k, k, am, bar);
             tma_box_pair(sb, &maps.weight_n, bn, v0 + k, bar);
@@ -338,11 +365,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
         if (i >= 2 && ok) ok = bar_wait<true>(tempty + 8 * b, (uint32_t)((i / 2 - 1) & 1));
         tmem_fence_after();
         const uint32_t d = tbase + (uint32_t)(b * 256);
-        const uint32_t idesc = OP != kOpGrad ? mma_idesc(256, 256, true, false, false)
-                                             : (t.dw ? mma_idesc(256, 256, true, true, true)
-                                                     : mma_idesc(256, 256, true, false, true));
+        const bool few = OP == kOpFewGrad && !t.dw;
+        const uint32_t idesc = !grad_op(OP) ? mma_idesc(256, 256, true, false, false)
+                                            : (t.dw ? mma_idesc(256, 256, true, true, true)
+                                                    : (few ? mma_idesc(256, cols, true, true, false)
+                                                           : mma_idesc(256, 256, true, false, true)));
         // K = 16 further: 32 bytes along the rows, or 16 rows
-        const uint64_t da = OP == kOpGrad && t.dw ? 2048 >> 4 : 32 >> 4, db = OP == kOpGrad ? 2048 >> 4 : 32 >> 4;
+        const uint64_t da = grad_op(OP) && (t.dw || few) ? 2048 >> 4 : 32 >> 4, db = grad_op(OP) && !few ? 2048 >> 4 : 32 >> 4;
         for (int kb = 0; kb < t.kb; ++kb, ++g) {
           const int s = g % kStages;
           if (ok) ok = bar_wait<true>(full + 8 * s, (uint32_t)((g / kStages) & 1));
@@ -399,12 +428,34 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
       const int col = t.n * kPairTile + half * 128;
       const uint32_t src = tbase + ((uint32_t)(q * 32) << 16) + (uint32_t)(b * 256 + half * 128);
       const bool live = row < n;
+      // few rows, d_hidden: a lane is an entry of d, the columns are rows, every second group of 32 for each half
+      const bool few = OP == kOpFewGrad && !t.dw;
       int lab = -1;
       float lse2 = 0.f, gr = 0.f, mx = -pos_inf(), sum = 0.f;
-      if (OP != kOpGrad && live) lab = a.lab[row] - v0;
+      if (!grad_op(OP) && live) lab = a.lab[row] - v0;
       if (OP == kOpDz && live) {
         lse2 = a.plse[row] * kLog2e;
         gr = a.pgrad[row];
+      }
+      if (few) {
+        const int x = t.n * kPairTile + (int)rank * 128 + q * 32 + lane;
+        const uint32_t at = tbase + ((uint32_t)(q * 32) << 16) + (uint32_t)(b * 256);
+#pragma unroll 1
+        for (int c = 32 * half; c < cols; c += 64) {
+          float z[32];
+          tmem_ld32(at + c, z);
+          float* dst = a.dh + ((size_t)t.part * a.Rp + c) * a.d + x;
+#pragma unroll
+          for (int k = 0; k < 32; ++k)
+            if (x < a.d && c + k < a.R) {
+              const float y = t.kb > 0 ? z[k] : 0.f;
+              dst[(size_t)k * a.d] = first ? y : dst[(size_t)k * a.d] + y;
+            }
+        }
+        tmem_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive_cluster(tempty0 + 8 * b);
+        continue;
       }
 #pragma unroll 1
       for (int c = 0; c < 128; c += 32) {
@@ -500,7 +551,8 @@ __device__ __forceinline__ void fold(float& m, float& s, float m2, float s2) {
 // memory delivers half a tile more.  So the roles change: the MMA's M is the
 // vocabulary (or d, for d_hidden) and its N the rows, in multiples of 32.
 //   logits    A = weight (128 entries a CTA at most), B = packed rows, K = d
-//   d_hidden  A = weight (its rows run along M = d), B = P, K = entries
+//   d_hidden  A = weight (its rows run along M = d), B = P, K = entries, together
+//             with d_weight's tiles in head_pair_kernel
 // (d_weight's product has few rows as its K, and stays as it is.)  The warps and
 // barriers are those of head_pair_kernel.  A thread of the epilogue holds one
 // entry's logits of all rows; a row's maximum and sum go across the warp's lanes
@@ -510,7 +562,7 @@ __device__ __forceinline__ void fold(float& m, float& s, float m2, float s2) {
 // The rows are not packed: an ignored row is a column of the MMA that is not
 // read, and a row of zeros in P.  d_weight's product, whose K the rows are, takes
 // a copy of them in which the ignored ones are zeros.
-enum FewOp { kFewStats, kFewDz, kFewDh };
+enum FewOp { kFewStats, kFewDz };
 constexpr int kFewRows = 128;
 constexpr int kFewStages = 9;
 constexpr int kFewBBytes = kFewRows / 2 * 128;         // this CTA's half of the rows
@@ -537,7 +589,7 @@ __device__ __forceinline__ float across(float (&w)[32], int lane, F f) {
 }
 
 struct FewPlan {
-  int height;            // entries of the vocabulary per CTA and tile (kFewStats, kFewDz)
+  int height;            // entries of the vocabulary per CTA and tile
   int cols;              // rows, a multiple of 32
   int tiles;
 };
@@ -578,48 +630,30 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
   tmem_fence_after();
   const uint32_t tbase = *s_taddr;                  // two accumulators of 128 columns
   const int mine = p.tiles > pair ? (p.tiles - pair + pairs - 1) / pairs : 0;
-  const int dt = (a.d + 255) / 256;
-  const int kall = OP == kFewDh ? (vlen + 63) / 64 : (a.d + 63) / 64;
-  const int kpart = OP == kFewDh ? (kall + a.split - 1) / a.split : kall;
-  // a tile's first block of K and their number
-  auto first_block = [&](int t) { return OP == kFewDh ? t / dt * kpart : 0; };
-  auto blocks = [&](int t) { return max(0, min(kpart, kall - first_block(t))); };
+  const int kb = (a.d + 63) / 64;                   // blocks of K
   bool ok = true;
 
   if (warp == 0) {
     if (lane == 0) {
       const uint32_t full0 = map_to(full, 0);
-      const uint32_t bytes = (OP == kFewDh ? 2 * kHalfBytes : (uint32_t)p.height * 256) + (uint32_t)p.cols * 128;
+      const uint32_t bytes = (uint32_t)(p.height * 256 + p.cols * 128);    // of both CTAs
       auto load_a = [&](int t, int k, int s) {
-        const uint32_t dst = base + s * kFewStage;
-        if (OP == kFewDh) {
-          const int x = t % dt * 256 + rank * 128, y = v0 + k * 64;
-          tma_box_pair(dst, &map_a, x, y, full0 + 8 * s);
-          tma_box_pair(dst + kHalfBytes / 2, &map_a, x + 64, y, full0 + 8 * s);
-        } else {
-          tma_box_pair(dst, &map_a, k * 64, v0 + (t * 2 + rank) * p.height, full0 + 8 * s);
-        }
+        if (rank == 0) mbar_arrive_tx(full + 8 * s, bytes);
+        tma_box_pair(base + s * kFewStage, &map_a, k * 64, v0 + (t * 2 + rank) * p.height, full0 + 8 * s);
       };
       // the weight's first stages do not wait for the kernel before (which has
       // started, so that what precedes it on the stream has ended)
-      const int early = mine > 0 ? min(kFewStages, blocks(pair)) : 0;
-      for (int s = 0; s < early; ++s) {
-        if (rank == 0) mbar_arrive_tx(full + 8 * s, bytes);
-        load_a(pair, first_block(pair) + s, s);
-      }
+      const int early = mine > 0 ? min(kFewStages, kb) : 0;
+      for (int s = 0; s < early; ++s) load_a(pair, s, s);
       asm volatile("griddepcontrol.wait;" ::: "memory");
       asm volatile("fence.proxy.async.global;" ::: "memory");
       int g = 0;
       for (int i = 0; i < mine; ++i) {
-        const int t = pair + i * pairs, k0 = first_block(t), kb = blocks(t);
         for (int k = 0; k < kb; ++k, ++g) {
           const int s = g % kFewStages;
           if (g >= kFewStages && ok) ok = bar_wait<true>(empty + 8 * s, (uint32_t)((g / kFewStages - 1) & 1));
-          if (g >= early) {
-            if (rank == 0) mbar_arrive_tx(full + 8 * s, bytes);
-            load_a(t, k0 + k, s);
-          }
-          tma_box_pair(base + s * kFewStage + kHalfBytes, &map_b, (k0 + k) * 64, rank * (p.cols / 2), full0 + 8 * s);
+          if (g >= early) load_a(pair + i * pairs, k, s);
+          tma_box_pair(base + s * kFewStage + kHalfBytes, &map_b, k * 64, rank * (p.cols / 2), full0 + 8 * s);
         }
       }
       for (int k = (g > kFewStages ? g - kFewStages : 0); k < g; ++k)
@@ -632,23 +666,22 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
       const bool leader = elect_lane();
       const uint32_t empty1 = map_to(empty, 1), tfull1 = map_to(tfull, 1);
       const uint32_t empty0 = map_to(empty, 0), tfull0 = map_to(tfull, 0);
-      const uint32_t idesc = mma_idesc(256, p.cols, true, OP == kFewDh, false);
-      constexpr uint64_t da = OP == kFewDh ? 2048 >> 4 : 32 >> 4;   // K = 16 further: 16 rows, or 32 bytes
-      int g = 0, s = 0;
+      const uint32_t idesc = mma_idesc(256, p.cols, true, false, false);
+      int s = 0;
       uint32_t phase = 0;
       for (int i = 0; i < mine; ++i) {
-        const int b = i & 1, kb = blocks(pair + i * pairs);
+        const int b = i & 1;
         if (i >= 2 && ok) ok = bar_wait<true>(tempty + 8 * b, (uint32_t)((i / 2 - 1) & 1));
         tmem_fence_after();
         const uint32_t d = tbase + (uint32_t)(b * 128);
-        for (int k = 0; k < kb; ++k, ++g) {
+        for (int k = 0; k < kb; ++k) {
           if (ok) ok = bar_wait<true>(full + 8 * s, phase);
           tmem_fence_after();
-          const uint64_t ad = mma_desc(base + s * kFewStage, kHalfBytes / 2);
+          const uint64_t ad = mma_desc(base + s * kFewStage, 0);
           const uint64_t bd = mma_desc(base + s * kFewStage + kHalfBytes, 0);
           if (leader) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) mma_pair(d, ad + j * da, bd + (uint64_t)(2 * j), idesc, (k | j) != 0);
+            for (int j = 0; j < 4; ++j) mma_pair(d, ad + (uint64_t)(2 * j), bd + (uint64_t)(2 * j), idesc, (k | j) != 0);
             mma_commit_pair(empty0 + 8 * s);
             mma_commit_pair(empty1 + 8 * s);
           }
@@ -669,41 +702,38 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
     const int q = warp & 3, half = (warp - 2) >> 2, e = tid - 64;
     const uint32_t tempty0 = map_to(tempty, 0);
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    if (OP != kFewDh) {
-      for (int c = e; c < p.cols; c += 32 * kEpiWarps) {
-        int4 x = make_int4(-1, 0, 0, 0);
-        const int label = c < a.R ? a.labels[c] : a.ignore;
-        if (kept(a, label)) {
-          x.x = label - v0;
-          x.w = 1;
-          if (OP == kFewDz) {
-            x.y = __float_as_int(a.lse_in[c] * kLog2e);
-            x.z = __float_as_int(a.grad[c]);
-          }
-        } else if (label != a.ignore && blockIdx.x == 0) {
-          atomicOr(a.err, 1u);
+    for (int c = e; c < p.cols; c += 32 * kEpiWarps) {
+      int4 x = make_int4(-1, 0, 0, 0);
+      const int label = c < a.R ? a.labels[c] : a.ignore;
+      if (kept(a, label)) {
+        x.x = label - v0;
+        x.w = 1;
+        if (OP == kFewDz) {
+          x.y = __float_as_int(a.lse_in[c] * kLog2e);
+          x.z = __float_as_int(a.grad[c]);
         }
-        s_table[c] = x;
+      } else if (label != a.ignore && blockIdx.x == 0) {
+        atomicOr(a.err, 1u);
       }
-      if (OP == kFewDz && a.d_weight && first) {     // a CTA a row, and some of zeros
-        for (int r = blockIdx.x; r < (a.R + 63) / 64 * 64; r += gridDim.x) {
-          const bool keep = r < a.R && kept(a, a.labels[r]);
-          const uint4* src = reinterpret_cast<const uint4*>(a.hidden + (size_t)(keep ? r : 0) * a.d);
-          for (int j = e; j < a.d / 8; j += 32 * kEpiWarps)
-            reinterpret_cast<uint4*>(a.packed + (size_t)r * a.d)[j] = keep ? src[j] : make_uint4(0, 0, 0, 0);
-        }
-        if (blockIdx.x == 0 && e == 0) *a.n = a.R;
-      }
-      asm volatile("bar.sync 1, 256;" ::: "memory");
+      s_table[c] = x;
     }
+    if (OP == kFewDz && a.d_weight && first) {     // a CTA a row, and some of zeros
+      for (int r = blockIdx.x; r < (a.R + 63) / 64 * 64; r += gridDim.x) {
+        const bool keep = r < a.R && kept(a, a.labels[r]);
+        const uint4* src = reinterpret_cast<const uint4*>(a.hidden + (size_t)(keep ? r : 0) * a.d);
+        for (int j = e; j < a.d / 8; j += 32 * kEpiWarps)
+          reinterpret_cast<uint4*>(a.packed + (size_t)r * a.d)[j] = keep ? src[j] : make_uint4(0, 0, 0, 0);
+      }
+    }
+    if (OP == kFewDz && first && blockIdx.x == 0 && e == 0) *a.n = a.R;
+    asm volatile("bar.sync 1, 256;" ::: "memory");
     // this warp's rows: every second group of 32
     float mx[2] = {-pos_inf(), -pos_inf()}, sum[2] = {0.f, 0.f};
     for (int i = 0; i < mine; ++i) {
       const int t = pair + i * pairs, b = i & 1;
       const int at = q * 32 + lane;                  // this thread's entry within the CTA's part
-      const int v = OP == kFewDh ? t % dt * 256 + rank * 128 + at : (t * 2 + rank) * p.height + at;
-      const bool live = OP == kFewDh ? v < a.d : at < p.height && v < vlen;
-      const bool some = blocks(t) > 0;
+      const int v = (t * 2 + rank) * p.height + at;
+      const bool live = at < p.height && v < vlen;
       if (ok) ok = bar_wait<true>(tfull + 8 * b, (uint32_t)((i / 2) & 1));
       __syncwarp();
       tmem_fence_after();
@@ -744,7 +774,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
           const float ts = across(x, lane, [](float f, float g) { return f + g; });
           sum[u] = (sum[u] > 0.f ? sum[u] * ex2(mx[u] - ref) : 0.f) + ts;
           mx[u] = nm;
-        } else if (OP == kFewDz) {
+        } else {
           uint16_t* dst = a.dz + (size_t)c0 * a.Vc + v;
 #pragma unroll
           for (int k = 0; k < 32; ++k) {
@@ -752,14 +782,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
             const float pr = (ex2(fmaf(z[k], kLog2e, -__int_as_float(x.y))) - (x.x == v ? 1.f : 0.f)) * __int_as_float(x.z);
             if (live) dst[(size_t)k * a.Vc] = x.w ? (uint16_t)pack_bf(pr, 0.f) : (uint16_t)0;
           }
-        } else {
-          float* dst = a.dh + ((size_t)(t / dt) * a.Rp + c0) * a.d + v;
-#pragma unroll
-          for (int k = 0; k < 32; ++k)
-            if (live && c0 + k < a.R) {
-              const float y = some ? z[k] : 0.f;
-              dst[(size_t)k * a.d] = first ? y : dst[(size_t)k * a.d] + y;
-            }
         }
       }
     }
@@ -937,18 +959,18 @@ cudaError_t allow_smem(K kernel, size_t smem, unsigned long long* done, int* pai
   return cudaSuccess;
 }
 template <int OP>
-cudaError_t launch_pairs(const HeadLossArgs& a, int v0, int vlen, int first, int64_t most, const Maps& maps,
+cudaError_t launch_pairs(const HeadLossArgs& a, int v0, int vlen, int first, int cols, int64_t most, const Maps& maps,
                          cudaStream_t s) {
   static unsigned long long done = 0ull;
   int pairs = 0;
   const cudaError_t e = allow_smem(head_pair_kernel<OP>, kPairSmem, &done, &pairs);
   if (e != cudaSuccess) return e;
   if (pairs > most) pairs = (int)most;
-  return launch(true, head_pair_kernel<OP>, (unsigned)(2 * pairs), kPairThreads, kPairSmem, s, a, v0, vlen, first, maps);
+  return launch(true, head_pair_kernel<OP>, (unsigned)(2 * pairs), kPairThreads, kPairSmem, s, a, v0, vlen, first, cols, maps);
 }
 
-// kFewStats, kFewDz: *ctas gets the CTAs, each of which leaves one partial
-// statistic a row (kFewParts at most)
+// *ctas gets the CTAs, each of which leaves one partial statistic a row
+// (kFewParts at most)
 template <int OP>
 cudaError_t launch_few(bool early, const HeadLossArgs& a, int v0, int vlen, int first, int* ctas, cudaStream_t s) {
   static unsigned long long done = 0ull;
@@ -961,15 +983,11 @@ cudaError_t launch_few(bool early, const HeadLossArgs& a, int v0, int vlen, int 
   // the vocabulary spread evenly over the pairs' rounds
   const int64_t wave = (int64_t)pairs * 256, waves = (vlen + wave - 1) / wave;
   p.height = (int)(((vlen + 2 * pairs * waves - 1) / (2 * pairs * waves) + 7) / 8 * 8);
-  p.tiles = OP == kFewDh ? (int)tiles(a.d, 256) * a.split : (int)tiles(vlen, 2 * p.height);
+  p.tiles = (int)tiles(vlen, 2 * p.height);
   const CUtensorMapDataType t = CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
   CUtensorMap ma, mb;
-  bool ok = tma_matrix(&ma, t, 2, a.weight, a.d, a.V, OP == kFewDh ? 64 : p.height);
-  if (OP == kFewDh)                                  // (P's entries and rows that were not written read as zeros)
-    ok = ok && tma_matrix(&mb, t, 2, a.dz, vlen, p.cols, p.cols / 2, a.Vc);
-  else
-    ok = ok && tma_matrix(&mb, t, 2, a.hidden, a.d, a.R, p.cols / 2);
-  if (!ok) return cudaErrorInvalidValue;
+  if (!tma_matrix(&ma, t, 2, a.weight, a.d, a.V, p.height) || !tma_matrix(&mb, t, 2, a.hidden, a.d, a.R, p.cols / 2))
+    return cudaErrorInvalidValue;
   if (pairs > p.tiles) pairs = p.tiles;
   if (ctas) *ctas = 2 * pairs;
   return launch(early, head_few_kernel<OP>, (unsigned)(2 * pairs), kPairThreads, kFewSmem, s, a, p, v0, vlen, first, ma, mb);
@@ -1007,36 +1025,35 @@ cudaError_t launch_head_loss(const HeadLossArgs& a, cudaStream_t s) {
   if (!encode_maps(a, false, &maps)) return cudaErrorInvalidValue;
   cudaError_t e = launch_pack(a, s);
   if (e != cudaSuccess) return e;
-  e = launch_pairs<kOpStats>(a, 0, a.V, 1, (int64_t)(a.Rp / kPairTile) * tiles(a.V, kPairTile), maps, s);
+  e = launch_pairs<kOpStats>(a, 0, a.V, 1, 0, (int64_t)(a.Rp / kPairTile) * tiles(a.V, kPairTile), maps, s);
   if (e != cudaSuccess) return e;
   return launch(true, head_merge_kernel<false>, tiles(a.R, 4), kMergeThreads, 0, s, a, (int)tiles(a.V, kHeadPart));
 }
 
 cudaError_t launch_head_loss_backward(const HeadLossArgs& a, cudaStream_t s) {
   const bool few = a.R <= kFewRows;
+  const int cols = (a.R + 31) / 32 * 32;
   Maps maps;
-  cudaError_t e = cudaSuccess;
-  if ((!few || a.d_weight) && !encode_maps(a, true, &maps)) return cudaErrorInvalidValue;
-  if (!few) e = launch_pack(a, s);
+  if (!encode_maps(a, true, &maps)) return cudaErrorInvalidValue;
+  cudaError_t e = few ? cudaSuccess : launch_pack(a, s);
   if (e != cudaSuccess) return e;
-  const int64_t mt = a.Rp / kPairTile, dt = tiles(a.d, kPairTile);
+  const int64_t mt = few ? 1 : a.Rp / kPairTile, dt = tiles(a.d, kPairTile);
   for (int64_t v0 = 0; v0 < a.V; v0 += a.Vc) {
     const int vlen = (int)min((int64_t)a.Vc, a.V - v0), first = v0 == 0;
     const int64_t vt = tiles(vlen, kPairTile);
-    HeadLossArgs w = a;
+    const int64_t most = (a.d_hidden ? mt * dt * a.split : 0) + (a.d_weight ? vt * dt : 0);
     if (few) {
+      // P's entries and rows that are not written read as zeros
+      const CUtensorMapDataType t = CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
+      if (!tma_matrix(&maps.dz_k, t, 2, a.dz, vlen, cols, cols / 2, a.Vc) ||
+          !tma_matrix(&maps.dz_m, t, 2, a.dz, vlen, cols, 64, a.Vc))
+        return cudaErrorInvalidValue;
       e = launch_few<kFewDz>(!first, a, (int)v0, vlen, first, nullptr, s);
-      if (e == cudaSuccess && a.d_hidden) e = launch_few<kFewDh>(true, a, (int)v0, vlen, first, nullptr, s);
-      if (e == cudaSuccess && a.d_weight &&
-          !tma_matrix(&maps.dz_m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, a.dz, vlen, (a.R + 31) / 32 * 32, 64, a.Vc))
-        e = cudaErrorInvalidValue;
-      w.d_hidden = nullptr;
+      if (e == cudaSuccess) e = launch_pairs<kOpFewGrad>(a, (int)v0, vlen, first, cols, most, maps, s);
     } else {
-      e = launch_pairs<kOpDz>(a, (int)v0, vlen, first, mt * vt, maps, s);
+      e = launch_pairs<kOpDz>(a, (int)v0, vlen, first, 0, mt * vt, maps, s);
+      if (e == cudaSuccess) e = launch_pairs<kOpGrad>(a, (int)v0, vlen, first, 0, most, maps, s);
     }
-    if (e != cudaSuccess) return e;
-    const int64_t most = (w.d_hidden ? mt * dt * a.split : 0) + (w.d_weight ? vt * dt : 0);
-    if (most > 0) e = launch_pairs<kOpGrad>(w, (int)v0, vlen, first, most, maps, s);
     if (e != cudaSuccess) return e;
   }
   if (!a.d_hidden) return cudaSuccess;
