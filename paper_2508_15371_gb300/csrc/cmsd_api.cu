@@ -653,7 +653,6 @@ size_t loss_layout(HeadLossArgs& a, bool backward, char* w) {
   a.n = (int*)take(sizeof(int));
   a.pos = (int*)take((size_t)R * 4);
   a.lab = (int*)take((size_t)Rp * 4);
-  a.row = (int*)take((size_t)Rp * 4);
   a.packed = (uint16_t*)take((size_t)Rp * a.d * 2);
   if (!backward) {
     a.zlab = (float*)take((size_t)Rp * 4);

@@ -28,8 +28,7 @@ struct HeadLossArgs {
   unsigned* err;
   int* n;                        // [1] kept rows
   int* pos;                      // [R] packed place of each row, -1: ignored
-  int* lab;                      // [Rp] label and row of each packed row
-  int* row;
+  int* lab;                      // [Rp] label of each packed row
   float* plse;                   // [Rp] lse and gradient of each packed row (backward)
   float* pgrad;
   uint16_t* packed;              // bf16 [Rp][d], zeros from row n to the next multiple of 64

@@ -74,7 +74,6 @@ __global__ void __launch_bounds__(kPackThreads) head_pack_kernel(const HeadLossA
       a.pos[mine] = keep ? p : -1;
       if (keep) {
         a.lab[p] = label;
-        a.row[p] = mine;
         if (a.plse) {
           a.plse[p] = a.lse_in[mine];
           a.pgrad[p] = a.grad[mine];
@@ -101,6 +100,13 @@ __global__ void __launch_bounds__(kPackThreads) head_pack_kernel(const HeadLossA
   }
 }
 
+// (maximum, sum) of two sets of entries, in base 2
+__device__ __forceinline__ void fold(float& m, float& s, float m2, float s2) {
+  const float mm = fmaxf(m, m2);
+  s = (s > 0.f ? s * ex2(m - mm) : 0.f) + (s2 > 0.f ? s2 * ex2(m2 - mm) : 0.f);
+  m = mm;
+}
+
 // ---- the products -------------------------------------------------------------------
 //
 // Three products of one shape: 256 x 256 outputs of a pair of CTAs
@@ -119,7 +125,8 @@ __global__ void __launch_bounds__(kPackThreads) head_pack_kernel(const HeadLossA
 //               counted at the first CTA's barrier;
 //   warp 1      lane 0 of the first CTA issues the MMAs of both;
 //   warps 2..9  the epilogue: warp w reads TMEM lanes 32 (w mod 4) .., the two
-//               warps of a quarter 128 of the 256 columns each.
+//               warps of a quarter 128 of the 256 columns each (the loss: warps
+//               2..17, 64 columns each, whose sums stay in registers).
 // Barriers: full (TMA -> MMA), empty (MMA -> TMA, in both CTAs), tfull (MMA ->
 // epilogue, in both) and tempty (both epilogues -> MMA) for each of the two
 // accumulators.  Every wait is bounded.
@@ -130,10 +137,19 @@ constexpr int kStages = 6;
 constexpr int kHalfBytes = 128 * 128;                 // 128 rows of 64 bf16
 constexpr int kStageBytes = 2 * kHalfBytes;           // A's and B's half
 constexpr int kEpiWarps = 8;
+__host__ __device__ constexpr int epi_warps(int op) { return op == kOpStats ? 16 : kEpiWarps; }
 constexpr int kPairThreads = 64 + 32 * kEpiWarps;
 constexpr int kOutBytes = 32 * 128;                   // a warp's 32 rows of 128 bytes on their way out
 constexpr size_t kPairSmem = 1024 + (size_t)kStages * kStageBytes + (size_t)kEpiWarps * kOutBytes + 8 * (2 * kStages + 4) + 16;
 constexpr int kTmemCols = 512;
+// The tensor cores round their sums towards zero at each step of 16 of K: at
+// d=2048 logits came out short by 1.5e-6 of their size, all in the same direction,
+// and losses wrong by 1.1e-6.  So the loss's sums are cut after kSumBlocks blocks of
+// 64 and added up in registers: each part is shorter and smaller (losses 5.5e-7 at
+// any d; parts of 8 blocks 2.6e-7, but 914 against 880 us at R=4096 d=2048
+// V=128256, 857 uncut).  Not so the sums that P is formed from, which is rounded to
+// bf16.
+constexpr int kSumBlocks = 16;
 static_assert(kPairSmem <= 227 * 1024, "shared memory");
 
 // One tile of a pair: rows and columns of 256, K from k0 in blocks of 64.
@@ -258,7 +274,7 @@ __device__ __forceinline__ uint32_t pack_bf(float lo, float hi) {
 // v0, vlen: the piece of the vocabulary; first: the first piece; cols: kOpFewGrad's
 // rows, a multiple of 32
 template <int OP>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(64 + 32 * epi_warps(OP), 1)
     head_pair_kernel(const HeadLossArgs a, const int v0, const int vlen, const int first, const int cols,
                      const __grid_constant__ Maps maps) {
   extern __shared__ __align__(1024) unsigned char pair_smem[];
@@ -276,7 +292,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
     }
     for (int b = 0; b < 2; ++b) {
       mbar_init(tfull + 8 * b, 1);
-      mbar_init(tempty + 8 * b, 2 * kEpiWarps);
+      mbar_init(tempty + 8 * b, 2 * epi_warps(OP));
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -358,13 +374,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
     if (lane == 0 && rank == 0) {
       const uint32_t empty1 = map_to(empty, 1), tfull1 = map_to(tfull, 1);
       const uint32_t empty0 = map_to(empty, 0), tfull0 = map_to(tfull, 0);
-      int g = 0;
+      int g = 0, c = 0;                              // stages; sums handed over
       for (int i = 0; i < w.total; ++i) {
         const Tile t = tile_of<OP>(a, w, i);
-        const int b = i & 1;
-        if (i >= 2 && ok) ok = bar_wait<true>(tempty + 8 * b, (uint32_t)((i / 2 - 1) & 1));
-        tmem_fence_after();
-        const uint32_t d = tbase + (uint32_t)(b * 256);
         const bool few = OP == kOpFewGrad && !t.dw;
         const uint32_t idesc = !grad_op(OP) ? mma_idesc(256, 256, true, false, false)
                                             : (t.dw ? mma_idesc(256, 256, true, true, true)
@@ -372,19 +384,30 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
                                                            : mma_idesc(256, 256, true, false, true)));
         // K = 16 further: 32 bytes along the rows, or 16 rows
         const uint64_t da = grad_op(OP) && (t.dw || few) ? 2048 >> 4 : 32 >> 4, db = grad_op(OP) && !few ? 2048 >> 4 : 32 >> 4;
-        for (int kb = 0; kb < t.kb; ++kb, ++g) {
-          const int s = g % kStages;
-          if (ok) ok = bar_wait<true>(full + 8 * s, (uint32_t)((g / kStages) & 1));
+        int kb = 0;
+        do {                                         // (once but for the loss)
+          const int end = OP == kOpStats ? min(t.kb, kb + kSumBlocks) : t.kb, b = c & 1;
+          if (c >= 2 && ok) ok = bar_wait<true>(tempty + 8 * b, (uint32_t)((c / 2 - 1) & 1));
           tmem_fence_after();
-          const uint64_t ad = mma_desc(base + s * kStageBytes, kHalfBytes / 2);
-          const uint64_t bd = mma_desc(base + s * kStageBytes + kHalfBytes, kHalfBytes / 2);
+          const uint32_t d = tbase + (uint32_t)(b * 256);
+          for (uint32_t more = 0; kb < end; ++kb, ++g) {
+            const int s = g % kStages;
+            if (ok) ok = bar_wait<true>(full + 8 * s, (uint32_t)((g / kStages) & 1));
+            tmem_fence_after();
+            const uint64_t ad = mma_desc(base + s * kStageBytes, kHalfBytes / 2);
+            const uint64_t bd = mma_desc(base + s * kStageBytes + kHalfBytes, kHalfBytes / 2);
 #pragma unroll
-          for (int ks = 0; ks < 4; ++ks) mma_pair(d, ad + ks * da, bd + ks * db, idesc, (kb | ks) != 0);
-          mma_commit_pair(empty0 + 8 * s);
-          mma_commit_pair(empty1 + 8 * s);
-        }
-        mma_commit_pair(tfull0 + 8 * b);
-        mma_commit_pair(tfull1 + 8 * b);
+            for (int ks = 0; ks < 4; ++ks) {
+              mma_pair(d, ad + ks * da, bd + ks * db, idesc, more);
+              more = 1;
+            }
+            mma_commit_pair(empty0 + 8 * s);
+            mma_commit_pair(empty1 + 8 * s);
+          }
+          mma_commit_pair(tfull0 + 8 * b);
+          mma_commit_pair(tfull1 + 8 * b);
+          ++c;
+        } while (kb < t.kb);
       }
     }
     __syncwarp();
@@ -393,139 +416,189 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const int n = *a.n;
     const Work w = work_of<OP>(a, n, vlen, a.d_hidden != nullptr, a.d_weight != nullptr);
-    const uint32_t tempty0 = map_to(tempty, 0);
-    const int q = warp & 3, half = (warp - 2) >> 2;
-    // this warp's rows on their way out: 128 bytes of each, swizzled as the boxes are
-    const uint32_t obuf = base + kStages * kStageBytes + (warp - 2) * kOutBytes, orow = obuf + lane * 128;
-    const uint32_t x8 = (uint32_t)(lane & 7);
-    // 32 columns of 32 rows as bf16; a box of 64 goes out with every second call
-    auto out_bf16 = [&](const float (&v)[32], int c, int y, int x, bool inside, const CUtensorMap* map) {
-      if ((c & 32) == 0) {
-        if (lane == 0) tma_store_wait_read();
-        __syncwarp();
-      }
+    if (OP == kOpStats) {
+      // ---- the loss's epilogue: each row's maximum and sum of a tile's entries ---------
+      const uint32_t tempty0 = map_to(tempty, 0);
+      const int q = warp & 3, group = (warp - 2) >> 2;
+      const uint32_t quarter = tbase + ((uint32_t)(q * 32) << 16) + (uint32_t)(group * 64);
+      float2* s_half = reinterpret_cast<float2*>(pair_smem + (base - raw) + kStages * kStageBytes);
+      int sums = 0;                                    // sums read
+      for (int i = 0; i < w.total; ++i) {
+        const Tile t = tile_of<OP>(a, w, i);
+        const int row = t.m * kPairTile + (int)rank * 128 + q * 32 + lane;
+        const int col = t.n * kPairTile + group * 64;
+        const bool live = row < n;
+        const int lab = live ? a.lab[row] : -1;
+        float z[64];
+        for (int kb = 0; kb < t.kb; kb += kSumBlocks, ++sums) {
+          const int b = sums & 1;
+          if (ok) ok = bar_wait<true>(tfull + 8 * b, (uint32_t)((sums / 2) & 1));
+          __syncwarp();
+          tmem_fence_after();
+          const uint32_t src = quarter + b * 256;
+          if (kb == 0) {                             // (a loop of its own: with one for both the sums spilled)
+            float y[32];
 #pragma unroll
-      for (int k = 0; k < 4; ++k)
-        st_shared(orow + (((uint32_t)(k + (c & 32) / 8) ^ x8) << 4), pack_bf(v[8 * k], v[8 * k + 1]),
-                  pack_bf(v[8 * k + 2], v[8 * k + 3]), pack_bf(v[8 * k + 4], v[8 * k + 5]),
-                  pack_bf(v[8 * k + 6], v[8 * k + 7]));
-      if (c & 32) {
-        smem_to_copies();
-        __syncwarp();
-        if (lane == 0 && inside) {                   // (part of a box may lie outside, not all of it)
-          tma_store(map, x - 32, y, obuf);
-          tma_store_commit();
-        }
-      }
-    };
-    for (int i = 0; i < w.total; ++i) {
-      const Tile t = tile_of<OP>(a, w, i);
-      const int b = i & 1;
-      if (ok) ok = bar_wait<true>(tfull + 8 * b, (uint32_t)((i / 2) & 1));
-      __syncwarp();
-      tmem_fence_after();
-      const int row0 = t.m * kPairTile + (int)rank * 128 + q * 32, row = row0 + lane;
-      const int col = t.n * kPairTile + half * 128;
-      const uint32_t src = tbase + ((uint32_t)(q * 32) << 16) + (uint32_t)(b * 256 + half * 128);
-      const bool live = row < n;
-      // few rows, d_hidden: a lane is an entry of d, the columns are rows, every second group of 32 for each half
-      const bool few = OP == kOpFewGrad && !t.dw;
-      int lab = -1;
-      float lse2 = 0.f, gr = 0.f, mx = -pos_inf(), sum = 0.f;
-      if (!grad_op(OP) && live) lab = a.lab[row] - v0;
-      if (OP == kOpDz && live) {
-        lse2 = a.plse[row] * kLog2e;
-        gr = a.pgrad[row];
-      }
-      if (few) {
-        const int x = t.n * kPairTile + (int)rank * 128 + q * 32 + lane;
-        const uint32_t at = tbase + ((uint32_t)(q * 32) << 16) + (uint32_t)(b * 256);
-#pragma unroll 1
-        for (int c = 32 * half; c < cols; c += 64) {
-          float z[32];
-          tmem_ld32(at + c, z);
-          float* dst = a.dh + ((size_t)t.part * a.Rp + c) * a.d + x;
+            for (int c = 0; c < 64; c += 32) {
+              tmem_ld32(src + c, y);
 #pragma unroll
-          for (int k = 0; k < 32; ++k)
-            if (x < a.d && c + k < a.R) {
-              const float y = t.kb > 0 ? z[k] : 0.f;
-              dst[(size_t)k * a.d] = first ? y : dst[(size_t)k * a.d] + y;
+              for (int k = 0; k < 32; ++k) z[c + k] = y[k];
             }
-        }
-        tmem_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive_cluster(tempty0 + 8 * b);
-        continue;
-      }
-#pragma unroll 1
-      for (int c = 0; c < 128; c += 32) {
-        float z[32];
-        if (t.kb > 0) {
-          tmem_ld32(src + c, z);
-        } else {
+          } else {
 #pragma unroll
-          for (int k = 0; k < 32; ++k) z[k] = 0.f;
-        }
-        if (c == 96) {
+            for (int c = 0; c < 64; c += 16) {
+              float y[16];
+              tmem_ld16_ahead(src + c, y);
+              tmem_ld_wait(y);
+#pragma unroll
+              for (int k = 0; k < 16; ++k) z[c + k] += y[k];
+            }
+          }
           tmem_fence_before();
           __syncwarp();
           if (lane == 0) mbar_arrive_cluster(tempty0 + 8 * b);   // this warp's columns have been read
         }
-        const int j0 = col + c;
-        if (OP == kOpStats) {
-          if (j0 + 32 > vlen) {
+        if (lab >= col && lab < col + 64) {
+          float zl = z[0];
 #pragma unroll
-            for (int k = 0; k < 32; ++k)
-              if (j0 + k >= vlen) z[k] = -pos_inf();
-          }
-          if (j0 < vlen) {
-            float m4[4] = {z[0], z[1], z[2], z[3]};
+          for (int k = 1; k < 64; ++k) zl = lab == col + k ? z[k] : zl;
+          a.zlab[row] = zl;
+        }
+        if (col + 64 > vlen) {
 #pragma unroll
-            for (int k = 4; k < 32; ++k) m4[k & 3] = fmaxf(m4[k & 3], z[k]);
-            const float nm = fmaxf(mx, fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])) * kLog2e);
-            float s4[4] = {0.f, 0.f, 0.f, 0.f};
+          for (int k = 0; k < 64; ++k)
+            if (col + k >= vlen) z[k] = -pos_inf();
+        }
+        float m4[4] = {z[0], z[1], z[2], z[3]};
 #pragma unroll
-            for (int k = 0; k < 32; ++k) s4[k & 3] += ex2(fmaf(z[k], kLog2e, -nm));
-            sum = sum * ex2(mx - nm) + ((s4[0] + s4[1]) + (s4[2] + s4[3]));
-            mx = nm;
-            if (lab >= j0 && lab < j0 + 32) {
-              float zl = z[0];
+        for (int k = 4; k < 64; ++k) m4[k & 3] = fmaxf(m4[k & 3], z[k]);
+        float mx = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])) * kLog2e;
+        const float ref = mx > -pos_inf() ? mx : 0.f;
+        float s4[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-              for (int k = 1; k < 32; ++k) zl = lab == j0 + k ? z[k] : zl;
-              a.zlab[row] = zl;
-            }
-          }
-        } else if (OP == kOpDz) {
-          float p[32];
-#pragma unroll
-          for (int k = 0; k < 32; ++k)
-            p[k] = live && j0 + k < vlen
-                       ? (ex2(fmaf(z[k], kLog2e, -lse2)) - (lab == j0 + k ? 1.f : 0.f)) * gr
-                       : 0.f;
-          out_bf16(p, c, row0, j0, true, &maps.dz_out);
-        } else if (t.dw) {
-          out_bf16(z, c, v0 + row0, j0, v0 + row0 < a.V && (j0 & ~63) < a.d, &maps.dw_out);
-        } else {
+        for (int k = 0; k < 64; ++k) s4[k & 3] += ex2(fmaf(z[k], kLog2e, -ref));
+        float sum = (s4[0] + s4[1]) + (s4[2] + s4[3]);
+        // the second 64 of 128 columns join the first (two buffers in turn: one barrier a tile)
+        float2* mine = s_half + ((i & 1) * 2 + (group >> 1)) * 128 + q * 32 + lane;
+        if (group & 1) *mine = make_float2(mx, sum);
+        asm volatile("bar.sync %0, 64;" ::"r"(1 + (group >> 1) * 4 + q) : "memory");
+        if (!(group & 1) && live && col < vlen) {
+          const float2 x = *mine;
+          fold(mx, sum, x.x, x.y);
+          a.part[(size_t)(col / kHeadPart) * a.Rp + row] = make_float2(mx, sum);
+        }
+      }
+    } else {
+      const uint32_t tempty0 = map_to(tempty, 0);
+      const int q = warp & 3, half = (warp - 2) >> 2;
+      // this warp's rows on their way out: 128 bytes of each, swizzled as the boxes are
+      const uint32_t obuf = base + kStages * kStageBytes + (warp - 2) * kOutBytes, orow = obuf + lane * 128;
+      const uint32_t x8 = (uint32_t)(lane & 7);
+      // 32 columns of 32 rows as bf16; a box of 64 goes out with every second call
+      auto out_bf16 = [&](const float (&v)[32], int c, int y, int x, bool inside, const CUtensorMap* map) {
+        if ((c & 32) == 0) {
           if (lane == 0) tma_store_wait_read();
           __syncwarp();
+        }
 #pragma unroll
-          for (int k = 0; k < 8; ++k)
-            st_shared(orow + (((uint32_t)k ^ x8) << 4), __float_as_uint(z[4 * k]), __float_as_uint(z[4 * k + 1]),
-                      __float_as_uint(z[4 * k + 2]), __float_as_uint(z[4 * k + 3]));
+        for (int k = 0; k < 4; ++k)
+          st_shared(orow + (((uint32_t)(k + (c & 32) / 8) ^ x8) << 4), pack_bf(v[8 * k], v[8 * k + 1]),
+                    pack_bf(v[8 * k + 2], v[8 * k + 3]), pack_bf(v[8 * k + 4], v[8 * k + 5]),
+                    pack_bf(v[8 * k + 6], v[8 * k + 7]));
+        if (c & 32) {
           smem_to_copies();
           __syncwarp();
-          if (lane == 0 && j0 < a.d) {
-            if (first)
-              tma_store(&maps.dh_out, j0, t.part * a.Rp + row0, obuf);
-            else                                     // (one addition a piece: the order is that of the pieces)
-              tma_add(&maps.dh_out, j0, t.part * a.Rp + row0, obuf);
+          if (lane == 0 && inside) {                   // (part of a box may lie outside, not all of it)
+            tma_store(map, x - 32, y, obuf);
             tma_store_commit();
           }
         }
+      };
+      for (int i = 0; i < w.total; ++i) {
+        const Tile t = tile_of<OP>(a, w, i);
+        const int b = i & 1;
+        if (ok) ok = bar_wait<true>(tfull + 8 * b, (uint32_t)((i / 2) & 1));
+        __syncwarp();
+        tmem_fence_after();
+        const int row0 = t.m * kPairTile + (int)rank * 128 + q * 32, row = row0 + lane;
+        const int col = t.n * kPairTile + half * 128;
+        const uint32_t src = tbase + ((uint32_t)(q * 32) << 16) + (uint32_t)(b * 256 + half * 128);
+        const bool live = row < n;
+        // few rows, d_hidden: a lane is an entry of d, the columns are rows, every second group of 32 for each half
+        const bool few = OP == kOpFewGrad && !t.dw;
+        int lab = -1;
+        float lse2 = 0.f, gr = 0.f;
+        if (!grad_op(OP) && live) lab = a.lab[row] - v0;
+        if (OP == kOpDz && live) {
+          lse2 = a.plse[row] * kLog2e;
+          gr = a.pgrad[row];
+        }
+        if (few) {
+          const int x = t.n * kPairTile + (int)rank * 128 + q * 32 + lane;
+          const uint32_t at = tbase + ((uint32_t)(q * 32) << 16) + (uint32_t)(b * 256);
+#pragma unroll 1
+          for (int c = 32 * half; c < cols; c += 64) {
+            float z[32];
+            tmem_ld32(at + c, z);
+            float* dst = a.dh + ((size_t)t.part * a.Rp + c) * a.d + x;
+#pragma unroll
+            for (int k = 0; k < 32; ++k)
+              if (x < a.d && c + k < a.R) {
+                const float y = t.kb > 0 ? z[k] : 0.f;
+                dst[(size_t)k * a.d] = first ? y : dst[(size_t)k * a.d] + y;
+              }
+          }
+          tmem_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive_cluster(tempty0 + 8 * b);
+          continue;
+        }
+#pragma unroll 1
+        for (int c = 0; c < 128; c += 32) {
+          float z[32];
+          if (t.kb > 0) {
+            tmem_ld32(src + c, z);
+          } else {
+#pragma unroll
+            for (int k = 0; k < 32; ++k) z[k] = 0.f;
+          }
+          if (c == 96) {
+            tmem_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive_cluster(tempty0 + 8 * b);   // this warp's columns have been read
+          }
+          const int j0 = col + c;
+          if (OP == kOpDz) {
+            float p[32];
+#pragma unroll
+            for (int k = 0; k < 32; ++k)
+              p[k] = live && j0 + k < vlen
+                         ? (ex2(fmaf(z[k], kLog2e, -lse2)) - (lab == j0 + k ? 1.f : 0.f)) * gr
+                         : 0.f;
+            out_bf16(p, c, row0, j0, true, &maps.dz_out);
+          } else if (t.dw) {
+            out_bf16(z, c, v0 + row0, j0, v0 + row0 < a.V && (j0 & ~63) < a.d, &maps.dw_out);
+          } else {
+            if (lane == 0) tma_store_wait_read();
+            __syncwarp();
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+              st_shared(orow + (((uint32_t)k ^ x8) << 4), __float_as_uint(z[4 * k]), __float_as_uint(z[4 * k + 1]),
+                        __float_as_uint(z[4 * k + 2]), __float_as_uint(z[4 * k + 3]));
+            smem_to_copies();
+            __syncwarp();
+            if (lane == 0 && j0 < a.d) {
+              if (first)
+                tma_store(&maps.dh_out, j0, t.part * a.Rp + row0, obuf);
+              else                                     // (one addition a piece: the order is that of the pieces)
+                tma_add(&maps.dh_out, j0, t.part * a.Rp + row0, obuf);
+              tma_store_commit();
+            }
+          }
+        }
       }
-      if (OP == kOpStats && live && col < vlen) a.part[(size_t)(col / kHeadPart) * a.Rp + row] = make_float2(mx, sum);
+      if (lane == 0) tma_store_wait();
     }
-    if (OP != kOpStats && lane == 0) tma_store_wait();
   }
   if (!ok) atomicOr(a.err, 4u);
   __syncwarp();
@@ -534,13 +607,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
   tmem_fence_after();
   if (warp == 1)
     asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tbase), "r"(kTmemCols) : "memory");
-}
-
-// (maximum, sum) of two sets of entries, in base 2
-__device__ __forceinline__ void fold(float& m, float& s, float m2, float s2) {
-  const float mm = fmaxf(m, m2);
-  s = (s > 0.f ? s * ex2(m - mm) : 0.f) + (s2 > 0.f ? s2 * ex2(m2 - mm) : 0.f);
-  m = mm;
 }
 
 // ---- few rows ------------------------------------------------------------------------
@@ -669,19 +735,21 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
       const uint32_t idesc = mma_idesc(256, p.cols, true, false, false);
       int s = 0;
       uint32_t phase = 0;
-      for (int i = 0; i < mine; ++i) {
-        const int b = i & 1;
-        if (i >= 2 && ok) ok = bar_wait<true>(tempty + 8 * b, (uint32_t)((i / 2 - 1) & 1));
+      const int parts = (kb + kSumBlocks - 1) / kSumBlocks;
+      for (int c = 0, k1 = 0; c < mine * parts; ++c) {       // sums
+        const int b = c & 1, k0 = k1 == kb ? 0 : k1;
+        if (c >= 2 && ok) ok = bar_wait<true>(tempty + 8 * b, (uint32_t)((c / 2 - 1) & 1));
         tmem_fence_after();
         const uint32_t d = tbase + (uint32_t)(b * 128);
-        for (int k = 0; k < kb; ++k) {
+        k1 = min(kb, k0 + kSumBlocks);
+        for (int k = k0; k < k1; ++k) {
           if (ok) ok = bar_wait<true>(full + 8 * s, phase);
           tmem_fence_after();
           const uint64_t ad = mma_desc(base + s * kFewStage, 0);
           const uint64_t bd = mma_desc(base + s * kFewStage + kHalfBytes, 0);
           if (leader) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) mma_pair(d, ad + (uint64_t)(2 * j), bd + (uint64_t)(2 * j), idesc, (k | j) != 0);
+            for (int j = 0; j < 4; ++j) mma_pair(d, ad + (uint64_t)(2 * j), bd + (uint64_t)(2 * j), idesc, k > k0 || j > 0);
             mma_commit_pair(empty0 + 8 * s);
             mma_commit_pair(empty1 + 8 * s);
           }
@@ -729,27 +797,37 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
     asm volatile("bar.sync 1, 256;" ::: "memory");
     // this warp's rows: every second group of 32
     float mx[2] = {-pos_inf(), -pos_inf()}, sum[2] = {0.f, 0.f};
-    for (int i = 0; i < mine; ++i) {
-      const int t = pair + i * pairs, b = i & 1;
+    for (int i = 0, sums = 0; i < mine; ++i) {
+      const int t = pair + i * pairs;
       const int at = q * 32 + lane;                  // this thread's entry within the CTA's part
       const int v = (t * 2 + rank) * p.height + at;
       const bool live = at < p.height && v < vlen;
-      if (ok) ok = bar_wait<true>(tfull + 8 * b, (uint32_t)((i / 2) & 1));
-      __syncwarp();
-      tmem_fence_after();
-      const uint32_t src = tbase + ((uint32_t)(q * 32) << 16) + (uint32_t)(b * 128);
+      float acc[2][32];                              // the logits, part by part
+      for (int k0 = 0; k0 < kb; k0 += kSumBlocks, ++sums) {
+        const int b = sums & 1;
+        if (ok) ok = bar_wait<true>(tfull + 8 * b, (uint32_t)((sums / 2) & 1));
+        __syncwarp();
+        tmem_fence_after();
+        const uint32_t src = tbase + ((uint32_t)(q * 32) << 16) + (uint32_t)(b * 128);
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          const int c0 = 32 * (2 * u + half);
+          if (c0 < p.cols) {
+            float y[32];
+            tmem_ld32(src + c0, y);
+#pragma unroll
+            for (int k = 0; k < 32; ++k) acc[u][k] = k0 == 0 ? y[k] : acc[u][k] + y[k];
+          }
+        }
+        tmem_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive_cluster(tempty0 + 8 * b);       // this warp's columns have been read
+      }
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
         const int c0 = 32 * (2 * u + half);
-        const bool more = u == 0 && c0 + 64 < p.cols;
-        float z[32];
-        if (c0 < p.cols) tmem_ld32(src + c0, z);
-        if (!more && (u == 0 || c0 < p.cols)) {
-          tmem_fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive_cluster(tempty0 + 8 * b);     // this warp's columns have been read
-        }
         if (c0 >= p.cols) break;
+        float (&z)[32] = acc[u];
         if (OP == kFewStats) {
           const int lab = s_table[c0 + lane].x, from = v - lane;
           unsigned hit = __ballot_sync(kFull, lab >= from && lab < from + 32 && q * 32 + lab - from < p.height);
@@ -813,26 +891,22 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
 
 // ---- a row's tiles merged -----------------------------------------------------------
 // Four rows a CTA (32 bytes of each tile's statistics), 64 tiles at a time.
-constexpr int kMergeThreads = 256;
+// The loss is a difference of two numbers that a trained head makes nearly equal:
+// it is formed from the maximum and the label's logit first.
 // kFew: the rows are not packed
+constexpr int kMergeThreads = 256;
 template <bool kFew>
 __global__ void __launch_bounds__(kMergeThreads) head_merge_kernel(const HeadLossArgs a, int parts) {
   __shared__ float s_m[kMergeThreads / 32][4], s_s[kMergeThreads / 32][4];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int r = blockIdx.x * 4 + (tid & 3);
+  const bool keep = r < a.R && kept(a, a.labels[r]);
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
-  const int n = kFew ? a.R : *a.n, p = blockIdx.x * 4 + (tid & 3);
-  // ignored rows (each CTA sees to four rows of either kind)
-  const bool gone = p < a.R && (kFew ? !kept(a, a.labels[p]) : a.pos[p] < 0);
-  if (tid < 4 && gone) {
-    a.lse[p] = 0.f;
-    if (a.loss) a.loss[p] = 0.f;
-  }
-  if ((int)blockIdx.x * 4 >= n) return;
-  const float zl = tid < 4 && p < n ? a.zlab[p] : 0.f;          // (requested with the statistics)
-  const int r = kFew || p >= n ? p : a.row[p];
+  const int p = keep ? (kFew ? r : a.pos[r]) : -1;
+  const float zl = tid < 4 && keep ? a.zlab[p] : 0.f;          // (requested with the statistics)
   float m = -pos_inf(), s = 0.f;
-  if (p < n) {
+  if (keep) {
     constexpr int kBatch = 8;
     for (int t0 = tid >> 2; t0 < parts; t0 += kBatch * (kMergeThreads / 4)) {
       float2 x[kBatch];
@@ -857,12 +931,17 @@ __global__ void __launch_bounds__(kMergeThreads) head_merge_kernel(const HeadLos
     s_s[warp][lane] = s;
   }
   __syncthreads();
-  if (tid < 4 && p < n && !(kFew && gone)) {
+  if (tid < 4 && r < a.R) {
+    float lse = 0.f, loss = 0.f;
+    if (keep) {
 #pragma unroll
-    for (int w = 1; w < kMergeThreads / 32; ++w) fold(m, s, s_m[w][tid], s_s[w][tid]);
-    const float lse = m * kLn2 + logf(s);
+      for (int w = 1; w < kMergeThreads / 32; ++w) fold(m, s, s_m[w][tid], s_s[w][tid]);
+      const float l = logf(s);
+      lse = m * kLn2 + l;
+      loss = fmaf(fmaf(-zl, kLog2e, m), kLn2, l);
+    }
     a.lse[r] = lse;
-    if (a.loss) a.loss[r] = lse - zl;
+    if (a.loss) a.loss[r] = loss;
   }
 }
 
@@ -966,7 +1045,7 @@ cudaError_t launch_pairs(const HeadLossArgs& a, int v0, int vlen, int first, int
   const cudaError_t e = allow_smem(head_pair_kernel<OP>, kPairSmem, &done, &pairs);
   if (e != cudaSuccess) return e;
   if (pairs > most) pairs = (int)most;
-  return launch(true, head_pair_kernel<OP>, (unsigned)(2 * pairs), kPairThreads, kPairSmem, s, a, v0, vlen, first, cols, maps);
+  return launch(true, head_pair_kernel<OP>, (unsigned)(2 * pairs), 64 + 32 * epi_warps(OP), kPairSmem, s, a, v0, vlen, first, cols, maps);
 }
 
 // *ctas gets the CTAs, each of which leaves one partial statistic a row
