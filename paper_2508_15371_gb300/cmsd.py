@@ -294,27 +294,35 @@ def lmhead_confidence(hidden, weight, p=None, logits=False, out=None, ws=None):
     return o
 
 
-def _need(*specs):
-    """Each (name, tensor, shape, dtype) a contiguous CUDA tensor of that shape and type on the current
-    device; returns its index."""
-    cur = None
-    for name, t, shape, dtype in specs:
-        if t is None or t.dtype is not dtype or t.shape != shape:
-            got = "nothing" if t is None else f"{t.dtype} {tuple(t.shape)}"
-            raise CmsdError(f"{name} must be {dtype} {tuple(shape)}, got {got}")
-        if not t.is_cuda:
-            raise CmsdError(f"{name} must be a CUDA tensor (the library has no CPU path)")
-        if cur is None:
-            cur = _torch_mod.cuda.current_device()
-        if t.get_device() != cur:
-            raise CmsdError(f"{name} must be on the current device")
-        if not t.is_contiguous():
-            raise CmsdError(f"{name} must be contiguous")
-    return cur
+def _refuse(name, t, shape, dtype, cur):
+    """Says what is wrong with a tensor that _need does not take."""
+    if t is None or t.dtype is not dtype or t.shape != shape:
+        got = "nothing" if t is None else f"{t.dtype} {tuple(t.shape)}"
+        raise CmsdError(f"{name} must be {dtype} {tuple(shape)}, got {got}")
+    if not t.is_cuda:
+        raise CmsdError(f"{name} must be a CUDA tensor (the library has no CPU path)")
+    if t.get_device() != cur:
+        raise CmsdError(f"{name} must be on the current device")
+    raise CmsdError(f"{name} must be contiguous")
+
+
+def _need(cur, specs):
+    """Each (tensor, shape, dtype, name) a contiguous CUDA tensor of that shape and type on device cur."""
+    for t, shape, dtype, name in specs:
+        if (t is None or t.dtype is not dtype or t.shape != shape or t.get_device() != cur
+                or not t.is_contiguous()):
+            _refuse(name, t, shape, dtype, cur)
+    if cur < 0:
+        raise CmsdError("all tensors must be CUDA tensors (the library has no CPU path)")
+
+
+def _current(t):
+    """The current device, where t is a CUDA tensor at all (-1 otherwise: nothing is asked of the runtime)."""
+    return _torch_mod.cuda.current_device() if t.is_cuda else -1
 
 
 def _need_ws(ws, cur):
-    if not ws.is_cuda or ws.get_device() != cur or not ws.is_contiguous():
+    if ws.get_device() != cur or not ws.is_contiguous():
         raise CmsdError("the workspace must be contiguous on the current device")
     return ws.numel() * ws.element_size()
 
@@ -324,9 +332,10 @@ def _stream_of(cur):
 
 
 def _head_sizes(hidden, weight):
-    if hidden.dim() != 2 or weight.dim() != 2 or hidden.shape[1] != weight.shape[1]:
+    h, w = hidden.shape, weight.shape
+    if len(h) != 2 or len(w) != 2 or h[1] != w[1]:
         raise CmsdError("hidden [R, d] and weight [V, d] must share d")
-    return hidden.shape[0], hidden.shape[1], weight.shape[0]
+    return h[0], h[1], w[0]
 
 
 def _given(out, name, shape, dtype, like):
@@ -369,8 +378,9 @@ def lmhead_loss(hidden, weight, labels, ignore_index=-100, out=None, ws=None):
     R, d, V = _head_sizes(hidden, weight)
     f32, bf16 = torch.float32, torch.bfloat16
     loss, lse = _given(out, "loss", (R,), f32, hidden), _given(out, "lse", (R,), f32, hidden)
-    cur = _need(("hidden", hidden, (R, d), bf16), ("weight", weight, (V, d), bf16), ("labels", labels, (R,), torch.int32),
-                ("loss", loss, (R,), f32), ("lse", lse, (R,), f32))
+    cur = _current(hidden)
+    _need(cur, ((hidden, (R, d), bf16, "hidden"), (weight, (V, d), bf16, "weight"),
+                (labels, (R,), torch.int32, "labels"), (loss, (R,), f32, "loss"), (lse, (R,), f32, "lse")))
     ws = ws if ws is not None else lmhead_loss_workspace(R, d, V)
     rc = lib().cmsd_lmhead_loss(hidden.data_ptr(), weight.data_ptr(), labels.data_ptr(), R, d, V, int(ignore_index),
                                 loss.data_ptr(), lse.data_ptr(), ws.data_ptr(), _need_ws(ws, cur), _stream_of(cur))
@@ -389,15 +399,16 @@ def lmhead_loss_backward(hidden, weight, labels, lse, grad_loss, ignore_index=-1
     R, d, V = _head_sizes(hidden, weight)
     f32, bf16 = torch.float32, torch.bfloat16
     o = {}
-    specs = [("hidden", hidden, (R, d), bf16), ("weight", weight, (V, d), bf16), ("labels", labels, (R,), torch.int32),
-             ("lse", lse, (R,), f32), ("grad_loss", grad_loss, (R,), f32)]
+    specs = [(hidden, (R, d), bf16, "hidden"), (weight, (V, d), bf16, "weight"),
+             (labels, (R,), torch.int32, "labels"), (lse, (R,), f32, "lse"), (grad_loss, (R,), f32, "grad_loss")]
     if hidden_grad:
         o["d_hidden"] = _given(out, "d_hidden", (R, d), bf16, hidden)
-        specs.append(("d_hidden", o["d_hidden"], (R, d), bf16))
+        specs.append((o["d_hidden"], (R, d), bf16, "d_hidden"))
     if weight_grad:
         o["d_weight"] = _given(out, "d_weight", (V, d), bf16, hidden)
-        specs.append(("d_weight", o["d_weight"], (V, d), bf16))
-    cur = _need(*specs)
+        specs.append((o["d_weight"], (V, d), bf16, "d_weight"))
+    cur = _current(hidden)
+    _need(cur, specs)
     ws = ws if ws is not None else lmhead_loss_backward_workspace(R, d, V)
     rc = lib().cmsd_lmhead_loss_backward(hidden.data_ptr(), weight.data_ptr(), labels.data_ptr(), lse.data_ptr(),
                                          grad_loss.data_ptr(), R, d, V, int(ignore_index), _ptr(o.get("d_hidden")),
@@ -417,7 +428,8 @@ def quantize_rows(x, out=None):
         raise CmsdError(f"x must be float32 or bfloat16, got {x.dtype}")
     R, d = x.shape
     q, scale = _given(out, "q", (R, d), torch.int8, x), _given(out, "scale", (R,), torch.float32, x)
-    cur = _need(("x", x, (R, d), x.dtype), ("q", q, (R, d), torch.int8), ("scale", scale, (R,), torch.float32))
+    cur = _current(x)
+    _need(cur, ((x, (R, d), x.dtype, "x"), (q, (R, d), torch.int8, "q"), (scale, (R,), torch.float32, "scale")))
     rc = lib().cmsd_quantize_rows(x.data_ptr(), F32 if x.dtype is torch.float32 else BF16, R, d, q.data_ptr(),
                                   scale.data_ptr(), _stream_of(cur))
     if rc != OK:
@@ -436,9 +448,10 @@ def lmhead_i8(hidden_q, hidden_scale, weight_q, weight_scale, dtype=None, out=No
     R, d, V = _head_sizes(hidden_q, weight_q)
     f32, i8 = torch.float32, torch.int8
     logits = _given(out, "logits", (R, V), dtype, hidden_q)
-    cur = _need(("hidden_q", hidden_q, (R, d), i8), ("hidden_scale", hidden_scale, (R,), f32),
-                ("weight_q", weight_q, (V, d), i8), ("weight_scale", weight_scale, (V,), f32),
-                ("logits", logits, (R, V), dtype))
+    cur = _current(hidden_q)
+    _need(cur, ((hidden_q, (R, d), i8, "hidden_q"), (hidden_scale, (R,), f32, "hidden_scale"),
+                (weight_q, (V, d), i8, "weight_q"), (weight_scale, (V,), f32, "weight_scale"),
+                (logits, (R, V), dtype, "logits")))
     ws = ws if ws is not None else lmhead_i8_workspace(R, d, V)
     rc = lib().cmsd_lmhead_i8(hidden_q.data_ptr(), hidden_scale.data_ptr(), weight_q.data_ptr(), weight_scale.data_ptr(),
                               R, d, V, logits.data_ptr(), F32 if dtype is f32 else BF16, ws.data_ptr(),

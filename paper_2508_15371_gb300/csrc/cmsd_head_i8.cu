@@ -139,31 +139,40 @@ __device__ __forceinline__ void quant_store(int8_t* dst, const uint32_t* o) {
 
 constexpr int kQuantThreads = 128;                  // four rows of a warp each
 constexpr int kQuantWide = 256;                     // one row
-// rows of up to 32 * NV vectors, a warp each
-template <typename T, int NV>
+// Rows of up to 32 * NV vectors, a warp kRows of them at once: short rows alone
+// leave too little in flight (R=128256 d=512 bf16 58 us with one, 39 with four).
+template <typename T, int NV, int kRows>
 __global__ void __launch_bounds__(kQuantThreads) quantize_warp_kernel(const T* __restrict__ x, int R, int d,
                                                                       int8_t* __restrict__ q, float* __restrict__ scale) {
   constexpr int kN = QuantVec<T>::kN;
   const int lane = threadIdx.x & 31, vecs = d / kN;
-  const int r = blockIdx.x * (kQuantThreads / 32) + (threadIdx.x >> 5);
-  if (r >= R) return;
-  const uint4* src = reinterpret_cast<const uint4*>(x + (size_t)r * d);
-  uint4 v[NV];
-  uint32_t m = 0;
+  const int64_t r0 = ((int64_t)blockIdx.x * (kQuantThreads / 32) + (threadIdx.x >> 5)) * kRows;
+  const int rows = (int)min((int64_t)kRows, R - r0);
+  if (rows <= 0) return;
+  const uint4* src = reinterpret_cast<const uint4*>(x + (size_t)r0 * d);
+  uint4 v[kRows][NV];
 #pragma unroll
-  for (int i = 0; i < NV; ++i) v[i] = lane + 32 * i < vecs ? ld_stream(src + lane + 32 * i) : make_uint4(0, 0, 0, 0);
+  for (int k = 0; k < kRows; ++k)
 #pragma unroll
-  for (int i = 0; i < NV; ++i) m = max(m, QuantVec<T>::mag(v[i]));
-  m = __reduce_max_sync(kFull, m);
-  const QuantRow row = quant_row(m);
-  int8_t* dst = q + (size_t)r * d;
+    for (int i = 0; i < NV; ++i)
+      v[k][i] = k < rows && lane + 32 * i < vecs ? ld_stream(src + k * vecs + lane + 32 * i) : make_uint4(0, 0, 0, 0);
 #pragma unroll
-  for (int i = 0; i < NV; ++i) {
-    uint32_t o[kN / 4];
-    quant_vec<T>(v[i], row, o);
-    if (lane + 32 * i < vecs) quant_store<T>(dst + (lane + 32 * i) * kN, o);
+  for (int k = 0; k < kRows; ++k) {
+    if (k >= rows) return;
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) m = max(m, QuantVec<T>::mag(v[k][i]));
+    m = __reduce_max_sync(kFull, m);
+    const QuantRow row = quant_row(m);
+    int8_t* dst = q + (size_t)(r0 + k) * d;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      uint32_t o[kN / 4];
+      quant_vec<T>(v[k][i], row, o);
+      if (lane + 32 * i < vecs) quant_store<T>(dst + (lane + 32 * i) * kN, o);
+    }
+    if (lane == 0) scale[r0 + k] = __fdiv_rn(__uint_as_float(m), 127.f);
   }
-  if (lane == 0) scale[r] = __fdiv_rn(__uint_as_float(m), 127.f);
 }
 // wider rows, a CTA each: up to kQuantWide * NV vectors in registers, what lies
 // beyond is read twice
@@ -208,13 +217,21 @@ __global__ void __launch_bounds__(kQuantWide) quantize_cta_kernel(const T* __res
 template <typename T>
 cudaError_t launch_quantize(const T* x, int R, int d, int8_t* q, float* scale, cudaStream_t s) {
   const int vecs = d / QuantVec<T>::kN;
-  const unsigned rows = (unsigned)((R + kQuantThreads / 32 - 1) / (kQuantThreads / 32));
-  if (vecs <= 32 * 4)
-    quantize_warp_kernel<T, 4><<<rows, kQuantThreads, 0, s>>>(x, R, d, q, scale);
+  auto ctas = [&](int per_warp) {
+    const int64_t per = kQuantThreads / 32 * per_warp;
+    return (unsigned)((R + per - 1) / per);
+  };
+  const bool many = R >= 8192;                      // several CTAs an SM with four rows a warp too
+  if (vecs <= 32 * 2 && many)
+    quantize_warp_kernel<T, 2, 4><<<ctas(4), kQuantThreads, 0, s>>>(x, R, d, q, scale);
+  else if (vecs <= 32 * 4 && many)
+    quantize_warp_kernel<T, 4, 2><<<ctas(2), kQuantThreads, 0, s>>>(x, R, d, q, scale);
+  else if (vecs <= 32 * 4)
+    quantize_warp_kernel<T, 4, 1><<<ctas(1), kQuantThreads, 0, s>>>(x, R, d, q, scale);
   else if (vecs <= 32 * 8)
-    quantize_warp_kernel<T, 8><<<rows, kQuantThreads, 0, s>>>(x, R, d, q, scale);
+    quantize_warp_kernel<T, 8, 1><<<ctas(1), kQuantThreads, 0, s>>>(x, R, d, q, scale);
   else if (vecs <= 32 * 16)
-    quantize_warp_kernel<T, 16><<<rows, kQuantThreads, 0, s>>>(x, R, d, q, scale);
+    quantize_warp_kernel<T, 16, 1><<<ctas(1), kQuantThreads, 0, s>>>(x, R, d, q, scale);
   else if (vecs <= kQuantWide * 4)
     quantize_cta_kernel<T, 4><<<(unsigned)(R < (1 << 20) ? R : 1 << 20), kQuantWide, 0, s>>>(x, R, d, q, scale);
   else
@@ -737,8 +754,10 @@ cudaError_t launch_head_i8(const HeadI8Args& a, cudaStream_t s) {
   p.vt = (int)((a.V + 2 * (int64_t)p.height - 1) / (2 * p.height));
   CUtensorMap mw, mh, mp;
   if (!tma_matrix(&mw, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, a.weight, a.d, a.V, p.height) ||
-      !tma_matrix(&mh, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, a.h16, a.d, a.R, p.cols / 2) ||
-      !tma_matrix(&mp, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, a.h16, a.d, a.R, (p.cols < kI8Part ? p.cols : kI8Part) / 2))
+      !tma_matrix(&mh, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, a.h16, a.d, a.R, p.cols / 2))
+    return cudaErrorInvalidValue;
+  mp = mh;                                          // (a part is the tile)
+  if (p.cols > kI8Part && !tma_matrix(&mp, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, a.h16, a.d, a.R, kI8Part / 2))
     return cudaErrorInvalidValue;
   head_i8_tokens_kernel<<<a.R < 65536 ? a.R : 65536, kTokenThreads, 0, s>>>(a);
   e = cudaGetLastError();

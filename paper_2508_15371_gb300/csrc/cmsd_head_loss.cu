@@ -100,10 +100,11 @@ __global__ void __launch_bounds__(kPackThreads) head_pack_kernel(const HeadLossA
   }
 }
 
-// (maximum, sum) of two sets of entries, in base 2
+// (maximum, sum) of two sets of entries, in base 2; an empty set is (-inf, 0), and
+// a NaN in either sum stays
 __device__ __forceinline__ void fold(float& m, float& s, float m2, float s2) {
   const float mm = fmaxf(m, m2);
-  s = (s > 0.f ? s * ex2(m - mm) : 0.f) + (s2 > 0.f ? s2 * ex2(m2 - mm) : 0.f);
+  s = (s != 0.f ? s * ex2(m - mm) : 0.f) + (s2 != 0.f ? s2 * ex2(m2 - mm) : 0.f);
   m = mm;
 }
 
@@ -850,7 +851,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
 #pragma unroll
           for (int k = 0; k < 32; ++k) x[k] = ex2(fmaf(z[k], kLog2e, -__shfl_sync(kFull, ref, k)));
           const float ts = across(x, lane, [](float f, float g) { return f + g; });
-          sum[u] = (sum[u] > 0.f ? sum[u] * ex2(mx[u] - ref) : 0.f) + ts;
+          sum[u] = (sum[u] != 0.f ? sum[u] * ex2(mx[u] - ref) : 0.f) + ts;
           mx[u] = nm;
         } else {
           uint16_t* dst = a.dz + (size_t)c0 * a.Vc + v;
@@ -918,9 +919,9 @@ __global__ void __launch_bounds__(kMergeThreads) head_merge_kernel(const HeadLos
       float mm = m;
 #pragma unroll
       for (int j = 0; j < kBatch; ++j) mm = fmaxf(mm, x[j].x);
-      s = s > 0.f ? s * ex2(m - mm) : 0.f;
+      s = s != 0.f ? s * ex2(m - mm) : 0.f;
 #pragma unroll
-      for (int j = 0; j < kBatch; ++j) s += x[j].y * ex2(x[j].x - mm);
+      for (int j = 0; j < kBatch; ++j) s += x[j].y != 0.f ? x[j].y * ex2(x[j].x - mm) : 0.f;
       m = mm;
     }
   }

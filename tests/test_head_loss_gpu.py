@@ -325,6 +325,28 @@ def test_equal_calls_on_streams_and_in_a_graph(cmsd):
             assert torch.equal(out[k], ref[k]), k
 
 
+@pytest.mark.parametrize("R", [40, 300])
+def test_nan_is_not_lost(cmsd, R):
+    """A kept row that holds a NaN has a NaN loss, alone; a NaN in one row of the weight reaches every loss."""
+    d, V = 136, 3000
+    h, w, y, _ = _inputs(R, d, V, ignored=0.2)
+    keep = torch.nonzero(y >= 0)[:, 0]
+    clean = cmsd.lmhead_loss(h, w, y)
+    h2 = h.clone()
+    h2[keep[3], 7] = float("nan")
+    o = cmsd.lmhead_loss(h2, w, y)
+    others = torch.ones(R, dtype=torch.bool, device="cuda")
+    others[keep[3]] = False
+    for k in clean:
+        assert torch.isnan(o[k][keep[3]]) and torch.equal(o[k][others], clean[k][others])
+    for v in (0, 1500, V - 1):
+        w2 = w.clone()
+        w2[v, 5] = float("nan")
+        o = cmsd.lmhead_loss(h, w2, y)
+        assert torch.isnan(o["loss"][keep]).all() and torch.isnan(o["lse"][keep]).all()
+        assert (o["loss"][y < 0] == 0).all()
+
+
 def test_calls_at_once_on_two_streams(cmsd):
     """Each with its own workspace; both kinds of kernels, many times over."""
     sizes = [(70, 256, 3000), (700, 136, 2500)]
