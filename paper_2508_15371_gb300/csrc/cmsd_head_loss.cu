@@ -947,35 +947,38 @@ __global__ void __launch_bounds__(kMergeThreads) head_merge_kernel(const HeadLos
 }
 
 // ---- the hidden states' gradient, rounded and put back in place -------------------
-template <bool kFew>
-__global__ void __launch_bounds__(256) head_unpack_kernel(const HeadLossArgs a) {
+// kLanes threads share four columns' parts (four where there are many parts: their
+// loads are in flight together).
+constexpr int kUnpackThreads = 128;
+template <bool kFew, int kLanes>
+__global__ void __launch_bounds__(kUnpackThreads) head_unpack_kernel(const HeadLossArgs a) {
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
-  const int per = a.d / 4;                           // four columns and every fourth part a thread
-  const size_t total = (size_t)a.R * per, step = (size_t)a.Rp * a.d;
-  const int lane = threadIdx.x & 31, sub = lane >> 3;
-  const size_t warps = (size_t)gridDim.x * 8, warp = (size_t)blockIdx.x * 8 + (threadIdx.x >> 5);
-  for (size_t i0 = warp * 8; i0 < total; i0 += warps * 8) {
-    const size_t i = i0 + (lane & 7);
-    const int r = i < total ? (int)(i / per) : 0, j = (int)(i - (size_t)r * per) * 4;
-    const int p = i < total ? (kFew ? (kept(a, a.labels[r]) ? r : -1) : a.pos[r]) : -1;
+  const int lane = threadIdx.x & 31, sub = kLanes == 1 ? 0 : lane >> 3;
+  constexpr int kCols = 32 / kLanes;                 // groups of four columns a warp
+  const int j = (int)((blockIdx.x * (kUnpackThreads / 32) + (threadIdx.x >> 5)) * kCols + (lane & (kCols - 1))) * 4;
+  const size_t step = (size_t)a.Rp * a.d;
+  for (int r = blockIdx.y; r < a.R; r += gridDim.y) {
+    const int p = kFew ? (kept(a, a.labels[r]) ? r : -1) : a.pos[r];
     float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (p >= 0) {
+    if (p >= 0 && j < a.d) {
       const float* src = a.dh + (size_t)p * a.d + j;
 #pragma unroll 4
-      for (int k = sub; k < a.split; k += 4) {
+      for (int k = sub; k < a.split; k += kLanes) {
         const float4 y = __ldcg(reinterpret_cast<const float4*>(src + k * step));
         x = make_float4(x.x + y.x, x.y + y.y, x.z + y.z, x.w + y.w);
       }
     }
+    if (kLanes > 1) {
 #pragma unroll
-    for (int o = 8; o <= 16; o <<= 1) {
-      x.x += __shfl_xor_sync(kFull, x.x, o);
-      x.y += __shfl_xor_sync(kFull, x.y, o);
-      x.z += __shfl_xor_sync(kFull, x.z, o);
-      x.w += __shfl_xor_sync(kFull, x.w, o);
+      for (int o = 8; o <= 16; o <<= 1) {
+        x.x += __shfl_xor_sync(kFull, x.x, o);
+        x.y += __shfl_xor_sync(kFull, x.y, o);
+        x.z += __shfl_xor_sync(kFull, x.z, o);
+        x.w += __shfl_xor_sync(kFull, x.w, o);
+      }
     }
-    if (sub == 0 && i < total)
+    if (sub == 0 && j < a.d)
       *reinterpret_cast<uint2*>(a.d_hidden + (size_t)r * a.d + j) = make_uint2(pack_bf(x.x, x.y), pack_bf(x.z, x.w));
   }
 }
@@ -984,10 +987,10 @@ unsigned tiles(int64_t n, int t) { return (unsigned)((n + t - 1) / t); }
 // a launch that may begin before what precedes it on the stream has ended (early:
 // the first launch of a call does not)
 template <typename... P, typename... A>
-cudaError_t launch(bool early, void (*kernel)(P...), unsigned grid, unsigned threads, size_t smem, cudaStream_t s,
+cudaError_t launch(bool early, void (*kernel)(P...), dim3 grid, unsigned threads, size_t smem, cudaStream_t s,
                    A... args) {
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(grid);
+  cfg.gridDim = grid;
   cfg.blockDim = dim3(threads);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = s;
@@ -1004,6 +1007,14 @@ cudaError_t launch_pack(const HeadLossArgs& a, cudaStream_t s) {
   const int ctas = (int)tiles(a.R, rows);
   head_pack_kernel<<<ctas + kPackZero, kPackThreads, 0, s>>>(a, rows, ctas);
   return cudaGetLastError();
+}
+
+template <bool kFew>
+cudaError_t launch_unpack(const HeadLossArgs& a, cudaStream_t s) {
+  const bool shared = a.split >= 4;
+  const dim3 grid(tiles(a.d, kUnpackThreads * (shared ? 1 : 4)), (unsigned)(a.R < 65535 ? a.R : 65535));
+  return shared ? launch(true, head_unpack_kernel<kFew, 4>, grid, kUnpackThreads, 0, s, a)
+                : launch(true, head_unpack_kernel<kFew, 1>, grid, kUnpackThreads, 0, s, a);
 }
 
 bool encode_maps(const HeadLossArgs& a, bool backward, Maps* m) {
@@ -1137,9 +1148,7 @@ cudaError_t launch_head_loss_backward(const HeadLossArgs& a, cudaStream_t s) {
     if (e != cudaSuccess) return e;
   }
   if (!a.d_hidden) return cudaSuccess;
-  const int64_t n4 = (int64_t)a.R * (a.d / 4);
-  return launch(true, few ? head_unpack_kernel<true> : head_unpack_kernel<false>,
-                tiles(n4 < 64 * 16384 ? n4 : 64 * 16384, 64), 256, 0, s, a);
+  return few ? launch_unpack<true>(a, s) : launch_unpack<false>(a, s);
 }
 
 }  // namespace cmsd
