@@ -28,7 +28,7 @@ def _quantized(x):
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 @pytest.mark.parametrize("R,d", [(1, 16), (3, 32), (7, 208), (33, 1024), (5, 2048), (2, 2064), (300, 4096), (3, 8176),
-                                 (2, 65536), (70000, 16), (8192, 512), (8193, 528), (9001, 256), (8195, 1024)])
+                                 (2, 65536), (70000, 16), (8192, 512), (8193, 528), (9001, 256), (32770, 1024)])
 def test_quantize_rows(cmsd, R, d, dtype):
     g = torch.Generator(device="cuda").manual_seed(R + d)
     x = torch.randn(R, d, generator=g, device="cuda") * torch.exp(4 * torch.randn(R, 1, generator=g, device="cuda"))
