@@ -222,9 +222,10 @@ cudaError_t launch_quantize(const T* x, int R, int d, int8_t* q, float* scale, c
     const int64_t per = kQuantThreads / 32 * per_warp;
     return (unsigned)((R + per - 1) / per);
   };
-  // Several rows a warp where that leaves several CTAs an SM (bf16, us with and
-  // without: d=512 R=2048 3.3, 2.7; R=4096 3.6, 3.5; R=8192 4.7, 5.3; R=65536 20, 30;
-  // two of d=1024 R=16384 10.8, 10.5; R=65536 33, 36)
+  // Several rows a warp where enough CTAs are left to fill the SMs (us with and
+  // without.  Four rows, bf16 d=512: R=2048 3.3, 2.7; 4096 3.6, 3.5; 8192 4.7, 5.3;
+  // 65536 20, 30.  Two rows, bf16 d=1024: R=16384 10.7, 10.5; 32768 17.8, 17.9; 65536
+  // 33.2, 35.5; f32 d=512: 8192 4.0, 3.9; 32768 12.0, 12.3; 65536 21.0, 21.8)
   if (vecs <= 32 * 2 && R >= 8192)
     quantize_warp_kernel<T, 2, 4><<<ctas(4), kQuantThreads, 0, s>>>(x, R, d, q, scale);
   else if (vecs <= 32 * 4 && R >= 32768)

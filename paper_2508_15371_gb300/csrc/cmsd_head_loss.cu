@@ -116,8 +116,9 @@ __device__ __forceinline__ void fold(float& m, float& s, float m2, float s2) {
 // 64.  A pair reads (256 + 256) * 2 bytes of its operands per K from L2 for
 // 256 * 256 products; one CTA alone with a 128 x 256 tile would read half as
 // much again per product, and L2 would bound the tensor cores.  (R=4096 d=2048
-// V=128256, 2867 rows kept: loss 857 us, 1.76 PFLOP/s, tensor pipe 80 %, L2 15.6
-// TB/s; both gradients 2685 us, 1.68 PFLOP/s.)
+// V=128256, 2867 rows kept: loss 855-885 us, 1.70-1.76 PFLOP/s; both gradients
+// 2680-2800 us, 1.61-1.69 PFLOP/s.  Counters at R=2048 d=2048 V=65536: loss 80 % of
+// the tensor pipe, 15.6 TB/s from L2; gradients 80 %; P 75 %.)
 //   logits   A = packed rows, B = weight, K = d; both rows of 128 bytes along K
 //   d_hidden A = P, B = weight (its rows run along N), K = the piece's entries
 //   d_weight A = P (its rows run along M), B = packed rows (along N), K = rows
