@@ -331,10 +331,24 @@ def _stream_of(cur):
     return _raw_stream(cur) if _raw_stream is not None else _torch_mod.cuda.current_stream().cuda_stream
 
 
+def _ints(what, *sizes):
+    """Refuses sizes that the library's 32-bit arguments do not hold (ctypes would take them modulo 2^32)."""
+    if max(sizes) > 0x7FFFFFFF:
+        raise CmsdError(f"{what}: sizes out of range")
+
+
+def _ignored(index):
+    index = int(index)
+    if not -0x80000000 <= index <= 0x7FFFFFFF:
+        raise CmsdError("ignore_index must be a 32-bit integer, as the labels are")
+    return index
+
+
 def _head_sizes(hidden, weight):
     h, w = hidden.shape, weight.shape
     if len(h) != 2 or len(w) != 2 or h[1] != w[1]:
         raise CmsdError("hidden [R, d] and weight [V, d] must share d")
+    _ints("hidden [R, d], weight [V, d]", h[0], h[1], w[0])
     return h[0], h[1], w[0]
 
 
@@ -346,6 +360,7 @@ def _given(out, name, shape, dtype, like):
 
 def _head_workspace(what, R, d, V):
     torch = _torch()
+    _ints(what, R, d, V)
     n = int(getattr(lib(), what)(int(R), int(d), int(V)))
     if n == 0:
         raise CmsdError(f"{what}: sizes out of range")
@@ -376,13 +391,14 @@ def lmhead_loss(hidden, weight, labels, ignore_index=-100, out=None, ws=None):
     loss and lse ([R], float32; 0 in rows whose label is ignore_index)."""
     torch = _torch()
     R, d, V = _head_sizes(hidden, weight)
+    ignore_index = _ignored(ignore_index)
     f32, bf16 = torch.float32, torch.bfloat16
     loss, lse = _given(out, "loss", (R,), f32, hidden), _given(out, "lse", (R,), f32, hidden)
     cur = _current(hidden)
     _need(cur, ((hidden, (R, d), bf16, "hidden"), (weight, (V, d), bf16, "weight"),
                 (labels, (R,), torch.int32, "labels"), (loss, (R,), f32, "loss"), (lse, (R,), f32, "lse")))
     ws = ws if ws is not None else lmhead_loss_workspace(R, d, V)
-    rc = lib().cmsd_lmhead_loss(hidden.data_ptr(), weight.data_ptr(), labels.data_ptr(), R, d, V, int(ignore_index),
+    rc = lib().cmsd_lmhead_loss(hidden.data_ptr(), weight.data_ptr(), labels.data_ptr(), R, d, V, ignore_index,
                                 loss.data_ptr(), lse.data_ptr(), ws.data_ptr(), _need_ws(ws, cur), _stream_of(cur))
     if rc != OK:
         _check(rc, "cmsd_lmhead_loss")
@@ -397,6 +413,7 @@ def lmhead_loss_backward(hidden, weight, labels, lse, grad_loss, ignore_index=-1
     [V, d], with weight_grad), written whole."""
     torch = _torch()
     R, d, V = _head_sizes(hidden, weight)
+    ignore_index = _ignored(ignore_index)
     f32, bf16 = torch.float32, torch.bfloat16
     o = {}
     specs = [(hidden, (R, d), bf16, "hidden"), (weight, (V, d), bf16, "weight"),
@@ -411,7 +428,7 @@ def lmhead_loss_backward(hidden, weight, labels, lse, grad_loss, ignore_index=-1
     _need(cur, specs)
     ws = ws if ws is not None else lmhead_loss_backward_workspace(R, d, V)
     rc = lib().cmsd_lmhead_loss_backward(hidden.data_ptr(), weight.data_ptr(), labels.data_ptr(), lse.data_ptr(),
-                                         grad_loss.data_ptr(), R, d, V, int(ignore_index), _ptr(o.get("d_hidden")),
+                                         grad_loss.data_ptr(), R, d, V, ignore_index, _ptr(o.get("d_hidden")),
                                          _ptr(o.get("d_weight")), ws.data_ptr(), _need_ws(ws, cur), _stream_of(cur))
     if rc != OK:
         _check(rc, "cmsd_lmhead_loss_backward")
@@ -427,6 +444,7 @@ def quantize_rows(x, out=None):
     if x.dtype not in (torch.float32, torch.bfloat16):
         raise CmsdError(f"x must be float32 or bfloat16, got {x.dtype}")
     R, d = x.shape
+    _ints("x [R, d]", R, d)
     q, scale = _given(out, "q", (R, d), torch.int8, x), _given(out, "scale", (R,), torch.float32, x)
     cur = _current(x)
     _need(cur, ((x, (R, d), x.dtype, "x"), (q, (R, d), torch.int8, "q"), (scale, (R,), torch.float32, "scale")))

@@ -149,3 +149,42 @@ def test_binding_refuses_before_the_library(cmsd):
     for call in bad:
         with pytest.raises(cmsd.CmsdError):
             call()
+
+
+# ---- sizes that a C int does not hold (they would be taken modulo 2^32) ----------------
+
+@pytest.mark.parametrize("call", ["lmhead_loss_workspace", "lmhead_loss_backward_workspace", "lmhead_i8_workspace"])
+@pytest.mark.parametrize("sizes", [(2**32 + 5, 64, 100), (5, 2**32 + 64, 100), (5, 64, 2**32 + 100), (2**31, 64, 100)])
+def test_workspace_sizes_past_32_bits(cmsd, call, sizes):
+    with pytest.raises(cmsd.CmsdError, match="out of range"):
+        getattr(cmsd, call)(*sizes)
+
+
+def test_rows_past_32_bits(cmsd):
+    torch = pytest.importorskip("torch")
+    big, few = (2**32 + 5, 64), (5, 64)
+    meta = {"device": "meta"}
+    bf16, i8 = torch.bfloat16, torch.int8
+    for h, w in ((big, few), (few, big)):
+        hidden, weight = torch.empty(h, dtype=bf16, **meta), torch.empty(w, dtype=bf16, **meta)
+        rows = torch.empty(h[0], **meta)
+        labels = torch.empty(h[0], dtype=torch.int32, **meta)
+        with pytest.raises(cmsd.CmsdError, match="out of range"):
+            cmsd.lmhead_loss(hidden, weight, labels)
+        with pytest.raises(cmsd.CmsdError, match="out of range"):
+            cmsd.lmhead_loss_backward(hidden, weight, labels, rows, rows)
+        with pytest.raises(cmsd.CmsdError, match="out of range"):
+            cmsd.lmhead_i8(hidden.to(i8), rows, weight.to(i8), torch.empty(w[0], **meta))
+    with pytest.raises(cmsd.CmsdError, match="out of range"):
+        cmsd.quantize_rows(torch.empty(big, **meta))
+
+
+@pytest.mark.parametrize("ignore", [2**32 - 100, 2**31, -2**31 - 1])
+def test_ignore_index_past_32_bits(cmsd, ignore):
+    torch = pytest.importorskip("torch")
+    h, w = torch.empty(5, 64, dtype=torch.bfloat16), torch.empty(9, 64, dtype=torch.bfloat16)
+    y, f = torch.zeros(5, dtype=torch.int32), torch.zeros(5)
+    with pytest.raises(cmsd.CmsdError, match="ignore_index"):
+        cmsd.lmhead_loss(h, w, y, ignore_index=ignore)
+    with pytest.raises(cmsd.CmsdError, match="ignore_index"):
+        cmsd.lmhead_loss_backward(h, w, y, f, f, ignore_index=ignore)
