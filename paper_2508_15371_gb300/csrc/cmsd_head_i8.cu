@@ -437,6 +437,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kI8Threads, 1)
         if (lane == 0) {
           for (int k = 0; k < ks; ++k, ++g) {
             if (ok) ok = bar_wait<false>(wempty + 8 * s, phase);
+            if (!ok) break;
             mbar_arrive_tx(wfull + 8 * s, bytes);
             tma_box(base + s * kI8WStage, &map_w, k * kI8K, y, wfull + 8 * s);
             if (++s == S::kW) {
@@ -472,6 +473,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kI8Threads, 1)
         if (lane == 0) {
           for (int k = 0; k < ks; ++k, ++g) {
             if (ok) ok = bar_wait<true>(hempty + 8 * s, phase);
+            if (!ok) break;
             if (rank == 0) mbar_arrive_tx(hfull + 8 * s, (uint32_t)(cols * kI8K * 2));   // both halves
             const uint32_t dst = hbase + s * S::kHStage;
             tma_box_pair(dst, map, k * kI8K, y, hfull0 + 8 * s);
@@ -514,7 +516,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kI8Threads, 1)
           tmem_fence_after();
           const uint64_t h0 = mma_desc(hbase + s * S::kHStage, 0), h1 = h0 + half;
           const uint32_t d = tbase + db * S::kSum, at = abase + b * 64;
-          if (leader) {
+          if (leader && ok) {
 #pragma unroll
             for (int j = 0; j < kI8K / 16; ++j)
               mma_pair_tmem_a(d, at + j * 8, (j >> 2 ? h1 : h0) + (uint64_t)(2 * (j & 3)), idesc,
@@ -694,7 +696,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kI8Threads, 1)
       }
     }
   }
-  if (!ok) atomicOr(a.err, 4u);
+  if (!ok) {
+    atomicOr(a.err, 4u);
+    let_settle();
+  }
   __syncwarp();
   tmem_fence_before();
   cluster_sync_all();
@@ -770,8 +775,7 @@ cudaError_t launch_head_i8(const HeadI8Args& a, cudaStream_t s) {
   head_i8_tokens_kernel<<<a.R < 65536 ? a.R : 65536, kTokenThreads, 0, s>>>(a);
   e = cudaGetLastError();
   if (e != cudaSuccess) return e;
-  const int64_t tiles = (int64_t)p.vt * p.rt;
-  if (tiles + pairs >= (1ll << 31)) return cudaErrorInvalidValue;   // (64 TB of logits)
+  const int64_t tiles = (int64_t)p.vt * p.rt;       // (31 bits hold them: R V < 2^46, V <= 2^30)
   const int grid = (int)(2 * (tiles < pairs ? tiles : pairs));
   return a.dtype == 0 ? launch_i8_cols<false>(a, p, grid, dev, mw, mh, mp, s) : launch_i8_cols<true>(a, p, grid, dev, mw, mh, mp, s);
 }

@@ -337,12 +337,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(64 + 32 * epi_warps(
       asm volatile("fence.proxy.async.global;" ::: "memory");
       const Work w = work_of<OP>(a, *a.n, vlen, a.d_hidden != nullptr, a.d_weight != nullptr);
       int g = 0;
-      for (int i = 0; i < w.total; ++i) {
+      for (int i = 0; i < w.total && ok; ++i) {
         const Tile t = tile_of<OP>(a, w, i);
         const int am = t.m * kPairTile + (int)rank * 128, bn = t.n * kPairTile + (int)rank * 128;
         for (int kb = 0; kb < t.kb; ++kb, ++g) {
           const int s = g % kStages;
           if (g >= kStages && ok) ok = bar_wait<true>(empty + 8 * s, (uint32_t)((g / kStages - 1) & 1));
+          if (!ok) break;
           if (rank == 0 && g >= early)
             mbar_arrive_tx(full + 8 * s, OP == kOpFewGrad && !t.dw ? 2 * kHalfBytes + (uint32_t)cols * 128 : 2 * kStageBytes);
           const uint32_t sa = base + s * kStageBytes, sb = sa + kHalfBytes, bar = full0 + 8 * s;
@@ -379,7 +380,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(64 + 32 * epi_warps(
       const uint32_t empty1 = map_to(empty, 1), tfull1 = map_to(tfull, 1);
       const uint32_t empty0 = map_to(empty, 0), tfull0 = map_to(tfull, 0);
       int g = 0, c = 0;                              // stages; sums handed over
-      for (int i = 0; i < w.total; ++i) {
+      for (int i = 0; i < w.total && ok; ++i) {
         const Tile t = tile_of<OP>(a, w, i);
         const bool few = OP == kOpFewGrad && !t.dw;
         const uint32_t idesc = !grad_op(OP) ? mma_idesc(256, 256, true, false, false)
@@ -397,6 +398,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(64 + 32 * epi_warps(
           for (uint32_t more = 0; kb < end; ++kb, ++g) {
             const int s = g % kStages;
             if (ok) ok = bar_wait<true>(full + 8 * s, (uint32_t)((g / kStages) & 1));
+            if (!ok) break;
             tmem_fence_after();
             const uint64_t ad = mma_desc(base + s * kStageBytes, kHalfBytes / 2);
             const uint64_t bd = mma_desc(base + s * kStageBytes + kHalfBytes, kHalfBytes / 2);
@@ -408,6 +410,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(64 + 32 * epi_warps(
             mma_commit_pair(empty0 + 8 * s);
             mma_commit_pair(empty1 + 8 * s);
           }
+          if (!ok) break;
           mma_commit_pair(tfull0 + 8 * b);
           mma_commit_pair(tfull1 + 8 * b);
           ++c;
@@ -604,7 +607,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(64 + 32 * epi_warps(
       if (lane == 0) tma_store_wait();
     }
   }
-  if (!ok) atomicOr(a.err, 4u);
+  if (!ok) {
+    atomicOr(a.err, 4u);
+    let_settle();
+  }
   __syncwarp();
   tmem_fence_before();
   cluster_sync_all();
@@ -617,8 +623,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(64 + 32 * epi_warps(
 //
 // With up to 128 rows the products are bound by memory as long as the tensor
 // cores do no more than they must: a tile of 256 rows takes 512 cycles for 64 of
-// K however few of them are live (R=33 d=1024 V=32001: the loss 26 us), in which
-// memory delivers half a tile more.  So the roles change: the MMA's M is the
+// K however few of them are live, in which memory delivers half a tile more.  So the roles change: the MMA's M is the
 // vocabulary (or d, for d_hidden) and its N the rows, in multiples of 32.
 //   logits    A = weight (128 entries a CTA at most), B = packed rows, K = d
 //   d_hidden  A = weight (its rows run along M = d), B = P, K = entries, together
@@ -721,10 +726,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
       asm volatile("griddepcontrol.wait;" ::: "memory");
       asm volatile("fence.proxy.async.global;" ::: "memory");
       int g = 0;
-      for (int i = 0; i < mine; ++i) {
+      for (int i = 0; i < mine && ok; ++i) {
         for (int k = 0; k < kb; ++k, ++g) {
           const int s = g % kFewStages;
           if (g >= kFewStages && ok) ok = bar_wait<true>(empty + 8 * s, (uint32_t)((g / kFewStages - 1) & 1));
+          if (!ok) break;
           if (g >= early) load_a(pair + i * pairs, k, s);
           tma_box_pair(base + s * kFewStage + kHalfBytes, &map_b, k * 64, rank * (p.cols / 2), full0 + 8 * s);
         }
@@ -754,7 +760,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
           tmem_fence_after();
           const uint64_t ad = mma_desc(base + s * kFewStage, 0);
           const uint64_t bd = mma_desc(base + s * kFewStage + kHalfBytes, 0);
-          if (leader) {
+          if (leader && ok) {
 #pragma unroll
             for (int j = 0; j < 4; ++j) mma_pair(d, ad + (uint64_t)(2 * j), bd + (uint64_t)(2 * j), idesc, k > k0 || j > 0);
             mma_commit_pair(empty0 + 8 * s);
@@ -766,7 +772,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
             phase ^= 1;
           }
         }
-        if (leader) {
+        if (leader && ok) {
           mma_commit_pair(tfull0 + 8 * b);
           mma_commit_pair(tfull1 + 8 * b);
         }
@@ -887,7 +893,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
       }
     }
   }
-  if (!ok) atomicOr(a.err, 4u);
+  if (!ok) {
+    atomicOr(a.err, 4u);
+    let_settle();
+  }
   __syncwarp();
   tmem_fence_before();
   cluster_sync_all();

@@ -234,5 +234,11 @@ __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity) {
   } while (clock64() - t0 < (1ll << 31));
   return false;
 }
+// After a wait gave up nothing more is issued; copies and MMAs in flight (of a few
+// microseconds) end within this millisecond, before their memory goes.
+__device__ __forceinline__ void let_settle() {
+  const long long t0 = clock64();
+  while (clock64() - t0 < (1ll << 21)) __nanosleep(1000);
+}
 
 }  // namespace cmsd
