@@ -331,15 +331,16 @@ def _stream_of(cur):
     return _raw_stream(cur) if _raw_stream is not None else _torch_mod.cuda.current_stream().cuda_stream
 
 
-def _ints(what, *sizes):
-    """Refuses sizes that the library's 32-bit arguments do not hold (ctypes would take them modulo 2^32)."""
-    if max(sizes) > 0x7FFFFFFF:
-        raise CmsdError(f"{what}: sizes out of range")
+_INT_MAX = 0x7FFFFFFF      # ctypes takes larger integers modulo 2^32
+
+
+def _too_large(what):
+    raise CmsdError(f"{what}: sizes out of range")
 
 
 def _ignored(index):
     index = int(index)
-    if not -0x80000000 <= index <= 0x7FFFFFFF:
+    if not -_INT_MAX - 1 <= index <= _INT_MAX:
         raise CmsdError("ignore_index must be a 32-bit integer, as the labels are")
     return index
 
@@ -348,8 +349,10 @@ def _head_sizes(hidden, weight):
     h, w = hidden.shape, weight.shape
     if len(h) != 2 or len(w) != 2 or h[1] != w[1]:
         raise CmsdError("hidden [R, d] and weight [V, d] must share d")
-    _ints("hidden [R, d], weight [V, d]", h[0], h[1], w[0])
-    return h[0], h[1], w[0]
+    R, d, V = h[0], h[1], w[0]
+    if R > _INT_MAX or d > _INT_MAX or V > _INT_MAX:
+        _too_large("hidden [R, d], weight [V, d]")
+    return R, d, V
 
 
 def _given(out, name, shape, dtype, like):
@@ -360,7 +363,8 @@ def _given(out, name, shape, dtype, like):
 
 def _head_workspace(what, R, d, V):
     torch = _torch()
-    _ints(what, R, d, V)
+    if max(R, d, V) > _INT_MAX:
+        _too_large(what)
     n = int(getattr(lib(), what)(int(R), int(d), int(V)))
     if n == 0:
         raise CmsdError(f"{what}: sizes out of range")
@@ -444,7 +448,8 @@ def quantize_rows(x, out=None):
     if x.dtype not in (torch.float32, torch.bfloat16):
         raise CmsdError(f"x must be float32 or bfloat16, got {x.dtype}")
     R, d = x.shape
-    _ints("x [R, d]", R, d)
+    if R > _INT_MAX or d > _INT_MAX:
+        _too_large("x [R, d]")
     q, scale = _given(out, "q", (R, d), torch.int8, x), _given(out, "scale", (R,), torch.float32, x)
     cur = _current(x)
     _need(cur, ((x, (R, d), x.dtype, "x"), (q, (R, d), torch.int8, "q"), (scale, (R,), torch.float32, "scale")))
