@@ -129,7 +129,7 @@ __device__ __forceinline__ void fold(float& m, float& s, float m2, float s2) {
 //               counted at the first CTA's barrier;
 //   warp 1      lane 0 of the first CTA issues the MMAs of both;
 //   warps 2..9  the epilogue: warp w reads TMEM lanes 32 (w mod 4) .., the two
-//               warps of a quarter 128 of the 256 columns each (the loss: warps
+//               warps of a quarter 128 of the 256 columns each (the logits: warps
 //               2..17, 64 columns each, whose sums stay in registers).
 // Barriers: full (TMA -> MMA), empty (MMA -> TMA, in both CTAs), tfull (MMA ->
 // epilogue, in both) and tempty (both epilogues -> MMA) for each of the two
@@ -141,18 +141,21 @@ constexpr int kStages = 6;
 constexpr int kHalfBytes = 128 * 128;                 // 128 rows of 64 bf16
 constexpr int kStageBytes = 2 * kHalfBytes;           // A's and B's half
 constexpr int kEpiWarps = 8;
-__host__ __device__ constexpr int epi_warps(int op) { return op == kOpStats ? 16 : kEpiWarps; }
+__host__ __device__ constexpr int epi_warps(int op) { return grad_op(op) ? kEpiWarps : 16; }
 constexpr int kPairThreads = 64 + 32 * kEpiWarps;
 constexpr int kOutBytes = 32 * 128;                   // a warp's 32 rows of 128 bytes on their way out
+constexpr int kDzBytes = 32 * 64;                     // a warp's 32 rows of 32 entries of P
+static_assert(16 * kDzBytes <= kEpiWarps * kOutBytes, "P's buffers");
 constexpr size_t kPairSmem = 1024 + (size_t)kStages * kStageBytes + (size_t)kEpiWarps * kOutBytes + 8 * (2 * kStages + 4) + 16;
 constexpr int kTmemCols = 512;
 // The tensor cores round their sums towards zero at each step of 16 of K: at
 // d=2048 logits came out short by 1.5e-6 of their size, all in the same direction,
-// and losses wrong by 1.1e-6.  So the loss's sums are cut after kSumBlocks blocks of
-// 64 and added up in registers: each part is shorter and smaller (losses 5.5e-7 at
-// any d; parts of 8 blocks 2.6e-7, but 914 against 880 us at R=4096 d=2048
-// V=128256, 857 uncut).  Not so the sums that P is formed from, which is rounded to
-// bf16.
+// and losses wrong by 1.1e-6.  So the logits' sums are cut after kSumBlocks blocks of
+// 64 and added up in registers: each part is shorter and smaller (losses 5.5e-7;
+// parts of 8 blocks 2.6e-7, but 914 against 880 us at R=4096 d=2048
+// V=128256, 857 uncut).  P is formed from sums cut alike: its logits are then those
+// of the lse that it is given, to the bit, and p - 1 of a label with nearly all of
+// the probability is right although both are off by more than it is.
 constexpr int kSumBlocks = 16;
 static_assert(kPairSmem <= 227 * 1024, "shared memory");
 
@@ -264,7 +267,7 @@ struct Maps {
   CUtensorMap weight_n;    // weight, 64 (d) x 64 entries
   CUtensorMap dz_k;        // P, 64 (entries) x 128 rows
   CUtensorMap dz_m;        // P, 64 (entries) x 64 rows
-  CUtensorMap dz_out;      // P, 64 (entries) x 32 rows
+  CUtensorMap dz_out;      // P, 32 (entries) x 32 rows
   CUtensorMap dw_out;      // d_weight, 64 (d) x 32 entries
   CUtensorMap dh_out;      // d_hidden's parts, 32 (d) x 32 rows
 };
@@ -390,8 +393,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(64 + 32 * epi_warps(
         // K = 16 further: 32 bytes along the rows, or 16 rows
         const uint64_t da = grad_op(OP) && (t.dw || few) ? 2048 >> 4 : 32 >> 4, db = grad_op(OP) && !few ? 2048 >> 4 : 32 >> 4;
         int kb = 0;
-        do {                                         // (once but for the loss)
-          const int end = OP == kOpStats ? min(t.kb, kb + kSumBlocks) : t.kb, b = c & 1;
+        do {                                         // (once but for the logits)
+          const int end = grad_op(OP) ? t.kb : min(t.kb, kb + kSumBlocks), b = c & 1;
           if (c >= 2 && ok) ok = bar_wait<true>(tempty + 8 * b, (uint32_t)((c / 2 - 1) & 1));
           tmem_fence_after();
           const uint32_t d = tbase + (uint32_t)(b * 256);
@@ -423,19 +426,22 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(64 + 32 * epi_warps(
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const int n = *a.n;
     const Work w = work_of<OP>(a, n, vlen, a.d_hidden != nullptr, a.d_weight != nullptr);
-    if (OP == kOpStats) {
-      // ---- the loss's epilogue: each row's maximum and sum of a tile's entries ---------
+    if (!grad_op(OP)) {
+      // ---- the logits' epilogue: each row's maximum and sum of a tile's entries, or P ---
       const uint32_t tempty0 = map_to(tempty, 0);
       const int q = warp & 3, group = (warp - 2) >> 2;
       const uint32_t quarter = tbase + ((uint32_t)(q * 32) << 16) + (uint32_t)(group * 64);
       float2* s_half = reinterpret_cast<float2*>(pair_smem + (base - raw) + kStages * kStageBytes);
+      // this warp's rows of P on their way out: 64 bytes of each, swizzled as the boxes are
+      const uint32_t obuf = base + kStages * kStageBytes + (warp - 2) * kDzBytes, orow = obuf + lane * 64;
+      const uint32_t x4 = (uint32_t)(lane >> 1 & 3);
       int sums = 0;                                    // sums read
       for (int i = 0; i < w.total; ++i) {
         const Tile t = tile_of<OP>(a, w, i);
         const int row = t.m * kPairTile + (int)rank * 128 + q * 32 + lane;
         const int col = t.n * kPairTile + group * 64;
         const bool live = row < n;
-        const int lab = live ? a.lab[row] : -1;
+        const int lab = live ? a.lab[row] - v0 : -1;   // (the loss: v0 is 0)
         float z[64];
         for (int kb = 0; kb < t.kb; kb += kSumBlocks, ++sums) {
           const int b = sums & 1;
@@ -464,6 +470,30 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(64 + 32 * epi_warps(
           tmem_fence_before();
           __syncwarp();
           if (lane == 0) mbar_arrive_cluster(tempty0 + 8 * b);   // this warp's columns have been read
+        }
+        if (OP == kOpDz) {
+          const float lse = live ? a.plse[row] : 0.f, gr = live ? a.pgrad[row] : 0.f;
+#pragma unroll
+          for (int c = 0; c < 64; c += 32) {
+#pragma unroll
+            for (int k = c; k < c + 32; ++k)
+              z[k] = live && col + k < vlen ? (ex2((z[k] - lse) * kLog2e) - (lab == col + k ? 1.f : 0.f)) * gr : 0.f;
+            if (lane == 0) tma_store_wait_read();
+            __syncwarp();
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              const float* v = z + c + 8 * k;
+              st_shared(orow + (((uint32_t)k ^ x4) << 4), pack_bf(v[0], v[1]), pack_bf(v[2], v[3]),
+                        pack_bf(v[4], v[5]), pack_bf(v[6], v[7]));
+            }
+            smem_to_copies();
+            __syncwarp();
+            if (lane == 0) {
+              tma_store(&maps.dz_out, col + c, row - lane, obuf);
+              tma_store_commit();
+            }
+          }
+          continue;
         }
         if (lab >= col && lab < col + 64) {
           float zl = z[0];
@@ -495,6 +525,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(64 + 32 * epi_warps(
           a.part[(size_t)(col / kHeadPart) * a.Rp + row] = make_float2(mx, sum);
         }
       }
+      if (OP == kOpDz && lane == 0) tma_store_wait();
     } else {
       const uint32_t tempty0 = map_to(tempty, 0);
       const int q = warp & 3, half = (warp - 2) >> 2;
@@ -527,19 +558,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(64 + 32 * epi_warps(
         if (ok) ok = bar_wait<true>(tfull + 8 * b, (uint32_t)((i / 2) & 1));
         __syncwarp();
         tmem_fence_after();
-        const int row0 = t.m * kPairTile + (int)rank * 128 + q * 32, row = row0 + lane;
+        const int row0 = t.m * kPairTile + (int)rank * 128 + q * 32;
         const int col = t.n * kPairTile + half * 128;
         const uint32_t src = tbase + ((uint32_t)(q * 32) << 16) + (uint32_t)(b * 256 + half * 128);
-        const bool live = row < n;
         // few rows, d_hidden: a lane is an entry of d, the columns are rows, every second group of 32 for each half
         const bool few = OP == kOpFewGrad && !t.dw;
-        int lab = -1;
-        float lse2 = 0.f, gr = 0.f;
-        if (!grad_op(OP) && live) lab = a.lab[row] - v0;
-        if (OP == kOpDz && live) {
-          lse2 = a.plse[row] * kLog2e;
-          gr = a.pgrad[row];
-        }
         if (few) {
           const int x = t.n * kPairTile + (int)rank * 128 + q * 32 + lane;
           const uint32_t at = tbase + ((uint32_t)(q * 32) << 16) + (uint32_t)(b * 256);
@@ -575,15 +598,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(64 + 32 * epi_warps(
             if (lane == 0) mbar_arrive_cluster(tempty0 + 8 * b);   // this warp's columns have been read
           }
           const int j0 = col + c;
-          if (OP == kOpDz) {
-            float p[32];
-#pragma unroll
-            for (int k = 0; k < 32; ++k)
-              p[k] = live && j0 + k < vlen
-                         ? (ex2(fmaf(z[k], kLog2e, -lse2)) - (lab == j0 + k ? 1.f : 0.f)) * gr
-                         : 0.f;
-            out_bf16(p, c, row0, j0, true, &maps.dz_out);
-          } else if (t.dw) {
+          if (t.dw) {
             out_bf16(z, c, v0 + row0, j0, v0 + row0 < a.V && (j0 & ~63) < a.d, &maps.dw_out);
           } else {
             if (lane == 0) tma_store_wait_read();
@@ -790,7 +805,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
         x.x = label - v0;
         x.w = 1;
         if (OP == kFewDz) {
-          x.y = __float_as_int(a.lse_in[c] * kLog2e);
+          x.y = __float_as_int(a.lse_in[c]);
           x.z = __float_as_int(a.grad[c]);
         }
       } else if (label != a.ignore && blockIdx.x == 0) {
@@ -870,7 +885,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
 #pragma unroll
           for (int k = 0; k < 32; ++k) {
             const int4 x = s_table[c0 + k];
-            const float pr = (ex2(fmaf(z[k], kLog2e, -__int_as_float(x.y))) - (x.x == v ? 1.f : 0.f)) * __int_as_float(x.z);
+            const float pr = (ex2((z[k] - __int_as_float(x.y)) * kLog2e) - (x.x == v ? 1.f : 0.f)) * __int_as_float(x.z);
             if (live) dst[(size_t)k * a.Vc] = x.w ? (uint16_t)pack_bf(pr, 0.f) : (uint16_t)0;
           }
         }
@@ -1045,7 +1060,7 @@ bool encode_maps(const HeadLossArgs& a, bool backward, Maps* m) {
     ok = ok && tma_matrix(&m->dh_out, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, a.dh, a.d, (int64_t)a.split * a.Rp, 32);
   return ok && tma_matrix(&m->rows_n, t, 2, a.packed, a.d, a.Rp, 64) && tma_matrix(&m->weight_n, t, 2, a.weight, a.d, a.V, 64) &&
          tma_matrix(&m->dz_k, t, 2, a.dz, a.Vc, a.Rp, 128) && tma_matrix(&m->dz_m, t, 2, a.dz, a.Vc, a.Rp, 64) &&
-         tma_matrix(&m->dz_out, t, 2, a.dz, a.Vc, a.Rp, 32);
+         tma_matrix(&m->dz_out, t, 2, a.dz, a.Vc, a.Rp, 32, 0, 64);
 }
 
 // `most`: tiles at most; one pair of CTAs for each two SMs runs through them

@@ -103,19 +103,19 @@ inline TmaEncodeFn tma_encode_fn() {
   }
   return fn;
 }
-// a row-major [rows][cols] matrix (rows `pitch` elements apart, cols if 0) read in
-// boxes of 128 bytes by box_rows rows with the 128-byte swizzle; what lies outside
-// reads as zeros
+// a row-major [rows][cols] matrix (rows `pitch` elements apart, cols if 0) read or
+// written in boxes of box_bytes (128 or 64) by box_rows rows with the swizzle of that
+// many bytes; what lies outside reads as zeros
 inline bool tma_matrix(CUtensorMap* m, CUtensorMapDataType type, int bytes, const void* base, int64_t cols,
-                       int64_t rows, int box_rows, int64_t pitch = 0) {
+                       int64_t rows, int box_rows, int64_t pitch = 0, int box_bytes = 128) {
   TmaEncodeFn fn = tma_encode_fn();
   if (!fn) return false;
   const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
   const cuuint64_t strides[1] = {(cuuint64_t)(pitch ? pitch : cols) * bytes};
-  const cuuint32_t box[2] = {(cuuint32_t)(128 / bytes), (cuuint32_t)box_rows};
+  const cuuint32_t box[2] = {(cuuint32_t)(box_bytes / bytes), (cuuint32_t)box_rows};
   const cuuint32_t estr[2] = {1, 1};
   return fn(m, type, 2, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+            box_bytes == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
