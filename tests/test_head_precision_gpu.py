@@ -74,6 +74,23 @@ CASES = [(R, d) for R in (24, 160) for d in (1040, 2048, 8192, 16384)]
 
 
 @pytest.mark.parametrize("R,d", CASES)
+def test_sums_over_k_are_cut(cmsd, R, d):
+    V = 192
+    h, w, best = _sure_rows(R, d, V, 20.0, 28.0, 17)
+    y = ((best + 1 + torch.arange(R, device="cuda")) % V).int()        # (labels of any entry)
+    o = cmsd.lmhead_loss(h, w, y)
+    z, e = _logits(h, w)
+    lse = torch.logsumexp(z, 1)
+    p = torch.exp(z - lse[:, None])
+    tol = (p * e).sum(1) * 1.001 + _eta(lse, V)
+    err = (o["lse"].double() - lse).abs()
+    assert err.le(tol).all(), (err / tol).max()
+    zy, ey = (t.gather(1, y.long()[:, None])[:, 0] for t in (z, e))
+    err = (o["loss"].double() - (lse - zy)).abs()
+    assert err.le(tol + ey).all(), (err / (tol + ey)).max()
+
+
+@pytest.mark.parametrize("R,d", CASES)
 def test_gradient_of_sure_rows(cmsd, R, d):
     """Rows whose label has nearly all of the probability: P there is p - 1, a difference of nearly equal
     numbers, and the gradients are those of the exact softmax."""
@@ -98,3 +115,27 @@ def test_gradient_of_sure_rows(cmsd, R, d):
         tol = tol + B16 * (want.abs() + tol)
         err = (o[name].double() - want).abs()
         assert err.le(tol).all(), (name, (err / tol).max())
+
+
+@pytest.mark.parametrize("R,d,V", [(97, 72, 39001), (32, 64, 20000), (5, 64, 32001), (300, 72, 39001), (130, 64, 20015)])
+def test_every_entry_of_the_last_tile_counts(cmsd, R, d, V):
+    """The entries behind the last multiple of 256 share half of the probability, and none of them is a label."""
+    g = torch.Generator(device="cuda").manual_seed(V + R)
+    n = V % 256
+    w = torch.randn(V, d, generator=g, device="cuda") / math.sqrt(d)
+    w[:, 0] = 0.0
+    w[V - n:, 0] = math.log((V - n) / n) / 8.0
+    w = w.bfloat16()
+    h = torch.randn(R, d, generator=g, device="cuda")
+    h[:, 0] = 8.0
+    h = h.bfloat16()
+    y = torch.randint(0, V - n, (R,), generator=g, device="cuda").int()
+    z, e = _logits(h, w)
+    lse = torch.logsumexp(z, 1)
+    p = torch.exp(z - lse[:, None])
+    share = p[:, V - n:]
+    tol = (p * e).sum(1) * 1.001 + _eta(lse, V)
+    assert share.sum(1).min() > 0.01
+    assert (tol < share.amin(1) * 0.9).float().mean() > 0.9            # (an entry left out shows in nine rows of ten)
+    err = (cmsd.lmhead_loss(h, w, y)["lse"].double() - lse).abs()
+    assert err.le(tol).all(), (err / tol).max()
