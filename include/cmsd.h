@@ -227,6 +227,7 @@ int cmsd_lmhead_confidence(const void* hidden, const void* weight, int R, int d,
  *     current device.  It needs no initialisation but for the error word, which
  *     cmsd_workspace_init zeroes and cmsd_workspace_errors reads (bit 0 as
  *     above; bit 2: a wait inside a kernel gave up, the results are void).
+ *     The device's own word (cmsd_lmhead_errors) gets the same bits.
  * Outputs and workspace share no bytes with each other or with an input
  * (CMSD_EINVAL), here and in the three entry points below.
  * Products are of exact bf16 values, accumulated in fp32 in an order that does
@@ -286,6 +287,15 @@ size_t cmsd_lmhead_i8_workspace_bytes(int R, int d, int V);
 int cmsd_lmhead_i8(const int8_t* hidden_q, const float* hidden_scale, const int8_t* weight_q,
                    const float* weight_scale, int R, int d, int V, void* logits, int dtype, void* ws,
                    size_t ws_bytes, void* stream);
+
+/*
+ * The error bits of all calls of cmsd_lmhead_loss, cmsd_lmhead_loss_backward and
+ * cmsd_lmhead_i8 on the current device since this was last read, whatever their
+ * workspace, for callers that keep none.  Clears them; the workspaces' own words
+ * stay.  Synchronises `stream`: of calls on other streams it shows what they have
+ * found by then.
+ */
+int cmsd_lmhead_errors(void* stream, uint32_t* flags_out);
 
 /*
  * Verification (Sec. III.B(c)) given the confidence of each present position.

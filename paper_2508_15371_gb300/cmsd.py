@@ -87,6 +87,7 @@ _SIGS = {
     "cmsd_quantize_rows": (_c_int, [_vp, _c_int, _c_int, _c_int, _vp, _vp, _vp]),
     "cmsd_lmhead_i8_workspace_bytes": (_c_sz, [_c_int, _c_int, _c_int]),
     "cmsd_lmhead_i8": (_c_int, [_vp, _vp, _vp, _vp, _c_int, _c_int, _c_int, _vp, _c_int, _vp, _c_sz, _vp]),
+    "cmsd_lmhead_errors": (_c_int, [_vp, ctypes.POINTER(ctypes.c_uint32)]),
     "cmsd_philox_u32": (_c_u32, [_c_u64, _c_u32, _c_u32, _c_u32, _c_u32, _c_int]),
     "cmsd_philox_fill": (_c_int, [_c_u64, _c_u32, _c_u32, _c_u32, _c_u32, _vp, _c_sz, _vp]),
     "cmsd_profile_start": (_c_int, [_c_int]),
@@ -388,11 +389,23 @@ def lmhead_i8_workspace(R, d, V):
     return _head_workspace("cmsd_lmhead_i8_workspace_bytes", R, d, V)
 
 
+def lmhead_errors():
+    """The error bits of the calls of lmhead_loss, lmhead_loss_backward and lmhead_i8 on the current device
+    since they were last read here, whether or not the caller keeps their workspace (bit 0: a label that is
+    neither in the vocabulary nor ignore_index; bit 2: a wait gave up, the results are void).  Clears them and
+    waits for the current stream."""
+    f = ctypes.c_uint32(0)
+    _torch()
+    _check(lib().cmsd_lmhead_errors(_stream(), ctypes.byref(f)), "cmsd_lmhead_errors")
+    return int(f.value)
+
+
 def lmhead_loss(hidden, weight, labels, ignore_index=-100, out=None, ws=None):
     """Softmax cross entropy of the head's logits hidden @ weight.T, which are not kept.
 
     hidden: bf16 [R, d], weight: bf16 [V, d], labels: int32 [R].  Returns dict
-    loss and lse ([R], float32; 0 in rows whose label is ignore_index)."""
+    loss and lse ([R], float32; 0 in rows whose label is ignore_index).  Without ws a workspace is made for the
+    call, here and in the calls below; what went wrong is read with lmhead_errors."""
     torch = _torch()
     R, d, V = _head_sizes(hidden, weight)
     ignore_index = _ignored(ignore_index)

@@ -891,6 +891,16 @@ int cmsd_lmhead_i8(const int8_t* hidden_q, const float* hidden_scale, const int8
   return e == cudaSuccess ? CMSD_OK : cuda_fail(e);
 }
 
+int cmsd_lmhead_errors(void* stream, uint32_t* flags_out) {
+  if (!flags_out) return CMSD_EINVAL;
+  unsigned a = 0, b = 0;
+  cudaError_t e = take_head_loss_errors(&a, (cudaStream_t)stream);
+  if (e == cudaSuccess) e = take_head_i8_errors(&b, (cudaStream_t)stream);
+  if (e != cudaSuccess) return cuda_fail(e);
+  *flags_out = a | b;
+  return CMSD_OK;
+}
+
 size_t cmsd_workspace_bytes(int B, int K, int V) {
   if (B < 0 || K < 0 || V < 2) return 0;
   int wmax = 0;

@@ -42,6 +42,7 @@ struct HeadLossArgs {
 int head_split(int Rp, int d, int Vc);
 cudaError_t launch_head_loss(const HeadLossArgs& a, cudaStream_t s);
 cudaError_t launch_head_loss_backward(const HeadLossArgs& a, cudaStream_t s);
+cudaError_t take_head_loss_errors(unsigned* flags, cudaStream_t s);
 
 // 8-bit rows and the product of the head in 8-bit integers (cmsd_head_i8.cu).
 struct HeadI8Args {
@@ -57,5 +58,6 @@ struct HeadI8Args {
 };
 cudaError_t launch_quantize_rows(const void* x, int dtype, int R, int d, int8_t* q, float* scale, cudaStream_t s);
 cudaError_t launch_head_i8(const HeadI8Args& a, cudaStream_t s);
+cudaError_t take_head_i8_errors(unsigned* flags, cudaStream_t s);
 
 }  // namespace cmsd

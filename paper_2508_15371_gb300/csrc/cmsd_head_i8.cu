@@ -697,7 +697,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kI8Threads, 1)
     }
   }
   if (!ok) {
-    atomicOr(a.err, 4u);
+    report(a.err, 4u);
     let_settle();
   }
   __syncwarp();
@@ -745,6 +745,8 @@ cudaError_t launch_quantize_rows(const void* x, int dtype, int R, int d, int8_t*
   return dtype == 0 ? launch_quantize((const float*)x, R, d, q, scale, s)
                     : launch_quantize((const __nv_bfloat16*)x, R, d, q, scale, s);
 }
+
+cudaError_t take_head_i8_errors(unsigned* flags, cudaStream_t s) { return take_errors(flags, s); }
 
 cudaError_t launch_head_i8(const HeadI8Args& a, cudaStream_t s) {
   int dev = 0, sms = 0;

@@ -79,7 +79,7 @@ __global__ void __launch_bounds__(kPackThreads) head_pack_kernel(const HeadLossA
           a.pgrad[p] = a.grad[mine];
         }
       } else if (label != a.ignore) {
-        atomicOr(a.err, 1u);
+        report(a.err, 1u);
       }
     }
     const int row = r + warp;
@@ -623,7 +623,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(64 + 32 * epi_warps(
     }
   }
   if (!ok) {
-    atomicOr(a.err, 4u);
+    report(a.err, 4u);
     let_settle();
   }
   __syncwarp();
@@ -809,7 +809,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
           x.z = __float_as_int(a.grad[c]);
         }
       } else if (label != a.ignore && blockIdx.x == 0) {
-        atomicOr(a.err, 1u);
+        report(a.err, 1u);
       }
       s_table[c] = x;
     }
@@ -909,7 +909,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
     }
   }
   if (!ok) {
-    atomicOr(a.err, 4u);
+    report(a.err, 4u);
     let_settle();
   }
   __syncwarp();
@@ -1134,6 +1134,8 @@ int head_split(int Rp, int d, int Vc) {
   }
   return best;
 }
+
+cudaError_t take_head_loss_errors(unsigned* flags, cudaStream_t s) { return take_errors(flags, s); }
 
 cudaError_t launch_head_loss(const HeadLossArgs& a, cudaStream_t s) {
   if (a.R <= kFewRows) {

@@ -1,5 +1,6 @@
 // Primitives of the head operators' kernels on the 5th-generation tensor
-// cores: pairs of CTAs (a cluster of two), tensor memory, TMA boxes.
+// cores: pairs of CTAs (a cluster of two), tensor memory, TMA boxes; their error
+// words.
 #pragma once
 #include <cuda.h>
 
@@ -200,6 +201,28 @@ __device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&r)[32
       : "memory");
 }
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+// ---- errors ---------------------------------------------------------------------------
+// What a kernel finds goes to its workspace's word and to one of the device (for
+// each translation unit), which outlives a workspace that nobody kept.
+namespace {
+__device__ unsigned g_errors, g_taken;
+__device__ __forceinline__ void report(unsigned* word, unsigned bits) {
+  atomicOr(word, bits);
+  atomicOr(&g_errors, bits);
+}
+__global__ void take_errors_kernel() { g_taken = atomicExch(&g_errors, 0u); }
+// the current device's word, which is cleared; s is waited for
+cudaError_t take_errors(unsigned* flags, cudaStream_t s) {
+  static std::mutex mu;                              // (one reader of g_taken at a time)
+  std::lock_guard<std::mutex> lk(mu);
+  take_errors_kernel<<<1, 1, 0, s>>>();
+  cudaError_t e = cudaGetLastError();
+  if (e == cudaSuccess) e = cudaMemcpyFromSymbolAsync(flags, g_taken, sizeof(unsigned), 0, cudaMemcpyDeviceToHost, s);
+  const cudaError_t f = cudaStreamSynchronize(s);    // (whatever e is: flags is the caller's)
+  return e != cudaSuccess ? e : f;
+}
+}  // namespace
 
 // ---- bounded waits ------------------------------------------------------------------
 // Waits for the phase of this parity of a barrier of this CTA; false after about

@@ -188,3 +188,7 @@ def test_ignore_index_past_32_bits(cmsd, ignore):
         cmsd.lmhead_loss(h, w, y, ignore_index=ignore)
     with pytest.raises(cmsd.CmsdError, match="ignore_index"):
         cmsd.lmhead_loss_backward(h, w, y, f, f, ignore_index=ignore)
+
+
+def test_errors_need_a_place(cmsd):
+    assert cmsd.lib().cmsd_lmhead_errors(None, None) == cmsd.EINVAL
