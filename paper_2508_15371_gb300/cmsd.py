@@ -403,10 +403,14 @@ def lmhead_errors():
 def lmhead_loss(hidden, weight, labels, ignore_index=-100, out=None, ws=None):
     """Softmax cross entropy of the head's logits hidden @ weight.T, which are not kept.
 
-    hidden: bf16 [R, d], weight: bf16 [V, d], labels: int32 [R].  Returns dict
+    hidden: bf16 [R, d], weight: bf16 [V, d], labels: int32 [R].  Nothing is recorded for autograd: tensors that
+    require gradients are refused while it records.  Returns dict
     loss and lse ([R], float32; 0 in rows whose label is ignore_index).  Without ws a workspace is made for the
     call, here and in the calls below; what went wrong is read with lmhead_errors."""
     torch = _torch()
+    if (hidden.requires_grad or weight.requires_grad) and torch.is_grad_enabled():
+        raise CmsdError("lmhead_loss records nothing for autograd: call it under torch.no_grad() (or from an "
+                        "autograd.Function) and take the gradients from lmhead_loss_backward")
     R, d, V = _head_sizes(hidden, weight)
     ignore_index = _ignored(ignore_index)
     f32, bf16 = torch.float32, torch.bfloat16

@@ -192,3 +192,51 @@ def test_ignore_index_past_32_bits(cmsd, ignore):
 
 def test_errors_need_a_place(cmsd):
     assert cmsd.lib().cmsd_lmhead_errors(None, None) == cmsd.EINVAL
+
+
+@pytest.mark.parametrize("who", ["hidden", "weight"])
+def test_loss_is_not_detached_in_silence(cmsd, who):
+    """Where autograd records, a loss that it could not follow is refused; else the next check is reached."""
+    torch = pytest.importorskip("torch")
+    t = {"hidden": torch.zeros(4, 64, dtype=torch.bfloat16), "weight": torch.zeros(100, 64, dtype=torch.bfloat16)}
+    t[who].requires_grad_()
+    y = torch.zeros(4, dtype=torch.int32)
+    with pytest.raises(cmsd.CmsdError, match="autograd"):
+        cmsd.lmhead_loss(t["hidden"], t["weight"], y)
+    with torch.no_grad(), pytest.raises(cmsd.CmsdError, match="CUDA"):
+        cmsd.lmhead_loss(t["hidden"], t["weight"], y)
+
+
+def test_loss_and_gradients_make_an_autograd_function(cmsd, monkeypatch):
+    """Both calls from inside an autograd.Function, on leaves that require gradients; the library is stood in for."""
+    torch = pytest.importorskip("torch")
+    monkeypatch.setattr(cmsd, "_need", lambda cur, specs: None)
+    monkeypatch.setattr(cmsd, "_stream_of", lambda cur: 0)
+    seen = []
+
+    class Lib:
+        def cmsd_lmhead_loss(self, *a):
+            seen.append("loss")
+            return cmsd.OK
+
+        def cmsd_lmhead_loss_backward(self, *a):
+            seen.append("backward")
+            return cmsd.OK
+    monkeypatch.setattr(cmsd, "lib", lambda: Lib())
+    ws = torch.zeros(64, dtype=torch.uint8)
+
+    class Loss(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, h, w, y):
+            o = cmsd.lmhead_loss(h, w, y, ws=ws)
+            ctx.save_for_backward(h, w, y, o["lse"])
+            return o["loss"]
+
+        @staticmethod
+        def backward(ctx, grad):
+            o = cmsd.lmhead_loss_backward(*ctx.saved_tensors, grad.contiguous(), ws=ws)
+            return o["d_hidden"].zero_(), o["d_weight"].zero_(), None
+    h = torch.zeros(4, 64, dtype=torch.bfloat16, requires_grad=True)
+    w = torch.zeros(100, 64, dtype=torch.bfloat16, requires_grad=True)
+    Loss.apply(h, w, torch.zeros(4, dtype=torch.int32)).sum().backward()
+    assert seen == ["loss", "backward"] and h.grad.shape == h.shape and w.grad.shape == w.shape
