@@ -297,6 +297,12 @@ int cmsd_lmhead_i8(const int8_t* hidden_q, const float* hidden_scale, const int8
  */
 int cmsd_lmhead_errors(void* stream, uint32_t* flags_out);
 
+/* Test support, no counterpart in the paper: one wait of the kind that the head
+ * operators' kernels make, limited to 2^24 cycles, at a barrier that has arrivals
+ * (arrive != 0) or never gets one; sets bit 2 of ws's error word and of the
+ * device's where it gave up. */
+int cmsd_test_head_wait(int arrive, void* ws, size_t ws_bytes, void* stream);
+
 /*
  * Verification (Sec. III.B(c)) given the confidence of each present position.
  * draft_tokens: int32 [B][K] device, the drafted token of each position.

@@ -891,6 +891,13 @@ int cmsd_lmhead_i8(const int8_t* hidden_q, const float* hidden_scale, const int8
   return e == cudaSuccess ? CMSD_OK : cuda_fail(e);
 }
 
+int cmsd_test_head_wait(int arrive, void* ws, size_t ws_bytes, void* stream) {
+  if (!ws || ws_bytes < sizeof(unsigned)) return CMSD_ENOWS;
+  if (!aligned4(ws)) return CMSD_EALIGN;
+  const cudaError_t e = launch_test_wait((unsigned*)ws, arrive, (cudaStream_t)stream);
+  return e == cudaSuccess ? CMSD_OK : cuda_fail(e);
+}
+
 int cmsd_lmhead_errors(void* stream, uint32_t* flags_out) {
   if (!flags_out) return CMSD_EINVAL;
   unsigned a = 0, b = 0;

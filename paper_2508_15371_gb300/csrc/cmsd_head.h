@@ -43,6 +43,7 @@ int head_split(int Rp, int d, int Vc);
 cudaError_t launch_head_loss(const HeadLossArgs& a, cudaStream_t s);
 cudaError_t launch_head_loss_backward(const HeadLossArgs& a, cudaStream_t s);
 cudaError_t take_head_loss_errors(unsigned* flags, cudaStream_t s);
+cudaError_t launch_test_wait(unsigned* err, int arrive, cudaStream_t s);
 
 // 8-bit rows and the product of the head in 8-bit integers (cmsd_head_i8.cu).
 struct HeadI8Args {

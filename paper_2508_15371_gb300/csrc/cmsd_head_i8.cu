@@ -559,7 +559,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kI8Threads, 1)
       do {
         if (ok) ok = bar_wait<true>(aempty + 8 * b, aphase);
         if (ok) ok = bar_wait<false>(wfull + 8 * s, phase);
-        __syncwarp();
+        ok = __all_sync(kFull, ok);
+        if (!ok) break;
         const uint32_t src = base + s * kI8WStage + wrow;
         uint32_t o[32];
 #pragma unroll
@@ -591,6 +592,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kI8Threads, 1)
         }
         ++g;
       } while (--left > 0);
+      if (!ok) break;
       if (g == ks && span.first(a, p, pair, pairs)) left = ks * (parts - 1);
       if (left == 0 && ++i < mine) left = span.next(a, p, pair + i * pairs, pairs) ? ks * parts : ks;
     }
@@ -634,7 +636,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kI8Threads, 1)
       };
       auto sum_wait = [&]() {
         if (ok) ok = bar_wait<true>(dfull + 8 * (c & 1), (uint32_t)((c / 2) & 1));
-        __syncwarp();
+        ok = __all_sync(kFull, ok);
         tmem_fence_after();
       };
       auto sum_done = [&]() {
@@ -645,6 +647,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kI8Threads, 1)
       };
       if (!apart) {
         sum_wait();
+        if (!ok) break;
         const uint32_t src = tbase + quarter + (c & 1) * S::kSum + 16 * set;
 #pragma unroll
         for (int u = 0; u < kMine; ++u) {
@@ -669,6 +672,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kI8Threads, 1)
 #pragma unroll 1
           for (int k = 0; k < sums; ++k) {
             sum_wait();
+            if (!ok) break;
             const uint32_t src = tbase + quarter + (c & 1) * S::kSum + 16 * set;
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
@@ -685,7 +689,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kI8Threads, 1)
 #pragma unroll
           for (int u = 0; u < 2; ++u) {
             const int n = j * kI8Part + 16 * (2 * u + set);
-            if (2 * j + u < kMine && n < p.cols) {
+            if (ok && 2 * j + u < kMine && n < p.cols) {
               float y[16];
 #pragma unroll
               for (int m = 0; m < 16; ++m) y[m] = (float)acc[u][m];

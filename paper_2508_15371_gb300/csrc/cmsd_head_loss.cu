@@ -446,7 +446,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(64 + 32 * epi_warps(
         for (int kb = 0; kb < t.kb; kb += kSumBlocks, ++sums) {
           const int b = sums & 1;
           if (ok) ok = bar_wait<true>(tfull + 8 * b, (uint32_t)((sums / 2) & 1));
-          __syncwarp();
+          ok = __all_sync(kFull, ok);
+          if (!ok) break;
           tmem_fence_after();
           const uint32_t src = quarter + b * 256;
           if (kb == 0) {                             // (a loop of its own: with one for both the sums spilled)
@@ -472,6 +473,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(64 + 32 * epi_warps(
           if (lane == 0) mbar_arrive_cluster(tempty0 + 8 * b);   // this warp's columns have been read
         }
         if (OP == kOpDz) {
+          if (!ok) break;
           const float lse = live ? a.plse[row] : 0.f, gr = live ? a.pgrad[row] : 0.f;
 #pragma unroll
           for (int c = 0; c < 64; c += 32) {
@@ -495,7 +497,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(64 + 32 * epi_warps(
           }
           continue;
         }
-        if (lab >= col && lab < col + 64) {
+        // (after a wait that gave up: on to the barrier, where another warp waits, and nothing is written)
+        if (ok && lab >= col && lab < col + 64) {
           float zl = z[0];
 #pragma unroll
           for (int k = 1; k < 64; ++k) zl = lab == col + k ? z[k] : zl;
@@ -519,7 +522,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(64 + 32 * epi_warps(
         float2* mine = s_half + ((i & 1) * 2 + (group >> 1)) * 128 + q * 32 + lane;
         if (group & 1) *mine = make_float2(mx, sum);
         asm volatile("bar.sync %0, 64;" ::"r"(1 + (group >> 1) * 4 + q) : "memory");
-        if (!(group & 1) && live && col < vlen) {
+        if (ok && !(group & 1) && live && col < vlen) {
           const float2 x = *mine;
           fold(mx, sum, x.x, x.y);
           a.part[(size_t)(col / kHeadPart) * a.Rp + row] = make_float2(mx, sum);
@@ -556,7 +559,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(64 + 32 * epi_warps(
         const Tile t = tile_of<OP>(a, w, i);
         const int b = i & 1;
         if (ok) ok = bar_wait<true>(tfull + 8 * b, (uint32_t)((i / 2) & 1));
-        __syncwarp();
+        ok = __all_sync(kFull, ok);
+        if (!ok) break;
         tmem_fence_after();
         const int row0 = t.m * kPairTile + (int)rank * 128 + q * 32;
         const int col = t.n * kPairTile + half * 128;
@@ -834,7 +838,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
       for (int k0 = 0; k0 < kb; k0 += kSumBlocks, ++sums) {
         const int b = sums & 1;
         if (ok) ok = bar_wait<true>(tfull + 8 * b, (uint32_t)((sums / 2) & 1));
-        __syncwarp();
+        ok = __all_sync(kFull, ok);
+        if (!ok) break;
         tmem_fence_after();
         const uint32_t src = tbase + ((uint32_t)(q * 32) << 16) + (uint32_t)(b * 128);
 #pragma unroll
@@ -851,6 +856,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
         __syncwarp();
         if (lane == 0) mbar_arrive_cluster(tempty0 + 8 * b);       // this warp's columns have been read
       }
+      if (!ok) break;
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
         const int c0 = 32 * (2 * u + half);
@@ -1133,6 +1139,25 @@ int head_split(int Rp, int d, int Vc) {
     }
   }
   return best;
+}
+
+// one wait at a barrier that has its one arrival, or never gets it
+__global__ void test_wait_kernel(unsigned* err, int arrive, long long limit) {
+  __shared__ __align__(8) unsigned long long s_bar;
+  const uint32_t bar = smem_addr(&s_bar);
+  if (threadIdx.x == 0) {
+    mbar_init(bar, 1);
+    if (arrive) mbar_arrive_local(bar);
+  }
+  __syncwarp();
+  if (!bar_wait<false>(bar, 0, limit)) {
+    report(err, 4u);
+    let_settle();
+  }
+}
+cudaError_t launch_test_wait(unsigned* err, int arrive, cudaStream_t s) {
+  test_wait_kernel<<<1, 32, 0, s>>>(err, arrive, 1ll << 24);
+  return cudaGetLastError();
 }
 
 cudaError_t take_head_loss_errors(unsigned* flags, cudaStream_t s) { return take_errors(flags, s); }

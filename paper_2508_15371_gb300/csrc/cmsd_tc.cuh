@@ -225,8 +225,8 @@ cudaError_t take_errors(unsigned* flags, cudaStream_t s) {
 }  // namespace
 
 // ---- bounded waits ------------------------------------------------------------------
-// Waits for the phase of this parity of a barrier of this CTA; false after about
-// a second (2^31 cycles; any wait here is for less than a launch takes).
+// Waits for the phase of this parity of a barrier of this CTA; false after `limit`
+// cycles (about a second; any wait here is for less than a launch takes).
 // kCluster: acquires what other CTAs' threads released to the cluster.
 template <bool kCluster>
 __device__ __forceinline__ bool mbar_poll(uint32_t bar, uint32_t parity) {
@@ -247,18 +247,20 @@ __device__ __forceinline__ bool mbar_poll(uint32_t bar, uint32_t parity) {
   return ok != 0;
 }
 template <bool kCluster>
-__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity) {
+__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, long long limit = 1ll << 31) {
   if (mbar_poll<kCluster>(bar, parity)) return true;
   const long long t0 = clock64();
   do {
 #pragma unroll 1
     for (int k = 0; k < 16; ++k)
       if (mbar_poll<kCluster>(bar, parity)) return true;
-  } while (clock64() - t0 < (1ll << 31));
+  } while (clock64() - t0 < limit);
   return false;
 }
-// After a wait gave up nothing more is issued; copies and MMAs in flight (of a few
-// microseconds) end within this millisecond, before their memory goes.
+// After a wait gave up its warp issues, stores and hands over nothing more (the
+// warps that wait for it give up in turn), and what is in flight gets this
+// millisecond before its memory goes: copies and MMAs of a few microseconds, whose
+// end is not waited for, as it is what did not come.
 __device__ __forceinline__ void let_settle() {
   const long long t0 = clock64();
   while (clock64() - t0 < (1ll << 21)) __nanosleep(1000);

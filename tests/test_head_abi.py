@@ -240,3 +240,9 @@ def test_loss_and_gradients_make_an_autograd_function(cmsd, monkeypatch):
     w = torch.zeros(100, 64, dtype=torch.bfloat16, requires_grad=True)
     Loss.apply(h, w, torch.zeros(4, dtype=torch.int32)).sum().backward()
     assert seen == ["loss", "backward"] and h.grad.shape == h.shape and w.grad.shape == w.shape
+
+
+def test_wait_test_needs_a_workspace(cmsd):
+    assert cmsd.lib().cmsd_test_head_wait(1, None, 256, None) == cmsd.ENOWS
+    assert cmsd.lib().cmsd_test_head_wait(1, A, 3, None) == cmsd.ENOWS
+    assert cmsd.lib().cmsd_test_head_wait(1, A + 2, 256, None) == cmsd.EALIGN

@@ -72,3 +72,16 @@ def test_the_8_bit_product_reports_nothing(cmsd):
     cmsd.lmhead_errors()
     cmsd.lmhead_i8(q, s, q, s)
     assert cmsd.lmhead_errors() == 0
+
+
+def test_a_wait_that_gives_up_is_reported(cmsd):
+    """A barrier that nobody arrives at: the kernel ends by itself, both words have bit 2, the next call is right."""
+    h, w, y = _inputs(40)
+    want = cmsd.lmhead_loss(h, w, y)
+    ws = cmsd.lmhead_loss_workspace(40, 64, 500)
+    cmsd.lmhead_errors()
+    for arrive, bits in ((1, 0), (0, 4)):
+        assert cmsd.lib().cmsd_test_head_wait(arrive, ws.data_ptr(), ws.numel(), cmsd._stream()) == cmsd.OK
+        assert cmsd.workspace_errors(ws) == bits and cmsd.lmhead_errors() == bits
+    got = cmsd.lmhead_loss(h, w, y, ws=ws)
+    assert torch.equal(got["loss"], want["loss"]) and cmsd.workspace_errors(ws) == 0
