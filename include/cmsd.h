@@ -246,10 +246,10 @@ int cmsd_lmhead_loss(const void* hidden, const void* weight, const int32_t* labe
  * CMSD_EINVAL).  Sizes, inputs, labels and the error word as for
  * cmsd_lmhead_loss; lse: float [R], that call's output; grad_loss: float [R]
  * device (the mean over n kept rows has 1 / n; entries of ignored rows are not
- * used).  P is formed again from h and W in pieces of the vocabulary of at most
- * 128 MB (and at least 256 entries), rounded to bf16 for the two products, which
- * are accumulated in fp32 and rounded to bf16 once.  Both outputs are written
- * whole, not added to.
+ * used).  P is formed again from h and W, by the sums that lse was formed by, in
+ * pieces of the vocabulary of at most 128 MB (and at least 256 entries), and
+ * rounded to bf16 for the two products, which are accumulated in fp32 and rounded
+ * to bf16 once.  Both outputs are written whole, not added to.
  */
 size_t cmsd_lmhead_loss_backward_workspace_bytes(int R, int d, int V);
 int cmsd_lmhead_loss_backward(const void* hidden, const void* weight, const int32_t* labels, const float* lse,

@@ -2,7 +2,7 @@
 // cmsd_lmhead_loss_backward).
 //
 // Forward: the logits of a tile of rows and vocabulary entries are formed in
-// registers and reduced at once to each row's maximum and sum of exponentials
+// tensor memory and reduced at once to each row's maximum and sum of exponentials
 // over the tile's entries; a second kernel merges a row's tiles.  Backward, a
 // piece of the vocabulary at a time: the logits again, from them the piece of
 // P (bf16), then P W, summed over the pieces in fp32, and P^T h.
@@ -116,9 +116,10 @@ __device__ __forceinline__ void fold(float& m, float& s, float m2, float s2) {
 // 64.  A pair reads (256 + 256) * 2 bytes of its operands per K from L2 for
 // 256 * 256 products; one CTA alone with a 128 x 256 tile would read half as
 // much again per product, and L2 would bound the tensor cores.  (R=4096 d=2048
-// V=128256, 2867 rows kept: loss 855-885 us, 1.70-1.76 PFLOP/s; both gradients
-// 2680-2800 us, 1.61-1.69 PFLOP/s.  Counters at R=2048 d=2048 V=65536: loss 80 % of
-// the tensor pipe, 15.6 TB/s from L2; gradients 80 %; P 75 %.)
+// V=128256, 2867 rows kept, a few calls in a graph: loss 855-885 us, 1.70-1.76
+// PFLOP/s; both gradients 2680-2800 us, 1.61-1.69.  Back to back, under the power
+// limit: 964-998 us, 1.51-1.56; 2970-3097 us, 1.46-1.52.  Counters at R=2048 d=2048
+// V=65536: loss 80 % of the tensor pipe, 15 TB/s from L2; gradients 80 %; P 72 %.)
 //   logits   A = packed rows, B = weight, K = d; both rows of 128 bytes along K
 //   d_hidden A = P, B = weight (its rows run along N), K = the piece's entries
 //   d_weight A = P (its rows run along M), B = packed rows (along N), K = rows
@@ -151,9 +152,9 @@ constexpr int kTmemCols = 512;
 // The tensor cores round their sums towards zero at each step of 16 of K: at
 // d=2048 logits came out short by 1.5e-6 of their size, all in the same direction,
 // and losses wrong by 1.1e-6.  So the logits' sums are cut after kSumBlocks blocks of
-// 64 and added up in registers: each part is shorter and smaller (losses 5.5e-7;
-// parts of 8 blocks 2.6e-7, but 914 against 880 us at R=4096 d=2048
-// V=128256, 857 uncut).  P is formed from sums cut alike: its logits are then those
+// 64 and added up in registers: each part is shorter and smaller (losses 4.5e-7 to
+// 5.9e-7 for d from 1024 to 2^20; parts of 8 blocks 2.6e-7, but 914 against 880 us at
+// R=4096 d=2048 V=128256, 857 uncut).  P is formed from sums cut alike: its logits are then those
 // of the lse that it is given, to the bit, and p - 1 of a label with nearly all of
 // the probability is right although both are off by more than it is.
 constexpr int kSumBlocks = 16;
@@ -1125,7 +1126,10 @@ cudaError_t launch_few(bool early, const HeadLossArgs& a, int v0, int vlen, int 
 // pairs of SMs: the least of rounds / parts, each part charged for its sums' way
 // through memory (8 bytes a sum and piece at 5 TB/s, against 2 Vc operations at
 // 1.7 PFLOP/s).  R=4096 d=2048 V=128256, both gradients: one part 2.96 ms, four
-// 3.07.  A part has at least four blocks of 64.
+// 3.07.  A part has at least four blocks of 64.  The 76 pairs are GB300's 152 SMs and
+// not asked of the device: the parts decide the workspace's size, which depends on the
+// call's sizes alone.  (The launch counts the device's SMs; with fewer of them the
+// parts are a worse choice, and right.)
 int head_split(int Rp, int d, int Vc) {
   const int64_t t = (int64_t)(Rp / kPairTile) * ((d + kPairTile - 1) / kPairTile);
   const int most = Vc / 256 < 32 ? Vc / 256 : 32;
