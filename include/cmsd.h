@@ -297,6 +297,99 @@ int cmsd_lmhead_i8(const int8_t* hidden_q, const float* hidden_scale, const int8
  */
 int cmsd_lmhead_errors(void* stream, uint32_t* flags_out);
 
+/*
+ * A drafter below its head, for training one and for the hidden states of a
+ * decode step: the token table's rows, layer norm, dropout, and their gradients.
+ * dtype is that of the tensors of entries (CMSD_F32 or CMSD_BF16); sums are
+ * held in fp32, results rounded to their dtype once.  Widths d are any number
+ * from 1 to 65536 (rows of a multiple of 16 bytes are the fast ones), rows
+ * R <= 2^28; tensors of entries and workspaces are 16-byte aligned.  Outputs and workspaces share no bytes with each other or with an
+ * input (CMSD_EINVAL).  Equal calls give equal results.
+ *
+ * cmsd_embedding: x_r = scale table_token(r)
+ *   tokens: int32 [R] device.  A row whose token is ignore_index is padding: its
+ *     entries are 0, and it has no part in the gradient.  ignore_index may be any
+ *     number, an entry of the vocabulary too.  Another token outside [0, V) is
+ *     treated as padding and sets bit 0 of the device's error word
+ *     (cmsd_embedding_errors).
+ *   table: dtype [V][d], 1 <= V <= 2^30, V*d below 2^46; x: dtype [R][d]; scale
+ *     finite.
+ *
+ * cmsd_embedding_backward: d_table_v = scale sum of d_x_r over the rows r with token v
+ *   d_x: dtype [R][d]; rows of padding are not read.  d_table: dtype [V][d].
+ *     add == 0: written whole, zeros where a token has no rows.  add != 0: the sum
+ *     is added to what d_table holds (the weight's gradient of a head that shares
+ *     the table, cmsd_lmhead_loss_backward's d_weight), and entries without rows
+ *     are not touched.
+ *   A token's rows are summed in an order that depends on tokens alone.
+ *   ws: cmsd_embedding_backward_workspace_bytes(R, d, V) bytes on the current
+ *     device.  It needs no initialisation but for the error word, which
+ *     cmsd_workspace_init zeroes and cmsd_workspace_errors reads (bit 0 as above).
+ *     The device's own word gets the same bit.
+ *   R == 0: zeros are written, or nothing with add.
+ *
+ * cmsd_embedding_errors: the error bits of all calls of the two on the current
+ * device since this was last read.  Clears them; the workspaces' own words stay.
+ * Synchronises `stream`.
+ */
+int cmsd_embedding(const int32_t* tokens, const void* table, int dtype, int R, int d, int V, int ignore_index,
+                   float scale, void* x, void* stream);
+size_t cmsd_embedding_backward_workspace_bytes(int R, int d, int V);
+int cmsd_embedding_backward(const int32_t* tokens, const void* d_x, int dtype, int R, int d, int V,
+                            int ignore_index, float scale, int add, void* d_table, void* ws, size_t ws_bytes,
+                            void* stream);
+int cmsd_embedding_errors(void* stream, uint32_t* flags_out);
+
+/*
+ * Layer norm of R rows of d entries:
+ *   mean_r = sum_j x_rj / d,  rstd_r = (sum_j (x_rj - mean_r)^2 / d + eps)^(-1/2)
+ *   y_rj = (x_rj - mean_r) rstd_r weight_j + bias_j
+ *   x, y: dtype [R][d]; weight, bias: wdtype (CMSD_F32 or CMSD_BF16) [d], 16-byte
+ *     aligned, or NULL (ones, zeros); 0 < eps, finite; mean, rstd: float [R], or
+ *     NULL where no gradients follow.  |x| < 2^54; a row with an infinity or a NaN
+ *     gives NaN in that row.
+ *
+ * cmsd_layernorm_backward: its gradients, given d_y = dL/dy and what the call above
+ * left.  With h_rj = (x_rj - mean_r) rstd_r and g_rj = d_y_rj weight_j:
+ *   d_x_rj     = rstd_r (g_rj - sum_k g_rk / d - h_rj sum_k g_rk h_rk / d)
+ *   d_weight_j = sum_r d_y_rj h_rj,  d_bias_j = sum_r d_y_rj
+ *   d_x: dtype [R][d]; d_weight, d_bias: wdtype [d].  Each may be NULL and is then
+ *     left out (all NULL is CMSD_EINVAL).  All are written whole.
+ *   The sums over rows are formed in an order that depends on R and d alone.
+ *   ws: cmsd_layernorm_backward_workspace_bytes(R, d) bytes on the current device,
+ *     no initialisation needed.
+ *   R == 0: the parameters' gradients are zero.
+ */
+int cmsd_layernorm(const void* x, const void* weight, const void* bias, int dtype, int wdtype, int R, int d,
+                   float eps, void* y, float* mean, float* rstd, void* stream);
+size_t cmsd_layernorm_backward_workspace_bytes(int R, int d);
+int cmsd_layernorm_backward(const void* x, const void* weight, const float* mean, const float* rstd,
+                            const void* d_y, int dtype, int wdtype, int R, int d, void* d_x, void* d_weight,
+                            void* d_bias, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * Dropout whose mask is made from the entries' places and never stored:
+ *   y_e = residual_e + x_e 2^16 / (2^16 - t)  where k_e >= t, else residual_e
+ *   t = p 2^16 rounded to the nearest whole number (ties to the even one),
+ *   0 <= p <= 1; k_e: sixteen bits of Philox4x32-10 with key (seed lo, seed hi):
+ *   half e & 1 (the low one first) of word (e >> 1) & 3 of counter
+ *   (g lo, g hi, site, it << 2 | 3), g = e >> 3, it = iteration + *step.
+ * A dropped entry of x reaches no result, whatever it holds.
+ *   x, y: dtype [n], 0 <= n < 2^46; residual: dtype [n], or NULL (zeros).
+ *   site: tells the uses of one iteration apart (a layer's number); step: NULL, or
+ *     a uint32 on the device that is added to iteration when the call runs, so that
+ *     a captured call draws another mask at each replay.  Iterations 2^30 apart
+ *     have the same mask.
+ *
+ * cmsd_dropout_backward: d_x_e = d_y_e 2^16 / (2^16 - t) where k_e >= t, else 0: the
+ * gradient, given the p, seed, iteration, site and step of that call (the residual's
+ * gradient is d_y itself).
+ */
+int cmsd_dropout(const void* x, const void* residual, int dtype, int64_t n, double p, uint64_t seed,
+                 uint32_t iteration, uint32_t site, const uint32_t* step, void* y, void* stream);
+int cmsd_dropout_backward(const void* d_y, int dtype, int64_t n, double p, uint64_t seed, uint32_t iteration,
+                          uint32_t site, const uint32_t* step, void* d_x, void* stream);
+
 /* Test support, no counterpart in the paper: one wait of the kind that the head
  * operators' kernels make, limited to 2^24 cycles, at a barrier that has arrivals
  * (arrive != 0) or never gets one; sets bit 2 of ws's error word and of the

@@ -22,7 +22,8 @@ NVCC_FLAGS = ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC", "-I" + IN
 
 LIBS = {
     "libcmsd.so": ["cmsd_stream_bf16.cu", "cmsd_stream_f32.cu", "cmsd_seq_bf16.cu", "cmsd_seq_f32.cu",
-                   "cmsd_api.cu", "cmsd_static.cu", "cmsd_lmhead.cu", "cmsd_head_loss.cu", "cmsd_head_i8.cu"],
+                   "cmsd_api.cu", "cmsd_static.cu", "cmsd_lmhead.cu", "cmsd_head_loss.cu", "cmsd_head_i8.cu",
+                   "cmsd_embed.cu", "cmsd_norm.cu", "cmsd_dropout.cu"],
     "libcmsd_workload.so": ["cmsd_workload.cu"],
 }
 

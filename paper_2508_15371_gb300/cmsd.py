@@ -87,6 +87,19 @@ _SIGS = {
     "cmsd_quantize_rows": (_c_int, [_vp, _c_int, _c_int, _c_int, _vp, _vp, _vp]),
     "cmsd_lmhead_i8_workspace_bytes": (_c_sz, [_c_int, _c_int, _c_int]),
     "cmsd_lmhead_i8": (_c_int, [_vp, _vp, _vp, _vp, _c_int, _c_int, _c_int, _vp, _c_int, _vp, _c_sz, _vp]),
+    "cmsd_embedding": (_c_int, [_vp, _vp, _c_int, _c_int, _c_int, _c_int, _c_int, ctypes.c_float, _vp, _vp]),
+    "cmsd_embedding_backward_workspace_bytes": (_c_sz, [_c_int, _c_int, _c_int]),
+    "cmsd_embedding_backward": (_c_int, [_vp, _vp, _c_int, _c_int, _c_int, _c_int, _c_int, ctypes.c_float, _c_int,
+                                         _vp, _vp, _c_sz, _vp]),
+    "cmsd_embedding_errors": (_c_int, [_vp, ctypes.POINTER(ctypes.c_uint32)]),
+    "cmsd_layernorm": (_c_int, [_vp, _vp, _vp, _c_int, _c_int, _c_int, _c_int, ctypes.c_float, _vp, _vp, _vp, _vp]),
+    "cmsd_layernorm_backward_workspace_bytes": (_c_sz, [_c_int, _c_int]),
+    "cmsd_layernorm_backward": (_c_int, [_vp, _vp, _vp, _vp, _vp, _c_int, _c_int, _c_int, _c_int, _vp, _vp, _vp, _vp,
+                                         _c_sz, _vp]),
+    "cmsd_dropout": (_c_int, [_vp, _vp, _c_int, ctypes.c_int64, ctypes.c_double, _c_u64, _c_u32, _c_u32, _vp, _vp,
+                              _vp]),
+    "cmsd_dropout_backward": (_c_int, [_vp, _c_int, ctypes.c_int64, ctypes.c_double, _c_u64, _c_u32, _c_u32, _vp,
+                                       _vp, _vp]),
     "cmsd_test_head_wait": (_c_int, [_c_int, _vp, _c_sz, _vp]),
     "cmsd_lmhead_errors": (_c_int, [_vp, ctypes.POINTER(ctypes.c_uint32)]),
     "cmsd_philox_u32": (_c_u32, [_c_u64, _c_u32, _c_u32, _c_u32, _c_u32, _c_int]),
@@ -343,7 +356,7 @@ def _too_large(what):
 def _ignored(index):
     index = int(index)
     if not -_INT_MAX - 1 <= index <= _INT_MAX:
-        raise CmsdError("ignore_index must be a 32-bit integer, as the labels are")
+        raise CmsdError("ignore_index must be a 32-bit integer, as labels and tokens are")
     return index
 
 
@@ -500,6 +513,222 @@ def lmhead_i8(hidden_q, hidden_scale, weight_q, weight_scale, dtype=None, out=No
     if rc != OK:
         _check(rc, "cmsd_lmhead_i8")
     return {"logits": logits}
+
+
+def _code(t, name):
+    torch = _torch_mod
+    if t.dtype is torch.bfloat16:
+        return BF16
+    if t.dtype is torch.float32:
+        return F32
+    raise CmsdError(f"{name} must be float32 or bfloat16, got {t.dtype}")
+
+
+def _not_recorded(what, *ts):
+    if _torch_mod.is_grad_enabled():
+        for t in ts:
+            if t is not None and t.requires_grad:
+                raise CmsdError(f"{what} records nothing for autograd: call it under torch.no_grad() (or from an "
+                                f"autograd.Function) and take the gradients from {what}_backward")
+
+
+def _rows(t, name):
+    if t.dim() != 2:
+        raise CmsdError(f"{name} must have two dimensions, got {tuple(t.shape)}")
+    n, d = t.shape
+    if n > _INT_MAX or d > _INT_MAX:
+        _too_large(name)
+    return n, d
+
+
+def embedding(tokens, table, scale=1.0, ignore_index=-100, out=None):
+    """Rows of the token table (float32 or bfloat16 [V, d]), scaled: returns dict x ([R, d], table's dtype; 0 in
+    rows whose token is ignore_index).
+
+    tokens: int32 [R].  Nothing is recorded for autograd: a table that requires gradients is refused while it
+    records.  Another token outside the vocabulary gives a row of zeros; embedding_errors tells."""
+    torch = _torch()
+    _not_recorded("embedding", table)
+    V, d = _rows(table, "table")
+    dtype = _code(table, "table")
+    R = tokens.numel()
+    if R > _INT_MAX:
+        _too_large("tokens [R]")
+    ignore_index = _ignored(ignore_index)
+    x = _given(out, "x", (R, d), table.dtype, table)
+    cur = _current(table)
+    _need(cur, ((tokens, (R,), torch.int32, "tokens"), (table, (V, d), table.dtype, "table"),
+                (x, (R, d), table.dtype, "x")))
+    rc = lib().cmsd_embedding(tokens.data_ptr(), table.data_ptr(), dtype, R, d, V, ignore_index, scale, x.data_ptr(),
+                              _stream_of(cur))
+    if rc != OK:
+        _check(rc, "cmsd_embedding")
+    return {"x": x}
+
+
+def embedding_backward_workspace(R, d, V):
+    """A workspace for embedding_backward of R rows on the current device (workspace_errors reads its error word)."""
+    return _head_workspace("cmsd_embedding_backward_workspace_bytes", R, d, V)
+
+
+def embedding_backward(tokens, d_x, V, scale=1.0, ignore_index=-100, add=False, out=None, ws=None):
+    """The table's gradient, scale times the sum of each token's rows of d_x (float32 or bfloat16 [R, d]): returns
+    dict d_table ([V, d], d_x's dtype), written whole.
+
+    With add, out["d_table"] is given and the sums are added to it: a head that shares the table passes the d_weight
+    of lmhead_loss_backward."""
+    torch = _torch()
+    R, d = _rows(d_x, "d_x")
+    V = int(V)
+    if not 0 < V <= _INT_MAX:
+        _too_large("V")
+    dtype = _code(d_x, "d_x")
+    ignore_index = _ignored(ignore_index)
+    if add and (out is None or out.get("d_table") is None):
+        raise CmsdError("add needs the d_table that is added to, in out")
+    d_table = _given(out, "d_table", (V, d), d_x.dtype, d_x)
+    cur = _current(d_x)
+    _need(cur, ((tokens, (R,), torch.int32, "tokens"), (d_x, (R, d), d_x.dtype, "d_x"),
+                (d_table, (V, d), d_x.dtype, "d_table")))
+    ws = ws if ws is not None else embedding_backward_workspace(R, d, V)
+    rc = lib().cmsd_embedding_backward(tokens.data_ptr(), d_x.data_ptr(), dtype, R, d, V, ignore_index, scale,
+                                       1 if add else 0, d_table.data_ptr(), ws.data_ptr(), _need_ws(ws, cur),
+                                       _stream_of(cur))
+    if rc != OK:
+        _check(rc, "cmsd_embedding_backward")
+    return {"d_table": d_table}
+
+
+def embedding_errors():
+    """The error bits of the calls of embedding and embedding_backward on the current device since they were last
+    read here (bit 0: a token that is neither in the vocabulary nor ignore_index).  Clears them and waits for the
+    current stream."""
+    f = ctypes.c_uint32(0)
+    _torch()
+    _check(lib().cmsd_embedding_errors(_stream(), ctypes.byref(f)), "cmsd_embedding_errors")
+    return int(f.value)
+
+
+def layernorm(x, weight=None, bias=None, eps=1e-5, stats=True, out=None):
+    """Layer norm of the rows of x (float32 or bfloat16 [R, d]); weight and bias: float32 or bfloat16 [d], both of
+    one dtype, or None (ones, zeros).
+
+    Returns dict y ([R, d], x's dtype) and, with stats, mean and rstd (float32 [R]) for layernorm_backward.  Nothing
+    is recorded for autograd: tensors that require gradients are refused while it records."""
+    torch = _torch()
+    _not_recorded("layernorm", x, weight, bias)
+    R, d = _rows(x, "x")
+    dtype = _code(x, "x")
+    p = weight if weight is not None else bias
+    wdtype = dtype if p is None else _code(p, "weight" if weight is not None else "bias")
+    y = _given(out, "y", (R, d), x.dtype, x)
+    cur = _current(x)
+    specs = [(x, (R, d), x.dtype, "x"), (y, (R, d), x.dtype, "y")]
+    if weight is not None:
+        specs.append((weight, (d,), p.dtype, "weight"))
+    if bias is not None:
+        specs.append((bias, (d,), p.dtype, "bias"))
+    o = {"y": y}
+    if stats:
+        for name in ("mean", "rstd"):
+            o[name] = _given(out, name, (R,), torch.float32, x)
+            specs.append((o[name], (R,), torch.float32, name))
+    _need(cur, specs)
+    rc = lib().cmsd_layernorm(x.data_ptr(), _ptr(weight), _ptr(bias), dtype, wdtype, R, d, eps, y.data_ptr(),
+                              _ptr(o.get("mean")), _ptr(o.get("rstd")), _stream_of(cur))
+    if rc != OK:
+        _check(rc, "cmsd_layernorm")
+    return o
+
+
+def layernorm_backward_workspace(R, d):
+    """A workspace for layernorm_backward of R rows on the current device."""
+    torch = _torch()
+    if max(R, d) > _INT_MAX:
+        _too_large("cmsd_layernorm_backward_workspace_bytes")
+    n = int(lib().cmsd_layernorm_backward_workspace_bytes(int(R), int(d)))
+    if n == 0:
+        _too_large("cmsd_layernorm_backward_workspace_bytes")
+    return torch.empty(n, dtype=torch.uint8, device="cuda")
+
+
+def layernorm_backward(x, weight, mean, rstd, d_y, x_grad=True, weight_grad=True, bias_grad=True, out=None, ws=None):
+    """The gradients of layernorm: mean and rstd are its outputs, d_y ([R, d], x's dtype) is dL/dy, weight as there
+    (None: ones).
+
+    Returns dict d_x ([R, d], x's dtype, with x_grad), d_weight (with weight_grad) and d_bias (with bias_grad), both
+    [d] of weight's dtype (x's without weight), written whole."""
+    torch = _torch()
+    R, d = _rows(x, "x")
+    dtype = _code(x, "x")
+    ptype = x.dtype if weight is None else weight.dtype
+    wdtype = dtype if weight is None else _code(weight, "weight")
+    f32 = torch.float32
+    specs = [(x, (R, d), x.dtype, "x"), (mean, (R,), f32, "mean"), (rstd, (R,), f32, "rstd"),
+             (d_y, (R, d), x.dtype, "d_y")]
+    if weight is not None:
+        specs.append((weight, (d,), ptype, "weight"))
+    o = {}
+    for name, want, shape, t in (("d_x", x_grad, (R, d), x.dtype), ("d_weight", weight_grad, (d,), ptype),
+                                 ("d_bias", bias_grad, (d,), ptype)):
+        if want:
+            o[name] = _given(out, name, shape, t, x)
+            specs.append((o[name], shape, t, name))
+    cur = _current(x)
+    _need(cur, specs)
+    ws = ws if ws is not None else layernorm_backward_workspace(R, d)
+    rc = lib().cmsd_layernorm_backward(x.data_ptr(), _ptr(weight), mean.data_ptr(), rstd.data_ptr(), d_y.data_ptr(),
+                                       dtype, wdtype, R, d, _ptr(o.get("d_x")), _ptr(o.get("d_weight")),
+                                       _ptr(o.get("d_bias")), ws.data_ptr(), _need_ws(ws, cur), _stream_of(cur))
+    if rc != OK:
+        _check(rc, "cmsd_layernorm_backward")
+    return o
+
+
+def _word(v, name):
+    v = int(v)
+    if not 0 <= v < 1 << 32:
+        raise CmsdError(f"{name} must be a 32-bit number that is not negative")
+    return v
+
+
+def _dropout(fn, x, xname, yname, p, seed, iteration, site, step, residual, out):
+    torch = _torch()
+    dtype = _code(x, xname)
+    iteration, site = _word(iteration, "iteration"), _word(site, "site")
+    y = _given(out, yname, x.shape, x.dtype, x)
+    cur = _current(x)
+    specs = [(x, x.shape, x.dtype, xname), (y, x.shape, x.dtype, yname)]
+    if residual is not None:
+        specs.append((residual, x.shape, x.dtype, "residual"))
+    if step is not None:
+        specs.append((step, (1,), torch.int32, "step"))
+    _need(cur, specs)
+    more = (_ptr(residual),) if fn == "cmsd_dropout" else ()
+    rc = getattr(lib(), fn)(x.data_ptr(), *more, dtype, x.numel(), p, int(seed), iteration, site, _ptr(step),
+                            y.data_ptr(), _stream_of(cur))
+    if rc != OK:
+        _check(rc, fn)
+    return {yname: y}
+
+
+def dropout(x, p, seed, iteration=0, site=0, residual=None, step=None, out=None):
+    """Dropout with rate p (a multiple of 2^-16, the nearest one) and kept entries scaled up, residual added:
+    returns dict y (x's shape and dtype, float32 or bfloat16).
+
+    The mask is a function of seed, iteration (a training step), site (a layer) and an entry's place in x, and is not
+    stored.  step: None, or an int32 [1] tensor that is added to iteration when the call runs (a captured call then
+    draws another mask at each replay).  Nothing is recorded for autograd: tensors that require gradients are refused
+    while it records."""
+    _torch()
+    _not_recorded("dropout", x, residual)
+    return _dropout("cmsd_dropout", x, "x", "y", p, seed, iteration, site, step, residual, out)
+
+
+def dropout_backward(d_y, p, seed, iteration=0, site=0, step=None, out=None):
+    """The gradient of dropout by x, given the same p, seed, iteration, site and step: returns dict d_x.  (The
+    residual's gradient is d_y itself.)"""
+    return _dropout("cmsd_dropout_backward", d_y, "d_y", "d_x", p, seed, iteration, site, step, None, out)
 
 
 def verify(draft, target, tokens, conf, draft_lse=None, k_row=None, p=None, seed=0, iteration=0,

@@ -15,6 +15,7 @@
 #include "cmsd_head.h"
 #include "cmsd_internal.h"
 #include "cmsd_philox.cuh"
+#include "cmsd_train.h"
 
 using namespace cmsd;
 
@@ -680,6 +681,33 @@ size_t i8_layout(HeadI8Args& a, char* w) {
   a.mag = (int*)(w ? w + kAlign + h : nullptr);
   return kAlign + h + up(R * 4);
 }
+bool is_dtype(int t) { return t == CMSD_F32 || t == CMSD_BF16; }
+size_t dtype_bytes(int t) { return t == CMSD_F32 ? 4 : 2; }
+int check_rows(int R, int d) {
+  return R < 0 || R > (1 << 28) || d < 1 || d > (1 << 16) ? CMSD_EINVAL : CMSD_OK;
+}
+int check_embed(int R, int d, int V) {
+  return check_rows(R, d) || V < 1 || V > (1 << 30) || (double)V * d >= 70368744177664.0 ? CMSD_EINVAL : CMSD_OK;
+}
+// both directions of dropout: y is d_x and x is d_y in the second
+int dropout(const void* x, const void* residual, int dtype, int64_t n, double p, uint64_t seed, uint32_t iteration,
+            uint32_t site, const uint32_t* step, void* y, void* stream) {
+  if (!is_dtype(dtype)) return CMSD_EDTYPE;
+  if (n < 0 || n >= (int64_t)1 << 46 || !(p >= 0.0 && p <= 1.0)) return CMSD_EINVAL;
+  if (n == 0) return CMSD_OK;
+  if (!x || !y) return CMSD_EINVAL;
+  if (!aligned16(x) || !aligned16(y) || !aligned16(residual) || !aligned4(step)) return CMSD_EALIGN;
+  const size_t nb = (size_t)n * dtype_bytes(dtype);
+  if (outputs_overlap({{y, nb}}, {{x, nb}, {residual, nb}, {step, 4}})) return CMSD_EINVAL;
+  DropArgs a = {};
+  a.x = x; a.residual = residual; a.y = y;
+  a.dtype = dtype; a.n = n;
+  a.drop = (uint32_t)nearbyint(p * 65536.0);
+  a.scale = a.drop < 65536u ? (float)(65536.0 / (65536.0 - a.drop)) : 0.f;
+  a.seed = seed; a.iteration = iteration; a.site = site; a.step = step;
+  const cudaError_t e = launch_dropout(a, (cudaStream_t)stream);
+  return e == cudaSuccess ? CMSD_OK : cuda_fail(e);
+}
 int check_lmhead(int R, int d, int V) {
   if (R < 0 || d < 64 || d % 64 != 0 || d > (1 << 20) || V < 2) return CMSD_EINVAL;
   if ((double)R * (double)V >= 70368744177664.0) return CMSD_EINVAL;   // 2^46 logits
@@ -889,6 +917,130 @@ int cmsd_lmhead_i8(const int8_t* hidden_q, const float* hidden_scale, const int8
   a.logits = logits;
   const cudaError_t e = launch_head_i8(a, (cudaStream_t)stream);
   return e == cudaSuccess ? CMSD_OK : cuda_fail(e);
+}
+
+int cmsd_embedding(const int32_t* tokens, const void* table, int dtype, int R, int d, int V, int ignore_index,
+                   float scale, void* x, void* stream) {
+  if (!is_dtype(dtype)) return CMSD_EDTYPE;
+  if (check_embed(R, d, V) || !isfinite(scale)) return CMSD_EINVAL;
+  if (R == 0) return CMSD_OK;
+  if (!tokens || !table || !x) return CMSD_EINVAL;
+  if (!aligned4(tokens) || !aligned16(table) || !aligned16(x)) return CMSD_EALIGN;
+  const size_t row = d * dtype_bytes(dtype);
+  if (outputs_overlap({{x, R * row}}, {{tokens, (size_t)R * 4}, {table, V * row}})) return CMSD_EINVAL;
+  EmbedArgs a = {};
+  a.tokens = tokens; a.table = table; a.x = x;
+  a.dtype = dtype; a.R = R; a.d = d; a.V = V; a.ignore = ignore_index; a.scale = scale;
+  const cudaError_t e = launch_embed(a, (cudaStream_t)stream);
+  return e == cudaSuccess ? CMSD_OK : cuda_fail(e);
+}
+
+size_t cmsd_embedding_backward_workspace_bytes(int R, int d, int V) {
+  if (check_embed(R, d, V)) return 0;
+  EmbedArgs a = {};
+  a.R = R; a.d = d; a.V = V;
+  return embed_layout(a, nullptr);
+}
+
+int cmsd_embedding_backward(const int32_t* tokens, const void* d_x, int dtype, int R, int d, int V,
+                            int ignore_index, float scale, int add, void* d_table, void* ws, size_t ws_bytes,
+                            void* stream) {
+  if (!is_dtype(dtype)) return CMSD_EDTYPE;
+  if (check_embed(R, d, V) || !isfinite(scale) || !d_table) return CMSD_EINVAL;
+  if (!aligned16(d_table)) return CMSD_EALIGN;
+  const size_t row = d * dtype_bytes(dtype);
+  if (R == 0) {
+    if (add) return CMSD_OK;
+    const cudaError_t e = cudaMemsetAsync(d_table, 0, V * row, (cudaStream_t)stream);
+    return e == cudaSuccess ? CMSD_OK : cuda_fail(e);
+  }
+  if (!tokens || !d_x) return CMSD_EINVAL;
+  if (!aligned4(tokens) || !aligned16(d_x)) return CMSD_EALIGN;
+  EmbedArgs a = {};
+  a.dtype = dtype; a.R = R; a.d = d; a.V = V; a.ignore = ignore_index; a.scale = scale; a.add = add != 0;
+  const size_t need = embed_layout(a, nullptr);
+  if (!ws || ws_bytes < need) return CMSD_ENOWS;
+  if (!aligned16(ws)) return CMSD_EALIGN;
+  if (outputs_overlap({{d_table, V * row}, {ws, need}}, {{tokens, (size_t)R * 4}, {d_x, R * row}})) return CMSD_EINVAL;
+  embed_layout(a, (char*)ws);
+  a.tokens = tokens; a.d_x = d_x; a.d_table = d_table;
+  const cudaError_t e = launch_embed_backward(a, (cudaStream_t)stream);
+  return e == cudaSuccess ? CMSD_OK : cuda_fail(e);
+}
+
+int cmsd_embedding_errors(void* stream, uint32_t* flags_out) {
+  if (!flags_out) return CMSD_EINVAL;
+  unsigned f = 0;
+  const cudaError_t e = take_embed_errors(&f, (cudaStream_t)stream);
+  if (e != cudaSuccess) return cuda_fail(e);
+  *flags_out = f;
+  return CMSD_OK;
+}
+
+int cmsd_layernorm(const void* x, const void* weight, const void* bias, int dtype, int wdtype, int R, int d,
+                   float eps, void* y, float* mean, float* rstd, void* stream) {
+  if (!is_dtype(dtype) || !is_dtype(wdtype)) return CMSD_EDTYPE;
+  if (check_rows(R, d) || !(eps > 0.f) || !isfinite(eps)) return CMSD_EINVAL;
+  if (R == 0) return CMSD_OK;
+  if (!x || !y) return CMSD_EINVAL;
+  if (!aligned16(x) || !aligned16(weight) || !aligned16(bias) || !aligned16(y) || !aligned4(mean) || !aligned4(rstd))
+    return CMSD_EALIGN;
+  const size_t nb = (size_t)R * d * dtype_bytes(dtype), pb = d * dtype_bytes(wdtype), r4 = (size_t)R * 4;
+  if (outputs_overlap({{y, nb}, {mean, r4}, {rstd, r4}}, {{x, nb}, {weight, pb}, {bias, pb}})) return CMSD_EINVAL;
+  NormArgs a = {};
+  a.x = x; a.weight = weight; a.bias = bias;
+  a.dtype = dtype; a.wdtype = wdtype; a.R = R; a.d = d; a.eps = eps;
+  a.y = y; a.mean = mean; a.rstd = rstd;
+  const cudaError_t e = launch_norm(a, (cudaStream_t)stream);
+  return e == cudaSuccess ? CMSD_OK : cuda_fail(e);
+}
+
+size_t cmsd_layernorm_backward_workspace_bytes(int R, int d) {
+  if (check_rows(R, d)) return 0;
+  NormArgs a = {};
+  a.R = R; a.d = d;
+  return norm_layout(a, nullptr);
+}
+
+int cmsd_layernorm_backward(const void* x, const void* weight, const float* mean, const float* rstd,
+                            const void* d_y, int dtype, int wdtype, int R, int d, void* d_x, void* d_weight,
+                            void* d_bias, void* ws, size_t ws_bytes, void* stream) {
+  if (!is_dtype(dtype) || !is_dtype(wdtype)) return CMSD_EDTYPE;
+  if (check_rows(R, d) || (!d_x && !d_weight && !d_bias)) return CMSD_EINVAL;
+  if (!aligned16(d_weight) || !aligned16(d_bias)) return CMSD_EALIGN;
+  const size_t nb = (size_t)R * d * dtype_bytes(dtype), pb = d * dtype_bytes(wdtype), r4 = (size_t)R * 4;
+  if (R == 0) {                                  // no rows: the parameters' gradients are zero
+    if (overlap(d_weight, pb, d_bias, pb)) return CMSD_EINVAL;
+    cudaError_t e = d_weight ? cudaMemsetAsync(d_weight, 0, pb, (cudaStream_t)stream) : cudaSuccess;
+    if (e == cudaSuccess && d_bias) e = cudaMemsetAsync(d_bias, 0, pb, (cudaStream_t)stream);
+    return e == cudaSuccess ? CMSD_OK : cuda_fail(e);
+  }
+  if (!x || !mean || !rstd || !d_y) return CMSD_EINVAL;
+  if (!aligned16(x) || !aligned16(weight) || !aligned16(d_y) || !aligned16(d_x) || !aligned4(mean) || !aligned4(rstd))
+    return CMSD_EALIGN;
+  NormArgs a = {};
+  a.dtype = dtype; a.wdtype = wdtype; a.R = R; a.d = d;
+  const size_t need = norm_layout(a, nullptr);
+  if (!ws || ws_bytes < need) return CMSD_ENOWS;
+  if (!aligned16(ws)) return CMSD_EALIGN;
+  if (outputs_overlap({{d_x, nb}, {d_weight, pb}, {d_bias, pb}, {ws, need}},
+                      {{x, nb}, {weight, pb}, {mean, r4}, {rstd, r4}, {d_y, nb}}))
+    return CMSD_EINVAL;
+  norm_layout(a, (char*)ws);
+  a.x = x; a.weight = weight; a.mean_in = mean; a.rstd_in = rstd; a.d_y = d_y;
+  a.d_x = d_x; a.d_weight = d_weight; a.d_bias = d_bias;
+  const cudaError_t e = launch_norm_backward(a, (cudaStream_t)stream);
+  return e == cudaSuccess ? CMSD_OK : cuda_fail(e);
+}
+
+int cmsd_dropout(const void* x, const void* residual, int dtype, int64_t n, double p, uint64_t seed,
+                 uint32_t iteration, uint32_t site, const uint32_t* step, void* y, void* stream) {
+  return dropout(x, residual, dtype, n, p, seed, iteration, site, step, y, stream);
+}
+
+int cmsd_dropout_backward(const void* d_y, int dtype, int64_t n, double p, uint64_t seed, uint32_t iteration,
+                          uint32_t site, const uint32_t* step, void* d_x, void* stream) {
+  return dropout(d_y, nullptr, dtype, n, p, seed, iteration, site, step, d_x, stream);
 }
 
 int cmsd_test_head_wait(int arrive, void* ws, size_t ws_bytes, void* stream) {
