@@ -375,7 +375,7 @@ int cmsd_layernorm_backward(const void* x, const void* weight, const float* mean
  *   half e & 1 (the low one first) of word (e >> 1) & 3 of counter
  *   (g lo, g hi, site, it << 2 | 3), g = e >> 3, it = iteration + *step.
  * A dropped entry of x reaches no result, whatever it holds.
- *   x, y: dtype [n], 0 <= n < 2^46; residual: dtype [n], or NULL (zeros).
+ *   x, y: dtype [n], 0 <= n < 2^42; residual: dtype [n], or NULL (zeros).
  *   site: tells the uses of one iteration apart (a layer's number); step: NULL, or
  *     a uint32 on the device that is added to iteration when the call runs, so that
  *     a captured call draws another mask at each replay.  Iterations 2^30 apart

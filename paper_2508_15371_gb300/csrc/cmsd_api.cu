@@ -693,7 +693,7 @@ int check_embed(int R, int d, int V) {
 int dropout(const void* x, const void* residual, int dtype, int64_t n, double p, uint64_t seed, uint32_t iteration,
             uint32_t site, const uint32_t* step, void* y, void* stream) {
   if (!is_dtype(dtype)) return CMSD_EDTYPE;
-  if (n < 0 || n >= (int64_t)1 << 46 || !(p >= 0.0 && p <= 1.0)) return CMSD_EINVAL;
+  if (n < 0 || n >= (int64_t)1 << 42 || !(p >= 0.0 && p <= 1.0)) return CMSD_EINVAL;
   if (n == 0) return CMSD_OK;
   if (!x || !y) return CMSD_EINVAL;
   if (!aligned16(x) || !aligned16(y) || !aligned16(residual) || !aligned4(step)) return CMSD_EALIGN;

@@ -9,6 +9,7 @@
 #include <cuda_bf16.h>
 
 #include "cmsd_head.h"
+#include "cmsd_launch.cuh"
 #include "cmsd_tc.cuh"
 
 namespace cmsd {
@@ -1021,23 +1022,6 @@ __global__ void __launch_bounds__(kUnpackThreads) head_unpack_kernel(const HeadL
 }
 
 unsigned tiles(int64_t n, int t) { return (unsigned)((n + t - 1) / t); }
-// a launch that may begin before what precedes it on the stream has ended (early:
-// the first launch of a call does not)
-template <typename... P, typename... A>
-cudaError_t launch(bool early, void (*kernel)(P...), dim3 grid, unsigned threads, size_t smem, cudaStream_t s,
-                   A... args) {
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = grid;
-  cfg.blockDim = dim3(threads);
-  cfg.dynamicSmemBytes = smem;
-  cfg.stream = s;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = early ? 1 : 0;
-  return cudaLaunchKernelEx(&cfg, kernel, args...);
-}
 cudaError_t launch_pack(const HeadLossArgs& a, cudaStream_t s) {
   int rows = kPackWarps;
   while ((int64_t)rows * 1024 < a.R) rows *= 2;

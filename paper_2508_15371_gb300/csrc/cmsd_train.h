@@ -15,8 +15,16 @@ struct EmbedArgs {
   void* d_table;                 // [V][d] (backward)
   int dtype, R, d, V, ignore, add;
   float scale;
+  int passes, bits, tile;        // radix passes, key bits of each, rows of a tile (backward)
   // workspace (backward)
   unsigned* err;
+  unsigned* key[2];              // [R] the rows' tokens in order (V: padding), where pass p writes: [p & 1]
+  int* order[2];                 // [R] the rows
+  int* count[4];                 // [tiles of rows][1 << bits] rows of each digit
+  int4* state;                   // [tiles of slots]
+  int pieces;                    // places in head and tail
+  float* head;                   // [pieces][d] pieces of sums that tiles' borders cut
+  float* tail;
 };
 size_t embed_layout(EmbedArgs& a, char* w);
 cudaError_t launch_embed(const EmbedArgs& a, cudaStream_t s);

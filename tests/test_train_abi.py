@@ -114,7 +114,7 @@ def test_norm_backward_refused(cmsd, kw, code):
 
 
 @pytest.mark.parametrize("kw,code", [
-    (dict(dtype=2), "EDTYPE"), (dict(n=-1), "EINVAL"), (dict(n=1 << 46), "EINVAL"), (dict(p=-0.1), "EINVAL"),
+    (dict(dtype=2), "EDTYPE"), (dict(n=-1), "EINVAL"), (dict(n=1 << 42), "EINVAL"), (dict(p=-0.1), "EINVAL"),
     (dict(p=1.0001), "EINVAL"), (dict(p=NAN), "EINVAL"), (dict(x=None), "EINVAL"), (dict(y=None), "EINVAL"),
     (dict(x=A + 8), "EALIGN"), (dict(y=A + 2), "EALIGN"), (dict(r=A + 4), "EALIGN"), (dict(step=A + 2), "EALIGN"),
     (dict(y=I1), "EINVAL"), (dict(y=I2 + 192), "EINVAL"), (dict(step=O1 + 4), "EINVAL"),
@@ -131,10 +131,10 @@ def test_errors_need_a_place(cmsd):
 
 
 def test_workspaces_are_small(cmsd):
-    """They grow with the rows and, for the norm, with the width; not with the vocabulary times the width."""
+    """They grow with the rows times the width, or with the width; not with the vocabulary times the width."""
     for R, d, V in ((1, 1, 1), (4096, 2048, 128256), (1 << 20, 2048, 1 << 20)):
         n = cmsd.lib().cmsd_embedding_backward_workspace_bytes(R, d, V)
-        assert 0 < n <= (1 << 20) + 64 * R + 16 * V + R * d // 2
+        assert 0 < n <= (1 << 20) + 64 * R + 16 * V + 8 * R * d
         n = cmsd.lib().cmsd_layernorm_backward_workspace_bytes(R, d)
         assert 0 < n <= 4096 + 1024 * 8 * d
 
