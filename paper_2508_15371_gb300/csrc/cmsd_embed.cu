@@ -6,6 +6,8 @@
 // every row of d_table written once.
 #include <cuda_bf16.h>
 
+#include <algorithm>
+
 #include "cmsd_device.cuh"
 #include "cmsd_errors.cuh"
 #include "cmsd_launch.cuh"
@@ -62,25 +64,58 @@ __device__ __forceinline__ unsigned key_of(const EmbedArgs& a, int token, bool& 
   return in && token != a.ignore ? (unsigned)token : (unsigned)a.V;
 }
 
+// A table that is written whole gets its zeros from the launches that put the rows
+// in order: that takes a few CTAs some microseconds a launch, and the others write
+// all of the table.  Rows that get a sum are written again, a fifth more bytes where
+// 32768 tokens meet a vocabulary of 128256 ranks (d = 2048 bf16: 123 us; leaving
+// them out, by looking each token up beside the sums, 136).
+constexpr int kFillThreads = 256;
+constexpr int kFillVecs = 16;                        // 16-byte vectors of a thread
+constexpr size_t kFillCta = (size_t)kFillThreads * kFillVecs * 16;
+__device__ __forceinline__ void fill(const EmbedArgs& a, size_t first, size_t last, int cta) {
+  const size_t at = first + (size_t)cta * kFillCta + threadIdx.x * 16;
+  char* p = static_cast<char*>(a.d_table) + at;
+#pragma unroll
+  for (int k = 0; k < kFillVecs; ++k) {
+    const size_t o = (size_t)k * kFillThreads * 16;
+    if (at + o + 16 <= last) *reinterpret_cast<uint4*>(p + o) = make_uint4(0, 0, 0, 0);
+    else if (at + o < last)                          // (the end of a table of odd rows)
+      for (size_t q = at + o; q < last; q += 2) *reinterpret_cast<uint16_t*>(static_cast<char*>(a.d_table) + q) = 0;
+  }
+}
+
 // Few rows: each row's place is the number of rows before it in (token, row)
 // order, counted by comparing it with all of them: R^2 comparisons, spread over
 // the GPU, in one launch.  A warp RPW rows, a lane every 32nd four of the others.
 constexpr int kRankRows = 8192;
 constexpr int kRankThreads = 256;
+constexpr int kRankAhead = 16;                       // tokens of a thread requested at once
 template <int RPW>
-__global__ void __launch_bounds__(kRankThreads) embed_rank_kernel(const EmbedArgs a) {
+__global__ void __launch_bounds__(kRankThreads) embed_rank_kernel(const EmbedArgs a, int row_ctas) {
   extern __shared__ uint4 s_key4[];
   unsigned* s_key = reinterpret_cast<unsigned*>(s_key4);
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  if ((int)blockIdx.x >= row_ctas) {
+    fill(a, a.fill[0], a.fill[1], blockIdx.x - row_ctas);
+    return;
+  }
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, padded = (a.R + 127) / 128 * 128;
-  for (int r = threadIdx.x; r < padded; r += kRankThreads) {
-    bool bad = false;
-    unsigned k = 0xFFFFFFFFu;
-    if (r < a.R) {
-      k = key_of(a, a.tokens[r], bad);
-      if (bad && blockIdx.x == 0) report(a.err, 1u);
+  for (int rb = threadIdx.x; rb < padded; rb += kRankThreads * kRankAhead) {
+    int token[kRankAhead];
+#pragma unroll
+    for (int u = 0; u < kRankAhead; ++u) {
+      const int r = rb + u * kRankThreads;
+      token[u] = r < a.R ? __ldg(a.tokens + r) : 0;
     }
-    s_key[r] = k;
+#pragma unroll
+    for (int u = 0; u < kRankAhead; ++u) {
+      const int r = rb + u * kRankThreads;
+      if (r >= padded) break;
+      bool bad;
+      const unsigned k = key_of(a, token[u], bad);
+      if (r < a.R && bad && blockIdx.x == 0) report(a.err, 1u);
+      s_key[r] = r < a.R ? k : 0x7FFFFFFFu;
+    }
   }
   __syncthreads();
   const int r0 = (blockIdx.x * (kRankThreads / 32) + warp) * RPW;
@@ -92,19 +127,22 @@ __global__ void __launch_bounds__(kRankThreads) embed_rank_kernel(const EmbedArg
     key[j] = s_key[min(r0 + j, a.R - 1)];
     n[j] = 0;
   }
-  // rows before: not above; rows behind: below
+  // rows before: not above; rows behind: below.  Keys are below 2^31, so a difference's sign bit tells
+  const auto below = [](const uint4& t, unsigned k) {
+    return (int)((t.x - k >> 31) + (t.y - k >> 31) + (t.z - k >> 31) + (t.w - k >> 31));
+  };
   const int own = r0 / 128, all = padded / 128;
 #pragma unroll 4
   for (int c = 0; c < own; ++c) {
     const uint4 t = s_key4[c * 32 + lane];
 #pragma unroll
-    for (int j = 0; j < RPW; ++j) n[j] += (t.x <= key[j]) + (t.y <= key[j]) + (t.z <= key[j]) + (t.w <= key[j]);
+    for (int j = 0; j < RPW; ++j) n[j] += below(t, key[j] + 1);
   }
 #pragma unroll 4
   for (int c = own + 1; c < all; ++c) {
     const uint4 t = s_key4[c * 32 + lane];
 #pragma unroll
-    for (int j = 0; j < RPW; ++j) n[j] += (t.x < key[j]) + (t.y < key[j]) + (t.z < key[j]) + (t.w < key[j]);
+    for (int j = 0; j < RPW; ++j) n[j] += below(t, key[j]);
   }
   const uint4 t = s_key4[own * 32 + lane];
   const int at = own * 128 + lane * 4;
@@ -129,17 +167,29 @@ __global__ void __launch_bounds__(kRankThreads) embed_rank_kernel(const EmbedArg
 constexpr int kRadixBits = 10;
 constexpr int kRadixThreads = 256, kRadixWarps = kRadixThreads / 32;
 constexpr int kTileMin = 2048;
-__global__ void __launch_bounds__(kRadixThreads) embed_count_kernel(const EmbedArgs a, int digits) {
+constexpr int kRound = 8;                            // rows of a lane requested at once
+__global__ void __launch_bounds__(kRadixThreads) embed_count_kernel(const EmbedArgs a, int digits, int tiles) {
   extern __shared__ int s_count[];
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  if ((int)blockIdx.x >= tiles) {
+    fill(a, a.fill[0], a.fill[1], blockIdx.x - tiles);
+    return;
+  }
   for (int g = threadIdx.x; g < digits; g += kRadixThreads) s_count[g] = 0;
   __syncthreads();
   const int64_t r0 = (int64_t)blockIdx.x * a.tile, r1 = r0 + a.tile < a.R ? r0 + a.tile : a.R;
-  for (int64_t r = r0 + threadIdx.x; r < r1; r += kRadixThreads) {
-    bool bad;
-    const unsigned k = key_of(a, a.tokens[r], bad);
-    if (bad) report(a.err, 1u);
-    atomicAdd(&s_count[k & (digits - 1)], 1);
+  for (int64_t rb = r0 + threadIdx.x; rb < r1; rb += kRadixThreads * kRound) {
+    int token[kRound];
+#pragma unroll
+    for (int u = 0; u < kRound; ++u) token[u] = rb + u * kRadixThreads < r1 ? __ldg(a.tokens + rb + u * kRadixThreads) : 0;
+#pragma unroll
+    for (int u = 0; u < kRound; ++u) {
+      if (rb + u * kRadixThreads >= r1) break;
+      bool bad;
+      const unsigned k = key_of(a, token[u], bad);
+      if (bad) report(a.err, 1u);
+      atomicAdd(&s_count[k & (digits - 1)], 1);
+    }
   }
   __syncthreads();
   for (int g = threadIdx.x; g < digits; g += kRadixThreads) {
@@ -167,24 +217,44 @@ __device__ __forceinline__ int cta_scan(int v) {
 }
 
 template <bool FIRST>
-__global__ void __launch_bounds__(kRadixThreads) embed_move_kernel(const EmbedArgs a, int pass, int bits) {
+__global__ void __launch_bounds__(kRadixThreads) embed_move_kernel(const EmbedArgs a, int pass, int bits, int tiles) {
   extern __shared__ int s_at[];                       // [kRadixWarps][digits]: counts, then the next place of each
-  const int digits = 1 << bits, lane = threadIdx.x & 31, warp = threadIdx.x >> 5, tiles = gridDim.x;
+  const int digits = 1 << bits, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  if ((int)blockIdx.x >= tiles) {                     // (nothing that the launch before makes is used)
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    fill(a, a.fill[pass + 1], a.fill[pass + 2], blockIdx.x - tiles);
+    return;
+  }
+  for (int g = threadIdx.x; g < kRadixWarps * digits; g += kRadixThreads) s_at[g] = 0;
+  __syncthreads();
   wait_for_previous();
   const int* count = a.count[pass];
   int* next = pass + 1 < a.passes ? a.count[pass + 1] : nullptr;
   const unsigned* key_in = a.key[(pass & 1) ^ 1];
   const int* order_in = a.order[(pass & 1) ^ 1];
   const int shift = pass * bits;
-  for (int g = threadIdx.x; g < kRadixWarps * digits; g += kRadixThreads) s_at[g] = 0;
-  __syncthreads();
   const int64_t r0 = (int64_t)blockIdx.x * a.tile, share = a.tile / kRadixWarps;
   const int64_t w0 = r0 + warp * share, w1 = w0 + share < a.R ? w0 + share : a.R;
   int* mine = s_at + warp * digits;
-  for (int64_t r = w0 + lane; r < w1; r += 32) {
-    bool bad;
-    const unsigned k = FIRST ? key_of(a, a.tokens[r], bad) : key_in[r];
-    atomicAdd(&mine[k >> shift & (digits - 1)], 1);
+  unsigned key[kRound];
+  const auto take = [&](int64_t rb) {                 // the keys of the next 32 * kRound rows
+#pragma unroll
+    for (int u = 0; u < kRound; ++u) {
+      const int64_t r = rb + 32 * u + lane;
+      key[u] = r < w1 ? (FIRST ? (unsigned)__ldg(a.tokens + r) : __ldcg(key_in + r)) : 0;
+    }
+    if (FIRST)
+#pragma unroll
+      for (int u = 0; u < kRound; ++u) {
+        bool bad;
+        key[u] = key_of(a, (int)key[u], bad);
+      }
+  };
+  for (int64_t rb = w0; rb < w1; rb += 32 * kRound) {
+    take(rb);
+#pragma unroll
+    for (int u = 0; u < kRound; ++u)
+      if (rb + 32 * u + lane < w1) atomicAdd(&mine[key[u] >> shift & (digits - 1)], 1);
   }
   __syncthreads();
   // the first place of each (warp, digit): digits below, the same one in earlier tiles, in earlier warps;
@@ -197,7 +267,7 @@ __global__ void __launch_bounds__(kRadixThreads) embed_move_kernel(const EmbedAr
     const int g = threadIdx.x * per + q;
     if (q >= per || g >= digits) continue;
     int b = 0, rest = 0;
-#pragma unroll 8
+#pragma unroll 16
     for (int t = 0; t < tiles; ++t) {
       const int c = __ldcg(count + (size_t)t * digits + g);
       if (t < (int)blockIdx.x) b += c;
@@ -221,64 +291,42 @@ __global__ void __launch_bounds__(kRadixThreads) embed_move_kernel(const EmbedAr
     base += all[q];
   }
   __syncthreads();
-  for (int64_t rb = w0; rb < w1; rb += 32) {          // 32 rows at a time, in order
-    const int64_t r = rb + lane;
-    const bool in = r < w1;
-    unsigned k = 0;
-    int row = (int)r;
-    if (in) {
-      bool bad;
-      k = FIRST ? key_of(a, a.tokens[r], bad) : key_in[r];
-      if (!FIRST) row = order_in[r];
-    }
-    const int g = in ? (int)(k >> shift & (digits - 1)) : digits;
-    const unsigned same = __match_any_sync(kFull, g);
-    int at = 0;
-    if (in) at = mine[g] + __popc(same & ((1u << lane) - 1u));
-    __syncwarp();
-    if (in && (same >> lane) == 1u) mine[g] = at + 1;   // the last of its digit
-    __syncwarp();
-    if (in) {
-      a.key[pass & 1][at] = k;
-      a.order[pass & 1][at] = row;
-      if (next) atomicAdd(next + (size_t)(at / a.tile) * digits + (k >> (shift + bits) & (digits - 1)), 1);
+  for (int64_t rb = w0; rb < w1; rb += 32 * kRound) {
+    if (share > 32 * kRound) take(rb);                // (else they are still there)
+    int row[kRound];
+    if (!FIRST)
+#pragma unroll
+      for (int u = 0; u < kRound; ++u) row[u] = rb + 32 * u + lane < w1 ? __ldcg(order_in + rb + 32 * u + lane) : 0;
+#pragma unroll
+    for (int u = 0; u < kRound; ++u) {                // 32 rows at a time, in order
+      const int64_t r = rb + 32 * u + lane;
+      const bool in = r < w1;
+      const int g = in ? (int)(key[u] >> shift & (digits - 1)) : digits;
+      const unsigned same = __match_any_sync(kFull, g);
+      int at = 0;
+      if (in) at = mine[g] + __popc(same & ((1u << lane) - 1u));
+      __syncwarp();
+      if (in && (same >> lane) == 1u) mine[g] = at + 1;   // the last of its digit
+      __syncwarp();
+      if (in) {
+        a.key[pass & 1][at] = key[u];
+        a.order[pass & 1][at] = FIRST ? (int)r : row[u];
+        if (next) atomicAdd(next + (size_t)(at / a.tile) * digits + (key[u] >> (shift + bits) & (digits - 1)), 1);
+      }
     }
   }
 }
 
 // ---- sums ------------------------------------------------------------------------------
-// The work is a list of slots, cut into equal tiles whatever the tokens are.
-// Written whole: token v has a slot for each of its rows and one more, so row i of
-// the ordered ones is slot key_i + i, and the slot after a token's rows writes
-// zeros where it had none.  Added to: row i is slot i.  A tile walks its slots with
-// the columns over its threads, kBatch rows requested at once; a token's last row
-// writes the sum.  A token that a border cuts leaves a piece of its sum (fp32) in
-// either tile, and embed_join_kernel adds those up.  Bound by memory.
-constexpr int kSlots = 64;                            // slots of a tile
+// The ordered rows, cut into equal tiles whatever their tokens are.  A tile walks its
+// rows with the columns over its threads, kBatch rows requested at once; a token's
+// last row writes the sum.  A token that a border cuts leaves a piece of its sum
+// (fp32) in either tile, and embed_join_kernel adds those up.  Bound by memory.
+constexpr int kSlots = 64;                            // rows of a tile at most
 constexpr int kBatch = 8;
-constexpr int kSumThreads = 256;
-
-template <bool ADD>
-__device__ __forceinline__ int64_t slot_of(const EmbedArgs& a, int64_t i, unsigned key) {
-  return ADD ? i : i + (int64_t)key;
-}
-// the first ordered row whose slot is not below `slot`, by a warp
-__device__ __forceinline__ int64_t first_row(const EmbedArgs& a, const unsigned* key, int64_t slot) {
-  int64_t lo = 0, hi = a.R;                           // it is in [lo, hi]
-  while (hi > lo) {
-    const int64_t step = (hi - lo + 31) / 32, i = lo + (threadIdx.x & 31) * step;
-    const bool below = i < hi && i + (int64_t)__ldcg(key + i) < slot;
-    const int n = __popc(__ballot_sync(kFull, below));
-    if (n == 0) return lo;
-    const int64_t last = lo + (n - 1) * step;         // the last probe below
-    hi = last + step < hi ? last + step : hi;
-    lo = last + 1;
-  }
-  return lo;
-}
-
-// A tile's state: the token whose rows go on behind it (-1: none), whether that one begins there or has all of the
-// tile's rows and others before them, and the place of the tile's pieces.
+constexpr int kSumThreads = 128;
+// A tile's state: the token whose rows go on behind it (-1: none), and whether that one begins there or has all of
+// the tile's rows and others before them.
 constexpr int kThrough = 1, kBegins = 2;
 
 template <typename T, int VE, bool ADD>
@@ -286,76 +334,53 @@ __global__ void __launch_bounds__(kSumThreads) embed_sum_kernel(const EmbedArgs 
   using V = RowVec<T, VE>;
   using Raw = typename V::Raw;
   __shared__ int2 s_slot[kSlots];                     // (row or -1, token to write or -1)
-  __shared__ int s_head, s_open, s_piece;             // the first rows go on from the tile before; the token left open
+  __shared__ int s_head, s_open;                      // the first rows go on from the tile before; the token left open
   const unsigned* key = a.key[last_pass & 1];
   const int* order = a.order[last_pass & 1];
-  const int64_t slot0 = (int64_t)blockIdx.x * kSlots;
+  const int nvec = a.d / VE;
   wait_for_previous();
+  const int tile = blockIdx.x, chunk = blockIdx.y;
   if (threadIdx.x < 32) {
-    const int lane = threadIdx.x;
-    const int64_t i0 = ADD ? slot0 : first_row(a, key, slot0);
-    // the rows of the tile, at most one a slot
+    const int lane = threadIdx.x, i0 = tile * a.slots;
     const unsigned prev = i0 > 0 ? __ldcg(key + i0 - 1) : 0xFFFFFFFFu;
     unsigned k[2], after[2];
-    int q[2];
-    unsigned rows[2] = {0, 0};
+    int row[2], n = 0;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      const int64_t i = i0 + lane + 32 * h;
-      k[h] = i < a.R ? __ldcg(key + i) : (unsigned)a.V;
-      after[h] = i + 1 < a.R ? __ldcg(key + i + 1) : 0xFFFFFFFFu;
-      const int64_t s = slot_of<ADD>(a, i, k[h]) - slot0;
-      q[h] = k[h] < (unsigned)a.V && s < kSlots ? (int)s : -1;
-      if (q[h] >= 0) rows[q[h] >> 5] |= 1u << (q[h] & 31);
+      const int i = i0 + lane + 32 * h;
+      const bool in = i < a.R && lane + 32 * h < a.slots;
+      k[h] = in ? __ldcg(key + i) : (unsigned)a.V;
+      row[h] = in ? __ldcg(order + i) : 0;
+      after[h] = in && i + 1 < a.R ? __ldcg(key + i + 1) : 0xFFFFFFFFu;
     }
-    rows[0] = __reduce_or_sync(kFull, rows[0]);
-    rows[1] = __reduce_or_sync(kFull, rows[1]);
-    const int n = __popc(rows[0]) + __popc(rows[1]);
-    // slots without a row: zeros, where the token has none
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      const int s = lane + 32 * h;
-      if (!(rows[h] >> lane & 1u)) {
-        const int before = (h ? __popc(rows[0]) : 0) + __popc(rows[h] & ((1u << lane) - 1u));
-        const int64_t v = slot0 + s - i0 - before;
-        int2 o = make_int2(-1, -1);
-        if (!ADD && v < a.V) {
-          const unsigned p = before > 0 ? __ldcg(key + i0 + before - 1) : prev;
-          if (p != (unsigned)v) o.y = (int)v;
-        }
-        s_slot[s] = o;
-      }
+      const bool in = k[h] < (unsigned)a.V;           // padding is behind all others
+      s_slot[lane + 32 * h] = make_int2(in ? row[h] : -1, in && after[h] != k[h] ? (int)k[h] : -1);
+      n += __popc(__ballot_sync(kFull, in));
     }
-#pragma unroll
-    for (int h = 0; h < 2; ++h)
-      if (q[h] >= 0)
-        s_slot[q[h]] = make_int2(order[i0 + lane + 32 * h], after[h] != k[h] ? (int)k[h] : -1);
     const int tail = n - 1;                           // the last row's lane and half
     const unsigned kt = __shfl_sync(kFull, tail >= 32 ? k[1] : k[0], tail & 31);
     const unsigned at = __shfl_sync(kFull, tail >= 32 ? after[1] : after[0], tail & 31);
-    const unsigned kf = __shfl_sync(kFull, k[0], 0);
     if (lane == 0) {
-      const bool head = n > 0 && kf == prev, open = n > 0 && at == kt;
+      const bool head = n > 0 && k[0] == prev, open = n > 0 && at == kt;
       s_head = head;
       s_open = open ? (int)kt : -1;
-      // (places by the first row where there are fewer rows than tiles)
-      s_piece = a.pieces == a.R ? (int)i0 : (int)blockIdx.x;
-      if (blockIdx.y == 0)
-        a.state[blockIdx.x] = make_int4(s_open, open ? (head && kf == kt ? kThrough : kBegins) : 0, s_piece, 0);
+      if (chunk == 0) a.state[tile] = make_int2(s_open, open ? (head && k[0] == kt ? kThrough : kBegins) : 0);
     }
   }
   __syncthreads();
-  const int nvec = a.d / VE, c = blockIdx.y * blockDim.x + threadIdx.x;
+  const int c = chunk * blockDim.x + threadIdx.x;
   if (c >= nvec) return;
   const Raw* d_x = static_cast<const Raw*>(a.d_x) + c;
   Raw* out = static_cast<Raw*>(a.d_table) + c;
-  const size_t piece = (size_t)s_piece * a.d + (size_t)c * VE;
+  const size_t piece = (size_t)tile * a.d + (size_t)c * VE;
   float sum[VE];
 #pragma unroll
   for (int j = 0; j < VE; ++j) sum[j] = 0.f;
   bool head = s_head != 0;
 #pragma unroll 1
-  for (int s0 = 0; s0 < kSlots; s0 += kBatch) {
+  for (int s0 = 0; s0 < a.slots; s0 += kBatch) {
     Raw x[kBatch], had[ADD ? kBatch : 1];
     int2 o[kBatch];
 #pragma unroll
@@ -367,19 +392,16 @@ __global__ void __launch_bounds__(kSumThreads) embed_sum_kernel(const EmbedArgs 
     }
 #pragma unroll
     for (int u = 0; u < kBatch; ++u) {
-      if (o[u].x >= 0) {
-        float f[VE];
-        V::get(x[u], f);
+      float f[VE];
+      V::get(x[u], f);
 #pragma unroll
-        for (int j = 0; j < VE; ++j) sum[j] += f[j];
-      }
+      for (int j = 0; j < VE; ++j) sum[j] += f[j];
       if (o[u].y >= 0) {
-        if (o[u].x >= 0 && head) {                    // (the join writes it)
+        if (head) {                                   // (the join writes it)
 #pragma unroll
           for (int j = 0; j < VE; ++j) a.head[piece + j] = sum[j];
           head = false;
         } else {
-          float f[VE];
           if (ADD) V::get(had[u], f);
 #pragma unroll
           for (int j = 0; j < VE; ++j) f[j] = ADD ? __fmaf_rn(sum[j], a.scale, f[j]) : sum[j] * a.scale;
@@ -396,43 +418,98 @@ __global__ void __launch_bounds__(kSumThreads) embed_sum_kernel(const EmbedArgs 
 }
 
 // Tokens that borders cut: the piece of the tile where one begins, those of the
-// tiles that it fills, and that of the tile where it ends, in this order.  A CTA 32
-// tiles; a warp a token and 32 of its columns.
-constexpr int kJoinThreads = 256;
-template <typename T, bool ADD>
+// tiles that it fills, and that of the tile where it ends, in this order.  A CTA
+// kJoinTiles tiles and, with others, their columns; a warp a token and 32 JV of its
+// columns, or, for a token of more than kLong tiles, the CTA's warps an eighth of the
+// tiles each.
+constexpr int kJoinThreads = 256, kJoinWarps = kJoinThreads / 32;
+constexpr int kJoinTiles = 8;
+constexpr int kLong = 16;
+template <int JV>
+__device__ __forceinline__ void add_piece(const float* p, float (&sum)[JV]) {
+  if constexpr (JV == 4) {
+    const float4 v = __ldcg(reinterpret_cast<const float4*>(p));
+    sum[0] += v.x; sum[1] += v.y; sum[2] += v.z; sum[3] += v.w;
+  } else {
+    sum[0] += __ldcg(p);
+  }
+}
+template <typename T, int JV, bool ADD>
 __global__ void __launch_bounds__(kJoinThreads) embed_join_kernel(const EmbedArgs a, int tiles) {
-  const int lane = threadIdx.x & 31;
+  __shared__ int s_fills[kJoinTiles];
+  __shared__ float s_sum[kJoinWarps][32][JV];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   wait_for_previous();
-  const int t0 = blockIdx.x * 32;
-  const int4 st = t0 + lane < tiles ? a.state[t0 + lane] : make_int4(-1, 0, 0, 0);
+  const int t0 = blockIdx.x * kJoinTiles;
+  const int2 st = lane < kJoinTiles && t0 + lane < tiles ? a.state[t0 + lane] : make_int2(-1, 0);
   const unsigned begins = __ballot_sync(kFull, st.y == kBegins);
-  const int groups = (a.d + 31) / 32, pairs = __popc(begins) * groups;
-  for (int p = (threadIdx.x >> 5) + blockIdx.y * (kJoinThreads / 32); p < pairs; p += gridDim.y * (kJoinThreads / 32)) {
-    const int b = __fns(begins, 0, p / groups + 1);
-    const int j = p % groups * 32 + lane, token = __shfl_sync(kFull, st.x, b);
-    const int place = __shfl_sync(kFull, st.z, b);
-    const int first = t0 + b;
-    // the tiles that the token fills
-    int n = 0;
+  if (!begins) return;                               // (the same in every warp)
+  for (int b = warp; b < kJoinTiles; b += kJoinWarps) {
+    if (!(begins >> b & 1u)) continue;
+    int n = 0;                                       // the tiles that the token fills
     for (;;) {
-      const int t = first + 1 + n + lane;
+      const int t = t0 + b + 1 + n + lane;
       const unsigned through = __ballot_sync(kFull, t < tiles && a.state[t].y == kThrough);
-      const int run = through == kFull ? 32 : __ffs(~through) - 1;
+      const int run = through == kFull ? 32 : __ffs((int)~through) - 1;
       n += run;
       if (run < 32) break;
     }
-    if (j >= a.d) continue;
-    float sum = __ldcg(a.tail + (size_t)place * a.d + j);
+    if (lane == 0) s_fills[b] = n;
+  }
+  __syncthreads();
+  const auto sums = [&](int first, int k0, int k1, int n, int j, float (&sum)[JV]) {   // pieces k0 .. k1 of 0 .. n + 1
+#pragma unroll
+    for (int q = 0; q < JV; ++q) sum[q] = 0.f;
 #pragma unroll 8
-    for (int k = 1; k <= n; ++k) sum += __ldcg(a.tail + (size_t)a.state[first + k].z * a.d + j);
-    sum += __ldcg(a.head + (size_t)a.state[first + n + 1].z * a.d + j);
+    for (int k = k0; k < k1; ++k) add_piece<JV>((k <= n ? a.tail : a.head) + (size_t)(first + k) * a.d + j, sum);
+  };
+  const auto write = [&](int token, int j, const float (&sum)[JV]) {
     T* out = static_cast<T*>(a.d_table) + (size_t)token * a.d + j;
-    *out = from_float<T>(ADD ? __fmaf_rn(sum, a.scale, to_float(*out)) : sum * a.scale);
+#pragma unroll
+    for (int q = 0; q < JV; ++q) out[q] = from_float<T>(ADD ? __fmaf_rn(sum[q], a.scale, to_float(out[q])) : sum[q] * a.scale);
+  };
+  const int groups = (a.d + 32 * JV - 1) / (32 * JV), pairs = __popc(begins) * groups;
+  for (int p = warp + blockIdx.y * kJoinWarps; p < pairs; p += gridDim.y * kJoinWarps) {
+    unsigned left = begins;
+    for (int k = p / groups; k > 0; --k) left &= left - 1;
+    const int b = __ffs((int)left) - 1, n = s_fills[b];
+    const int j = (p % groups * 32 + lane) * JV, token = __shfl_sync(kFull, st.x, b);
+    if (n > kLong || j >= a.d) continue;
+    float sum[JV];
+    sums(t0 + b, 0, n + 2, n, j, sum);
+    write(token, j, sum);
+  }
+  for (unsigned m = begins; m; m &= m - 1) {
+    const int b = __ffs((int)m) - 1, n = s_fills[b], token = __shfl_sync(kFull, st.x, b);
+    if (n <= kLong) continue;
+    const int share = (n + 2 + kJoinWarps - 1) / kJoinWarps;
+    for (int g = blockIdx.y; g < groups; g += gridDim.y) {
+      const int j = (g * 32 + lane) * JV;
+      float sum[JV];
+      sums(t0 + b, min(warp * share, n + 2), min((warp + 1) * share, n + 2), n, min(j, a.d - JV), sum);
+#pragma unroll
+      for (int q = 0; q < JV; ++q) s_sum[warp][lane][q] = sum[q];
+      __syncthreads();
+      if (warp == 0 && j < a.d) {
+#pragma unroll
+        for (int q = 0; q < JV; ++q)
+          for (int w = 1; w < kJoinWarps; ++w) sum[q] += s_sum[w][lane][q];
+        write(token, j, sum);
+      }
+      __syncthreads();
+    }
   }
 }
 
 size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 int ceil_div(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
+// Rows of a tile, at least kBatch, for some tiles an SM where there are few rows.
+constexpr int kTiles = 608;
+int slot_count(int R) {
+  int n = kBatch;
+  while (n < kSlots && R > n * kTiles) n *= 2;
+  return n;
+}
 
 }  // namespace
 
@@ -456,11 +533,11 @@ size_t embed_layout(EmbedArgs& a, char* w) {
   }
   if (R > kRankRows)
     for (int p = 0; p < a.passes; ++p) a.count[p] = (int*)take((size_t)ceil_div(R, a.tile) << (a.bits + 2));
-  const int tiles = ceil_div((int64_t)a.V + R, kSlots);
-  a.pieces = R < tiles ? R : tiles;
-  a.state = (int4*)take((size_t)tiles * 16);
-  a.head = (float*)take((size_t)a.pieces * a.d * 4);
-  a.tail = (float*)take((size_t)a.pieces * a.d * 4);
+  a.slots = slot_count(R);
+  const size_t tiles = ceil_div(R, a.slots);
+  a.state = (int2*)take(tiles * 8);
+  a.head = (float*)take(tiles * a.d * 4);
+  a.tail = (float*)take(tiles * a.d * 4);
   return o;
 }
 cudaError_t take_embed_errors(unsigned* flags, cudaStream_t s) { return take_errors(flags, s); }
@@ -482,29 +559,37 @@ cudaError_t launch_embed(const EmbedArgs& a, cudaStream_t s) {
 namespace {
 template <typename T, int VE, bool ADD>
 cudaError_t launch_sums(const EmbedArgs& a, cudaStream_t s) {
-  const int nvec = a.d / VE, tiles = ceil_div(ADD ? (int64_t)a.R : (int64_t)a.V + a.R, kSlots);
+  const int nvec = a.d / VE, tiles = ceil_div(a.R, a.slots);
   const int threads = nvec < kSumThreads ? (nvec + 31) / 32 * 32 : kSumThreads;
-  cudaError_t e = launch(true, embed_sum_kernel<T, VE, ADD>, dim3(tiles, ceil_div(nvec, threads)), threads, 0, s, a,
-                         a.passes - 1);
+  cudaError_t e = launch(true, embed_sum_kernel<T, VE, ADD>, dim3(tiles, ceil_div(nvec, threads)), threads, 0, s, a, a.passes - 1);
   if (e != cudaSuccess) return e;
-  const int groups = ceil_div(a.d, 32);
-  return launch(true, embed_join_kernel<T, ADD>, dim3(ceil_div(tiles, 32), groups < 8 ? 1 : 4), kJoinThreads, 0, s, a, tiles);
+  constexpr int JV = VE * sizeof(T) == 16 ? 4 : 1;
+  const int groups = ceil_div(a.d, 32 * JV);
+  return launch(true, embed_join_kernel<T, JV, ADD>, dim3(ceil_div(tiles, kJoinTiles), groups < 16 ? groups : 16),
+                kJoinThreads, 0, s, a, tiles);
 }
 }  // namespace
 
-cudaError_t launch_embed_backward(const EmbedArgs& a, cudaStream_t s) {
+cudaError_t launch_embed_backward(const EmbedArgs& args, cudaStream_t s) {
+  EmbedArgs a = args;
+  // the k-th of the launches that order the rows fills bytes [fill[k], fill[k + 1])
+  const size_t all = a.add ? 0 : (size_t)a.V * a.d * (a.dtype == 0 ? 4 : 2);
+  const int launches = a.R <= kRankRows ? 1 : a.passes + 1;
+  for (int k = 0; k < launches; ++k) a.fill[k] = all / launches / 16 * 16 * k;
+  a.fill[launches] = all;
+  const auto fill_ctas = [&](int k) { return ceil_div(a.fill[k + 1] - a.fill[k], kFillCta); };
   cudaError_t e;
   if (a.R <= kRankRows) {
     const size_t smem = (size_t)(a.R + 127) / 128 * 512;
-    if (a.R <= 2432) e = launch(false, embed_rank_kernel<1>, ceil_div(a.R, 8), kRankThreads, smem, s, a);
-    else e = launch(false, embed_rank_kernel<4>, ceil_div(a.R, 32), kRankThreads, smem, s, a);
+    const int per = a.R <= 2432 ? 8 : 32, ctas = ceil_div(a.R, per);
+    e = launch(false, per == 8 ? embed_rank_kernel<1> : embed_rank_kernel<4>, ctas + fill_ctas(0), kRankThreads, smem, s, a, ctas);
   } else {
     const int digits = 1 << a.bits, tiles = ceil_div(a.R, a.tile);
     const size_t smem = (size_t)kRadixWarps * digits * 4;
-    e = launch(false, embed_count_kernel, tiles, kRadixThreads, (size_t)digits * 4, s, a, digits);
+    e = launch(false, embed_count_kernel, tiles + fill_ctas(0), kRadixThreads, (size_t)digits * 4, s, a, digits, tiles);
     for (int p = 0; p < a.passes && e == cudaSuccess; ++p)
-      e = p == 0 ? launch(true, embed_move_kernel<true>, tiles, kRadixThreads, smem, s, a, p, a.bits)
-                 : launch(true, embed_move_kernel<false>, tiles, kRadixThreads, smem, s, a, p, a.bits);
+      e = launch(true, p == 0 ? embed_move_kernel<true> : embed_move_kernel<false>, tiles + fill_ctas(p + 1), kRadixThreads, smem,
+                 s, a, p, a.bits, tiles);
   }
   if (e != cudaSuccess) return e;
   return by_row_type(a.dtype, a.d, [&](auto t) {

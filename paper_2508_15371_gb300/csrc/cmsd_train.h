@@ -16,14 +16,15 @@ struct EmbedArgs {
   int dtype, R, d, V, ignore, add;
   float scale;
   int passes, bits, tile;        // radix passes, key bits of each, rows of a tile (backward)
+  int slots;                     // rows of a tile of the sums
+  size_t fill[6];                // borders of the bytes that each launch that orders rows fills with zeros
   // workspace (backward)
   unsigned* err;
   unsigned* key[2];              // [R] the rows' tokens in order (V: padding), where pass p writes: [p & 1]
   int* order[2];                 // [R] the rows
   int* count[4];                 // [tiles of rows][1 << bits] rows of each digit
-  int4* state;                   // [tiles of slots]
-  int pieces;                    // places in head and tail
-  float* head;                   // [pieces][d] pieces of sums that tiles' borders cut
+  int2* state;                   // [tiles of the sums]
+  float* head;                   // [tiles][d] pieces of sums that tiles' borders cut
   float* tail;
 };
 size_t embed_layout(EmbedArgs& a, char* w);
