@@ -5,6 +5,8 @@
 // row's sums and what they give.  Bound by memory.
 #include <cuda_bf16.h>
 
+#include <algorithm>
+
 #include "cmsd_device.cuh"
 #include "cmsd_launch.cuh"
 #include "cmsd_rows.cuh"
@@ -65,15 +67,105 @@ __device__ __forceinline__ void row_sums(float (&v)[N], float* buf) {
     for (int k = 0; k < N; ++k) v[k] += buf[j * N + k];
 }
 
+// ---- numbers of a vector ------------------------------------------------------------------
+// VE numbers in pairs, two an instruction, or one by one where rows begin on odd
+// entries.
+template <int VE>
+struct Num {
+  using N = u64;
+  static constexpr int kN = VE / 2;
+  static __device__ __forceinline__ N all(float x) { return pack2(x, x); }
+  static __device__ __forceinline__ N add(N a, N b) { return add2(a, b); }
+  static __device__ __forceinline__ N mul(N a, N b) { return mul2(a, b); }
+  static __device__ __forceinline__ N fma(N a, N b, N c) { return fma2(a, b, c); }
+  static __device__ __forceinline__ float sum(N a) { return lo32f(a) + hi32f(a); }
+  static __device__ __forceinline__ float first(N a) { return lo32f(a); }
+  static __device__ __forceinline__ N of(const float (&f)[VE], int j) { return pack2(f[2 * j], f[2 * j + 1]); }
+  static __device__ __forceinline__ void to(N a, float* f) { f[0] = lo32f(a); f[1] = hi32f(a); }
+  template <typename T>
+  static __device__ __forceinline__ void get(const typename RowVec<T, VE>::Raw& r, N (&n)[kN]) { get_pairs<T, VE>(r, n); }
+  template <typename T>
+  static __device__ __forceinline__ typename RowVec<T, VE>::Raw put(const N (&n)[kN]) { return put_pairs<T, VE>(n); }
+};
+template <>
+struct Num<1> {
+  using N = float;
+  static constexpr int kN = 1;
+  static __device__ __forceinline__ N all(float x) { return x; }
+  static __device__ __forceinline__ N add(N a, N b) { return a + b; }
+  static __device__ __forceinline__ N mul(N a, N b) { return a * b; }
+  static __device__ __forceinline__ N fma(N a, N b, N c) { return __fmaf_rn(a, b, c); }
+  static __device__ __forceinline__ float sum(N a) { return a; }
+  static __device__ __forceinline__ float first(N a) { return a; }
+  static __device__ __forceinline__ N of(const float (&f)[1], int) { return f[0]; }
+  static __device__ __forceinline__ void to(N a, float* f) { f[0] = a; }
+  template <typename T>
+  static __device__ __forceinline__ void get(const typename RowVec<T, 1>::Raw& r, N (&n)[1]) { RowVec<T, 1>::get(r, n); }
+  template <typename T>
+  static __device__ __forceinline__ typename RowVec<T, 1>::Raw put(const N (&n)[1]) { return RowVec<T, 1>::put(n); }
+};
+
+// ---- rows on their way through shared memory ---------------------------------------------
+// A row is copied as the 16-byte pieces that it touches (the last row's end alone is
+// cut short), so rows that begin anywhere come as fast as aligned ones; those are
+// then read by other threads than copied them, and a barrier stands between.
+template <typename T, int VE>
+__host__ __device__ constexpr bool aligned_rows() { return VE * sizeof(T) == 16; }
+__device__ __forceinline__ void copy_async(uint32_t to, const void* from, int bytes) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void close_copies() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copies_but() {       // all but the last N groups have arrived
+  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
+// row `row` of x [R][d] by threads t of n, kTurns pieces each; in: there is such a row
+template <typename T, int VE, int kTurns>
+__device__ __forceinline__ void request_row(uint32_t to, const void* x, int64_t row, const NormArgs& a, bool in, int t, int n) {
+  const int64_t first = row * a.d * (int64_t)sizeof(T), last = first + a.d * (int64_t)sizeof(T);
+  const int64_t all = (int64_t)a.R * a.d * (int64_t)sizeof(T);
+  const char* p = static_cast<const char*>(x);
+  if constexpr (VE * sizeof(T) == 16) {
+#pragma unroll
+    for (int k = 0; k < kTurns; ++k) {
+      const int64_t at = first + (t + n * k) * 16;
+      const bool here = in && at < last;
+      copy_async(to + (t + n * k) * 16, p + (here ? at : 0), here ? 16 : 0);
+    }
+  } else {
+    const int64_t base = first & ~(int64_t)15;
+#pragma unroll
+    for (int k = 0; k <= kTurns; ++k) {
+      const int c = t + n * k;
+      if (k == kTurns && c > n * kTurns) break;      // (one piece more than an aligned row has)
+      const int64_t at = base + c * 16;
+      if (in && at < last) copy_async(to + c * 16, p + at, (int)(all - at < 16 ? all - at : 16));
+    }
+  }
+}
+// its vector v (VE entries); row's first byte is at `to` + lead
+template <typename T, int VE>
+__device__ __forceinline__ typename RowVec<T, VE>::Raw staged(const char* to, int lead, int v) {
+  return *reinterpret_cast<const typename RowVec<T, VE>::Raw*>(to + lead + v * (int)(VE * sizeof(T)));
+}
+template <typename T, int VE>
+__device__ __forceinline__ int lead_of(int64_t row, int d) {
+  return VE * sizeof(T) == 16 ? 0 : (int)(row * d * (int64_t)sizeof(T) & 15);
+}
+
 // ---- forward ---------------------------------------------------------------------------
 // W warps a row, NV vectors of VE entries a thread.  Sums are of differences from
 // the row's first entry, so that a mean far from zero cancels before anything is
-// rounded, and a row of one number gives exactly bias.
+// rounded, and a row of one number gives exactly bias; what their mean c still
+// lacks, e, comes with the squares.
 template <typename T, int VE, int NV, int W>
 __global__ void __launch_bounds__(W > 8 ? 32 * W : 256) norm_kernel(const NormArgs a) {
   using V = RowVec<T, VE>;
   using Raw = typename V::Raw;
-  __shared__ float s_sum[W > 1 ? 2 * W : 1];
+  using M = Num<VE>;
+  using N = typename M::N;
+  constexpr int kN = M::kN;
+  __shared__ float s_sum[W > 1 ? 3 * W : 1];
   const int nvec = a.d / VE, lane = threadIdx.x & 31, t = W == 1 ? lane : threadIdx.x;
   const int64_t row = W == 1 ? (int64_t)blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5) : blockIdx.x;
   if (row >= a.R) return;                            // (whole warps, and none that a barrier waits for)
@@ -86,50 +178,65 @@ __global__ void __launch_bounds__(W > 8 ? 32 * W : 256) norm_kernel(const NormAr
     if (t + 32 * W * k < nvec) raw[k] = __ldcs(x + t + 32 * W * k);
   }
   const float pilot = to_float(static_cast<const T*>(a.x)[(size_t)row * a.d]);
-  float s[1] = {0.f};
+  // few entries a thread: the parameters' too are requested before the sums
+  constexpr bool kEarly = VE * NV <= 16;
+  float w[kEarly ? NV : 1][VE], b[kEarly ? NV : 1][VE];
+  const auto parameters = [&](int k, int v) {
+    if (a.weight) params<VE>(a.weight, a.wdtype, v * VE, w[k]);
+    if (a.bias) params<VE>(a.bias, a.wdtype, v * VE, b[k]);
+  };
+  if constexpr (kEarly) {
 #pragma unroll
-  for (int k = 0; k < NV; ++k) {
-    float f[VE];
-    V::get(raw[k], f);
-    if (t + 32 * W * k < nvec)
-#pragma unroll
-      for (int j = 0; j < VE; ++j) s[0] += f[j] - pilot;
+    for (int k = 0; k < NV; ++k)
+      if (t + 32 * W * k < nvec) parameters(k, t + 32 * W * k);
   }
-  row_sums<1, W>(s, s_sum);
-  const float c = s[0] / a.d;
-  s[0] = 0.f;
+  N h[NV][kN], n1 = M::all(0.f), n2 = M::all(0.f), p = M::all(-pilot);
 #pragma unroll
   for (int k = 0; k < NV; ++k) {
-    float f[VE];
-    V::get(raw[k], f);
+    M::template get<T>(raw[k], h[k]);
     if (t + 32 * W * k < nvec)
 #pragma unroll
-      for (int j = 0; j < VE; ++j) {
-        const float h = (f[j] - pilot) - c;
-        s[0] = __fmaf_rn(h, h, s[0]);
+      for (int j = 0; j < kN; ++j) {
+        h[k][j] = M::add(h[k][j], p);
+        n1 = M::add(n1, h[k][j]);
       }
   }
-  row_sums<1, W>(s, s_sum + W);
-  const float rstd = 1.f / sqrtf(s[0] / a.d + a.eps);
+  float s[1] = {M::sum(n1)};
+  row_sums<1, W>(s, s_sum);
+  const float c = s[0] / a.d;
+  p = M::all(-c);
+  n1 = M::all(0.f);
+#pragma unroll
+  for (int k = 0; k < NV; ++k)
+    if (t + 32 * W * k < nvec)
+#pragma unroll
+      for (int j = 0; j < kN; ++j) {
+        h[k][j] = M::add(h[k][j], p);
+        n1 = M::add(n1, h[k][j]);
+        n2 = M::fma(h[k][j], h[k][j], n2);
+      }
+  float q[2] = {M::sum(n1), M::sum(n2)};
+  row_sums<2, W>(q, s_sum + W);
+  const float e = q[0] / a.d, rstd = 1.f / sqrtf((q[1] / a.d - e * e) + a.eps);
   if (t == 0) {
-    if (a.mean) a.mean[row] = pilot + c;
+    if (a.mean) a.mean[row] = pilot + (c + e);
     if (a.rstd) a.rstd[row] = rstd;
   }
+  const N scale = M::all(rstd), shift = M::all(-e * rstd);
 #pragma unroll
   for (int k = 0; k < NV; ++k) {
     const int v = t + 32 * W * k;
     if (v >= nvec) continue;
-    float f[VE], w[VE], b[VE];
-    V::get(raw[k], f);
-    if (a.weight) params<VE>(a.weight, a.wdtype, v * VE, w);
-    if (a.bias) params<VE>(a.bias, a.wdtype, v * VE, b);
+    const int q = kEarly ? k : 0;
+    if (!kEarly) parameters(q, v);
 #pragma unroll
-    for (int j = 0; j < VE; ++j) {
-      f[j] = ((f[j] - pilot) - c) * rstd;
-      if (a.weight) f[j] *= w[j];
-      if (a.bias) f[j] += b[j];
+    for (int j = 0; j < kN; ++j) {
+      h[k][j] = M::fma(h[k][j], scale, shift);
+      if (a.weight && a.bias) h[k][j] = M::fma(h[k][j], M::of(w[q], j), M::of(b[q], j));
+      else if (a.weight) h[k][j] = M::mul(h[k][j], M::of(w[q], j));
+      else if (a.bias) h[k][j] = M::add(h[k][j], M::of(b[q], j));
     }
-    y[v] = V::put(f);
+    y[v] = M::template put<T>(h[k]);
   }
 }
 
@@ -137,7 +244,7 @@ __global__ void __launch_bounds__(W > 8 ? 32 * W : 256) norm_kernel(const NormAr
 constexpr int kWide = 1024;
 template <typename T>
 __global__ void __launch_bounds__(kWide) norm_wide_kernel(const NormArgs a) {
-  __shared__ float s_sum[2 * kWide / 32];
+  __shared__ float s_sum[3 * kWide / 32];
   const T* x = static_cast<const T*>(a.x) + (size_t)blockIdx.x * a.d;
   T* y = static_cast<T*>(a.y) + (size_t)blockIdx.x * a.d;
   const float pilot = to_float(x[0]);
@@ -145,167 +252,331 @@ __global__ void __launch_bounds__(kWide) norm_wide_kernel(const NormArgs a) {
   for (int j = threadIdx.x; j < a.d; j += kWide) s[0] += to_float(x[j]) - pilot;
   row_sums<1, kWide / 32>(s, s_sum);
   const float c = s[0] / a.d;
-  s[0] = 0.f;
+  float q[2] = {0.f, 0.f};
   for (int j = threadIdx.x; j < a.d; j += kWide) {
     const float h = (to_float(x[j]) - pilot) - c;
-    s[0] = __fmaf_rn(h, h, s[0]);
+    q[0] += h;
+    q[1] = __fmaf_rn(h, h, q[1]);
   }
-  row_sums<1, kWide / 32>(s, s_sum + kWide / 32);
-  const float rstd = 1.f / sqrtf(s[0] / a.d + a.eps);
+  row_sums<2, kWide / 32>(q, s_sum + kWide / 32);
+  const float e = q[0] / a.d, rstd = 1.f / sqrtf((q[1] / a.d - e * e) + a.eps);
   if (threadIdx.x == 0) {
-    if (a.mean) a.mean[blockIdx.x] = pilot + c;
+    if (a.mean) a.mean[blockIdx.x] = pilot + (c + e);
     if (a.rstd) a.rstd[blockIdx.x] = rstd;
   }
   for (int j = threadIdx.x; j < a.d; j += kWide) {
-    float h = ((to_float(x[j]) - pilot) - c) * rstd;
+    float h = (((to_float(x[j]) - pilot) - c) - e) * rstd;
     if (a.weight) h *= param(a.weight, a.wdtype, j);
     if (a.bias) h += param(a.bias, a.wdtype, j);
     y[j] = from_float<T>(h);
   }
 }
 
-// ---- gradients ---------------------------------------------------------------------------
-// A thread has the same eight columns in all of its rows and keeps their two sums
-// over rows in registers; W warps a row, kGroups rows at a time in a CTA, rows_at_once
-// of them requested together.  The CTAs' sums (kParts of them at most) are joined by
-// norm_join_kernel, in the order of the CTAs.
-constexpr int kCols = 8;                             // columns of a thread
-__host__ __device__ constexpr int rows_at_once(int w) { return w > 16 ? 1 : 2; }
-constexpr int kParts = 456;
+// ---- many rows -----------------------------------------------------------------------------
+// A grid that stays: a thread has the same columns in all of its rows, with their
+// parameters (forward) or their sums over rows (gradients) in registers; W warps a
+// row, kGroups * kRows rows of a CTA at a time.  Rows come through a ring in shared
+// memory.
+constexpr int kSms = 152;
+__host__ __device__ constexpr int cta_threads(int w) { return w > 8 ? 32 * w : 256; }
+__host__ __device__ constexpr int cta_groups(int w) { return cta_threads(w) / (32 * w); }
+__host__ __device__ constexpr int staged_bytes(int w, int cols, int size) { return 32 * w * cols * size + 16; }     // of a row
+// a barrier of the W warps of a row (the CTA's groups go their own ways)
+template <int W>
+__device__ __forceinline__ void group_sync(int group) {
+  if (W == 1) __syncwarp();
+  else asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "n"(32 * W) : "memory");
+}
+// the sums of N numbers over a group's warps, in every thread; buf: [N][W], not in use by another exchange between
+// whose barrier and this one's there is none
+template <int N, int W>
+__device__ __forceinline__ void group_sums(float (&v)[N], float* buf, int group) {
+#pragma unroll
+  for (int o = 16; o; o >>= 1)
+#pragma unroll
+    for (int k = 0; k < N; ++k) v[k] += __shfl_xor_sync(kFull, v[k], o);
+  if (W == 1) return;
+  if ((threadIdx.x & 31) == 0)
+#pragma unroll
+    for (int k = 0; k < N; ++k) buf[k * W + (threadIdx.x >> 5) % W] = v[k];
+  group_sync<W>(group);
+#pragma unroll
+  for (int k = 0; k < N; ++k) {
+    v[k] = 0.f;
+    if constexpr (W % 4 == 0) {
+#pragma unroll
+      for (int j = 0; j < W; j += 4) {
+        const float4 p = *reinterpret_cast<const float4*>(buf + k * W + j);
+        v[k] += (p.x + p.y) + (p.z + p.w);
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < W; ++j) v[k] += buf[k * W + j];
+    }
+  }
+}
+
+// whether a thread's vector k is in the row: a row that takes W > 1 warps fills half of what they hold
+template <int W, int NV>
+__device__ __forceinline__ bool in_row(int t, int k, int nvec) {
+  return (W > 1 && 2 * (k + 1) <= NV) || t + 32 * W * k < nvec;
+}
+
+constexpr int kCols = 16;                            // columns of a thread
+constexpr int kNormRows = 1;
+constexpr int kNormStages = 3;
+constexpr int kNormCtas = 3;                         // an SM, by registers
 template <typename T, int VE, int W>
-__global__ void __launch_bounds__(W > 8 ? 32 * W : 256, W > 8 ? 1 : 3) norm_backward_kernel(const NormArgs a) {
-  using V = RowVec<T, VE>;
-  using Raw = typename V::Raw;
-  constexpr int NV = kCols / VE, kGroups = W > 8 ? 1 : 8 / W, kRows = rows_at_once(W);
-  __shared__ float s_sum[W > 1 ? 2 * kGroups * W * 2 * kRows : 1];
+__global__ void __launch_bounds__(cta_threads(W), kNormCtas) norm_many_kernel(const NormArgs a) {
+  using Raw = typename RowVec<T, VE>::Raw;
+  using M = Num<VE>;
+  using N = typename M::N;
+  constexpr int kN = M::kN, NV = kCols / VE, kGroups = cta_groups(W), kRows = kNormRows;
+  constexpr int kRowBytes = staged_bytes(W, kCols, sizeof(T)), kTurns = kCols * sizeof(T) / 16;
+  extern __shared__ uint4 s_ring4[];
+  __shared__ __align__(16) float s_sum[W > 1 ? 2 * kGroups * kRows * W : 1];
   const int nvec = a.d / VE, t = threadIdx.x % (32 * W), group = threadIdx.x / (32 * W);
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  float w[NV][VE], dw[NV][VE], db[NV][VE];
+  const int64_t first = (int64_t)blockIdx.x * kGroups * kRows + group, step = (int64_t)gridDim.x * kGroups * kRows;
+  char* ring = reinterpret_cast<char*>(s_ring4) + group * kNormStages * kRows * kRowBytes;       // [kNormStages][kRows]
+  const uint32_t ring_at = (uint32_t)__cvta_generic_to_shared(ring);
+  float* sums = s_sum + (W > 1 ? 2 * group * kRows * W : 0);
+  const auto request = [&](int64_t r0, int stage) {
+#pragma unroll
+    for (int u = 0; u < kRows; ++u) {
+      const int64_t row = r0 + u * kGroups;
+      request_row<T, VE, kTurns>(ring_at + (stage * kRows + u) * kRowBytes, a.x, row, a, row < a.R, t, 32 * W);
+    }
+    close_copies();
+  };
+#pragma unroll
+  for (int k = 0; k < kNormStages - 1; ++k) request(first + k * step, k);
+  N w[NV][kN], b[NV][kN];
 #pragma unroll
   for (int k = 0; k < NV; ++k) {
+    float f[VE], h[VE];
 #pragma unroll
     for (int j = 0; j < VE; ++j) {
-      w[k][j] = 1.f;
-      dw[k][j] = db[k][j] = 0.f;
+      f[j] = 1.f;
+      h[j] = 0.f;
     }
-    if (a.weight && t + 32 * W * k < nvec) params<VE>(a.weight, a.wdtype, (t + 32 * W * k) * VE, w[k]);
+    if (in_row<W, NV>(t, k, nvec)) {
+      if (a.weight) params<VE>(a.weight, a.wdtype, (t + 32 * W * k) * VE, f);
+      if (a.bias) params<VE>(a.bias, a.wdtype, (t + 32 * W * k) * VE, h);
+    }
+#pragma unroll
+    for (int j = 0; j < kN; ++j) {
+      w[k][j] = M::of(f, j);
+      b[k][j] = M::of(h, j);
+    }
   }
   const float over_d = 1.f / a.d;
-  int turn = 0;
-  const int64_t step = (int64_t)gridDim.x * kGroups * kRows;
-  for (int64_t r0 = ((int64_t)blockIdx.x * kGroups) * kRows; r0 < a.R; r0 += step, turn ^= 1) {
-    Raw xr[kRows][NV], gr[kRows][NV];
-    float mean[kRows], rstd[kRows], s[2 * kRows];
+  int stage = 0;
+  for (int64_t r0 = first; r0 < a.R; r0 += step) {
+    copies_but<kNormStages - 2>();
+    group_sync<W>(group);                             // (the first entry is another thread's copy, if no more is)
+    request(r0 + (kNormStages - 1) * step, stage == 0 ? kNormStages - 1 : stage - 1);
+    N h[kRows][NV][kN];
+    float pilot[kRows], s[kRows], q[kRows];
 #pragma unroll
     for (int u = 0; u < kRows; ++u) {
-      const int64_t row = r0 + u * kGroups + group;
-      const bool in = row < a.R;
-      mean[u] = in ? __ldg(a.mean_in + row) : 0.f;
-      rstd[u] = in ? __ldg(a.rstd_in + row) : 0.f;
+      const char* from = ring + (stage * kRows + u) * kRowBytes;
+      const int lead = lead_of<T, VE>(r0 + u * kGroups, a.d);
+      pilot[u] = to_float(*reinterpret_cast<const T*>(from + lead));
+      const N p = M::all(-pilot[u]);
+      N sum = M::all(0.f);
 #pragma unroll
-      for (int k = 0; k < NV; ++k) {
-        const int v = t + 32 * W * k;
-        xr[u][k] = gr[u][k] = V::zero();
-        if (in && v < nvec) {
-          xr[u][k] = __ldcs(static_cast<const Raw*>(a.x) + (size_t)row * nvec + v);
-          gr[u][k] = __ldcs(static_cast<const Raw*>(a.d_y) + (size_t)row * nvec + v);
+      for (int k = 0; k < NV; ++k)
+        if (in_row<W, NV>(t, k, nvec)) {
+          M::template get<T>(staged<T, VE>(from, lead, t + 32 * W * k), h[u][k]);
+#pragma unroll
+          for (int j = 0; j < kN; ++j) {
+            h[u][k][j] = M::add(h[u][k][j], p);
+            sum = M::add(sum, h[u][k][j]);
+          }
         }
-      }
+      s[u] = M::sum(sum);
     }
+    stage = stage + 1 == kNormStages ? 0 : stage + 1;
+    group_sums<kRows, W>(s, sums, group);
 #pragma unroll
     for (int u = 0; u < kRows; ++u) {
-      s[2 * u] = s[2 * u + 1] = 0.f;
-      const bool in = r0 + u * kGroups + group < a.R;
+      s[u] *= over_d;
+      const N p = M::all(-s[u]);
+      N sum = M::all(0.f);
 #pragma unroll
-      for (int k = 0; k < NV; ++k) {
-        float x[VE], g[VE];
-        V::get(xr[u][k], x);
-        V::get(gr[u][k], g);
-        if (in && t + 32 * W * k < nvec)
+      for (int k = 0; k < NV; ++k)
+        if (in_row<W, NV>(t, k, nvec))
 #pragma unroll
-          for (int j = 0; j < VE; ++j) {
-            const float h = (x[j] - mean[u]) * rstd[u], gw = g[j] * w[k][j];
-            dw[k][j] = __fmaf_rn(g[j], h, dw[k][j]);
-            db[k][j] += g[j];
-            s[2 * u] += gw;
-            s[2 * u + 1] = __fmaf_rn(gw, h, s[2 * u + 1]);
+          for (int j = 0; j < kN; ++j) {
+            h[u][k][j] = M::add(h[u][k][j], p);
+            sum = M::fma(h[u][k][j], h[u][k][j], sum);
           }
-      }
+      q[u] = M::sum(sum);
     }
-    if (a.d_x) {                                      // (the same in the whole grid)
-      row_sums<2 * kRows, W>(s, s_sum + (W > 1 ? (turn * kGroups + group) * W * 2 * kRows : 0));
+    group_sums<kRows, W>(q, sums + kRows * W, group);
 #pragma unroll
-      for (int u = 0; u < kRows; ++u) {
-        const int64_t row = r0 + u * kGroups + group;
-        const float m1 = s[2 * u] * over_d, m2 = s[2 * u + 1] * over_d;
-#pragma unroll
-        for (int k = 0; k < NV; ++k) {
-          const int v = t + 32 * W * k;
-          if (row >= a.R || v >= nvec) continue;
-          float x[VE], g[VE];
-          V::get(xr[u][k], x);
-          V::get(gr[u][k], g);
-#pragma unroll
-          for (int j = 0; j < VE; ++j) {
-            const float h = (x[j] - mean[u]) * rstd[u];
-            g[j] = rstd[u] * ((g[j] * w[k][j] - m1) - h * m2);
-          }
-          static_cast<Raw*>(a.d_x)[(size_t)row * nvec + v] = V::put(g);
-        }
+    for (int u = 0; u < kRows; ++u) {
+      const int64_t row = r0 + u * kGroups;
+      if (row >= a.R) continue;
+      const float rstd = 1.f / sqrtf(q[u] * over_d + a.eps);
+      if (t == 0) {
+        if (a.mean) a.mean[row] = pilot[u] + s[u];
+        if (a.rstd) a.rstd[row] = rstd;
       }
+      const N scale = M::all(rstd);
+      Raw* y = static_cast<Raw*>(a.y) + (size_t)row * nvec;
+#pragma unroll
+      for (int k = 0; k < NV; ++k)
+        if (in_row<W, NV>(t, k, nvec)) {
+#pragma unroll
+          for (int j = 0; j < kN; ++j) h[u][k][j] = M::fma(M::mul(h[u][k][j], scale), w[k][j], b[k][j]);
+          y[t + 32 * W * k] = M::template put<T>(h[u][k]);
+        }
     }
   }
+  copies_but<0>();
+}
+
+// ---- gradients ---------------------------------------------------------------------------
+// The CTAs' sums over rows are joined by norm_join_kernel, in the order of the CTAs.
+__host__ __device__ constexpr int grad_stages(int size) { return size == 2 ? 3 : 2; }
+__host__ __device__ constexpr int grad_smem(int w, int size) { return grad_stages(size) * 2 * cta_groups(w) * staged_bytes(w, kCols, size); }
+__host__ __device__ constexpr int grad_ctas(int w) { return w > 8 ? 1 : 2; }       // an SM, by registers
+template <typename T, int VE, int W>
+__global__ void __launch_bounds__(cta_threads(W), grad_ctas(W)) norm_backward_kernel(const NormArgs a) {
+  using Raw = typename RowVec<T, VE>::Raw;
+  using M = Num<VE>;
+  using N = typename M::N;
+  constexpr int kN = M::kN, NV = kCols / VE, kGroups = cta_groups(W), kThreads = cta_threads(W);
+  constexpr int kStages = grad_stages(sizeof(T)), kRowBytes = staged_bytes(W, kCols, sizeof(T)), kTurns = kCols * sizeof(T) / 16;
+  extern __shared__ uint4 s_ring4[];
+  __shared__ __align__(16) float s_sum[W > 1 ? 2 * kGroups * 2 * W : 1];
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  const int nvec = a.d / VE, t = threadIdx.x % (32 * W), group = threadIdx.x / (32 * W);
+  const int64_t first = (int64_t)blockIdx.x * kGroups + group, step = (int64_t)gridDim.x * kGroups;
+  char* ring = reinterpret_cast<char*>(s_ring4) + group * kStages * 2 * kRowBytes;             // [kStages][2]
+  const uint32_t ring_at = (uint32_t)__cvta_generic_to_shared(ring);
+  const auto request = [&](int64_t row, int stage) {
+    const uint32_t to = ring_at + stage * 2 * kRowBytes;
+    request_row<T, VE, kTurns>(to, a.x, row, a, row < a.R, t, 32 * W);
+    request_row<T, VE, kTurns>(to + kRowBytes, a.d_y, row, a, row < a.R, t, 32 * W);
+    close_copies();
+  };
+#pragma unroll
+  for (int k = 0; k < kStages - 1; ++k) request(first + k * step, k);
+  float mean = first < a.R ? __ldg(a.mean_in + first) : 0.f, rstd = first < a.R ? __ldg(a.rstd_in + first) : 0.f;
+  N w[NV][kN], dw[NV][kN], db[NV][kN];
+#pragma unroll
+  for (int k = 0; k < NV; ++k) {
+    float f[VE];
+#pragma unroll
+    for (int j = 0; j < VE; ++j) f[j] = 1.f;
+    if (a.weight && in_row<W, NV>(t, k, nvec)) params<VE>(a.weight, a.wdtype, (t + 32 * W * k) * VE, f);
+#pragma unroll
+    for (int j = 0; j < kN; ++j) {
+      w[k][j] = M::of(f, j);
+      dw[k][j] = db[k][j] = M::all(0.f);
+    }
+  }
+  const float over_d = 1.f / a.d;
+  int stage = 0, turn = 0;
+  for (int64_t row = first; row < a.R; row += step, turn ^= 1) {
+    copies_but<kStages - 2>();
+    if (!aligned_rows<T, VE>()) group_sync<W>(group);
+    request(row + (kStages - 1) * step, stage == 0 ? kStages - 1 : stage - 1);
+    const char* from = ring + stage * 2 * kRowBytes;
+    const int lead = lead_of<T, VE>(row, a.d);
+    stage = stage + 1 == kStages ? 0 : stage + 1;
+    const N m = M::all(-mean), rs = M::all(rstd);
+    if (row + step < a.R) {
+      mean = __ldg(a.mean_in + row + step);
+      rstd = __ldg(a.rstd_in + row + step);
+    }
+    N h[NV][kN], g[NV][kN], s1 = M::all(0.f), s2 = M::all(0.f);
+#pragma unroll
+    for (int k = 0; k < NV; ++k)
+      if (in_row<W, NV>(t, k, nvec)) {
+        M::template get<T>(staged<T, VE>(from, lead, t + 32 * W * k), h[k]);
+        M::template get<T>(staged<T, VE>(from + kRowBytes, lead, t + 32 * W * k), g[k]);
+#pragma unroll
+        for (int j = 0; j < kN; ++j) {
+          h[k][j] = M::mul(M::add(h[k][j], m), rs);
+          dw[k][j] = M::fma(g[k][j], h[k][j], dw[k][j]);
+          db[k][j] = M::add(db[k][j], g[k][j]);
+          g[k][j] = M::mul(g[k][j], w[k][j]);
+          s1 = M::add(s1, g[k][j]);
+          s2 = M::fma(g[k][j], h[k][j], s2);
+        }
+      }
+    if (!a.d_x) continue;                             // (the same in the whole grid)
+    float s[2] = {M::sum(s1), M::sum(s2)};
+    group_sums<2, W>(s, s_sum + (W > 1 ? (turn * kGroups + group) * 2 * W : 0), group);
+    const N m1 = M::all(-s[0] * over_d), m2 = M::all(-s[1] * over_d);
+    Raw* d_x = static_cast<Raw*>(a.d_x) + (size_t)row * nvec;
+#pragma unroll
+    for (int k = 0; k < NV; ++k)
+      if (in_row<W, NV>(t, k, nvec)) {
+#pragma unroll
+        for (int j = 0; j < kN; ++j) g[k][j] = M::mul(rs, M::fma(h[k][j], m2, M::add(g[k][j], m1)));
+        d_x[t + 32 * W * k] = M::template put<T>(g[k]);
+      }
+  }
+  copies_but<0>();
   if (!a.d_weight && !a.d_bias) return;
-  // the groups' sums, in their order
-  __shared__ float s_col[kGroups > 1 ? 256 * kCols : 1];
+  // the groups' sums, in their order, through the ring's memory
+  float* s_col = reinterpret_cast<float*>(s_ring4);
   float* part = a.part + (size_t)blockIdx.x * 2 * a.d;
 #pragma unroll
   for (int which = 0; which < 2; ++which) {
+    float sum[NV][VE];
+#pragma unroll
+    for (int k = 0; k < NV; ++k)
+#pragma unroll
+      for (int j = 0; j < kN; ++j) M::to(which ? db[k][j] : dw[k][j], &sum[k][VE / kN * j]);
     if (kGroups > 1) {
       __syncthreads();
 #pragma unroll
       for (int k = 0; k < NV; ++k)
 #pragma unroll
-        for (int j = 0; j < VE; ++j)
-          s_col[(group * kCols + k * VE + j) * 32 * W + t] = which ? db[k][j] : dw[k][j];
+        for (int j = 0; j < VE; ++j) s_col[(k * VE + j) * kThreads + threadIdx.x] = sum[k][j];
       __syncthreads();
     }
-    if (group == 0)
+    if (group == 0) {
 #pragma unroll
       for (int k = 0; k < NV; ++k)
-        if (t + 32 * W * k < nvec)
+        if (in_row<W, NV>(t, k, nvec))
 #pragma unroll
           for (int j = 0; j < VE; ++j) {
-            float v = which ? db[k][j] : dw[k][j];
-            if (kGroups > 1)
-              for (int q = 1; q < kGroups; ++q) v += s_col[(q * kCols + k * VE + j) * 32 * W + t];
-            part[which * a.d + (t + 32 * W * k) * VE + j] = v;
+            for (int q = 1; q < kGroups; ++q) sum[k][j] += s_col[(k * VE + j) * kThreads + 32 * W * q + t];
+            part[which * a.d + (t + 32 * W * k) * VE + j] = sum[k][j];
           }
+    }
   }
 }
 
-// a CTA 32 columns of one of the two, a warp every eighth of the parts
-__global__ void __launch_bounds__(256) norm_join_kernel(const NormArgs a, int parts) {
-  __shared__ float s_part[8][32];
-  const int j = blockIdx.x * 32 + (threadIdx.x & 31), which = blockIdx.y, warp = threadIdx.x >> 5;
+// a CTA 32 columns of one of the two, each of its warps a part of the CTAs' sums
+constexpr int kJoinWarps = 32;
+__global__ void __launch_bounds__(32 * kJoinWarps) norm_join_kernel(const NormArgs a, int parts) {
+  __shared__ float s_part[kJoinWarps][32];
+  const int lane = threadIdx.x & 31, j = blockIdx.x * 32 + lane, which = blockIdx.y, warp = threadIdx.x >> 5;
   void* out = which ? a.d_bias : a.d_weight;
   asm volatile("griddepcontrol.wait;" ::: "memory");
   if (!out) return;
   float v = 0.f;
   if (j < a.d)
 #pragma unroll 8
-    for (int p = warp; p < parts; p += 8) v += __ldcg(a.part + ((size_t)p * 2 + which) * a.d + j);
-  s_part[warp][threadIdx.x & 31] = v;
+    for (int p = warp; p < parts; p += kJoinWarps) v += __ldcg(a.part + ((size_t)p * 2 + which) * a.d + j);
+  s_part[warp][lane] = v;
   __syncthreads();
   if (warp || j >= a.d) return;
 #pragma unroll
-  for (int k = 1; k < 8; ++k) v += s_part[k][threadIdx.x];
+  for (int k = 1; k < kJoinWarps; ++k) v += s_part[k][lane];
   if (a.wdtype == 0) static_cast<float*>(out)[j] = v;
   else static_cast<__nv_bfloat16*>(out)[j] = __float2bfloat16_rn(v);
 }
 
-// rows of over kWideCols columns: d_x by a CTA a row, the sums over rows by a CTA 32 columns
 constexpr int kWideCols = 8192;
+// rows of over kWideCols columns: d_x by a CTA a row, the sums over rows by a CTA 32 columns
 template <typename T>
 __global__ void __launch_bounds__(kWide) norm_wide_dx_kernel(const NormArgs a) {
   __shared__ float s_sum[2 * kWide / 32];
@@ -354,7 +625,7 @@ __global__ void __launch_bounds__(256) norm_wide_sums_kernel(const NormArgs a) {
 }
 
 int ceil_div(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
-// warps of a row in norm_backward_kernel: kCols columns a thread
+// warps of a row, a thread kCols columns of it
 int row_warps(int d) {
   int w = 1;
   while (w * 32 * kCols < d) w *= 2;
@@ -363,46 +634,60 @@ int row_warps(int d) {
 // CTAs whose sums over rows are joined, by R and d alone
 int part_count(int R, int d) {
   if (d > kWideCols) return R < 64 * 8 ? ceil_div(R, 8) : 64;
-  const int w = row_warps(d), at_once = (w > 8 ? 1 : 8 / w) * rows_at_once(w), most = w > 16 ? kParts / 3 : (w > 8 ? kParts / 3 * 2 : kParts);
-  const int n = ceil_div(R, at_once);
-  return n < most ? n : most;
+  const int w = row_warps(d), n = ceil_div(R, cta_groups(w));
+  return std::min(n, kSms * grad_ctas(w));
 }
 
+constexpr int kFewRows = 608;
+template <typename T, int VE, int W>
+cudaError_t launch_many(const NormArgs& a, cudaStream_t s) {
+  constexpr int smem = kNormStages * kNormRows * cta_groups(W) * staged_bytes(W, kCols, sizeof(T));
+  const auto kernel = norm_many_kernel<T, VE, W>;
+  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  if (e != cudaSuccess) return e;
+  kernel<<<std::min(ceil_div(a.R, cta_groups(W) * kNormRows), kSms * kNormCtas), cta_threads(W), smem, s>>>(a);
+  return cudaGetLastError();
+}
 template <typename T, int VE>
 cudaError_t launch_rows(const NormArgs& a, cudaStream_t s) {
-  const auto one = [&](auto kernel) {
-    // a warp a CTA until every SM has two, then four
-    const int warps = a.R <= 304 ? 1 : 4;
-    kernel<<<ceil_div(a.R, warps), 32 * warps, 0, s>>>(a);
-    return cudaGetLastError();
-  };
-  const auto many = [&](auto kernel, int threads) {
+  const auto few = [&](auto kernel, int threads) {   // a CTA a row
     kernel<<<a.R, threads, 0, s>>>(a);
     return cudaGetLastError();
   };
-  if (a.d <= 256) return one(norm_kernel<T, VE, 8 / VE, 1>);
-  if (a.d <= 512) return one(norm_kernel<T, VE, 16 / VE, 1>);
-  if (a.d <= 1024) return one(norm_kernel<T, VE, 32 / VE, 1>);
-  if (a.d <= 2048) return one(norm_kernel<T, VE, 64 / VE, 1>);
-  if (a.d <= 4096) return many(norm_kernel<T, VE, 16 / VE, 8>, 256);
-  if (a.d <= 8192) return many(norm_kernel<T, VE, 32 / VE, 8>, 256);
-  if (a.d <= 32768) return many(norm_kernel<T, VE, 32 / VE, 32>, 1024);
-  return many(norm_wide_kernel<T>, kWide);
+  if (a.R > kFewRows && a.d <= 4096) switch (row_warps(a.d)) {
+      case 1: return launch_many<T, VE, 1>(a, s);
+      case 2: return launch_many<T, VE, 2>(a, s);
+      case 4: return launch_many<T, VE, 4>(a, s);
+      default: return launch_many<T, VE, 8>(a, s);
+    }
+  if (a.d <= 256) return few(norm_kernel<T, VE, 8 / VE, 1>, 32);
+  if (a.d <= 2048) return few(norm_kernel<T, VE, 8 / VE, 8>, 256);
+  if (a.d <= 4096) return few(norm_kernel<T, VE, 16 / VE, 8>, 256);
+  if (a.d <= 8192) return few(norm_kernel<T, VE, 32 / VE, 8>, 256);
+  if (a.d <= 32768) return few(norm_kernel<T, VE, 32 / VE, 32>, 1024);
+  return few(norm_wide_kernel<T>, kWide);
 }
 
+template <typename T, int VE, int W>
+cudaError_t launch_gradients(const NormArgs& a, int parts, cudaStream_t s) {
+  constexpr int smem = grad_smem(W, sizeof(T));
+  static_assert(smem >= kCols * 4 * cta_threads(W) || W > 8, "the groups' sums pass through the ring");
+  const auto kernel = norm_backward_kernel<T, VE, W>;
+  if (smem > 48 * 1024) {
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    if (e != cudaSuccess) return e;
+  }
+  kernel<<<parts, cta_threads(W), smem, s>>>(a);
+  return cudaGetLastError();
+}
 template <typename T, int VE>
 cudaError_t launch_gradients(const NormArgs& a, int parts, cudaStream_t s) {
-  const auto go = [&](auto kernel, int threads) {
-    kernel<<<parts, threads, 0, s>>>(a);
-    return cudaGetLastError();
-  };
   switch (row_warps(a.d)) {
-    case 1: return go(norm_backward_kernel<T, VE, 1>, 256);
-    case 2: return go(norm_backward_kernel<T, VE, 2>, 256);
-    case 4: return go(norm_backward_kernel<T, VE, 4>, 256);
-    case 8: return go(norm_backward_kernel<T, VE, 8>, 256);
-    case 16: return go(norm_backward_kernel<T, VE, 16>, 512);
-    default: return go(norm_backward_kernel<T, VE, 32>, 1024);
+    case 1: return launch_gradients<T, VE, 1>(a, parts, s);
+    case 2: return launch_gradients<T, VE, 2>(a, parts, s);
+    case 4: return launch_gradients<T, VE, 4>(a, parts, s);
+    case 8: return launch_gradients<T, VE, 8>(a, parts, s);
+    default: return launch_gradients<T, VE, 16>(a, parts, s);
   }
 }
 template <typename T>
@@ -434,7 +719,7 @@ cudaError_t launch_norm_backward(const NormArgs& a, cudaStream_t s) {
       return launch_gradients<typename decltype(t)::T, decltype(t)::VE>(a, parts, s);
     });
   if (e != cudaSuccess || (!a.d_weight && !a.d_bias)) return e;
-  return launch(true, norm_join_kernel, dim3(ceil_div(a.d, 32), 2), 256, 0, s, a, parts);
+  return launch(true, norm_join_kernel, dim3(ceil_div(a.d, 32), 2), 32 * kJoinWarps, 0, s, a, parts);
 }
 
 }  // namespace cmsd

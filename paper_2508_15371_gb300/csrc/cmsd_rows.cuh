@@ -75,6 +75,29 @@ struct RowVec<__nv_bfloat16, 1> {
   static __device__ __forceinline__ void get(const Raw& r, float (&f)[1]) { f[0] = __uint_as_float((uint32_t)r << 16); }
   static __device__ __forceinline__ Raw put(const float (&f)[1]) { return (uint16_t)pack_bf16(f[0], 0.f); }
 };
+// VE entries (an even number) as pairs for the packed fp32 instructions
+template <typename T, int VE>
+__device__ __forceinline__ void get_pairs(const typename RowVec<T, VE>::Raw& r, u64 (&p)[VE / 2]) {
+  if constexpr (sizeof(T) == 2 && VE == 8) {
+    p[0] = bf2_to_f2(r.x); p[1] = bf2_to_f2(r.y); p[2] = bf2_to_f2(r.z); p[3] = bf2_to_f2(r.w);
+  } else {
+    float f[VE];
+    RowVec<T, VE>::get(r, f);
+#pragma unroll
+    for (int j = 0; j < VE / 2; ++j) p[j] = pack2(f[2 * j], f[2 * j + 1]);
+  }
+}
+template <typename T, int VE>
+__device__ __forceinline__ typename RowVec<T, VE>::Raw put_pairs(const u64 (&p)[VE / 2]) {
+  float f[VE];
+#pragma unroll
+  for (int j = 0; j < VE / 2; ++j) {
+    f[2 * j] = lo32f(p[j]);
+    f[2 * j + 1] = hi32f(p[j]);
+  }
+  return RowVec<T, VE>::put(f);
+}
+
 // f(RowType<T, VE>) with the widest vectors that every row of d entries begins on
 template <typename T_, int VE_>
 struct RowType {
