@@ -524,21 +524,35 @@ def _code(t, name):
     raise CmsdError(f"{name} must be float32 or bfloat16, got {t.dtype}")
 
 
-def _not_recorded(what, *ts):
-    if _torch_mod.is_grad_enabled():
-        for t in ts:
-            if t is not None and t.requires_grad:
-                raise CmsdError(f"{what} records nothing for autograd: call it under torch.no_grad() (or from an "
-                                f"autograd.Function) and take the gradients from {what}_backward")
+def _not_recorded(what):
+    raise CmsdError(f"{what} records nothing for autograd: call it under torch.no_grad() (or from an "
+                    f"autograd.Function) and take the gradients from {what}_backward")
 
 
 def _rows(t, name):
-    if t.dim() != 2:
-        raise CmsdError(f"{name} must have two dimensions, got {tuple(t.shape)}")
-    n, d = t.shape
+    shape = t.shape
+    if len(shape) != 2:
+        raise CmsdError(f"{name} must have two dimensions, got {tuple(shape)}")
+    n, d = shape
     if n > _INT_MAX or d > _INT_MAX:
         _too_large(name)
     return n, d
+
+
+def _fits(t, shape, dtype, cur):
+    """What _need asks of one tensor."""
+    return (t is not None and t.dtype is dtype and t.shape == shape and t.get_device() == cur >= 0
+            and t.is_contiguous())
+
+
+def _result(out, name, shape, dtype, like, cur):
+    """out's tensor of that name, which must fit, or a new one."""
+    if out is not None and name in out:
+        t = out[name]
+        if not _fits(t, shape, dtype, cur):
+            _need(cur, ((t, shape, dtype, name),))
+        return t
+    return _torch_mod.empty(shape, dtype=dtype, device=like.device)
 
 
 def embedding(tokens, table, scale=1.0, ignore_index=-100, out=None):
@@ -548,18 +562,19 @@ def embedding(tokens, table, scale=1.0, ignore_index=-100, out=None):
     tokens: int32 [R].  Nothing is recorded for autograd: a table that requires gradients is refused while it
     records.  Another token outside the vocabulary gives a row of zeros; embedding_errors tells."""
     torch = _torch()
-    _not_recorded("embedding", table)
+    if table.requires_grad and torch.is_grad_enabled():
+        _not_recorded("embedding")
     V, d = _rows(table, "table")
-    dtype = _code(table, "table")
+    code, dtype = _code(table, "table"), table.dtype
     R = tokens.numel()
     if R > _INT_MAX:
         _too_large("tokens [R]")
     ignore_index = _ignored(ignore_index)
-    x = _given(out, "x", (R, d), table.dtype, table)
     cur = _current(table)
-    _need(cur, ((tokens, (R,), torch.int32, "tokens"), (table, (V, d), table.dtype, "table"),
-                (x, (R, d), table.dtype, "x")))
-    rc = lib().cmsd_embedding(tokens.data_ptr(), table.data_ptr(), dtype, R, d, V, ignore_index, scale, x.data_ptr(),
+    if not (_fits(tokens, (R,), torch.int32, cur) and _fits(table, (V, d), dtype, cur)):
+        _need(cur, ((tokens, (R,), torch.int32, "tokens"), (table, (V, d), dtype, "table")))
+    x = _result(out, "x", (R, d), dtype, table, cur)
+    rc = lib().cmsd_embedding(tokens.data_ptr(), table.data_ptr(), code, R, d, V, ignore_index, float(scale), x.data_ptr(),
                               _stream_of(cur))
     if rc != OK:
         _check(rc, "cmsd_embedding")
@@ -582,16 +597,16 @@ def embedding_backward(tokens, d_x, V, scale=1.0, ignore_index=-100, add=False, 
     V = int(V)
     if not 0 < V <= _INT_MAX:
         _too_large("V")
-    dtype = _code(d_x, "d_x")
+    code, dtype = _code(d_x, "d_x"), d_x.dtype
     ignore_index = _ignored(ignore_index)
     if add and (out is None or out.get("d_table") is None):
         raise CmsdError("add needs the d_table that is added to, in out")
-    d_table = _given(out, "d_table", (V, d), d_x.dtype, d_x)
     cur = _current(d_x)
-    _need(cur, ((tokens, (R,), torch.int32, "tokens"), (d_x, (R, d), d_x.dtype, "d_x"),
-                (d_table, (V, d), d_x.dtype, "d_table")))
+    if not (_fits(tokens, (R,), torch.int32, cur) and _fits(d_x, (R, d), dtype, cur)):
+        _need(cur, ((tokens, (R,), torch.int32, "tokens"), (d_x, (R, d), dtype, "d_x")))
+    d_table = _result(out, "d_table", (V, d), dtype, d_x, cur)
     ws = ws if ws is not None else embedding_backward_workspace(R, d, V)
-    rc = lib().cmsd_embedding_backward(tokens.data_ptr(), d_x.data_ptr(), dtype, R, d, V, ignore_index, scale,
+    rc = lib().cmsd_embedding_backward(tokens.data_ptr(), d_x.data_ptr(), code, R, d, V, ignore_index, float(scale),
                                        1 if add else 0, d_table.data_ptr(), ws.data_ptr(), _need_ws(ws, cur),
                                        _stream_of(cur))
     if rc != OK:
@@ -616,26 +631,28 @@ def layernorm(x, weight=None, bias=None, eps=1e-5, stats=True, out=None):
     Returns dict y ([R, d], x's dtype) and, with stats, mean and rstd (float32 [R]) for layernorm_backward.  Nothing
     is recorded for autograd: tensors that require gradients are refused while it records."""
     torch = _torch()
-    _not_recorded("layernorm", x, weight, bias)
+    if torch.is_grad_enabled() and (x.requires_grad or weight is not None and weight.requires_grad
+                                    or bias is not None and bias.requires_grad):
+        _not_recorded("layernorm")
     R, d = _rows(x, "x")
-    dtype = _code(x, "x")
-    p = weight if weight is not None else bias
-    wdtype = dtype if p is None else _code(p, "weight" if weight is not None else "bias")
-    y = _given(out, "y", (R, d), x.dtype, x)
-    cur = _current(x)
-    specs = [(x, (R, d), x.dtype, "x"), (y, (R, d), x.dtype, "y")]
+    code, dtype = _code(x, "x"), x.dtype
+    wcode, wtype = code, dtype
     if weight is not None:
-        specs.append((weight, (d,), p.dtype, "weight"))
-    if bias is not None:
-        specs.append((bias, (d,), p.dtype, "bias"))
-    o = {"y": y}
+        wcode, wtype = _code(weight, "weight"), weight.dtype
+    elif bias is not None:
+        wcode, wtype = _code(bias, "bias"), bias.dtype
+    cur = _current(x)
+    if not (_fits(x, (R, d), dtype, cur) and (weight is None or _fits(weight, (d,), wtype, cur))
+            and (bias is None or _fits(bias, (d,), wtype, cur))):
+        _need(cur, ((x, (R, d), dtype, "x"),) + (((weight, (d,), wtype, "weight"),) if weight is not None else ())
+              + (((bias, (d,), wtype, "bias"),) if bias is not None else ()))
+    o = {"y": _result(out, "y", (R, d), dtype, x, cur)}
+    mean = rstd = None
     if stats:
-        for name in ("mean", "rstd"):
-            o[name] = _given(out, name, (R,), torch.float32, x)
-            specs.append((o[name], (R,), torch.float32, name))
-    _need(cur, specs)
-    rc = lib().cmsd_layernorm(x.data_ptr(), _ptr(weight), _ptr(bias), dtype, wdtype, R, d, eps, y.data_ptr(),
-                              _ptr(o.get("mean")), _ptr(o.get("rstd")), _stream_of(cur))
+        o["mean"] = mean = _result(out, "mean", (R,), torch.float32, x, cur)
+        o["rstd"] = rstd = _result(out, "rstd", (R,), torch.float32, x, cur)
+    rc = lib().cmsd_layernorm(x.data_ptr(), _ptr(weight), _ptr(bias), code, wcode, R, d, float(eps), o["y"].data_ptr(),
+                              _ptr(mean), _ptr(rstd), _stream_of(cur))
     if rc != OK:
         _check(rc, "cmsd_layernorm")
     return o
@@ -660,56 +677,41 @@ def layernorm_backward(x, weight, mean, rstd, d_y, x_grad=True, weight_grad=True
     [d] of weight's dtype (x's without weight), written whole."""
     torch = _torch()
     R, d = _rows(x, "x")
-    dtype = _code(x, "x")
-    ptype = x.dtype if weight is None else weight.dtype
-    wdtype = dtype if weight is None else _code(weight, "weight")
+    code, dtype = _code(x, "x"), x.dtype
+    wcode, wtype = (code, dtype) if weight is None else (_code(weight, "weight"), weight.dtype)
     f32 = torch.float32
-    specs = [(x, (R, d), x.dtype, "x"), (mean, (R,), f32, "mean"), (rstd, (R,), f32, "rstd"),
-             (d_y, (R, d), x.dtype, "d_y")]
-    if weight is not None:
-        specs.append((weight, (d,), ptype, "weight"))
-    o = {}
-    for name, want, shape, t in (("d_x", x_grad, (R, d), x.dtype), ("d_weight", weight_grad, (d,), ptype),
-                                 ("d_bias", bias_grad, (d,), ptype)):
-        if want:
-            o[name] = _given(out, name, shape, t, x)
-            specs.append((o[name], shape, t, name))
     cur = _current(x)
-    _need(cur, specs)
+    if not (_fits(x, (R, d), dtype, cur) and _fits(mean, (R,), f32, cur) and _fits(rstd, (R,), f32, cur)
+            and _fits(d_y, (R, d), dtype, cur) and (weight is None or _fits(weight, (d,), wtype, cur))):
+        _need(cur, ((x, (R, d), dtype, "x"), (mean, (R,), f32, "mean"), (rstd, (R,), f32, "rstd"),
+                    (d_y, (R, d), dtype, "d_y")) + (((weight, (d,), wtype, "weight"),) if weight is not None else ()))
+    o = {}
+    if x_grad:
+        o["d_x"] = _result(out, "d_x", (R, d), dtype, x, cur)
+    if weight_grad:
+        o["d_weight"] = _result(out, "d_weight", (d,), wtype, x, cur)
+    if bias_grad:
+        o["d_bias"] = _result(out, "d_bias", (d,), wtype, x, cur)
     ws = ws if ws is not None else layernorm_backward_workspace(R, d)
     rc = lib().cmsd_layernorm_backward(x.data_ptr(), _ptr(weight), mean.data_ptr(), rstd.data_ptr(), d_y.data_ptr(),
-                                       dtype, wdtype, R, d, _ptr(o.get("d_x")), _ptr(o.get("d_weight")),
+                                       code, wcode, R, d, _ptr(o.get("d_x")), _ptr(o.get("d_weight")),
                                        _ptr(o.get("d_bias")), ws.data_ptr(), _need_ws(ws, cur), _stream_of(cur))
     if rc != OK:
         _check(rc, "cmsd_layernorm_backward")
     return o
 
 
-def _word(v, name):
-    v = int(v)
-    if not 0 <= v < 1 << 32:
-        raise CmsdError(f"{name} must be a 32-bit number that is not negative")
-    return v
-
-
-def _dropout(fn, x, xname, yname, p, seed, iteration, site, step, residual, out):
-    torch = _torch()
-    dtype = _code(x, xname)
-    iteration, site = _word(iteration, "iteration"), _word(site, "site")
-    y = _given(out, yname, x.shape, x.dtype, x)
+def _dropout_args(x, name, yname, iteration, site, step, out):
+    code, dtype, shape = _code(x, name), x.dtype, x.shape
+    iteration, site = int(iteration), int(site)
+    if not (0 <= iteration < 1 << 32 and 0 <= site < 1 << 32):
+        raise CmsdError("iteration and site must be 32-bit numbers that are not negative")
     cur = _current(x)
-    specs = [(x, x.shape, x.dtype, xname), (y, x.shape, x.dtype, yname)]
-    if residual is not None:
-        specs.append((residual, x.shape, x.dtype, "residual"))
-    if step is not None:
-        specs.append((step, (1,), torch.int32, "step"))
-    _need(cur, specs)
-    more = (_ptr(residual),) if fn == "cmsd_dropout" else ()
-    rc = getattr(lib(), fn)(x.data_ptr(), *more, dtype, x.numel(), p, int(seed), iteration, site, _ptr(step),
-                            y.data_ptr(), _stream_of(cur))
-    if rc != OK:
-        _check(rc, fn)
-    return {yname: y}
+    if not _fits(x, shape, dtype, cur):
+        _need(cur, ((x, shape, dtype, name),))
+    if step is not None and not _fits(step, (1,), _torch_mod.int32, cur):
+        _need(cur, ((step, (1,), _torch_mod.int32, "step"),))
+    return code, cur, iteration, site, _result(out, yname, shape, dtype, x, cur)
 
 
 def dropout(x, p, seed, iteration=0, site=0, residual=None, step=None, out=None):
@@ -720,15 +722,29 @@ def dropout(x, p, seed, iteration=0, site=0, residual=None, step=None, out=None)
     stored.  step: None, or an int32 [1] tensor that is added to iteration when the call runs (a captured call then
     draws another mask at each replay).  Nothing is recorded for autograd: tensors that require gradients are refused
     while it records."""
-    _torch()
-    _not_recorded("dropout", x, residual)
-    return _dropout("cmsd_dropout", x, "x", "y", p, seed, iteration, site, step, residual, out)
+    torch = _torch()
+    if torch.is_grad_enabled() and (x.requires_grad or residual is not None and residual.requires_grad):
+        _not_recorded("dropout")
+    code, cur, iteration, site, y = _dropout_args(x, "x", "y", iteration, site, step, out)
+    if residual is not None and not _fits(residual, x.shape, x.dtype, cur):
+        _need(cur, ((residual, x.shape, x.dtype, "residual"),))
+    rc = lib().cmsd_dropout(x.data_ptr(), _ptr(residual), code, x.numel(), float(p), int(seed), iteration, site, _ptr(step),
+                            y.data_ptr(), _stream_of(cur))
+    if rc != OK:
+        _check(rc, "cmsd_dropout")
+    return {"y": y}
 
 
 def dropout_backward(d_y, p, seed, iteration=0, site=0, step=None, out=None):
     """The gradient of dropout by x, given the same p, seed, iteration, site and step: returns dict d_x.  (The
     residual's gradient is d_y itself.)"""
-    return _dropout("cmsd_dropout_backward", d_y, "d_y", "d_x", p, seed, iteration, site, step, None, out)
+    _torch()
+    code, cur, iteration, site, d_x = _dropout_args(d_y, "d_y", "d_x", iteration, site, step, out)
+    rc = lib().cmsd_dropout_backward(d_y.data_ptr(), code, d_y.numel(), float(p), int(seed), iteration, site, _ptr(step),
+                                     d_x.data_ptr(), _stream_of(cur))
+    if rc != OK:
+        _check(rc, "cmsd_dropout_backward")
+    return {"d_x": d_x}
 
 
 def verify(draft, target, tokens, conf, draft_lse=None, k_row=None, p=None, seed=0, iteration=0,

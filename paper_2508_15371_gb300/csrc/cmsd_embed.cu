@@ -322,7 +322,7 @@ __global__ void __launch_bounds__(kRadixThreads) embed_move_kernel(const EmbedAr
 // rows with the columns over its threads, kBatch rows requested at once; a token's
 // last row writes the sum.  A token that a border cuts leaves a piece of its sum
 // (fp32) in either tile, and embed_join_kernel adds those up.  Bound by memory.
-constexpr int kSlots = 64;                            // rows of a tile at most
+constexpr int kSlots = 64;                            // rows of a tile at most: two of a lane
 constexpr int kBatch = 8;
 constexpr int kSumThreads = 128;
 // A tile's state: the token whose rows go on behind it (-1: none), and whether that one begins there or has all of

@@ -23,5 +23,18 @@ cudaError_t launch(bool early, void (*kernel)(P...), dim3 grid, unsigned threads
   return cudaLaunchKernelEx(&cfg, kernel, args...);
 }
 
+// Dynamic shared memory above 48 KB, once for each kernel (its own `done`) and device.
+template <typename K>
+cudaError_t allow_smem(K kernel, size_t smem, unsigned long long* done) {
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  const unsigned long long bit = 1ull << (dev & 63);
+  if (__atomic_load_n(done, __ATOMIC_ACQUIRE) & bit) return cudaSuccess;
+  e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  if (e == cudaSuccess) __atomic_fetch_or(done, bit, __ATOMIC_ACQ_REL);
+  return e;
+}
+
 }  // namespace
 }  // namespace cmsd

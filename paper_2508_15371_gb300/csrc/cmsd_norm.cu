@@ -119,27 +119,27 @@ template <int N>
 __device__ __forceinline__ void copies_but() {       // all but the last N groups have arrived
   asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
 }
-// row `row` of x [R][d] by threads t of n, kTurns pieces each; in: there is such a row
+// row `row` of x [R][d], if there is one, by threads t of n, kTurns pieces each (a row that begins within a piece
+// may have one more)
 template <typename T, int VE, int kTurns>
-__device__ __forceinline__ void request_row(uint32_t to, const void* x, int64_t row, const NormArgs& a, bool in, int t, int n) {
-  const int64_t first = row * a.d * (int64_t)sizeof(T), last = first + a.d * (int64_t)sizeof(T);
-  const int64_t all = (int64_t)a.R * a.d * (int64_t)sizeof(T);
-  const char* p = static_cast<const char*>(x);
+__device__ __forceinline__ void request_row(uint32_t to, const void* x, int64_t row, const NormArgs& a, int t, int n) {
+  if (row >= a.R) return;
+  const int bytes = a.d * (int)sizeof(T);
+  const char* p = static_cast<const char*>(x) + row * bytes;
   if constexpr (VE * sizeof(T) == 16) {
+    p += t * 16;
+    to += t * 16;
 #pragma unroll
-    for (int k = 0; k < kTurns; ++k) {
-      const int64_t at = first + (t + n * k) * 16;
-      const bool here = in && at < last;
-      copy_async(to + (t + n * k) * 16, p + (here ? at : 0), here ? 16 : 0);
-    }
+    for (int k = 0; k < kTurns; ++k)
+      if ((t + n * k) * 16 < bytes) copy_async(to + n * k * 16, p + n * k * 16, 16);
   } else {
-    const int64_t base = first & ~(int64_t)15;
+    const int lead = (int)(reinterpret_cast<uintptr_t>(p) & 15), last = lead + bytes;
+    const int64_t rest = (a.R - row) * bytes + lead;          // bytes from the first piece to the end of x
+    p -= lead;
 #pragma unroll
     for (int k = 0; k <= kTurns; ++k) {
-      const int c = t + n * k;
-      if (k == kTurns && c > n * kTurns) break;      // (one piece more than an aligned row has)
-      const int64_t at = base + c * 16;
-      if (in && at < last) copy_async(to + c * 16, p + at, (int)(all - at < 16 ? all - at : 16));
+      const int at = (t + n * k) * 16;
+      if ((k < kTurns || t == 0) && at < last) copy_async(to + at, p + at, rest - at < 16 ? (int)(rest - at) : 16);
     }
   }
 }
@@ -344,7 +344,7 @@ __global__ void __launch_bounds__(cta_threads(W), kNormCtas) norm_many_kernel(co
 #pragma unroll
     for (int u = 0; u < kRows; ++u) {
       const int64_t row = r0 + u * kGroups;
-      request_row<T, VE, kTurns>(ring_at + (stage * kRows + u) * kRowBytes, a.x, row, a, row < a.R, t, 32 * W);
+      request_row<T, VE, kTurns>(ring_at + (stage * kRows + u) * kRowBytes, a.x, row, a, t, 32 * W);
     }
     close_copies();
   };
@@ -458,8 +458,8 @@ __global__ void __launch_bounds__(cta_threads(W), grad_ctas(W)) norm_backward_ke
   const uint32_t ring_at = (uint32_t)__cvta_generic_to_shared(ring);
   const auto request = [&](int64_t row, int stage) {
     const uint32_t to = ring_at + stage * 2 * kRowBytes;
-    request_row<T, VE, kTurns>(to, a.x, row, a, row < a.R, t, 32 * W);
-    request_row<T, VE, kTurns>(to + kRowBytes, a.d_y, row, a, row < a.R, t, 32 * W);
+    request_row<T, VE, kTurns>(to, a.x, row, a, t, 32 * W);
+    request_row<T, VE, kTurns>(to + kRowBytes, a.d_y, row, a, t, 32 * W);
     close_copies();
   };
 #pragma unroll
@@ -643,7 +643,8 @@ template <typename T, int VE, int W>
 cudaError_t launch_many(const NormArgs& a, cudaStream_t s) {
   constexpr int smem = kNormStages * kNormRows * cta_groups(W) * staged_bytes(W, kCols, sizeof(T));
   const auto kernel = norm_many_kernel<T, VE, W>;
-  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  static unsigned long long done = 0ull;
+  const cudaError_t e = allow_smem(kernel, smem, &done);
   if (e != cudaSuccess) return e;
   kernel<<<std::min(ceil_div(a.R, cta_groups(W) * kNormRows), kSms * kNormCtas), cta_threads(W), smem, s>>>(a);
   return cudaGetLastError();
@@ -673,10 +674,9 @@ cudaError_t launch_gradients(const NormArgs& a, int parts, cudaStream_t s) {
   constexpr int smem = grad_smem(W, sizeof(T));
   static_assert(smem >= kCols * 4 * cta_threads(W) || W > 8, "the groups' sums pass through the ring");
   const auto kernel = norm_backward_kernel<T, VE, W>;
-  if (smem > 48 * 1024) {
-    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
-    if (e != cudaSuccess) return e;
-  }
+  static unsigned long long done = 0ull;
+  const cudaError_t e = allow_smem(kernel, smem, &done);
+  if (e != cudaSuccess) return e;
   kernel<<<parts, cta_threads(W), smem, s>>>(a);
   return cudaGetLastError();
 }
