@@ -322,16 +322,14 @@ __device__ __forceinline__ bool in_row(int t, int k, int nvec) {
   return (W > 1 && 2 * (k + 1) <= NV) || t + 32 * W * k < nvec;
 }
 
-constexpr int kCols = 16;                            // columns of a thread
-constexpr int kNormRows = 1;
 constexpr int kNormStages = 3;
-constexpr int kNormCtas = 3;                         // an SM, by registers
-template <typename T, int VE, int W>
-__global__ void __launch_bounds__(cta_threads(W), kNormCtas) norm_many_kernel(const NormArgs a) {
+__host__ __device__ constexpr int norm_ctas(int cols) { return cols > 8 ? 3 : 4; }             // an SM, by registers
+template <typename T, int VE, int kCols, int W>
+__global__ void __launch_bounds__(cta_threads(W), norm_ctas(kCols)) norm_many_kernel(const NormArgs a) {
   using Raw = typename RowVec<T, VE>::Raw;
   using M = Num<VE>;
   using N = typename M::N;
-  constexpr int kN = M::kN, NV = kCols / VE, kGroups = cta_groups(W), kRows = kNormRows;
+  constexpr int kN = M::kN, NV = kCols / VE, kGroups = cta_groups(W), kRows = 1;
   constexpr int kRowBytes = staged_bytes(W, kCols, sizeof(T)), kTurns = kCols * sizeof(T) / 16;
   extern __shared__ uint4 s_ring4[];
   __shared__ __align__(16) float s_sum[W > 1 ? 2 * kGroups * kRows * W : 1];
@@ -440,10 +438,12 @@ __global__ void __launch_bounds__(cta_threads(W), kNormCtas) norm_many_kernel(co
 // ---- gradients ---------------------------------------------------------------------------
 // The CTAs' sums over rows are joined by norm_join_kernel, in the order of the CTAs.
 __host__ __device__ constexpr int grad_stages(int size) { return size == 2 ? 3 : 2; }
-__host__ __device__ constexpr int grad_smem(int w, int size) { return grad_stages(size) * 2 * cta_groups(w) * staged_bytes(w, kCols, size); }
-__host__ __device__ constexpr int grad_ctas(int w) { return w > 8 ? 1 : 2; }       // an SM, by registers
-template <typename T, int VE, int W>
-__global__ void __launch_bounds__(cta_threads(W), grad_ctas(W)) norm_backward_kernel(const NormArgs a) {
+__host__ __device__ constexpr int grad_smem(int w, int cols, int size) {
+  return grad_stages(size) * 2 * cta_groups(w) * staged_bytes(w, cols, size);
+}
+__host__ __device__ constexpr int grad_ctas(int w, int cols) { return w > 8 ? 1 : (cols > 8 ? 2 : 3); }       // an SM, by registers
+template <typename T, int VE, int kCols, int W>
+__global__ void __launch_bounds__(cta_threads(W), grad_ctas(W, kCols)) norm_backward_kernel(const NormArgs a) {
   using Raw = typename RowVec<T, VE>::Raw;
   using M = Num<VE>;
   using N = typename M::N;
@@ -576,77 +576,117 @@ __global__ void __launch_bounds__(32 * kJoinWarps) norm_join_kernel(const NormAr
 }
 
 constexpr int kWideCols = 8192;
-// rows of over kWideCols columns: d_x by a CTA a row, the sums over rows by a CTA 32 columns
-template <typename T>
+// rows of over kWideCols columns: d_x by a CTA a row, the sums over rows by a CTA 32 vectors of columns
+template <typename T, int VE>
 __global__ void __launch_bounds__(kWide) norm_wide_dx_kernel(const NormArgs a) {
+  using V = RowVec<T, VE>;
+  using Raw = typename V::Raw;
   __shared__ float s_sum[2 * kWide / 32];
-  const size_t at = (size_t)blockIdx.x * a.d;
-  const T* x = static_cast<const T*>(a.x) + at;
-  const T* dy = static_cast<const T*>(a.d_y) + at;
+  const int nvec = a.d / VE;
+  const size_t at = (size_t)blockIdx.x * nvec;
+  const Raw* xs = static_cast<const Raw*>(a.x) + at;
+  const Raw* gs = static_cast<const Raw*>(a.d_y) + at;
   const float mean = a.mean_in[blockIdx.x], rstd = a.rstd_in[blockIdx.x], over_d = 1.f / a.d;
+  const auto take = [&](int v, float (&h)[VE], float (&g)[VE]) {
+    float w[VE];
+    V::get(xs[v], h);
+    V::get(gs[v], g);
+    if (a.weight) params<VE>(a.weight, a.wdtype, v * VE, w);
+#pragma unroll
+    for (int j = 0; j < VE; ++j) {
+      h[j] = (h[j] - mean) * rstd;
+      if (a.weight) g[j] *= w[j];
+    }
+  };
   float s[2] = {0.f, 0.f};
-  for (int j = threadIdx.x; j < a.d; j += kWide) {
-    const float g = to_float(dy[j]) * (a.weight ? param(a.weight, a.wdtype, j) : 1.f);
-    s[0] += g;
-    s[1] = __fmaf_rn(g, (to_float(x[j]) - mean) * rstd, s[1]);
+#pragma unroll 2
+  for (int v = threadIdx.x; v < nvec; v += kWide) {
+    float h[VE], g[VE];
+    take(v, h, g);
+#pragma unroll
+    for (int j = 0; j < VE; ++j) {
+      s[0] += g[j];
+      s[1] = __fmaf_rn(g[j], h[j], s[1]);
+    }
   }
   row_sums<2, kWide / 32>(s, s_sum);
   const float m1 = s[0] * over_d, m2 = s[1] * over_d;
-  for (int j = threadIdx.x; j < a.d; j += kWide) {
-    const float g = to_float(dy[j]) * (a.weight ? param(a.weight, a.wdtype, j) : 1.f);
-    const float h = (to_float(x[j]) - mean) * rstd;
-    static_cast<T*>(a.d_x)[at + j] = from_float<T>(rstd * ((g - m1) - h * m2));
+#pragma unroll 2
+  for (int v = threadIdx.x; v < nvec; v += kWide) {   // (again, from L2)
+    float h[VE], g[VE];
+    take(v, h, g);
+#pragma unroll
+    for (int j = 0; j < VE; ++j) g[j] = rstd * ((g[j] - m1) - h[j] * m2);
+    static_cast<Raw*>(a.d_x)[at + v] = V::put(g);
   }
 }
-template <typename T>
+template <typename T, int VE>
 __global__ void __launch_bounds__(256) norm_wide_sums_kernel(const NormArgs a) {
-  __shared__ float s_w[8][32], s_b[8][32];
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, j = blockIdx.x * 32 + lane;
-  float w = 0.f, b = 0.f;
-  if (j < a.d)
-#pragma unroll 8
-    for (int64_t r = (int64_t)blockIdx.y * 8 + warp; r < a.R; r += (int64_t)gridDim.y * 8) {
-      const float g = to_float(static_cast<const T*>(a.d_y)[(size_t)r * a.d + j]);
-      w = __fmaf_rn(g, (to_float(static_cast<const T*>(a.x)[(size_t)r * a.d + j]) - a.mean_in[r]) * a.rstd_in[r], w);
-      b += g;
-    }
-  s_w[warp][lane] = w;
-  s_b[warp][lane] = b;
-  __syncthreads();
-  if (warp || j >= a.d) return;
+  using V = RowVec<T, VE>;
+  using Raw = typename V::Raw;
+  __shared__ float s_w[8][32 * VE], s_b[8][32 * VE];
+  const int nvec = a.d / VE, lane = threadIdx.x & 31, warp = threadIdx.x >> 5, v = blockIdx.x * 32 + lane;
+  float w[VE], b[VE];
 #pragma unroll
-  for (int k = 1; k < 8; ++k) {
-    w += s_w[k][lane];
-    b += s_b[k][lane];
+  for (int j = 0; j < VE; ++j) w[j] = b[j] = 0.f;
+  if (v < nvec)
+#pragma unroll 4
+    for (int64_t r = (int64_t)blockIdx.y * 8 + warp; r < a.R; r += (int64_t)gridDim.y * 8) {
+      const float mean = a.mean_in[r], rstd = a.rstd_in[r];
+      float x[VE], g[VE];
+      V::get(static_cast<const Raw*>(a.x)[(size_t)r * nvec + v], x);
+      V::get(static_cast<const Raw*>(a.d_y)[(size_t)r * nvec + v], g);
+#pragma unroll
+      for (int j = 0; j < VE; ++j) {
+        w[j] = __fmaf_rn(g[j], (x[j] - mean) * rstd, w[j]);
+        b[j] += g[j];
+      }
+    }
+#pragma unroll
+  for (int j = 0; j < VE; ++j) {
+    s_w[warp][lane * VE + j] = w[j];
+    s_b[warp][lane * VE + j] = b[j];
   }
+  __syncthreads();
   float* part = a.part + (size_t)blockIdx.y * 2 * a.d;
-  part[j] = w;
-  part[a.d + j] = b;
+  for (int k = threadIdx.x; k < 32 * VE; k += 256) {
+    const int j = blockIdx.x * 32 * VE + k;
+    if (j >= a.d) break;
+    float sw = 0.f, sb = 0.f;
+#pragma unroll
+    for (int q = 0; q < 8; ++q) {
+      sw += s_w[q][k];
+      sb += s_b[q][k];
+    }
+    part[j] = sw;
+    part[a.d + j] = sb;
+  }
 }
 
 int ceil_div(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
-// warps of a row, a thread kCols columns of it
+// columns of a thread, and warps of a row
+int row_cols(int d) { return d <= 256 ? 8 : 16; }
 int row_warps(int d) {
   int w = 1;
-  while (w * 32 * kCols < d) w *= 2;
+  while (w * 32 * row_cols(d) < d) w *= 2;
   return w;
 }
 // CTAs whose sums over rows are joined, by R and d alone
 int part_count(int R, int d) {
   if (d > kWideCols) return R < 64 * 8 ? ceil_div(R, 8) : 64;
   const int w = row_warps(d), n = ceil_div(R, cta_groups(w));
-  return std::min(n, kSms * grad_ctas(w));
+  return std::min(n, kSms * grad_ctas(w, row_cols(d)));
 }
 
 constexpr int kFewRows = 608;
-template <typename T, int VE, int W>
+template <typename T, int VE, int kCols, int W>
 cudaError_t launch_many(const NormArgs& a, cudaStream_t s) {
-  constexpr int smem = kNormStages * kNormRows * cta_groups(W) * staged_bytes(W, kCols, sizeof(T));
-  const auto kernel = norm_many_kernel<T, VE, W>;
+  constexpr int smem = kNormStages * cta_groups(W) * staged_bytes(W, kCols, sizeof(T));
+  const auto kernel = norm_many_kernel<T, VE, kCols, W>;
   static unsigned long long done = 0ull;
   const cudaError_t e = allow_smem(kernel, smem, &done);
   if (e != cudaSuccess) return e;
-  kernel<<<std::min(ceil_div(a.R, cta_groups(W) * kNormRows), kSms * kNormCtas), cta_threads(W), smem, s>>>(a);
+  kernel<<<std::min(ceil_div(a.R, cta_groups(W)), kSms * norm_ctas(kCols)), cta_threads(W), smem, s>>>(a);
   return cudaGetLastError();
 }
 template <typename T, int VE>
@@ -656,10 +696,10 @@ cudaError_t launch_rows(const NormArgs& a, cudaStream_t s) {
     return cudaGetLastError();
   };
   if (a.R > kFewRows && a.d <= 4096) switch (row_warps(a.d)) {
-      case 1: return launch_many<T, VE, 1>(a, s);
-      case 2: return launch_many<T, VE, 2>(a, s);
-      case 4: return launch_many<T, VE, 4>(a, s);
-      default: return launch_many<T, VE, 8>(a, s);
+      case 1: return a.d <= 256 ? launch_many<T, VE, 8, 1>(a, s) : launch_many<T, VE, 16, 1>(a, s);
+      case 2: return launch_many<T, VE, 16, 2>(a, s);
+      case 4: return launch_many<T, VE, 16, 4>(a, s);
+      default: return launch_many<T, VE, 16, 8>(a, s);
     }
   if (a.d <= 256) return few(norm_kernel<T, VE, 8 / VE, 1>, 32);
   if (a.d <= 2048) return few(norm_kernel<T, VE, 8 / VE, 8>, 256);
@@ -669,11 +709,11 @@ cudaError_t launch_rows(const NormArgs& a, cudaStream_t s) {
   return few(norm_wide_kernel<T>, kWide);
 }
 
-template <typename T, int VE, int W>
+template <typename T, int VE, int kCols, int W>
 cudaError_t launch_gradients(const NormArgs& a, int parts, cudaStream_t s) {
-  constexpr int smem = grad_smem(W, sizeof(T));
+  constexpr int smem = grad_smem(W, kCols, sizeof(T));
   static_assert(smem >= kCols * 4 * cta_threads(W) || W > 8, "the groups' sums pass through the ring");
-  const auto kernel = norm_backward_kernel<T, VE, W>;
+  const auto kernel = norm_backward_kernel<T, VE, kCols, W>;
   static unsigned long long done = 0ull;
   const cudaError_t e = allow_smem(kernel, smem, &done);
   if (e != cudaSuccess) return e;
@@ -683,17 +723,17 @@ cudaError_t launch_gradients(const NormArgs& a, int parts, cudaStream_t s) {
 template <typename T, int VE>
 cudaError_t launch_gradients(const NormArgs& a, int parts, cudaStream_t s) {
   switch (row_warps(a.d)) {
-    case 1: return launch_gradients<T, VE, 1>(a, parts, s);
-    case 2: return launch_gradients<T, VE, 2>(a, parts, s);
-    case 4: return launch_gradients<T, VE, 4>(a, parts, s);
-    case 8: return launch_gradients<T, VE, 8>(a, parts, s);
-    default: return launch_gradients<T, VE, 16>(a, parts, s);
+    case 1: return a.d <= 256 ? launch_gradients<T, VE, 8, 1>(a, parts, s) : launch_gradients<T, VE, 16, 1>(a, parts, s);
+    case 2: return launch_gradients<T, VE, 16, 2>(a, parts, s);
+    case 4: return launch_gradients<T, VE, 16, 4>(a, parts, s);
+    case 8: return launch_gradients<T, VE, 16, 8>(a, parts, s);
+    default: return launch_gradients<T, VE, 16, 16>(a, parts, s);
   }
 }
-template <typename T>
+template <typename T, int VE>
 cudaError_t launch_wide_gradients(const NormArgs& a, int parts, cudaStream_t s) {
-  if (a.d_x) norm_wide_dx_kernel<T><<<a.R, kWide, 0, s>>>(a);
-  if (a.d_weight || a.d_bias) norm_wide_sums_kernel<T><<<dim3(ceil_div(a.d, 32), parts), 256, 0, s>>>(a);
+  if (a.d_x) norm_wide_dx_kernel<T, VE><<<a.R, kWide, 0, s>>>(a);
+  if (a.d_weight || a.d_bias) norm_wide_sums_kernel<T, VE><<<dim3(ceil_div(a.d / VE, 32), parts), 256, 0, s>>>(a);
   return cudaGetLastError();
 }
 
@@ -711,13 +751,11 @@ cudaError_t launch_norm(const NormArgs& a, cudaStream_t s) {
 
 cudaError_t launch_norm_backward(const NormArgs& a, cudaStream_t s) {
   const int parts = part_count(a.R, a.d);
-  cudaError_t e;
-  if (a.d > kWideCols)
-    e = a.dtype == 0 ? launch_wide_gradients<float>(a, parts, s) : launch_wide_gradients<__nv_bfloat16>(a, parts, s);
-  else
-    e = by_row_type(a.dtype, a.d, [&](auto t) {
-      return launch_gradients<typename decltype(t)::T, decltype(t)::VE>(a, parts, s);
-    });
+  const cudaError_t e = by_row_type(a.dtype, a.d, [&](auto t) {
+    using Row = decltype(t);
+    return a.d > kWideCols ? launch_wide_gradients<typename Row::T, Row::VE>(a, parts, s)
+                           : launch_gradients<typename Row::T, Row::VE>(a, parts, s);
+  });
   if (e != cudaSuccess || (!a.d_weight && !a.d_bias)) return e;
   return launch(true, norm_join_kernel, dim3(ceil_div(a.d, 32), 2), 32 * kJoinWarps, 0, s, a, parts);
 }
