@@ -45,7 +45,7 @@ __device__ __forceinline__ void params(const void* p, int dtype, int j, float (&
   }
 }
 
-// the sums of N numbers over W warps (those of one row), in every thread; buf: [W][N] for each use, so that no
+// the sums of N numbers over a CTA of W warps, in every thread; buf: [W][N] for each use, so that no
 // two uses without a barrier between them share one
 template <int N, int W>
 __device__ __forceinline__ void row_sums(float (&v)[N], float* buf) {
@@ -53,8 +53,7 @@ __device__ __forceinline__ void row_sums(float (&v)[N], float* buf) {
   for (int o = 16; o; o >>= 1)
 #pragma unroll
     for (int k = 0; k < N; ++k) v[k] += __shfl_xor_sync(kFull, v[k], o);
-  if (W == 1) return;
-  const int w = (threadIdx.x >> 5) % W;
+  const int w = threadIdx.x >> 5;
   if ((threadIdx.x & 31) == 0)
 #pragma unroll
     for (int k = 0; k < N; ++k) buf[w * N + k] = v[k];
@@ -153,22 +152,21 @@ __device__ __forceinline__ int lead_of(int64_t row, int d) {
   return VE * sizeof(T) == 16 ? 0 : (int)(row * d * (int64_t)sizeof(T) & 15);
 }
 
-// ---- forward ---------------------------------------------------------------------------
-// W warps a row, NV vectors of VE entries a thread.  Sums are of differences from
+// ---- few rows, and wide ones -----------------------------------------------------------------
+// A CTA of W warps a row, NV vectors of VE entries a thread.  Sums are of differences from
 // the row's first entry, so that a mean far from zero cancels before anything is
 // rounded, and a row of one number gives exactly bias; what their mean c still
 // lacks, e, comes with the squares.
 template <typename T, int VE, int NV, int W>
-__global__ void __launch_bounds__(W > 8 ? 32 * W : 256) norm_kernel(const NormArgs a) {
+__global__ void __launch_bounds__(32 * W) norm_kernel(const NormArgs a) {
   using V = RowVec<T, VE>;
   using Raw = typename V::Raw;
   using M = Num<VE>;
   using N = typename M::N;
   constexpr int kN = M::kN;
-  __shared__ float s_sum[W > 1 ? 3 * W : 1];
-  const int nvec = a.d / VE, lane = threadIdx.x & 31, t = W == 1 ? lane : threadIdx.x;
-  const int64_t row = W == 1 ? (int64_t)blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5) : blockIdx.x;
-  if (row >= a.R) return;                            // (whole warps, and none that a barrier waits for)
+  __shared__ float s_sum[3 * W];
+  const int nvec = a.d / VE, t = threadIdx.x;
+  const int64_t row = blockIdx.x;
   const Raw* x = static_cast<const Raw*>(a.x) + (size_t)row * nvec;
   Raw* y = static_cast<Raw*>(a.y) + (size_t)row * nvec;
   Raw raw[NV];
@@ -695,15 +693,13 @@ cudaError_t launch_rows(const NormArgs& a, cudaStream_t s) {
     kernel<<<a.R, threads, 0, s>>>(a);
     return cudaGetLastError();
   };
-  if (a.R > kFewRows && a.d <= 4096) switch (row_warps(a.d)) {
+  if (a.d <= 4096 && (a.R > kFewRows || a.d <= 256 || a.d > 2048)) switch (row_warps(a.d)) {
       case 1: return a.d <= 256 ? launch_many<T, VE, 8, 1>(a, s) : launch_many<T, VE, 16, 1>(a, s);
       case 2: return launch_many<T, VE, 16, 2>(a, s);
       case 4: return launch_many<T, VE, 16, 4>(a, s);
       default: return launch_many<T, VE, 16, 8>(a, s);
     }
-  if (a.d <= 256) return few(norm_kernel<T, VE, 8 / VE, 1>, 32);
   if (a.d <= 2048) return few(norm_kernel<T, VE, 8 / VE, 8>, 256);
-  if (a.d <= 4096) return few(norm_kernel<T, VE, 16 / VE, 8>, 256);
   if (a.d <= 8192) return few(norm_kernel<T, VE, 32 / VE, 8>, 256);
   if (a.d <= 32768) return few(norm_kernel<T, VE, 32 / VE, 32>, 1024);
   return few(norm_wide_kernel<T>, kWide);
