@@ -119,6 +119,32 @@ def test_wide_rows(cmsd, R, d, V, dtype):
     _check_table(cmsd.embedding_backward(tokens, d_x, V)["d_table"], tokens, d_x, V, 1.0)
 
 
+@pytest.mark.parametrize("R,V", [(600011, 40), (8193, 1 << 20), (9000, (1 << 21) + 5), (530000, 3000), (10000, 1)])
+def test_many_rows_and_tokens(cmsd, R, V):
+    """Ordering with over 2048 rows a CTA, with two and three passes, and of one token alone."""
+    d = 8
+    g = _gen(R, V, 8)
+    tokens = _tokens(R, V, g, ignored=0.1)
+    d_x = torch.randn(R, d, generator=g, device="cuda")
+    _check_table(cmsd.embedding_backward(tokens, d_x, V)["d_table"], tokens, d_x, V, 1.0)
+
+
+def test_the_largest_vocabulary(cmsd):
+    """2^30 - 1 tokens, one column: four passes; the table's last bytes are not a whole vector."""
+    V, R = (1 << 30) - 1, 9001
+    g = _gen(5)
+    tokens = torch.randint(0, V, (R,), generator=g, device="cuda").int()
+    tokens[:3000] = tokens[3000:6000]
+    tokens[0], tokens[1], tokens[2] = V - 1, V - 1, 0
+    d_x = torch.randint(1, 5, (R, 1), generator=g, device="cuda").bfloat16()
+    out = torch.full((V + 128, 1), 7.0, dtype=torch.bfloat16, device="cuda")
+    got = cmsd.embedding_backward(tokens, d_x, V, out={"d_table": out[:V]})["d_table"]
+    rows, at = torch.unique(tokens.long(), return_inverse=True)
+    want = torch.zeros(rows.numel(), dtype=torch.float64, device="cuda").index_add_(0, at, d_x[:, 0].double())
+    assert torch.equal(got[rows, 0].double(), want)                  # small whole numbers: exact
+    assert int(torch.count_nonzero(got)) == rows.numel() and (out[V:] == 7).all()
+
+
 @pytest.mark.parametrize("R", [1, 33, 5000])
 def test_every_row_padding(cmsd, R):
     d, V = 24, 100
