@@ -168,13 +168,15 @@ def params(K, rule="paper", preset="full", **kw):
 
 _torch_mod = None
 _raw_stream = None      # (device index) -> cudaStream_t of the current stream, without a Stream object
+_get_device = None      # () -> index of the current device, of a runtime that is initialised
 
 
 def _torch():
-    global _torch_mod, _raw_stream
+    global _torch_mod, _raw_stream, _get_device
     if _torch_mod is None:
         import torch
         _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        _get_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
         _torch_mod = torch
     return _torch_mod
 
@@ -333,7 +335,7 @@ def _need(cur, specs):
 
 def _current(t):
     """The current device, where t is a CUDA tensor at all (-1 otherwise: nothing is asked of the runtime)."""
-    return _torch_mod.cuda.current_device() if t.is_cuda else -1
+    return _get_device() if t.is_cuda else -1
 
 
 def _need_ws(ws, cur):
@@ -545,6 +547,11 @@ def _fits(t, shape, dtype, cur):
             and t.is_contiguous())
 
 
+def _here(t, cur):
+    """The same of a tensor that shapes and types are taken from."""
+    return t.get_device() == cur >= 0 and t.is_contiguous()
+
+
 def _result(out, name, shape, dtype, like, cur):
     """out's tensor of that name, which must fit, or a new one."""
     if out is not None and name in out:
@@ -571,7 +578,7 @@ def embedding(tokens, table, scale=1.0, ignore_index=-100, out=None):
         _too_large("tokens [R]")
     ignore_index = _ignored(ignore_index)
     cur = _current(table)
-    if not (_fits(tokens, (R,), torch.int32, cur) and _fits(table, (V, d), dtype, cur)):
+    if not (_fits(tokens, (R,), torch.int32, cur) and _here(table, cur)):
         _need(cur, ((tokens, (R,), torch.int32, "tokens"), (table, (V, d), dtype, "table")))
     x = _result(out, "x", (R, d), dtype, table, cur)
     rc = lib().cmsd_embedding(tokens.data_ptr(), table.data_ptr(), code, R, d, V, ignore_index, float(scale), x.data_ptr(),
@@ -602,7 +609,7 @@ def embedding_backward(tokens, d_x, V, scale=1.0, ignore_index=-100, add=False, 
     if add and (out is None or out.get("d_table") is None):
         raise CmsdError("add needs the d_table that is added to, in out")
     cur = _current(d_x)
-    if not (_fits(tokens, (R,), torch.int32, cur) and _fits(d_x, (R, d), dtype, cur)):
+    if not (_fits(tokens, (R,), torch.int32, cur) and _here(d_x, cur)):
         _need(cur, ((tokens, (R,), torch.int32, "tokens"), (d_x, (R, d), dtype, "d_x")))
     d_table = _result(out, "d_table", (V, d), dtype, d_x, cur)
     ws = ws if ws is not None else embedding_backward_workspace(R, d, V)
@@ -642,7 +649,7 @@ def layernorm(x, weight=None, bias=None, eps=1e-5, stats=True, out=None):
     elif bias is not None:
         wcode, wtype = _code(bias, "bias"), bias.dtype
     cur = _current(x)
-    if not (_fits(x, (R, d), dtype, cur) and (weight is None or _fits(weight, (d,), wtype, cur))
+    if not (_here(x, cur) and (weight is None or _fits(weight, (d,), wtype, cur))
             and (bias is None or _fits(bias, (d,), wtype, cur))):
         _need(cur, ((x, (R, d), dtype, "x"),) + (((weight, (d,), wtype, "weight"),) if weight is not None else ())
               + (((bias, (d,), wtype, "bias"),) if bias is not None else ()))
@@ -681,7 +688,7 @@ def layernorm_backward(x, weight, mean, rstd, d_y, x_grad=True, weight_grad=True
     wcode, wtype = (code, dtype) if weight is None else (_code(weight, "weight"), weight.dtype)
     f32 = torch.float32
     cur = _current(x)
-    if not (_fits(x, (R, d), dtype, cur) and _fits(mean, (R,), f32, cur) and _fits(rstd, (R,), f32, cur)
+    if not (_here(x, cur) and _fits(mean, (R,), f32, cur) and _fits(rstd, (R,), f32, cur)
             and _fits(d_y, (R, d), dtype, cur) and (weight is None or _fits(weight, (d,), wtype, cur))):
         _need(cur, ((x, (R, d), dtype, "x"), (mean, (R,), f32, "mean"), (rstd, (R,), f32, "rstd"),
                     (d_y, (R, d), dtype, "d_y")) + (((weight, (d,), wtype, "weight"),) if weight is not None else ()))
@@ -707,7 +714,7 @@ def _dropout_args(x, name, yname, iteration, site, step, out):
     if not (0 <= iteration < 1 << 32 and 0 <= site < 1 << 32):
         raise CmsdError("iteration and site must be 32-bit numbers that are not negative")
     cur = _current(x)
-    if not _fits(x, shape, dtype, cur):
+    if not _here(x, cur):
         _need(cur, ((x, shape, dtype, name),))
     if step is not None and not _fits(step, (1,), _torch_mod.int32, cur):
         _need(cur, ((step, (1,), _torch_mod.int32, "step"),))
