@@ -9,6 +9,7 @@
 #include <cuda_bf16.h>
 
 #include "cmsd_device.cuh"
+#include "cmsd_launch.cuh"
 #include "cmsd_philox.cuh"
 #include "cmsd_rows.cuh"
 #include "cmsd_train.h"
@@ -29,6 +30,7 @@ template <typename T, bool RESIDUAL>
 __global__ void __launch_bounds__(kThreads) dropout_kernel(const DropArgs a) {
   constexpr int kVecs = sizeof(T) / 2, kIn = 8 / kVecs;        // 16-byte vectors of eight entries, entries of one
   using V = RowVec<T, kIn>;
+  wait_for_previous();
   const int64_t whole = a.n >> 3;                    // counters with all of their entries
   const int64_t g0 = (int64_t)blockIdx.x * (kThreads * kEach) + threadIdx.x;
   const uint4* x = static_cast<const uint4*>(a.x);
@@ -78,9 +80,7 @@ __global__ void __launch_bounds__(kThreads) dropout_kernel(const DropArgs a) {
 template <typename T>
 cudaError_t launch_typed(const DropArgs& a, cudaStream_t s) {
   const int64_t ctas = ((a.n + 7) / 8 + kThreads * kEach - 1) / (kThreads * kEach);   // (n < 2^42: below 2^31 of them)
-  if (a.residual) dropout_kernel<T, true><<<(unsigned)ctas, kThreads, 0, s>>>(a);
-  else dropout_kernel<T, false><<<(unsigned)ctas, kThreads, 0, s>>>(a);
-  return cudaGetLastError();
+  return launch(true, a.residual ? dropout_kernel<T, true> : dropout_kernel<T, false>, (unsigned)ctas, kThreads, 0, s, a);
 }
 
 }  // namespace

@@ -17,11 +17,6 @@
 namespace cmsd {
 namespace {
 
-__device__ __forceinline__ void wait_for_previous() {
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  asm volatile("griddepcontrol.wait;" ::: "memory");
-}
-
 // ---- rows of the table ------------------------------------------------------------
 // A warp a piece of 256 vectors of a row, eight requested at once.
 constexpr int kAhead = 8;
@@ -29,6 +24,7 @@ template <typename T, int VE>
 __global__ void __launch_bounds__(256) embed_kernel(const EmbedArgs a, int pieces) {
   using V = RowVec<T, VE>;
   using Raw = typename V::Raw;
+  wait_for_previous();
   const int lane = threadIdx.x & 31, nvec = a.d / VE;
   const int64_t units = (int64_t)a.R * pieces, step = (int64_t)gridDim.x * (blockDim.x >> 5);
   for (int64_t u = (int64_t)blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5); u < units; u += step) {
@@ -94,7 +90,7 @@ template <int RPW>
 __global__ void __launch_bounds__(kRankThreads) embed_rank_kernel(const EmbedArgs a, int row_ctas) {
   extern __shared__ uint4 s_key4[];
   unsigned* s_key = reinterpret_cast<unsigned*>(s_key4);
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  wait_for_previous();
   if ((int)blockIdx.x >= row_ctas) {
     fill(a, a.fill[0], a.fill[1], blockIdx.x - row_ctas);
     return;
@@ -170,7 +166,7 @@ constexpr int kTileMin = 2048;
 constexpr int kRound = 8;                            // rows of a lane requested at once
 __global__ void __launch_bounds__(kRadixThreads) embed_count_kernel(const EmbedArgs a, int digits, int tiles) {
   extern __shared__ int s_count[];
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  wait_for_previous();
   if ((int)blockIdx.x >= tiles) {
     fill(a, a.fill[0], a.fill[1], blockIdx.x - tiles);
     return;
@@ -551,8 +547,8 @@ cudaError_t launch_embed(const EmbedArgs& a, cudaStream_t s) {
     int warps = 1;
     while (warps < 8 && units > 304 * warps) warps *= 2;
     const int64_t ctas = (units + warps - 1) / warps;
-    embed_kernel<typename Row::T, Row::VE><<<(unsigned)(ctas < (1 << 30) ? ctas : 1 << 30), 32 * warps, 0, s>>>(a, pieces);
-    return cudaGetLastError();
+    return launch(true, embed_kernel<typename Row::T, Row::VE>, (unsigned)(ctas < (1 << 30) ? ctas : 1 << 30), 32 * warps, 0, s, a,
+                  pieces);
   });
 }
 
@@ -582,11 +578,13 @@ cudaError_t launch_embed_backward(const EmbedArgs& args, cudaStream_t s) {
   if (a.R <= kRankRows) {
     const size_t smem = (size_t)(a.R + 127) / 128 * 512;
     const int per = a.R <= 2432 ? 8 : 32, ctas = ceil_div(a.R, per);
-    e = launch(false, per == 8 ? embed_rank_kernel<1> : embed_rank_kernel<4>, ctas + fill_ctas(0), kRankThreads, smem, s, a, ctas);
+    // (of many rows it is bound by the SMs' instructions, and CTAs that come early crowd on a few of them: R = 8192 36.6
+    // us a call in a row of them instead of 29.1; of few it is short, R = 333 25.2 instead of 27.4)
+    e = launch(per == 8, per == 8 ? embed_rank_kernel<1> : embed_rank_kernel<4>, ctas + fill_ctas(0), kRankThreads, smem, s, a, ctas);
   } else {
     const int digits = 1 << a.bits, tiles = ceil_div(a.R, a.tile);
     const size_t smem = (size_t)kRadixWarps * digits * 4;
-    e = launch(false, embed_count_kernel, tiles + fill_ctas(0), kRadixThreads, (size_t)digits * 4, s, a, digits, tiles);
+    e = launch(true, embed_count_kernel, tiles + fill_ctas(0), kRadixThreads, (size_t)digits * 4, s, a, digits, tiles);
     for (int p = 0; p < a.passes && e == cudaSuccess; ++p)
       e = launch(true, p == 0 ? embed_move_kernel<true> : embed_move_kernel<false>, tiles + fill_ctas(p + 1), kRadixThreads, smem,
                  s, a, p, a.bits, tiles);

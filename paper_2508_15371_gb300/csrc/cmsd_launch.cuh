@@ -5,8 +5,15 @@
 namespace cmsd {
 namespace {
 
-// a launch that may begin before what precedes it on the stream has ended (early:
-// the first launch of a call does not)
+// Waits for the end of the launch before, then lets the next one of the stream take
+// its place on the GPU: the first thing in a kernel of an early launch.  (The other
+// way about, whole calls would queue up on the SMs behind one another: a gradient of
+// 32768 rows in a graph of such calls took 51 us instead of 32.)
+__device__ __forceinline__ void wait_for_previous() {
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+}
+// a launch that may begin before what precedes it on the stream has ended (early)
 template <typename... P, typename... A>
 cudaError_t launch(bool early, void (*kernel)(P...), dim3 grid, unsigned threads, size_t smem, cudaStream_t s,
                    A... args) {

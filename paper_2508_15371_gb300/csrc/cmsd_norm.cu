@@ -165,6 +165,7 @@ __global__ void __launch_bounds__(32 * W) norm_kernel(const NormArgs a) {
   using N = typename M::N;
   constexpr int kN = M::kN;
   __shared__ float s_sum[3 * W];
+  wait_for_previous();
   const int nvec = a.d / VE, t = threadIdx.x;
   const int64_t row = blockIdx.x;
   const Raw* x = static_cast<const Raw*>(a.x) + (size_t)row * nvec;
@@ -243,6 +244,7 @@ constexpr int kWide = 1024;
 template <typename T>
 __global__ void __launch_bounds__(kWide) norm_wide_kernel(const NormArgs a) {
   __shared__ float s_sum[3 * kWide / 32];
+  wait_for_previous();
   const T* x = static_cast<const T*>(a.x) + (size_t)blockIdx.x * a.d;
   T* y = static_cast<T*>(a.y) + (size_t)blockIdx.x * a.d;
   const float pilot = to_float(x[0]);
@@ -331,6 +333,7 @@ __global__ void __launch_bounds__(cta_threads(W), norm_ctas(kCols)) norm_many_ke
   constexpr int kRowBytes = staged_bytes(W, kCols, sizeof(T)), kTurns = kCols * sizeof(T) / 16;
   extern __shared__ uint4 s_ring4[];
   __shared__ __align__(16) float s_sum[W > 1 ? 2 * kGroups * kRows * W : 1];
+  wait_for_previous();
   const int nvec = a.d / VE, t = threadIdx.x % (32 * W), group = threadIdx.x / (32 * W);
   const int64_t first = (int64_t)blockIdx.x * kGroups * kRows + group, step = (int64_t)gridDim.x * kGroups * kRows;
   char* ring = reinterpret_cast<char*>(s_ring4) + group * kNormStages * kRows * kRowBytes;       // [kNormStages][kRows]
@@ -449,7 +452,7 @@ __global__ void __launch_bounds__(cta_threads(W), grad_ctas(W, kCols)) norm_back
   constexpr int kStages = grad_stages(sizeof(T)), kRowBytes = staged_bytes(W, kCols, sizeof(T)), kTurns = kCols * sizeof(T) / 16;
   extern __shared__ uint4 s_ring4[];
   __shared__ __align__(16) float s_sum[W > 1 ? 2 * kGroups * 2 * W : 1];
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  wait_for_previous();
   const int nvec = a.d / VE, t = threadIdx.x % (32 * W), group = threadIdx.x / (32 * W);
   const int64_t first = (int64_t)blockIdx.x * kGroups + group, step = (int64_t)gridDim.x * kGroups;
   char* ring = reinterpret_cast<char*>(s_ring4) + group * kStages * 2 * kRowBytes;             // [kStages][2]
@@ -558,7 +561,7 @@ __global__ void __launch_bounds__(32 * kJoinWarps) norm_join_kernel(const NormAr
   __shared__ float s_part[kJoinWarps][32];
   const int lane = threadIdx.x & 31, j = blockIdx.x * 32 + lane, which = blockIdx.y, warp = threadIdx.x >> 5;
   void* out = which ? a.d_bias : a.d_weight;
-  asm volatile("griddepcontrol.wait;" ::: "memory");
+  wait_for_previous();
   if (!out) return;
   float v = 0.f;
   if (j < a.d)
@@ -580,6 +583,7 @@ __global__ void __launch_bounds__(kWide) norm_wide_dx_kernel(const NormArgs a) {
   using V = RowVec<T, VE>;
   using Raw = typename V::Raw;
   __shared__ float s_sum[2 * kWide / 32];
+  wait_for_previous();
   const int nvec = a.d / VE;
   const size_t at = (size_t)blockIdx.x * nvec;
   const Raw* xs = static_cast<const Raw*>(a.x) + at;
@@ -623,6 +627,7 @@ __global__ void __launch_bounds__(256) norm_wide_sums_kernel(const NormArgs a) {
   using V = RowVec<T, VE>;
   using Raw = typename V::Raw;
   __shared__ float s_w[8][32 * VE], s_b[8][32 * VE];
+  wait_for_previous();
   const int nvec = a.d / VE, lane = threadIdx.x & 31, warp = threadIdx.x >> 5, v = blockIdx.x * 32 + lane;
   float w[VE], b[VE];
 #pragma unroll
@@ -684,15 +689,11 @@ cudaError_t launch_many(const NormArgs& a, cudaStream_t s) {
   static unsigned long long done = 0ull;
   const cudaError_t e = allow_smem(kernel, smem, &done);
   if (e != cudaSuccess) return e;
-  kernel<<<std::min(ceil_div(a.R, cta_groups(W)), kSms * norm_ctas(kCols)), cta_threads(W), smem, s>>>(a);
-  return cudaGetLastError();
+  return launch(true, kernel, std::min(ceil_div(a.R, cta_groups(W)), kSms * norm_ctas(kCols)), cta_threads(W), smem, s, a);
 }
 template <typename T, int VE>
 cudaError_t launch_rows(const NormArgs& a, cudaStream_t s) {
-  const auto few = [&](auto kernel, int threads) {   // a CTA a row
-    kernel<<<a.R, threads, 0, s>>>(a);
-    return cudaGetLastError();
-  };
+  const auto few = [&](auto kernel, int threads) { return launch(true, kernel, a.R, threads, 0, s, a); };   // a CTA a row
   if (a.d <= 4096 && (a.R > kFewRows || a.d <= 256 || a.d > 2048)) switch (row_warps(a.d)) {
       case 1: return a.d <= 256 ? launch_many<T, VE, 8, 1>(a, s) : launch_many<T, VE, 16, 1>(a, s);
       case 2: return launch_many<T, VE, 16, 2>(a, s);
@@ -713,8 +714,7 @@ cudaError_t launch_gradients(const NormArgs& a, int parts, cudaStream_t s) {
   static unsigned long long done = 0ull;
   const cudaError_t e = allow_smem(kernel, smem, &done);
   if (e != cudaSuccess) return e;
-  kernel<<<parts, cta_threads(W), smem, s>>>(a);
-  return cudaGetLastError();
+  return launch(true, kernel, parts, cta_threads(W), smem, s, a);
 }
 template <typename T, int VE>
 cudaError_t launch_gradients(const NormArgs& a, int parts, cudaStream_t s) {
@@ -728,9 +728,10 @@ cudaError_t launch_gradients(const NormArgs& a, int parts, cudaStream_t s) {
 }
 template <typename T, int VE>
 cudaError_t launch_wide_gradients(const NormArgs& a, int parts, cudaStream_t s) {
-  if (a.d_x) norm_wide_dx_kernel<T, VE><<<a.R, kWide, 0, s>>>(a);
-  if (a.d_weight || a.d_bias) norm_wide_sums_kernel<T, VE><<<dim3(ceil_div(a.d / VE, 32), parts), 256, 0, s>>>(a);
-  return cudaGetLastError();
+  cudaError_t e = a.d_x ? launch(true, norm_wide_dx_kernel<T, VE>, a.R, kWide, 0, s, a) : cudaSuccess;
+  if (e == cudaSuccess && (a.d_weight || a.d_bias))
+    e = launch(true, norm_wide_sums_kernel<T, VE>, dim3(ceil_div(a.d / VE, 32), parts), 256, 0, s, a);
+  return e;
 }
 
 }  // namespace
