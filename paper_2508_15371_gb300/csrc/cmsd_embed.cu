@@ -62,27 +62,36 @@ __device__ __forceinline__ unsigned key_of(const EmbedArgs& a, int token, bool& 
 
 // A table that is written whole gets its zeros from the launches that put the rows
 // in order: that takes a few CTAs some microseconds a launch, and the others write
-// all of the table.  Rows that get a sum are written again, a fifth more bytes where
-// 32768 tokens meet a vocabulary of 128256 ranks (d = 2048 bf16: 123 us; leaving
-// them out, by looking each token up beside the sums, 136).
+// all of the table, equal shares of it.  Rows that get a sum are written again, a
+// tenth more bytes where 32768 tokens meet a vocabulary of 128256 (d = 2048 bf16:
+// 108 us; with the zeros written beside the sums, where a search finds no rows, 136).
+// Chunks of 8 KB: of 16, 32 and 64 KB the ordering CTAs wait longer for their loads
+// (110, 112, 116 us), of 4 KB launching CTAs is what bounds (170 us).
 constexpr int kFillThreads = 256;
-constexpr int kFillVecs = 16;                        // 16-byte vectors of a thread
-constexpr size_t kFillCta = (size_t)kFillThreads * kFillVecs * 16;
-__device__ __forceinline__ void fill(const EmbedArgs& a, size_t first, size_t last, int cta) {
-  const size_t at = first + (size_t)cta * kFillCta + threadIdx.x * 16;
-  char* p = static_cast<char*>(a.d_table) + at;
+constexpr int kFillVecs = 2;                         // 16-byte vectors of a thread
+constexpr size_t kFillChunk = (size_t)kFillThreads * kFillVecs * 16;
+constexpr size_t kFillCtas = 1 << 24;                // at most
+// bytes [first, last) of the table, by this and `ctas` - 1 other CTAs
+__device__ __forceinline__ void fill(const EmbedArgs& a, size_t first, size_t last, int cta, int ctas) {
+  char* table = static_cast<char*>(a.d_table);
+  for (size_t chunk = first + (size_t)cta * kFillChunk; chunk < last; chunk += (size_t)ctas * kFillChunk) {
+    const size_t at = chunk + threadIdx.x * 16;
 #pragma unroll
-  for (int k = 0; k < kFillVecs; ++k) {
-    const size_t o = (size_t)k * kFillThreads * 16;
-    if (at + o + 16 <= last) *reinterpret_cast<uint4*>(p + o) = make_uint4(0, 0, 0, 0);
-    else if (at + o < last)                          // (the end of a table of odd rows)
-      for (size_t q = at + o; q < last; q += 2) *reinterpret_cast<uint16_t*>(static_cast<char*>(a.d_table) + q) = 0;
+    for (int k = 0; k < kFillVecs; ++k) {
+      const size_t o = at + (size_t)k * kFillThreads * 16;
+      if (o + 16 <= last) *reinterpret_cast<uint4*>(table + o) = make_uint4(0, 0, 0, 0);
+      else                                           // (the end of a table of odd rows)
+        for (size_t q = o; q < last; q += 2) *reinterpret_cast<uint16_t*>(table + q) = 0;
+    }
   }
 }
 
 // Few rows: each row's place is the number of rows before it in (token, row)
-// order, counted by comparing it with all of them: R^2 comparisons, spread over
-// the GPU, in one launch.  A warp RPW rows, a lane every 32nd four of the others.
+// order, counted by comparing it with all of them: R^2 comparisons of two
+// instructions, spread over the GPU, in one launch.  A warp RPW rows, a lane every
+// 32nd four of the others.  d_x of R x 1024 added to a table, sums and all: R = 4096
+// 12.9 us (in passes of the radix sort below 22.8), 8192 19.3 (25.9), 12288 29.3
+// (28.4); written whole, d = 2048, 4096 81.3 us (81.9), 8192 90.6 (85.2).
 constexpr int kRankRows = 8192;
 constexpr int kRankThreads = 256;
 constexpr int kRankAhead = 16;                       // tokens of a thread requested at once
@@ -92,7 +101,7 @@ __global__ void __launch_bounds__(kRankThreads) embed_rank_kernel(const EmbedArg
   unsigned* s_key = reinterpret_cast<unsigned*>(s_key4);
   wait_for_previous();
   if ((int)blockIdx.x >= row_ctas) {
-    fill(a, a.fill[0], a.fill[1], blockIdx.x - row_ctas);
+    fill(a, a.fill[0], a.fill[1], blockIdx.x - row_ctas, gridDim.x - row_ctas);
     return;
   }
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, padded = (a.R + 127) / 128 * 128;
@@ -168,7 +177,7 @@ __global__ void __launch_bounds__(kRadixThreads) embed_count_kernel(const EmbedA
   extern __shared__ int s_count[];
   wait_for_previous();
   if ((int)blockIdx.x >= tiles) {
-    fill(a, a.fill[0], a.fill[1], blockIdx.x - tiles);
+    fill(a, a.fill[0], a.fill[1], blockIdx.x - tiles, gridDim.x - tiles);
     return;
   }
   for (int g = threadIdx.x; g < digits; g += kRadixThreads) s_count[g] = 0;
@@ -218,7 +227,7 @@ __global__ void __launch_bounds__(kRadixThreads) embed_move_kernel(const EmbedAr
   const int digits = 1 << bits, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   if ((int)blockIdx.x >= tiles) {                     // (nothing that the launch before makes is used)
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    fill(a, a.fill[pass + 1], a.fill[pass + 2], blockIdx.x - tiles);
+    fill(a, a.fill[pass + 1], a.fill[pass + 2], blockIdx.x - tiles, gridDim.x - tiles);
     return;
   }
   for (int g = threadIdx.x; g < kRadixWarps * digits; g += kRadixThreads) s_at[g] = 0;
@@ -573,11 +582,11 @@ cudaError_t launch_embed_backward(const EmbedArgs& args, cudaStream_t s) {
   const int launches = a.R <= kRankRows ? 1 : a.passes + 1;
   for (int k = 0; k < launches; ++k) a.fill[k] = all / launches / 16 * 16 * k;
   a.fill[launches] = all;
-  const auto fill_ctas = [&](int k) { return ceil_div(a.fill[k + 1] - a.fill[k], kFillCta); };
+  const auto fill_ctas = [&](int k) { return (int)std::min((a.fill[k + 1] - a.fill[k] + kFillChunk - 1) / kFillChunk, kFillCtas); };
   cudaError_t e;
   if (a.R <= kRankRows) {
     const size_t smem = (size_t)(a.R + 127) / 128 * 512;
-    const int per = a.R <= 2432 ? 8 : 32, ctas = ceil_div(a.R, per);
+    const int per = a.R <= 1216 ? 8 : 32, ctas = ceil_div(a.R, per);
     // (of many rows it is bound by the SMs' instructions, and CTAs that come early crowd on a few of them: R = 8192 36.6
     // us a call in a row of them instead of 29.1; of few it is short, R = 333 25.2 instead of 27.4)
     e = launch(per == 8, per == 8 ? embed_rank_kernel<1> : embed_rank_kernel<4>, ctas + fill_ctas(0), kRankThreads, smem, s, a, ctas);

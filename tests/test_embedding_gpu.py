@@ -119,7 +119,7 @@ def test_wide_rows(cmsd, R, d, V, dtype):
     _check_table(cmsd.embedding_backward(tokens, d_x, V)["d_table"], tokens, d_x, V, 1.0)
 
 
-@pytest.mark.parametrize("R,V", [(600011, 40), (8193, 1 << 20), (9000, (1 << 21) + 5), (530000, 3000), (10000, 1)])
+@pytest.mark.parametrize("R,V", [(8192, 300), (600011, 40), (8193, 1 << 20), (9000, (1 << 21) + 5), (530000, 3000), (10000, 1)])
 def test_many_rows_and_tokens(cmsd, R, V):
     """Ordering with over 2048 rows a CTA, with two and three passes, and of one token alone."""
     d = 8
