@@ -5,7 +5,8 @@
 // of bf16.  Sixteen bits an entry, not 32, because the generator would bound the
 // call otherwise (2^27 bf16 entries without a residual: 78.0 us, 6.9 TB/s; with a
 // word an entry 110.7 us, 4.9 TB/s), at rates that are multiples of 2^-16; the kept
-// entries' scale is that of the rounded rate.
+// entries' scale is that of the rounded rate.  Bound by memory: R = 16384 d = 2048 bf16
+// with a residual 30.4 us, 6.6 TB/s; without 22.1, 6.1.
 #include <cuda_bf16.h>
 
 #include "cmsd_device.cuh"
