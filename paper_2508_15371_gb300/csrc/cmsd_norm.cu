@@ -121,10 +121,10 @@ __device__ __forceinline__ void copies_but() {       // all but the last N group
 // row `row` of x [R][d], if there is one, by threads t of n, kTurns pieces each (a row that begins within a piece
 // may have one more)
 template <typename T, int VE, int kTurns>
-__device__ __forceinline__ void request_row(uint32_t to, const void* x, int64_t row, const NormArgs& a, int t, int n) {
+__device__ __forceinline__ void request_row(uint32_t to, const void* x, int row, const NormArgs& a, int t, int n) {
   if (row >= a.R) return;
   const int bytes = a.d * (int)sizeof(T);
-  const char* p = static_cast<const char*>(x) + row * bytes;
+  const char* p = static_cast<const char*>(x) + (int64_t)row * bytes;
   if constexpr (VE * sizeof(T) == 16) {
     p += t * 16;
     to += t * 16;
@@ -133,7 +133,7 @@ __device__ __forceinline__ void request_row(uint32_t to, const void* x, int64_t 
       if ((t + n * k) * 16 < bytes) copy_async(to + n * k * 16, p + n * k * 16, 16);
   } else {
     const int lead = (int)(reinterpret_cast<uintptr_t>(p) & 15), last = lead + bytes;
-    const int64_t rest = (a.R - row) * bytes + lead;          // bytes from the first piece to the end of x
+    const int64_t rest = (int64_t)(a.R - row) * bytes + lead;          // bytes from the first piece to the end of x
     p -= lead;
 #pragma unroll
     for (int k = 0; k <= kTurns; ++k) {
@@ -148,8 +148,8 @@ __device__ __forceinline__ typename RowVec<T, VE>::Raw staged(const char* to, in
   return *reinterpret_cast<const typename RowVec<T, VE>::Raw*>(to + lead + v * (int)(VE * sizeof(T)));
 }
 template <typename T, int VE>
-__device__ __forceinline__ int lead_of(int64_t row, int d) {
-  return VE * sizeof(T) == 16 ? 0 : (int)(row * d * (int64_t)sizeof(T) & 15);
+__device__ __forceinline__ int lead_of(int row, int d) {
+  return VE * sizeof(T) == 16 ? 0 : (int)((unsigned)row * (unsigned)d * (unsigned)sizeof(T) & 15u);
 }
 
 // ---- few rows, and wide ones -----------------------------------------------------------------
@@ -290,6 +290,22 @@ __device__ __forceinline__ void group_sync(int group) {
   if (W == 1) __syncwarp();
   else asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "n"(32 * W) : "memory");
 }
+// the sum of W numbers in shared memory
+template <int W>
+__device__ __forceinline__ float sum_of(const float* buf) {
+  float v = 0.f;
+  if constexpr (W % 4 == 0) {
+#pragma unroll
+    for (int j = 0; j < W; j += 4) {
+      const float4 p = *reinterpret_cast<const float4*>(buf + j);
+      v += (p.x + p.y) + (p.z + p.w);
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < W; ++j) v += buf[j];
+  }
+  return v;
+}
 // the sums of N numbers over a group's warps, in every thread; buf: [N][W], not in use by another exchange between
 // whose barrier and this one's there is none
 template <int N, int W>
@@ -304,19 +320,27 @@ __device__ __forceinline__ void group_sums(float (&v)[N], float* buf, int group)
     for (int k = 0; k < N; ++k) buf[k * W + (threadIdx.x >> 5) % W] = v[k];
   group_sync<W>(group);
 #pragma unroll
-  for (int k = 0; k < N; ++k) {
-    v[k] = 0.f;
-    if constexpr (W % 4 == 0) {
+  for (int k = 0; k < N; ++k) v[k] = sum_of<W>(buf + k * W);
+}
+
+// The same of two numbers: from the first exchange on, half of the lanes have one and half the other.
+template <int W>
+__device__ __forceinline__ void group_two_sums(float (&v)[2], float* buf, int group) {
+  const int lane = threadIdx.x & 31;
+  const bool second = (lane & 16) != 0;
+  const float gives = second ? v[0] : v[1], keeps = second ? v[1] : v[0];
+  float x = keeps + __shfl_xor_sync(kFull, gives, 16);
 #pragma unroll
-      for (int j = 0; j < W; j += 4) {
-        const float4 p = *reinterpret_cast<const float4*>(buf + k * W + j);
-        v[k] += (p.x + p.y) + (p.z + p.w);
-      }
-    } else {
-#pragma unroll
-      for (int j = 0; j < W; ++j) v[k] += buf[k * W + j];
-    }
+  for (int o = 8; o; o >>= 1) x += __shfl_xor_sync(kFull, x, o);
+  if (W == 1) {
+    v[0] = __shfl_sync(kFull, x, 0);
+    v[1] = __shfl_sync(kFull, x, 16);
+    return;
   }
+  if ((lane & 15) == 0) buf[(lane >> 4) * W + (threadIdx.x >> 5) % W] = x;
+  group_sync<W>(group);
+#pragma unroll
+  for (int k = 0; k < 2; ++k) v[k] = sum_of<W>(buf + k * W);
 }
 
 // whether a thread's vector k is in the row: a row that takes W > 1 warps fills half of what they hold
@@ -457,10 +481,10 @@ __global__ void __launch_bounds__(cta_threads(W), grad_ctas(W, kCols)) norm_back
   __shared__ __align__(16) float s_sum[W > 1 ? 2 * kGroups * 2 * W : 1];
   wait_for_previous();
   const int nvec = a.d / VE, t = threadIdx.x % (32 * W), group = threadIdx.x / (32 * W);
-  const int64_t first = (int64_t)blockIdx.x * kGroups + group, step = (int64_t)gridDim.x * kGroups;
+  const int first = blockIdx.x * kGroups + group, step = gridDim.x * kGroups;
   char* ring = reinterpret_cast<char*>(s_ring4) + group * kStages * 2 * kRowBytes;             // [kStages][2]
   const uint32_t ring_at = (uint32_t)__cvta_generic_to_shared(ring);
-  const auto request = [&](int64_t row, int stage) {
+  const auto request = [&](int row, int stage) {
     const uint32_t to = ring_at + stage * 2 * kRowBytes;
     request_row<T, VE, kTurns>(to, a.x, row, a, t, 32 * W);
     request_row<T, VE, kTurns>(to + kRowBytes, a.d_y, row, a, t, 32 * W);
@@ -484,14 +508,15 @@ __global__ void __launch_bounds__(cta_threads(W), grad_ctas(W, kCols)) norm_back
   }
   const float over_d = 1.f / a.d;
   int stage = 0, turn = 0;
-  for (int64_t row = first; row < a.R; row += step, turn ^= 1) {
+  for (int row = first; row < a.R; row += step, turn ^= 1) {
     copies_but<kStages - 2>();
     if (!aligned_rows<T, VE>()) group_sync<W>(group);
     request(row + (kStages - 1) * step, stage == 0 ? kStages - 1 : stage - 1);
     const char* from = ring + stage * 2 * kRowBytes;
     const int lead = lead_of<T, VE>(row, a.d);
     stage = stage + 1 == kStages ? 0 : stage + 1;
-    const N m = M::all(-mean), rs = M::all(rstd);
+    const float r = rstd;
+    const N m = M::all(-mean), rs = M::all(r);
     if (row + step < a.R) {
       mean = __ldg(a.mean_in + row + step);
       rstd = __ldg(a.rstd_in + row + step);
@@ -514,14 +539,14 @@ __global__ void __launch_bounds__(cta_threads(W), grad_ctas(W, kCols)) norm_back
       }
     if (!a.d_x) continue;                             // (the same in the whole grid)
     float s[2] = {M::sum(s1), M::sum(s2)};
-    group_sums<2, W>(s, s_sum + (W > 1 ? (turn * kGroups + group) * 2 * W : 0), group);
-    const N m1 = M::all(-s[0] * over_d), m2 = M::all(-s[1] * over_d);
+    group_two_sums<W>(s, s_sum + (W > 1 ? (turn * kGroups + group) * 2 * W : 0), group);
+    const N m1 = M::all(-s[0] * over_d * r), m2 = M::all(-s[1] * over_d * r);
     Raw* d_x = static_cast<Raw*>(a.d_x) + (size_t)row * nvec;
 #pragma unroll
     for (int k = 0; k < NV; ++k)
       if (in_row<W, NV>(t, k, nvec)) {
 #pragma unroll
-        for (int j = 0; j < kN; ++j) g[k][j] = M::mul(rs, M::fma(h[k][j], m2, M::add(g[k][j], m1)));
+        for (int j = 0; j < kN; ++j) g[k][j] = M::fma(h[k][j], m2, M::fma(g[k][j], rs, m1));
         d_x[t + 32 * W * k] = M::template put<T>(g[k]);
       }
   }
