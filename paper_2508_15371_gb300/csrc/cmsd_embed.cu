@@ -53,6 +53,140 @@ __global__ void __launch_bounds__(256) embed_kernel(const EmbedArgs a, int piece
   }
 }
 
+// ---- few rows ----------------------------------------------------------------------------
+// All in one launch, nothing put in order: every CTA has all tokens in shared
+// memory.  CTAs of kFewTile rows look up which of theirs come first of their token,
+// list the rows of those tokens in order, and add them up, the columns over the
+// threads; the others write zeros to the rows of kFewFill bytes of the table that
+// no token is of.  Bound by memory (R = 333 d = 1000 of 32001 f32 21.1 us, 6.1 TB/s),
+// or by the row of loads: tokens, rows, and a batch of them after another where a
+// token has many.  Against the three launches below, d = 2048 of 128256 bf16: R = 1
+// 69.1 against 71.5 us, 512 70.5 and 75.5; added to a table, d = 1024, R = 256 4.7
+// and 6.3, 512 7.2 and 7.7, 1024 11.9 and 8.7.
+constexpr int kFewRows = 512, kFewTile = 4, kFewThreads = 128, kFewTokens = 1024;
+constexpr size_t kFewFill = (size_t)48 << 10;
+template <typename T, int VE, bool ADD>
+__global__ void __launch_bounds__(kFewThreads) embed_few_kernel(const EmbedArgs a, int tiles, int chunks, int per) {
+  using V = RowVec<T, VE>;
+  using Raw = typename V::Raw;
+  constexpr int kBatch = ADD ? 8 : 16;
+  wait_for_previous();
+  const int nvec = a.d / VE, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  if ((int)blockIdx.x >= tiles * chunks) {
+    __shared__ uint8_t s_there[kFewTokens];
+    const int64_t v0 = (int64_t)((int)blockIdx.x - tiles * chunks) * per;
+    const int n = (int)(a.V - v0 < per ? a.V - v0 : per);
+    for (int c = threadIdx.x; c < n; c += kFewThreads) s_there[c] = 0;
+    __syncthreads();
+    for (int k = threadIdx.x; k < a.R; k += kFewThreads) {
+      const int token = __ldg(a.tokens + k);
+      if (token != a.ignore && token >= v0 && token - v0 < n) s_there[token - v0] = 1;
+    }
+    __syncthreads();
+    Raw* out = static_cast<Raw*>(a.d_table) + (size_t)v0 * nvec;
+    if (nvec >= kFewThreads) {
+      for (int c = 0; c < n; ++c)
+        if (!s_there[c])
+          for (int j = threadIdx.x; j < nvec; j += kFewThreads) out[(size_t)c * nvec + j] = V::zero();
+    } else {
+      for (int j = threadIdx.x; j < n * nvec; j += kFewThreads)
+        if (!s_there[j / nvec]) out[j] = V::zero();
+    }
+    return;
+  }
+  __shared__ int s_token[kFewRows];                   // -1: padding
+  __shared__ int2 s_list[kFewRows + 16];              // (row or -1, token to write or -1)
+  __shared__ int s_count[kFewTile];
+  const int tile = blockIdx.x % tiles, chunk = blockIdx.x / tiles, r0 = tile * kFewTile;
+  for (int k = threadIdx.x; k < a.R; k += kFewThreads) {
+    const int token = __ldg(a.tokens + k);
+    const bool in = token >= 0 && token < a.V;
+    if (!in && token != a.ignore && blockIdx.x == 0) report(a.err, 1u);
+    s_token[k] = in && token != a.ignore ? token : -1;
+  }
+  __syncthreads();
+  for (int u = warp; u < kFewTile; u += kFewThreads / 32) {
+    const int r = r0 + u, token = r < a.R ? s_token[r] : -1;
+    int n = 0;
+    if (token >= 0) {
+      bool first = true;
+      for (int k = lane; k - lane < a.R; k += 32) {
+        const unsigned same = __ballot_sync(kFull, k < a.R && s_token[k] == token);
+        const int before = r - (k - lane);            // lanes of rows before r
+        first = first && !(same & (before >= 32 ? kFull : before > 0 ? (1u << before) - 1u : 0u));
+        n += __popc(same);
+      }
+      if (!first) n = 0;
+    }
+    if (lane == 0) s_count[u] = n;
+  }
+  __syncthreads();
+  int total = 0;
+  for (int u = 0; u < kFewTile; ++u) {
+    const int n = s_count[u];
+    if (u % (kFewThreads / 32) == warp && n > 0) {
+      const int token = s_token[r0 + u];
+      int at = total;
+      for (int k = (r0 + u) / 32 * 32 + lane; k - lane < a.R; k += 32) {
+        const bool mine = k < a.R && s_token[k] == token;
+        const unsigned same = __ballot_sync(kFull, mine);
+        const int p = at + __popc(same & ((1u << lane) - 1u));
+        if (mine) s_list[p] = make_int2(k, p == total + n - 1 ? token : -1);
+        at += __popc(same);
+      }
+    }
+    total += n;
+  }
+  if (total == 0) return;                             // (the same in every thread)
+  if (threadIdx.x < 16) s_list[total + threadIdx.x] = make_int2(-1, -1);
+  __syncthreads();
+  const int c = chunk * kFewThreads + threadIdx.x;
+  if (c >= nvec) return;
+  const Raw* d_x = static_cast<const Raw*>(a.d_x) + c;
+  Raw* out = static_cast<Raw*>(a.d_table) + c;
+  float sum[VE];
+#pragma unroll
+  for (int j = 0; j < VE; ++j) sum[j] = 0.f;
+#pragma unroll 1
+  for (int k0 = 0; k0 < total; k0 += kBatch) {
+    Raw x[kBatch], had[ADD ? kBatch : 1];
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u) {
+      const int2 o = s_list[k0 + u];
+      x[u] = V::zero();
+      if (o.x >= 0) x[u] = d_x[(size_t)o.x * nvec];
+      if (ADD && o.y >= 0) had[u] = out[(size_t)o.y * nvec];
+    }
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u) {
+      const int token = s_list[k0 + u].y;
+      float f[VE];
+      V::get(x[u], f);
+#pragma unroll
+      for (int j = 0; j < VE; ++j) sum[j] += f[j];
+      if (token >= 0) {
+        if (ADD) V::get(had[ADD ? u : 0], f);
+#pragma unroll
+        for (int j = 0; j < VE; ++j) {
+          f[j] = ADD ? __fmaf_rn(sum[j], a.scale, f[j]) : sum[j] * a.scale;
+          sum[j] = 0.f;
+        }
+        out[(size_t)token * nvec] = V::put(f);
+      }
+    }
+  }
+}
+
+int ceil_div(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
+template <typename T, int VE, bool ADD>
+cudaError_t launch_few(const EmbedArgs& a, cudaStream_t s) {
+  const size_t row = (size_t)a.d * sizeof(T);
+  const int tiles = ceil_div(a.R, kFewTile), chunks = ceil_div(a.d / VE, kFewThreads);
+  const int per = (int)std::min<size_t>(kFewTokens, std::max<size_t>(1, kFewFill / row));
+  return launch(true, embed_few_kernel<T, VE, ADD>, tiles * chunks + (ADD ? 0 : ceil_div(a.V, per)), kFewThreads, 0, s, a, tiles,
+                chunks, per);
+}
+
 // ---- the rows in their tokens' order ------------------------------------------------
 // What a row is ordered by: its token, or V (behind all tokens) for padding.
 __device__ __forceinline__ unsigned key_of(const EmbedArgs& a, int token, bool& bad) {
@@ -512,7 +646,6 @@ __global__ void __launch_bounds__(kJoinThreads) embed_join_kernel(const EmbedArg
 }
 
 size_t up256(size_t x) { return (x + 255) / 256 * 256; }
-int ceil_div(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
 // Rows of a tile, at least kBatch, for four tiles an SM where there are few rows (for eight, 32768 rows of 1000 tokens
 // took 41 us instead of 35: borders cut twice as many tokens).
 constexpr int kTiles = 608;
@@ -583,6 +716,11 @@ cudaError_t launch_sums(const EmbedArgs& a, cudaStream_t s) {
 
 cudaError_t launch_embed_backward(const EmbedArgs& args, cudaStream_t s) {
   EmbedArgs a = args;
+  if (a.R <= kFewRows)
+    return by_row_type(a.dtype, a.d, [&](auto t) {
+      using Row = decltype(t);
+      return a.add ? launch_few<typename Row::T, Row::VE, true>(a, s) : launch_few<typename Row::T, Row::VE, false>(a, s);
+    });
   // the k-th of the launches that order the rows fills bytes [fill[k], fill[k + 1])
   const size_t all = a.add ? 0 : (size_t)a.V * a.d * (a.dtype == 0 ? 4 : 2);
   const int launches = a.R <= kRankRows ? 1 : a.passes + 1;
@@ -594,7 +732,7 @@ cudaError_t launch_embed_backward(const EmbedArgs& args, cudaStream_t s) {
     const size_t smem = (size_t)(a.R + 127) / 128 * 512;
     const int per = a.R <= 1216 ? 8 : 32, ctas = ceil_div(a.R, per);
     // (of many rows it is bound by the SMs' instructions, and CTAs that come early crowd on a few of them: R = 8192 36.6
-    // us a call in a row of them instead of 29.1; of few it is short, R = 333 25.2 instead of 27.4)
+    // us a call in a row of them instead of 29.1)
     e = launch(per == 8, per == 8 ? embed_rank_kernel<1> : embed_rank_kernel<4>, ctas + fill_ctas(0), kRankThreads, smem, s, a, ctas);
   } else {
     const int digits = 1 << a.bits, tiles = ceil_div(a.R, a.tile);
