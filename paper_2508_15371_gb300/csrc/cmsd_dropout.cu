@@ -47,7 +47,7 @@ __global__ void __launch_bounds__(kThreads) dropout_kernel(const DropArgs a) {
         if (RESIDUAL) rv[u][k] = __ldcs(r + g * kVecs + k);
       }
   }
-  const uint32_t it = iter_word(a.iteration + (a.step ? __ldg(a.step) : 0u), kPurposeDropout);
+  const uint32_t it = iter_word(a.iteration + (a.step ? *a.step : 0u), kPurposeDropout);
 #pragma unroll
   for (int u = 0; u < kEach; ++u) {
     const int64_t g = g0 + u * kThreads;

@@ -39,7 +39,7 @@ __global__ void __launch_bounds__(256) embed_kernel(const EmbedArgs a, int piece
 #pragma unroll
     for (int k = 0; k < kAhead; ++k) {
       w[k] = V::zero();
-      if (keep && v0 + 32 * k < nvec) w[k] = __ldg(row + v0 + 32 * k);
+      if (keep && v0 + 32 * k < nvec) w[k] = row[v0 + 32 * k];
     }
 #pragma unroll
     for (int k = 0; k < kAhead; ++k)
@@ -79,7 +79,7 @@ __global__ void __launch_bounds__(kFewThreads) embed_few_kernel(const EmbedArgs 
     for (int c = threadIdx.x; c < n; c += kFewThreads) s_there[c] = 0;
     __syncthreads();
     for (int k = threadIdx.x; k < a.R; k += kFewThreads) {
-      const int token = __ldg(a.tokens + k);
+      const int token = a.tokens[k];
       if (token != a.ignore && token >= v0 && token - v0 < n) s_there[token - v0] = 1;
     }
     __syncthreads();
@@ -99,7 +99,7 @@ __global__ void __launch_bounds__(kFewThreads) embed_few_kernel(const EmbedArgs 
   __shared__ int s_count[kFewTile];
   const int tile = blockIdx.x % tiles, chunk = blockIdx.x / tiles, r0 = tile * kFewTile;
   for (int k = threadIdx.x; k < a.R; k += kFewThreads) {
-    const int token = __ldg(a.tokens + k);
+    const int token = a.tokens[k];
     const bool in = token >= 0 && token < a.V;
     if (!in && token != a.ignore && blockIdx.x == 0) report(a.err, 1u);
     s_token[k] = in && token != a.ignore ? token : -1;
@@ -245,7 +245,7 @@ __global__ void __launch_bounds__(kRankThreads) embed_rank_kernel(const EmbedArg
 #pragma unroll
     for (int u = 0; u < kRankAhead; ++u) {
       const int r = rb + u * kRankThreads;
-      token[u] = r < a.R ? __ldg(a.tokens + r) : 0;
+      token[u] = r < a.R ? a.tokens[r] : 0;
     }
 #pragma unroll
     for (int u = 0; u < kRankAhead; ++u) {
@@ -323,7 +323,7 @@ __global__ void __launch_bounds__(kRadixThreads) embed_count_kernel(const EmbedA
   for (int64_t rb = r0 + threadIdx.x; rb < r1; rb += kRadixThreads * kRound) {
     int token[kRound];
 #pragma unroll
-    for (int u = 0; u < kRound; ++u) token[u] = rb + u * kRadixThreads < r1 ? __ldg(a.tokens + rb + u * kRadixThreads) : 0;
+    for (int u = 0; u < kRound; ++u) token[u] = rb + u * kRadixThreads < r1 ? a.tokens[rb + u * kRadixThreads] : 0;
 #pragma unroll
     for (int u = 0; u < kRound; ++u) {
       if (rb + u * kRadixThreads >= r1) break;
@@ -383,7 +383,7 @@ __global__ void __launch_bounds__(kRadixThreads) embed_move_kernel(const EmbedAr
 #pragma unroll
     for (int u = 0; u < kRound; ++u) {
       const int64_t r = rb + 32 * u + lane;
-      key[u] = r < w1 ? (FIRST ? (unsigned)__ldg(a.tokens + r) : __ldcg(key_in + r)) : 0;
+      key[u] = r < w1 ? (FIRST ? (unsigned)a.tokens[r] : __ldcg(key_in + r)) : 0;
     }
     if (FIRST)
 #pragma unroll

@@ -8,7 +8,9 @@ namespace {
 // Waits for the end of the launch before, then lets the next one of the stream take
 // its place on the GPU: the first thing in a kernel of an early launch.  (The other
 // way about, whole calls would queue up on the SMs behind one another: a gradient of
-// 32768 rows in a graph of such calls took 51 us instead of 32.)
+// 32768 rows in a graph of such calls took 51 us instead of 32.)  Such a kernel
+// has no read-only loads (__ldg): what it reads may be written while its CTAs are
+// already there, and the wait orders ordinary loads alone.
 __device__ __forceinline__ void wait_for_previous() {
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");

@@ -23,24 +23,24 @@ __device__ __forceinline__ void params(const void* p, int dtype, int j, float (&
     if constexpr (VE % 4 == 0) {
 #pragma unroll
       for (int k = 0; k < VE; k += 4) {
-        const float4 v = __ldg(reinterpret_cast<const float4*>(q + k));
+        const float4 v = *reinterpret_cast<const float4*>(q + k);
         f[k] = v.x; f[k + 1] = v.y; f[k + 2] = v.z; f[k + 3] = v.w;
       }
     } else {
 #pragma unroll
-      for (int k = 0; k < VE; ++k) f[k] = __ldg(q + k);
+      for (int k = 0; k < VE; ++k) f[k] = q[k];
     }
   } else {
     const uint16_t* q = static_cast<const uint16_t*>(p) + j;
     if constexpr (VE % 4 == 0) {
 #pragma unroll
       for (int k = 0; k < VE; k += 4) {
-        const uint2 v = __ldg(reinterpret_cast<const uint2*>(q + k));
+        const uint2 v = *reinterpret_cast<const uint2*>(q + k);
         f[k] = bf_lo(v.x); f[k + 1] = bf_hi(v.x); f[k + 2] = bf_lo(v.y); f[k + 3] = bf_hi(v.y);
       }
     } else {
 #pragma unroll
-      for (int k = 0; k < VE; ++k) f[k] = __uint_as_float((uint32_t)__ldg(q + k) << 16);
+      for (int k = 0; k < VE; ++k) f[k] = __uint_as_float((uint32_t)q[k] << 16);
     }
   }
 }
@@ -235,8 +235,10 @@ __global__ void __launch_bounds__(32 * W) norm_kernel(const NormArgs a) {
       else if (a.weight) h[k][j] = M::mul(h[k][j], M::of(w[q], j));
       else if (a.bias) h[k][j] = M::add(h[k][j], M::of(b[q], j));
     }
-    y[v] = M::template put<T>(h[k]);
   }
+#pragma unroll
+  for (int k = 0; k < NV; ++k)                       // (apart: no load above waits for a store)
+    if (t + 32 * W * k < nvec) y[t + 32 * W * k] = M::template put<T>(h[k]);
 }
 
 // rows of over 32768 entries, which do not fit: a CTA a row, read three times (from L2)
@@ -492,7 +494,7 @@ __global__ void __launch_bounds__(cta_threads(W), grad_ctas(W, kCols)) norm_back
   };
 #pragma unroll
   for (int k = 0; k < kStages - 1; ++k) request(first + k * step, k);
-  float mean = first < a.R ? __ldg(a.mean_in + first) : 0.f, rstd = first < a.R ? __ldg(a.rstd_in + first) : 0.f;
+  float mean = first < a.R ? a.mean_in[first] : 0.f, rstd = first < a.R ? a.rstd_in[first] : 0.f;
   N w[NV][kN], dw[NV][kN], db[NV][kN];
 #pragma unroll
   for (int k = 0; k < NV; ++k) {
@@ -518,8 +520,8 @@ __global__ void __launch_bounds__(cta_threads(W), grad_ctas(W, kCols)) norm_back
     const float r = rstd;
     const N m = M::all(-mean), rs = M::all(r);
     if (row + step < a.R) {
-      mean = __ldg(a.mean_in + row + step);
-      rstd = __ldg(a.rstd_in + row + step);
+      mean = a.mean_in[row + step];
+      rstd = a.rstd_in[row + step];
     }
     N h[NV][kN], g[NV][kN], s1 = M::all(0.f), s2 = M::all(0.f);
 #pragma unroll
@@ -598,8 +600,14 @@ __global__ void __launch_bounds__(32 * kJoinWarps) norm_join_kernel(const NormAr
   s_part[warp][lane] = v;
   __syncthreads();
   if (warp || j >= a.d) return;
+  float sum[kJoinWarps];                             // in pairs: one after another is 1.4e-7 off, not 0.9e-7, at R = 333
 #pragma unroll
-  for (int k = 1; k < kJoinWarps; ++k) v += s_part[k][lane];
+  for (int k = 0; k < kJoinWarps; ++k) sum[k] = s_part[k][lane];
+#pragma unroll
+  for (int o = kJoinWarps / 2; o; o >>= 1)
+#pragma unroll
+    for (int k = 0; k < o; ++k) sum[k] += sum[k + o];
+  v = sum[0];
   if (a.wdtype == 0) static_cast<float*>(out)[j] = v;
   else static_cast<__nv_bfloat16*>(out)[j] = __float2bfloat16_rn(v);
 }
