@@ -612,6 +612,126 @@ __global__ void __launch_bounds__(32 * kJoinWarps) norm_join_kernel(const NormAr
   else static_cast<__nv_bfloat16*>(out)[j] = __float2bfloat16_rn(v);
 }
 
+// ---- gradients of few rows ---------------------------------------------------------------
+// One launch, nothing joined: the first `cols` CTAs have kFewCols vectors of columns
+// each and all rows' sums of them (32 rows at once, eight of a thread requested
+// together), the others a row of d_x each.  Inputs are read twice, the second time
+// from L2; a few loads in a row bound it.
+constexpr int kFewCols = 8, kFewLanes = 32, kFewThreads = kFewCols * kFewLanes, kFewAhead = 8;
+template <typename T, int VE>
+__global__ void __launch_bounds__(kFewThreads) norm_backward_few_kernel(const NormArgs a, int cols) {
+  using V = RowVec<T, VE>;
+  using Raw = typename V::Raw;
+  using M = Num<VE>;
+  using N = typename M::N;
+  constexpr int kN = M::kN, NV = 8 / VE, W = kFewThreads / 32;
+  __shared__ float s_sum[2 * W];
+  __shared__ float s_col[2][kFewLanes][kFewCols * VE + 1];
+  wait_for_previous();
+  const int nvec = a.d / VE, t = threadIdx.x;
+  const Raw* xs = static_cast<const Raw*>(a.x);
+  const Raw* gs = static_cast<const Raw*>(a.d_y);
+  if ((int)blockIdx.x < cols) {
+    const int v = blockIdx.x * kFewCols + t % kFewCols, lane = t / kFewCols;
+    N w[kN], b[kN];
+#pragma unroll
+    for (int j = 0; j < kN; ++j) w[j] = b[j] = M::all(0.f);
+    if (v < nvec)
+#pragma unroll 1
+      for (int r0 = lane; r0 < a.R; r0 += kFewLanes * kFewAhead) {
+        Raw x[kFewAhead], y[kFewAhead];
+        float mean[kFewAhead], rstd[kFewAhead];
+#pragma unroll
+        for (int u = 0; u < kFewAhead; ++u) {
+          const int r = r0 + u * kFewLanes;
+          x[u] = y[u] = V::zero();
+          mean[u] = rstd[u] = 0.f;
+          if (r < a.R) {
+            x[u] = xs[(size_t)r * nvec + v];
+            y[u] = gs[(size_t)r * nvec + v];
+            mean[u] = a.mean_in[r];
+            rstd[u] = a.rstd_in[r];
+          }
+        }
+#pragma unroll
+        for (int u = 0; u < kFewAhead; ++u) {
+          N h[kN], g[kN];
+          M::template get<T>(x[u], h);
+          M::template get<T>(y[u], g);
+          const N m = M::all(-mean[u]), rs = M::all(rstd[u]);
+#pragma unroll
+          for (int j = 0; j < kN; ++j) {
+            w[j] = M::fma(g[j], M::mul(M::add(h[j], m), rs), w[j]);
+            b[j] = M::add(b[j], g[j]);
+          }
+        }
+      }
+#pragma unroll
+    for (int j = 0; j < kN; ++j) {
+      M::to(w[j], &s_col[0][lane][t % kFewCols * VE + VE / kN * j]);
+      M::to(b[j], &s_col[1][lane][t % kFewCols * VE + VE / kN * j]);
+    }
+    __syncthreads();
+    const int which = t / (kFewCols * VE), c = t % (kFewCols * VE), j = blockIdx.x * (kFewCols * VE) + c;
+    void* out = which ? a.d_bias : a.d_weight;
+    if (which > 1 || j >= a.d || !out) return;
+    float sum[kFewLanes];                            // in pairs, as norm_join_kernel
+#pragma unroll
+    for (int k = 0; k < kFewLanes; ++k) sum[k] = s_col[which][k][c];
+#pragma unroll
+    for (int o = kFewLanes / 2; o; o >>= 1)
+#pragma unroll
+      for (int k = 0; k < o; ++k) sum[k] += sum[k + o];
+    if (a.wdtype == 0) static_cast<float*>(out)[j] = sum[0];
+    else static_cast<__nv_bfloat16*>(out)[j] = __float2bfloat16_rn(sum[0]);
+    return;
+  }
+  const int row = blockIdx.x - cols;
+  xs += (size_t)row * nvec;
+  gs += (size_t)row * nvec;
+  Raw x[NV], y[NV];
+  float w[NV][VE];
+#pragma unroll
+  for (int k = 0; k < NV; ++k) {
+    const int v = t + kFewThreads * k;
+    x[k] = y[k] = V::zero();
+#pragma unroll
+    for (int j = 0; j < VE; ++j) w[k][j] = 1.f;
+    if (v < nvec) {
+      x[k] = xs[v];
+      y[k] = gs[v];
+      if (a.weight) params<VE>(a.weight, a.wdtype, v * VE, w[k]);
+    }
+  }
+  const float r = a.rstd_in[row], over_d = 1.f / a.d;
+  const N m = M::all(-a.mean_in[row]), rs = M::all(r);
+  N h[NV][kN], g[NV][kN], s1 = M::all(0.f), s2 = M::all(0.f);
+#pragma unroll
+  for (int k = 0; k < NV; ++k)
+    if (t + kFewThreads * k < nvec) {
+      M::template get<T>(x[k], h[k]);
+      M::template get<T>(y[k], g[k]);
+#pragma unroll
+      for (int j = 0; j < kN; ++j) {
+        h[k][j] = M::mul(M::add(h[k][j], m), rs);
+        g[k][j] = M::mul(g[k][j], M::of(w[k], j));
+        s1 = M::add(s1, g[k][j]);
+        s2 = M::fma(g[k][j], h[k][j], s2);
+      }
+    }
+  float s[2] = {M::sum(s1), M::sum(s2)};
+  row_sums<2, W>(s, s_sum);
+  const N m1 = M::all(-s[0] * over_d * r), m2 = M::all(-s[1] * over_d * r);
+  Raw* d_x = static_cast<Raw*>(a.d_x) + (size_t)row * nvec;
+#pragma unroll
+  for (int k = 0; k < NV; ++k)
+    if (t + kFewThreads * k < nvec) {
+#pragma unroll
+      for (int j = 0; j < kN; ++j) g[k][j] = M::fma(h[k][j], m2, M::fma(g[k][j], rs, m1));
+      d_x[t + kFewThreads * k] = M::template put<T>(g[k]);
+    }
+}
+
 constexpr int kWideCols = 8192;
 // rows of over kWideCols columns: d_x by a CTA a row, the sums over rows by a CTA 32 vectors of columns; both read
 // both inputs (R = 2048 d = 16384 bf16 113 us, 1.8 TB/s of what is needed)
@@ -722,6 +842,10 @@ int part_count(int R, int d) {
 // us, 608 3.01 and 3.03, 1216 4.52 and 4.12; d = 1001 608 3.98 and 6.23, 1216 6.18 and 6.64.  Narrower and wider rows go
 // to the latter always (R = 16 d = 256 1.93 against 2.01, d = 4096 2.48 against 2.69).
 constexpr int kFewRows = 608;
+// Up to this many rows of up to 2048 entries norm_backward_few_kernel, else the grid that stays and its join, bf16: R = 16
+// d = 1024 1.5 against 3.8 us, R = 333 d = 1001 3.8 and 4.8, R = 608 d = 64 3.7 and 3.6, d = 2048 4.4 and 9.5; R = 900
+// d = 64 4.7 and 4.1, d = 1001 6.1 and 7.0, R = 1216 d = 1001 7.6 and 6.1.
+constexpr int kFewGradRows = 608, kFewGradCols = 2048;
 template <typename T, int VE, int kCols, int W>
 cudaError_t launch_many(const NormArgs& a, cudaStream_t s) {
   constexpr int smem = kNormStages * cta_groups(W) * staged_bytes(W, kCols, sizeof(T));
@@ -767,6 +891,11 @@ cudaError_t launch_gradients(const NormArgs& a, int parts, cudaStream_t s) {
   }
 }
 template <typename T, int VE>
+cudaError_t launch_few_gradients(const NormArgs& a, cudaStream_t s) {
+  const int cols = a.d_weight || a.d_bias ? ceil_div(a.d / VE, kFewCols) : 0;
+  return launch(true, norm_backward_few_kernel<T, VE>, cols + (a.d_x ? a.R : 0), kFewThreads, 0, s, a, cols);
+}
+template <typename T, int VE>
 cudaError_t launch_wide_gradients(const NormArgs& a, int parts, cudaStream_t s) {
   cudaError_t e = a.d_x ? launch(true, norm_wide_dx_kernel<T, VE>, a.R, kWide, 0, s, a) : cudaSuccess;
   if (e == cudaSuccess && (a.d_weight || a.d_bias))
@@ -787,6 +916,8 @@ cudaError_t launch_norm(const NormArgs& a, cudaStream_t s) {
 }
 
 cudaError_t launch_norm_backward(const NormArgs& a, cudaStream_t s) {
+  if (a.R <= kFewGradRows && a.d <= kFewGradCols)
+    return by_row_type(a.dtype, a.d, [&](auto t) { return launch_few_gradients<typename decltype(t)::T, decltype(t)::VE>(a, s); });
   const int parts = part_count(a.R, a.d);
   const cudaError_t e = by_row_type(a.dtype, a.d, [&](auto t) {
     using Row = decltype(t);

@@ -122,6 +122,46 @@ def test_norm_and_gradients(cmsd, R, d, dtype, wdtype):
     _check_grads(gr, x, w, o["mean"], o["rstd"], d_y)
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("R,d", [(255, 2048), (256, 2047), (257, 2046), (608, 2048), (608, 65), (609, 2048), (609, 65), (608, 2050)])
+def test_gradients_about_the_rows_of_one_launch(cmsd, R, d, dtype):
+    """Rows about those that a thread requests at once, and about the most that are summed without a join."""
+    x, w, b, d_y = _inputs(R, d, dtype, F32, seed=3)
+    o = cmsd.layernorm(x, w, b, eps=EPS)
+    _check_grads(cmsd.layernorm_backward(x, w, o["mean"], o["rstd"], d_y), x, w, o["mean"], o["rstd"], d_y)
+
+
+@pytest.mark.parametrize("R", [3, 700])
+def test_captured_behind_another_stream(cmsd, R):
+    """In a graph, calls that wait for the launch before and for another stream's work at once."""
+    d = 264
+    x, w, b, d_y = _inputs(R, d, BF16, F32, seed=4)
+    ref = cmsd.layernorm(x, w, b)
+    want = cmsd.layernorm_backward(x, w, ref["mean"], ref["rstd"], d_y)
+    src, src_y = x.clone(), d_y.clone()
+    x.zero_()
+    d_y.zero_()
+    out = {k: torch.empty_like(v) for k, v in {**ref, **want}.items()}
+    ws = cmsd.layernorm_backward_workspace(R, d)
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        main = torch.cuda.current_stream()
+        side.wait_stream(main)
+        with torch.cuda.stream(side):
+            d_y.copy_(src_y)
+        x.copy_(src)
+        cmsd.layernorm(x, w, b, out=out)
+        main.wait_stream(side)
+        cmsd.layernorm_backward(x, w, out["mean"], out["rstd"], d_y, out=out, ws=ws)
+        cmsd.dropout(out["d_x"], 0.0, 1, out={"y": x})
+    for _ in range(2):
+        graph.replay()
+        torch.cuda.synchronize()
+        for k in out:
+            assert torch.equal(out[k], {**ref, **want}[k]), k
+        assert torch.equal(x, want["d_x"])
+
+
 @pytest.mark.parametrize("R,d", [(1, 16), (70, 1000), (300, 2048), (40, 1001), (9, 20000)])
 @pytest.mark.parametrize("dtype", [F32, BF16])
 def test_without_parameters(cmsd, R, d, dtype):
