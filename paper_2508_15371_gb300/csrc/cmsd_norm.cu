@@ -575,12 +575,21 @@ __global__ void __launch_bounds__(cta_threads(W), grad_ctas(W, kCols)) norm_back
     if (group == 0) {
 #pragma unroll
       for (int k = 0; k < NV; ++k)
-        if (in_row<W, NV>(t, k, nvec))
+        if (in_row<W, NV>(t, k, nvec)) {
 #pragma unroll
-          for (int j = 0; j < VE; ++j) {
+          for (int j = 0; j < VE; ++j)
             for (int q = 1; q < kGroups; ++q) sum[k][j] += s_col[(k * VE + j) * kThreads + 32 * W * q + t];
-            part[which * a.d + (t + 32 * W * k) * VE + j] = sum[k][j];
+          float* p = part + which * a.d + (t + 32 * W * k) * VE;
+          if constexpr (VE % 4 == 0) {                // (one by one, each to a sector of its own: R = 4096 d = 2048 17.4 us instead of 14.3)
+#pragma unroll
+            for (int j = 0; j < VE; j += 4)
+              *reinterpret_cast<float4*>(p + j) = make_float4(sum[k][j], sum[k][j + 1], sum[k][j + 2], sum[k][j + 3]);
+          } else if constexpr (VE == 2) {
+            *reinterpret_cast<float2*>(p) = make_float2(sum[k][0], sum[k][1]);
+          } else {
+            *p = sum[k][0];
           }
+        }
     }
   }
 }
