@@ -559,7 +559,7 @@ def _result(out, name, shape, dtype, like, cur):
         if not _fits(t, shape, dtype, cur):
             _need(cur, ((t, shape, dtype, name),))
         return t
-    return like.new_empty(shape) if like.dtype is dtype else like.new_empty(shape, dtype=dtype)
+    return _torch_mod.empty(shape, dtype=dtype, device=like.device)
 
 
 def embedding(tokens, table, scale=1.0, ignore_index=-100, out=None):

@@ -7,6 +7,7 @@
 #include <cuda_bf16.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "cmsd_device.cuh"
 #include "cmsd_errors.cuh"
@@ -53,6 +54,46 @@ __global__ void __launch_bounds__(256) embed_kernel(const EmbedArgs a, int piece
   }
 }
 
+// Narrow rows, many of them: a warp 256 vectors of x in a row, whatever rows they are of.  R = 32768 d = 64 bf16
+// 2.8 us, a warp a row 7.6; R = 600000 18 and 143; R = 16384 d = 512 4.8 and 5.0; 6000 d = 64 2.7 and 2.2.
+constexpr int kNarrowVecs = 64, kNarrowRows = 8192;
+template <typename T, int VE>
+__global__ void __launch_bounds__(256) embed_narrow_kernel(const EmbedArgs a) {
+  using V = RowVec<T, VE>;
+  using Raw = typename V::Raw;
+  wait_for_previous();
+  const int lane = threadIdx.x & 31, nvec = a.d / VE;
+  const int64_t all = (int64_t)a.R * nvec, step = (int64_t)gridDim.x * 256 * kAhead;
+  for (int64_t q0 = ((int64_t)blockIdx.x * 8 + (threadIdx.x >> 5)) * 32 * kAhead; q0 < all; q0 += step) {
+    const int r0 = (int)(q0 / nvec), v0 = (int)(q0 % nvec) + lane;
+    int token[kAhead], v[kAhead];
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      const int i = v0 + 32 * k, r = (int)((unsigned)i / (unsigned)nvec);
+      v[k] = q0 + lane + 32 * k < all ? i - r * nvec : -1;
+      token[k] = v[k] >= 0 ? a.tokens[r0 + r] : a.ignore;
+    }
+    Raw w[kAhead];
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      const bool in = token[k] >= 0 && token[k] < a.V;
+      if (!in && token[k] != a.ignore && v[k] == 0) report(nullptr, 1u);
+      if (!in || token[k] == a.ignore) token[k] = -1;
+      w[k] = V::zero();
+      if (token[k] >= 0) w[k] = static_cast<const Raw*>(a.table)[(size_t)token[k] * nvec + v[k]];
+    }
+    Raw* x = static_cast<Raw*>(a.x) + q0 + lane;
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      float f[VE];
+      V::get(w[k], f);
+#pragma unroll
+      for (int j = 0; j < VE; ++j) f[j] *= a.scale;
+      if (v[k] >= 0) x[32 * k] = token[k] >= 0 ? V::put(f) : V::zero();
+    }
+  }
+}
+
 // ---- few rows ----------------------------------------------------------------------------
 // All in one launch, nothing put in order: every CTA has all tokens in shared
 // memory.  CTAs of kFewTile rows look up which of theirs come first of their token,
@@ -83,14 +124,50 @@ __global__ void __launch_bounds__(kFewThreads) embed_few_kernel(const EmbedArgs 
       if (token != a.ignore && token >= v0 && token - v0 < n) s_there[token - v0] = 1;
     }
     __syncthreads();
-    Raw* out = static_cast<Raw*>(a.d_table) + (size_t)v0 * nvec;
-    if (nvec >= kFewThreads) {
-      for (int c = 0; c < n; ++c)
-        if (!s_there[c])
-          for (int j = threadIdx.x; j < nvec; j += kFewThreads) out[(size_t)c * nvec + j] = V::zero();
+    if constexpr (VE * sizeof(T) == 16) {
+      Raw* out = static_cast<Raw*>(a.d_table) + (size_t)v0 * nvec;
+      if (nvec >= kFewThreads) {
+        for (int c = 0; c < n; ++c)
+          if (!s_there[c])
+            for (int j = threadIdx.x; j < nvec; j += kFewThreads) out[(size_t)c * nvec + j] = V::zero();
+      } else {
+        for (int j = threadIdx.x; j < n * nvec; j += kFewThreads)
+          if (!s_there[j / nvec]) out[j] = V::zero();
+      }
     } else {
-      for (int j = threadIdx.x; j < n * nvec; j += kFewThreads)
-        if (!s_there[j / nvec]) out[j] = V::zero();
+      // 16-byte pieces wherever one is of these rows and of none with a sum, entries in the others
+      constexpr int kPiece = 16 / (int)sizeof(T);
+      const size_t first = (size_t)v0 * a.d;
+      if (a.d >= kPiece * kFewThreads / 2) {         // row by row: the pieces within it, and its ends
+        for (int c = 0; c < n; ++c) {
+          if (s_there[c]) continue;
+          const size_t at = first + (size_t)c * a.d;
+          T* out = static_cast<T*>(a.d_table) + at;
+          const int front = (int)(-at % kPiece), pieces = (a.d - front) / kPiece, back = front + pieces * kPiece;
+          for (int j = threadIdx.x; j < pieces; j += kFewThreads)
+            *reinterpret_cast<uint4*>(out + front + j * kPiece) = make_uint4(0, 0, 0, 0);
+          if ((int)threadIdx.x < front) out[threadIdx.x] = from_float<T>(0.f);
+          else if ((int)threadIdx.x >= kFewThreads - kPiece && back + (int)threadIdx.x - (kFewThreads - kPiece) < a.d)
+            out[back + threadIdx.x - (kFewThreads - kPiece)] = from_float<T>(0.f);
+        }
+        return;
+      }
+      const int lead = (int)(first % kPiece), all = n * a.d;           // (below 2^17: kFewFill bytes, or one row)
+      T* out = static_cast<T*>(a.d_table) + first;
+      for (int e0 = threadIdx.x * kPiece - lead; e0 < all; e0 += kFewThreads * kPiece) {
+        const int begin = e0 > 0 ? e0 : 0, end = e0 + kPiece < all ? e0 + kPiece : all, last = (end - 1) / a.d;
+        int c = begin / a.d;
+        bool none = true;
+        for (int q = c; q <= last; ++q) none = none && !s_there[q];
+        if (none && end - begin == kPiece) {
+          *reinterpret_cast<uint4*>(out + e0) = make_uint4(0, 0, 0, 0);
+        } else {
+          for (int e = begin; e < end; ++e) {
+            if (e >= (c + 1) * a.d) ++c;
+            if (!s_there[c]) out[e] = from_float<T>(0.f);
+          }
+        }
+      }
     }
     return;
   }
@@ -224,10 +301,10 @@ __device__ __forceinline__ void fill(const EmbedArgs& a, size_t first, size_t la
 // Few rows: each row's place is the number of rows before it in (token, row)
 // order, counted by comparing it with all of them: R^2 comparisons of two
 // instructions, spread over the GPU, in one launch.  A warp RPW rows, a lane every
-// 32nd four of the others.  d_x of R x 1024 added to a table, sums and all: R = 4096
-// 12.9 us (in passes of the radix sort below 22.8), 8192 19.3 (25.9), 12288 29.3
-// (28.4); written whole, d = 2048, 4096 81.3 us (81.9), 8192 90.6 (85.2).
-constexpr int kRankRows = 8192;
+// 32nd four of the others.  The whole gradient, R x 1024 of 32000 bf16 added to:
+// R = 4096 11.9 us (in passes of the radix sort below 16.9), 6000 15.1 (17.3), 8192
+// 18.6 (18.4); written whole 18.8 (20.7), 21.0 (22.1), 24.4 (22.9).
+constexpr int kRankRows = 7168;
 constexpr int kRankThreads = 256;
 constexpr int kRankAhead = 16;                       // tokens of a thread requested at once
 template <int RPW>
@@ -308,8 +385,12 @@ __global__ void __launch_bounds__(kRankThreads) embed_rank_kernel(const EmbedArg
 // 525 MB of zeros, which take 77 at a copy's rate.
 constexpr int kRadixBits = 10;
 constexpr int kRadixThreads = 256, kRadixWarps = kRadixThreads / 32;
-constexpr int kTileMin = 2048;
+// Tiles of fewer rows where there are few, so that more SMs take part while a batch or two still has all tiles' counts.
+// R x d of V: 8192 x 1024 of 32000 with tiles of 512 22.5 us, of 1024 23.4; 16384 26.8 and 27.8; 25000 x 1024 of 5000 with
+// 1024 30.0, with 2048 31.9; 32768 of 1000 29.7 and 28.8.
+constexpr int kTileMin = 2048, kShortRows = 16384;
 constexpr int kRound = 8;                            // rows of a lane requested at once
+constexpr int kCountsAhead = 32;                     // counts of a thread (one by one, 20000 rows of 64 took 30.5 us, not 22.1)
 __global__ void __launch_bounds__(kRadixThreads) embed_count_kernel(const EmbedArgs a, int digits, int tiles) {
   extern __shared__ int s_count[];
   wait_for_previous();
@@ -402,23 +483,32 @@ __global__ void __launch_bounds__(kRadixThreads) embed_move_kernel(const EmbedAr
   // the first place of each (warp, digit): digits below, the same one in earlier tiles, in earlier warps;
   // a thread up to four neighbouring digits
   const int per = (digits + kRadixThreads - 1) / kRadixThreads;
-  int all[4], before[4], sum = 0;
+  int all[4] = {}, before[4] = {}, sum = 0;
+  const auto counts = [&](auto p) {
+    constexpr int PER = decltype(p)::value, kTiles = kCountsAhead / PER;
+    for (int t0 = 0; t0 < tiles; t0 += kTiles) {
+      int c[kTiles][PER];
 #pragma unroll
-  for (int q = 0; q < 4; ++q) {
-    all[q] = before[q] = 0;
-    const int g = threadIdx.x * per + q;
-    if (q >= per || g >= digits) continue;
-    int b = 0, rest = 0;
-#pragma unroll 16
-    for (int t = 0; t < tiles; ++t) {
-      const int c = __ldcg(count + (size_t)t * digits + g);
-      if (t < (int)blockIdx.x) b += c;
-      else rest += c;
+      for (int u = 0; u < kTiles; ++u)
+#pragma unroll
+        for (int q = 0; q < PER; ++q) {
+          const int g = threadIdx.x * PER + q;
+          c[u][q] = g < digits && t0 + u < tiles ? __ldcg(count + (size_t)(t0 + u) * digits + g) : 0;
+        }
+#pragma unroll
+      for (int u = 0; u < kTiles; ++u)
+#pragma unroll
+        for (int q = 0; q < PER; ++q) {
+          all[q] += c[u][q];
+          if (t0 + u < (int)blockIdx.x) before[q] += c[u][q];
+        }
     }
-    before[q] = b;
-    all[q] = b + rest;
-    sum += all[q];
-  }
+  };
+  if (per == 1) counts(std::integral_constant<int, 1>());
+  else if (per == 2) counts(std::integral_constant<int, 2>());
+  else counts(std::integral_constant<int, 4>());
+#pragma unroll
+  for (int q = 0; q < 4; ++q) sum += all[q];
   int base = cta_scan(sum);
 #pragma unroll
   for (int q = 0; q < 4; ++q) {
@@ -569,13 +659,14 @@ __global__ void __launch_bounds__(kSumThreads) embed_sum_kernel(const EmbedArgs 
 constexpr int kJoinThreads = 256, kJoinWarps = kJoinThreads / 32;
 constexpr int kJoinTiles = 8;
 constexpr int kLong = 16;
+constexpr int kPieces = 8;                            // requested at once
 template <int JV>
-__device__ __forceinline__ void add_piece(const float* p, float (&sum)[JV]) {
+__device__ __forceinline__ void get_piece(const float* p, float (&f)[JV]) {
   if constexpr (JV == 4) {
     const float4 v = __ldcg(reinterpret_cast<const float4*>(p));
-    sum[0] += v.x; sum[1] += v.y; sum[2] += v.z; sum[3] += v.w;
+    f[0] = v.x; f[1] = v.y; f[2] = v.z; f[3] = v.w;
   } else {
-    sum[0] += __ldcg(p);
+    f[0] = __ldcg(p);
   }
 }
 template <typename T, int JV, bool ADD>
@@ -604,8 +695,17 @@ __global__ void __launch_bounds__(kJoinThreads) embed_join_kernel(const EmbedArg
   const auto sums = [&](int first, int k0, int k1, int n, int j, float (&sum)[JV]) {   // pieces k0 .. k1 of 0 .. n + 1
 #pragma unroll
     for (int q = 0; q < JV; ++q) sum[q] = 0.f;
-#pragma unroll 8
-    for (int k = k0; k < k1; ++k) add_piece<JV>((k <= n ? a.tail : a.head) + (size_t)(first + k) * a.d + j, sum);
+    for (int kb = k0; kb < k1; kb += kPieces) {
+      float p[kPieces][JV];
+#pragma unroll
+      for (int u = 0; u < kPieces; ++u)
+        if (kb + u < k1) get_piece<JV>((kb + u <= n ? a.tail : a.head) + (size_t)(first + kb + u) * a.d + j, p[u]);
+#pragma unroll
+      for (int u = 0; u < kPieces; ++u)
+#pragma unroll
+        for (int q = 0; q < JV; ++q)
+          if (kb + u < k1) sum[q] += p[u][q];
+    }
   };
   const auto write = [&](int token, int j, const float (&sum)[JV]) {
     T* out = static_cast<T*>(a.d_table) + (size_t)token * a.d + j;
@@ -670,7 +770,7 @@ size_t embed_layout(EmbedArgs& a, char* w) {
   while (((int64_t)1 << bits) <= a.V) ++bits;         // keys 0 .. V
   a.passes = R <= kRankRows ? 1 : ceil_div(bits, kRadixBits);
   a.bits = ceil_div(bits, a.passes);
-  a.tile = kTileMin * ceil_div(R, (int64_t)kTileMin * 256);
+  a.tile = R <= kShortRows ? kTileMin / 4 : R < 2 * kShortRows ? kTileMin / 2 : kTileMin * ceil_div(R, (int64_t)kTileMin * 256);
   for (int k = 0; k < (a.passes > 1 ? 2 : 1); ++k) {
     a.key[k] = (unsigned*)take((size_t)R * 4);
     a.order[k] = (int*)take((size_t)R * 4);
@@ -691,6 +791,11 @@ cudaError_t launch_embed(const EmbedArgs& a, cudaStream_t s) {
     using Row = decltype(t);
     const int pieces = ceil_div(a.d / Row::VE, 32 * kAhead);
     const int64_t units = (int64_t)a.R * pieces;
+    if constexpr (Row::VE * sizeof(typename Row::T) == 16)
+      if (a.d / Row::VE <= kNarrowVecs && a.R >= kNarrowRows) {
+        const int64_t ctas = ((int64_t)a.R * (a.d / Row::VE) + 256 * kAhead - 1) / (256 * kAhead);
+        return launch(true, embed_narrow_kernel<typename Row::T, Row::VE>, (unsigned)(ctas < (1 << 30) ? ctas : 1 << 30), 256, 0, s, a);
+      }
     // a warp a CTA until every SM has some, then eight
     int warps = 1;
     while (warps < 8 && units > 304 * warps) warps *= 2;

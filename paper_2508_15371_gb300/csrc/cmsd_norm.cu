@@ -595,7 +595,7 @@ __global__ void __launch_bounds__(cta_threads(W), grad_ctas(W, kCols)) norm_back
 }
 
 // a CTA 32 columns of one of the two, each of its warps a part of the CTAs' sums
-constexpr int kJoinWarps = 32;
+constexpr int kJoinWarps = 32, kJoinAhead = 10;         // (10 parts of a warp requested at once: all of 304)
 __global__ void __launch_bounds__(32 * kJoinWarps) norm_join_kernel(const NormArgs a, int parts) {
   __shared__ float s_part[kJoinWarps][32];
   const int lane = threadIdx.x & 31, j = blockIdx.x * 32 + lane, which = blockIdx.y, warp = threadIdx.x >> 5;
@@ -604,8 +604,16 @@ __global__ void __launch_bounds__(32 * kJoinWarps) norm_join_kernel(const NormAr
   if (!out) return;
   float v = 0.f;
   if (j < a.d)
-#pragma unroll 8
-    for (int p = warp; p < parts; p += kJoinWarps) v += __ldcg(a.part + ((size_t)p * 2 + which) * a.d + j);
+    for (int p0 = warp; p0 < parts; p0 += kJoinWarps * kJoinAhead) {
+      float x[kJoinAhead];
+#pragma unroll
+      for (int u = 0; u < kJoinAhead; ++u) {
+        const int p = p0 + u * kJoinWarps;
+        x[u] = p < parts ? __ldcg(a.part + ((size_t)p * 2 + which) * a.d + j) : 0.f;
+      }
+#pragma unroll
+      for (int u = 0; u < kJoinAhead; ++u) v += x[u];
+    }
   s_part[warp][lane] = v;
   __syncthreads();
   if (warp || j >= a.d) return;

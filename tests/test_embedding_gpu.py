@@ -119,6 +119,21 @@ def test_wide_rows(cmsd, R, d, V, dtype):
     _check_table(cmsd.embedding_backward(tokens, d_x, V)["d_table"], tokens, d_x, V, 1.0)
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("R,d,V", [(8191, 64, 900), (8192, 64, 900), (8193, 512, 40), (9001, 504, 3000), (40000, 8, 70000), (8200, 520, 50),
+                                   (12001, 256, 2000), (7168, 64, 900), (7169, 64, 900), (16384, 24, 40),
+                                   (16385, 24, 40), (32767, 24, 3000), (32768, 24, 3000)])
+def test_narrow_rows(cmsd, R, d, V, dtype):
+    """Many rows of up to 64 vectors, which are looked up whatever row a vector is of, and one that is wider."""
+    tokens = _tokens(R, V, _gen(R, 9), ignored=0.2)
+    tokens[5], tokens[R - 1], tokens[0] = V, -1, 0
+    table, d_x = (torch.randn(n, d, generator=_gen(d, 9), device="cuda").to(dtype) for n in (V, R))
+    _check_rows(cmsd.embedding(tokens, table, scale=1.5)["x"], tokens, table, 1.5)
+    assert cmsd.embedding_errors() == 1
+    _check_table(cmsd.embedding_backward(tokens, d_x, V, scale=1.5)["d_table"], tokens, d_x, V, 1.5)
+    assert cmsd.embedding_errors() == 1
+
+
 @pytest.mark.parametrize("R,V", [(8192, 300), (600011, 40), (8193, 1 << 20), (9000, (1 << 21) + 5), (530000, 3000), (10000, 1)])
 def test_many_rows_and_tokens(cmsd, R, V):
     """Ordering with over 2048 rows a CTA, with two and three passes, and of one token alone."""
@@ -143,6 +158,19 @@ def test_the_largest_vocabulary(cmsd):
     want = torch.zeros(rows.numel(), dtype=torch.float64, device="cuda").index_add_(0, at, d_x[:, 0].double())
     assert torch.equal(got[rows, 0].double(), want)                  # small whole numbers: exact
     assert int(torch.count_nonzero(got)) == rows.numel() and (out[V:] == 7).all()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("R,d,V", [(400, 129, 20011), (100, 1001, 3001), (512, 3, 100003), (70, 2046, 700), (9, 1, 5000), (300, 130, 301), (5, 65533, 7)])
+def test_zeros_of_rows_off_16_bytes(cmsd, R, d, V, dtype):
+    """Few tokens: what was there goes everywhere, and no sum is written over."""
+    tokens = _tokens(R, V, _gen(R, 8), ignored=0.1)
+    tokens[0] = V - 1
+    d_x = torch.randn(R, d, generator=_gen(d, 8), device="cuda").to(dtype)
+    for _ in range(3):
+        t = torch.full((V, d), 77, dtype=dtype, device="cuda")
+        cmsd.embedding_backward(tokens, d_x, V, out={"d_table": t})
+        _check_table(t, tokens, d_x, V, 1.0)
 
 
 @pytest.mark.parametrize("R", [1, 33, 5000])
