@@ -235,10 +235,8 @@ __global__ void __launch_bounds__(32 * W) norm_kernel(const NormArgs a) {
       else if (a.weight) h[k][j] = M::mul(h[k][j], M::of(w[q], j));
       else if (a.bias) h[k][j] = M::add(h[k][j], M::of(b[q], j));
     }
+    y[v] = M::template put<T>(h[k]);
   }
-#pragma unroll
-  for (int k = 0; k < NV; ++k)                       // (apart: no load above waits for a store)
-    if (t + 32 * W * k < nvec) y[t + 32 * W * k] = M::template put<T>(h[k]);
 }
 
 // rows of over 32768 entries, which do not fit: a CTA a row, read three times (from L2)
@@ -595,7 +593,9 @@ __global__ void __launch_bounds__(cta_threads(W), grad_ctas(W, kCols)) norm_back
 }
 
 // a CTA 32 columns of one of the two, each of its warps a part of the CTAs' sums
-constexpr int kJoinWarps = 32, kJoinAhead = 10;         // (10 parts of a warp requested at once: all of 304)
+// (eight warps or 32 by the parts: 32 of few parts, 1024 x 16384 f32, 8 us more)
+constexpr int kJoinAhead = 10;                       // parts of a warp requested at once
+template <int kJoinWarps>
 __global__ void __launch_bounds__(32 * kJoinWarps) norm_join_kernel(const NormArgs a, int parts) {
   __shared__ float s_part[kJoinWarps][32];
   const int lane = threadIdx.x & 31, j = blockIdx.x * 32 + lane, which = blockIdx.y, warp = threadIdx.x >> 5;
@@ -756,6 +756,7 @@ template <typename T, int VE>
 __global__ void __launch_bounds__(kWide) norm_wide_dx_kernel(const NormArgs a) {
   using V = RowVec<T, VE>;
   using Raw = typename V::Raw;
+  constexpr int kKept = VE == 8 ? 2 : 4;              // a thread's first vectors stay in registers
   __shared__ float s_sum[2 * kWide / 32];
   wait_for_previous();
   const int nvec = a.d / VE;
@@ -763,10 +764,10 @@ __global__ void __launch_bounds__(kWide) norm_wide_dx_kernel(const NormArgs a) {
   const Raw* xs = static_cast<const Raw*>(a.x) + at;
   const Raw* gs = static_cast<const Raw*>(a.d_y) + at;
   const float mean = a.mean_in[blockIdx.x], rstd = a.rstd_in[blockIdx.x], over_d = 1.f / a.d;
-  const auto take = [&](int v, float (&h)[VE], float (&g)[VE]) {
+  const auto values = [&](int v, const Raw& x, const Raw& y, float (&h)[VE], float (&g)[VE]) {
     float w[VE];
-    V::get(xs[v], h);
-    V::get(gs[v], g);
+    V::get(x, h);
+    V::get(y, g);
     if (a.weight) params<VE>(a.weight, a.wdtype, v * VE, w);
 #pragma unroll
     for (int j = 0; j < VE; ++j) {
@@ -775,26 +776,47 @@ __global__ void __launch_bounds__(kWide) norm_wide_dx_kernel(const NormArgs a) {
     }
   };
   float s[2] = {0.f, 0.f};
-#pragma unroll 2
-  for (int v = threadIdx.x; v < nvec; v += kWide) {
+  const auto add = [&](int v, const Raw& x, const Raw& y) {
     float h[VE], g[VE];
-    take(v, h, g);
+    values(v, x, y, h, g);
 #pragma unroll
     for (int j = 0; j < VE; ++j) {
       s[0] += g[j];
       s[1] = __fmaf_rn(g[j], h[j], s[1]);
     }
+  };
+  Raw x[kKept], y[kKept];
+#pragma unroll
+  for (int k = 0; k < kKept; ++k) {
+    const int v = threadIdx.x + kWide * k;
+    x[k] = y[k] = V::zero();
+    if (v < nvec) {
+      x[k] = xs[v];
+      y[k] = gs[v];
+    }
   }
+#pragma unroll
+  for (int k = 0; k < kKept; ++k)
+    if ((int)threadIdx.x + kWide * k < nvec) add(threadIdx.x + kWide * k, x[k], y[k]);
+#pragma unroll 2
+  for (int v = threadIdx.x + kWide * kKept; v < nvec; v += kWide) add(v, xs[v], gs[v]);
   row_sums<2, kWide / 32>(s, s_sum);
   const float m1 = s[0] * over_d, m2 = s[1] * over_d;
-#pragma unroll 2
-  for (int v = threadIdx.x; v < nvec; v += kWide) {   // (again, from L2)
+  const auto result = [&](int v, const Raw& x, const Raw& y) {
     float h[VE], g[VE];
-    take(v, h, g);
+    values(v, x, y, h, g);
 #pragma unroll
     for (int j = 0; j < VE; ++j) g[j] = rstd * ((g[j] - m1) - h[j] * m2);
-    static_cast<Raw*>(a.d_x)[at + v] = V::put(g);
-  }
+    return V::put(g);
+  };
+  Raw* d_x = static_cast<Raw*>(a.d_x) + at;
+#pragma unroll
+  for (int k = 0; k < kKept; ++k)
+    if ((int)threadIdx.x + kWide * k < nvec) x[k] = result(threadIdx.x + kWide * k, x[k], y[k]);
+#pragma unroll
+  for (int k = 0; k < kKept; ++k)                     // (apart: no weight's load waits for a store)
+    if ((int)threadIdx.x + kWide * k < nvec) d_x[threadIdx.x + kWide * k] = x[k];
+  for (int v = threadIdx.x + kWide * kKept; v < nvec; v += kWide) d_x[v] = result(v, xs[v], gs[v]);     // (again, from L2)
 }
 template <typename T, int VE>
 __global__ void __launch_bounds__(256) norm_wide_sums_kernel(const NormArgs a) {
@@ -883,6 +905,7 @@ cudaError_t launch_rows(const NormArgs& a, cudaStream_t s) {
     }
   if (a.d <= 2048) return few(norm_kernel<T, VE, 8 / VE, 8>, 256);
   if (a.d <= 8192) return few(norm_kernel<T, VE, 32 / VE, 8>, 256);
+  if (a.d <= 16384) return few(norm_kernel<T, VE, 32 / VE, 16>, 512);
   if (a.d <= 32768) return few(norm_kernel<T, VE, 32 / VE, 32>, 1024);
   return few(norm_wide_kernel<T>, kWide);
 }
@@ -942,7 +965,9 @@ cudaError_t launch_norm_backward(const NormArgs& a, cudaStream_t s) {
                            : launch_gradients<typename Row::T, Row::VE>(a, parts, s);
   });
   if (e != cudaSuccess || (!a.d_weight && !a.d_bias)) return e;
-  return launch(true, norm_join_kernel, dim3(ceil_div(a.d, 32), 2), 32 * kJoinWarps, 0, s, a, parts);
+  const dim3 grid(ceil_div(a.d, 32), 2);
+  if (parts <= 8 * kJoinAhead) return launch(true, norm_join_kernel<8>, grid, 256, 0, s, a, parts);
+  return launch(true, norm_join_kernel<32>, grid, 1024, 0, s, a, parts);
 }
 
 }  // namespace cmsd
