@@ -752,12 +752,13 @@ __global__ void __launch_bounds__(kFewThreads) norm_backward_few_kernel(const No
 constexpr int kWideCols = 8192;
 // rows of over kWideCols columns: d_x by a CTA a row, the sums over rows by a CTA 32 vectors of columns; both read
 // both inputs (R = 2048 d = 16384 bf16 113 us, 1.8 TB/s of what is needed)
+constexpr int kWideDx = 512;                          // (two rows an SM: with 1024 threads a row 106 us where this takes 92, R = 2048 d = 16384 bf16)
 template <typename T, int VE>
-__global__ void __launch_bounds__(kWide) norm_wide_dx_kernel(const NormArgs a) {
+__global__ void __launch_bounds__(kWideDx, 2) norm_wide_dx_kernel(const NormArgs a) {
   using V = RowVec<T, VE>;
   using Raw = typename V::Raw;
-  constexpr int kKept = VE == 8 ? 2 : 4;              // a thread's first vectors stay in registers
-  __shared__ float s_sum[2 * kWide / 32];
+  constexpr int kKept = 4;                            // a thread's first vectors stay in registers
+  __shared__ float s_sum[2 * kWideDx / 32];
   wait_for_previous();
   const int nvec = a.d / VE;
   const size_t at = (size_t)blockIdx.x * nvec;
@@ -788,7 +789,7 @@ __global__ void __launch_bounds__(kWide) norm_wide_dx_kernel(const NormArgs a) {
   Raw x[kKept], y[kKept];
 #pragma unroll
   for (int k = 0; k < kKept; ++k) {
-    const int v = threadIdx.x + kWide * k;
+    const int v = threadIdx.x + kWideDx * k;
     x[k] = y[k] = V::zero();
     if (v < nvec) {
       x[k] = xs[v];
@@ -797,10 +798,10 @@ __global__ void __launch_bounds__(kWide) norm_wide_dx_kernel(const NormArgs a) {
   }
 #pragma unroll
   for (int k = 0; k < kKept; ++k)
-    if ((int)threadIdx.x + kWide * k < nvec) add(threadIdx.x + kWide * k, x[k], y[k]);
+    if ((int)threadIdx.x + kWideDx * k < nvec) add(threadIdx.x + kWideDx * k, x[k], y[k]);
 #pragma unroll 2
-  for (int v = threadIdx.x + kWide * kKept; v < nvec; v += kWide) add(v, xs[v], gs[v]);
-  row_sums<2, kWide / 32>(s, s_sum);
+  for (int v = threadIdx.x + kWideDx * kKept; v < nvec; v += kWideDx) add(v, xs[v], gs[v]);
+  row_sums<2, kWideDx / 32>(s, s_sum);
   const float m1 = s[0] * over_d, m2 = s[1] * over_d;
   const auto result = [&](int v, const Raw& x, const Raw& y) {
     float h[VE], g[VE];
@@ -812,11 +813,11 @@ __global__ void __launch_bounds__(kWide) norm_wide_dx_kernel(const NormArgs a) {
   Raw* d_x = static_cast<Raw*>(a.d_x) + at;
 #pragma unroll
   for (int k = 0; k < kKept; ++k)
-    if ((int)threadIdx.x + kWide * k < nvec) x[k] = result(threadIdx.x + kWide * k, x[k], y[k]);
+    if ((int)threadIdx.x + kWideDx * k < nvec) x[k] = result(threadIdx.x + kWideDx * k, x[k], y[k]);
 #pragma unroll
   for (int k = 0; k < kKept; ++k)                     // (apart: no weight's load waits for a store)
-    if ((int)threadIdx.x + kWide * k < nvec) d_x[threadIdx.x + kWide * k] = x[k];
-  for (int v = threadIdx.x + kWide * kKept; v < nvec; v += kWide) d_x[v] = result(v, xs[v], gs[v]);     // (again, from L2)
+    if ((int)threadIdx.x + kWideDx * k < nvec) d_x[threadIdx.x + kWideDx * k] = x[k];
+  for (int v = threadIdx.x + kWideDx * kKept; v < nvec; v += kWideDx) d_x[v] = result(v, xs[v], gs[v]);     // (again, from L2)
 }
 template <typename T, int VE>
 __global__ void __launch_bounds__(256) norm_wide_sums_kernel(const NormArgs a) {
@@ -937,7 +938,7 @@ cudaError_t launch_few_gradients(const NormArgs& a, cudaStream_t s) {
 }
 template <typename T, int VE>
 cudaError_t launch_wide_gradients(const NormArgs& a, int parts, cudaStream_t s) {
-  cudaError_t e = a.d_x ? launch(true, norm_wide_dx_kernel<T, VE>, a.R, kWide, 0, s, a) : cudaSuccess;
+  cudaError_t e = a.d_x ? launch(true, norm_wide_dx_kernel<T, VE>, a.R, kWideDx, 0, s, a) : cudaSuccess;
   if (e == cudaSuccess && (a.d_weight || a.d_bias))
     e = launch(true, norm_wide_sums_kernel<T, VE>, dim3(ceil_div(a.d / VE, 32), parts), 256, 0, s, a);
   return e;
