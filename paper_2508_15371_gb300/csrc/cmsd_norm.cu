@@ -277,7 +277,7 @@ __global__ void __launch_bounds__(kWide) norm_wide_kernel(const NormArgs a) {
 // parameters (forward) or their sums over rows (gradients) in registers; W warps a
 // row, kGroups * kRows rows of a CTA at a time.  Rows come through a ring in shared
 // memory.  Bound by memory forward (R = 16384 d = 2048 bf16 22.8 us, 5.9 TB/s), by
-// instructions beside it backward (37 us and 2.5 of the join, 5.4 TB/s).  Sixteen
+// memory and a barrier a row backward (36.6 us with the join, 5.5 TB/s).  Sixteen
 // columns a thread: of eight, exchanging a row's sums is most of the work (46 us
 // forward); with a warp a row the parameters are read again for every row (34 us).
 constexpr int kSms = 152;
@@ -635,13 +635,13 @@ __global__ void __launch_bounds__(32 * kJoinWarps) norm_join_kernel(const NormAr
 // together), the others a row of d_x each.  Inputs are read twice, the second time
 // from L2; a few loads in a row bound it.
 constexpr int kFewCols = 8, kFewLanes = 32, kFewThreads = kFewCols * kFewLanes, kFewAhead = 8;
-template <typename T, int VE>
+template <typename T, int VE, int NV>
 __global__ void __launch_bounds__(kFewThreads) norm_backward_few_kernel(const NormArgs a, int cols) {
   using V = RowVec<T, VE>;
   using Raw = typename V::Raw;
   using M = Num<VE>;
   using N = typename M::N;
-  constexpr int kN = M::kN, NV = 8 / VE, W = kFewThreads / 32;
+  constexpr int kN = M::kN, W = kFewThreads / 32;
   __shared__ float s_sum[2 * W];
   __shared__ float s_col[2][kFewLanes][kFewCols * VE + 1];
   wait_for_previous();
@@ -751,7 +751,7 @@ __global__ void __launch_bounds__(kFewThreads) norm_backward_few_kernel(const No
 
 constexpr int kWideCols = 8192;
 // rows of over kWideCols columns: d_x by a CTA a row, the sums over rows by a CTA 32 vectors of columns; both read
-// both inputs (R = 2048 d = 16384 bf16 113 us, 1.8 TB/s of what is needed)
+// both inputs (R = 2048 d = 16384 bf16 92 us, 2.2 TB/s of what is needed)
 constexpr int kWideDx = 512;                          // (two rows an SM: with 1024 threads a row 106 us where this takes 92, R = 2048 d = 16384 bf16)
 template <typename T, int VE>
 __global__ void __launch_bounds__(kWideDx, 2) norm_wide_dx_kernel(const NormArgs a) {
@@ -882,10 +882,11 @@ int part_count(int R, int d) {
 // us, 608 3.01 and 3.03, 1216 4.52 and 4.12; d = 1001 608 3.98 and 6.23, 1216 6.18 and 6.64.  Narrower and wider rows go
 // to the latter always (R = 16 d = 256 1.93 against 2.01, d = 4096 2.48 against 2.69).
 constexpr int kFewRows = 608;
-// Up to this many rows of up to 2048 entries norm_backward_few_kernel, else the grid that stays and its join, bf16: R = 16
-// d = 1024 1.5 against 3.8 us, R = 333 d = 1001 3.8 and 4.8, R = 608 d = 64 3.7 and 3.6, d = 2048 4.4 and 9.5; R = 900
-// d = 64 4.7 and 4.1, d = 1001 6.1 and 7.0, R = 1216 d = 1001 7.6 and 6.1.
-constexpr int kFewGradRows = 608, kFewGradCols = 2048;
+// Whether the gradients are norm_backward_few_kernel's, else the grid's that stays and its join.  bf16: R = 16 d = 1024 1.5
+// against 3.8 us, R = 333 d = 1001 3.8 and 4.8, R = 608 d = 64 3.7 and 3.7, d = 2048 4.4 and 6.0, d = 8192 8.6 and 14.9,
+// R = 900 d = 64 4.7 and 3.9, R = 1216 d = 1001 7.6 and 6.0.  Wide rows that begin anywhere: d = 4097 R = 200 7.3 and
+// 7.9, R = 400 10.2 and 9.2.
+bool few_gradients(int R, int d) { return d <= kWideCols && R <= (d <= 2048 || d % 4 == 0 ? 608 : 304); }
 template <typename T, int VE, int kCols, int W>
 cudaError_t launch_many(const NormArgs& a, cudaStream_t s) {
   constexpr int smem = kNormStages * cta_groups(W) * staged_bytes(W, kCols, sizeof(T));
@@ -931,10 +932,10 @@ cudaError_t launch_gradients(const NormArgs& a, int parts, cudaStream_t s) {
     default: return launch_gradients<T, VE, 16, 16>(a, parts, s);
   }
 }
-template <typename T, int VE>
+template <typename T, int VE, int NV>
 cudaError_t launch_few_gradients(const NormArgs& a, cudaStream_t s) {
   const int cols = a.d_weight || a.d_bias ? ceil_div(a.d / VE, kFewCols) : 0;
-  return launch(true, norm_backward_few_kernel<T, VE>, cols + (a.d_x ? a.R : 0), kFewThreads, 0, s, a, cols);
+  return launch(true, norm_backward_few_kernel<T, VE, NV>, cols + (a.d_x ? a.R : 0), kFewThreads, 0, s, a, cols);
 }
 template <typename T, int VE>
 cudaError_t launch_wide_gradients(const NormArgs& a, int parts, cudaStream_t s) {
@@ -957,8 +958,12 @@ cudaError_t launch_norm(const NormArgs& a, cudaStream_t s) {
 }
 
 cudaError_t launch_norm_backward(const NormArgs& a, cudaStream_t s) {
-  if (a.R <= kFewGradRows && a.d <= kFewGradCols)
-    return by_row_type(a.dtype, a.d, [&](auto t) { return launch_few_gradients<typename decltype(t)::T, decltype(t)::VE>(a, s); });
+  if (few_gradients(a.R, a.d))
+    return by_row_type(a.dtype, a.d, [&](auto t) {
+      using Row = decltype(t);
+      return a.d <= 2048 ? launch_few_gradients<typename Row::T, Row::VE, 8 / Row::VE>(a, s)
+                         : launch_few_gradients<typename Row::T, Row::VE, 32 / Row::VE>(a, s);
+    });
   const int parts = part_count(a.R, a.d);
   const cudaError_t e = by_row_type(a.dtype, a.d, [&](auto t) {
     using Row = decltype(t);

@@ -123,7 +123,8 @@ def test_norm_and_gradients(cmsd, R, d, dtype, wdtype):
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
-@pytest.mark.parametrize("R,d", [(255, 2048), (256, 2047), (257, 2046), (608, 2048), (608, 65), (609, 2048), (609, 65), (608, 2050)])
+@pytest.mark.parametrize("R,d", [(255, 2048), (256, 2047), (257, 2046), (608, 2048), (608, 65), (609, 2048), (609, 65), (608, 2050),
+                                 (304, 4097), (305, 4097), (608, 2056), (100, 8192), (30, 8191), (30, 8194)])
 def test_gradients_about_the_rows_of_one_launch(cmsd, R, d, dtype):
     """Rows about those that a thread requests at once, and about the most that are summed without a join."""
     x, w, b, d_y = _inputs(R, d, dtype, F32, seed=3)
