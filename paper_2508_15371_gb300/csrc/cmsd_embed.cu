@@ -390,7 +390,7 @@ constexpr int kRadixThreads = 256, kRadixWarps = kRadixThreads / 32;
 // 1024 30.0, with 2048 31.9; 32768 of 1000 29.7 and 28.8.
 constexpr int kTileMin = 2048, kShortRows = 16384;
 constexpr int kRound = 8;                            // rows of a lane requested at once
-constexpr int kCountsAhead = 32;                     // counts of a thread (one by one, 20000 rows of 64 took 30.5 us, not 22.1)
+constexpr int kCountsAhead = 32;                     // counts of a thread (one by one, 20000 rows of 64 took 30.5 us, not 22.6)
 __global__ void __launch_bounds__(kRadixThreads) embed_count_kernel(const EmbedArgs a, int digits, int tiles) {
   extern __shared__ int s_count[];
   wait_for_previous();
@@ -748,10 +748,13 @@ __global__ void __launch_bounds__(kJoinThreads) embed_join_kernel(const EmbedArg
 size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 // Rows of a tile, at least kBatch, for four tiles an SM where there are few rows (for eight, 32768 rows of 1000 tokens
 // took 41 us instead of 35: borders cut twice as many tokens).
+// Narrow rows up to four times as many, since a tile's batches go one after another: R = 20000 of 120000, d = 256 with
+// tiles of 64 31.4 us, of 16 24.9, d = 512 36.5 and (32) 32.0; eight times, d = 128 R = 32768 of 3000 24.2 against 21.4.
 constexpr int kTiles = 608;
-int slot_count(int R) {
+int slot_count(int R, int d) {
+  const int tiles = kTiles * std::max(1, std::min(4, 1024 / d));
   int n = kBatch;
-  while (n < kSlots && R > n * kTiles) n *= 2;
+  while (n < kSlots && R > n * tiles) n *= 2;
   return n;
 }
 
@@ -777,7 +780,7 @@ size_t embed_layout(EmbedArgs& a, char* w) {
   }
   if (R > kRankRows)
     for (int p = 0; p < a.passes; ++p) a.count[p] = (int*)take((size_t)ceil_div(R, a.tile) << (a.bits + 2));
-  a.slots = slot_count(R);
+  a.slots = slot_count(R, a.d);
   const size_t tiles = ceil_div(R, a.slots);
   a.state = (int2*)take(tiles * 8);
   a.head = (float*)take(tiles * a.d * 4);

@@ -122,7 +122,8 @@ def test_wide_rows(cmsd, R, d, V, dtype):
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("R,d,V", [(8191, 64, 900), (8192, 64, 900), (8193, 512, 40), (9001, 504, 3000), (40000, 8, 70000), (8200, 520, 50),
                                    (12001, 256, 2000), (7168, 64, 900), (7169, 64, 900), (16384, 24, 40),
-                                   (16385, 24, 40), (32767, 24, 3000), (32768, 24, 3000)])
+                                   (16385, 24, 40), (32767, 24, 3000), (32768, 24, 3000), (9728, 64, 30),
+                                   (9729, 64, 30), (19457, 512, 300), (50000, 128, 12), (38913, 256, 7)])
 def test_narrow_rows(cmsd, R, d, V, dtype):
     """Many rows of up to 64 vectors, which are looked up whatever row a vector is of, and one that is wider."""
     tokens = _tokens(R, V, _gen(R, 9), ignored=0.2)
