@@ -797,7 +797,8 @@ cudaError_t launch_embed(const EmbedArgs& a, cudaStream_t s) {
     if constexpr (Row::VE * sizeof(typename Row::T) == 16)
       if (a.d / Row::VE <= kNarrowVecs && a.R >= kNarrowRows) {
         const int64_t ctas = ((int64_t)a.R * (a.d / Row::VE) + 256 * kAhead - 1) / (256 * kAhead);
-        return launch(true, embed_narrow_kernel<typename Row::T, Row::VE>, (unsigned)(ctas < (1 << 30) ? ctas : 1 << 30), 256, 0, s, a);
+        return launch(true, embed_narrow_kernel<typename Row::T, Row::VE>, (unsigned)(ctas < (1 << 30) ? ctas : 1 << 30), 256, 0,
+                      s, a);
       }
     // a warp a CTA until every SM has some, then eight
     int warps = 1;

@@ -578,7 +578,8 @@ __global__ void __launch_bounds__(cta_threads(W), grad_ctas(W, kCols)) norm_back
           for (int j = 0; j < VE; ++j)
             for (int q = 1; q < kGroups; ++q) sum[k][j] += s_col[(k * VE + j) * kThreads + 32 * W * q + t];
           float* p = part + which * a.d + (t + 32 * W * k) * VE;
-          if constexpr (VE % 4 == 0) {                // (one by one, each to a sector of its own: R = 4096 d = 2048 17.4 us instead of 14.3)
+          // (one by one, each goes to a sector of its own: R = 4096 d = 2048 17.4 us instead of 14.3)
+          if constexpr (VE % 4 == 0) {
 #pragma unroll
             for (int j = 0; j < VE; j += 4)
               *reinterpret_cast<float4*>(p + j) = make_float4(sum[k][j], sum[k][j + 1], sum[k][j + 2], sum[k][j + 3]);
@@ -752,7 +753,7 @@ __global__ void __launch_bounds__(kFewThreads) norm_backward_few_kernel(const No
 constexpr int kWideCols = 8192;
 // rows of over kWideCols columns: d_x by a CTA a row, the sums over rows by a CTA 32 vectors of columns; both read
 // both inputs (R = 2048 d = 16384 bf16 92 us, 2.2 TB/s of what is needed)
-constexpr int kWideDx = 512;                          // (two rows an SM: with 1024 threads a row 106 us where this takes 92, R = 2048 d = 16384 bf16)
+constexpr int kWideDx = 512;                          // (two rows an SM: with 1024 threads 106 us where this takes 92)
 template <typename T, int VE>
 __global__ void __launch_bounds__(kWideDx, 2) norm_wide_dx_kernel(const NormArgs a) {
   using V = RowVec<T, VE>;
