@@ -153,10 +153,11 @@ __device__ __forceinline__ int lead_of(int row, int d) {
 }
 
 // ---- few rows, and wide ones -----------------------------------------------------------------
-// A CTA of W warps a row, NV vectors of VE entries a thread.  Sums are of differences from
-// the row's first entry, so that a mean far from zero cancels before anything is
-// rounded, and a row of one number gives exactly bias; what their mean c still
-// lacks, e, comes with the squares.
+// A CTA of W warps a row, NV vectors of VE entries a thread.  A first mean c is that of
+// the differences from the row's first entry, so that a row of one number gives
+// exactly bias; it is as far off as that entry's size makes it.  Differences from c
+// are of the entries themselves, and what c lacks, e, is their mean and comes with
+// their squares: no entry loses bits to another one, wherever a large one stands.
 template <typename T, int VE, int NV, int W>
 __global__ void __launch_bounds__(32 * W) norm_kernel(const NormArgs a) {
   using V = RowVec<T, VE>;
@@ -195,14 +196,11 @@ __global__ void __launch_bounds__(32 * W) norm_kernel(const NormArgs a) {
     M::template get<T>(raw[k], h[k]);
     if (t + 32 * W * k < nvec)
 #pragma unroll
-      for (int j = 0; j < kN; ++j) {
-        h[k][j] = M::add(h[k][j], p);
-        n1 = M::add(n1, h[k][j]);
-      }
+      for (int j = 0; j < kN; ++j) n1 = M::add(n1, M::add(h[k][j], p));
   }
   float s[1] = {M::sum(n1)};
   row_sums<1, W>(s, s_sum);
-  const float c = s[0] / a.d;
+  const float c = pilot + s[0] / a.d;
   p = M::all(-c);
   n1 = M::all(0.f);
 #pragma unroll
@@ -218,7 +216,7 @@ __global__ void __launch_bounds__(32 * W) norm_kernel(const NormArgs a) {
   row_sums<2, W>(q, s_sum + W);
   const float e = q[0] / a.d, rstd = 1.f / sqrtf((q[1] / a.d - e * e) + a.eps);
   if (t == 0) {
-    if (a.mean) a.mean[row] = pilot + (c + e);
+    if (a.mean) a.mean[row] = c + e;
     if (a.rstd) a.rstd[row] = rstd;
   }
   const N scale = M::all(rstd), shift = M::all(-e * rstd);
@@ -251,21 +249,21 @@ __global__ void __launch_bounds__(kWide) norm_wide_kernel(const NormArgs a) {
   float s[1] = {0.f};
   for (int j = threadIdx.x; j < a.d; j += kWide) s[0] += to_float(x[j]) - pilot;
   row_sums<1, kWide / 32>(s, s_sum);
-  const float c = s[0] / a.d;
+  const float c = pilot + s[0] / a.d;
   float q[2] = {0.f, 0.f};
   for (int j = threadIdx.x; j < a.d; j += kWide) {
-    const float h = (to_float(x[j]) - pilot) - c;
+    const float h = to_float(x[j]) - c;
     q[0] += h;
     q[1] = __fmaf_rn(h, h, q[1]);
   }
   row_sums<2, kWide / 32>(q, s_sum + kWide / 32);
   const float e = q[0] / a.d, rstd = 1.f / sqrtf((q[1] / a.d - e * e) + a.eps);
   if (threadIdx.x == 0) {
-    if (a.mean) a.mean[blockIdx.x] = pilot + (c + e);
+    if (a.mean) a.mean[blockIdx.x] = c + e;
     if (a.rstd) a.rstd[blockIdx.x] = rstd;
   }
   for (int j = threadIdx.x; j < a.d; j += kWide) {
-    float h = (((to_float(x[j]) - pilot) - c) - e) * rstd;
+    float h = ((to_float(x[j]) - c) - e) * rstd;
     if (a.weight) h *= param(a.weight, a.wdtype, j);
     if (a.bias) h += param(a.bias, a.wdtype, j);
     y[j] = from_float<T>(h);
@@ -280,6 +278,13 @@ __global__ void __launch_bounds__(kWide) norm_wide_kernel(const NormArgs a) {
 // memory and a barrier a row backward (36.6 us with the join, 5.5 TB/s).  Sixteen
 // columns a thread: of eight, exchanging a row's sums is most of the work (46 us
 // forward); with a warp a row the parameters are read again for every row (34 us).
+// Forward, bf16 rows of over 256 entries take the first mean c (see norm_kernel) from
+// the threads' first eight columns alone, which every row fills: a power of two of
+// entries added in pairs, so that of equal ones it is exact.  It is off by at most s,
+// the mean of |x - mean|, beside its rounding, which is far below a bf16 entry's: the
+// mean of squares that e's square is taken from is not above var + s^2 <= 2 var.  From
+// all columns 0.6 us more.  f32 rows, whose last bits a sum of entries would touch, have
+// their bytes to wait for: 22.5 us either way (R = 8192 d = 2048).
 constexpr int kSms = 152;
 __host__ __device__ constexpr int cta_threads(int w) { return w > 8 ? 32 * w : 256; }
 __host__ __device__ constexpr int cta_groups(int w) { return cta_threads(w) / (32 * w); }
@@ -343,6 +348,13 @@ __device__ __forceinline__ void group_two_sums(float (&v)[2], float* buf, int gr
   for (int k = 0; k < 2; ++k) v[k] = sum_of<W>(buf + k * W);
 }
 
+// v^(-1/2): one Newton step behind CUDA's, to 2 u.  (With 1 / sqrtf, whose steps wait for one another, R = 16384
+// d = 2048 bf16 took 23.3 us forward instead of 22.6, d = 256 8.5 instead of 7.9.)
+__device__ __forceinline__ float inverse_root(float v) {
+  const float near = rsqrtf(v);
+  return __fmaf_rn(near * 0.5f, __fmaf_rn(-near * v, near, 1.f), near);
+}
+
 // whether a thread's vector k is in the row: a row that takes W > 1 warps fills half of what they hold
 template <int W, int NV>
 __device__ __forceinline__ bool in_row(int t, int k, int nvec) {
@@ -358,14 +370,16 @@ __global__ void __launch_bounds__(cta_threads(W), norm_ctas(kCols)) norm_many_ke
   using N = typename M::N;
   constexpr int kN = M::kN, NV = kCols / VE, kGroups = cta_groups(W), kRows = 1;
   constexpr int kRowBytes = staged_bytes(W, kCols, sizeof(T)), kTurns = kCols * sizeof(T) / 16;
+  // vectors of a thread that every row fills (W = 1: rows of over 256) and that c is made from, or 0: from all
+  constexpr int kHalf = sizeof(T) == 2 && kCols > 8 ? NV / 2 : 0;
   extern __shared__ uint4 s_ring4[];
-  __shared__ __align__(16) float s_sum[W > 1 ? 2 * kGroups * kRows * W : 1];
+  __shared__ __align__(16) float s_sum[W > 1 ? 3 * kGroups * W : 1];
   wait_for_previous();
   const int nvec = a.d / VE, t = threadIdx.x % (32 * W), group = threadIdx.x / (32 * W);
   const int64_t first = (int64_t)blockIdx.x * kGroups * kRows + group, step = (int64_t)gridDim.x * kGroups * kRows;
   char* ring = reinterpret_cast<char*>(s_ring4) + group * kNormStages * kRows * kRowBytes;       // [kNormStages][kRows]
   const uint32_t ring_at = (uint32_t)__cvta_generic_to_shared(ring);
-  float* sums = s_sum + (W > 1 ? 2 * group * kRows * W : 0);
+  float* sums = s_sum + (W > 1 ? 3 * group * W : 0);
   const auto request = [&](int64_t r0, int stage) {
 #pragma unroll
     for (int u = 0; u < kRows; ++u) {
@@ -401,64 +415,67 @@ __global__ void __launch_bounds__(cta_threads(W), norm_ctas(kCols)) norm_many_ke
     copies_but<kNormStages - 2>();
     group_sync<W>(group);                             // (the first entry is another thread's copy, if no more is)
     request(r0 + (kNormStages - 1) * step, stage == 0 ? kNormStages - 1 : stage - 1);
-    N h[kRows][NV][kN];
-    float pilot[kRows], s[kRows], q[kRows];
+    const char* from = ring + stage * kRows * kRowBytes;
+    const int lead = lead_of<T, VE>(r0, a.d);
+    N h[NV][kN];
+    float s[1], c;
+    if constexpr (kHalf > 0) {
 #pragma unroll
-    for (int u = 0; u < kRows; ++u) {
-      const char* from = ring + (stage * kRows + u) * kRowBytes;
-      const int lead = lead_of<T, VE>(r0 + u * kGroups, a.d);
-      pilot[u] = to_float(*reinterpret_cast<const T*>(from + lead));
-      const N p = M::all(-pilot[u]);
+      for (int k = 0; k < NV; ++k)
+        if (in_row<W, NV>(t, k, nvec)) M::template get<T>(staged<T, VE>(from, lead, t + 32 * W * k), h[k]);
+      N v[kHalf * kN];
+#pragma unroll
+      for (int j = 0; j < kHalf * kN; ++j) v[j] = h[j / kN][j % kN];
+#pragma unroll
+      for (int o = kHalf * kN / 2; o; o >>= 1)
+#pragma unroll
+        for (int j = 0; j < o; ++j) v[j] = M::add(v[j], v[j + o]);
+      s[0] = M::sum(v[0]);
+      group_sums<1, W>(s, sums, group);
+      c = s[0] * (1.f / (32 * W * kHalf * VE));
+    } else {
+      const float first_entry = to_float(*reinterpret_cast<const T*>(from + lead));
       N sum = M::all(0.f);
 #pragma unroll
       for (int k = 0; k < NV; ++k)
         if (in_row<W, NV>(t, k, nvec)) {
-          M::template get<T>(staged<T, VE>(from, lead, t + 32 * W * k), h[u][k]);
+          M::template get<T>(staged<T, VE>(from, lead, t + 32 * W * k), h[k]);
 #pragma unroll
-          for (int j = 0; j < kN; ++j) {
-            h[u][k][j] = M::add(h[u][k][j], p);
-            sum = M::add(sum, h[u][k][j]);
-          }
+          for (int j = 0; j < kN; ++j) sum = M::add(sum, M::add(h[k][j], M::all(-first_entry)));
         }
-      s[u] = M::sum(sum);
+      s[0] = M::sum(sum);
+      group_sums<1, W>(s, sums, group);
+      c = __fmaf_rn(s[0], over_d, first_entry);
     }
     stage = stage + 1 == kNormStages ? 0 : stage + 1;
-    group_sums<kRows, W>(s, sums, group);
+    const N p = M::all(-c);
+    N n1 = M::all(0.f), n2 = M::all(0.f);
 #pragma unroll
-    for (int u = 0; u < kRows; ++u) {
-      s[u] *= over_d;
-      const N p = M::all(-s[u]);
-      N sum = M::all(0.f);
+    for (int k = 0; k < NV; ++k)
+      if (in_row<W, NV>(t, k, nvec))
 #pragma unroll
-      for (int k = 0; k < NV; ++k)
-        if (in_row<W, NV>(t, k, nvec))
-#pragma unroll
-          for (int j = 0; j < kN; ++j) {
-            h[u][k][j] = M::add(h[u][k][j], p);
-            sum = M::fma(h[u][k][j], h[u][k][j], sum);
-          }
-      q[u] = M::sum(sum);
-    }
-    group_sums<kRows, W>(q, sums + kRows * W, group);
-#pragma unroll
-    for (int u = 0; u < kRows; ++u) {
-      const int64_t row = r0 + u * kGroups;
-      if (row >= a.R) continue;
-      const float rstd = 1.f / sqrtf(q[u] * over_d + a.eps);
-      if (t == 0) {
-        if (a.mean) a.mean[row] = pilot[u] + s[u];
-        if (a.rstd) a.rstd[row] = rstd;
-      }
-      const N scale = M::all(rstd);
-      Raw* y = static_cast<Raw*>(a.y) + (size_t)row * nvec;
-#pragma unroll
-      for (int k = 0; k < NV; ++k)
-        if (in_row<W, NV>(t, k, nvec)) {
-#pragma unroll
-          for (int j = 0; j < kN; ++j) h[u][k][j] = M::fma(M::mul(h[u][k][j], scale), w[k][j], b[k][j]);
-          y[t + 32 * W * k] = M::template put<T>(h[u][k]);
+        for (int j = 0; j < kN; ++j) {
+          h[k][j] = M::add(h[k][j], p);
+          n1 = M::add(n1, h[k][j]);
+          n2 = M::fma(h[k][j], h[k][j], n2);
         }
+    float q[2] = {M::sum(n1), M::sum(n2)};
+    if (W == 1) group_sums<2, W>(q, sums + W, group);   // (every lane has both at once: d = 512 4.84 us, not 4.94)
+    else group_two_sums<W>(q, sums + W, group);
+    const float e = q[0] * over_d, rstd = inverse_root(__fmaf_rn(-e, e, __fmaf_rn(q[1], over_d, a.eps)));
+    if (t == 0) {
+      if (a.mean) a.mean[r0] = c + e;
+      if (a.rstd) a.rstd[r0] = rstd;
     }
+    const N scale = M::all(rstd), shift = M::all(-e * rstd);
+    Raw* y = static_cast<Raw*>(a.y) + (size_t)r0 * nvec;
+#pragma unroll
+    for (int k = 0; k < NV; ++k)
+      if (in_row<W, NV>(t, k, nvec)) {
+#pragma unroll
+        for (int j = 0; j < kN; ++j) h[k][j] = M::fma(M::fma(h[k][j], scale, shift), w[k][j], b[k][j]);
+        y[t + 32 * W * k] = M::template put<T>(h[k]);
+      }
   }
   copies_but<0>();
 }
