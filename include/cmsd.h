@@ -323,7 +323,8 @@ int cmsd_lmhead_errors(void* stream, uint32_t* flags_out);
  *     are not touched.
  *   A token's rows are summed in an order that depends on tokens alone.
  *   ws: cmsd_embedding_backward_workspace_bytes(R, d, V) bytes on the current
- *     device.  It needs no initialisation but for the error word, which
+ *     device; enough for any fewer rows of that d and V, too.  It needs no
+ *     initialisation but for the error word, which
  *     cmsd_workspace_init zeroes and cmsd_workspace_errors reads (bit 0 as above).
  *     The device's own word gets the same bit.
  *   R == 0: zeros are written, or nothing with add.
@@ -357,7 +358,7 @@ int cmsd_embedding_errors(void* stream, uint32_t* flags_out);
  *     left out (all NULL is CMSD_EINVAL).  All are written whole.
  *   The sums over rows are formed in an order that depends on R and d alone.
  *   ws: cmsd_layernorm_backward_workspace_bytes(R, d) bytes on the current device,
- *     no initialisation needed.
+ *     enough for any fewer rows of that d, too; no initialisation needed.
  *   R == 0: the parameters' gradients are zero.
  */
 int cmsd_layernorm(const void* x, const void* weight, const void* bias, int dtype, int wdtype, int R, int d,

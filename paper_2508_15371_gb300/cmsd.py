@@ -589,7 +589,8 @@ def embedding(tokens, table, scale=1.0, ignore_index=-100, out=None):
 
 
 def embedding_backward_workspace(R, d, V):
-    """A workspace for embedding_backward of R rows on the current device (workspace_errors reads its error word)."""
+    """A workspace for embedding_backward of R rows or fewer on the current device (workspace_errors reads its error
+    word)."""
     return _head_workspace("cmsd_embedding_backward_workspace_bytes", R, d, V)
 
 
@@ -666,7 +667,7 @@ def layernorm(x, weight=None, bias=None, eps=1e-5, stats=True, out=None):
 
 
 def layernorm_backward_workspace(R, d):
-    """A workspace for layernorm_backward of R rows on the current device."""
+    """A workspace for layernorm_backward of R rows or fewer on the current device."""
     torch = _torch()
     if max(R, d) > _INT_MAX:
         _too_large("cmsd_layernorm_backward_workspace_bytes")

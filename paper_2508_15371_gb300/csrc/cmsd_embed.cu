@@ -752,12 +752,22 @@ size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 // Narrow rows up to four times as many, since a tile's batches go one after another: R = 20000 of 120000, d = 256 with
 // tiles of 64 31.4 us, of 16 24.9, d = 512 36.5 and (32) 32.0; eight times, d = 128 R = 32768 of 3000 24.2 against 21.4.
 constexpr int kTiles = 608;
+int wanted_tiles(int d) { return kTiles * std::max(1, std::min(4, 1024 / d)); }
 int slot_count(int R, int d) {
-  const int tiles = kTiles * std::max(1, std::min(4, 1024 / d));
   int n = kBatch;
-  while (n < kSlots && R > n * tiles) n *= 2;
+  while (n < kSlots && R > n * wanted_tiles(d)) n *= 2;
   return n;
 }
+int tile_rows(int R) {
+  if (R <= kShortRows) return kTileMin / 4;
+  return R < 2 * kShortRows ? kTileMin / 2 : kTileMin * ceil_div(R, (int64_t)kTileMin * 256);
+}
+// The most tiles that R rows or fewer have, of the ordering and of the sums: a workspace that is enough for R rows is
+// for fewer, although their tiles are smaller ones and may be more.
+int most_tiles(int R) {
+  return R <= kShortRows ? ceil_div(R, kTileMin / 4) : std::max(kShortRows / (kTileMin / 4), std::min(256, ceil_div(R, kTileMin)));
+}
+int most_sum_tiles(int R, int d) { return std::min(ceil_div(R, kBatch), std::max(wanted_tiles(d), ceil_div(R, kSlots))); }
 
 }  // namespace
 
@@ -774,15 +784,15 @@ size_t embed_layout(EmbedArgs& a, char* w) {
   while (((int64_t)1 << bits) <= a.V) ++bits;         // keys 0 .. V
   a.passes = R <= kRankRows ? 1 : ceil_div(bits, kRadixBits);
   a.bits = ceil_div(bits, a.passes);
-  a.tile = R <= kShortRows ? kTileMin / 4 : R < 2 * kShortRows ? kTileMin / 2 : kTileMin * ceil_div(R, (int64_t)kTileMin * 256);
+  a.tile = tile_rows(R);
   for (int k = 0; k < (a.passes > 1 ? 2 : 1); ++k) {
     a.key[k] = (unsigned*)take((size_t)R * 4);
     a.order[k] = (int*)take((size_t)R * 4);
   }
   if (R > kRankRows)
-    for (int p = 0; p < a.passes; ++p) a.count[p] = (int*)take((size_t)ceil_div(R, a.tile) << (a.bits + 2));
+    for (int p = 0; p < a.passes; ++p) a.count[p] = (int*)take((size_t)most_tiles(R) << (a.bits + 2));
   a.slots = slot_count(R, a.d);
-  const size_t tiles = ceil_div(R, a.slots);
+  const size_t tiles = most_sum_tiles(R, a.d);
   a.state = (int2*)take(tiles * 8);
   a.head = (float*)take(tiles * a.d * 4);
   a.tail = (float*)take(tiles * a.d * 4);
