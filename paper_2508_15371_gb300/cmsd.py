@@ -531,6 +531,15 @@ def _not_recorded(what):
                     f"autograd.Function) and take the gradients from {what}_backward")
 
 
+def _once(what, *tensors):
+    """Refuses a gradient's call where autograd would follow one of the tensors to a second derivative."""
+    if _torch_mod.is_grad_enabled():
+        for t in tensors:
+            if t is not None and t.requires_grad:
+                raise CmsdError(f"{what} records nothing for autograd: call it under torch.no_grad() (or from an "
+                                f"autograd.Function that is differentiated once)")
+
+
 def _rows(t, name):
     shape = t.shape
     if len(shape) != 2:
@@ -599,8 +608,10 @@ def embedding_backward(tokens, d_x, V, scale=1.0, ignore_index=-100, add=False, 
     dict d_table ([V, d], d_x's dtype), written whole.
 
     With add, out["d_table"] is given and the sums are added to it: a head that shares the table passes the d_weight
-    of lmhead_loss_backward."""
+    of lmhead_loss_backward.  There are no second derivatives, here and in the gradients below: tensors that require
+    them are refused while autograd records."""
     torch = _torch()
+    _once("embedding_backward", d_x, out.get("d_table") if add and out is not None else None)
     R, d = _rows(d_x, "d_x")
     V = int(V)
     if not 0 < V <= _INT_MAX:
@@ -684,6 +695,7 @@ def layernorm_backward(x, weight, mean, rstd, d_y, x_grad=True, weight_grad=True
     Returns dict d_x ([R, d], x's dtype, with x_grad), d_weight (with weight_grad) and d_bias (with bias_grad), both
     [d] of weight's dtype (x's without weight), written whole."""
     torch = _torch()
+    _once("layernorm_backward", x, weight, mean, rstd, d_y)
     R, d = _rows(x, "x")
     code, dtype = _code(x, "x"), x.dtype
     wcode, wtype = (code, dtype) if weight is None else (_code(weight, "weight"), weight.dtype)
@@ -747,6 +759,7 @@ def dropout_backward(d_y, p, seed, iteration=0, site=0, step=None, out=None):
     """The gradient of dropout by x, given the same p, seed, iteration, site and step: returns dict d_x.  (The
     residual's gradient is d_y itself.)"""
     _torch()
+    _once("dropout_backward", d_y)
     code, cur, iteration, site, d_x = _dropout_args(d_y, "d_y", "d_x", iteration, site, step, out)
     rc = lib().cmsd_dropout_backward(d_y.data_ptr(), code, d_y.numel(), float(p), int(seed), iteration, site, _ptr(step),
                                      d_x.data_ptr(), _stream_of(cur))
