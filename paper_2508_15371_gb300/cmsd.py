@@ -169,14 +169,16 @@ def params(K, rule="paper", preset="full", **kw):
 _torch_mod = None
 _raw_stream = None      # (device index) -> cudaStream_t of the current stream, without a Stream object
 _get_device = None      # () -> index of the current device, of a runtime that is initialised
+_forward_ad = None      # torch.autograd.forward_ad
 
 
 def _torch():
-    global _torch_mod, _raw_stream, _get_device
+    global _torch_mod, _raw_stream, _get_device, _forward_ad
     if _torch_mod is None:
         import torch
         _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
         _get_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+        _forward_ad = torch.autograd.forward_ad
         _torch_mod = torch
     return _torch_mod
 
@@ -526,18 +528,20 @@ def _code(t, name):
     raise CmsdError(f"{name} must be float32 or bfloat16, got {t.dtype}")
 
 
-def _not_recorded(what):
-    raise CmsdError(f"{what} records nothing for autograd: call it under torch.no_grad() (or from an "
-                    f"autograd.Function) and take the gradients from {what}_backward")
-
-
-def _once(what, *tensors):
-    """Refuses a gradient's call where autograd would follow one of the tensors to a second derivative."""
+def _unfollowed(what, *tensors):
+    """Refuses a call where autograd would follow one of the tensors: nothing is recorded, and no tangent goes on."""
     if _torch_mod.is_grad_enabled():
         for t in tensors:
             if t is not None and t.requires_grad:
+                how = (" that is differentiated once)" if what.endswith("_backward")
+                       else f") and take the gradients from {what}_backward")
                 raise CmsdError(f"{what} records nothing for autograd: call it under torch.no_grad() (or from an "
-                                f"autograd.Function that is differentiated once)")
+                                f"autograd.Function{how}")
+    if _forward_ad._current_level >= 0 and _torch_mod._C._is_fwd_grad_enabled():
+        for t in tensors:
+            if t is not None and _forward_ad.unpack_dual(t).tangent is not None:
+                raise CmsdError(f"{what} passes no tangent on to autograd: call it on tensors without one (or from an "
+                                f"autograd.Function with a jvp of its own)")
 
 
 def _rows(t, name):
@@ -576,10 +580,9 @@ def embedding(tokens, table, scale=1.0, ignore_index=-100, out=None):
     rows whose token is ignore_index).
 
     tokens: int32 [R].  Nothing is recorded for autograd: a table that requires gradients is refused while it
-    records.  Another token outside the vocabulary gives a row of zeros; embedding_errors tells."""
+    records, and one with a tangent.  Another token outside the vocabulary gives a row of zeros; embedding_errors tells."""
     torch = _torch()
-    if table.requires_grad and torch.is_grad_enabled():
-        _not_recorded("embedding")
+    _unfollowed("embedding", table)
     V, d = _rows(table, "table")
     code, dtype = _code(table, "table"), table.dtype
     R = tokens.numel()
@@ -609,9 +612,9 @@ def embedding_backward(tokens, d_x, V, scale=1.0, ignore_index=-100, add=False, 
 
     With add, out["d_table"] is given and the sums are added to it: a head that shares the table passes the d_weight
     of lmhead_loss_backward.  There are no second derivatives, here and in the gradients below: tensors that require
-    them are refused while autograd records."""
+    them are refused while autograd records, and ones with a tangent."""
     torch = _torch()
-    _once("embedding_backward", d_x, out.get("d_table") if add and out is not None else None)
+    _unfollowed("embedding_backward", d_x, out.get("d_table") if add and out is not None else None)
     R, d = _rows(d_x, "d_x")
     V = int(V)
     if not 0 < V <= _INT_MAX:
@@ -648,11 +651,10 @@ def layernorm(x, weight=None, bias=None, eps=1e-5, stats=True, out=None):
     one dtype, or None (ones, zeros).
 
     Returns dict y ([R, d], x's dtype) and, with stats, mean and rstd (float32 [R]) for layernorm_backward.  Nothing
-    is recorded for autograd: tensors that require gradients are refused while it records."""
+    is recorded for autograd: tensors that require gradients are refused while it records, and ones with
+    a tangent."""
     torch = _torch()
-    if torch.is_grad_enabled() and (x.requires_grad or weight is not None and weight.requires_grad
-                                    or bias is not None and bias.requires_grad):
-        _not_recorded("layernorm")
+    _unfollowed("layernorm", x, weight, bias)
     R, d = _rows(x, "x")
     code, dtype = _code(x, "x"), x.dtype
     wcode, wtype = code, dtype
@@ -695,7 +697,7 @@ def layernorm_backward(x, weight, mean, rstd, d_y, x_grad=True, weight_grad=True
     Returns dict d_x ([R, d], x's dtype, with x_grad), d_weight (with weight_grad) and d_bias (with bias_grad), both
     [d] of weight's dtype (x's without weight), written whole."""
     torch = _torch()
-    _once("layernorm_backward", x, weight, mean, rstd, d_y)
+    _unfollowed("layernorm_backward", x, weight, mean, rstd, d_y)
     R, d = _rows(x, "x")
     code, dtype = _code(x, "x"), x.dtype
     wcode, wtype = (code, dtype) if weight is None else (_code(weight, "weight"), weight.dtype)
@@ -741,10 +743,9 @@ def dropout(x, p, seed, iteration=0, site=0, residual=None, step=None, out=None)
     The mask is a function of seed, iteration (a training step), site (a layer) and an entry's place in x, and is not
     stored.  step: None, or an int32 [1] tensor that is added to iteration when the call runs (a captured call then
     draws another mask at each replay).  Nothing is recorded for autograd: tensors that require gradients are refused
-    while it records."""
-    torch = _torch()
-    if torch.is_grad_enabled() and (x.requires_grad or residual is not None and residual.requires_grad):
-        _not_recorded("dropout")
+    while it records, and ones with a tangent."""
+    _torch()
+    _unfollowed("dropout", x, residual)
     code, cur, iteration, site, y = _dropout_args(x, "x", "y", iteration, site, step, out)
     if residual is not None and not _fits(residual, x.shape, x.dtype, cur):
         _need(cur, ((residual, x.shape, x.dtype, "residual"),))
@@ -759,7 +760,7 @@ def dropout_backward(d_y, p, seed, iteration=0, site=0, step=None, out=None):
     """The gradient of dropout by x, given the same p, seed, iteration, site and step: returns dict d_x.  (The
     residual's gradient is d_y itself.)"""
     _torch()
-    _once("dropout_backward", d_y)
+    _unfollowed("dropout_backward", d_y)
     code, cur, iteration, site, d_x = _dropout_args(d_y, "d_y", "d_x", iteration, site, step, out)
     rc = lib().cmsd_dropout_backward(d_y.data_ptr(), code, d_y.numel(), float(p), int(seed), iteration, site, _ptr(step),
                                      d_x.data_ptr(), _stream_of(cur))

@@ -78,3 +78,47 @@ def test_from_a_function(cmsd):
     assert torch.equal(x.grad, want["d_x"]) and torch.equal(w.grad, want["d_weight"])
     with pytest.raises(cmsd.CmsdError, match="autograd"):
         torch.autograd.grad((Norm.apply(x, w) * c).sum(), x, create_graph=True)
+
+
+# the tensors that a forward derivative may come with
+FORWARD = {
+    "embedding(table)": (TABLE, lambda c, t: c.embedding(TOKENS, t)),
+    "layernorm(x)": (X, lambda c, t: c.layernorm(t, P, P)),
+    "layernorm(weight)": (P, lambda c, t: c.layernorm(X, t, P)),
+    "layernorm(bias)": (P, lambda c, t: c.layernorm(X, P, t)),
+    "dropout(x)": (X, lambda c, t: c.dropout(t, 0.1, 1)),
+    "dropout(residual)": (X, lambda c, t: c.dropout(X, 0.1, 1, residual=t)),
+}
+
+
+@pytest.mark.parametrize("name", [*FORWARD, *BACKWARD])
+def test_tangents(cmsd, name):
+    t, call = {**FORWARD, **BACKWARD}[name]
+    with fwAD.dual_level():
+        dual = fwAD.make_dual(t, torch.ones_like(t))
+        with pytest.raises(cmsd.CmsdError, match="autograd"):
+            call(cmsd, dual)
+        with torch.no_grad(), pytest.raises(cmsd.CmsdError, match="autograd"):      # (stops no tangent)
+            call(cmsd, dual)
+        with pytest.raises(cmsd.CmsdError, match="CUDA"):
+            call(cmsd, t)
+        with pytest.raises(cmsd.CmsdError, match="CUDA"):
+            call(cmsd, fwAD.unpack_dual(dual).primal)
+
+
+def test_tangents_of_a_function_are_its_own(cmsd):
+    """In an autograd.Function's forward nothing follows the tangents: its jvp makes them."""
+    class Norm(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, x):
+            with pytest.raises(cmsd.CmsdError, match="CUDA"):
+                cmsd.layernorm(x, P, P)
+            return x * 2
+
+        @staticmethod
+        def jvp(ctx, t):
+            return t * 2
+
+    with fwAD.dual_level():
+        y = Norm.apply(fwAD.make_dual(X.clone(), torch.ones_like(X)))
+        assert (fwAD.unpack_dual(y).tangent == 2).all()
