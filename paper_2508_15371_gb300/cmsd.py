@@ -690,26 +690,32 @@ def layernorm_backward_workspace(R, d):
     return torch.empty(n, dtype=torch.uint8, device="cuda")
 
 
-def layernorm_backward(x, weight, mean, rstd, d_y, x_grad=True, weight_grad=True, bias_grad=True, out=None, ws=None):
+def layernorm_backward(x, weight, mean, rstd, d_y, x_grad=True, weight_grad=True, bias_grad=True, out=None, ws=None,
+                       dtype=None):
     """The gradients of layernorm: mean and rstd are its outputs, d_y ([R, d], x's dtype) is dL/dy, weight as there
     (None: ones).
 
     Returns dict d_x ([R, d], x's dtype, with x_grad), d_weight (with weight_grad) and d_bias (with bias_grad), both
-    [d] of weight's dtype (x's without weight), written whole."""
+    [d] of weight's dtype, written whole.  Without weight dtype says theirs (float32 or bfloat16, a bias's of its own;
+    None: x's)."""
     torch = _torch()
     _unfollowed("layernorm_backward", x, weight, mean, rstd, d_y)
     R, d = _rows(x, "x")
-    code, dtype = _code(x, "x"), x.dtype
-    wcode, wtype = (code, dtype) if weight is None else (_code(weight, "weight"), weight.dtype)
+    code, xtype = _code(x, "x"), x.dtype
+    wcode, wtype = (code, xtype) if weight is None else (_code(weight, "weight"), weight.dtype)
     f32 = torch.float32
+    if dtype is not None and dtype is not wtype:
+        if weight is not None or dtype not in (f32, torch.bfloat16):
+            raise CmsdError(f"dtype must be weight's, or float32 or bfloat16 without one, got {dtype}")
+        wcode, wtype = F32 if dtype is f32 else BF16, dtype
     cur = _current(x)
     if not (_here(x, cur) and _fits(mean, (R,), f32, cur) and _fits(rstd, (R,), f32, cur)
-            and _fits(d_y, (R, d), dtype, cur) and (weight is None or _fits(weight, (d,), wtype, cur))):
-        _need(cur, ((x, (R, d), dtype, "x"), (mean, (R,), f32, "mean"), (rstd, (R,), f32, "rstd"),
-                    (d_y, (R, d), dtype, "d_y")) + (((weight, (d,), wtype, "weight"),) if weight is not None else ()))
+            and _fits(d_y, (R, d), xtype, cur) and (weight is None or _fits(weight, (d,), wtype, cur))):
+        _need(cur, ((x, (R, d), xtype, "x"), (mean, (R,), f32, "mean"), (rstd, (R,), f32, "rstd"),
+                    (d_y, (R, d), xtype, "d_y")) + (((weight, (d,), wtype, "weight"),) if weight is not None else ()))
     o = {}
     if x_grad:
-        o["d_x"] = _result(out, "d_x", (R, d), dtype, x, cur)
+        o["d_x"] = _result(out, "d_x", (R, d), xtype, x, cur)
     if weight_grad:
         o["d_weight"] = _result(out, "d_weight", (d,), wtype, x, cur)
     if bias_grad:
