@@ -78,7 +78,6 @@ struct Num {
   static __device__ __forceinline__ N mul(N a, N b) { return mul2(a, b); }
   static __device__ __forceinline__ N fma(N a, N b, N c) { return fma2(a, b, c); }
   static __device__ __forceinline__ float sum(N a) { return lo32f(a) + hi32f(a); }
-  static __device__ __forceinline__ float first(N a) { return lo32f(a); }
   static __device__ __forceinline__ N of(const float (&f)[VE], int j) { return pack2(f[2 * j], f[2 * j + 1]); }
   static __device__ __forceinline__ void to(N a, float* f) { f[0] = lo32f(a); f[1] = hi32f(a); }
   template <typename T>
@@ -95,7 +94,6 @@ struct Num<1> {
   static __device__ __forceinline__ N mul(N a, N b) { return a * b; }
   static __device__ __forceinline__ N fma(N a, N b, N c) { return __fmaf_rn(a, b, c); }
   static __device__ __forceinline__ float sum(N a) { return a; }
-  static __device__ __forceinline__ float first(N a) { return a; }
   static __device__ __forceinline__ N of(const float (&f)[1], int) { return f[0]; }
   static __device__ __forceinline__ void to(N a, float* f) { f[0] = a; }
   template <typename T>
@@ -273,7 +271,7 @@ __global__ void __launch_bounds__(kWide) norm_wide_kernel(const NormArgs a) {
 // ---- many rows -----------------------------------------------------------------------------
 // A grid that stays: a thread has the same columns in all of its rows, with their
 // parameters (forward) or their sums over rows (gradients) in registers; W warps a
-// row, kGroups * kRows rows of a CTA at a time.  Rows come through a ring in shared
+// row, kGroups rows of a CTA at a time.  Rows come through a ring in shared
 // memory.  Bound by memory forward (R = 16384 d = 2048 bf16 22.8 us, 5.9 TB/s), by
 // memory and a barrier a row backward (36.6 us with the join, 5.5 TB/s).  Sixteen
 // columns a thread: of eight, exchanging a row's sums is most of the work (46 us
@@ -368,7 +366,7 @@ __global__ void __launch_bounds__(cta_threads(W), norm_ctas(kCols)) norm_many_ke
   using Raw = typename RowVec<T, VE>::Raw;
   using M = Num<VE>;
   using N = typename M::N;
-  constexpr int kN = M::kN, NV = kCols / VE, kGroups = cta_groups(W), kRows = 1;
+  constexpr int kN = M::kN, NV = kCols / VE, kGroups = cta_groups(W);
   constexpr int kRowBytes = staged_bytes(W, kCols, sizeof(T)), kTurns = kCols * sizeof(T) / 16;
   // vectors of a thread that every row fills (W = 1: rows of over 256) and that c is made from, or 0: from all
   constexpr int kHalf = sizeof(T) == 2 && kCols > 8 ? NV / 2 : 0;
@@ -376,16 +374,12 @@ __global__ void __launch_bounds__(cta_threads(W), norm_ctas(kCols)) norm_many_ke
   __shared__ __align__(16) float s_sum[W > 1 ? 3 * kGroups * W : 1];
   wait_for_previous();
   const int nvec = a.d / VE, t = threadIdx.x % (32 * W), group = threadIdx.x / (32 * W);
-  const int64_t first = (int64_t)blockIdx.x * kGroups * kRows + group, step = (int64_t)gridDim.x * kGroups * kRows;
-  char* ring = reinterpret_cast<char*>(s_ring4) + group * kNormStages * kRows * kRowBytes;       // [kNormStages][kRows]
+  const int64_t first = (int64_t)blockIdx.x * kGroups + group, step = (int64_t)gridDim.x * kGroups;
+  char* ring = reinterpret_cast<char*>(s_ring4) + group * kNormStages * kRowBytes;       // [kNormStages]
   const uint32_t ring_at = (uint32_t)__cvta_generic_to_shared(ring);
   float* sums = s_sum + (W > 1 ? 3 * group * W : 0);
-  const auto request = [&](int64_t r0, int stage) {
-#pragma unroll
-    for (int u = 0; u < kRows; ++u) {
-      const int64_t row = r0 + u * kGroups;
-      request_row<T, VE, kTurns>(ring_at + (stage * kRows + u) * kRowBytes, a.x, row, a, t, 32 * W);
-    }
+  const auto request = [&](int64_t row, int stage) {
+    request_row<T, VE, kTurns>(ring_at + stage * kRowBytes, a.x, row, a, t, 32 * W);
     close_copies();
   };
 #pragma unroll
@@ -411,12 +405,12 @@ __global__ void __launch_bounds__(cta_threads(W), norm_ctas(kCols)) norm_many_ke
   }
   const float over_d = 1.f / a.d;
   int stage = 0;
-  for (int64_t r0 = first; r0 < a.R; r0 += step) {
+  for (int64_t row = first; row < a.R; row += step) {
     copies_but<kNormStages - 2>();
     group_sync<W>(group);                             // (the first entry is another thread's copy, if no more is)
-    request(r0 + (kNormStages - 1) * step, stage == 0 ? kNormStages - 1 : stage - 1);
-    const char* from = ring + stage * kRows * kRowBytes;
-    const int lead = lead_of<T, VE>(r0, a.d);
+    request(row + (kNormStages - 1) * step, stage == 0 ? kNormStages - 1 : stage - 1);
+    const char* from = ring + stage * kRowBytes;
+    const int lead = lead_of<T, VE>(row, a.d);
     N h[NV][kN];
     float s[1], c;
     if constexpr (kHalf > 0) {
@@ -464,11 +458,11 @@ __global__ void __launch_bounds__(cta_threads(W), norm_ctas(kCols)) norm_many_ke
     else group_two_sums<W>(q, sums + W, group);
     const float e = q[0] * over_d, rstd = inverse_root(__fmaf_rn(-e, e, __fmaf_rn(q[1], over_d, a.eps)));
     if (t == 0) {
-      if (a.mean) a.mean[r0] = c + e;
-      if (a.rstd) a.rstd[r0] = rstd;
+      if (a.mean) a.mean[row] = c + e;
+      if (a.rstd) a.rstd[row] = rstd;
     }
     const N scale = M::all(rstd), shift = M::all(-e * rstd);
-    Raw* y = static_cast<Raw*>(a.y) + (size_t)r0 * nvec;
+    Raw* y = static_cast<Raw*>(a.y) + (size_t)row * nvec;
 #pragma unroll
     for (int k = 0; k < NV; ++k)
       if (in_row<W, NV>(t, k, nvec)) {
