@@ -283,7 +283,8 @@ constexpr int kFillThreads = 256;
 constexpr int kFillVecs = 2;                         // 16-byte vectors of a thread
 constexpr size_t kFillChunk = (size_t)kFillThreads * kFillVecs * 16;
 constexpr size_t kFillCtas = 1 << 24;                // at most
-constexpr size_t kManyZeros = (size_t)64 << 20;
+constexpr size_t kManyZeros = (size_t)64 << 20;      // beside which rows are ordered by an early launch, and so many a row
+constexpr size_t kManyZerosRow = (size_t)16 << 10;
 // bytes [first, last) of the table, by this and `ctas` - 1 other CTAs
 __device__ __forceinline__ void fill(const EmbedArgs& a, size_t first, size_t last, int cta, int ctas) {
   char* table = static_cast<char*>(a.d_table);
@@ -852,9 +853,11 @@ cudaError_t launch_embed_backward(const EmbedArgs& args, cudaStream_t s) {
     const size_t smem = (size_t)(a.R + 127) / 128 * 512;
     const int per = a.R <= 1216 ? 8 : 32, ctas = ceil_div(a.R, per);
     // (of many rows it is bound by the SMs' instructions, and CTAs that come early crowd on a few of them: R = 4096 d = 512
-    // added to 18.3 us a call in a row of them instead of 10.2, written whole, 33 MB, 16.4 and 13.6; behind 262 MB of zeros
-    // nobody waits for them, and R = 4096 d = 1024 of 128256 takes 45.7 instead of 48.3)
-    const bool early = per == 8 || all >= kManyZeros;
+    // added to 18.3 us a call in a row of them instead of 10.2, written whole, 33 MB, 16.4 and 13.6; behind zeros that take
+    // longer nobody waits for them.  Early and not, d = 1024, MB of zeros: R = 2500 48 15.8 and 14.9, 64 16.8 and 17.1; R =
+    // 4096 64 19.8 and 19.3, 96 23.6 and 24.0, 256 45.0 and 45.6; R = 7168 64 29.8 and 22.7, 96 30.3 and 27.7, 128 31.5
+    // and 32.3)
+    const bool early = per == 8 || all >= std::max(kManyZeros, a.R * kManyZerosRow);
     e = launch(early, per == 8 ? embed_rank_kernel<1> : embed_rank_kernel<4>, ctas + fill_ctas(0), kRankThreads, smem, s, a, ctas);
   } else {
     const int digits = 1 << a.bits, tiles = ceil_div(a.R, a.tile);

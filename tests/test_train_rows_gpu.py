@@ -34,9 +34,10 @@ def test_rings_of_rows_off_16_bytes(cmsd, R, d, dtype):
     N._check_grads(cmsd.layernorm_backward(x, w, o["mean"], o["rstd"], d_y), x, w, o["mean"], o["rstd"], d_y)
 
 
-# tables of 64 MB, one row less, and more; rows about those that are ordered by comparing them
+# tables of 64 MB, one row less, and more; of 16 KB a row and less; rows about those that are ordered by comparing them
 @pytest.mark.parametrize("R,d,V,dtype", [(1217, 1024, 32768, BF16), (1217, 1024, 32767, BF16), (4096, 2048, 40001, BF16),
-                                         (7168, 513, 70001, BF16), (5000, 260, 70001, F32), (1216, 512, 70000, BF16)])
+                                         (7168, 1024, 57344, BF16),
+                                         (7168, 1024, 57343, BF16), (7168, 513, 70001, BF16), (5000, 260, 80001, F32), (1216, 512, 70000, BF16)])
 def test_rows_ordered_beside_many_zeros(cmsd, R, d, V, dtype):
     """Calls one behind the other, whose tokens and rows the launch before them writes and whose workspace is the same."""
     g = E._gen(R, d, V, 5)
