@@ -303,8 +303,9 @@ int cmsd_lmhead_errors(void* stream, uint32_t* flags_out);
  * dtype is that of the tensors of entries (CMSD_F32 or CMSD_BF16); sums are
  * held in fp32, results rounded to their dtype once.  Widths d are any number
  * from 1 to 65536 (rows of a multiple of 16 bytes are the fast ones), rows
- * R <= 2^28; tensors of entries and workspaces are 16-byte aligned.  Outputs and workspaces share no bytes with each other or with an
- * input (CMSD_EINVAL).  Equal calls give equal results.
+ * R <= 2^28; tensors of entries and workspaces are 16-byte aligned.  Outputs and
+ * workspaces share no bytes with each other or with an input (CMSD_EINVAL).  Equal
+ * calls give equal results.
  *
  * cmsd_embedding: x_r = scale table_token(r)
  *   tokens: int32 [R] device.  A row whose token is ignore_index is padding: its
@@ -321,7 +322,8 @@ int cmsd_lmhead_errors(void* stream, uint32_t* flags_out);
  *     is added to what d_table holds (the weight's gradient of a head that shares
  *     the table, cmsd_lmhead_loss_backward's d_weight), and entries without rows
  *     are not touched.
- *   A token's rows are summed in an order that depends on tokens alone.
+ *   A token's rows are summed in an order that depends on tokens (R among them) and
+ *     d alone.
  *   ws: cmsd_embedding_backward_workspace_bytes(R, d, V) bytes on the current
  *     device; enough for any fewer rows of that d and V, too.  It needs no
  *     initialisation but for the error word, which
@@ -345,6 +347,9 @@ int cmsd_embedding_errors(void* stream, uint32_t* flags_out);
  * Layer norm of R rows of d entries:
  *   mean_r = sum_j x_rj / d,  rstd_r = (sum_j (x_rj - mean_r)^2 / d + eps)^(-1/2)
  *   y_rj = (x_rj - mean_r) rstd_r weight_j + bias_j
+ *   A row's sums are formed in an order that depends on R, d and dtype: the same row
+ *     among another number of rows may differ in its last bits.  Large entries cost the
+ *     others of their row no bits, in whatever columns they stand.
  *   x, y: dtype [R][d]; weight, bias: wdtype (CMSD_F32 or CMSD_BF16) [d], 16-byte
  *     aligned, or NULL (ones, zeros); 0 < eps, finite; mean, rstd: float [R], or
  *     NULL where no gradients follow.  |x| < 2^54; a row with an infinity or a NaN
@@ -356,7 +361,8 @@ int cmsd_embedding_errors(void* stream, uint32_t* flags_out);
  *   d_weight_j = sum_r d_y_rj h_rj,  d_bias_j = sum_r d_y_rj
  *   d_x: dtype [R][d]; d_weight, d_bias: wdtype [d].  Each may be NULL and is then
  *     left out (all NULL is CMSD_EINVAL).  All are written whole.
- *   The sums over rows are formed in an order that depends on R and d alone.
+ *   The sums over rows are formed in an order that depends on R and d alone, those
+ *     along a row as above.
  *   ws: cmsd_layernorm_backward_workspace_bytes(R, d) bytes on the current device,
  *     enough for any fewer rows of that d, too; no initialisation needed.
  *   R == 0: the parameters' gradients are zero.

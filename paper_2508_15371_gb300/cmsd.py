@@ -746,8 +746,8 @@ def dropout(x, p, seed, iteration=0, site=0, residual=None, step=None, out=None)
     """Dropout with rate p (a multiple of 2^-16, the nearest one) and kept entries scaled up, residual added:
     returns dict y (x's shape and dtype, float32 or bfloat16).
 
-    The mask is a function of seed, iteration (a training step), site (a layer) and an entry's place in x, and is not
-    stored.  step: None, or an int32 [1] tensor that is added to iteration when the call runs (a captured call then
+    The mask is a function of seed (any integer, modulo 2^64), iteration (a training step), site (a layer) and an
+    entry's place in x, and is not stored.  step: None, or an int32 [1] tensor that is added to iteration when the call runs (a captured call then
     draws another mask at each replay).  Nothing is recorded for autograd: tensors that require gradients are refused
     while it records, and ones with a tangent."""
     _torch()

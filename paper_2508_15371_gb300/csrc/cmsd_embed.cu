@@ -1,9 +1,11 @@
 // Scaled rows of the token table (include/cmsd.h, cmsd_embedding) and the
 // table's gradient (cmsd_embedding_backward).
 //
-// The gradient's rows are put into the order of their tokens first (stable: rows
-// of one token keep theirs), by tokens alone; then every row of d_x is read and
-// every row of d_table written once.
+// Of more than 512 rows the gradient's are put into the order of their tokens first
+// (stable: rows of one token keep theirs), by tokens alone, while a table that is not
+// added to gets its zeros; then the rows of d_x with a token are read once each, and
+// the sums written, over zeros where there are some.  Fewer rows are not put in order:
+// one launch reads them, writes the sums, and zeros elsewhere.
 #include <cuda_bf16.h>
 
 #include <algorithm>
@@ -103,7 +105,10 @@ __global__ void __launch_bounds__(256) embed_narrow_kernel(const EmbedArgs a) {
 // or by the row of loads: tokens, rows, and a batch of them after another where a
 // token has many.  Against the three launches below, d = 2048 of 128256 bf16: R = 1
 // 69.1 against 71.5 us, 512 70.5 and 75.5; added to a table, d = 1024, R = 256 4.7
-// and 6.3, 512 7.2 and 7.7, 1024 11.9 and 8.7.
+// and 6.3, 512 7.2 and 7.7, 1024 11.9 and 8.7: all with frequencies that fall as one
+// over the rank.  The rule does not look at the tokens, and one CTA has all rows of
+// its tokens: at R = 512 d = 1024 of 32000 with a tenth, half, all rows of one token
+// 14.4, 35, 60 us (added 8.7, 23, 41), where 513 rows take 14.6, 15.2, 15.7 (6.5, 6.9, 7.4).
 constexpr int kFewRows = 512, kFewTile = 4, kFewThreads = 128, kFewTokens = 1024;
 constexpr size_t kFewFill = (size_t)48 << 10;
 template <typename T, int VE, bool ADD>
@@ -657,7 +662,9 @@ __global__ void __launch_bounds__(kSumThreads) embed_sum_kernel(const EmbedArgs 
 // tiles that it fills, and that of the tile where it ends, in this order.  A CTA
 // kJoinTiles tiles and, with others, their columns; a warp a token and 32 JV of its
 // columns, or, for a token of more than kLong tiles, the CTA's warps an eighth of the
-// tiles each.  A few loads in a row: 5 us of a call.
+// tiles each.  A few loads in a row: 5 us of a call; of a token that fills thousands of
+// tiles many: R = 600000 d = 256 of 32000, a tenth, half, all rows of one token 146, 232,
+// 342 us, with none above the others 128.
 constexpr int kJoinThreads = 256, kJoinWarps = kJoinThreads / 32;
 constexpr int kJoinTiles = 8;
 constexpr int kLong = 16;

@@ -1,8 +1,10 @@
 // Layer norm (include/cmsd.h, cmsd_layernorm) and its gradients
 // (cmsd_layernorm_backward).
 //
-// Both read each row once: it stays in the registers of its threads between the
-// row's sums and what they give.  Bound by memory.
+// A row stays in the registers of its threads between its sums and what they give,
+// and is read once, but for rows over 32768 columns forward (three times), gradients
+// of few rows (twice) and of over 8192 columns (d_x and the sums over rows each by
+// itself).  Bound by memory.
 #include <cuda_bf16.h>
 
 #include <algorithm>
@@ -272,7 +274,7 @@ __global__ void __launch_bounds__(kWide) norm_wide_kernel(const NormArgs a) {
 // A grid that stays: a thread has the same columns in all of its rows, with their
 // parameters (forward) or their sums over rows (gradients) in registers; W warps a
 // row, kGroups rows of a CTA at a time.  Rows come through a ring in shared
-// memory.  Bound by memory forward (R = 16384 d = 2048 bf16 22.8 us, 5.9 TB/s), by
+// memory.  Bound by memory forward (R = 16384 d = 2048 bf16 22.7 us, 5.9 TB/s), by
 // memory and a barrier a row backward (36.6 us with the join, 5.5 TB/s).  Sixteen
 // columns a thread: of eight, exchanging a row's sums is most of the work (46 us
 // forward); with a warp a row the parameters are read again for every row (34 us).
@@ -890,14 +892,18 @@ int part_count(int R, int d) {
   return std::min(n, kSms * grad_ctas(w, row_cols(d)));
 }
 
-// Up to this many rows of 257 to 2048 entries a CTA a row, else the grid that stays: R = 304 d = 2048 2.48 against 2.59
-// us, 608 3.01 and 3.03, 1216 4.52 and 4.12; d = 1001 608 3.98 and 6.23, 1216 6.18 and 6.64.  Narrower and wider rows go
-// to the latter always (R = 16 d = 256 1.93 against 2.01, d = 4096 2.48 against 2.69).
+// Up to this many rows of 257 to 2048 entries a CTA a row, else the grid that stays: bf16 R = 16 d = 1024 1.8 against 2.0
+// us, d = 2048 R = 304 2.2 and 2.1, 608 3.1 and 3.2, 1216 4.8 and 4.1; f32 d = 2048 R = 608 3.0 and 3.3, 1216 4.6 and
+// 4.6.  Up to 1024 entries the grid is ahead from some 305 rows on (d = 1001 R = 304 2.05 and 2.05, 608 2.7 and 2.1).
+// Narrower and wider rows go to the grid always (R = 16 d = 256 1.8 against 1.5, d = 4096 2.3 against 2.0, R = 608 3.7 and 4.1).
 constexpr int kFewRows = 608;
 // Whether the gradients are norm_backward_few_kernel's, else the grid's that stays and its join.  bf16: R = 16 d = 1024 1.5
 // against 3.8 us, R = 333 d = 1001 3.8 and 4.8, R = 608 d = 64 3.7 and 3.7, d = 2048 4.4 and 6.0, d = 8192 8.6 and 14.9,
-// R = 900 d = 64 4.7 and 3.9, R = 1216 d = 1001 7.6 and 6.0.  Wide rows that begin anywhere: d = 4097 R = 200 7.3 and
-// 7.9, R = 400 10.2 and 9.2.
+// R = 900 d = 64 4.7 and 3.9, R = 1216 d = 1001 7.6 and 6.0.  Over 2048 columns, rows of multiples of four, in pairs for
+// bf16: d = 2052 R = 608 5.7 and 6.0, d = 8188 13.7 and 14.8 (R = 760 6.9 and 7.8, 16.2 and 16.4); d = 4096 f32 8.1 and
+// 10.5.  Others are one entry at a time for f32, for bf16 where odd: d = 2049 R = 304 6.3 and 5.7, R = 608 10.1 and 6.6;
+// d = 4097 R = 152 6.9 and 6.5; f32 d = 4097 R = 304 8.1 and 8.5, R = 608 15.2 and 12.3.  Even ones of bf16 stay with
+// them, since the order of the sums is the same for both types: d = 4098 R = 608 7.6 and 9.2.
 bool few_gradients(int R, int d) { return d <= kWideCols && R <= (d <= 2048 || d % 4 == 0 ? 608 : 304); }
 template <typename T, int VE, int kCols, int W>
 cudaError_t launch_many(const NormArgs& a, cudaStream_t s) {
