@@ -82,16 +82,17 @@ def test_an_outlier_costs_the_others_nothing(cmsd, R, d, columns, size, dtype):
     _check(cmsd.layernorm(x, w, b, eps=EPS), x, w, b)
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("mean", [1e3, 1e6])
 @pytest.mark.parametrize("R,d", SIZES)
-def test_outliers_of_rows_far_from_zero(cmsd, R, d, mean):
+def test_outliers_of_rows_far_from_zero(cmsd, R, d, mean, dtype):
     g = torch.Generator(device="cuda")
     g.manual_seed(R + 7 * d + 1)
     n = lambda *s: torch.randn(*s, generator=g, device="cuda")  # noqa: E731
     x = mean * (1 + torch.rand(R, 1, generator=g, device="cuda")) + n(R, d)
     x[::2, 0] = -3e4
     x[1::3, 0] = 0.0
-    w, b = 1 + 0.2 * n(d), 0.3 * n(d)
+    x, w, b = x.to(dtype), 1 + 0.2 * n(d), 0.3 * n(d)
     _check(cmsd.layernorm(x, w, b, eps=EPS), x, w, b)
 
 
@@ -104,3 +105,21 @@ def test_rows_of_one_number_give_the_bias(cmsd, R, d, dtype):
     b = torch.randn(d, generator=g, device="cuda")
     o = cmsd.layernorm(v.expand(R, d).contiguous(), torch.full_like(b, 3.0), b, eps=EPS)
     assert torch.equal(o["y"], b.to(dtype).expand(R, d)) and torch.equal(o["mean"], v[:, 0].float())
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("R,d", [(12, 1000), (700, 300), (700, 1000), (700, 1001), (12, 4096), (12, 9000)])
+def test_not_finite_stays_in_its_row(cmsd, R, d, dtype):
+    """Infinities and NaN among the entries that a first mean is made from, and among the others."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(R + 7 * d + 3)
+    n = lambda *s: torch.randn(*s, generator=g, device="cuda")  # noqa: E731
+    x, w, b = n(R, d).to(dtype), n(d), n(d)
+    good, bad, inf = cmsd.layernorm(x, w, b), x.clone(), float("inf")
+    bad[1, 0], bad[2, -1], bad[4, d // 2], bad[5, 3], bad[7, -1] = inf, inf, -inf, float("nan"), float("nan")
+    bad[8, 0], bad[8, -1] = inf, -inf
+    o = cmsd.layernorm(bad, w, b)
+    rows = [1, 2, 4, 5, 7, 8]
+    assert o["y"][rows].isnan().all() and o["rstd"][rows].isnan().all() and not o["mean"][rows].isfinite().any()
+    rest = [r for r in range(R) if r not in rows]
+    assert all(torch.equal(o[k][rest], good[k][rest]) for k in o)
